@@ -466,6 +466,216 @@ int sc_layer_norm_forward(int B, int L, int D, const int32_t* rows, const float*
                           const float* gamma, const float* beta, float eps, uint16_t* out,
                           void* stream);
 
+/*
+ * Expert feed-forward block: the operators of a mixture-of-experts block in
+ * place of the encoder layer's dense one, forward and backward.  A token is a
+ * row (b, r) of a [B][L] batch, number t = b L + r, in use when r < rows[b]
+ * (rows == NULL: all; the encoder layer's len_out).  A slot is one (token,
+ * choice) pair in expert order: expert e has the slots offsets[e] ..
+ * offsets[e + 1].  No size below depends on a value the host would have to
+ * read back: the sizes M, T = B L are capacities, offsets and rows live on the
+ * device.  Rows and slots that are not in use are neither read nor written
+ * unless a field says so.
+ */
+#define SC_MAX_EXPERTS 256
+#define SC_MAX_CHOICES 8
+#define SC_MAX_EXPERT_DIM 8192 /* widest row (D, N, K) */
+
+/* Bytes of workspace the calls below need (256-byte aligned device memory that
+ * was zeroed once; it starts with the status word that sc_workspace_status
+ * reads; 0 on invalid sizes).  D: the widest row.  One workspace serves all
+ * calls of one stream; calls that overlap need one each. */
+size_t sc_expert_workspace_size(int B, int L, int E, int k, int D);
+
+/*
+ * Routing: k of E experts for each token.
+ *
+ * logits   fp32 [B L][E], rows `ld` >= E floats apart.  -inf and NaN: the expert
+ *          is masked for this token; every other value may be chosen (+inf and
+ *          the type's lowest value too).
+ * Chosen are the k largest logits in descending order, ties to the lowest
+ * expert; fewer where fewer are unmasked.  The gate of choice j is
+ * exp(l_j - m) / sum_i exp(l_i - m), m the row's largest logit, the sum over
+ * the chosen experts (renormalize != 0) or over all E.
+ * expert   int32 [B L][k] out, gate fp32 [B L][k] out: the choices; -1 and 0
+ *          where there is none (masked, or a token not in use).
+ * offsets  int32 [E + 1] out: first slot of each expert; offsets[E] = slots in use.
+ * slot     int32 [B L][k] out: the slot of each choice, or -1.  An expert's
+ *          slots are in token order.
+ * token    int32 [B L k] out: the token of each slot; -1 from offsets[E] on.
+ * 1 <= k <= min(E, SC_MAX_CHOICES), E <= SC_MAX_EXPERTS, B L k < 2^31.
+ */
+typedef struct {
+  int B, L, E, k;
+  const float* logits;
+  long long ld;
+  const int32_t* rows;
+  int renormalize;
+  int32_t* expert;
+  float* gate;
+  int32_t* offsets;
+  int32_t* slot;
+  int32_t* token;
+} sc_expert_route_args;
+
+int sc_expert_route_forward(const sc_expert_route_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Gradient of the gates with respect to the logits.  expert, gate: as the
+ * forward call wrote them; dgate fp32 [B L][k]; dlogits fp32 [B L][E] out,
+ * written for every token (0 for one without a choice or not in use). */
+typedef struct {
+  int B, L, E, k;
+  const float* logits;
+  long long ld;
+  const int32_t* rows;
+  int renormalize;
+  const int32_t* expert;
+  const float* gate;
+  const float* dgate;
+  float* dlogits;
+} sc_expert_route_backward_args;
+
+int sc_expert_route_backward(const sc_expert_route_backward_args* args, void* stream);
+
+/*
+ * Products grouped by expert, for the slots s of each expert e:
+ *   forward   y[s][n] = sum_k X[row(s)][k] W[e][n][k] + bias[e][n];
+ *             out = GELU(y) when gelu != 0, else y; pre = y
+ *   backward  dX[s][k] = (sum_n dY[s][n] W[e][n][k]) (GELU'(pre[s][k]) if pre)
+ *   backward  dW[e][n][k] = sum_s dY[s][n] X[row(s)][k]; dbias[e][n] = sum_s dY[s][n]
+ * row(s) = token[s] (token == NULL: s).
+ *
+ * M        capacity in slots (rows of out / dY / dX).
+ * X        bf16, x_rows rows of K, `ldx` elements apart (x_rows >= M when token
+ *          is NULL).  token's entries in use lie in [0, x_rows).
+ * dY       bf16 [M] rows of N, `ldy` elements apart.
+ * offsets  int32 [E + 1]: non-decreasing, offsets[0] >= 0, offsets[E] <= M.
+ * W        bf16 [E][N][K] ([out][in], as the encoder's weights).
+ * bias     fp32 [E][N] or NULL.
+ * pre      bf16: forward, out [M][N] (y before GELU, for the backward pass) or
+ *          NULL; backward, in [M][K] or NULL.
+ * out, dX  [M][N], [M][K]: bf16, or fp32 when out_f32.
+ * dW       [E][N][K]: bf16, or fp32 when out_f32, written for every expert (0 for
+ *          one without slots); dbias fp32 [E][N] or NULL.
+ * Products of bf16 values, sums in fp32, one rounding at the end.  Two calls with
+ * the same arguments give the same bits.
+ * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; ldx and ldy multiples of 8;
+ * every bf16 pointer, out, dX and dW 16-byte aligned.
+ */
+typedef struct {
+  int M, E, N, K;
+  const uint16_t* X;
+  long long ldx;
+  int x_rows;
+  const int32_t* token;
+  const int32_t* offsets;
+  const uint16_t* W;
+  const float* bias;
+  int gelu;
+  uint16_t* pre;
+  void* out;
+  int out_f32;
+} sc_expert_linear_args;
+
+int sc_expert_linear_forward(const sc_expert_linear_args* args, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int M, E, N, K;
+  const uint16_t* dY;
+  long long ldy;
+  const int32_t* offsets;
+  const uint16_t* W;
+  const uint16_t* pre;
+  void* dX;
+  int out_f32;
+} sc_expert_linear_backward_input_args;
+
+int sc_expert_linear_backward_input(const sc_expert_linear_backward_input_args* args,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int M, E, N, K;
+  const uint16_t* dY;
+  long long ldy;
+  const uint16_t* X;
+  long long ldx;
+  int x_rows;
+  const int32_t* token;
+  const int32_t* offsets;
+  void* dW;
+  int out_f32;
+  float* dbias;
+} sc_expert_linear_backward_weight_args;
+
+int sc_expert_linear_backward_weight(const sc_expert_linear_backward_weight_args* args,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The end of the block: the experts' rows summed under their gates, the scaled
+ * residual, and a layer norm.  For every token t in use:
+ *   S[t] = res_scale res[t] + sum_j gate[t][j] Y[slot[t][j]]   (slot -1: nothing)
+ *   out[t] = (S[t] - mean) / sqrt(var + eps) * gamma + beta    (over the D features)
+ *
+ * Y        bf16 [M][D], slots; slot int32 [B L][k]; gate fp32 [B L][k] or NULL (1).
+ * res      bf16 [B L][D] or NULL.
+ * gamma, beta  fp32 [D], both or neither (no norm; out is then not used).
+ * sum      bf16 [B L][D] out (S, e.g. the residual of the next pre-norm block) or
+ *          NULL; out bf16 [B L][D].  The norm takes the unrounded S.
+ * Without norm, gate and res: the sum of a token's rows, e.g. the gradient that
+ * its slots' dX give the token.
+ * D a multiple of 8, at most SC_MAX_EXPERT_DIM; bf16 pointers 16-byte aligned.
+ */
+typedef struct {
+  int B, L, D, k, M;
+  const int32_t* rows;
+  const uint16_t* Y;
+  const int32_t* slot;
+  const float* gate;
+  const uint16_t* res;
+  float res_scale;
+  const float* gamma;
+  const float* beta;
+  float eps;
+  uint16_t* sum;
+  uint16_t* out;
+} sc_expert_combine_args;
+
+int sc_expert_combine_forward(const sc_expert_combine_args* args, void* stream);
+
+/*
+ * Its gradients, from dout (of out; bf16 [B L][D]; NULL exactly when gamma is)
+ * and dsum (of S; bf16 [B L][D] or NULL; at least one of the two):
+ *   dY      bf16 [M][D] out, the slots of the tokens in use
+ *   dgate   fp32 [B L][k] out or NULL; 0 where slot is -1 and for tokens not in use
+ *   dres    bf16 [B L][D] out or NULL
+ *   dgamma, dbeta  fp32 [D] out (NULL exactly when gamma is)
+ * S, its mean and variance are computed again from Y, slot, gate and res.  The
+ * sums over tokens are taken in a fixed order.
+ */
+typedef struct {
+  int B, L, D, k, M;
+  const int32_t* rows;
+  const uint16_t* Y;
+  const int32_t* slot;
+  const float* gate;
+  const uint16_t* res;
+  float res_scale;
+  const float* gamma;
+  float eps;
+  const uint16_t* dout;
+  const uint16_t* dsum;
+  uint16_t* dY;
+  float* dgate;
+  uint16_t* dres;
+  float* dgamma;
+  float* dbeta;
+} sc_expert_combine_backward_args;
+
+int sc_expert_combine_backward(const sc_expert_combine_backward_args* args, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* sc_status_string(int status);
 

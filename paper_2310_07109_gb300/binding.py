@@ -93,7 +93,11 @@ EXPORTED = ["sc_layer_forward", "sc_layer_forward_noalloc", "sc_stack_forward",
             "sc_workspace_size", "sc_workspace_status", "sc_status_string", "sc_last_error",
             "sc_encoder_layer_forward", "sc_encoder_workspace_size", "sc_linear_forward",
             "sc_layer_norm_forward", "sc_layer_noalloc_status", "sc_debug_stall_waits",
-            "sc_select_rows_kernel", "sc_debug_graph_counts"]
+            "sc_select_rows_kernel", "sc_debug_graph_counts",
+            "sc_expert_workspace_size", "sc_expert_route_forward", "sc_expert_route_backward",
+            "sc_expert_linear_forward", "sc_expert_linear_backward_input",
+            "sc_expert_linear_backward_weight", "sc_expert_combine_forward",
+            "sc_expert_combine_backward"]
 
 
 def library_path() -> str:

@@ -33,6 +33,7 @@ cudaError_t configure_encoder();
 cudaError_t launch_gemm(const GemmParams& p, cudaStream_t st);
 cudaError_t launch_layernorm(const LayerNormParams& p, cudaStream_t st);
 cudaError_t launch_row_gather(const RowGatherParams& p, cudaStream_t st);
+cudaError_t configure_expert();
 }  // namespace sc
 
 namespace {
@@ -230,6 +231,7 @@ int ensure_configured() {
     cudaError_t e = configure_kernels();
     if (e == cudaSuccess) e = configure_tail();
     if (e == cudaSuccess) e = configure_encoder();
+    if (e == cudaSuccess) e = configure_expert();
     if (e != cudaSuccess) return fail_cuda("kernel attributes", e);
     done[dev] = true;
   }
@@ -1570,3 +1572,15 @@ extern "C" int sc_encoder_layer_forward(const sc_encoder_args* a, void* workspac
   if ((e = launch_layernorm(ln, st)) != cudaSuccess) return fail_cuda("launch layer norm 2", e);
   return SC_OK;
 }
+
+// ---------------------------------------------------------------------------
+// shared with the entry points of the expert feed-forward operators
+// ---------------------------------------------------------------------------
+namespace sc {
+
+int api_fail(int code, const char* what, const char* detail) { return fail(code, what, detail); }
+int api_fail_cuda(const char* what, cudaError_t e) { return fail_cuda(what, e); }
+int api_ensure_configured() { return ensure_configured(); }
+PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder() { return get_encoder(); }
+
+}  // namespace sc

@@ -1,0 +1,312 @@
+"""ctypes binding of the expert feed-forward operators (include/sparsecoder.h).
+
+Routing of tokens to experts, matrix products grouped by expert and the gated sum
+with residual and layer norm, forward and backward.  As in ``binding``: argument
+marshalling and checks of types and shapes only, asynchronous on torch's current
+stream (or ``stream``), no CPU fallback.  Tokens are the rows of a [B][L] batch with
+``rows[b]`` of them in use; slots are (token, choice) pairs in expert order.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding as _b
+
+MAX_EXPERTS = 256
+MAX_CHOICES = 8
+MAX_EXPERT_DIM = 8192
+
+_I, _P, _F, _LL = ctypes.c_int, ctypes.c_void_p, ctypes.c_float, ctypes.c_longlong
+
+
+class RouteArgs(ctypes.Structure):
+    _fields_ = [("B", _I), ("L", _I), ("E", _I), ("k", _I), ("logits", _P), ("ld", _LL),
+                ("rows", _P), ("renormalize", _I), ("expert", _P), ("gate", _P),
+                ("offsets", _P), ("slot", _P), ("token", _P)]
+
+
+class RouteBackwardArgs(ctypes.Structure):
+    _fields_ = [("B", _I), ("L", _I), ("E", _I), ("k", _I), ("logits", _P), ("ld", _LL),
+                ("rows", _P), ("renormalize", _I), ("expert", _P), ("gate", _P),
+                ("dgate", _P), ("dlogits", _P)]
+
+
+class ExpertLinearArgs(ctypes.Structure):
+    _fields_ = [("M", _I), ("E", _I), ("N", _I), ("K", _I), ("X", _P), ("ldx", _LL),
+                ("x_rows", _I), ("token", _P), ("offsets", _P), ("W", _P), ("bias", _P),
+                ("gelu", _I), ("pre", _P), ("out", _P), ("out_f32", _I)]
+
+
+class ExpertLinearBackwardInputArgs(ctypes.Structure):
+    _fields_ = [("M", _I), ("E", _I), ("N", _I), ("K", _I), ("dY", _P), ("ldy", _LL),
+                ("offsets", _P), ("W", _P), ("pre", _P), ("dX", _P), ("out_f32", _I)]
+
+
+class ExpertLinearBackwardWeightArgs(ctypes.Structure):
+    _fields_ = [("M", _I), ("E", _I), ("N", _I), ("K", _I), ("dY", _P), ("ldy", _LL), ("X", _P),
+                ("ldx", _LL), ("x_rows", _I), ("token", _P), ("offsets", _P), ("dW", _P),
+                ("out_f32", _I), ("dbias", _P)]
+
+
+class ExpertCombineArgs(ctypes.Structure):
+    _fields_ = [("B", _I), ("L", _I), ("D", _I), ("k", _I), ("M", _I), ("rows", _P), ("Y", _P),
+                ("slot", _P), ("gate", _P), ("res", _P), ("res_scale", _F), ("gamma", _P),
+                ("beta", _P), ("eps", _F), ("sum", _P), ("out", _P)]
+
+
+class ExpertCombineBackwardArgs(ctypes.Structure):
+    _fields_ = [("B", _I), ("L", _I), ("D", _I), ("k", _I), ("M", _I), ("rows", _P), ("Y", _P),
+                ("slot", _P), ("gate", _P), ("res", _P), ("res_scale", _F), ("gamma", _P),
+                ("eps", _F), ("dout", _P), ("dsum", _P), ("dY", _P), ("dgate", _P), ("dres", _P),
+                ("dgamma", _P), ("dbeta", _P)]
+
+
+# calls with a workspace and its size before the stream, and those without
+_WITH_WORKSPACE = {"sc_expert_route_forward": RouteArgs,
+                   "sc_expert_linear_forward": ExpertLinearArgs,
+                   "sc_expert_linear_backward_input": ExpertLinearBackwardInputArgs,
+                   "sc_expert_linear_backward_weight": ExpertLinearBackwardWeightArgs,
+                   "sc_expert_combine_backward": ExpertCombineBackwardArgs}
+_WITHOUT_WORKSPACE = {"sc_expert_route_backward": RouteBackwardArgs,
+                      "sc_expert_combine_forward": ExpertCombineArgs}
+_bound = None
+
+
+def _library():
+    global _bound
+    if _bound is None:
+        lib = _b.load()
+        for name, args in _WITH_WORKSPACE.items():
+            getattr(lib, name).argtypes = [ctypes.POINTER(args), _P, ctypes.c_size_t, _P]
+        for name, args in _WITHOUT_WORKSPACE.items():
+            getattr(lib, name).argtypes = [ctypes.POINTER(args), _P]
+        lib.sc_expert_workspace_size.restype = ctypes.c_size_t
+        lib.sc_expert_workspace_size.argtypes = [_I] * 5
+        _bound = lib
+    return _bound
+
+
+def _refuse(what):
+    raise _b.SparseCoderError(_b.SC_ERR_INVALID_ARG, what)
+
+
+def _at(t, name, dtype, shape=None):
+    """The address of a contiguous cuda tensor of this type and shape; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        _refuse("%s: a contiguous cuda tensor of %s is wanted" % (name, dtype))
+    if shape is not None and t.shape != shape:
+        _refuse("%s: shape %s is wanted, not %s" % (name, tuple(shape), tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _rows_at(t, name, dtype):
+    """Address, rows, width and row distance of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype is not dtype or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
+        _refuse("%s: a cuda matrix of %s with contiguous rows is wanted" % (name, dtype))
+    rows, width = t.shape
+    return t.data_ptr(), rows, width, t.stride(0) if rows > 1 else max(t.stride(0), width)
+
+
+def _stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _out_type(t):
+    if t.dtype is torch.float32:
+        return 1
+    if t.dtype is torch.bfloat16:
+        return 0
+    _refuse("outputs are bfloat16 or float32")
+
+
+def expert_workspace_size(B, L, E, k, D) -> int:
+    return int(_library().sc_expert_workspace_size(int(B), int(L), int(E), int(k), int(D)))
+
+
+def new_expert_workspace(B, L, E, k, D, device=None) -> torch.Tensor:
+    """Workspace of the expert operators for a [B][L] batch, E experts, k choices and rows
+    of at most D features (zeroed, 256-byte aligned)."""
+    n = expert_workspace_size(B, L, E, k, D)
+    if n == 0:
+        raise _b.SparseCoderError(_b.SC_ERR_INVALID_ARG, "invalid expert workspace sizes")
+    ws = torch.zeros(n + 256, dtype=torch.uint8, device=device or "cuda")
+    off = (-ws.data_ptr()) % 256
+    return ws[off:off + n]
+
+
+def _work(workspace, device, stream, B, L, E, k, D):
+    if workspace is not None:
+        return workspace
+    ws = new_expert_workspace(B, L, E, k, D, device)
+    if stream is not None:
+        # made (and zeroed) on the current stream, used and let go on another
+        stream.wait_stream(torch.cuda.current_stream(device))
+        ws.record_stream(stream)
+    return ws
+
+
+def _call(name, args, ws, stream):
+    rc = getattr(_library(), name)(args, ws.data_ptr(), ws.numel(), _stream(stream))
+    if rc:
+        _b._check(rc)
+
+
+def expert_route_forward(logits, *, k, B, L, rows=None, renormalize=True, out=None, workspace=None,
+                         stream=None):
+    """``sc_expert_route_forward``: logits fp32 [B*L, E] (any row stride) to k experts a token.
+    Returns dict(expert [B*L, k] int32, gate [B*L, k] fp32, offsets [E + 1], slot [B*L, k],
+    token [B*L*k] int32)."""
+    at, T, E, ld = _rows_at(logits, "logits", torch.float32)
+    if T != B * L:
+        _refuse("logits: B * L rows are wanted")
+    if out is None:
+        new = lambda *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+        out = {"expert": new(T, k), "gate": new(T, k, dtype=torch.float32), "offsets": new(E + 1),
+               "slot": new(T, k), "token": new(T * k)}
+    i32 = torch.int32
+    a = RouteArgs(B, L, E, k, at, ld, _at(rows, "rows", i32, (B,)), 1 if renormalize else 0,
+                  _at(out["expert"], "expert", i32, (T, k)),
+                  _at(out["gate"], "gate", torch.float32, (T, k)),
+                  _at(out["offsets"], "offsets", i32, (E + 1,)),
+                  _at(out["slot"], "slot", i32, (T, k)), _at(out["token"], "token", i32, (T * k,)))
+    _call("sc_expert_route_forward", a, _work(workspace, logits.device, stream, B, L, E, k, 8), stream)
+    return out
+
+
+def expert_route_backward(logits, expert, gate, dgate, *, B, L, rows=None, renormalize=True, out=None,
+                          stream=None):
+    """``sc_expert_route_backward``: the gradient of the logits, fp32 [B*L, E]."""
+    at, T, E, ld = _rows_at(logits, "logits", torch.float32)
+    if T != B * L:
+        _refuse("logits: B * L rows are wanted")
+    k = expert.shape[-1]
+    if out is None:
+        out = torch.empty((T, E), dtype=torch.float32, device=logits.device)
+    f32 = torch.float32
+    a = RouteBackwardArgs(B, L, E, k, at, ld, _at(rows, "rows", torch.int32, (B,)),
+                          1 if renormalize else 0, _at(expert, "expert", torch.int32, (T, k)),
+                          _at(gate, "gate", f32, (T, k)), _at(dgate, "dgate", f32, (T, k)),
+                          _at(out, "dlogits", f32, (T, E)))
+    rc = _library().sc_expert_route_backward(a, _stream(stream))
+    if rc:
+        _b._check(rc)
+    return out
+
+
+def _product_ws(workspace, t, stream):
+    return _work(workspace, t.device, stream, 1, 1, 1, 1, 8)
+
+
+def expert_linear_forward(X, W, offsets, *, token=None, bias=None, gelu=False, pre=None, out=None,
+                          out_f32=False, workspace=None, stream=None):
+    """``sc_expert_linear_forward``: X bf16 [rows, K] (any row stride), W bf16 [E, N, K], offsets
+    int32 [E + 1], bias fp32 [E, N].  Slot s reads row token[s] of X, or row s.  ``pre``: a
+    bf16 [M, N] tensor that receives the values before GELU.  Returns out [M, N], M = len(token),
+    or the rows of X."""
+    at, xr, K, ld = _rows_at(X, "X", torch.bfloat16)
+    E, N, _ = W.shape
+    M = xr if token is None else token.shape[0]
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.float32 if out_f32 else torch.bfloat16, device=X.device)
+    i32 = torch.int32
+    a = ExpertLinearArgs(M, E, N, K, at, ld, xr, _at(token, "token", i32),
+                         _at(offsets, "offsets", i32, (E + 1,)), _at(W, "W", torch.bfloat16, (E, N, K)),
+                         _at(bias, "bias", torch.float32, (E, N)), 1 if gelu else 0,
+                         _at(pre, "pre", torch.bfloat16, (M, N)), _at(out, "out", out.dtype, (M, N)),
+                         _out_type(out))
+    _call("sc_expert_linear_forward", a, _product_ws(workspace, X, stream), stream)
+    return out
+
+
+def expert_linear_backward_input(dY, W, offsets, *, pre=None, out=None, out_f32=False, workspace=None,
+                                 stream=None):
+    """``sc_expert_linear_backward_input``: dY bf16 [M, N] (any row stride), W bf16 [E, N, K]; with
+    ``pre`` bf16 [M, K] the result is multiplied by GELU'(pre).  Returns dX [M, K]."""
+    at, M, N, ld = _rows_at(dY, "dY", torch.bfloat16)
+    E, _, K = W.shape
+    if out is None:
+        out = torch.empty((M, K), dtype=torch.float32 if out_f32 else torch.bfloat16, device=dY.device)
+    a = ExpertLinearBackwardInputArgs(M, E, N, K, at, ld, _at(offsets, "offsets", torch.int32, (E + 1,)),
+                                      _at(W, "W", torch.bfloat16, (E, N, K)),
+                                      _at(pre, "pre", torch.bfloat16, (M, K)),
+                                      _at(out, "out", out.dtype, (M, K)), _out_type(out))
+    _call("sc_expert_linear_backward_input", a, _product_ws(workspace, dY, stream), stream)
+    return out
+
+
+def expert_linear_backward_weight(dY, X, offsets, *, token=None, bias=True, out=None, out_f32=True,
+                                  workspace=None, stream=None):
+    """``sc_expert_linear_backward_weight``: dY bf16 [M, N], X bf16 [rows, K] (any row strides).
+    Returns dict(dW [E, N, K], dbias fp32 [E, N]); without dbias when ``bias`` is False (or
+    ``out`` has none)."""
+    ay, M, N, ldy = _rows_at(dY, "dY", torch.bfloat16)
+    ax, xr, K, ldx = _rows_at(X, "X", torch.bfloat16)
+    E = offsets.shape[0] - 1
+    if token is not None and token.shape[0] != M:
+        _refuse("token: one entry for each row of dY is wanted")
+    if out is None:
+        out = {"dW": torch.empty((E, N, K), dtype=torch.float32 if out_f32 else torch.bfloat16,
+                                 device=X.device)}
+        if bias:
+            out["dbias"] = torch.empty((E, N), dtype=torch.float32, device=X.device)
+    dW = out["dW"]
+    a = ExpertLinearBackwardWeightArgs(M, E, N, K, ay, ldy, ax, ldx, xr,
+                                       _at(token, "token", torch.int32),
+                                       _at(offsets, "offsets", torch.int32),
+                                       _at(dW, "dW", dW.dtype, (E, N, K)), _out_type(dW),
+                                       _at(out.get("dbias"), "dbias", torch.float32, (E, N)))
+    _call("sc_expert_linear_backward_weight", a, _product_ws(workspace, X, stream), stream)
+    return out
+
+
+def expert_combine_forward(Y, slot, gate=None, *, B, L, rows=None, res=None, res_scale=1.0, gamma=None,
+                           beta=None, eps=1e-5, out=None, stream=None):
+    """``sc_expert_combine_forward``: Y bf16 [M, D] rows of the slots, slot int32 [B*L, k], gate fp32
+    [B*L, k] or None (1), res bf16 [B*L, D].  Returns dict(sum [B*L, D] bf16, out) (``out`` with
+    gamma and beta only); a given ``out`` may lack "sum" where there is a norm."""
+    M, D = Y.shape
+    T, k = B * L, slot.shape[-1]
+    if out is None:
+        out = {"sum": torch.empty((T, D), dtype=torch.bfloat16, device=Y.device)}
+        if gamma is not None:
+            out["out"] = torch.empty((T, D), dtype=torch.bfloat16, device=Y.device)
+    bf, f32 = torch.bfloat16, torch.float32
+    a = ExpertCombineArgs(B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf),
+                          _at(slot, "slot", torch.int32, (T, k)), _at(gate, "gate", f32, (T, k)),
+                          _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)),
+                          _at(beta, "beta", f32, (D,)), eps, _at(out.get("sum"), "sum", bf, (T, D)),
+                          _at(out.get("out"), "out", bf, (T, D)))
+    rc = _library().sc_expert_combine_forward(a, _stream(stream))
+    if rc:
+        _b._check(rc)
+    return out
+
+
+def expert_combine_backward(Y, slot, gate=None, *, B, L, dout=None, dsum=None, rows=None, res=None,
+                            res_scale=1.0, gamma=None, eps=1e-5, out=None, workspace=None, stream=None):
+    """``sc_expert_combine_backward``: gradients from dout (with gamma) and dsum, bf16 [B*L, D].
+    Returns dict(dY [M, D] bf16, dgate [B*L, k] fp32, dres [B*L, D] bf16 where res is given, dgamma
+    and dbeta [D] fp32 where gamma is)."""
+    M, D = Y.shape
+    T, k = B * L, slot.shape[-1]
+    bf, f32 = torch.bfloat16, torch.float32
+    if out is None:
+        new = lambda *shape, dtype=f32: torch.empty(shape, dtype=dtype, device=Y.device)  # noqa: E731
+        out = {"dY": new(M, D, dtype=bf), "dgate": new(T, k)}
+        if res is not None:
+            out["dres"] = new(T, D, dtype=bf)
+        if gamma is not None:
+            out.update(dgamma=new(D), dbeta=new(D))
+    a = ExpertCombineBackwardArgs(
+        B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf),
+        _at(slot, "slot", torch.int32, (T, k)), _at(gate, "gate", f32, (T, k)),
+        _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)), eps,
+        _at(dout, "dout", bf, (T, D)), _at(dsum, "dsum", bf, (T, D)), _at(out["dY"], "dY", bf, (M, D)),
+        _at(out.get("dgate"), "dgate", f32, (T, k)), _at(out.get("dres"), "dres", bf, (T, D)),
+        _at(out.get("dgamma"), "dgamma", f32, (D,)), _at(out.get("dbeta"), "dbeta", f32, (D,)))
+    _call("sc_expert_combine_backward", a, _work(workspace, Y.device, stream, B, L, 1, 1, D), stream)
+    return out
