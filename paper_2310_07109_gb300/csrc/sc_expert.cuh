@@ -50,6 +50,8 @@ struct RouteBackParams {
   float* dlogits;            // [T][E]
 };
 
+constexpr int kExpertTimeout = 1;   // status word: a bounded wait expired
+
 // One product grouped by expert.  Expert e has the slots offsets[e] .. offsets[e + 1].
 enum class ExpertProduct { kForward, kBackInput, kBackWeight };
 struct ExpertLinearParams {

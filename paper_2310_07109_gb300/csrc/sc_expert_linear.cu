@@ -1,10 +1,23 @@
 // sc_expert_linear.cu -- matrix products grouped by expert, ragged sizes known on
 // the device alone.  Expert e has the slots offsets[e] .. offsets[e + 1]:
-//   forward       out[s][n]   = act(sum_k x[row(s)][k] W_e[n][k] + b_e[n])
-//   back (input)  out[s][k]   = (sum_n dy[s][n] W_e[n][k]) GELU'(pre[s][k])
+//   forward       out[s][n]    = act(sum_k x[row(s)][k] W_e[n][k] + b_e[n])
+//   back (input)  out[s][k]    = (sum_n dy[s][n] W_e[n][k]) GELU'(pre[s][k])
 //   back (weight) out[e][n][k] = sum_s dy[s][n] x[row(s)][k],  db_e[n] = sum_s dy[s][n]
+//
+// Pair kernel: tcgen05 products of two CTAs (cta_group::2), M = 256.  The weight's
+// features are the M side, so it is always full; the ragged slots are the N side,
+// whose width follows what an expert has (64 to 256, evenly split over its tiles)
+// -- or, in the weight gradient, the contraction.  Persistent CTA pairs walk the
+// tiles that exist; every role counts them out from the offsets.
+//   warp 0    copies both operands, 64 of the contraction a stage, six stages
+//   warp 1    (even CTA) issues the products into one of two 256-column accumulators
+//   warps 2-9 read the other accumulator back
+// Operands as they lie in memory: K-major where the contraction is contiguous
+// (forward; dy in back (input)), else MN-major (W in back (input), both sides of the
+// weight gradient), 128-byte swizzle throughout.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <cudaTypedefs.h>
 #include <cstdint>
 
 #include "sc_expert.cuh"
@@ -12,135 +25,654 @@
 
 namespace sc {
 
-constexpr int kSimpleTile = 64, kSimpleDepth = 16, kSimpleThreads = 256;
+PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder();
+
+constexpr int kPairThreads = 320;
+constexpr int kPairEpiWarps = 8;     // two per tensor-memory lane quarter, every other chunk
+constexpr int kPairM = 128;          // features per CTA, 256 per pair
+constexpr int kPairN = 256;          // widest tile on the other side; half of it per CTA
+constexpr int kPairStep = 64;        // contraction per stage: one 128-byte swizzle atom
+constexpr int kPairStages = 6;
+constexpr int kPairChunk = 32;       // columns read back at a time
+constexpr uint32_t kPairABytes = kPairM * kPairStep * 2;
+constexpr uint32_t kPairBBytes = kPairN / 2 * kPairStep * 2;
+constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes;
+constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN-major operand
+// write-back staging: a 32 x 256-byte area per group of four warps
+constexpr uint32_t kPairOutBytes = 32 * 256;
+constexpr uint32_t kPairDyn = kPairStages * kPairStageBytes + 4 * kPairOutBytes + 1024;
+
+struct PairParams {
+  ExpertLinearParams p;
+  CUtensorMap map_a;     // forward: W, 128 x 64; back (input): W, 64 x 64; back (weight): dy, 64 x 64
+  CUtensorMap map_b;     // other side: 128 x 64, back (weight) 64 x 64; gathered: one row
+  CUtensorMap map_b32;   // ... 32 x 64 (tiles narrower than 256)
+};
+
+struct PairSmem {
+  uint64_t full[kPairStages], empty[kPairStages];   // full: of the even CTA, both CTAs' copies
+  uint64_t tfull[2], tempty[2];                     // tempty: of the even CTA
+  uint32_t tmem_base;
+  int abort;
+  int tile0[kMaxExperts + 1];   // forward, back (input): tiles of slots of the experts before
+};
+
+static_assert(sizeof(PairSmem) + kPairDyn <= 227 * 1024, "one CTA's shared memory");
 
 __device__ __forceinline__ float bf(uint16_t v) {
   return __uint_as_float(static_cast<uint32_t>(v) << 16);
 }
+__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
-__device__ __forceinline__ float gelu_exact(float x) {
-  return 0.5f * x * (1.f + erff(x * 0.70710678118654752f));
+// Phi(-|x|), the lower tail of the normal distribution, by Abramowitz & Stegun 7.1.26
+// (erf, |error| <= 1.5e-7), and e = exp(-x^2 / 2).
+__device__ __forceinline__ float normal_tail(float x, float& e) {
+  const float z = fabsf(x) * 0.70710678118654752f;
+  const float t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
+  e = ex2(z * z * -1.44269504088896341f);
+  float q = fmaf(0.5307027145f, t, -0.7265760135f);
+  q = fmaf(q, t, 0.7107068705f);
+  q = fmaf(q, t, -0.142248368f);
+  q = fmaf(q, t, 0.127414796f);
+  return q * t * e;
 }
+__device__ __forceinline__ float gelu(float x) {
+  float e;
+  const float h = normal_tail(x, e);
+  return x * (x >= 0.f ? 1.f - h : h);
+}
+// GELU'(x) = Phi(x) + x phi(x)
 __device__ __forceinline__ float gelu_slope(float x) {
-  return 0.5f * (1.f + erff(x * 0.70710678118654752f)) +
-         x * expf(-0.5f * x * x) * 0.3989422804014327f;
+  float e;
+  const float h = normal_tail(x, e);
+  return fmaf(x * 0.3989422804014327f, e, x >= 0.f ? 1.f - h : h);
 }
 
-// 64 x 64 outputs a CTA, 4 x 4 a thread, operands through shared memory in fp32.
+// One output tile of the pair: features f0 .. f0 + 256 of expert e, and slots
+// lo + i0 .. (n of them, `width` columns) or, in the weight gradient, the columns
+// i0 .. of the other side with the slots lo .. hi as the contraction.
+struct PairTile {
+  int e, lo, hi, f0, i0, n, width;
+};
+
+// Slots of a tile of an expert with n slots: evenly split, multiples of 64.
+__device__ __forceinline__ int tile_slots(int n) {
+  const int tiles = (n + kPairN - 1) / kPairN;
+  return tiles == 0 ? 64 : ((n + tiles - 1) / tiles + 63) & ~63;
+}
+
 template <ExpertProduct kWhat>
-__global__ void __launch_bounds__(kSimpleThreads) sc_expert_simple_kernel(
-    const __grid_constant__ ExpertLinearParams p) {
-  __shared__ float as[kSimpleDepth][kSimpleTile + 1], bs[kSimpleDepth][kSimpleTile + 1];
+__device__ __forceinline__ int features(const ExpertLinearParams& p) {
+  return kWhat == ExpertProduct::kBackInput ? p.K : p.N;
+}
+
+// Tile t (in increasing order per role: t.e is advanced).
+template <ExpertProduct kWhat>
+__device__ __forceinline__ void pair_tile(const ExpertLinearParams& p, const PairSmem& sm, int t,
+                                          PairTile& g) {
+  const int tiles_f = (features<kWhat>(p) + 255) / 256;
+  const int rest = t / tiles_f;
+  g.f0 = (t - rest * tiles_f) * 256;
+  if constexpr (kWhat == ExpertProduct::kBackWeight) {
+    const int tiles_k = (p.K + kPairN - 1) / kPairN;
+    g.e = rest / tiles_k;
+    g.i0 = (rest - g.e * tiles_k) * kPairN;
+    expert_range(p, g.e, g.lo, g.hi);
+    g.n = min(kPairN, p.K - g.i0);
+  } else {
+    while (sm.tile0[g.e + 1] <= rest) ++g.e;
+    expert_range(p, g.e, g.lo, g.hi);
+    const int w = tile_slots(g.hi - g.lo);
+    g.i0 = (rest - sm.tile0[g.e]) * w;
+    g.n = min(w, g.hi - g.lo - g.i0);
+  }
+  g.width = (g.n + 63) & ~63;
+}
+
+template <ExpertProduct kWhat>
+__device__ __forceinline__ int pair_steps(const ExpertLinearParams& p, const PairTile& g) {
+  const int depth = kWhat == ExpertProduct::kForward ? p.K
+                    : kWhat == ExpertProduct::kBackInput ? p.N : g.hi - g.lo;
+  return (depth + kPairStep - 1) / kPairStep;
+}
+
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait_cluster(bar, parity, abort));
+}
+
+// Four warps that share a staging area meet.
+__device__ __forceinline__ void group_sync(int g) {
+  asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
+}
+
+// Byte offset in a group's staging area of the 16-byte piece c (8 features) of column r.
+__device__ __forceinline__ uint32_t piece(int r, int c) {
+  return static_cast<uint32_t>(r * 256 + ((c ^ (r & 7)) << 4));
+}
+
+// The rows of a last, partial stage of the weight gradient: 64 slots x 128 columns of a
+// matrix into two 64 x 64 boxes, zeros past the expert's slots and the matrix's columns
+// (a product with what lies there would not be 0 for NaN), by the copying warp itself.
+template <bool kGather>
+__device__ __forceinline__ void copy_partial(const ExpertLinearParams& p, uint32_t dst,
+                                             const uint16_t* src, long long ld, int col0, int cols,
+                                             int s0, int hi) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 4
+  for (int q = lane; q < 2 * 64 * 8; q += 32) {
+    const int c = q & 15, r = q >> 4;              // 16-byte piece of row r
+    const int s = s0 + r, col = col0 + 8 * c;
+    const bool in = s < hi && col < cols;
+    const long long row = !in ? 0 : kGather ? expert_row(p, s) : s;
+    cp_async16(dst + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7), src + (in ? row * ld + col : 0),
+               in);
+  }
+}
+
+template <ExpertProduct kWhat, bool kGather>
+__global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
+    const __grid_constant__ PairParams P) {
+  constexpr bool kFwd = kWhat == ExpertProduct::kForward;
+  constexpr bool kBackX = kWhat == ExpertProduct::kBackInput;
+  constexpr bool kBackW = kWhat == ExpertProduct::kBackWeight;
+  const ExpertLinearParams& p = P.p;
+  extern __shared__ uint8_t dyn_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  __shared__ PairSmem sm;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = static_cast<int>(cluster_rank());
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (tid == 0) {
+    for (int s = 0; s < kPairStages; ++s) {
+      mbar_init(&sm.full[s], 2);    // one arrival (with its bytes) per CTA
+      mbar_init(&sm.empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(&sm.tfull[a], 1);
+      mbar_init(&sm.tempty[a], 2 * kPairEpiWarps);
+    }
+    sm.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc_pair(&sm.tmem_base, 512);
+  // what the launch before this one writes is read from here on
   pdl_wait();
   pdl_launch_dependents();
-  const int tid = threadIdx.x;
-  int e = 0, lo = 0, hi = 0, i0, ni;
-  const int j0 = blockIdx.x * kSimpleTile, nj = kWhat == ExpertProduct::kForward ? p.N : p.K;
-  if constexpr (kWhat == ExpertProduct::kBackWeight) {
-    e = blockIdx.z;
-    expert_range(p, e, lo, hi);
-    i0 = blockIdx.y * kSimpleTile;
-    ni = p.N;
+  if constexpr (!kBackW) {
+    if (warp == 0) {
+      int total = 0;
+#pragma unroll 1
+      for (int e0 = 0; e0 < p.E; e0 += 32) {
+        const int e = e0 + lane;
+        int x = 0;
+        if (e < p.E) {
+          int lo, hi;
+          expert_range(p, e, lo, hi);
+          const int w = tile_slots(hi - lo);
+          x = (hi - lo + w - 1) / w;
+        }
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {   // inclusive scan
+          const int y = __shfl_up_sync(0xffffffffu, x, off);
+          if (lane >= off) x += y;
+        }
+        if (e < p.E) sm.tile0[e + 1] = total + x;
+        total += __shfl_sync(0xffffffffu, x, 31);
+      }
+      if (lane == 0) sm.tile0[0] = 0;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // the other CTA's barriers are set up
+  tc_fence_after();
+  const uint32_t tm = sm.tmem_base;
+  volatile int* abort_flag = &sm.abort;
+  const uint32_t ring = smem_u32(base);
+  const int tiles = ((features<kWhat>(p) + 255) / 256) *
+                    (kBackW ? p.E * ((p.K + kPairN - 1) / kPairN) : sm.tile0[p.E]);
+  PairTile g;
+  g.e = 0;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------- copies
+    bool ok = true;
+    int s = 0, use = 0;
+    for (int t = pair; ok && t < tiles; t += pairs) {
+      pair_tile<kWhat>(p, sm, t, g);
+      const int steps = pair_steps<kWhat>(p, g);
+      const int f = g.f0 + rank * kPairM;             // this CTA's features
+      const int half = kBackW ? kPairN / 2 : g.width / 2;
+      const int b0 = g.i0 + rank * half;              // ... and its columns of the tile
+      int row[4] = {0, 0, 0, 0};
+      if constexpr (kGather && kFwd) {
+        // this lane's four rows of x; columns past the tile repeat its last slot
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          row[k] = expert_row(p, g.lo + min(b0 + 4 * lane + k, g.i0 + g.n - 1));
+      }
+#pragma unroll 1
+      for (int kt = 0; kt < steps; ++kt) {
+        if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
+        const uint32_t a = ring + s * kPairStageBytes, b = a + kPairABytes;
+        const uint32_t full = dsmem_addr(smem_u32(&sm.full[s]), 0);
+        const int c0 = kt * kPairStep;
+        if constexpr (kBackW) {
+          const int s0 = g.lo + c0;
+          if (s0 + kPairStep > g.hi) {
+            copy_partial<false>(p, a, p.dy, p.ldy, f, p.N, s0, g.hi);
+            copy_partial<kGather>(p, b, p.x, p.ldx, b0, p.K, s0, g.hi);
+            cp_async_wait_all();
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(full);
+          } else {
+            if (lane == 0) {
+              mbar_arrive_expect_tx_cluster(full, kPairStageBytes);
+              tma_load_2d_pair(a, &P.map_a, f, s0, full);
+              tma_load_2d_pair(a + kPairBoxBytes, &P.map_a, f + 64, s0, full);
+            }
+            if constexpr (kGather) {
+              // lanes 0-15 the first 64 columns, four slots each, 16-31 the others
+              int r[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) r[k] = expert_row(p, s0 + 4 * (lane & 15) + k);
+              __syncwarp();
+              tma_gather4_pair(b + 512 * lane, &P.map_b, b0 + 64 * (lane >> 4), r[0], r[1], r[2], r[3],
+                               full);
+            } else if (lane == 0) {
+              tma_load_2d_pair(b, &P.map_b, b0, s0, full);
+              tma_load_2d_pair(b + kPairBoxBytes, &P.map_b, b0 + 64, s0, full);
+            }
+          }
+        } else {
+          const uint32_t b_bytes = half * kPairStep * 2;
+          if (lane == 0) {
+            mbar_arrive_expect_tx_cluster(full, kPairABytes + b_bytes);
+            if constexpr (kFwd) {
+              tma_load_3d_pair(a, &P.map_a, c0, f, g.e, full);
+            } else {
+              tma_load_3d_pair(a, &P.map_a, f, c0, g.e, full);
+              tma_load_3d_pair(a + kPairBoxBytes, &P.map_a, f + 64, c0, g.e, full);
+            }
+          }
+          if constexpr (kGather && kFwd) {
+            __syncwarp();
+            if (4 * lane < half)
+              tma_gather4_pair(b + 512 * lane, &P.map_b, c0, row[0], row[1], row[2], row[3], full);
+          } else if (lane == 0) {
+            if (half == kPairN / 2) {
+              tma_load_2d_pair(b, &P.map_b, c0, g.lo + b0, full);
+            } else {
+              for (int q = 0; q < half; q += 32)
+                tma_load_2d_pair(b + q * 128, &P.map_b32, c0, g.lo + b0 + q, full);
+            }
+          }
+        }
+        __syncwarp();
+        if (++s == kPairStages) {
+          s = 0;
+          ++use;
+        }
+      }
+    }
+    // every stage's products are done, and their arrivals have come, before this CTA ends
+#pragma unroll 1
+    for (int q = 0; q < kPairStages; ++q) {
+      const int fills = use + (q < s ? 1 : 0);
+      if (fills > 0) warp_wait(&sm.empty[q], (fills - 1) & 1, abort_flag);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------- products
+    if (rank == 0 && elect_one()) {
+      bool ok = true;
+      int s = 0, use = 0, j = 0;
+      for (int t = pair; ok && t < tiles; t += pairs) {
+        pair_tile<kWhat>(p, sm, t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+        if (steps == 0) continue;
+        const int acc = j & 1;
+        if (j >= 2 && !(ok = mbar_wait_cluster(&sm.tempty[acc], ((j >> 1) - 1) & 1, abort_flag))) break;
+        tc_fence_after();
+        const uint32_t d = tm + acc * kPairN;
+        const uint32_t idesc = idesc_bf16(256, kBackW ? kPairN : g.width, !kFwd, kBackW);
+        // low descriptor words: K-major operands advance 32 bytes per 16 of the
+        // contraction, MN-major ones two groups of eight 128-byte rows; their other
+        // 64-feature boxes lie 8 KB apart
+        constexpr uint32_t kFar = (kPairBoxBytes >> 4) << 16, kNear = 1u << 16;
+        constexpr uint32_t kStepA = kFwd ? 2 : 128, kStepB = kBackW ? 128 : 2;
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          if (!(ok = mbar_wait_cluster(&sm.full[s], use & 1, abort_flag))) break;
+          tc_fence_after();
+          const uint32_t at = ring + s * kPairStageBytes;
+          const uint32_t a = (at >> 4) | (kFwd ? kNear : kFar);
+          const uint32_t b = ((at + kPairABytes) >> 4) | (kBackW ? kFar : kNear);
+#pragma unroll
+          for (int k = 0; k < kPairStep / 16; ++k)
+            umma_bf16_pair_lo(d, a + kStepA * k, b + kStepB * k, idesc, (kt | k) != 0);
+          umma_commit_pair(&sm.empty[s]);
+          if (++s == kPairStages) {
+            s = 0;
+            ++use;
+          }
+        }
+        umma_commit_pair(&sm.tfull[acc]);
+        ++j;
+      }
+    }
+    __syncwarp();
   } else {
-    int t = blockIdx.y;
-    for (;; ++e) {
-      if (e == p.E) return;
-      expert_range(p, e, lo, hi);
-      const int tiles = (hi - lo + kSimpleTile - 1) / kSimpleTile;
-      if (t < tiles) break;
-      t -= tiles;
-    }
-    i0 = t * kSimpleTile;
-    ni = hi - lo;
-  }
-  const uint16_t* w = p.w + static_cast<long long>(e) * p.N * p.K;
-  const int depth = kWhat == ExpertProduct::kForward ? p.K
-                    : kWhat == ExpertProduct::kBackInput ? p.N : hi - lo;
-  float acc[4][4] = {};
-  float rows = 0.f;   // kBackWeight: the sum over the slots of row i0 + tid of dy^T
-  for (int d0 = 0; d0 < depth; d0 += kSimpleDepth) {
-    for (int q = tid; q < kSimpleTile * kSimpleDepth; q += kSimpleThreads) {
-      // i and j of the operands along the unit stride of their memory
-      int d, i;
-      if constexpr (kWhat == ExpertProduct::kBackWeight) i = q % kSimpleTile, d = q / kSimpleTile;
-      else d = q % kSimpleDepth, i = q / kSimpleDepth;
-      float a = 0.f, b = 0.f;
-      if (d0 + d < depth && i0 + i < ni) {
-        if constexpr (kWhat == ExpertProduct::kForward)
-          a = bf(p.x[static_cast<long long>(expert_row(p, lo + i0 + i)) * p.ldx + d0 + d]);
-        else if constexpr (kWhat == ExpertProduct::kBackInput)
-          a = bf(p.dy[static_cast<long long>(lo + i0 + i) * p.ldy + d0 + d]);
-        else
-          a = bf(p.dy[static_cast<long long>(lo + d0 + d) * p.ldy + i0 + i]);
+    // ------------------------------------------------------------- write back
+    const int q = warp & 3, grp = (warp - 2) >> 2;
+    const int gt = tid - 64 - 128 * grp;               // thread of the group
+    uint8_t* const stg = base + kPairStages * kPairStageBytes + 2 * grp * kPairOutBytes;
+    uint8_t* const stg2 = stg + kPairOutBytes;
+    const uint32_t tempty0 = dsmem_addr(smem_u32(&sm.tempty[0]), 0);
+    bool ok = true;
+    int j = 0;
+    for (int t = pair; t < tiles; t += pairs) {
+      pair_tile<kWhat>(p, sm, t, g);
+      const int steps = pair_steps<kWhat>(p, g);
+      const int acc = j & 1;
+      const int f = g.f0 + rank * kPairM;
+      float bias[2][2] = {};
+      if constexpr (kFwd) {
+        if (p.bias != nullptr)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int n = f + 32 * q + 16 * h + 8 * u + lane / 4;
+              if (n < p.N) bias[h][u] = __ldg(p.bias + static_cast<size_t>(g.e) * p.N + n);
+            }
       }
-      as[d][i] = a;
-      if constexpr (kWhat == ExpertProduct::kBackInput) i = q % kSimpleTile, d = q / kSimpleTile;
-      if (d0 + d < depth && j0 + i < nj) {
-        if constexpr (kWhat == ExpertProduct::kForward)
-          b = bf(w[static_cast<long long>(j0 + i) * p.K + d0 + d]);
-        else if constexpr (kWhat == ExpertProduct::kBackInput)
-          b = bf(w[static_cast<long long>(d0 + d) * p.K + j0 + i]);
-        else
-          b = bf(p.x[static_cast<long long>(expert_row(p, lo + d0 + d)) * p.ldx + j0 + i]);
-      }
-      bs[d][i] = b;
-    }
-    __syncthreads();
+      if (steps > 0) ok = ok && warp_wait(&sm.tfull[acc], (j >> 1) & 1, abort_flag);
+      tc_fence_after();
+      const uint32_t d = tm + acc * kPairN + (static_cast<uint32_t>(32 * q) << 16);
+      if constexpr (kBackW) {
+        // rows are features, columns contiguous in memory
+        const int rows = min(32, p.N - f - 32 * q);
+        const uint32_t mask = !ok || rows <= 0 ? 0u : rows == 32 ? 0xffffffffu : (1u << rows) - 1u;
+        uint8_t* const mine = base + kPairStages * kPairStageBytes + (warp - 2) * 4096;
+        const size_t row0 = (static_cast<size_t>(g.e) * p.N + f + 32 * q) * p.K + g.i0;
+#pragma unroll 1
+        for (int c = kPairChunk * grp; mask != 0u && c < g.n; c += 2 * kPairChunk) {
+          float v[32];
+          if (steps > 0) {
+            tmem_ld32(d + c, v);
+            tmem_ld_wait();
+          } else {
 #pragma unroll
-    for (int d = 0; d < kSimpleDepth; ++d) {
+            for (int k = 0; k < 32; ++k) v[k] = 0.f;   // an expert without slots
+          }
+          const int here = min(kPairChunk, g.n - c);    // multiple of 8
+          if (p.out_f32) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+            for (int k = 0; k < 32; k += 4)
+              stage_row_piece<8>(mine, k / 4,
+                                 make_uint4(__float_as_uint(v[k]), __float_as_uint(v[k + 1]),
+                                            __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3])));
+            __syncwarp();
+            float* out = static_cast<float*>(p.out) + row0 + c;
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-          acc[u][v] = fmaf(as[d][(tid / 16) + 16 * u], bs[d][(tid % 16) + 16 * v], acc[u][v]);
-      if (kWhat == ExpertProduct::kBackWeight && tid < kSimpleTile) rows += as[d][tid];
-    }
-    __syncthreads();
-  }
-  if constexpr (kWhat == ExpertProduct::kBackWeight) {
-    if (p.dbias != nullptr && blockIdx.x == 0 && tid < kSimpleTile && i0 + tid < ni)
-      p.dbias[static_cast<long long>(e) * p.N + i0 + tid] = rows;
-  }
+            for (int k = 0; k < 8; ++k) {
+              const int r = 4 * k + lane / 8, x = lane & 7;
+              const uint4 o = *reinterpret_cast<const uint4*>(mine + stage_offset<8>(r, x));
+              if (((mask >> r) & 1u) && 4 * x < here)
+                *reinterpret_cast<uint4*>(out + static_cast<size_t>(r) * p.K + 4 * x) = o;
+            }
+          } else {
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
+            for (int k = 0; k < 32; k += 8)
+              stage_row_piece<4>(mine, k / 8,
+                                 make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
+                                            pack_bf16x2(v[k + 4], v[k + 5]),
+                                            pack_bf16x2(v[k + 6], v[k + 7])));
+            __syncwarp();
+            uint16_t* out = static_cast<uint16_t*>(p.out) + row0 + c;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int i = i0 + tid / 16 + 16 * u, j = j0 + tid % 16 + 16 * v;
-      if (i >= ni || j >= nj) continue;
-      float y = acc[u][v];
-      long long at;
-      if constexpr (kWhat == ExpertProduct::kForward) {
-        at = static_cast<long long>(lo + i) * p.N + j;
-        if (p.bias != nullptr) y += p.bias[static_cast<long long>(e) * p.N + j];
-        if (p.pre != nullptr) p.pre[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
-        if (p.gelu) y = gelu_exact(y);
-      } else if constexpr (kWhat == ExpertProduct::kBackInput) {
-        at = static_cast<long long>(lo + i) * p.K + j;
-        if (p.pre_in != nullptr) y *= gelu_slope(bf(p.pre_in[at]));
+            for (int k = 0; k < 4; ++k) {
+              const int r = 8 * k + lane / 4, x = lane & 3;
+              const uint4 o = *reinterpret_cast<const uint4*>(mine + stage_offset<4>(r, x));
+              if (((mask >> r) & 1u) && 8 * x < here)
+                *reinterpret_cast<uint4*>(out + static_cast<size_t>(r) * p.K + 8 * x) = o;
+            }
+          }
+          __syncwarp();
+        }
       } else {
-        at = (static_cast<long long>(e) * p.N + i) * p.K + j;
+        // rows are features, columns slots: transposed on the way out
+        const int width = features<kWhat>(p);
+        const size_t slot0 = static_cast<size_t>(g.lo) + g.i0;
+        // the group's 32 columns x 128 features of a staged chunk, 16 bytes a thread
+        const auto flush = [&](const uint8_t* from, uint16_t* to, int c) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = 8 * k + (gt >> 4), x = gt & 15;
+            const uint4 o = *reinterpret_cast<const uint4*>(from + piece(r, x));
+            if (c + r < g.n && f + 8 * x < width)
+              *reinterpret_cast<uint4*>(to + (slot0 + c + r) * width + f + 8 * x) = o;
+          }
+        };
+        const int mi = lane >> 3;   // fragment whose row address this lane gives
+#pragma unroll 1
+        for (int c = kPairChunk * grp; c < g.n; c += 2 * kPairChunk) {
+          if (kBackX && p.pre_in != nullptr) {
+            // the chunk of `pre`, so that its fragments match the accumulator's
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int r = 8 * k + (gt >> 4), x = gt & 15;
+              uint4 o = make_uint4(0, 0, 0, 0);
+              if (c + r < g.n && f + 8 * x < width)
+                o = __ldg(reinterpret_cast<const uint4*>(p.pre_in + (slot0 + c + r) * width + f + 8 * x));
+              *reinterpret_cast<uint4*>(stg2 + piece(r, x)) = o;
+            }
+            group_sync(grp);
+          }
+          float v[2][16];
+          tmem_ld_frag32(d + c, v[0]);
+          tmem_ld_frag32(d + c + (16u << 16), v[1]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < 4; b += 2) {
+              const int r = 8 * (b + (mi >> 1)) + (lane & 7), x = 4 * q + 2 * h + (mi & 1);
+              float* w = v[h] + 4 * b;
+              if constexpr (kFwd) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] += bias[h][(k >> 1) & 1];
+                if (p.pre != nullptr)
+                  stmatrix4_trans(smem_u32(stg2 + piece(r, x)), pack_bf16x2(w[0], w[1]),
+                                  pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
+                                  pack_bf16x2(w[6], w[7]));
+                if (p.gelu)
+#pragma unroll
+                  for (int k = 0; k < 8; ++k) w[k] = gelu(w[k]);
+              } else if (p.pre_in != nullptr) {
+                uint32_t z[4];
+                ldmatrix4_trans(smem_u32(stg2 + piece(r, x)), z);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  w[2 * k] *= gelu_slope(bf_lo(z[k]));
+                  w[2 * k + 1] *= gelu_slope(bf_hi(z[k]));
+                }
+              }
+              if (!p.out_f32) {
+                stmatrix4_trans(smem_u32(stg + piece(r, x)), pack_bf16x2(w[0], w[1]),
+                                pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
+                                pack_bf16x2(w[6], w[7]));
+              } else if (ok) {
+                // eight lanes write 32 consecutive bytes of a slot
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const int col = c + 8 * (b + (k >> 2)) + 2 * (lane & 3) + (k & 1);
+                  const int n = f + 32 * q + 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
+                  if (col < g.n && n < width)
+                    static_cast<float*>(p.out)[(slot0 + col) * width + n] = w[k];
+                }
+              }
+            }
+          group_sync(grp);
+          if (ok) {
+            if (!p.out_f32) flush(stg, static_cast<uint16_t*>(p.out), c);
+            if (kFwd && p.pre != nullptr) flush(stg2, p.pre, c);
+          }
+          group_sync(grp);   // the staging areas may be written again
+        }
       }
-      if (p.out_f32) static_cast<float*>(p.out)[at] = y;
-      else static_cast<uint16_t*>(p.out)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+      if (steps > 0) {
+        // the accumulator may take the tile after next
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * acc);
+        ++j;
+      }
     }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // nothing of the pair is in flight to or from the other CTA
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tm, 512);
+  }
+  if (tid == 0 && sm.abort) atomicOr(p.status, kExpertTimeout);
+}
+
+// Bias gradient: the sum over an expert's slots of 64 columns of dy, in slot order
+// within each of 32 interleaved partial sums, those in order.
+constexpr int kBiasThreads = 256;
+__global__ void __launch_bounds__(kBiasThreads) sc_expert_bias_kernel(
+    const __grid_constant__ ExpertLinearParams p) {
+  __shared__ float red[32][64 + 4];
+  const int tid = threadIdx.x, c = tid & 7, r = tid >> 3;
+  const int col = blockIdx.x * 64 + 8 * c;
+  pdl_wait();
+  pdl_launch_dependents();
+  int lo, hi;
+  expert_range(p, blockIdx.y, lo, hi);
+  float a[8] = {};
+  if (col < p.N) {
+#pragma unroll 4
+    for (int s = lo + r; s < hi; s += 32) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p.dy + static_cast<long long>(s) * p.ldy + col));
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a[2 * k] += bf_lo(w[k]);
+        a[2 * k + 1] += bf_hi(w[k]);
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) red[r][8 * c + k] = a[k];
+  __syncthreads();
+  const int n = blockIdx.x * 64 + tid;
+  if (tid < 64 && n < p.N) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s += red[k][tid];
+    p.dbias[static_cast<size_t>(blockIdx.y) * p.N + n] = s;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launch
+// ---------------------------------------------------------------------------
+// bf16 rows of `cols` elements, `ld` apart, as a tensor map of 64-column boxes with the
+// 128-byte swizzle; with experts > 0, that many matrices of `rows` rows each (3-D).
+static bool encode_rows(CUtensorMap* m, const void* base, long long rows, int cols, long long ld,
+                        int experts, int box_rows) {
+  const auto enc = api_tensor_map_encoder();
+  if (!enc) return false;
+  const cuuint64_t dim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
+                             static_cast<cuuint64_t>(experts > 0 ? experts : 1)};
+  const cuuint64_t stride[2] = {static_cast<cuuint64_t>(ld) * 2,
+                                static_cast<cuuint64_t>(ld) * 2 * static_cast<cuuint64_t>(rows)};
+  const cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(box_rows), 1u}, one[3] = {1u, 1u, 1u};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, experts > 0 ? 3 : 2, const_cast<void*>(base), dim,
+             stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <ExpertProduct kWhat, bool kGather>
+static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
+  static int sms = 0;
+  if (sms == 0) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+  }
+  const long long pairs = most_tiles < sms / 2 ? most_tiles : sms / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = kPairDyn;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, sc_expert_pair_kernel<kWhat, kGather>, P);
 }
 
 cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p, cudaStream_t st) {
-  const auto tiles = [](int n) { return static_cast<unsigned>((n + kSimpleTile - 1) / kSimpleTile); };
-  if (what == ExpertProduct::kBackWeight)
-    return launch_chained(sc_expert_simple_kernel<ExpertProduct::kBackWeight>,
-                          dim3(tiles(p.K), tiles(p.N), p.E), dim3(kSimpleThreads), 0, st, p);
-  // no more tiles than full ones and one begun for each expert
-  const unsigned rows = static_cast<unsigned>(p.M / kSimpleTile + (p.E < p.M ? p.E : p.M));
-  if (what == ExpertProduct::kForward)
-    return launch_chained(sc_expert_simple_kernel<ExpertProduct::kForward>, dim3(tiles(p.N), rows),
-                          dim3(kSimpleThreads), 0, st, p);
-  return launch_chained(sc_expert_simple_kernel<ExpertProduct::kBackInput>, dim3(tiles(p.K), rows),
-                        dim3(kSimpleThreads), 0, st, p);
+  PairParams P;
+  P.p = p;
+  const bool gather = p.token != nullptr;
+  // no more tiles of slots than full ones and two begun for each expert
+  const long long slot_tiles = p.M / kPairN + 2ll * (p.E < p.M ? p.E : p.M);
+  bool ok;
+  if (what == ExpertProduct::kForward) {
+    ok = encode_rows(&P.map_a, p.w, p.N, p.K, p.K, p.E, kPairM) &&
+         encode_rows(&P.map_b, p.x, gather ? p.x_rows : p.M, p.K, p.ldx, 0, gather ? 1 : kPairN / 2) &&
+         (gather || encode_rows(&P.map_b32, p.x, p.M, p.K, p.ldx, 0, 32));
+    if (!ok) return cudaErrorInvalidValue;
+    const long long tiles = slot_tiles * ((p.N + 255) / 256);
+    return gather ? launch_pair<ExpertProduct::kForward, true>(P, tiles, st)
+                  : launch_pair<ExpertProduct::kForward, false>(P, tiles, st);
+  }
+  if (what == ExpertProduct::kBackInput) {
+    ok = encode_rows(&P.map_a, p.w, p.N, p.K, p.K, p.E, kPairStep) &&
+         encode_rows(&P.map_b, p.dy, p.M, p.N, p.ldy, 0, kPairN / 2) &&
+         encode_rows(&P.map_b32, p.dy, p.M, p.N, p.ldy, 0, 32);
+    if (!ok) return cudaErrorInvalidValue;
+    return launch_pair<ExpertProduct::kBackInput, false>(P, slot_tiles * ((p.K + 255) / 256), st);
+  }
+  ok = encode_rows(&P.map_a, p.dy, p.M, p.N, p.ldy, 0, kPairStep) &&
+       encode_rows(&P.map_b, p.x, gather ? p.x_rows : p.M, p.K, p.ldx, 0, gather ? 1 : kPairStep);
+  if (!ok) return cudaErrorInvalidValue;
+  const long long tiles = static_cast<long long>(p.E) * ((p.N + 255) / 256) * ((p.K + kPairN - 1) / kPairN);
+  const cudaError_t e = gather ? launch_pair<ExpertProduct::kBackWeight, true>(P, tiles, st)
+                               : launch_pair<ExpertProduct::kBackWeight, false>(P, tiles, st);
+  if (e != cudaSuccess || p.dbias == nullptr) return e;
+  return launch_chained(sc_expert_bias_kernel, dim3((p.N + 63) / 64, p.E), dim3(kBiasThreads), 0, st, p);
 }
 
 cudaError_t configure_combine();
 
-cudaError_t configure_expert() { return configure_combine(); }
+cudaError_t configure_expert() {
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const int bytes = static_cast<int>(kPairDyn);
+  cudaError_t e = configure_combine();
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kForward, false>, attr, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kForward, true>, attr, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kBackInput, false>, attr, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kBackWeight, false>, attr, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kBackWeight, true>, attr, bytes);
+  return e;
+}
 
 }  // namespace sc
