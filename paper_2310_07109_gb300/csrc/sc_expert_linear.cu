@@ -138,7 +138,7 @@ __device__ __forceinline__ int pair_steps(const ExpertLinearParams& p, const Pai
 }
 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  return __all_sync(0xffffffffu, mbar_wait_cluster(bar, parity, abort));
+  return __all_sync(0xffffffffu, mbar_wait_poll(bar, parity, abort));
 }
 
 // Four warps that share a staging area meet.
@@ -268,7 +268,10 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
             cp_async_wait_all();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(full);
+            if (lane == 0) {
+              fence_cluster();
+              mbar_arrive_cluster(full);
+            }
           } else {
             if (lane == 0) {
               mbar_arrive_expect_tx_cluster(full, kPairStageBytes);
@@ -335,7 +338,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
         const int steps = pair_steps<kWhat>(p, g);
         if (steps == 0) continue;
         const int acc = j & 1;
-        if (j >= 2 && !(ok = mbar_wait_cluster(&sm.tempty[acc], ((j >> 1) - 1) & 1, abort_flag))) break;
+        if (j >= 2 && !(ok = mbar_wait_poll(&sm.tempty[acc], ((j >> 1) - 1) & 1, abort_flag))) break;
         tc_fence_after();
         const uint32_t d = tm + acc * kPairN;
         const uint32_t idesc = idesc_bf16(256, kBackW ? kPairN : g.width, !kFwd, kBackW);
@@ -346,7 +349,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
         constexpr uint32_t kStepA = kFwd ? 2 : 128, kStepB = kBackW ? 128 : 2;
 #pragma unroll 1
         for (int kt = 0; kt < steps; ++kt) {
-          if (!(ok = mbar_wait_cluster(&sm.full[s], use & 1, abort_flag))) break;
+          if (!(ok = mbar_wait_poll(&sm.full[s], use & 1, abort_flag))) break;
+          if (kBackW && g.lo + (kt + 1) * kPairStep > g.hi) {
+            // a partial stage was written by the copying warps of both CTAs
+            fence_cluster();
+            fence_proxy_async_smem();
+          }
           tc_fence_after();
           const uint32_t at = ring + s * kPairStageBytes;
           const uint32_t a = (at >> 4) | (kFwd ? kNear : kFar);
