@@ -9,9 +9,14 @@
 // whose width follows what an expert has (64 to 256, evenly split over its tiles)
 // -- or, in the weight gradient, the contraction.  Persistent CTA pairs walk the
 // tiles that exist; every role counts them out from the offsets.
-//   warp 0    copies both operands, 64 of the contraction a stage, six stages
-//   warp 1    (even CTA) issues the products into one of two 256-column accumulators
-//   warps 2-9 read the other accumulator back
+//   warp 0      copies the operands, 64 of the contraction a stage, six stages
+//   warp 1      (even CTA) issues the products into one of two 256-column accumulators
+//   warps 4-11  read the other accumulator back
+//   four warps more (rows of x gathered) copy these rows, 16 bytes a thread: four-row
+//               TMA gathers of 128-byte rows took 81 cycles each, 8 x 1024 rows x 2
+//               experts 768 -> 1536 99 us against 34 without the gather
+//   four warps more (weight gradient) sum dy over the slots for the bias, from the
+//               stages in shared memory
 // Operands as they lie in memory: K-major where the contraction is contiguous
 // (forward; dy in back (input)), else MN-major (W in back (input), both sides of the
 // weight gradient), 128-byte swizzle throughout.
@@ -27,7 +32,7 @@ namespace sc {
 
 PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder();
 
-constexpr int kPairThreads = 320;
+constexpr int kPairThreads = 384;    // without the gathering and the summing warps
 constexpr int kPairEpiWarps = 8;     // two per tensor-memory lane quarter, every other chunk
 constexpr int kPairM = 128;          // features per CTA, 256 per pair
 constexpr int kPairN = 256;          // widest tile on the other side; half of it per CTA
@@ -45,16 +50,21 @@ constexpr uint32_t kPairDyn = kPairStages * kPairStageBytes + 4 * kPairOutBytes 
 struct PairParams {
   ExpertLinearParams p;
   CUtensorMap map_a;     // forward: W, 128 x 64; back (input): W, 64 x 64; back (weight): dy, 64 x 64
-  CUtensorMap map_b;     // other side: 128 x 64, back (weight) 64 x 64; gathered: one row
+  CUtensorMap map_b;     // other side, not gathered: 128 x 64, back (weight) 64 x 64
   CUtensorMap map_b32;   // ... 32 x 64 (tiles narrower than 256)
 };
 
 struct PairSmem {
   uint64_t full[kPairStages], empty[kPairStages];   // full: of the even CTA, both CTAs' copies
+  uint64_t done[kPairStages];                       // products done, the bias sums not yet
+  uint64_t landed[kPairStages];                     // this CTA's gathered rows
   uint64_t tfull[2], tempty[2];                     // tempty: of the even CTA
   uint32_t tmem_base;
   int abort;
-  int tile0[kMaxExperts + 1];   // forward, back (input): tiles of slots of the experts before
+  union {
+    int tile0[kMaxExperts + 1];   // forward, back (input): tiles of slots of the experts before
+    alignas(16) float sums[2][kPairM];   // weight gradient: bias sums of two warps each
+  };
 };
 
 static_assert(sizeof(PairSmem) + kPairDyn <= 227 * 1024, "one CTA's shared memory");
@@ -65,28 +75,46 @@ __device__ __forceinline__ float bf(uint16_t v) {
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
-// Phi(-|x|), the lower tail of the normal distribution, by Abramowitz & Stegun 7.1.26
-// (erf, |error| <= 1.5e-7), and e = exp(-x^2 / 2).
-__device__ __forceinline__ float normal_tail(float x, float& e) {
-  const float z = fabsf(x) * 0.70710678118654752f;
-  const float t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
-  e = ex2(z * z * -1.44269504088896341f);
-  float q = fmaf(0.5307027145f, t, -0.7265760135f);
-  q = fmaf(q, t, 0.7107068705f);
-  q = fmaf(q, t, -0.142248368f);
-  q = fmaf(q, t, 0.127414796f);
-  return q * t * e;
+// GELU and its slope with the normal distribution's lower tail Phi(-|x|) = q(t) e,
+// e = exp(-x^2 / 2), t = 1 / (1 + p |x| / sqrt 2), by Abramowitz & Stegun 7.1.26 (erf,
+// |error| <= 1.5e-7), in packed pairs: the read-back warps bound products with GELU.
+__device__ __forceinline__ uint64_t f2_both(float x) { return f2_pack(x, x); }
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
-__device__ __forceinline__ float gelu(float x) {
-  float e;
-  const float h = normal_tail(x, e);
-  return x * (x >= 0.f ? 1.f - h : h);
+// q(t) t and e of |x|
+__device__ __forceinline__ void normal_tail2(uint64_t ax, uint64_t& qt, uint64_t& e) {
+  float d0, d1, e0, e1;
+  f2_unpack(f2_fma(ax, f2_both(0.3275911f * 0.70710678118654752f), f2_both(1.f)), d0, d1);
+  f2_unpack(f2_mul(f2_mul(ax, ax), f2_both(-0.5f * 1.44269504088896341f)), e0, e1);
+  const uint64_t t = f2_pack(rcp_approx(d0), rcp_approx(d1));
+  uint64_t q = f2_fma(f2_both(0.5307027145f), t, f2_both(-0.7265760135f));
+  q = f2_fma(q, t, f2_both(0.7107068705f));
+  q = f2_fma(q, t, f2_both(-0.142248368f));
+  q = f2_fma(q, t, f2_both(0.127414796f));
+  qt = f2_mul(q, t);
+  e = f2_pack(ex2(e0), ex2(e1));
 }
-// GELU'(x) = Phi(x) + x phi(x)
-__device__ __forceinline__ float gelu_slope(float x) {
-  float e;
-  const float h = normal_tail(x, e);
-  return fmaf(x * 0.3989422804014327f, e, x >= 0.f ? 1.f - h : h);
+// GELU(x) = max(x, 0) - |x| Phi(-|x|)
+__device__ __forceinline__ void gelu2(float& x0, float& x1) {
+  const uint64_t ax = f2_pack(fabsf(x0), fabsf(x1));
+  uint64_t qt, e;
+  normal_tail2(ax, qt, e);
+  f2_unpack(f2_fma(f2_mul(ax, f2_mul(qt, f2_both(-1.f))), e, f2_pack(fmaxf(x0, 0.f), fmaxf(x1, 0.f))),
+            x0, x1);
+}
+// y *= GELU'(x) = 1/2 + sign(x) (1/2 - Phi(-|x|) + |x| phi(x))
+__device__ __forceinline__ void gelu_slope2(float x0, float x1, float& y0, float& y1) {
+  const uint64_t ax = f2_pack(fabsf(x0), fabsf(x1));
+  uint64_t qt, e;
+  normal_tail2(ax, qt, e);
+  float u0, u1;
+  f2_unpack(f2_fma(f2_fma(ax, f2_both(0.3989422804014327f), f2_mul(qt, f2_both(-1.f))), e, f2_both(0.5f)),
+            u0, u1);
+  y0 *= 0.5f + copysignf(u0, x0);
+  y1 *= 0.5f + copysignf(u1, x1);
 }
 
 // One output tile of the pair: features f0 .. f0 + 256 of expert e, and slots
@@ -154,24 +182,26 @@ __device__ __forceinline__ uint32_t piece(int r, int c) {
 // The rows of a last, partial stage of the weight gradient: 64 slots x 128 columns of a
 // matrix into two 64 x 64 boxes, zeros past the expert's slots and the matrix's columns
 // (a product with what lies there would not be 0 for NaN), by the copying warp itself.
-template <bool kGather>
-__device__ __forceinline__ void copy_partial(const ExpertLinearParams& p, uint32_t dst,
-                                             const uint16_t* src, long long ld, int col0, int cols,
-                                             int s0, int hi) {
+__device__ __forceinline__ void copy_partial(uint32_t dst, const uint16_t* src, long long ld, int col0,
+                                             int cols, int s0, int hi) {
   const int lane = threadIdx.x & 31;
 #pragma unroll 4
   for (int q = lane; q < 2 * 64 * 8; q += 32) {
     const int c = q & 15, r = q >> 4;              // 16-byte piece of row r
     const int s = s0 + r, col = col0 + 8 * c;
     const bool in = s < hi && col < cols;
-    const long long row = !in ? 0 : kGather ? expert_row(p, s) : s;
-    cp_async16(dst + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7), src + (in ? row * ld + col : 0),
-               in);
+    cp_async16(dst + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7),
+               src + (in ? static_cast<long long>(s) * ld + col : 0), in);
   }
 }
 
 template <ExpertProduct kWhat, bool kGather>
-__global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
+__host__ __device__ constexpr int pair_threads() {
+  return kPairThreads + (kGather ? 128 : 0) + (kWhat == ExpertProduct::kBackWeight ? 128 : 0);
+}
+
+template <ExpertProduct kWhat, bool kGather>
+__global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_pair_kernel(
     const __grid_constant__ PairParams P) {
   constexpr bool kFwd = kWhat == ExpertProduct::kForward;
   constexpr bool kBackX = kWhat == ExpertProduct::kBackInput;
@@ -184,11 +214,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = static_cast<int>(cluster_rank());
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  constexpr int kGatherWarp = 12, kSumWarp = kGather ? 16 : 12;   // first of four
+  const bool sums = kBackW && p.dbias != nullptr;
 
   if (tid == 0) {
     for (int s = 0; s < kPairStages; ++s) {
-      mbar_init(&sm.full[s], 2);    // one arrival (with its bytes) per CTA
-      mbar_init(&sm.empty[s], 1);
+      mbar_init(&sm.full[s], kGather ? 4 : 2);     // per CTA: the copies' (with their bytes), gathered rows
+      mbar_init(&sm.landed[s], 128);
+      mbar_init(&sm.empty[s], sums ? 4 : 1);       // the products', or the summing warps'
+      mbar_init(&sm.done[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&sm.tfull[a], 1);
@@ -247,67 +281,36 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
       const int f = g.f0 + rank * kPairM;             // this CTA's features
       const int half = kBackW ? kPairN / 2 : g.width / 2;
       const int b0 = g.i0 + rank * half;              // ... and its columns of the tile
-      int row[4] = {0, 0, 0, 0};
-      if constexpr (kGather && kFwd) {
-        // this lane's four rows of x; columns past the tile repeat its last slot
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          row[k] = expert_row(p, g.lo + min(b0 + 4 * lane + k, g.i0 + g.n - 1));
-      }
+      const uint32_t bytes = kPairABytes + (kGather ? 0 : half * kPairStep * 2);
 #pragma unroll 1
       for (int kt = 0; kt < steps; ++kt) {
         if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
         const uint32_t a = ring + s * kPairStageBytes, b = a + kPairABytes;
         const uint32_t full = dsmem_addr(smem_u32(&sm.full[s]), 0);
         const int c0 = kt * kPairStep;
-        if constexpr (kBackW) {
-          const int s0 = g.lo + c0;
-          if (s0 + kPairStep > g.hi) {
-            copy_partial<false>(p, a, p.dy, p.ldy, f, p.N, s0, g.hi);
-            copy_partial<kGather>(p, b, p.x, p.ldx, b0, p.K, s0, g.hi);
-            cp_async_wait_all();
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              fence_cluster();
-              mbar_arrive_cluster(full);
-            }
+        if (kBackW && g.lo + c0 + kPairStep > g.hi) {
+          copy_partial(a, p.dy, p.ldy, f, p.N, g.lo + c0, g.hi);
+          if constexpr (!kGather) copy_partial(b, p.x, p.ldx, b0, p.K, g.lo + c0, g.hi);
+          cp_async_wait_all();
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(full);
+        } else if (lane == 0) {
+          mbar_arrive_expect_tx_cluster(full, bytes);
+          if constexpr (kFwd) {
+            tma_load_3d_pair(a, &P.map_a, c0, f, g.e, full);
+          } else if constexpr (kBackX) {
+            tma_load_3d_pair(a, &P.map_a, f, c0, g.e, full);
+            tma_load_3d_pair(a + kPairBoxBytes, &P.map_a, f + 64, c0, g.e, full);
           } else {
-            if (lane == 0) {
-              mbar_arrive_expect_tx_cluster(full, kPairStageBytes);
-              tma_load_2d_pair(a, &P.map_a, f, s0, full);
-              tma_load_2d_pair(a + kPairBoxBytes, &P.map_a, f + 64, s0, full);
-            }
-            if constexpr (kGather) {
-              // lanes 0-15 the first 64 columns, four slots each, 16-31 the others
-              int r[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) r[k] = expert_row(p, s0 + 4 * (lane & 15) + k);
-              __syncwarp();
-              tma_gather4_pair(b + 512 * lane, &P.map_b, b0 + 64 * (lane >> 4), r[0], r[1], r[2], r[3],
-                               full);
-            } else if (lane == 0) {
-              tma_load_2d_pair(b, &P.map_b, b0, s0, full);
-              tma_load_2d_pair(b + kPairBoxBytes, &P.map_b, b0 + 64, s0, full);
-            }
+            tma_load_2d_pair(a, &P.map_a, f, g.lo + c0, full);
+            tma_load_2d_pair(a + kPairBoxBytes, &P.map_a, f + 64, g.lo + c0, full);
           }
-        } else {
-          const uint32_t b_bytes = half * kPairStep * 2;
-          if (lane == 0) {
-            mbar_arrive_expect_tx_cluster(full, kPairABytes + b_bytes);
-            if constexpr (kFwd) {
-              tma_load_3d_pair(a, &P.map_a, c0, f, g.e, full);
-            } else {
-              tma_load_3d_pair(a, &P.map_a, f, c0, g.e, full);
-              tma_load_3d_pair(a + kPairBoxBytes, &P.map_a, f + 64, c0, g.e, full);
-            }
-          }
-          if constexpr (kGather && kFwd) {
-            __syncwarp();
-            if (4 * lane < half)
-              tma_gather4_pair(b + 512 * lane, &P.map_b, c0, row[0], row[1], row[2], row[3], full);
-          } else if (lane == 0) {
-            if (half == kPairN / 2) {
+          if constexpr (!kGather) {
+            if constexpr (kBackW) {
+              tma_load_2d_pair(b, &P.map_b, b0, g.lo + c0, full);
+              tma_load_2d_pair(b + kPairBoxBytes, &P.map_b, b0 + 64, g.lo + c0, full);
+            } else if (half == kPairN / 2) {
               tma_load_2d_pair(b, &P.map_b, c0, g.lo + b0, full);
             } else {
               for (int q = 0; q < half; q += 32)
@@ -350,10 +353,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
 #pragma unroll 1
         for (int kt = 0; kt < steps; ++kt) {
           if (!(ok = mbar_wait_poll(&sm.full[s], use & 1, abort_flag))) break;
-          if (kBackW && g.lo + (kt + 1) * kPairStep > g.hi) {
-            // a partial stage was written by the copying warps of both CTAs
-            fence_cluster();
-            fence_proxy_async_smem();
+          if (kGather || (kBackW && g.lo + (kt + 1) * kPairStep > g.hi)) {
+            fence_proxy_async_smem();   // written by threads
           }
           tc_fence_after();
           const uint32_t at = ring + s * kPairStageBytes;
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
 #pragma unroll
           for (int k = 0; k < kPairStep / 16; ++k)
             umma_bf16_pair_lo(d, a + kStepA * k, b + kStepB * k, idesc, (kt | k) != 0);
-          umma_commit_pair(&sm.empty[s]);
+          umma_commit_pair(sums ? &sm.done[s] : &sm.empty[s]);
           if (++s == kPairStages) {
             s = 0;
             ++use;
@@ -373,10 +374,145 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
       }
     }
     __syncwarp();
-  } else {
+  } else if (kGather && warp >= kGatherWarp && warp < kGatherWarp + 4) {
+    // ------------------------------------------------------------- gathered rows
+    // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
+    // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
+    const int l = tid - 32 * kGatherWarp;
+    constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
+    const int c = l % kPieces, r0 = l / kPieces;
+    bool ok = true;
+    int s = 0, use = 0;
+    for (int t = pair; ok && t < tiles; t += pairs) {
+      pair_tile<kWhat>(p, sm, t, g);
+      const int steps = pair_steps<kWhat>(p, g);
+      const int half = kBackW ? kPairN / 2 : g.width / 2;
+      const int b0 = g.i0 + rank * half;
+      const uint16_t* src[8];
+      int row[2][8];   // of this stage and the next
+      if constexpr (kFwd) {
+        // columns past the tile repeat its last slot
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          src[i] = p.x + 8 * c +
+                   p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int at = g.lo + r0 + kRowStep * i;
+          row[0][i] = expert_row(p, min(at, p.M - 1));
+          row[1][i] = expert_row(p, min(at + kPairStep, p.M - 1));
+        }
+      }
+#pragma unroll 1
+      for (int kt = 0; kt < steps; ++kt) {
+        if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
+        const uint32_t b = ring + s * kPairStageBytes + kPairABytes;
+        const int c0 = kt * kPairStep;
+        if constexpr (kFwd) {
+          const bool in = c0 + 8 * c < p.K;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (r0 + kRowStep * i < half)
+              cp_async16(b + sw128_offset(r0 + kRowStep * i, c), src[i] + (in ? c0 : 0), in);
+        } else {
+          const int col = b0 + 8 * c;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + kRowStep * i;
+            const bool in = g.lo + c0 + r < g.hi && col < p.K;
+            cp_async16(b + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7),
+                       p.x + (in ? row[0][i] * p.ldx + col : 0), in);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            row[0][i] = row[1][i];
+            row[1][i] = expert_row(p, min(g.lo + c0 + 2 * kPairStep + r0 + kRowStep * i, p.M - 1));
+          }
+        }
+        cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
+        if (++s == kPairStages) {
+          s = 0;
+          ++use;
+        }
+      }
+    }
+    cp_async_wait_all();
+  } else if (kGather && warp == 2) {
+    // ------------------------------------------------------------- gathered rows handed over
+    // What threads write to shared memory is ordered before the products by the proxy
+    // fence.  Only the signal crosses to the even CTA: the rows are read where they lie,
+    // by their own CTA's tensor core, so nothing has to become visible outside the CTA
+    // (a release over the cluster for each stage takes twice the time: 69 us, not 35).
+    if (elect_one()) {
+      bool ok = true;
+      int s = 0, use = 0;
+      for (int t = pair; ok && t < tiles; t += pairs) {
+        pair_tile<kWhat>(p, sm, t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          if (!(ok = mbar_wait_poll(&sm.landed[s], use & 1, abort_flag))) break;
+          fence_proxy_async_smem();
+          mbar_arrive_cluster(dsmem_addr(smem_u32(&sm.full[s]), 0));
+          if (++s == kPairStages) {
+            s = 0;
+            ++use;
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (kBackW && warp >= kSumWarp) {
+    // ------------------------------------------------------------- bias sums
+    // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
+    // the 64 slots.
+    if (sums) {
+      const int l = tid - 32 * kSumWarp, w = l >> 5;
+      bool ok = true;   // no early exit: the four warps meet at every tile with a sum
+      int s = 0, use = 0;
+      for (int t = pair; t < tiles; t += pairs) {
+        pair_tile<kWhat>(p, sm, t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+        float a[4] = {};
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
+          if (ok && g.i0 == 0) {
+            const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint2 v = *reinterpret_cast<const uint2*>(at + sw128_offset(16 * w + i, (lane & 15) >> 1));
+              a[0] += bf_lo(v.x);
+              a[1] += bf_hi(v.x);
+              a[2] += bf_lo(v.y);
+              a[3] += bf_hi(v.y);
+            }
+          }
+          warp_arrive(&sm.empty[s]);
+          if (++s == kPairStages) {
+            s = 0;
+            ++use;
+          }
+        }
+        if (g.i0 == 0) {
+          float4& mine = *reinterpret_cast<float4*>(&sm.sums[w & 1][4 * lane]);
+          if (w >= 2) mine = make_float4(a[0], a[1], a[2], a[3]);
+          asm volatile("bar.sync 3, 128;" ::: "memory");
+          if (w < 2)
+            mine = make_float4(a[0] + mine.x, a[1] + mine.y, a[2] + mine.z, a[3] + mine.w);
+          asm volatile("bar.sync 3, 128;" ::: "memory");
+          const int n = g.f0 + rank * kPairM + l;
+          if (ok && n < p.N)
+            p.dbias[static_cast<size_t>(g.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
+          asm volatile("bar.sync 3, 128;" ::: "memory");
+        }
+      }
+    }
+  } else if (warp >= 4 && warp < 4 + kPairEpiWarps) {
     // ------------------------------------------------------------- write back
-    const int q = warp & 3, grp = (warp - 2) >> 2;
-    const int gt = tid - 64 - 128 * grp;               // thread of the group
+    const int q = warp & 3, grp = (warp - 4) >> 2;
+    const int gt = tid - 128 - 128 * grp;              // thread of the group
     uint8_t* const stg = base + kPairStages * kPairStageBytes + 2 * grp * kPairOutBytes;
     uint8_t* const stg2 = stg + kPairOutBytes;
     const uint32_t tempty0 = dsmem_addr(smem_u32(&sm.tempty[0]), 0);
@@ -398,6 +534,22 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
               if (n < p.N) bias[h][u] = __ldg(p.bias + static_cast<size_t>(g.e) * p.N + n);
             }
       }
+      // the values before GELU of this thread's pieces of a chunk, loaded two chunks
+      // ahead (in place, a chunk's latency was paid four times a tile: 34 us of 69)
+      uint4 z[2][4];
+      const auto load_pre = [&](uint4 (&to)[4], int c) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 8 * k + (gt >> 4), x = f + 8 * (gt & 15);
+          if (c + r < g.n && x < p.K)
+            to[k] = __ldg(reinterpret_cast<const uint4*>(
+                p.pre_in + (static_cast<size_t>(g.lo) + g.i0 + c + r) * p.K + x));
+        }
+      };
+      if (kBackX && p.pre_in != nullptr) {
+        load_pre(z[0], kPairChunk * grp);
+        load_pre(z[1], kPairChunk * (grp + 2));
+      }
       if (steps > 0) ok = ok && warp_wait(&sm.tfull[acc], (j >> 1) & 1, abort_flag);
       tc_fence_after();
       const uint32_t d = tm + acc * kPairN + (static_cast<uint32_t>(32 * q) << 16);
@@ -405,7 +557,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
         // rows are features, columns contiguous in memory
         const int rows = min(32, p.N - f - 32 * q);
         const uint32_t mask = !ok || rows <= 0 ? 0u : rows == 32 ? 0xffffffffu : (1u << rows) - 1u;
-        uint8_t* const mine = base + kPairStages * kPairStageBytes + (warp - 2) * 4096;
+        uint8_t* const mine = base + kPairStages * kPairStageBytes + (warp - 4) * 4096;
         const size_t row0 = (static_cast<size_t>(g.e) * p.N + f + 32 * q) * p.K + g.i0;
 #pragma unroll 1
         for (int c = kPairChunk * grp; mask != 0u && c < g.n; c += 2 * kPairChunk) {
@@ -470,61 +622,76 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
 #pragma unroll 1
         for (int c = kPairChunk * grp; c < g.n; c += 2 * kPairChunk) {
           if (kBackX && p.pre_in != nullptr) {
-            // the chunk of `pre`, so that its fragments match the accumulator's
+            // staged like the output, so that its fragments match the accumulator's
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int r = 8 * k + (gt >> 4), x = gt & 15;
-              uint4 o = make_uint4(0, 0, 0, 0);
-              if (c + r < g.n && f + 8 * x < width)
-                o = __ldg(reinterpret_cast<const uint4*>(p.pre_in + (slot0 + c + r) * width + f + 8 * x));
-              *reinterpret_cast<uint4*>(stg2 + piece(r, x)) = o;
+              *reinterpret_cast<uint4*>(stg2 + piece(8 * k + (gt >> 4), gt & 15)) = z[0][k];
+              z[0][k] = z[1][k];
             }
+            load_pre(z[1], c + 4 * kPairChunk);
             group_sync(grp);
           }
           float v[2][16];
           tmem_ld_frag32(d + c, v[0]);
           tmem_ld_frag32(d + c + (16u << 16), v[1]);
-          tmem_ld_wait();
+          // where this lane's row of fragment pair (h, b) is staged
+          const auto at = [&](int h, int b) {
+            return piece(8 * (b + (mi >> 1)) + (lane & 7), 4 * q + 2 * h + (mi & 1));
+          };
+          const auto store = [&](uint8_t* area) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < 4; b += 2) {
-              const int r = 8 * (b + (mi >> 1)) + (lane & 7), x = 4 * q + 2 * h + (mi & 1);
-              float* w = v[h] + 4 * b;
-              if constexpr (kFwd) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] += bias[h][(k >> 1) & 1];
-                if (p.pre != nullptr)
-                  stmatrix4_trans(smem_u32(stg2 + piece(r, x)), pack_bf16x2(w[0], w[1]),
-                                  pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
-                                  pack_bf16x2(w[6], w[7]));
-                if (p.gelu)
-#pragma unroll
-                  for (int k = 0; k < 8; ++k) w[k] = gelu(w[k]);
-              } else if (p.pre_in != nullptr) {
-                uint32_t z[4];
-                ldmatrix4_trans(smem_u32(stg2 + piece(r, x)), z);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  w[2 * k] *= gelu_slope(bf_lo(z[k]));
-                  w[2 * k + 1] *= gelu_slope(bf_hi(z[k]));
-                }
-              }
-              if (!p.out_f32) {
-                stmatrix4_trans(smem_u32(stg + piece(r, x)), pack_bf16x2(w[0], w[1]),
+              for (int b = 0; b < 4; b += 2) {
+                const float* w = v[h] + 4 * b;
+                stmatrix4_trans(smem_u32(area + at(h, b)), pack_bf16x2(w[0], w[1]),
                                 pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
                                 pack_bf16x2(w[6], w[7]));
-              } else if (ok) {
-                // eight lanes write 32 consecutive bytes of a slot
+              }
+          };
+          if constexpr (kFwd) {
+            tmem_ld_wait();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int k = 0; k < 16; ++k) v[h][k] += bias[h][(k >> 1) & 1];
+            if (p.pre != nullptr) store(stg2);
+            if (p.gelu)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 16; k += 2) gelu2(v[h][k], v[h][k + 1]);
+          } else {
+            uint32_t zf[2][2][4];
+            if (p.pre_in != nullptr)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int b = 0; b < 4; b += 2) ldmatrix4_trans(smem_u32(stg2 + at(h, b)), zf[h][b / 2]);
+            tmem_ld_wait();
+            if (p.pre_in != nullptr)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                  const int col = c + 8 * (b + (k >> 2)) + 2 * (lane & 3) + (k & 1);
-                  const int n = f + 32 * q + 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
-                  if (col < g.n && n < width)
-                    static_cast<float*>(p.out)[(slot0 + col) * width + n] = w[k];
+                  const uint32_t x = zf[h][k >> 2][k & 3];
+                  gelu_slope2(bf_lo(x), bf_hi(x), v[h][2 * k], v[h][2 * k + 1]);
                 }
+          }
+          if (!p.out_f32) {
+            store(stg);
+          } else if (ok) {
+            // eight lanes write 32 consecutive bytes of a slot
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                const int col = c + 8 * (k >> 2) + 2 * (lane & 3) + (k & 1);
+                const int n = f + 32 * q + 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
+                if (col < g.n && n < width)
+                  static_cast<float*>(p.out)[(slot0 + col) * width + n] = v[h][k];
               }
-            }
+          }
           group_sync(grp);
           if (ok) {
             if (!p.out_f32) flush(stg, static_cast<uint16_t*>(p.out), c);
@@ -551,43 +718,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) sc_expert_pair_kernel(
     tmem_dealloc_pair(tm, 512);
   }
   if (tid == 0 && sm.abort) atomicOr(p.status, kExpertTimeout);
-}
-
-// Bias gradient: the sum over an expert's slots of 64 columns of dy, in slot order
-// within each of 32 interleaved partial sums, those in order.
-constexpr int kBiasThreads = 256;
-__global__ void __launch_bounds__(kBiasThreads) sc_expert_bias_kernel(
-    const __grid_constant__ ExpertLinearParams p) {
-  __shared__ float red[32][64 + 4];
-  const int tid = threadIdx.x, c = tid & 7, r = tid >> 3;
-  const int col = blockIdx.x * 64 + 8 * c;
-  pdl_wait();
-  pdl_launch_dependents();
-  int lo, hi;
-  expert_range(p, blockIdx.y, lo, hi);
-  float a[8] = {};
-  if (col < p.N) {
-#pragma unroll 4
-    for (int s = lo + r; s < hi; s += 32) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p.dy + static_cast<long long>(s) * p.ldy + col));
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        a[2 * k] += bf_lo(w[k]);
-        a[2 * k + 1] += bf_hi(w[k]);
-      }
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 8; ++k) red[r][8 * c + k] = a[k];
-  __syncthreads();
-  const int n = blockIdx.x * 64 + tid;
-  if (tid < 64 && n < p.N) {
-    float s = 0.f;
-#pragma unroll
-    for (int k = 0; k < 32; ++k) s += red[k][tid];
-    p.dbias[static_cast<size_t>(blockIdx.y) * p.N + n] = s;
-  }
 }
 
 // ---------------------------------------------------------------------------
@@ -621,7 +751,7 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
   const long long pairs = most_tiles < sms / 2 ? most_tiles : sms / 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
-  cfg.blockDim = dim3(kPairThreads);
+  cfg.blockDim = dim3(pair_threads<kWhat, kGather>());
   cfg.dynamicSmemBytes = kPairDyn;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -645,8 +775,8 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
   bool ok;
   if (what == ExpertProduct::kForward) {
     ok = encode_rows(&P.map_a, p.w, p.N, p.K, p.K, p.E, kPairM) &&
-         encode_rows(&P.map_b, p.x, gather ? p.x_rows : p.M, p.K, p.ldx, 0, gather ? 1 : kPairN / 2) &&
-         (gather || encode_rows(&P.map_b32, p.x, p.M, p.K, p.ldx, 0, 32));
+         (gather || (encode_rows(&P.map_b, p.x, p.M, p.K, p.ldx, 0, kPairN / 2) &&
+                     encode_rows(&P.map_b32, p.x, p.M, p.K, p.ldx, 0, 32)));
     if (!ok) return cudaErrorInvalidValue;
     const long long tiles = slot_tiles * ((p.N + 255) / 256);
     return gather ? launch_pair<ExpertProduct::kForward, true>(P, tiles, st)
@@ -660,13 +790,11 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
     return launch_pair<ExpertProduct::kBackInput, false>(P, slot_tiles * ((p.K + 255) / 256), st);
   }
   ok = encode_rows(&P.map_a, p.dy, p.M, p.N, p.ldy, 0, kPairStep) &&
-       encode_rows(&P.map_b, p.x, gather ? p.x_rows : p.M, p.K, p.ldx, 0, gather ? 1 : kPairStep);
+       (gather || encode_rows(&P.map_b, p.x, p.M, p.K, p.ldx, 0, kPairStep));
   if (!ok) return cudaErrorInvalidValue;
   const long long tiles = static_cast<long long>(p.E) * ((p.N + 255) / 256) * ((p.K + kPairN - 1) / kPairN);
-  const cudaError_t e = gather ? launch_pair<ExpertProduct::kBackWeight, true>(P, tiles, st)
-                               : launch_pair<ExpertProduct::kBackWeight, false>(P, tiles, st);
-  if (e != cudaSuccess || p.dbias == nullptr) return e;
-  return launch_chained(sc_expert_bias_kernel, dim3((p.N + 63) / 64, p.E), dim3(kBiasThreads), 0, st, p);
+  return gather ? launch_pair<ExpertProduct::kBackWeight, true>(P, tiles, st)
+                : launch_pair<ExpertProduct::kBackWeight, false>(P, tiles, st);
 }
 
 cudaError_t configure_combine();

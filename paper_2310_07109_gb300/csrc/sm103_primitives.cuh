@@ -477,17 +477,13 @@ __device__ __forceinline__ void umma_commit_pair(uint64_t* bar) {
       : "memory");
 }
 
-// Arrivals on a barrier given by its address in the cluster's shared window.  They
-// order nothing this thread wrote itself for the other CTA (fence_cluster() does).
+// Arrivals on a barrier given by its address in the cluster's shared window.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_expect_tx_cluster(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
                : "memory");
-}
-__device__ __forceinline__ void fence_cluster() {
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
 }
 
 // Copies into this CTA's shared memory that complete on a barrier of either CTA of
@@ -617,6 +613,12 @@ __device__ __forceinline__ void cp_async16(uint32_t saddr, const void* gptr, boo
 
 __device__ __forceinline__ void cp_async_wait_all() {
   asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// Arrives on `bar` when this thread's cp_async16 copies so far have landed (one of the
+// arrivals that the barrier was set up for).
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
 // Hint: bring the 128-byte line holding `gptr` into L2.
