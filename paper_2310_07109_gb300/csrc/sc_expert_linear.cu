@@ -9,9 +9,10 @@
 // whose width follows what an expert has (64 to 256, evenly split over its tiles)
 // -- or, in the weight gradient, the contraction.  Persistent CTA pairs walk the
 // tiles that exist; every role counts them out from the offsets.
-//   warp 0      copies the operands, 64 of the contraction a stage, six stages
+//   warp 0      copies the operands, 64 of the contraction a stage, four or five stages
 //   warp 1      (even CTA) issues the products into one of two 256-column accumulators
-//   warps 4-11  read the other accumulator back
+//   warps 4-11  read the other accumulator back, 32 features x 32 columns at a time,
+//               through a staging area of the warp's own and tiled copies
 //   four warps more (rows of x gathered) copy these rows, 16 bytes a thread: four-row
 //               TMA gathers of 128-byte rows took 81 cycles each, 8 x 1024 rows x 2
 //               experts 768 -> 1536 99 us against 34 without the gather
@@ -37,27 +38,46 @@ constexpr int kPairEpiWarps = 8;     // two per tensor-memory lane quarter, ever
 constexpr int kPairM = 128;          // features per CTA, 256 per pair
 constexpr int kPairN = 256;          // widest tile on the other side; half of it per CTA
 constexpr int kPairStep = 64;        // contraction per stage: one 128-byte swizzle atom
-constexpr int kPairStages = 6;
+constexpr int kPairMaxStages = 5;
 constexpr int kPairChunk = 32;       // columns read back at a time
 constexpr uint32_t kPairABytes = kPairM * kPairStep * 2;
 constexpr uint32_t kPairBBytes = kPairN / 2 * kPairStep * 2;
 constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes;
 constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN-major operand
-// write-back staging: a 32 x 256-byte area per group of four warps
-constexpr uint32_t kPairOutBytes = 32 * 256;
-constexpr uint32_t kPairDyn = kPairStages * kPairStageBytes + 4 * kPairOutBytes + 1024;
+// Write-back areas per warp.  Forward, back (weight): two of 4 KB (32 x 32 in fp32, or
+// the output and the value before GELU in bf16), the copies of one on their way while
+// the other is filled.  Back (input): 4 KB for the output and a ring of three 2 KB
+// chunks of the value before GELU, copied ahead across tiles: behind the copies of the
+// operands a load waits 3000 cycles (loaded in place 69 us instead of 3x).
+constexpr int kPreSlots = 3;
+constexpr uint32_t kPreBytes = 2048;
+
+template <ExpertProduct kWhat>
+__host__ __device__ constexpr int pair_stages() {
+  return kWhat == ExpertProduct::kBackInput ? 4 : kPairMaxStages;
+}
+template <ExpertProduct kWhat>
+__host__ __device__ constexpr uint32_t pair_out_bytes() {
+  return kWhat == ExpertProduct::kBackInput ? 4096 + kPreSlots * kPreBytes : 8192;
+}
+template <ExpertProduct kWhat>
+__host__ __device__ constexpr uint32_t pair_dyn() {
+  return pair_stages<kWhat>() * kPairStageBytes + kPairEpiWarps * pair_out_bytes<kWhat>() + 1024;
+}
 
 struct PairParams {
   ExpertLinearParams p;
   CUtensorMap map_a;     // forward: W, 128 x 64; back (input): W, 64 x 64; back (weight): dy, 64 x 64
   CUtensorMap map_b;     // other side, not gathered: 128 x 64, back (weight) 64 x 64
   CUtensorMap map_b32;   // ... 32 x 64 (tiles narrower than 256)
+  CUtensorMap map_out;   // output, 32 x 32 boxes (128-byte swizzle in fp32, 64-byte in bf16)
+  CUtensorMap map_pre;   // forward: the value before GELU, likewise
 };
 
 struct PairSmem {
-  uint64_t full[kPairStages], empty[kPairStages];   // full: of the even CTA, both CTAs' copies
-  uint64_t done[kPairStages];                       // products done, the bias sums not yet
-  uint64_t landed[kPairStages];                     // this CTA's gathered rows
+  uint64_t full[kPairMaxStages], empty[kPairMaxStages];   // full: of the even CTA, both CTAs' copies
+  uint64_t done[kPairMaxStages];                       // products done, the bias sums not yet
+  uint64_t landed[kPairMaxStages];                     // this CTA's gathered rows
   uint64_t tfull[2], tempty[2];                     // tempty: of the even CTA
   uint32_t tmem_base;
   int abort;
@@ -67,7 +87,9 @@ struct PairSmem {
   };
 };
 
-static_assert(sizeof(PairSmem) + kPairDyn <= 227 * 1024, "one CTA's shared memory");
+static_assert(sizeof(PairSmem) + pair_dyn<ExpertProduct::kForward>() <= 227 * 1024 &&
+                  sizeof(PairSmem) + pair_dyn<ExpertProduct::kBackInput>() <= 227 * 1024,
+              "one CTA's shared memory");
 
 __device__ __forceinline__ float bf(uint16_t v) {
   return __uint_as_float(static_cast<uint32_t>(v) << 16);
@@ -84,12 +106,23 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// min(|x|, 16): the tail is 0 from there on, and a pair may share a reciprocal
+__device__ __forceinline__ uint64_t clamped_abs2(float x0, float x1) {
+  return f2_pack(fminf(fabsf(x0), 16.f), fminf(fabsf(x1), 16.f));
+}
+__device__ __forceinline__ float relu_nan(float x) {
+  float y;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x));
+  return y;
+}
 // q(t) t and e of |x|
 __device__ __forceinline__ void normal_tail2(uint64_t ax, uint64_t& qt, uint64_t& e) {
   float d0, d1, e0, e1;
-  f2_unpack(f2_fma(ax, f2_both(0.3275911f * 0.70710678118654752f), f2_both(1.f)), d0, d1);
+  const uint64_t d = f2_fma(ax, f2_both(0.3275911f * 0.70710678118654752f), f2_both(1.f));
+  f2_unpack(d, d0, d1);
   f2_unpack(f2_mul(f2_mul(ax, ax), f2_both(-0.5f * 1.44269504088896341f)), e0, e1);
-  const uint64_t t = f2_pack(rcp_approx(d0), rcp_approx(d1));
+  // 1 / d0 and 1 / d1 from one reciprocal (|x| is at most 16)
+  const uint64_t t = f2_mul(f2_pack(d1, d0), f2_both(rcp_approx(d0 * d1)));
   uint64_t q = f2_fma(f2_both(0.5307027145f), t, f2_both(-0.7265760135f));
   q = f2_fma(q, t, f2_both(0.7107068705f));
   q = f2_fma(q, t, f2_both(-0.142248368f));
@@ -99,22 +132,24 @@ __device__ __forceinline__ void normal_tail2(uint64_t ax, uint64_t& qt, uint64_t
 }
 // GELU(x) = max(x, 0) - |x| Phi(-|x|)
 __device__ __forceinline__ void gelu2(float& x0, float& x1) {
-  const uint64_t ax = f2_pack(fabsf(x0), fabsf(x1));
+  const uint64_t ax = clamped_abs2(x0, x1);
   uint64_t qt, e;
   normal_tail2(ax, qt, e);
-  f2_unpack(f2_fma(f2_mul(ax, f2_mul(qt, f2_both(-1.f))), e, f2_pack(fmaxf(x0, 0.f), fmaxf(x1, 0.f))),
-            x0, x1);
+  f2_unpack(f2_fma(f2_mul(ax, f2_mul(qt, f2_both(-1.f))), e, f2_pack(relu_nan(x0), relu_nan(x1))), x0, x1);
 }
 // y *= GELU'(x) = 1/2 + sign(x) (1/2 - Phi(-|x|) + |x| phi(x))
 __device__ __forceinline__ void gelu_slope2(float x0, float x1, float& y0, float& y1) {
-  const uint64_t ax = f2_pack(fabsf(x0), fabsf(x1));
+  const uint64_t ax = clamped_abs2(x0, x1);
   uint64_t qt, e;
   normal_tail2(ax, qt, e);
   float u0, u1;
   f2_unpack(f2_fma(f2_fma(ax, f2_both(0.3989422804014327f), f2_mul(qt, f2_both(-1.f))), e, f2_both(0.5f)),
             u0, u1);
-  y0 *= 0.5f + copysignf(u0, x0);
-  y1 *= 0.5f + copysignf(u1, x1);
+  // + 0 x: NaN where x is (or infinite, as x phi(x) is)
+  f2_unpack(f2_mul(f2_pack(y0, y1),
+                   f2_fma(f2_pack(x0, x1), f2_both(0.f),
+                          f2_add(f2_pack(copysignf(u0, x0), copysignf(u1, x1)), f2_both(0.5f)))),
+            y0, y1);
 }
 
 // One output tile of the pair: features f0 .. f0 + 256 of expert e, and slots
@@ -169,16 +204,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xffffffffu, mbar_wait_poll(bar, parity, abort));
 }
 
-// Four warps that share a staging area meet.
-__device__ __forceinline__ void group_sync(int g) {
-  asm volatile("bar.sync %0, 128;" ::"r"(1 + g) : "memory");
-}
-
-// Byte offset in a group's staging area of the 16-byte piece c (8 features) of column r.
-__device__ __forceinline__ uint32_t piece(int r, int c) {
-  return static_cast<uint32_t>(r * 256 + ((c ^ (r & 7)) << 4));
-}
-
 // The rows of a last, partial stage of the weight gradient: 64 slots x 128 columns of a
 // matrix into two 64 x 64 boxes, zeros past the expert's slots and the matrix's columns
 // (a product with what lies there would not be 0 for NaN), by the copying warp itself.
@@ -195,6 +220,30 @@ __device__ __forceinline__ void copy_partial(uint32_t dst, const uint16_t* src, 
   }
 }
 
+// A warp's staged chunk, 32 features of up to 32 slots (`left` of them in the tile), to
+// rows slot0 .. of a [.][width] output: one tiled copy, or, where the tile ends within
+// the chunk, the lanes' own stores of the slots that are there (the rows after it are
+// another expert's).
+template <bool kF32>
+__device__ __forceinline__ void put_chunk(const CUtensorMap& map, void* out, const uint8_t* from, int slot0,
+                                          int left, int f, int width, bool ok) {
+  const int lane = threadIdx.x & 31;
+  if (!ok || f >= width) return;
+  if (left >= kPairChunk) {
+    if (lane == 0) tma_store_2d(&map, f, slot0, smem_u32(from));
+    return;
+  }
+  constexpr int kPieces = kF32 ? 8 : 4, kPer = kF32 ? 4 : 8;   // 16-byte pieces a row, values a piece
+  const int x = lane % kPieces;
+#pragma unroll 1
+  for (int r = lane / kPieces; r < left; r += 32 / kPieces) {
+    if (f + kPer * x >= width) break;
+    const size_t at = static_cast<size_t>(slot0 + r) * width + f + kPer * x;
+    *reinterpret_cast<uint4*>(static_cast<uint8_t*>(out) + at * (kF32 ? 4 : 2)) =
+        *reinterpret_cast<const uint4*>(from + stage_offset<kPieces>(r, x));
+  }
+}
+
 template <ExpertProduct kWhat, bool kGather>
 __host__ __device__ constexpr int pair_threads() {
   return kPairThreads + (kGather ? 128 : 0) + (kWhat == ExpertProduct::kBackWeight ? 128 : 0);
@@ -206,6 +255,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   constexpr bool kFwd = kWhat == ExpertProduct::kForward;
   constexpr bool kBackX = kWhat == ExpertProduct::kBackInput;
   constexpr bool kBackW = kWhat == ExpertProduct::kBackWeight;
+  constexpr int kStages = pair_stages<kWhat>();
   const ExpertLinearParams& p = P.p;
   extern __shared__ uint8_t dyn_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) &
@@ -218,7 +268,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   const bool sums = kBackW && p.dbias != nullptr;
 
   if (tid == 0) {
-    for (int s = 0; s < kPairStages; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(&sm.full[s], kGather ? 4 : 2);     // per CTA: the copies' (with their bytes), gathered rows
       mbar_init(&sm.landed[s], 128);
       mbar_init(&sm.empty[s], sums ? 4 : 1);       // the products', or the summing warps'
@@ -319,7 +369,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           }
         }
         __syncwarp();
-        if (++s == kPairStages) {
+        if (++s == kStages) {
           s = 0;
           ++use;
         }
@@ -327,7 +377,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     }
     // every stage's products are done, and their arrivals have come, before this CTA ends
 #pragma unroll 1
-    for (int q = 0; q < kPairStages; ++q) {
+    for (int q = 0; q < kStages; ++q) {
       const int fills = use + (q < s ? 1 : 0);
       if (fills > 0) warp_wait(&sm.empty[q], (fills - 1) & 1, abort_flag);
     }
@@ -364,7 +414,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           for (int k = 0; k < kPairStep / 16; ++k)
             umma_bf16_pair_lo(d, a + kStepA * k, b + kStepB * k, idesc, (kt | k) != 0);
           umma_commit_pair(sums ? &sm.done[s] : &sm.empty[s]);
-          if (++s == kPairStages) {
+          if (++s == kStages) {
             s = 0;
             ++use;
           }
@@ -431,7 +481,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           }
         }
         cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
-        if (++s == kPairStages) {
+        if (++s == kStages) {
           s = 0;
           ++use;
         }
@@ -455,7 +505,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           if (!(ok = mbar_wait_poll(&sm.landed[s], use & 1, abort_flag))) break;
           fence_proxy_async_smem();
           mbar_arrive_cluster(dsmem_addr(smem_u32(&sm.full[s]), 0));
-          if (++s == kPairStages) {
+          if (++s == kStages) {
             s = 0;
             ++use;
           }
@@ -490,7 +540,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
             }
           }
           warp_arrive(&sm.empty[s]);
-          if (++s == kPairStages) {
+          if (++s == kStages) {
             s = 0;
             ++use;
           }
@@ -512,55 +562,86 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   } else if (warp >= 4 && warp < 4 + kPairEpiWarps) {
     // ------------------------------------------------------------- write back
     const int q = warp & 3, grp = (warp - 4) >> 2;
-    const int gt = tid - 128 - 128 * grp;              // thread of the group
-    uint8_t* const stg = base + kPairStages * kPairStageBytes + 2 * grp * kPairOutBytes;
-    uint8_t* const stg2 = stg + kPairOutBytes;
+    uint8_t* const stg = base + kStages * kPairStageBytes + (warp - 4) * pair_out_bytes<kWhat>();
+    uint8_t* const ring_pre = stg + 4096;
+    const int pr = lane >> 2, px = lane & 3;   // this lane's 16-byte piece of columns pr + 8 k
+    const int mi = lane >> 3;                  // fragment whose row address this lane gives
     const uint32_t tempty0 = dsmem_addr(smem_u32(&sm.tempty[0]), 0);
     bool ok = true;
-    int j = 0;
+    int j = 0, n_out = 0;
+    // the next chunk's area: no earlier copy reads it any more
+    const auto next_area = [&]() {
+      const bool one = kBackX && p.out_f32;
+      if (lane == 0) {
+        if (one) bulk_wait_read<0>();
+        else bulk_wait_read<1>();
+      }
+      __syncwarp();
+      return stg + (one ? 0 : (n_out++ & 1) * (kBackX ? 2048 : 4096));
+    };
+    // back (input): chunks of `pre` on their way
+    PairTile h;
+    h.e = h.n = 0;
+    int ht = pair - pairs, hc = 0, slot_in = 0, slot_out = 0;
+    const auto copy_pre = [&]() {
+      hc += 2 * kPairChunk;
+      while (ht < tiles && hc >= h.n) {
+        ht += pairs;
+        hc = kPairChunk * grp;
+        if (ht < tiles) pair_tile<kWhat>(p, sm, ht, h);
+      }
+      if (ht < tiles) {
+        const int x = h.f0 + rank * kPairM + 32 * q + 8 * px;
+        const uint32_t to = smem_u32(ring_pre + slot_in * kPreBytes);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 8 * k + pr;
+          const bool in = hc + r < h.n && x < p.K;
+          cp_async16(to + stage_offset<4>(r, px),
+                     p.pre_in + (in ? (static_cast<size_t>(h.lo) + h.i0 + hc + r) * p.K + x : 0), in);
+        }
+      }
+      cp_async_commit();
+      slot_in = slot_in + 1 == kPreSlots ? 0 : slot_in + 1;
+    };
+    if (kBackX && p.pre_in != nullptr)
+#pragma unroll 1
+      for (int i = 0; i < kPreSlots; ++i) copy_pre();
+    // forward: a tile's bias is loaded during the tile before
+    float bias[2][2] = {}, bias_next[2][2] = {};
+    const auto load_bias = [&](const PairTile& g1) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int n = g1.f0 + rank * kPairM + 32 * q + 16 * h + 8 * u + lane / 4;
+          if (n < p.N) bias_next[h][u] = __ldg(p.bias + static_cast<size_t>(g1.e) * p.N + n);
+        }
+    };
+    if (kFwd && p.bias != nullptr && pair < tiles) {
+      pair_tile<kWhat>(p, sm, pair, h);
+      load_bias(h);
+    }
     for (int t = pair; t < tiles; t += pairs) {
       pair_tile<kWhat>(p, sm, t, g);
       const int steps = pair_steps<kWhat>(p, g);
       const int acc = j & 1;
-      const int f = g.f0 + rank * kPairM;
-      float bias[2][2] = {};
-      if constexpr (kFwd) {
-        if (p.bias != nullptr)
+      const int f = g.f0 + rank * kPairM + 32 * q;   // this warp's features
+      if (kFwd && p.bias != nullptr) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int n = f + 32 * q + 16 * h + 8 * u + lane / 4;
-              if (n < p.N) bias[h][u] = __ldg(p.bias + static_cast<size_t>(g.e) * p.N + n);
-            }
-      }
-      // the values before GELU of this thread's pieces of a chunk, loaded two chunks
-      // ahead (in place, a chunk's latency was paid four times a tile: 34 us of 69)
-      uint4 z[2][4];
-      const auto load_pre = [&](uint4 (&to)[4], int c) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int r = 8 * k + (gt >> 4), x = f + 8 * (gt & 15);
-          if (c + r < g.n && x < p.K)
-            to[k] = __ldg(reinterpret_cast<const uint4*>(
-                p.pre_in + (static_cast<size_t>(g.lo) + g.i0 + c + r) * p.K + x));
+        for (int h = 0; h < 2; ++h) bias[h][0] = bias_next[h][0], bias[h][1] = bias_next[h][1];
+        if (t + pairs < tiles) {
+          pair_tile<kWhat>(p, sm, t + pairs, h);
+          load_bias(h);
         }
-      };
-      if (kBackX && p.pre_in != nullptr) {
-        load_pre(z[0], kPairChunk * grp);
-        load_pre(z[1], kPairChunk * (grp + 2));
       }
       if (steps > 0) ok = ok && warp_wait(&sm.tfull[acc], (j >> 1) & 1, abort_flag);
       tc_fence_after();
       const uint32_t d = tm + acc * kPairN + (static_cast<uint32_t>(32 * q) << 16);
       if constexpr (kBackW) {
         // rows are features, columns contiguous in memory
-        const int rows = min(32, p.N - f - 32 * q);
-        const uint32_t mask = !ok || rows <= 0 ? 0u : rows == 32 ? 0xffffffffu : (1u << rows) - 1u;
-        uint8_t* const mine = base + kPairStages * kPairStageBytes + (warp - 4) * 4096;
-        const size_t row0 = (static_cast<size_t>(g.e) * p.N + f + 32 * q) * p.K + g.i0;
 #pragma unroll 1
-        for (int c = kPairChunk * grp; mask != 0u && c < g.n; c += 2 * kPairChunk) {
+        for (int c = kPairChunk * grp; ok && f < p.N && c < g.n; c += 2 * kPairChunk) {
           float v[32];
           if (steps > 0) {
             tmem_ld32(d + c, v);
@@ -569,74 +650,40 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
 #pragma unroll
             for (int k = 0; k < 32; ++k) v[k] = 0.f;   // an expert without slots
           }
-          const int here = min(kPairChunk, g.n - c);    // multiple of 8
+          uint8_t* const to = next_area();
           if (p.out_f32) {
 #pragma unroll
             for (int k = 0; k < 32; k += 4)
-              stage_row_piece<8>(mine, k / 4,
+              stage_row_piece<8>(to, k / 4,
                                  make_uint4(__float_as_uint(v[k]), __float_as_uint(v[k + 1]),
                                             __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3])));
-            __syncwarp();
-            float* out = static_cast<float*>(p.out) + row0 + c;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int r = 4 * k + lane / 8, x = lane & 7;
-              const uint4 o = *reinterpret_cast<const uint4*>(mine + stage_offset<8>(r, x));
-              if (((mask >> r) & 1u) && 4 * x < here)
-                *reinterpret_cast<uint4*>(out + static_cast<size_t>(r) * p.K + 4 * x) = o;
-            }
           } else {
 #pragma unroll
             for (int k = 0; k < 32; k += 8)
-              stage_row_piece<4>(mine, k / 8,
+              stage_row_piece<4>(to, k / 8,
                                  make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
                                             pack_bf16x2(v[k + 4], v[k + 5]),
                                             pack_bf16x2(v[k + 6], v[k + 7])));
-            __syncwarp();
-            uint16_t* out = static_cast<uint16_t*>(p.out) + row0 + c;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int r = 8 * k + lane / 4, x = lane & 3;
-              const uint4 o = *reinterpret_cast<const uint4*>(mine + stage_offset<4>(r, x));
-              if (((mask >> r) & 1u) && 8 * x < here)
-                *reinterpret_cast<uint4*>(out + static_cast<size_t>(r) * p.K + 8 * x) = o;
-            }
           }
+          fence_proxy_async_smem();
           __syncwarp();
+          if (lane == 0) {
+            tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(to));   // cut at N and K
+            bulk_commit();
+          }
         }
       } else {
         // rows are features, columns slots: transposed on the way out
         const int width = features<kWhat>(p);
-        const size_t slot0 = static_cast<size_t>(g.lo) + g.i0;
-        // the group's 32 columns x 128 features of a staged chunk, 16 bytes a thread
-        const auto flush = [&](const uint8_t* from, uint16_t* to, int c) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int r = 8 * k + (gt >> 4), x = gt & 15;
-            const uint4 o = *reinterpret_cast<const uint4*>(from + piece(r, x));
-            if (c + r < g.n && f + 8 * x < width)
-              *reinterpret_cast<uint4*>(to + (slot0 + c + r) * width + f + 8 * x) = o;
-          }
-        };
-        const int mi = lane >> 3;   // fragment whose row address this lane gives
+        const int slot0 = g.lo + g.i0;
 #pragma unroll 1
         for (int c = kPairChunk * grp; c < g.n; c += 2 * kPairChunk) {
-          if (kBackX && p.pre_in != nullptr) {
-            // staged like the output, so that its fragments match the accumulator's
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              *reinterpret_cast<uint4*>(stg2 + piece(8 * k + (gt >> 4), gt & 15)) = z[0][k];
-              z[0][k] = z[1][k];
-            }
-            load_pre(z[1], c + 4 * kPairChunk);
-            group_sync(grp);
-          }
           float v[2][16];
           tmem_ld_frag32(d + c, v[0]);
           tmem_ld_frag32(d + c + (16u << 16), v[1]);
           // where this lane's row of fragment pair (h, b) is staged
           const auto at = [&](int h, int b) {
-            return piece(8 * (b + (mi >> 1)) + (lane & 7), 4 * q + 2 * h + (mi & 1));
+            return stage_offset<4>(8 * (b + (mi >> 1)) + (lane & 7), 2 * h + (mi & 1));
           };
           const auto store = [&](uint8_t* area) {
 #pragma unroll
@@ -649,55 +696,78 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
                                 pack_bf16x2(w[6], w[7]));
               }
           };
-          if constexpr (kFwd) {
+          if (kBackX && p.pre_in != nullptr) {
+            // in the staging's layout, so that its fragments match the accumulator's
+            uint32_t zf[2][2][4];
+            cp_async_wait<kPreSlots - 1>();
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int b = 0; b < 4; b += 2)
+                ldmatrix4_trans(smem_u32(ring_pre + slot_out * kPreBytes + at(h, b)), zf[h][b / 2]);
+            __syncwarp();
+            slot_out = slot_out + 1 == kPreSlots ? 0 : slot_out + 1;
+            copy_pre();
             tmem_ld_wait();
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const uint32_t x = zf[h][k >> 2][k & 3];
+                gelu_slope2(bf_lo(x), bf_hi(x), v[h][2 * k], v[h][2 * k + 1]);
+              }
+          } else {
+            tmem_ld_wait();
+          }
+          if constexpr (kFwd) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
               for (int k = 0; k < 16; ++k) v[h][k] += bias[h][(k >> 1) & 1];
-            if (p.pre != nullptr) store(stg2);
+          }
+          uint8_t* const to = next_area();
+          if constexpr (kFwd) {
+            if (p.pre != nullptr) store(to + (p.out_f32 ? 0 : 2048));
+            if (p.pre != nullptr && p.out_f32) {
+              // no room for both: the value before GELU leaves first
+              fence_proxy_async_smem();
+              __syncwarp();
+              put_chunk<false>(P.map_pre, p.pre, to, slot0 + c, g.n - c, f, width, ok);
+              if (lane == 0) {
+                bulk_commit();
+                bulk_wait_read<0>();
+              }
+              __syncwarp();
+            }
             if (p.gelu)
 #pragma unroll
               for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int k = 0; k < 16; k += 2) gelu2(v[h][k], v[h][k + 1]);
-          } else {
-            uint32_t zf[2][2][4];
-            if (p.pre_in != nullptr)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int b = 0; b < 4; b += 2) ldmatrix4_trans(smem_u32(stg2 + at(h, b)), zf[h][b / 2]);
-            tmem_ld_wait();
-            if (p.pre_in != nullptr)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const uint32_t x = zf[h][k >> 2][k & 3];
-                  gelu_slope2(bf_lo(x), bf_hi(x), v[h][2 * k], v[h][2 * k + 1]);
-                }
           }
-          if (!p.out_f32) {
-            store(stg);
-          } else if (ok) {
-            // eight lanes write 32 consecutive bytes of a slot
+          if (p.out_f32) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
               for (int k = 0; k < 16; ++k) {
-                const int col = c + 8 * (k >> 2) + 2 * (lane & 3) + (k & 1);
-                const int n = f + 32 * q + 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
-                if (col < g.n && n < width)
-                  static_cast<float*>(p.out)[(slot0 + col) * width + n] = v[h][k];
+                const int r = 8 * (k >> 2) + 2 * (lane & 3) + (k & 1);
+                const int n = 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
+                *reinterpret_cast<float*>(to + stage_offset<8>(r, n >> 2) + 4 * (n & 3)) = v[h][k];
               }
+          } else {
+            store(to);
           }
-          group_sync(grp);
-          if (ok) {
-            if (!p.out_f32) flush(stg, static_cast<uint16_t*>(p.out), c);
-            if (kFwd && p.pre != nullptr) flush(stg2, p.pre, c);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (p.out_f32) {
+            put_chunk<true>(P.map_out, p.out, to, slot0 + c, g.n - c, f, width, ok);
+          } else {
+            put_chunk<false>(P.map_out, p.out, to, slot0 + c, g.n - c, f, width, ok);
+            if (kFwd && p.pre != nullptr)
+              put_chunk<false>(P.map_pre, p.pre, to + 2048, slot0 + c, g.n - c, f, width, ok);
           }
-          group_sync(grp);   // the staging areas may be written again
+          if (lane == 0) bulk_commit();
         }
       }
       if (steps > 0) {
@@ -708,6 +778,8 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
         ++j;
       }
     }
+    if (lane == 0) bulk_wait_all();
+    if (kBackX) cp_async_wait_all();
   }
 
   tc_fence_before();
@@ -739,6 +811,21 @@ static bool encode_rows(CUtensorMap* m, const void* base, long long rows, int co
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// An output of rows x cols (x experts), in boxes of 32 x 32.
+static bool encode_out(CUtensorMap* m, void* base, bool f32, long long rows, int cols, int experts) {
+  const auto enc = api_tensor_map_encoder();
+  if (!enc) return false;
+  const cuuint64_t dim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
+                             static_cast<cuuint64_t>(experts > 0 ? experts : 1)};
+  const cuuint64_t row = static_cast<cuuint64_t>(cols) * (f32 ? 4 : 2);
+  const cuuint64_t stride[2] = {row, row * static_cast<cuuint64_t>(rows)};
+  const cuuint32_t box[3] = {32u, 32u, 1u}, one[3] = {1u, 1u, 1u};
+  return enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+             experts > 0 ? 3 : 2, base, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
   static int sms = 0;
@@ -752,7 +839,7 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
   cfg.blockDim = dim3(pair_threads<kWhat, kGather>());
-  cfg.dynamicSmemBytes = kPairDyn;
+  cfg.dynamicSmemBytes = pair_dyn<kWhat>();
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -776,7 +863,9 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
   if (what == ExpertProduct::kForward) {
     ok = encode_rows(&P.map_a, p.w, p.N, p.K, p.K, p.E, kPairM) &&
          (gather || (encode_rows(&P.map_b, p.x, p.M, p.K, p.ldx, 0, kPairN / 2) &&
-                     encode_rows(&P.map_b32, p.x, p.M, p.K, p.ldx, 0, 32)));
+                     encode_rows(&P.map_b32, p.x, p.M, p.K, p.ldx, 0, 32))) &&
+         encode_out(&P.map_out, p.out, p.out_f32, p.M, p.N, 0) &&
+         (p.pre == nullptr || encode_out(&P.map_pre, p.pre, false, p.M, p.N, 0));
     if (!ok) return cudaErrorInvalidValue;
     const long long tiles = slot_tiles * ((p.N + 255) / 256);
     return gather ? launch_pair<ExpertProduct::kForward, true>(P, tiles, st)
@@ -785,12 +874,14 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
   if (what == ExpertProduct::kBackInput) {
     ok = encode_rows(&P.map_a, p.w, p.N, p.K, p.K, p.E, kPairStep) &&
          encode_rows(&P.map_b, p.dy, p.M, p.N, p.ldy, 0, kPairN / 2) &&
-         encode_rows(&P.map_b32, p.dy, p.M, p.N, p.ldy, 0, 32);
+         encode_rows(&P.map_b32, p.dy, p.M, p.N, p.ldy, 0, 32) &&
+         encode_out(&P.map_out, p.out, p.out_f32, p.M, p.K, 0);
     if (!ok) return cudaErrorInvalidValue;
     return launch_pair<ExpertProduct::kBackInput, false>(P, slot_tiles * ((p.K + 255) / 256), st);
   }
   ok = encode_rows(&P.map_a, p.dy, p.M, p.N, p.ldy, 0, kPairStep) &&
-       (gather || encode_rows(&P.map_b, p.x, p.M, p.K, p.ldx, 0, kPairStep));
+       (gather || encode_rows(&P.map_b, p.x, p.M, p.K, p.ldx, 0, kPairStep)) &&
+       encode_out(&P.map_out, p.out, p.out_f32, p.N, p.K, p.E);
   if (!ok) return cudaErrorInvalidValue;
   const long long tiles = static_cast<long long>(p.E) * ((p.N + 255) / 256) * ((p.K + kPairN - 1) / kPairN);
   return gather ? launch_pair<ExpertProduct::kBackWeight, true>(P, tiles, st)
@@ -799,15 +890,20 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
 
 cudaError_t configure_combine();
 
+template <ExpertProduct kWhat, bool kGather>
+static cudaError_t configure_pair() {
+  return cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(pair_dyn<kWhat>()));
+}
+
 cudaError_t configure_expert() {
-  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  const int bytes = static_cast<int>(kPairDyn);
   cudaError_t e = configure_combine();
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kForward, false>, attr, bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kForward, true>, attr, bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kBackInput, false>, attr, bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kBackWeight, false>, attr, bytes);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(sc_expert_pair_kernel<ExpertProduct::kBackWeight, true>, attr, bytes);
+  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kForward, false>();
+  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kForward, true>();
+  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackInput, false>();
+  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackWeight, false>();
+  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackWeight, true>();
   return e;
 }
 
