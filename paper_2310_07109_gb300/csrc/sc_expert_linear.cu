@@ -85,6 +85,7 @@ struct PairSmem {
     int tile0[kMaxExperts + 1];   // forward, back (input): tiles of slots of the experts before
     alignas(16) float sums[2][kPairM];   // weight gradient: bias sums of two warps each
   };
+  uint8_t order[kMaxExperts];   // weight gradient: experts by decreasing number of slots
 };
 
 static_assert(sizeof(PairSmem) + pair_dyn<ExpertProduct::kForward>() <= 227 * 1024 &&
@@ -97,9 +98,12 @@ __device__ __forceinline__ float bf(uint16_t v) {
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
-// GELU and its slope with the normal distribution's lower tail Phi(-|x|) = q(t) e,
-// e = exp(-x^2 / 2), t = 1 / (1 + p |x| / sqrt 2), by Abramowitz & Stegun 7.1.26 (erf,
-// |error| <= 1.5e-7), in packed pairs: the read-back warps bound products with GELU.
+// GELU and its slope from the normal distribution's lower tail Phi(-|x|), in packed
+// pairs: the read-back warps bound products with GELU.  GELU: by Abramowitz & Stegun
+// 7.1.28, 1 / (2 (1 + a1 z + .. + a6 z^6)^16), z = |x| / sqrt 2 (erf, |error| <= 3e-7):
+// half an operation of the transcendental unit a value, which paced 7.1.26 with two.
+// The slope needs exp(-x^2 / 2) too, so there 7.1.26 (|error| <= 1.5e-7): q(t) exp(-x^2 / 2),
+// t = 1 / (1 + p z).
 __device__ __forceinline__ uint64_t f2_both(float x) { return f2_pack(x, x); }
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
@@ -133,9 +137,21 @@ __device__ __forceinline__ void normal_tail2(uint64_t ax, uint64_t& qt, uint64_t
 // GELU(x) = max(x, 0) - |x| Phi(-|x|)
 __device__ __forceinline__ void gelu2(float& x0, float& x1) {
   const uint64_t ax = clamped_abs2(x0, x1);
-  uint64_t qt, e;
-  normal_tail2(ax, qt, e);
-  f2_unpack(f2_fma(f2_mul(ax, f2_mul(qt, f2_both(-1.f))), e, f2_pack(relu_nan(x0), relu_nan(x1))), x0, x1);
+  // the coefficients times 2^(-i/2)
+  uint64_t d = f2_fma(ax, f2_both(0.0000430638f * 0.125f), f2_both(0.0002765672f * 0.17677669529663688f));
+  d = f2_fma(d, ax, f2_both(0.0001520143f * 0.25f));
+  d = f2_fma(d, ax, f2_both(0.0092705272f * 0.35355339059327376f));
+  d = f2_fma(d, ax, f2_both(0.0422820123f * 0.5f));
+  d = f2_fma(d, ax, f2_both(0.0705230784f * 0.70710678118654752f));
+  d = f2_fma(d, ax, f2_both(1.f));
+  d = f2_mul(d, d);
+  d = f2_mul(d, d);
+  d = f2_mul(d, d);
+  d = f2_mul(d, d);   // at most 3e34: where the product of two overflows, both tails are 0
+  float d0, d1;
+  f2_unpack(d, d0, d1);
+  const uint64_t h = f2_mul(f2_mul(ax, f2_both(-0.5f * rcp_approx(d0 * d1))), f2_pack(d1, d0));
+  f2_unpack(f2_add(h, f2_pack(relu_nan(x0), relu_nan(x1))), x0, x1);
 }
 // y *= GELU'(x) = 1/2 + sign(x) (1/2 - Phi(-|x|) + |x| phi(x))
 __device__ __forceinline__ void gelu_slope2(float x0, float x1, float& y0, float& y1) {
@@ -159,7 +175,10 @@ struct PairTile {
   int e, lo, hi, f0, i0, n, width;
 };
 
-// Slots of a tile of an expert with n slots: evenly split, multiples of 64.
+// Slots of a tile of an expert with n slots: evenly split, multiples of 64.  As wide as
+// they go: the L2's rate to the SMs bounds long products (32 KB a stage and SM at about
+// 54 bytes a cycle, 600 cycles where the products take 512), so narrower tiles lose more
+// by copying the weights again than they win by evener rounds (96 columns: 81 us, not 34).
 __device__ __forceinline__ int tile_slots(int n) {
   const int tiles = (n + kPairN - 1) / kPairN;
   return tiles == 0 ? 64 : ((n + tiles - 1) / tiles + 63) & ~63;
@@ -178,9 +197,9 @@ __device__ __forceinline__ void pair_tile(const ExpertLinearParams& p, const Pai
   const int rest = t / tiles_f;
   g.f0 = (t - rest * tiles_f) * 256;
   if constexpr (kWhat == ExpertProduct::kBackWeight) {
-    const int tiles_k = (p.K + kPairN - 1) / kPairN;
-    g.e = rest / tiles_k;
-    g.i0 = (rest - g.e * tiles_k) * kPairN;
+    const int tiles_k = (p.K + kPairN - 1) / kPairN, o = rest / tiles_k;
+    g.e = sm.order[o];
+    g.i0 = (rest - o * tiles_k) * kPairN;
     expert_range(p, g.e, g.lo, g.hi);
     g.n = min(kPairN, p.K - g.i0);
   } else {
@@ -191,6 +210,16 @@ __device__ __forceinline__ void pair_tile(const ExpertLinearParams& p, const Pai
     g.n = min(w, g.hi - g.lo - g.i0);
   }
   g.width = (g.n + 63) & ~63;
+}
+
+// The tile a pair takes after tile t.  Weight gradient: its tiles come by decreasing
+// contraction, so the pairs take them in turn there and back (8 experts of 1002 to 3884
+// slots, two tiles a pair: the longest pair has 76 steps instead of 98, the mean is 61).
+template <ExpertProduct kWhat>
+__device__ __forceinline__ int next_tile(int t, int pair, int pairs) {
+  if constexpr (kWhat != ExpertProduct::kBackWeight) return t + pairs;
+  const bool there = t % pairs == pair && (t / pairs) % 2 == 0;
+  return t - t % pairs + pairs + (there ? pairs - 1 - pair : pair);
 }
 
 template <ExpertProduct kWhat>
@@ -309,6 +338,19 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       if (lane == 0) sm.tile0[0] = 0;
     }
   }
+  if constexpr (kBackW) {
+    // ranks by (slots, expert)
+    for (int e = tid; e < p.E; e += blockDim.x) {
+      int lo, hi, rank_e = 0;
+      expert_range(p, e, lo, hi);
+      const int n = hi - lo;
+      for (int o = 0; o < p.E; ++o) {
+        expert_range(p, o, lo, hi);
+        rank_e += hi - lo > n || (hi - lo == n && o < e);
+      }
+      sm.order[rank_e] = static_cast<uint8_t>(e);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   cluster_sync();   // the other CTA's barriers are set up
@@ -325,7 +367,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     // ------------------------------------------------------------- copies
     bool ok = true;
     int s = 0, use = 0;
-    for (int t = pair; ok && t < tiles; t += pairs) {
+    for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
       pair_tile<kWhat>(p, sm, t, g);
       const int steps = pair_steps<kWhat>(p, g);
       const int f = g.f0 + rank * kPairM;             // this CTA's features
@@ -386,7 +428,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     if (rank == 0 && elect_one()) {
       bool ok = true;
       int s = 0, use = 0, j = 0;
-      for (int t = pair; ok && t < tiles; t += pairs) {
+      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
         pair_tile<kWhat>(p, sm, t, g);
         const int steps = pair_steps<kWhat>(p, g);
         if (steps == 0) continue;
@@ -433,7 +475,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     const int c = l % kPieces, r0 = l / kPieces;
     bool ok = true;
     int s = 0, use = 0;
-    for (int t = pair; ok && t < tiles; t += pairs) {
+    for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
       pair_tile<kWhat>(p, sm, t, g);
       const int steps = pair_steps<kWhat>(p, g);
       const int half = kBackW ? kPairN / 2 : g.width / 2;
@@ -497,7 +539,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     if (elect_one()) {
       bool ok = true;
       int s = 0, use = 0;
-      for (int t = pair; ok && t < tiles; t += pairs) {
+      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
         pair_tile<kWhat>(p, sm, t, g);
         const int steps = pair_steps<kWhat>(p, g);
 #pragma unroll 1
@@ -521,7 +563,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       const int l = tid - 32 * kSumWarp, w = l >> 5;
       bool ok = true;   // no early exit: the four warps meet at every tile with a sum
       int s = 0, use = 0;
-      for (int t = pair; t < tiles; t += pairs) {
+      for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
         pair_tile<kWhat>(p, sm, t, g);
         const int steps = pair_steps<kWhat>(p, g);
         float a[4] = {};
@@ -622,7 +664,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       pair_tile<kWhat>(p, sm, pair, h);
       load_bias(h);
     }
-    for (int t = pair; t < tiles; t += pairs) {
+    for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
       pair_tile<kWhat>(p, sm, t, g);
       const int steps = pair_steps<kWhat>(p, g);
       const int acc = j & 1;
