@@ -11,8 +11,10 @@
 // tiles that exist; every role counts them out from the offsets.
 //   warp 0      copies the operands, 64 of the contraction a stage, four or five stages
 //   warp 1      (even CTA) issues the products into one of two 256-column accumulators
-//   warps 4-11  read the other accumulator back, 32 features x 32 columns at a time,
-//               through a staging area of the warp's own and tiled copies
+//   16 warps    (weight gradient: eight) read the other accumulator back, 32 features x
+//               32 columns at a time, through a staging area of the warp's own and tiled
+//               copies.  Each chunk is a chain of short waits, so the more warps the
+//               better hidden: with eight, GELU cost 7 us of 41
 //   four warps more (rows of x gathered) copy these rows, 16 bytes a thread: four-row
 //               TMA gathers of 128-byte rows took 81 cycles each, 8 x 1024 rows x 2
 //               experts 768 -> 1536 99 us against 34 without the gather
@@ -33,8 +35,6 @@ namespace sc {
 
 PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder();
 
-constexpr int kPairThreads = 384;    // without the gathering and the summing warps
-constexpr int kPairEpiWarps = 8;     // two per tensor-memory lane quarter, every other chunk
 constexpr int kPairM = 128;          // features per CTA, 256 per pair
 constexpr int kPairN = 256;          // widest tile on the other side; half of it per CTA
 constexpr int kPairStep = 64;        // contraction per stage: one 128-byte swizzle atom
@@ -44,25 +44,28 @@ constexpr uint32_t kPairABytes = kPairM * kPairStep * 2;
 constexpr uint32_t kPairBBytes = kPairN / 2 * kPairStep * 2;
 constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes;
 constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN-major operand
-// Write-back areas per warp.  Forward, back (weight): two of 4 KB (32 x 32 in fp32, or
-// the output and the value before GELU in bf16), the copies of one on their way while
-// the other is filled.  Back (input): 4 KB for the output and a ring of three 2 KB
-// chunks of the value before GELU, copied ahead across tiles: behind the copies of the
-// operands a load waits 3000 cycles (loaded in place 69 us instead of 3x).
-constexpr int kPreSlots = 3;
+// Write-back areas per warp.  Forward: 4 KB, a chunk in fp32, or the output and the value
+// before GELU in bf16.  Back (weight): two of these, the copy of one on its way while the
+// other is filled.  Back (input): 2 KB for the output (fp32: 4) and a ring of two 2 KB
+// chunks (fp32: one) of the value before GELU, copied ahead across tiles: behind the
+// copies of the operands a load waits 3000 cycles.
 constexpr uint32_t kPreBytes = 2048;
 
+template <ExpertProduct kWhat>
+__host__ __device__ constexpr int pair_epi_warps() {
+  return kWhat == ExpertProduct::kBackWeight ? 8 : 16;
+}
 template <ExpertProduct kWhat>
 __host__ __device__ constexpr int pair_stages() {
   return kWhat == ExpertProduct::kBackInput ? 4 : kPairMaxStages;
 }
 template <ExpertProduct kWhat>
 __host__ __device__ constexpr uint32_t pair_out_bytes() {
-  return kWhat == ExpertProduct::kBackInput ? 4096 + kPreSlots * kPreBytes : 8192;
+  return kWhat == ExpertProduct::kBackInput ? 6144 : kWhat == ExpertProduct::kForward ? 4096 : 8192;
 }
 template <ExpertProduct kWhat>
 __host__ __device__ constexpr uint32_t pair_dyn() {
-  return pair_stages<kWhat>() * kPairStageBytes + kPairEpiWarps * pair_out_bytes<kWhat>() + 1024;
+  return pair_stages<kWhat>() * kPairStageBytes + pair_epi_warps<kWhat>() * pair_out_bytes<kWhat>() + 1024;
 }
 
 struct PairParams {
@@ -275,7 +278,8 @@ __device__ __forceinline__ void put_chunk(const CUtensorMap& map, void* out, con
 
 template <ExpertProduct kWhat, bool kGather>
 __host__ __device__ constexpr int pair_threads() {
-  return kPairThreads + (kGather ? 128 : 0) + (kWhat == ExpertProduct::kBackWeight ? 128 : 0);
+  return 128 + 32 * pair_epi_warps<kWhat>() + (kGather ? 128 : 0) +
+         (kWhat == ExpertProduct::kBackWeight ? 128 : 0);
 }
 
 template <ExpertProduct kWhat, bool kGather>
@@ -293,7 +297,8 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = static_cast<int>(cluster_rank());
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  constexpr int kGatherWarp = 12, kSumWarp = kGather ? 16 : 12;   // first of four
+  constexpr int kEpiWarps = pair_epi_warps<kWhat>(), kGroups = kEpiWarps / 4;
+  constexpr int kGatherWarp = 4 + kEpiWarps, kSumWarp = kGatherWarp + (kGather ? 4 : 0);   // first of four
   const bool sums = kBackW && p.dbias != nullptr;
 
   if (tid == 0) {
@@ -305,7 +310,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&sm.tfull[a], 1);
-      mbar_init(&sm.tempty[a], 2 * kPairEpiWarps);
+      mbar_init(&sm.tempty[a], 2 * kEpiWarps);
     }
     sm.abort = 0;
     fence_mbar_init();
@@ -481,7 +486,17 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       const int half = kBackW ? kPairN / 2 : g.width / 2;
       const int b0 = g.i0 + rank * half;
       const uint16_t* src[8];
-      int row[2][8];   // of this stage and the next
+      // weight gradient: the 16 rows that this warp copies of each of eight stages, two
+      // stages a register; those of the eight after them are loaded meanwhile (a load
+      // waits up to 3000 cycles behind the operands: two stages ahead 62 us, not 41)
+      int row[4], row_next[4];
+      const auto load_rows = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
+          row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
+        }
+      };
       if constexpr (kFwd) {
         // columns past the tile repeat its last slot
 #pragma unroll
@@ -489,12 +504,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           src[i] = p.x + 8 * c +
                    p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
       } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int at = g.lo + r0 + kRowStep * i;
-          row[0][i] = expert_row(p, min(at, p.M - 1));
-          row[1][i] = expert_row(p, min(at + kPairStep, p.M - 1));
-        }
+        load_rows(0);
       }
 #pragma unroll 1
       for (int kt = 0; kt < steps; ++kt) {
@@ -509,17 +519,19 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
               cp_async16(b + sw128_offset(r0 + kRowStep * i, c), src[i] + (in ? c0 : 0), in);
         } else {
           const int col = b0 + 8 * c;
+          if (kt % 8 == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) row[i] = row_next[i];
+            load_rows(kt + 8);
+          }
+          const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int r = r0 + kRowStep * i;
+            const int at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
             const bool in = g.lo + c0 + r < g.hi && col < p.K;
             cp_async16(b + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7),
-                       p.x + (in ? row[0][i] * p.ldx + col : 0), in);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            row[0][i] = row[1][i];
-            row[1][i] = expert_row(p, min(g.lo + c0 + 2 * kPairStep + r0 + kRowStep * i, p.M - 1));
+                       p.x + (in ? at * p.ldx + col : 0), in);
           }
         }
         cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
@@ -601,11 +613,13 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
         }
       }
     }
-  } else if (warp >= 4 && warp < 4 + kPairEpiWarps) {
+  } else if (warp >= 4 && warp < 4 + kEpiWarps) {
     // ------------------------------------------------------------- write back
     const int q = warp & 3, grp = (warp - 4) >> 2;
     uint8_t* const stg = base + kStages * kPairStageBytes + (warp - 4) * pair_out_bytes<kWhat>();
-    uint8_t* const ring_pre = stg + 4096;
+    // back (input): the ring
+    const int pre_slots = p.out_f32 ? 1 : 2;
+    uint8_t* const ring_pre = stg + (p.out_f32 ? 4096 : 2048);
     const int pr = lane >> 2, px = lane & 3;   // this lane's 16-byte piece of columns pr + 8 k
     const int mi = lane >> 3;                  // fragment whose row address this lane gives
     const uint32_t tempty0 = dsmem_addr(smem_u32(&sm.tempty[0]), 0);
@@ -613,42 +627,38 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
     int j = 0, n_out = 0;
     // the next chunk's area: no earlier copy reads it any more
     const auto next_area = [&]() {
-      const bool one = kBackX && p.out_f32;
-      if (lane == 0) {
-        if (one) bulk_wait_read<0>();
-        else bulk_wait_read<1>();
-      }
+      if (lane == 0) bulk_wait_read<kBackW ? 1 : 0>();
       __syncwarp();
-      return stg + (one ? 0 : (n_out++ & 1) * (kBackX ? 2048 : 4096));
+      return stg + (kBackW ? (n_out++ & 1) * 4096 : 0);
     };
     // back (input): chunks of `pre` on their way
-    PairTile h;
-    h.e = h.n = 0;
+    PairTile ahead;
+    ahead.e = ahead.n = 0;
     int ht = pair - pairs, hc = 0, slot_in = 0, slot_out = 0;
     const auto copy_pre = [&]() {
-      hc += 2 * kPairChunk;
-      while (ht < tiles && hc >= h.n) {
+      hc += kGroups * kPairChunk;
+      while (ht < tiles && hc >= ahead.n) {
         ht += pairs;
         hc = kPairChunk * grp;
-        if (ht < tiles) pair_tile<kWhat>(p, sm, ht, h);
+        if (ht < tiles) pair_tile<kWhat>(p, sm, ht, ahead);
       }
       if (ht < tiles) {
-        const int x = h.f0 + rank * kPairM + 32 * q + 8 * px;
+        const int x = ahead.f0 + rank * kPairM + 32 * q + 8 * px;
         const uint32_t to = smem_u32(ring_pre + slot_in * kPreBytes);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int r = 8 * k + pr;
-          const bool in = hc + r < h.n && x < p.K;
+          const bool in = hc + r < ahead.n && x < p.K;
           cp_async16(to + stage_offset<4>(r, px),
-                     p.pre_in + (in ? (static_cast<size_t>(h.lo) + h.i0 + hc + r) * p.K + x : 0), in);
+                     p.pre_in + (in ? (static_cast<size_t>(ahead.lo) + ahead.i0 + hc + r) * p.K + x : 0), in);
         }
       }
       cp_async_commit();
-      slot_in = slot_in + 1 == kPreSlots ? 0 : slot_in + 1;
+      slot_in = slot_in + 1 == pre_slots ? 0 : slot_in + 1;
     };
     if (kBackX && p.pre_in != nullptr)
 #pragma unroll 1
-      for (int i = 0; i < kPreSlots; ++i) copy_pre();
+      for (int i = 0; i < pre_slots; ++i) copy_pre();
     // forward: a tile's bias is loaded during the tile before
     float bias[2][2] = {}, bias_next[2][2] = {};
     const auto load_bias = [&](const PairTile& g1) {
@@ -661,8 +671,8 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
         }
     };
     if (kFwd && p.bias != nullptr && pair < tiles) {
-      pair_tile<kWhat>(p, sm, pair, h);
-      load_bias(h);
+      pair_tile<kWhat>(p, sm, pair, ahead);
+      load_bias(ahead);
     }
     for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
       pair_tile<kWhat>(p, sm, t, g);
@@ -671,10 +681,10 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       const int f = g.f0 + rank * kPairM + 32 * q;   // this warp's features
       if (kFwd && p.bias != nullptr) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) bias[h][0] = bias_next[h][0], bias[h][1] = bias_next[h][1];
+        for (int u = 0; u < 4; ++u) bias[u >> 1][u & 1] = bias_next[u >> 1][u & 1];
         if (t + pairs < tiles) {
-          pair_tile<kWhat>(p, sm, t + pairs, h);
-          load_bias(h);
+          pair_tile<kWhat>(p, sm, t + pairs, ahead);
+          load_bias(ahead);
         }
       }
       if (steps > 0) ok = ok && warp_wait(&sm.tfull[acc], (j >> 1) & 1, abort_flag);
@@ -683,7 +693,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       if constexpr (kBackW) {
         // rows are features, columns contiguous in memory
 #pragma unroll 1
-        for (int c = kPairChunk * grp; ok && f < p.N && c < g.n; c += 2 * kPairChunk) {
+        for (int c = kPairChunk * grp; ok && f < p.N && c < g.n; c += kGroups * kPairChunk) {
           float v[32];
           if (steps > 0) {
             tmem_ld32(d + c, v);
@@ -719,7 +729,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
         const int width = features<kWhat>(p);
         const int slot0 = g.lo + g.i0;
 #pragma unroll 1
-        for (int c = kPairChunk * grp; c < g.n; c += 2 * kPairChunk) {
+        for (int c = kPairChunk * grp; c < g.n; c += kGroups * kPairChunk) {
           float v[2][16];
           tmem_ld_frag32(d + c, v[0]);
           tmem_ld_frag32(d + c + (16u << 16), v[1]);
@@ -741,7 +751,8 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           if (kBackX && p.pre_in != nullptr) {
             // in the staging's layout, so that its fragments match the accumulator's
             uint32_t zf[2][2][4];
-            cp_async_wait<kPreSlots - 1>();
+            if (pre_slots == 2) cp_async_wait<1>();
+            else cp_async_wait<0>();
             __syncwarp();
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -749,7 +760,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
               for (int b = 0; b < 4; b += 2)
                 ldmatrix4_trans(smem_u32(ring_pre + slot_out * kPreBytes + at(h, b)), zf[h][b / 2]);
             __syncwarp();
-            slot_out = slot_out + 1 == kPreSlots ? 0 : slot_out + 1;
+            slot_out = slot_out + 1 == pre_slots ? 0 : slot_out + 1;
             copy_pre();
             tmem_ld_wait();
 #pragma unroll
