@@ -85,7 +85,7 @@ __device__ __forceinline__ int expert_row(const ExpertLinearParams& p, int s) {
   return p.token == nullptr ? s : min(max(__ldg(p.token + s), 0), p.x_rows - 1);
 }
 
-constexpr int kCombineMaxCtas = 304;   // CTAs of the backward kernel: partial sums per feature
+constexpr int kCombineMaxParts = 256;   // CTAs of the gradient: partial sums per feature
 
 struct CombineParams {
   int B, L, D, k, M;

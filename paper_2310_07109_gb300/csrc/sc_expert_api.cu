@@ -33,7 +33,7 @@ ExpertLayout expert_layout(int E, int D) {
   ExpertLayout w;
   w.counts = kAlign;
   w.part = align_up(w.counts + sizeof(int32_t) * kRouteMaxCtas * static_cast<size_t>(E));
-  w.total = align_up(w.part + sizeof(float) * kCombineMaxCtas * 2 * static_cast<size_t>(D));
+  w.total = align_up(w.part + sizeof(float) * kCombineMaxParts * 2 * static_cast<size_t>(D));
   return w;
 }
 

@@ -8,6 +8,14 @@
 //   dY[slot] = g dS;  dg = dS . Y[slot];  dres = a dS
 //   dgamma = sum_t dOut h;  dbeta = sum_t dOut   (rows in a fixed order)
 // All sums in fp32; the norm takes the unrounded S; outputs are rounded once.
+//
+// Bound by memory.  Each thread copies the 16-byte vectors that it will use itself, a
+// row ahead, into shared memory of its own (cp.async), so that a whole row more than the
+// one at work is on its way per warp, whatever the registers hold, and no thread waits for
+// another's copies.  A warp has a row of up to 1024 features; wider rows have several
+// warps, whose sums meet in shared memory.  Rows in registers, loaded when they were
+// needed, kept too little on its way: 8192 rows x 1024, k = 4, gradient 155 us with a
+// warp a row, 106 us with a thread per eight features.
 #include <cuda_runtime.h>
 #include <cstdint>
 
@@ -16,8 +24,8 @@
 
 namespace sc {
 
-constexpr int kCombineThreads = 256;
-constexpr int kCombineVecs = 4;   // 16-byte vectors of 8 features per thread: D <= 32 x threads of a row
+constexpr int kCombineWarps = 8;       // most of a CTA
+constexpr int kCombineChunk = 4;       // choices whose dot products are summed together
 
 __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -33,285 +41,402 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
                     pack_bf16x2(f[6], f[7]));
 }
 
-// Sums of two values over the kRow threads of a row (a warp, or the whole CTA).
-template <int kRow>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* red) {
+// How a launch is cut: warps of a row, rows of a CTA at a time, copied tensors of a row,
+// rows on their way per row group (two, or one where two do not fit).
+struct CombineCut {
+  int warps, groups, segs, ctas;
+};
+
+struct CombineSmem {
+  float red[kCombineWarps][2][kCombineChunk][kCombineWarps];   // a row group's sums, two in turn
+  int slot[kCombineWarps][2][kMaxChoices];                     // per warp: rows on their way
+  float gate[kCombineWarps][2][kMaxChoices];
+  int in[kCombineWarps][2];
+};
+
+// Sums of N values over a row's threads, the same in each of them; its warps in order.
+template <int N>
+__device__ __forceinline__ void row_sum(const CombineCut& cut, CombineSmem& sm, int group, int w, int& turn,
+                                        float (&v)[N]) {
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, off);
-    b += __shfl_xor_sync(0xffffffffu, b, off);
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], off);
+  if (cut.warps == 1) return;
+  turn ^= 1;   // the other half was read before the last meeting
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) sm.red[group][turn][i][w] = v[i];
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * cut.warps) : "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    v[i] = sm.red[group][turn][i][0];
+    for (int o = 1; o < cut.warps; ++o) v[i] += sm.red[group][turn][i][o];
   }
-  if constexpr (kRow > 32) {
-    __syncthreads();   // the previous sum has been read
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_float2(a, b);
+}
+
+// V vectors of 8 features a thread; kRows rows on their way per row group.
+template <bool kBack, int V, int kRows>
+__global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
+    sc_combine_kernel(const __grid_constant__ CombineParams p, const CombineCut cut) {
+  __shared__ CombineSmem sm;
+  extern __shared__ uint4 fifo[];   // per warp [kRows][segs][V][32], then gamma (and beta)
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = warp / cut.warps, w = warp - group * cut.warps;
+  const int vecs = p.D / 8;
+  // gamma and beta, the first four and the last four features of each vector apart (one
+  // load each from global memory was 32 bytes from the next lane's: 23 us of 8192 x 768)
+  float4* const gam = reinterpret_cast<float4*>(
+      fifo + static_cast<size_t>(cut.warps) * cut.groups * kRows * cut.segs * V * 32);
+  float4* const bet = gam + 2 * vecs;
+  uint4* const mine = fifo + static_cast<size_t>(warp) * kRows * cut.segs * V * 32 + lane;
+  // this thread's vector v is number 32 (w + v warps) + lane of a row
+  const int at0 = 32 * w + lane, at_step = 32 * cut.warps;
+  const bool norm = p.gamma != nullptr;
+  const bool need_y = !kBack || norm || p.dgate != nullptr;
+  const bool need_res = p.res != nullptr && (!kBack || norm);
+  // segments after the choices'
+  const int seg_res = p.k, seg_dout = seg_res + (need_res ? 1 : 0), seg_dsum = seg_dout + (norm ? 1 : 0);
+  const long long step = static_cast<long long>(gridDim.x) * cut.groups;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (norm) {
+    for (int i = threadIdx.x; i < p.D; i += blockDim.x) {
+      const int to = ((i >> 2 & 1) * vecs + (i >> 3)) * 4 + (i & 3);
+      reinterpret_cast<float*>(gam)[to] = __ldg(p.gamma + i);
+      if (!kBack) reinterpret_cast<float*>(bet)[to] = __ldg(p.beta + i);
+    }
     __syncthreads();
-    a = b = 0.f;
-#pragma unroll
-    for (int w = 0; w < kRow / 32; ++w) {
-      a += red[w].x;
-      b += red[w].y;
-    }
   }
-  return make_float2(a, b);
-}
+  const auto param = [&](const float4* v, int at, float (&f)[8]) {
+    const float4 a = v[at], b = v[vecs + at];
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  };
 
-__device__ __forceinline__ int clamp_slot(const CombineParams& p, int s) {
-  return s >= 0 && s < p.M ? s : -1;
-}
-
-// S of row t, this thread's features (vector c + i kRow of 8).
-template <int kRow>
-__device__ __forceinline__ void combine_sum(const CombineParams& p, long long t, int c, int vecs,
-                                            float (&s)[kCombineVecs][8]) {
-#pragma unroll
-  for (int i = 0; i < kCombineVecs; ++i) {
-    const int at = c + i * kRow;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) s[i][q] = 0.f;
-    if (p.res != nullptr && at < vecs) {
-      float f[8];
-      unpack8(__ldg(reinterpret_cast<const uint4*>(p.res + t * p.D) + at), f);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) s[i][q] = p.res_scale * f[q];
+  // lane j has choice j of the row whose copies start next
+  int slot_next = -1, in_next = 0;
+  float gate_next = 1.f;
+  const auto load_plan = [&](long long t) {
+    in_next = t < p.T;
+    if (in_next && p.rows != nullptr) {
+      const long long b = t / p.L;
+      in_next = t - b * p.L < __ldg(p.rows + b);
     }
-  }
-  for (int j = 0; j < p.k; ++j) {
-    const int sl = clamp_slot(p, __ldg(p.slot + t * p.k + j));
-    if (sl < 0) continue;
-    const float g = p.gate ? __ldg(p.gate + t * p.k + j) : 1.f;
-    const uint4* y = reinterpret_cast<const uint4*>(p.y + static_cast<long long>(sl) * p.D);
-#pragma unroll
-    for (int i = 0; i < kCombineVecs; ++i) {
-      const int at = c + i * kRow;
-      if (at >= vecs) continue;
-      float f[8];
-      unpack8(__ldg(y + at), f);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) s[i][q] = fmaf(g, f[q], s[i][q]);
+    slot_next = -1;
+    gate_next = 1.f;
+    if (in_next && lane < p.k) {
+      slot_next = __ldg(p.slot + t * p.k + lane);
+      if (slot_next >= p.M) slot_next = -1;
+      if (p.gate != nullptr) gate_next = __ldg(p.gate + t * p.k + lane);
     }
-  }
-}
-
-// Mean and 1 / sigma of a row (two passes over the registers).
-template <int kRow>
-__device__ __forceinline__ float2 row_moments(const CombineParams& p, int c, int vecs,
-                                              const float (&s)[kCombineVecs][8], float2* red) {
-  float a = 0.f;
+  };
+  const auto copy = [&](int r, int seg, const uint16_t* row) {
 #pragma unroll
-  for (int i = 0; i < kCombineVecs; ++i)
-#pragma unroll
-    for (int q = 0; q < 8; ++q) a += s[i][q];   // features past D are 0
-  const float mean = row_sum2<kRow>(a, 0.f, red).x / static_cast<float>(p.D);
-  float b = 0.f;
-#pragma unroll
-  for (int i = 0; i < kCombineVecs; ++i)
-    if (c + i * kRow < vecs)
-#pragma unroll
-      for (int q = 0; q < 8; ++q) b += (s[i][q] - mean) * (s[i][q] - mean);
-  const float var = row_sum2<kRow>(b, 0.f, red).x / static_cast<float>(p.D);
-  return make_float2(mean, 1.f / sqrtf(var + p.eps));
-}
-
-__device__ __forceinline__ bool row_in_use(const CombineParams& p, long long t) {
-  if (p.rows == nullptr) return true;
-  const long long b = t / p.L;
-  return t - b * p.L < __ldg(p.rows + b);
-}
-
-template <int kRow>
-__global__ void __launch_bounds__(kCombineThreads) sc_combine_kernel(
-    const __grid_constant__ CombineParams p) {
-  __shared__ float2 red[kCombineThreads / 32];
-  pdl_wait();
-  pdl_launch_dependents();
-  const int c = threadIdx.x % kRow;
-  const long long t = static_cast<long long>(blockIdx.x) * (kCombineThreads / kRow) + threadIdx.x / kRow;
-  if (t >= p.T || !row_in_use(p, t)) return;
-  const int vecs = p.D / 8;
-  float s[kCombineVecs][8];
-  combine_sum<kRow>(p, t, c, vecs, s);
-  if (p.sum != nullptr)
-#pragma unroll
-    for (int i = 0; i < kCombineVecs; ++i)
-      if (c + i * kRow < vecs) reinterpret_cast<uint4*>(p.sum + t * p.D)[c + i * kRow] = pack8(s[i]);
-  if (p.gamma == nullptr) return;
-  const float2 m = row_moments<kRow>(p, c, vecs, s, red);
-#pragma unroll
-  for (int i = 0; i < kCombineVecs; ++i) {
-    const int at = c + i * kRow;
-    if (at >= vecs) continue;
-    float o[8];
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-      o[q] = (s[i][q] - m.x) * m.y * __ldg(p.gamma + 8 * at + q) + __ldg(p.beta + 8 * at + q);
-    reinterpret_cast<uint4*>(p.out + t * p.D)[at] = pack8(o);
-  }
-}
-
-template <int kRow>
-__global__ void __launch_bounds__(kCombineThreads) sc_combine_back_kernel(
-    const __grid_constant__ CombineParams p) {
-  __shared__ float2 red[kCombineThreads / 32];
-  extern __shared__ float part[];   // [rows of the CTA][2][D]
-  pdl_wait();
-  pdl_launch_dependents();
-  constexpr int kRows = kCombineThreads / kRow;
-  const int c = threadIdx.x % kRow, r = threadIdx.x / kRow;
-  const int vecs = p.D / 8;
-  float dgam[kCombineVecs][8] = {}, dbet[kCombineVecs][8] = {};
-  for (long long t = static_cast<long long>(blockIdx.x) * kRows + r; t < p.T;
-       t += static_cast<long long>(gridDim.x) * kRows) {
-    if (!row_in_use(p, t)) {
-      if (c < p.k && p.dgate) p.dgate[t * p.k + c] = 0.f;
-      continue;
+    for (int v = 0; v < V; ++v) {
+      const int at = at0 + v * at_step;
+      const bool in = at < vecs;
+      cp_async16(smem_u32(mine + (r * cut.segs + seg) * V * 32 + 32 * v), row + (in ? 8 * at : 0), in);
     }
-    float ds[kCombineVecs][8];
+  };
+  // starts the copies of row t into place r, by the plan at hand, and loads the next plan
+  const auto start = [&](long long t, int r) {
+    __syncwarp();   // the place's plan has been read
+    if (lane < kMaxChoices) {
+      sm.slot[warp][r][lane] = slot_next;
+      sm.gate[warp][r][lane] = gate_next;
+    }
+    if (lane == 0) sm.in[warp][r] = in_next;
+    if (in_next) {
+      for (int j = 0; j < p.k; ++j) {
+        const int s = __shfl_sync(0xffffffffu, slot_next, j);
+        if (s >= 0 && need_y) copy(r, j, p.y + static_cast<size_t>(s) * p.D);
+      }
+      if (need_res) copy(r, seg_res, p.res + t * p.D);
+      if (kBack && norm) copy(r, seg_dout, p.dout + t * p.D);
+      if (kBack && p.dsum != nullptr) copy(r, seg_dsum, p.dsum + t * p.D);
+    }
+    cp_async_commit();
+    load_plan(t + step);
+    __syncwarp();
+  };
+  const auto piece = [&](int r, int seg, int v, float (&f)[8]) {
+    unpack8(mine[(r * cut.segs + seg) * V * 32 + 32 * v], f);
+  };
+
+  float dgam[kBack ? V : 1][8] = {}, dbet[kBack ? V : 1][8] = {};
+  int turn = 0;
+  long long t = static_cast<long long>(blockIdx.x) * cut.groups + group;
+  load_plan(t);
+  start(t, 0);
+  for (int r = 0; t < p.T; t += step, r = kRows == 2 ? r ^ 1 : 0) {
+    if (kRows == 2) {
+      start(t + step, r ^ 1);
+      cp_async_wait<1>();
+    } else {
+      cp_async_wait<0>();
+    }
+    if (sm.in[warp][r]) {
+      // S, and its normal form
+      float s[V][8], inv = 0.f;
+      if (!kBack || norm) {
 #pragma unroll
-    for (int i = 0; i < kCombineVecs; ++i)
+        for (int v = 0; v < V; ++v) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q) ds[i][q] = 0.f;
-    if (p.dout != nullptr) {
-      float s[kCombineVecs][8];
-      combine_sum<kRow>(p, t, c, vecs, s);
-      const float2 m = row_moments<kRow>(p, c, vecs, s, red);
-      float a = 0.f, b = 0.f;
+          for (int q = 0; q < 8; ++q) s[v][q] = 0.f;
+          if (need_res) {
+            float f[8];
+            piece(r, seg_res, v, f);
 #pragma unroll
-      for (int i = 0; i < kCombineVecs; ++i) {
-        const int at = c + i * kRow;
-        if (at >= vecs) continue;
-        unpack8(__ldg(reinterpret_cast<const uint4*>(p.dout + t * p.D) + at), ds[i]);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          s[i][q] = (s[i][q] - m.x) * m.y;
-          dgam[i][q] += ds[i][q] * s[i][q];
-          dbet[i][q] += ds[i][q];
-          ds[i][q] *= __ldg(p.gamma + 8 * at + q);
-          a += ds[i][q];
-          b += ds[i][q] * s[i][q];
+            for (int q = 0; q < 8; ++q) s[v][q] = p.res_scale * f[q];
+          }
         }
+        for (int j = 0; j < p.k; ++j) {
+          if (sm.slot[warp][r][j] < 0) continue;
+          const float g = sm.gate[warp][r][j];
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            float f[8];
+            piece(r, j, v, f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[v][q] = fmaf(g, f[q], s[v][q]);
+          }
+        }
+        if (!kBack && p.sum != nullptr)
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (at0 + v * at_step < vecs)
+              reinterpret_cast<uint4*>(p.sum + t * p.D)[at0 + v * at_step] = pack8(s[v]);
       }
-      const float2 ab = row_sum2<kRow>(a, b, red);
-      const float ma = ab.x / static_cast<float>(p.D), mb = ab.y / static_cast<float>(p.D);
+      if (norm) {
+        // two sums, so that a mean far from 0 costs no digits of the variance
+        float a[1] = {0.f};
 #pragma unroll
-      for (int i = 0; i < kCombineVecs; ++i)
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) ds[i][q] = m.y * (ds[i][q] - ma - s[i][q] * mb);
-    }
+          for (int q = 0; q < 8; ++q) a[0] += s[v][q];
+        row_sum(cut, sm, group, w, turn, a);
+        const float mean = a[0] / static_cast<float>(p.D);
+        a[0] = 0.f;
 #pragma unroll
-    for (int i = 0; i < kCombineVecs; ++i) {
-      const int at = c + i * kRow;
-      if (at >= vecs) continue;
-      if (p.dsum != nullptr) {
-        float f[8];
-        unpack8(__ldg(reinterpret_cast<const uint4*>(p.dsum + t * p.D) + at), f);
+        for (int v = 0; v < V; ++v) {
+          const bool in = at0 + v * at_step < vecs;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) ds[i][q] += f[q];
+          for (int q = 0; q < 8; ++q) {
+            s[v][q] = in ? s[v][q] - mean : 0.f;
+            a[0] += s[v][q] * s[v][q];
+          }
+        }
+        row_sum(cut, sm, group, w, turn, a);
+        inv = 1.f / sqrtf(a[0] / static_cast<float>(p.D) + p.eps);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) s[v][q] *= inv;
       }
-      if (p.dres != nullptr) {
-        float f[8];
+      if constexpr (!kBack) {
+        if (norm)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) f[q] = p.res_scale * ds[i][q];
-        reinterpret_cast<uint4*>(p.dres + t * p.D)[at] = pack8(f);
-      }
-    }
-    for (int j = 0; j < p.k; ++j) {
-      const int sl = clamp_slot(p, __ldg(p.slot + t * p.k + j));
-      if (sl < 0) {
-        if (c == 0 && p.dgate) p.dgate[t * p.k + j] = 0.f;
-        continue;
-      }
-      const float g = p.gate ? __ldg(p.gate + t * p.k + j) : 1.f;
-      const uint4* y = reinterpret_cast<const uint4*>(p.y + static_cast<long long>(sl) * p.D);
-      uint4* dy = reinterpret_cast<uint4*>(p.dy + static_cast<long long>(sl) * p.D);
-      float dot = 0.f;
+          for (int v = 0; v < V; ++v) {
+            const int at = at0 + v * at_step;
+            if (at >= vecs) continue;
+            float ga[8], be[8];
+            param(gam, at, ga);
+            param(bet, at, be);
 #pragma unroll
-      for (int i = 0; i < kCombineVecs; ++i) {
-        const int at = c + i * kRow;
-        if (at >= vecs) continue;
-        float f[8], o[8];
-        if (p.dgate) {
-          unpack8(__ldg(y + at), f);
+            for (int q = 0; q < 8; ++q) s[v][q] = fmaf(s[v][q], ga[q], be[q]);
+            reinterpret_cast<uint4*>(p.out + t * p.D)[at] = pack8(s[v]);
+          }
+      } else {
+        float ds[V][8];
+        float ab[2] = {0.f, 0.f};
 #pragma unroll
-          for (int q = 0; q < 8; ++q) dot = fmaf(ds[i][q], f[q], dot);
+        for (int v = 0; v < V; ++v) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) ds[v][q] = 0.f;
+          const int at = at0 + v * at_step;
+          if (!norm || at >= vecs) continue;
+          float f[8], ga[8];
+          piece(r, seg_dout, v, f);
+          param(gam, at, ga);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            dgam[v][q] = fmaf(f[q], s[v][q], dgam[v][q]);
+            dbet[v][q] += f[q];
+            ds[v][q] = f[q] * ga[q];
+            ab[0] += ds[v][q];
+            ab[1] = fmaf(ds[v][q], s[v][q], ab[1]);
+          }
+        }
+        if (norm) {
+          row_sum(cut, sm, group, w, turn, ab);
+          const float ma = ab[0] / static_cast<float>(p.D), mb = ab[1] / static_cast<float>(p.D);
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) ds[v][q] = inv * (ds[v][q] - ma - s[v][q] * mb);
         }
 #pragma unroll
-        for (int q = 0; q < 8; ++q) o[q] = g * ds[i][q];
-        dy[at] = pack8(o);
+        for (int v = 0; v < V; ++v) {
+          const int at = at0 + v * at_step;
+          const bool in = at < vecs;
+          float f[8];
+          if (p.dsum != nullptr) {
+            piece(r, seg_dsum, v, f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) ds[v][q] += f[q];
+          }
+          if (p.dres != nullptr && in) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] = p.res_scale * ds[v][q];
+            reinterpret_cast<uint4*>(p.dres + t * p.D)[at] = pack8(f);
+          }
+        }
+        for (int j0 = 0; j0 < p.k; j0 += kCombineChunk) {
+          float dot[kCombineChunk];
+#pragma unroll
+          for (int j = 0; j < kCombineChunk; ++j) {
+            dot[j] = 0.f;
+            const int sl = j0 + j < p.k ? sm.slot[warp][r][j0 + j] : -1;
+            if (sl < 0) continue;
+            const float g = sm.gate[warp][r][j0 + j];
+            uint4* const dy = reinterpret_cast<uint4*>(p.dy + static_cast<size_t>(sl) * p.D);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              const int at = at0 + v * at_step;
+              if (at >= vecs) continue;
+              float f[8];
+              if (p.dgate != nullptr) {
+                piece(r, j0 + j, v, f);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) dot[j] = fmaf(ds[v][q], f[q], dot[j]);
+              }
+#pragma unroll
+              for (int q = 0; q < 8; ++q) f[q] = g * ds[v][q];
+              dy[at] = pack8(f);
+            }
+          }
+          if (p.dgate != nullptr) {
+            row_sum(cut, sm, group, w, turn, dot);
+#pragma unroll
+            for (int j = 0; j < kCombineChunk; ++j)
+              if (w == 0 && lane == 0 && j0 + j < p.k) p.dgate[t * p.k + j0 + j] = dot[j];
+          }
+        }
       }
-      if (p.dgate) {
-        dot = row_sum2<kRow>(dot, 0.f, red).x;
-        if (c == 0) p.dgate[t * p.k + j] = dot;
+    } else if (kBack && p.dgate != nullptr && w == 0 && lane < p.k) {
+      p.dgate[t * p.k + lane] = 0.f;
+    }
+    if (kRows == 1) start(t + step, 0);
+  }
+  if constexpr (kBack) {
+    cp_async_wait_all();
+    if (p.dgamma == nullptr) return;
+    // the CTA's row groups in order, through the copies' place
+    float* const part = reinterpret_cast<float*>(fifo);
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int at = at0 + v * at_step;
+      if (at >= vecs) continue;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        part[(2 * group) * p.D + 8 * at + q] = dgam[v][q];
+        part[(2 * group + 1) * p.D + 8 * at + q] = dbet[v][q];
       }
     }
-  }
-  if (p.dgamma == nullptr) return;
-  // the CTA's rows, in order, into its part of the workspace
-#pragma unroll
-  for (int i = 0; i < kCombineVecs; ++i) {
-    const int at = c + i * kRow;
-    if (at >= vecs) continue;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      part[(r * 2) * p.D + 8 * at + q] = dgam[i][q];
-      part[(r * 2 + 1) * p.D + 8 * at + q] = dbet[i][q];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.D; i += blockDim.x) {
+      float x = part[i];
+      for (int o = 1; o < cut.groups; ++o) x += part[o * 2 * p.D + i];
+      p.part[static_cast<long long>(blockIdx.x) * 2 * p.D + i] = x;
     }
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 2 * p.D; i += kCombineThreads) {
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < kRows; ++w) v += part[w * 2 * p.D + i];
-    p.part[static_cast<long long>(blockIdx.x) * 2 * p.D + i] = v;
+  } else {
+    cp_async_wait_all();
   }
 }
 
-// dgamma and dbeta: the CTAs' parts in order.  32 features a CTA, its eight warps take
-// every eighth part.
-__global__ void __launch_bounds__(256) sc_combine_reduce_kernel(
-    const __grid_constant__ CombineParams p, int parts) {
-  __shared__ float red[8][32];
+// dgamma and dbeta: the CTAs' parts, 32 features a CTA, its 32 warps every 32nd part in
+// order, then the warps in order.
+__global__ void __launch_bounds__(1024) sc_combine_reduce_kernel(const __grid_constant__ CombineParams p,
+                                                                 int parts) {
+  __shared__ float red[32][33];
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int f = blockIdx.x * 32 + lane;
   float v = 0.f;
   if (f < 2 * p.D)
-    for (int c = w; c < parts; c += 8) v += __ldcg(p.part + static_cast<long long>(c) * 2 * p.D + f);
+#pragma unroll 8
+    for (int c = w; c < parts; c += 32) v += __ldcg(p.part + static_cast<long long>(c) * 2 * p.D + f);
   red[w][lane] = v;
   __syncthreads();
   if (w != 0 || f >= 2 * p.D) return;
-  for (int i = 1; i < 8; ++i) v += red[i][lane];
+#pragma unroll
+  for (int i = 1; i < 32; ++i) v += red[i][lane];
   if (f < p.D) p.dgamma[f] = v;
   else p.dbeta[f - p.D] = v;
 }
 
-static bool row_per_warp(const CombineParams& p) { return p.D <= 32 * 8 * kCombineVecs; }
+// ---------------------------------------------------------------------------
+// launch
+// ---------------------------------------------------------------------------
+constexpr size_t kCombineBytes = 220 * 1024;   // shared memory for copies per SM
 
-cudaError_t launch_combine(const CombineParams& p, cudaStream_t st) {
-  const int per = row_per_warp(p) ? kCombineThreads / 32 : 1;
-  const dim3 grid(static_cast<unsigned>((p.T + per - 1) / per));
-  return launch_chained(row_per_warp(p) ? sc_combine_kernel<32> : sc_combine_kernel<kCombineThreads>,
-                        grid, dim3(kCombineThreads), 0, st, p);
-}
-
-cudaError_t launch_combine_back(const CombineParams& p, cudaStream_t st) {
-  const int per = row_per_warp(p) ? kCombineThreads / 32 : 1;
-  const long long want = (p.T + per - 1) / per;
-  const int ctas = static_cast<int>(want < kCombineMaxCtas ? want : kCombineMaxCtas);
-  const size_t smem = p.dgamma ? sizeof(float) * 2 * p.D * per : 0;
-  cudaError_t e = launch_chained(
-      row_per_warp(p) ? sc_combine_back_kernel<32> : sc_combine_back_kernel<kCombineThreads>,
-      dim3(ctas), dim3(kCombineThreads), smem, st, p);
-  if (e != cudaSuccess || p.dgamma == nullptr) return e;
-  return launch_chained(sc_combine_reduce_kernel, dim3((2 * p.D + 31) / 32), dim3(256), 0, st, p, ctas);
-}
-
-cudaError_t configure_combine() {
-  const cudaError_t e = cudaFuncSetAttribute(sc_combine_back_kernel<32>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, 65536);
+template <bool kBack, int V, int kRows>
+static cudaError_t launch_cut(const CombineParams& p, const CombineCut& cut, size_t smem, cudaStream_t st) {
+  static bool set[64] = {};   // per device
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(sc_combine_back_kernel<kCombineThreads>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize, 65536);
+  if (dev >= 64 || !set[dev]) {
+    e = cudaFuncSetAttribute(sc_combine_kernel<kBack, V, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(kCombineBytes));
+    if (e != cudaSuccess) return e;
+    if (dev < 64) set[dev] = true;
+  }
+  return launch_chained(sc_combine_kernel<kBack, V, kRows>, dim3(cut.ctas),
+                        dim3(32 * cut.warps * cut.groups), smem, st, p, cut);
 }
+
+template <bool kBack, int kRows>
+static cudaError_t launch_vecs(const CombineParams& p, const CombineCut& cut, int vecs, size_t smem,
+                               cudaStream_t st) {
+  return vecs == 1   ? launch_cut<kBack, 1, kRows>(p, cut, smem, st)
+         : vecs == 2 ? launch_cut<kBack, 2, kRows>(p, cut, smem, st)
+         : vecs == 3 ? launch_cut<kBack, 3, kRows>(p, cut, smem, st)
+                     : launch_cut<kBack, 4, kRows>(p, cut, smem, st);
+}
+
+template <bool kBack>
+static cudaError_t combine(const CombineParams& p, cudaStream_t st) {
+  const bool norm = p.gamma != nullptr;
+  CombineCut cut;
+  cut.warps = (p.D + 1023) / 1024;
+  cut.segs = p.k + (p.res != nullptr && (!kBack || norm) ? 1 : 0) +
+             (kBack ? (norm ? 1 : 0) + (p.dsum != nullptr ? 1 : 0) : 0);
+  const int vecs = (p.D + 256 * cut.warps - 1) / (256 * cut.warps);
+  // as many row groups as the shared memory has room for two rows each: two CTAs an SM
+  // (the gradient, which has more registers: one); one row where even one group has not
+  const size_t row = static_cast<size_t>(cut.segs) * vecs * cut.warps * 512;
+  const size_t params = norm ? sizeof(float) * p.D * (kBack ? 1 : 2) : 0;
+  const size_t most = (kBack ? kCombineBytes : kCombineBytes / 2) - params;
+  const int rows = row * 2 <= most ? 2 : 1;
+  cut.groups = kCombineWarps / cut.warps;
+  while (cut.groups > 1 && row * rows * cut.groups > most) --cut.groups;
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  const long long want = (p.T + cut.groups - 1) / cut.groups;
+  const long long room = kBack ? (sms < kCombineMaxParts ? sms : kCombineMaxParts) : 2ll * sms;
+  cut.ctas = static_cast<int>(want < room ? want : room);
+  const size_t smem = row * rows * cut.groups + params;
+  e = rows == 2 ? launch_vecs<kBack, 2>(p, cut, vecs, smem, st) : launch_vecs<kBack, 1>(p, cut, vecs, smem, st);
+  if (e != cudaSuccess || !kBack || !norm) return e;
+  return launch_chained(sc_combine_reduce_kernel, dim3((2 * p.D + 31) / 32), dim3(1024), 0, st, p, cut.ctas);
+}
+
+cudaError_t launch_combine(const CombineParams& p, cudaStream_t st) { return combine<false>(p, st); }
+cudaError_t launch_combine_back(const CombineParams& p, cudaStream_t st) { return combine<true>(p, st); }
 
 }  // namespace sc

@@ -941,8 +941,6 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
                 : launch_pair<ExpertProduct::kBackWeight, false>(P, tiles, st);
 }
 
-cudaError_t configure_combine();
-
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t configure_pair() {
   return cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather>,
@@ -951,8 +949,7 @@ static cudaError_t configure_pair() {
 }
 
 cudaError_t configure_expert() {
-  cudaError_t e = configure_combine();
-  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kForward, false>();
+  cudaError_t e = configure_pair<ExpertProduct::kForward, false>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kForward, true>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackInput, false>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackWeight, false>();

@@ -111,8 +111,9 @@ def _rows_at(t, name, dtype):
     return t.data_ptr(), rows, width, t.stride(0) if rows > 1 else max(t.stride(0), width)
 
 
-def _stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+def _stream(stream, t):
+    # the raw handle: torch.cuda.current_stream() takes as long as a small kernel
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
 def _out_type(t):
@@ -150,7 +151,7 @@ def _work(workspace, device, stream, B, L, E, k, D):
 
 
 def _call(name, args, ws, stream):
-    rc = getattr(_library(), name)(args, ws.data_ptr(), ws.numel(), _stream(stream))
+    rc = getattr(_library(), name)(args, ws.data_ptr(), ws.numel(), _stream(stream, ws))
     if rc:
         _b._check(rc)
 
@@ -191,7 +192,7 @@ def expert_route_backward(logits, expert, gate, dgate, *, B, L, rows=None, renor
                           1 if renormalize else 0, _at(expert, "expert", torch.int32, (T, k)),
                           _at(gate, "gate", f32, (T, k)), _at(dgate, "dgate", f32, (T, k)),
                           _at(out, "dlogits", f32, (T, E)))
-    rc = _library().sc_expert_route_backward(a, _stream(stream))
+    rc = _library().sc_expert_route_backward(a, _stream(stream, logits))
     if rc:
         _b._check(rc)
     return out
@@ -280,7 +281,7 @@ def expert_combine_forward(Y, slot, gate=None, *, B, L, rows=None, res=None, res
                           _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)),
                           _at(beta, "beta", f32, (D,)), eps, _at(out.get("sum"), "sum", bf, (T, D)),
                           _at(out.get("out"), "out", bf, (T, D)))
-    rc = _library().sc_expert_combine_forward(a, _stream(stream))
+    rc = _library().sc_expert_combine_forward(a, _stream(stream, Y))
     if rc:
         _b._check(rc)
     return out
