@@ -24,7 +24,9 @@
 
 namespace sc {
 
-constexpr int kCombineWarps = 8;       // most of a CTA
+constexpr int kCombineWarps = 14;      // most of a CTA
+template <bool kBack>
+__host__ __device__ constexpr int combine_warps() { return kBack ? kCombineWarps : 8; }
 constexpr int kCombineChunk = 4;       // choices whose dot products are summed together
 
 __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
@@ -77,7 +79,7 @@ __device__ __forceinline__ void row_sum(const CombineCut& cut, CombineSmem& sm, 
 
 // V vectors of 8 features a thread; kRows rows on their way per row group.
 template <bool kBack, int V, int kRows>
-__global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
+__global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
     sc_combine_kernel(const __grid_constant__ CombineParams p, const CombineCut cut) {
   __shared__ CombineSmem sm;
   extern __shared__ uint4 fifo[];   // per warp [kRows][segs][V][32], then gamma (and beta)
@@ -380,7 +382,8 @@ __global__ void __launch_bounds__(1024) sc_combine_reduce_kernel(const __grid_co
 // ---------------------------------------------------------------------------
 // launch
 // ---------------------------------------------------------------------------
-constexpr size_t kCombineBytes = 220 * 1024;   // shared memory for copies per SM
+constexpr size_t kCombineBytes = 216 * 1024;   // shared memory for copies per SM
+static_assert(kCombineBytes + sizeof(CombineSmem) <= 227 * 1024, "one CTA's shared memory");
 
 template <bool kBack, int V, int kRows>
 static cudaError_t launch_cut(const CombineParams& p, const CombineCut& cut, size_t smem, cudaStream_t st) {
@@ -411,17 +414,21 @@ template <bool kBack>
 static cudaError_t combine(const CombineParams& p, cudaStream_t st) {
   const bool norm = p.gamma != nullptr;
   CombineCut cut;
-  cut.warps = (p.D + 1023) / 1024;
+  // Forward: a warp a row up to 1024 features (three warps for 768 features: 25 us, not
+  // 16).  The gradient: half as many features a thread while a CTA has the warps, for its
+  // long chain of arithmetic a row.
+  const int per_warp = kBack && p.D <= 512 * kCombineWarps ? 512 : 1024;
+  cut.warps = (p.D + per_warp - 1) / per_warp;
+  const int vecs = (p.D + 256 * cut.warps - 1) / (256 * cut.warps);
   cut.segs = p.k + (p.res != nullptr && (!kBack || norm) ? 1 : 0) +
              (kBack ? (norm ? 1 : 0) + (p.dsum != nullptr ? 1 : 0) : 0);
-  const int vecs = (p.D + 256 * cut.warps - 1) / (256 * cut.warps);
   // as many row groups as the shared memory has room for two rows each: two CTAs an SM
   // (the gradient, which has more registers: one); one row where even one group has not
   const size_t row = static_cast<size_t>(cut.segs) * vecs * cut.warps * 512;
   const size_t params = norm ? sizeof(float) * p.D * (kBack ? 1 : 2) : 0;
   const size_t most = (kBack ? kCombineBytes : kCombineBytes / 2) - params;
   const int rows = row * 2 <= most ? 2 : 1;
-  cut.groups = kCombineWarps / cut.warps;
+  cut.groups = combine_warps<kBack>() / cut.warps;
   while (cut.groups > 1 && row * rows * cut.groups > most) --cut.groups;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);

@@ -17,8 +17,13 @@
 
 namespace sc {
 
-constexpr int kRouteThreads = 256;
+// Few values and short work per token: latency bounds both kernels (16384 tokens, E = 64,
+// k = 8: 5 MB).  Hence 32 warps a CTA with the logits of a warp's four tokens on their way
+// together, counts added up by all threads, and one kernel where one CTA has every token.
+constexpr int kRouteThreads = 1024;
+constexpr int kRouteBackThreads = 256;
 constexpr int kRouteWords = kRouteTokens / 32;
+constexpr int kRoutePerWarp = kRouteTokens / (kRouteThreads / 32);   // tokens of a warp per chunk
 
 // Order-preserving map of a float to an unsigned number; 0 below every value that
 // may be chosen (NaN, -inf).
@@ -44,39 +49,79 @@ __device__ __forceinline__ bool token_in_use(const int32_t* rows, int L, long lo
   return t - b * L < __ldg(rows + b);
 }
 
+// Exclusive sums of v[0 .. n), n <= kMaxExperts, added to `to`; the total to *total.  One warp.
+__device__ __forceinline__ void scan_experts(const int* v, int n, int* to, int* total) {
+  const int lane = threadIdx.x & 31;
+  int run = 0;
+  for (int e0 = 0; e0 < n; e0 += 32) {
+    const int e = e0 + lane, mine = e < n ? v[e] : 0;
+    int x = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, off);
+      if (lane >= off) x += y;
+    }
+    if (e < n) to[e] += run + x - mine;
+    run += __shfl_sync(0xffffffffu, x, 31);
+  }
+  if (lane == 0) *total = run;
+}
+
+// From the ranks in `slot` to slots, and the slots' tokens: items i0 .. i1 (token x choice).
+__device__ __forceinline__ void place_items(const RouteParams& p, const int* base, int total, int i0, int i1) {
+  for (int i = i0 + threadIdx.x; i < i1; i += kRouteThreads) {
+    const int e = p.expert[i];
+    if (e >= 0) {
+      const int s = base[e] + p.slot[i];
+      p.slot[i] = s;
+      p.token[s] = i / p.k;
+    }
+    if (i >= total) p.token[i] = -1;
+  }
+}
+
 // One warp per token, V logits a lane (expert lane + 32 v).  Writes the choices, the
 // gates and, in `slot`, each choice's rank among the CTA's tokens with the same
 // expert: the tokens of a chunk that chose an expert are bits of its mask, so the
-// rank is a count of lower bits, whatever order the warps come in.
+// rank is a count of lower bits, whatever order the warps come in.  Where there is
+// one CTA it goes on to the slots.
 template <int V>
 __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
     const __grid_constant__ RouteParams p) {
-  extern __shared__ uint32_t route_smem[];
-  uint32_t* mask = route_smem;                              // [E][kRouteWords]
-  int* count = reinterpret_cast<int*>(mask + p.E * kRouteWords);   // [E] before this chunk
+  __shared__ int count[kMaxExperts], base[kMaxExperts], total;   // count: before this chunk
+  extern __shared__ uint32_t mask[];                             // [E][kRouteWords]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   for (int i = tid; i < p.E * kRouteWords; i += kRouteThreads) mask[i] = 0;
-  for (int i = tid; i < p.E; i += kRouteThreads) count[i] = 0;
+  for (int i = tid; i < p.E; i += kRouteThreads) count[i] = base[i] = 0;
   pdl_wait();
   pdl_launch_dependents();
   __syncthreads();
-  const long long t0 = static_cast<long long>(blockIdx.x) * p.per_cta;
-  const long long t1 = min(t0 + p.per_cta, p.T);
-  for (long long c0 = t0; c0 < t1; c0 += kRouteTokens) {
-    const int n = static_cast<int>(min(t1 - c0, static_cast<long long>(kRouteTokens)));
-    for (int i = warp; i < n; i += kRouteThreads / 32) {
-      const long long t = c0 + i;
-      float x[V];
-      uint32_t key[V];
-      const bool in = token_in_use(p.rows, p.L, t);
+  const int t0 = blockIdx.x * p.per_cta;
+  const int t1 = static_cast<int>(min(static_cast<long long>(t0) + p.per_cta, p.T));
+  for (int c0 = t0; c0 < t1; c0 += kRouteTokens) {
+    const int n = min(t1 - c0, kRouteTokens);
+    float x[kRoutePerWarp][V];
+#pragma unroll
+    for (int u = 0; u < kRoutePerWarp; ++u) {
+      const int i = warp * kRoutePerWarp + u, t = c0 + i;
+      const bool in = i < n && token_in_use(p.rows, p.L, t);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int e = lane + 32 * v;
-        x[v] = in && e < p.E ? __ldg(p.logits + t * p.ld + e) : -INFINITY;
-        key[v] = route_key(x[v]);
-        if (key[v] == 0u) x[v] = -INFINITY;
+        x[u][v] = in && e < p.E ? __ldg(p.logits + t * p.ld + e) : -INFINITY;
       }
-      float top = 0.f, total = 0.f, mine = 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kRoutePerWarp; ++u) {
+      const int i = warp * kRoutePerWarp + u, t = c0 + i;
+      if (i >= n) break;
+      uint32_t key[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        key[v] = route_key(x[u][v]);
+        if (key[v] == 0u) x[u][v] = -INFINITY;
+      }
+      float top = 0.f, sum = 0.f, mine = 0.f;
       int my_expert = -1;
       for (int j = 0; j < p.k; ++j) {
         uint32_t best = key[0];
@@ -88,7 +133,7 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
         float val = 0.f;
 #pragma unroll
         for (int v = V - 1; v >= 0; --v)
-          if (key[v] == best) at = lane + 32 * v, val = x[v];
+          if (key[v] == best) at = lane + 32 * v, val = x[u][v];
         const int e = __reduce_min_sync(0xffffffffu, at);
         val = __shfl_sync(0xffffffffu, val, e & 31);
 #pragma unroll
@@ -97,26 +142,26 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
         if (j == 0) {
           top = val;
           if (!p.renormalize) {
-            float s = 0.f;
+            float all = 0.f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) s += route_exp(x[v], top);
-            total = warp_sum(s);
+            for (int v = 0; v < V; ++v) all += route_exp(x[u][v], top);
+            sum = warp_sum(all);
           }
         }
-        const float w = route_exp(val, top);
-        if (p.renormalize) total += w;
-        if (lane == j) mine = w, my_expert = e;
+        if (lane == j) mine = val, my_expert = e;
       }
+      mine = my_expert >= 0 ? route_exp(mine, top) : 0.f;
+      if (p.renormalize) sum = warp_sum(mine);
       if (lane < p.k) {
         p.expert[t * p.k + lane] = my_expert;
-        p.gate[t * p.k + lane] = my_expert >= 0 ? mine / total : 0.f;
+        p.gate[t * p.k + lane] = my_expert >= 0 ? mine / sum : 0.f;
         if (my_expert >= 0)
           atomicOr(&mask[my_expert * kRouteWords + (i >> 5)], 1u << (i & 31));
       }
     }
     __syncthreads();
     for (int i = tid; i < n * p.k; i += kRouteThreads) {
-      const long long at = c0 * p.k + i;
+      const int at = c0 * p.k + i;
       const int e = p.expert[at], r = i / p.k;
       int rank = -1;
       if (e >= 0) {
@@ -138,8 +183,14 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
     }
     __syncthreads();
   }
-  for (int e = tid; e < p.E; e += kRouteThreads)
-    p.counts[static_cast<long long>(blockIdx.x) * p.E + e] = count[e];
+  if (gridDim.x > 1) {
+    for (int e = tid; e < p.E; e += kRouteThreads) p.counts[blockIdx.x * p.E + e] = count[e];
+    return;
+  }
+  if (warp == 0) scan_experts(count, p.E, base, &total);
+  __syncthreads();
+  for (int e = tid; e <= p.E; e += kRouteThreads) p.offsets[e] = e < p.E ? base[e] : total;
+  place_items(p, base, total, t0 * p.k, t1 * p.k);
 }
 
 // Adds up the counts: an expert's first slot, and within it this CTA's; then turns
@@ -149,53 +200,43 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_place_kernel(
   __shared__ int base[kMaxExperts], all[kMaxExperts];
   __shared__ int total;
   const int tid = threadIdx.x;
+  for (int e = tid; e < p.E; e += kRouteThreads) base[e] = all[e] = 0;
   pdl_wait();
   pdl_launch_dependents();
-  if (tid < p.E) {
+  __syncthreads();
+  // thread: expert tid % E of every (threads / E)-th CTA; whole numbers, any order
+  const int per = kRouteThreads / p.E, e = tid % p.E, g = tid / p.E;
+  if (g < per) {
     int before = 0, sum = 0;
-    for (unsigned c = 0; c < gridDim.x; ++c) {
-      const int v = __ldcg(p.counts + static_cast<long long>(c) * p.E + tid);
-      if (c < blockIdx.x) before += v;
+#pragma unroll 8
+    for (int c = g; c < static_cast<int>(gridDim.x); c += per) {
+      const int v = __ldcg(p.counts + c * p.E + e);
+      before += c < static_cast<int>(blockIdx.x) ? v : 0;
       sum += v;
     }
-    base[tid] = before;
-    all[tid] = sum;
+    if (before != 0) atomicAdd(&base[e], before);
+    if (sum != 0) atomicAdd(&all[e], sum);
   }
   __syncthreads();
-  if (tid == 0) {
-    int run = 0;
-    for (int e = 0; e < p.E; ++e) {
-      base[e] += run;
-      if (blockIdx.x == 0) p.offsets[e] = run;
-      run += all[e];
-    }
-    if (blockIdx.x == 0) p.offsets[p.E] = run;
-    total = run;
-  }
+  if (tid < 32) scan_experts(all, p.E, base, &total);
   __syncthreads();
-  const long long i0 = static_cast<long long>(blockIdx.x) * p.per_cta * p.k;
-  const long long i1 = min(i0 + static_cast<long long>(p.per_cta) * p.k, p.T * p.k);
-  for (long long i = i0 + tid; i < i1; i += kRouteThreads) {
-    const int e = p.expert[i];
-    if (e >= 0) {
-      const int s = base[e] + p.slot[i];
-      p.slot[i] = s;
-      p.token[s] = static_cast<int>(i / p.k);
-    }
-    if (i >= total) p.token[i] = -1;
-  }
+  if (blockIdx.x == 0)   // its own slots begin where the experts' do
+    for (int o = tid; o <= p.E; o += kRouteThreads) p.offsets[o] = o < p.E ? base[o] : total;
+  const int i0 = blockIdx.x * p.per_cta * p.k;
+  const int i1 = static_cast<int>(min(static_cast<long long>(i0) + p.per_cta * p.k, p.T * p.k));
+  place_items(p, base, total, i0, i1);
 }
 
 // d logits of the gates.  With inner = sum_j g_j dg_j: at a chosen expert
 // g_j (dg_j - inner) and 0 elsewhere (renormalize), or p_e ([e chosen] dg_e - inner)
 // with p the softmax over all E.  A token without a choice has gradient 0.
 template <int V>
-__global__ void __launch_bounds__(kRouteThreads) sc_route_back_kernel(
+__global__ void __launch_bounds__(kRouteBackThreads) sc_route_back_kernel(
     const __grid_constant__ RouteBackParams p) {
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const long long t = static_cast<long long>(blockIdx.x) * (kRouteThreads / 32) + (threadIdx.x >> 5);
+  const long long t = static_cast<long long>(blockIdx.x) * (kRouteBackThreads / 32) + (threadIdx.x >> 5);
   if (t >= p.T) return;
   const bool in = token_in_use(p.rows, p.L, t);
   int e = -1;
@@ -257,22 +298,22 @@ int route_ctas(long long T, int* per_cta) {
 cudaError_t launch_route(const RouteParams& in, cudaStream_t st) {
   RouteParams p = in;
   const int ctas = route_ctas(p.T, &p.per_cta);
-  const size_t smem = static_cast<size_t>(p.E) * (kRouteWords + 1) * 4;
+  const size_t smem = static_cast<size_t>(p.E) * kRouteWords * 4;
   auto choose = p.E <= 32 ? sc_route_choose_kernel<1>
                 : p.E <= 64 ? sc_route_choose_kernel<2>
                 : p.E <= 128 ? sc_route_choose_kernel<4> : sc_route_choose_kernel<8>;
   const cudaError_t e = launch_chained(choose, dim3(ctas), dim3(kRouteThreads), smem, st, p);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || ctas == 1) return e;
   return launch_chained(sc_route_place_kernel, dim3(ctas), dim3(kRouteThreads), 0, st, p);
 }
 
 cudaError_t launch_route_back(const RouteBackParams& p, cudaStream_t st) {
-  constexpr int per = kRouteThreads / 32;
+  constexpr int per = kRouteBackThreads / 32;
   const dim3 grid(static_cast<unsigned>((p.T + per - 1) / per));
   auto k = p.E <= 32 ? sc_route_back_kernel<1>
            : p.E <= 64 ? sc_route_back_kernel<2>
            : p.E <= 128 ? sc_route_back_kernel<4> : sc_route_back_kernel<8>;
-  return launch_chained(k, grid, dim3(kRouteThreads), 0, st, p);
+  return launch_chained(k, grid, dim3(kRouteBackThreads), 0, st, p);
 }
 
 }  // namespace sc

@@ -460,6 +460,7 @@ def combine_ref(c, gated, scale, res):
 COMBINE = [
     (1, 1, 8, 1, None), (1, 1, 768, 2, None), (2, 9, 64, 2, [9, 4]), (3, 33, 136, 3, [0, 33, 1]),
     (1, 70, 1024, 8, None), (2, 40, 1032, 4, [40, 39]), (1, 5, 8192, 2, None), (4, 500, 768, 2, [500, 1, 0, 321]),
+    (1, 3, 8192, 8, None), (1, 700, 520, 3, [699]),
 ]
 
 
