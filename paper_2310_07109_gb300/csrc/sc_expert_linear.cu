@@ -845,6 +845,63 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   if (tid == 0 && sm.abort) atomicOr(p.status, kExpertTimeout);
 }
 
+// Forward with few slots (single tokens being served): the weights' rows are all there is
+// to read and the pair kernel's set-up and pipeline latency most of its time.  One warp
+// per two features of a slot reads them once, 16 bytes a lane; slots of the same expert
+// read them again, from the L2.
+constexpr int kFewSlots = 16;
+constexpr int kFewThreads = 256;
+constexpr int kFewFeatures = 2;
+
+__global__ void __launch_bounds__(kFewThreads) sc_expert_few_kernel(
+    const __grid_constant__ ExpertLinearParams p) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = blockIdx.y;
+  const int n = (blockIdx.x * (kFewThreads / 32) + warp) * kFewFeatures;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (n >= p.N) return;
+  int e = -1;
+  for (int e0 = 0; e0 < p.E && e < 0; e0 += 32) {
+    int lo = 0, hi = 0;
+    if (e0 + lane < p.E) expert_range(p, e0 + lane, lo, hi);
+    const uint32_t has = __ballot_sync(0xffffffffu, s >= lo && s < hi);
+    if (has != 0u) e = e0 + __ffs(has) - 1;
+  }
+  if (e < 0) return;   // a slot that is not in use
+  const uint4* x = reinterpret_cast<const uint4*>(p.x + expert_row(p, s) * p.ldx);
+  const uint4* w = reinterpret_cast<const uint4*>(p.w + (static_cast<size_t>(e) * p.N + n) * p.K);
+  const int vecs = p.K / 8;
+  float a[kFewFeatures] = {};
+#pragma unroll 4
+  for (int i = lane; i < vecs; i += 32) {
+    const uint4 xv = __ldg(x + i);
+    const uint32_t xs[4] = {xv.x, xv.y, xv.z, xv.w};
+#pragma unroll
+    for (int f = 0; f < kFewFeatures; ++f) {
+      const uint4 wv = __ldg(w + f * vecs + i);
+      const uint32_t ws[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        a[f] = fmaf(bf_lo(xs[q]), bf_lo(ws[q]), a[f]);
+        a[f] = fmaf(bf_hi(xs[q]), bf_hi(ws[q]), a[f]);
+      }
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < kFewFeatures; ++f)
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) a[f] += __shfl_xor_sync(0xffffffffu, a[f], off);
+  if (lane != 0) return;
+  if (p.bias != nullptr)
+#pragma unroll
+    for (int f = 0; f < kFewFeatures; ++f) a[f] += __ldg(p.bias + static_cast<size_t>(e) * p.N + n + f);
+  const size_t at = static_cast<size_t>(s) * p.N + n;
+  if (p.pre != nullptr) *reinterpret_cast<uint32_t*>(p.pre + at) = pack_bf16x2(a[0], a[1]);
+  if (p.gelu) gelu2(a[0], a[1]);
+  if (p.out_f32) *reinterpret_cast<float2*>(static_cast<float*>(p.out) + at) = make_float2(a[0], a[1]);
+  else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack_bf16x2(a[0], a[1]);
+}
+
 // ---------------------------------------------------------------------------
 // launch
 // ---------------------------------------------------------------------------
@@ -907,6 +964,10 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
 }
 
 cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p, cudaStream_t st) {
+  if (what == ExpertProduct::kForward && p.M <= kFewSlots) {
+    constexpr int per = kFewThreads / 32 * kFewFeatures;
+    return launch_chained(sc_expert_few_kernel, dim3((p.N + per - 1) / per, p.M), dim3(kFewThreads), 0, st, p);
+  }
   PairParams P;
   P.p = p;
   const bool gather = p.token != nullptr;
