@@ -44,29 +44,38 @@ constexpr uint32_t kPairABytes = kPairM * kPairStep * 2;
 constexpr uint32_t kPairBBytes = kPairN / 2 * kPairStep * 2;
 constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes;
 constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN-major operand
-// Write-back areas per warp.  Forward: 4 KB, a chunk in fp32, or the output and the value
-// before GELU in bf16.  Back (weight): two of these, the copy of one on its way while the
-// other is filled.  Back (input): 2 KB for the output (fp32: 4) and a ring of two 2 KB
-// chunks (fp32: one) of the value before GELU, copied ahead across tiles: behind the
-// copies of the operands a load waits 3000 cycles.
-constexpr uint32_t kPreBytes = 2048;
-
-template <ExpertProduct kWhat>
-__host__ __device__ constexpr int pair_epi_warps() {
-  return kWhat == ExpertProduct::kBackWeight ? 8 : 16;
-}
-template <ExpertProduct kWhat>
-__host__ __device__ constexpr int pair_stages() {
-  return kWhat == ExpertProduct::kBackInput ? 4 : kPairMaxStages;
-}
-template <ExpertProduct kWhat>
-__host__ __device__ constexpr uint32_t pair_out_bytes() {
-  return kWhat == ExpertProduct::kBackInput ? 6144 : kWhat == ExpertProduct::kForward ? 4096 : 8192;
-}
-template <ExpertProduct kWhat>
-__host__ __device__ constexpr uint32_t pair_dyn() {
-  return pair_stages<kWhat>() * kPairStageBytes + pair_epi_warps<kWhat>() * pair_out_bytes<kWhat>() + 1024;
-}
+// The tensor cores add to an fp32 accumulator with truncation, half a unit in the last
+// place per 16 of the contraction: 2048 slots, 3.7e-6.  bf16 outputs do not show it.  For
+// fp32 outputs an accumulator takes kSpan stages (256 of the contraction) only; eight
+// write-back warps add it, rounded, to sums in their registers (128 a thread).
+constexpr int kSpan = 4;
+template <ExpertProduct kWhat, bool kGather_, bool kF32_>
+struct PairKind {
+  static constexpr bool kFwd = kWhat == ExpertProduct::kForward;
+  static constexpr bool kBackX = kWhat == ExpertProduct::kBackInput;
+  static constexpr bool kBackW = kWhat == ExpertProduct::kBackWeight;
+  static constexpr bool kGather = kGather_, kF32 = kF32_;
+  static constexpr int kSteps = kF32 ? kSpan : 1 << 30;   // stages an accumulator takes
+  // Warps: four (copies, products), the write-back, four that gather, four that sum dy.
+  static constexpr int kEpiWarps = kBackW || kF32 ? 8 : 16;
+  static constexpr int kGatherWarp = 4 + kEpiWarps, kSumWarp = kGatherWarp + (kGather ? 4 : 0);
+  static constexpr int kThreads = 32 * (kSumWarp + (kBackW ? 4 : 0));
+  // Registers of the write-back warps, and of the others, where the sums need them: what
+  // 65536 registers (61440 with 640 threads) leave.
+  static constexpr int kEpiRegs = kThreads <= 384 ? 208 : kThreads <= 512 ? 200 : 168;
+  static constexpr int kOtherRegs = kThreads <= 384 ? 88 : kThreads <= 512 ? 56 : 48;
+  // Write-back areas per warp.  Forward: a chunk of the output (bf16 2 KB, fp32 4) and one
+  // of the value before GELU.  Back (weight): two chunks of 4 KB, the copy of one on its
+  // way while the other is filled.  Back (input): a chunk of the output and a ring of two
+  // chunks of the value before GELU, copied ahead across tiles: behind the copies of the
+  // operands a load waits 3000 cycles.
+  static constexpr uint32_t kChunkBytes = kF32 || kBackW ? 4096 : 2048;
+  static constexpr uint32_t kPreBytes = 2048;
+  static constexpr uint32_t kOutBytes =
+      kBackW || kF32 ? 8192 : kBackX ? kChunkBytes + 2 * kPreBytes : kChunkBytes + kPreBytes;
+  static constexpr int kStages = kBackX && !kF32 ? 4 : kPairMaxStages;
+  static constexpr uint32_t kDyn = kStages * kPairStageBytes + kEpiWarps * kOutBytes + 1024;
+};
 
 struct PairParams {
   ExpertLinearParams p;
@@ -90,10 +99,6 @@ struct PairSmem {
   };
   uint8_t order[kMaxExperts];   // weight gradient: experts by decreasing number of slots
 };
-
-static_assert(sizeof(PairSmem) + pair_dyn<ExpertProduct::kForward>() <= 227 * 1024 &&
-                  sizeof(PairSmem) + pair_dyn<ExpertProduct::kBackInput>() <= 227 * 1024,
-              "one CTA's shared memory");
 
 __device__ __forceinline__ float bf(uint16_t v) {
   return __uint_as_float(static_cast<uint32_t>(v) << 16);
@@ -276,19 +281,14 @@ __device__ __forceinline__ void put_chunk(const CUtensorMap& map, void* out, con
   }
 }
 
-template <ExpertProduct kWhat, bool kGather>
-__host__ __device__ constexpr int pair_threads() {
-  return 128 + 32 * pair_epi_warps<kWhat>() + (kGather ? 128 : 0) +
-         (kWhat == ExpertProduct::kBackWeight ? 128 : 0);
-}
-
-template <ExpertProduct kWhat, bool kGather>
-__global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_pair_kernel(
-    const __grid_constant__ PairParams P) {
-  constexpr bool kFwd = kWhat == ExpertProduct::kForward;
-  constexpr bool kBackX = kWhat == ExpertProduct::kBackInput;
-  constexpr bool kBackW = kWhat == ExpertProduct::kBackWeight;
-  constexpr int kStages = pair_stages<kWhat>();
+template <ExpertProduct kWhat, bool kGather, bool kF32>
+__global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
+    sc_expert_pair_kernel(const __grid_constant__ PairParams P) {
+  using Kind = PairKind<kWhat, kGather, kF32>;
+  constexpr bool kFwd = Kind::kFwd, kBackX = Kind::kBackX, kBackW = Kind::kBackW;
+  constexpr int kStages = Kind::kStages, kEpiWarps = Kind::kEpiWarps, kGroups = kEpiWarps / 4;
+  constexpr int kGatherWarp = Kind::kGatherWarp, kSumWarp = Kind::kSumWarp;
+  static_assert(sizeof(PairSmem) + Kind::kDyn <= 227 * 1024, "one CTA's shared memory");
   const ExpertLinearParams& p = P.p;
   extern __shared__ uint8_t dyn_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) &
@@ -297,8 +297,6 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = static_cast<int>(cluster_rank());
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  constexpr int kEpiWarps = pair_epi_warps<kWhat>(), kGroups = kEpiWarps / 4;
-  constexpr int kGatherWarp = 4 + kEpiWarps, kSumWarp = kGatherWarp + (kGather ? 4 : 0);   // first of four
   const bool sums = kBackW && p.dbias != nullptr;
 
   if (tid == 0) {
@@ -368,258 +366,12 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
   PairTile g;
   g.e = 0;
 
-  if (warp == 0) {
-    // ------------------------------------------------------------- copies
-    bool ok = true;
-    int s = 0, use = 0;
-    for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-      pair_tile<kWhat>(p, sm, t, g);
-      const int steps = pair_steps<kWhat>(p, g);
-      const int f = g.f0 + rank * kPairM;             // this CTA's features
-      const int half = kBackW ? kPairN / 2 : g.width / 2;
-      const int b0 = g.i0 + rank * half;              // ... and its columns of the tile
-      const uint32_t bytes = kPairABytes + (kGather ? 0 : half * kPairStep * 2);
-#pragma unroll 1
-      for (int kt = 0; kt < steps; ++kt) {
-        if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
-        const uint32_t a = ring + s * kPairStageBytes, b = a + kPairABytes;
-        const uint32_t full = dsmem_addr(smem_u32(&sm.full[s]), 0);
-        const int c0 = kt * kPairStep;
-        if (kBackW && g.lo + c0 + kPairStep > g.hi) {
-          copy_partial(a, p.dy, p.ldy, f, p.N, g.lo + c0, g.hi);
-          if constexpr (!kGather) copy_partial(b, p.x, p.ldx, b0, p.K, g.lo + c0, g.hi);
-          cp_async_wait_all();
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(full);
-        } else if (lane == 0) {
-          mbar_arrive_expect_tx_cluster(full, bytes);
-          if constexpr (kFwd) {
-            tma_load_3d_pair(a, &P.map_a, c0, f, g.e, full);
-          } else if constexpr (kBackX) {
-            tma_load_3d_pair(a, &P.map_a, f, c0, g.e, full);
-            tma_load_3d_pair(a + kPairBoxBytes, &P.map_a, f + 64, c0, g.e, full);
-          } else {
-            tma_load_2d_pair(a, &P.map_a, f, g.lo + c0, full);
-            tma_load_2d_pair(a + kPairBoxBytes, &P.map_a, f + 64, g.lo + c0, full);
-          }
-          if constexpr (!kGather) {
-            if constexpr (kBackW) {
-              tma_load_2d_pair(b, &P.map_b, b0, g.lo + c0, full);
-              tma_load_2d_pair(b + kPairBoxBytes, &P.map_b, b0 + 64, g.lo + c0, full);
-            } else if (half == kPairN / 2) {
-              tma_load_2d_pair(b, &P.map_b, c0, g.lo + b0, full);
-            } else {
-              for (int q = 0; q < half; q += 32)
-                tma_load_2d_pair(b + q * 128, &P.map_b32, c0, g.lo + b0 + q, full);
-            }
-          }
-        }
-        __syncwarp();
-        if (++s == kStages) {
-          s = 0;
-          ++use;
-        }
-      }
-    }
-    // every stage's products are done, and their arrivals have come, before this CTA ends
-#pragma unroll 1
-    for (int q = 0; q < kStages; ++q) {
-      const int fills = use + (q < s ? 1 : 0);
-      if (fills > 0) warp_wait(&sm.empty[q], (fills - 1) & 1, abort_flag);
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------- products
-    if (rank == 0 && elect_one()) {
-      bool ok = true;
-      int s = 0, use = 0, j = 0;
-      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-        pair_tile<kWhat>(p, sm, t, g);
-        const int steps = pair_steps<kWhat>(p, g);
-        if (steps == 0) continue;
-        const int acc = j & 1;
-        if (j >= 2 && !(ok = mbar_wait_poll(&sm.tempty[acc], ((j >> 1) - 1) & 1, abort_flag))) break;
-        tc_fence_after();
-        const uint32_t d = tm + acc * kPairN;
-        const uint32_t idesc = idesc_bf16(256, kBackW ? kPairN : g.width, !kFwd, kBackW);
-        // low descriptor words: K-major operands advance 32 bytes per 16 of the
-        // contraction, MN-major ones two groups of eight 128-byte rows; their other
-        // 64-feature boxes lie 8 KB apart
-        constexpr uint32_t kFar = (kPairBoxBytes >> 4) << 16, kNear = 1u << 16;
-        constexpr uint32_t kStepA = kFwd ? 2 : 128, kStepB = kBackW ? 128 : 2;
-#pragma unroll 1
-        for (int kt = 0; kt < steps; ++kt) {
-          if (!(ok = mbar_wait_poll(&sm.full[s], use & 1, abort_flag))) break;
-          if (kGather || (kBackW && g.lo + (kt + 1) * kPairStep > g.hi)) {
-            fence_proxy_async_smem();   // written by threads
-          }
-          tc_fence_after();
-          const uint32_t at = ring + s * kPairStageBytes;
-          const uint32_t a = (at >> 4) | (kFwd ? kNear : kFar);
-          const uint32_t b = ((at + kPairABytes) >> 4) | (kBackW ? kFar : kNear);
-#pragma unroll
-          for (int k = 0; k < kPairStep / 16; ++k)
-            umma_bf16_pair_lo(d, a + kStepA * k, b + kStepB * k, idesc, (kt | k) != 0);
-          umma_commit_pair(sums ? &sm.done[s] : &sm.empty[s]);
-          if (++s == kStages) {
-            s = 0;
-            ++use;
-          }
-        }
-        umma_commit_pair(&sm.tfull[acc]);
-        ++j;
-      }
-    }
-    __syncwarp();
-  } else if (kGather && warp >= kGatherWarp && warp < kGatherWarp + 4) {
-    // ------------------------------------------------------------- gathered rows
-    // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
-    // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
-    const int l = tid - 32 * kGatherWarp;
-    constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
-    const int c = l % kPieces, r0 = l / kPieces;
-    bool ok = true;
-    int s = 0, use = 0;
-    for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-      pair_tile<kWhat>(p, sm, t, g);
-      const int steps = pair_steps<kWhat>(p, g);
-      const int half = kBackW ? kPairN / 2 : g.width / 2;
-      const int b0 = g.i0 + rank * half;
-      const uint16_t* src[8];
-      // weight gradient: the 16 rows that this warp copies of each of eight stages, two
-      // stages a register; those of the eight after them are loaded meanwhile (a load
-      // waits up to 3000 cycles behind the operands: two stages ahead 62 us, not 41)
-      int row[4], row_next[4];
-      const auto load_rows = [&](int kt) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
-          row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
-        }
-      };
-      if constexpr (kFwd) {
-        // columns past the tile repeat its last slot
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          src[i] = p.x + 8 * c +
-                   p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
-      } else {
-        load_rows(0);
-      }
-#pragma unroll 1
-      for (int kt = 0; kt < steps; ++kt) {
-        if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
-        const uint32_t b = ring + s * kPairStageBytes + kPairABytes;
-        const int c0 = kt * kPairStep;
-        if constexpr (kFwd) {
-          const bool in = c0 + 8 * c < p.K;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (r0 + kRowStep * i < half)
-              cp_async16(b + sw128_offset(r0 + kRowStep * i, c), src[i] + (in ? c0 : 0), in);
-        } else {
-          const int col = b0 + 8 * c;
-          if (kt % 8 == 0) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) row[i] = row_next[i];
-            load_rows(kt + 8);
-          }
-          const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = r0 + kRowStep * i;
-            const int at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
-            const bool in = g.lo + c0 + r < g.hi && col < p.K;
-            cp_async16(b + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7),
-                       p.x + (in ? at * p.ldx + col : 0), in);
-          }
-        }
-        cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
-        if (++s == kStages) {
-          s = 0;
-          ++use;
-        }
-      }
-    }
-    cp_async_wait_all();
-  } else if (kGather && warp == 2) {
-    // ------------------------------------------------------------- gathered rows handed over
-    // What threads write to shared memory is ordered before the products by the proxy
-    // fence.  Only the signal crosses to the even CTA: the rows are read where they lie,
-    // by their own CTA's tensor core, so nothing has to become visible outside the CTA
-    // (a release over the cluster for each stage takes twice the time: 69 us, not 35).
-    if (elect_one()) {
-      bool ok = true;
-      int s = 0, use = 0;
-      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-        pair_tile<kWhat>(p, sm, t, g);
-        const int steps = pair_steps<kWhat>(p, g);
-#pragma unroll 1
-        for (int kt = 0; kt < steps; ++kt) {
-          if (!(ok = mbar_wait_poll(&sm.landed[s], use & 1, abort_flag))) break;
-          fence_proxy_async_smem();
-          mbar_arrive_cluster(dsmem_addr(smem_u32(&sm.full[s]), 0));
-          if (++s == kStages) {
-            s = 0;
-            ++use;
-          }
-        }
-      }
-    }
-    __syncwarp();
-  } else if (kBackW && warp >= kSumWarp) {
-    // ------------------------------------------------------------- bias sums
-    // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
-    // the 64 slots.
-    if (sums) {
-      const int l = tid - 32 * kSumWarp, w = l >> 5;
-      bool ok = true;   // no early exit: the four warps meet at every tile with a sum
-      int s = 0, use = 0;
-      for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-        pair_tile<kWhat>(p, sm, t, g);
-        const int steps = pair_steps<kWhat>(p, g);
-        float a[4] = {};
-#pragma unroll 1
-        for (int kt = 0; kt < steps; ++kt) {
-          ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
-          if (ok && g.i0 == 0) {
-            const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const uint2 v = *reinterpret_cast<const uint2*>(at + sw128_offset(16 * w + i, (lane & 15) >> 1));
-              a[0] += bf_lo(v.x);
-              a[1] += bf_hi(v.x);
-              a[2] += bf_lo(v.y);
-              a[3] += bf_hi(v.y);
-            }
-          }
-          warp_arrive(&sm.empty[s]);
-          if (++s == kStages) {
-            s = 0;
-            ++use;
-          }
-        }
-        if (g.i0 == 0) {
-          float4& mine = *reinterpret_cast<float4*>(&sm.sums[w & 1][4 * lane]);
-          if (w >= 2) mine = make_float4(a[0], a[1], a[2], a[3]);
-          asm volatile("bar.sync 3, 128;" ::: "memory");
-          if (w < 2)
-            mine = make_float4(a[0] + mine.x, a[1] + mine.y, a[2] + mine.z, a[3] + mine.w);
-          asm volatile("bar.sync 3, 128;" ::: "memory");
-          const int n = g.f0 + rank * kPairM + l;
-          if (ok && n < p.N)
-            p.dbias[static_cast<size_t>(g.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
-          asm volatile("bar.sync 3, 128;" ::: "memory");
-        }
-      }
-    }
-  } else if (warp >= 4 && warp < 4 + kEpiWarps) {
+  if (warp >= 4 && warp < 4 + kEpiWarps) {
+    if constexpr (kF32) regs_alloc<Kind::kEpiRegs>();
     // ------------------------------------------------------------- write back
     const int q = warp & 3, grp = (warp - 4) >> 2;
-    uint8_t* const stg = base + kStages * kPairStageBytes + (warp - 4) * pair_out_bytes<kWhat>();
-    // back (input): the ring
-    const int pre_slots = p.out_f32 ? 1 : 2;
-    uint8_t* const ring_pre = stg + (p.out_f32 ? 4096 : 2048);
+    uint8_t* const stg = base + kStages * kPairStageBytes + (warp - 4) * Kind::kOutBytes;
+    uint8_t* const stg_pre = stg + Kind::kChunkBytes;   // forward: of the value before GELU; back (input): ring
     const int pr = lane >> 2, px = lane & 3;   // this lane's 16-byte piece of columns pr + 8 k
     const int mi = lane >> 3;                  // fragment whose row address this lane gives
     const uint32_t tempty0 = dsmem_addr(smem_u32(&sm.tempty[0]), 0);
@@ -644,7 +396,7 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       }
       if (ht < tiles) {
         const int x = ahead.f0 + rank * kPairM + 32 * q + 8 * px;
-        const uint32_t to = smem_u32(ring_pre + slot_in * kPreBytes);
+        const uint32_t to = smem_u32(stg_pre + slot_in * Kind::kPreBytes);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int r = 8 * k + pr;
@@ -654,11 +406,12 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
         }
       }
       cp_async_commit();
-      slot_in = slot_in + 1 == pre_slots ? 0 : slot_in + 1;
+      slot_in ^= 1;
     };
-    if (kBackX && p.pre_in != nullptr)
-#pragma unroll 1
-      for (int i = 0; i < pre_slots; ++i) copy_pre();
+    if (kBackX && p.pre_in != nullptr) {
+      copy_pre();
+      copy_pre();
+    }
     // forward: a tile's bias is loaded during the tile before
     float bias[2][2] = {}, bias_next[2][2] = {};
     const auto load_bias = [&](const PairTile& g1) {
@@ -674,10 +427,107 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
       pair_tile<kWhat>(p, sm, pair, ahead);
       load_bias(ahead);
     }
+    // weight gradient: 32 rows (features) of 32 columns, contiguous in memory, from column c
+    const auto put_rows = [&](int f, int c, const float (&v)[32]) {
+      uint8_t* const to = next_area();
+      if constexpr (kF32) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 4)
+          stage_row_piece<8>(to, k / 4,
+                             make_uint4(__float_as_uint(v[k]), __float_as_uint(v[k + 1]),
+                                        __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3])));
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; k += 8)
+          stage_row_piece<4>(to, k / 8,
+                             make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
+                                        pack_bf16x2(v[k + 4], v[k + 5]), pack_bf16x2(v[k + 6], v[k + 7])));
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(to));   // cut at N and K
+        bulk_commit();
+      }
+    };
+    // forward, back (input): 32 rows (features) of the 32 columns (slots) from c, in
+    // fragments, transposed on the way out
+    const auto put_columns = [&](int f, int c, float (&v)[2][16]) {
+      const int width = features<kWhat>(p), slot0 = g.lo + g.i0 + c, left = g.n - c;
+      // where this lane's row of fragment pair (h, b) is staged
+      const auto at = [&](int h, int b) {
+        return stage_offset<4>(8 * (b + (mi >> 1)) + (lane & 7), 2 * h + (mi & 1));
+      };
+      const auto store = [&](uint8_t* area) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < 4; b += 2) {
+            const float* w = v[h] + 4 * b;
+            stmatrix4_trans(smem_u32(area + at(h, b)), pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3]),
+                            pack_bf16x2(w[4], w[5]), pack_bf16x2(w[6], w[7]));
+          }
+      };
+      if (kBackX && p.pre_in != nullptr) {
+        // in the staging's layout, so that its fragments match the accumulator's
+        uint32_t zf[2][2][4];
+        cp_async_wait<1>();
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < 4; b += 2)
+            ldmatrix4_trans(smem_u32(stg_pre + slot_out * Kind::kPreBytes + at(h, b)), zf[h][b / 2]);
+        __syncwarp();
+        slot_out ^= 1;
+        copy_pre();
+        if (!kF32) tmem_ld_wait();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t x = zf[h][k >> 2][k & 3];
+            gelu_slope2(bf_lo(x), bf_hi(x), v[h][2 * k], v[h][2 * k + 1]);
+          }
+      } else if (!kF32) {
+        tmem_ld_wait();
+      }
+      if constexpr (kFwd) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[h][k] += bias[h][(k >> 1) & 1];
+      }
+      uint8_t* const to = next_area();
+      if constexpr (kFwd) {
+        if (p.pre != nullptr) store(stg_pre);
+        if (p.gelu)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) gelu2(v[h][k], v[h][k + 1]);
+      }
+      if constexpr (kF32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const int r = 8 * (k >> 2) + 2 * (lane & 3) + (k & 1);
+            const int n = 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
+            *reinterpret_cast<float*>(to + stage_offset<8>(r, n >> 2) + 4 * (n & 3)) = v[h][k];
+          }
+      } else {
+        store(to);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      put_chunk<kF32>(P.map_out, p.out, to, slot0, left, f, width, ok);
+      if (kFwd && p.pre != nullptr) put_chunk<false>(P.map_pre, p.pre, stg_pre, slot0, left, f, width, ok);
+      if (lane == 0) bulk_commit();
+    };
     for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
       pair_tile<kWhat>(p, sm, t, g);
       const int steps = pair_steps<kWhat>(p, g);
-      const int acc = j & 1;
       const int f = g.f0 + rank * kPairM + 32 * q;   // this warp's features
       if (kFwd && p.bias != nullptr) {
 #pragma unroll
@@ -687,152 +537,335 @@ __global__ void __launch_bounds__(pair_threads<kWhat, kGather>(), 1) sc_expert_p
           load_bias(ahead);
         }
       }
-      if (steps > 0) ok = ok && warp_wait(&sm.tfull[acc], (j >> 1) & 1, abort_flag);
-      tc_fence_after();
-      const uint32_t d = tm + acc * kPairN + (static_cast<uint32_t>(32 * q) << 16);
-      if constexpr (kBackW) {
-        // rows are features, columns contiguous in memory
-#pragma unroll 1
-        for (int c = kPairChunk * grp; ok && f < p.N && c < g.n; c += kGroups * kPairChunk) {
-          float v[32];
-          if (steps > 0) {
-            tmem_ld32(d + c, v);
-            tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = 0.f;   // an expert without slots
-          }
-          uint8_t* const to = next_area();
-          if (p.out_f32) {
-#pragma unroll
-            for (int k = 0; k < 32; k += 4)
-              stage_row_piece<8>(to, k / 4,
-                                 make_uint4(__float_as_uint(v[k]), __float_as_uint(v[k + 1]),
-                                            __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3])));
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; k += 8)
-              stage_row_piece<4>(to, k / 8,
-                                 make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
-                                            pack_bf16x2(v[k + 4], v[k + 5]),
-                                            pack_bf16x2(v[k + 6], v[k + 7])));
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(to));   // cut at N and K
-            bulk_commit();
-          }
-        }
-      } else {
-        // rows are features, columns slots: transposed on the way out
-        const int width = features<kWhat>(p);
-        const int slot0 = g.lo + g.i0;
-#pragma unroll 1
-        for (int c = kPairChunk * grp; c < g.n; c += kGroups * kPairChunk) {
-          float v[2][16];
-          tmem_ld_frag32(d + c, v[0]);
-          tmem_ld_frag32(d + c + (16u << 16), v[1]);
-          // where this lane's row of fragment pair (h, b) is staged
-          const auto at = [&](int h, int b) {
-            return stage_offset<4>(8 * (b + (mi >> 1)) + (lane & 7), 2 * h + (mi & 1));
-          };
-          const auto store = [&](uint8_t* area) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int b = 0; b < 4; b += 2) {
-                const float* w = v[h] + 4 * b;
-                stmatrix4_trans(smem_u32(area + at(h, b)), pack_bf16x2(w[0], w[1]),
-                                pack_bf16x2(w[2], w[3]), pack_bf16x2(w[4], w[5]),
-                                pack_bf16x2(w[6], w[7]));
-              }
-          };
-          if (kBackX && p.pre_in != nullptr) {
-            // in the staging's layout, so that its fragments match the accumulator's
-            uint32_t zf[2][2][4];
-            if (pre_slots == 2) cp_async_wait<1>();
-            else cp_async_wait<0>();
-            __syncwarp();
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int b = 0; b < 4; b += 2)
-                ldmatrix4_trans(smem_u32(ring_pre + slot_out * kPreBytes + at(h, b)), zf[h][b / 2]);
-            __syncwarp();
-            slot_out = slot_out + 1 == pre_slots ? 0 : slot_out + 1;
-            copy_pre();
-            tmem_ld_wait();
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const uint32_t x = zf[h][k >> 2][k & 3];
-                gelu_slope2(bf_lo(x), bf_hi(x), v[h][2 * k], v[h][2 * k + 1]);
-              }
-          } else {
-            tmem_ld_wait();
-          }
-          if constexpr (kFwd) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int k = 0; k < 16; ++k) v[h][k] += bias[h][(k >> 1) & 1];
-          }
-          uint8_t* const to = next_area();
-          if constexpr (kFwd) {
-            if (p.pre != nullptr) store(to + (p.out_f32 ? 0 : 2048));
-            if (p.pre != nullptr && p.out_f32) {
-              // no room for both: the value before GELU leaves first
-              fence_proxy_async_smem();
-              __syncwarp();
-              put_chunk<false>(P.map_pre, p.pre, to, slot0 + c, g.n - c, f, width, ok);
-              if (lane == 0) {
-                bulk_commit();
-                bulk_wait_read<0>();
-              }
-              __syncwarp();
-            }
-            if (p.gelu)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 16; k += 2) gelu2(v[h][k], v[h][k + 1]);
-          }
-          if (p.out_f32) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                const int r = 8 * (k >> 2) + 2 * (lane & 3) + (k & 1);
-                const int n = 16 * h + 8 * ((k >> 1) & 1) + lane / 4;
-                *reinterpret_cast<float*>(to + stage_offset<8>(r, n >> 2) + 4 * (n & 3)) = v[h][k];
-              }
-          } else {
-            store(to);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (p.out_f32) {
-            put_chunk<true>(P.map_out, p.out, to, slot0 + c, g.n - c, f, width, ok);
-          } else {
-            put_chunk<false>(P.map_out, p.out, to, slot0 + c, g.n - c, f, width, ok);
-            if (kFwd && p.pre != nullptr)
-              put_chunk<false>(P.map_pre, p.pre, to + 2048, slot0 + c, g.n - c, f, width, ok);
-          }
-          if (lane == 0) bulk_commit();
-        }
-      }
-      if (steps > 0) {
-        // the accumulator may take the tile after next
+      const auto await_sum = [&]() {   // of the tile, or of its next stages
+        ok = ok && warp_wait(&sm.tfull[j & 1], (j >> 1) & 1, abort_flag);
+        tc_fence_after();
+        return tm + (j & 1) * kPairN + (static_cast<uint32_t>(32 * q) << 16);
+      };
+      const auto release_sum = [&]() {   // the accumulator may be written again
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * acc);
+        if (lane == 0) mbar_arrive_cluster(tempty0 + 8 * (j & 1));
         ++j;
+      };
+      if constexpr (!kF32) {
+        const uint32_t d = steps > 0 ? await_sum() : 0;
+#pragma unroll 1
+        for (int c = kPairChunk * grp; c < g.n; c += kGroups * kPairChunk) {
+          if constexpr (kBackW) {
+            if (!ok || f >= p.N) break;
+            float v[32];
+            if (steps > 0) {
+              tmem_ld32(d + c, v);
+              tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) v[k] = 0.f;   // an expert without slots
+            }
+            put_rows(f, c, v);
+          } else {
+            float v[2][16];
+            tmem_ld_frag32(d + c, v[0]);
+            tmem_ld_frag32(d + c + (16u << 16), v[1]);
+            put_columns(f, c, v);
+          }
+        }
+        if (steps > 0) release_sum();
+      } else {
+        // columns 32 grp + 64 i
+        float sum[4][2][16];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int k = 0; k < 32; ++k) sum[i][k >> 4][k & 15] = 0.f;
+#pragma unroll 1
+        for (int k0 = 0; k0 < steps; k0 += Kind::kSteps) {
+          const uint32_t d = await_sum();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int c = kPairChunk * (grp + 2 * i);
+            if (c >= g.n) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float v[16];
+              if constexpr (kBackW) tmem_ld16(d + c + 16 * h, v);
+              else tmem_ld_frag32(d + c + (static_cast<uint32_t>(16 * h) << 16), v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) sum[i][h][k] += v[k];
+            }
+          }
+          release_sum();
+        }
+#pragma unroll 1
+        for (int c = kPairChunk * grp; c < g.n; c += 2 * kPairChunk) {
+          if constexpr (kBackW) {
+            if (!ok || f >= p.N) break;
+            put_rows(f, c, reinterpret_cast<const float(&)[32]>(sum[0]));
+          } else {
+            put_columns(f, c, sum[0]);
+          }
+#pragma unroll
+          for (int i = 0; i < 3; ++i)
+#pragma unroll
+            for (int k = 0; k < 32; ++k) sum[i][k >> 4][k & 15] = sum[i + 1][k >> 4][k & 15];
+        }
       }
     }
     if (lane == 0) bulk_wait_all();
     if (kBackX) cp_async_wait_all();
+  } else {
+    if constexpr (kF32) regs_dealloc<Kind::kOtherRegs>();
+    if (warp == 0) {
+      // ------------------------------------------------------------- copies
+      bool ok = true;
+      int s = 0, use = 0;
+      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
+        pair_tile<kWhat>(p, sm, t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+        const int f = g.f0 + rank * kPairM;             // this CTA's features
+        const int half = kBackW ? kPairN / 2 : g.width / 2;
+        const int b0 = g.i0 + rank * half;              // ... and its columns of the tile
+        const uint32_t bytes = kPairABytes + (kGather ? 0 : half * kPairStep * 2);
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
+          const uint32_t a = ring + s * kPairStageBytes, b = a + kPairABytes;
+          const uint32_t full = dsmem_addr(smem_u32(&sm.full[s]), 0);
+          const int c0 = kt * kPairStep;
+          if (kBackW && g.lo + c0 + kPairStep > g.hi) {
+            copy_partial(a, p.dy, p.ldy, f, p.N, g.lo + c0, g.hi);
+            if constexpr (!kGather) copy_partial(b, p.x, p.ldx, b0, p.K, g.lo + c0, g.hi);
+            cp_async_wait_all();
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(full);
+          } else if (lane == 0) {
+            mbar_arrive_expect_tx_cluster(full, bytes);
+            if constexpr (kFwd) {
+              tma_load_3d_pair(a, &P.map_a, c0, f, g.e, full);
+            } else if constexpr (kBackX) {
+              tma_load_3d_pair(a, &P.map_a, f, c0, g.e, full);
+              tma_load_3d_pair(a + kPairBoxBytes, &P.map_a, f + 64, c0, g.e, full);
+            } else {
+              tma_load_2d_pair(a, &P.map_a, f, g.lo + c0, full);
+              tma_load_2d_pair(a + kPairBoxBytes, &P.map_a, f + 64, g.lo + c0, full);
+            }
+            if constexpr (!kGather) {
+              if constexpr (kBackW) {
+                tma_load_2d_pair(b, &P.map_b, b0, g.lo + c0, full);
+                tma_load_2d_pair(b + kPairBoxBytes, &P.map_b, b0 + 64, g.lo + c0, full);
+              } else if (half == kPairN / 2) {
+                tma_load_2d_pair(b, &P.map_b, c0, g.lo + b0, full);
+              } else {
+                for (int q = 0; q < half; q += 32)
+                  tma_load_2d_pair(b + q * 128, &P.map_b32, c0, g.lo + b0 + q, full);
+              }
+            }
+          }
+          __syncwarp();
+          if (++s == kStages) {
+            s = 0;
+            ++use;
+          }
+        }
+      }
+      // every stage's products are done, and their arrivals have come, before this CTA ends
+#pragma unroll 1
+      for (int q = 0; q < kStages; ++q) {
+        const int fills = use + (q < s ? 1 : 0);
+        if (fills > 0) warp_wait(&sm.empty[q], (fills - 1) & 1, abort_flag);
+      }
+    } else if (warp == 1) {
+      // ------------------------------------------------------------- products
+      if (rank == 0 && elect_one()) {
+        bool ok = true;
+        int s = 0, use = 0, j = 0;
+        for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
+          pair_tile<kWhat>(p, sm, t, g);
+          const int steps = pair_steps<kWhat>(p, g);
+          if (steps == 0) continue;
+          const uint32_t idesc = idesc_bf16(256, kBackW ? kPairN : g.width, !kFwd, kBackW);
+          // low descriptor words: K-major operands advance 32 bytes per 16 of the
+          // contraction, MN-major ones two groups of eight 128-byte rows; their other
+          // 64-feature boxes lie 8 KB apart
+          constexpr uint32_t kFar = (kPairBoxBytes >> 4) << 16, kNear = 1u << 16;
+          constexpr uint32_t kStepA = kFwd ? 2 : 128, kStepB = kBackW ? 128 : 2;
+#pragma unroll 1
+          for (int kt = 0; kt < steps; ++kt) {
+            const int acc = j & 1, k0 = kt % Kind::kSteps;
+            // the accumulator's previous sum has been read back
+            if (k0 == 0 && j >= 2 &&
+                !(ok = mbar_wait_poll(&sm.tempty[acc], ((j >> 1) - 1) & 1, abort_flag)))
+              break;
+            const uint32_t d = tm + acc * kPairN;
+            if (!(ok = mbar_wait_poll(&sm.full[s], use & 1, abort_flag))) break;
+            if (kGather || (kBackW && g.lo + (kt + 1) * kPairStep > g.hi)) {
+              fence_proxy_async_smem();   // written by threads
+            }
+            tc_fence_after();
+            const uint32_t at = ring + s * kPairStageBytes;
+            const uint32_t a = (at >> 4) | (kFwd ? kNear : kFar);
+            const uint32_t b = ((at + kPairABytes) >> 4) | (kBackW ? kFar : kNear);
+#pragma unroll
+            for (int k = 0; k < kPairStep / 16; ++k)
+              umma_bf16_pair_lo(d, a + kStepA * k, b + kStepB * k, idesc, (k0 | k) != 0);
+            umma_commit_pair(sums ? &sm.done[s] : &sm.empty[s]);
+            if (++s == kStages) {
+              s = 0;
+              ++use;
+            }
+            if (k0 == Kind::kSteps - 1 || kt == steps - 1) {
+              umma_commit_pair(&sm.tfull[acc]);
+              ++j;
+            }
+          }
+        }
+      }
+      __syncwarp();
+    } else if (kGather && warp >= kGatherWarp && warp < kGatherWarp + 4) {
+      // ------------------------------------------------------------- gathered rows
+      // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
+      // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
+      const int l = tid - 32 * kGatherWarp;
+      constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
+      const int c = l % kPieces, r0 = l / kPieces;
+      bool ok = true;
+      int s = 0, use = 0;
+      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
+        pair_tile<kWhat>(p, sm, t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+        const int half = kBackW ? kPairN / 2 : g.width / 2;
+        const int b0 = g.i0 + rank * half;
+        const uint16_t* src[8];
+        // weight gradient: the 16 rows that this warp copies of each of eight stages, two
+        // stages a register; those of the eight after them are loaded meanwhile (a load
+        // waits up to 3000 cycles behind the operands: two stages ahead 62 us, not 41)
+        int row[4], row_next[4];
+        const auto load_rows = [&](int kt) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
+            row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
+          }
+        };
+        if constexpr (kFwd) {
+          // columns past the tile repeat its last slot
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            src[i] = p.x + 8 * c +
+                     p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
+        } else {
+          load_rows(0);
+        }
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
+          const uint32_t b = ring + s * kPairStageBytes + kPairABytes;
+          const int c0 = kt * kPairStep;
+          if constexpr (kFwd) {
+            const bool in = c0 + 8 * c < p.K;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (r0 + kRowStep * i < half)
+                cp_async16(b + sw128_offset(r0 + kRowStep * i, c), src[i] + (in ? c0 : 0), in);
+          } else {
+            const int col = b0 + 8 * c;
+            if (kt % 8 == 0) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) row[i] = row_next[i];
+              load_rows(kt + 8);
+            }
+            const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = r0 + kRowStep * i;
+              const int at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
+              const bool in = g.lo + c0 + r < g.hi && col < p.K;
+              cp_async16(b + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7),
+                         p.x + (in ? at * p.ldx + col : 0), in);
+            }
+          }
+          cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
+          if (++s == kStages) {
+            s = 0;
+            ++use;
+          }
+        }
+      }
+      cp_async_wait_all();
+    } else if (kGather && warp == 2) {
+      // ------------------------------------------------------------- gathered rows handed over
+      // What threads write to shared memory is ordered before the products by the proxy
+      // fence.  Only the signal crosses to the even CTA: the rows are read where they lie,
+      // by their own CTA's tensor core, so nothing has to become visible outside the CTA
+      // (a release over the cluster for each stage takes twice the time: 69 us, not 35).
+      if (elect_one()) {
+        bool ok = true;
+        int s = 0, use = 0;
+        for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
+          pair_tile<kWhat>(p, sm, t, g);
+          const int steps = pair_steps<kWhat>(p, g);
+#pragma unroll 1
+          for (int kt = 0; kt < steps; ++kt) {
+            if (!(ok = mbar_wait_poll(&sm.landed[s], use & 1, abort_flag))) break;
+            fence_proxy_async_smem();
+            mbar_arrive_cluster(dsmem_addr(smem_u32(&sm.full[s]), 0));
+            if (++s == kStages) {
+              s = 0;
+              ++use;
+            }
+          }
+        }
+      }
+      __syncwarp();
+    } else if (kBackW && warp >= kSumWarp) {
+      // ------------------------------------------------------------- bias sums
+      // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
+      // the 64 slots.
+      if (sums) {
+        const int l = tid - 32 * kSumWarp, w = l >> 5;
+        bool ok = true;   // no early exit: the four warps meet at every tile with a sum
+        int s = 0, use = 0;
+        for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
+          pair_tile<kWhat>(p, sm, t, g);
+          const int steps = pair_steps<kWhat>(p, g);
+          float a[4] = {};
+#pragma unroll 1
+          for (int kt = 0; kt < steps; ++kt) {
+            ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
+            if (ok && g.i0 == 0) {
+              const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const uint2 v = *reinterpret_cast<const uint2*>(at + sw128_offset(16 * w + i, (lane & 15) >> 1));
+                a[0] += bf_lo(v.x);
+                a[1] += bf_hi(v.x);
+                a[2] += bf_lo(v.y);
+                a[3] += bf_hi(v.y);
+              }
+            }
+            warp_arrive(&sm.empty[s]);
+            if (++s == kStages) {
+              s = 0;
+              ++use;
+            }
+          }
+          if (g.i0 == 0) {
+            float4& mine = *reinterpret_cast<float4*>(&sm.sums[w & 1][4 * lane]);
+            if (w >= 2) mine = make_float4(a[0], a[1], a[2], a[3]);
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+            if (w < 2)
+              mine = make_float4(a[0] + mine.x, a[1] + mine.y, a[2] + mine.z, a[3] + mine.w);
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+            const int n = g.f0 + rank * kPairM + l;
+            if (ok && n < p.N)
+              p.dbias[static_cast<size_t>(g.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
+            asm volatile("bar.sync 3, 128;" ::: "memory");
+          }
+        }
+      }
+    }
   }
 
   tc_fence_before();
@@ -936,8 +969,9 @@ static bool encode_out(CUtensorMap* m, void* base, bool f32, long long rows, int
              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <ExpertProduct kWhat, bool kGather>
+template <ExpertProduct kWhat, bool kGather, bool kF32>
 static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
+  using Kind = PairKind<kWhat, kGather, kF32>;
   static int sms = 0;
   if (sms == 0) {
     int dev = 0;
@@ -948,8 +982,8 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
   const long long pairs = most_tiles < sms / 2 ? most_tiles : sms / 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
-  cfg.blockDim = dim3(pair_threads<kWhat, kGather>());
-  cfg.dynamicSmemBytes = pair_dyn<kWhat>();
+  cfg.blockDim = dim3(Kind::kThreads);
+  cfg.dynamicSmemBytes = Kind::kDyn;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -960,7 +994,13 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, sc_expert_pair_kernel<kWhat, kGather>, P);
+  return cudaLaunchKernelEx(&cfg, sc_expert_pair_kernel<kWhat, kGather, kF32>, P);
+}
+
+template <ExpertProduct kWhat, bool kGather>
+static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
+  return P.p.out_f32 ? launch_pair<kWhat, kGather, true>(P, most_tiles, st)
+                     : launch_pair<kWhat, kGather, false>(P, most_tiles, st);
 }
 
 cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p, cudaStream_t st) {
@@ -1004,9 +1044,12 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
 
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t configure_pair() {
-  return cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather>,
-                              cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(pair_dyn<kWhat>()));
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  const cudaError_t e = cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather, false>, attr,
+                                             static_cast<int>(PairKind<kWhat, kGather, false>::kDyn));
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather, true>, attr,
+                              static_cast<int>(PairKind<kWhat, kGather, true>::kDyn));
 }
 
 cudaError_t configure_expert() {
