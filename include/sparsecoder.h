@@ -560,8 +560,8 @@ int sc_expert_route_backward(const sc_expert_route_backward_args* args, void* st
  *          one without slots); dbias fp32 [E][N] or NULL.
  * Products of bf16 values, sums in fp32, one rounding at the end.  Two calls with
  * the same arguments give the same bits.
- * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; ldx and ldy multiples of 8;
- * every bf16 pointer, out, dX and dW 16-byte aligned.
+ * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; ldx and ldy multiples of 8
+ * below 2^30; every bf16 pointer, out, dX and dW 16-byte aligned.
  */
 typedef struct {
   int M, E, N, K;

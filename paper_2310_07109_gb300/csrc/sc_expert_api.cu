@@ -55,7 +55,7 @@ int check_product(int M, int E, int N, int K, const int32_t* offsets) {
 }
 
 bool good_matrix(const void* p, long long ld, int width) {
-  return p && aligned(p, 16) && ld >= width && ld % 8 == 0;
+  return p && aligned(p, 16) && ld >= width && ld % 8 == 0 && ld < (1ll << 30);
 }
 
 int launch_product(ExpertProduct what, const ExpertLinearParams& p, void* stream) {

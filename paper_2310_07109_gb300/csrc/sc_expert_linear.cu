@@ -19,7 +19,7 @@
 //               TMA gathers of 128-byte rows took 81 cycles each, 8 x 1024 rows x 2
 //               experts 768 -> 1536 99 us against 34 without the gather
 //   four warps more (weight gradient) sum dy over the slots for the bias, from the
-//               stages in shared memory
+//               stages in shared memory; the gathering warps, where there are some
 // Operands as they lie in memory: K-major where the contraction is contiguous
 // (forward; dy in back (input)), else MN-major (W in back (input), both sides of the
 // weight gradient), 128-byte swizzle throughout.
@@ -46,9 +46,11 @@ constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes;
 constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN-major operand
 // The tensor cores add to an fp32 accumulator with truncation, half a unit in the last
 // place per 16 of the contraction: 2048 slots, 3.7e-6.  bf16 outputs do not show it.  For
-// fp32 outputs an accumulator takes kSpan stages (256 of the contraction) only; eight
-// write-back warps add it, rounded, to sums in their registers (128 a thread).
-constexpr int kSpan = 4;
+// fp32 outputs an accumulator takes kSpan stages (512 of the contraction) only; eight
+// write-back warps add it, rounded, to sums in their registers (128 a thread; weight
+// gradient: 64, and as many in the write-back areas, for the registers of the other
+// warps).  2048 slots: 4.8e-7, torch's fp32 product 3.9e-7.
+constexpr int kSpan = 8;
 template <ExpertProduct kWhat, bool kGather_, bool kF32_>
 struct PairKind {
   static constexpr bool kFwd = kWhat == ExpertProduct::kForward;
@@ -58,12 +60,14 @@ struct PairKind {
   static constexpr int kSteps = kF32 ? kSpan : 1 << 30;   // stages an accumulator takes
   // Warps: four (copies, products), the write-back, four that gather, four that sum dy.
   static constexpr int kEpiWarps = kBackW || kF32 ? 8 : 16;
-  static constexpr int kGatherWarp = 4 + kEpiWarps, kSumWarp = kGatherWarp + (kGather ? 4 : 0);
-  static constexpr int kThreads = 32 * (kSumWarp + (kBackW ? 4 : 0));
-  // Registers of the write-back warps, and of the others, where the sums need them: what
-  // 65536 registers (61440 with 640 threads) leave.
-  static constexpr int kEpiRegs = kThreads <= 384 ? 208 : kThreads <= 512 ? 200 : 168;
-  static constexpr int kOtherRegs = kThreads <= 384 ? 88 : kThreads <= 512 ? 56 : 48;
+  static constexpr int kAuxWarp = 4 + kEpiWarps;   // four that gather, or sum dy, or both
+  static constexpr int kThreads = 32 * (kAuxWarp + (kGather || kBackW ? 4 : 0));
+  // Registers where fp32 sums need them, of the write-back warps, of the first four and of
+  // the last four: what 65536 leave.
+  static constexpr bool kSplit = kF32 && !kBackW;
+  static constexpr int kEpiRegs = kThreads <= 384 ? 208 : 192;
+  static constexpr int kFirstRegs = kThreads <= 384 ? 88 : 56;
+  static constexpr int kAuxRegs = 72;
   // Write-back areas per warp.  Forward: a chunk of the output (bf16 2 KB, fp32 4) and one
   // of the value before GELU.  Back (weight): two chunks of 4 KB, the copy of one on its
   // way while the other is filled.  Back (input): a chunk of the output and a ring of two
@@ -287,7 +291,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
   using Kind = PairKind<kWhat, kGather, kF32>;
   constexpr bool kFwd = Kind::kFwd, kBackX = Kind::kBackX, kBackW = Kind::kBackW;
   constexpr int kStages = Kind::kStages, kEpiWarps = Kind::kEpiWarps, kGroups = kEpiWarps / 4;
-  constexpr int kGatherWarp = Kind::kGatherWarp, kSumWarp = Kind::kSumWarp;
+  constexpr int kAuxWarp = Kind::kAuxWarp;
   static_assert(sizeof(PairSmem) + Kind::kDyn <= 227 * 1024, "one CTA's shared memory");
   const ExpertLinearParams& p = P.p;
   extern __shared__ uint8_t dyn_raw[];
@@ -367,7 +371,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
   g.e = 0;
 
   if (warp >= 4 && warp < 4 + kEpiWarps) {
-    if constexpr (kF32) regs_alloc<Kind::kEpiRegs>();
+    if constexpr (Kind::kSplit) regs_alloc<Kind::kEpiRegs>();
     // ------------------------------------------------------------- write back
     const int q = warp & 3, grp = (warp - 4) >> 2;
     uint8_t* const stg = base + kStages * kPairStageBytes + (warp - 4) * Kind::kOutBytes;
@@ -427,22 +431,15 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       pair_tile<kWhat>(p, sm, pair, ahead);
       load_bias(ahead);
     }
-    // weight gradient: 32 rows (features) of 32 columns, contiguous in memory, from column c
+    // weight gradient in bf16: 32 rows (features) of 32 columns, contiguous in memory, from
+    // column c
     const auto put_rows = [&](int f, int c, const float (&v)[32]) {
       uint8_t* const to = next_area();
-      if constexpr (kF32) {
 #pragma unroll
-        for (int k = 0; k < 32; k += 4)
-          stage_row_piece<8>(to, k / 4,
-                             make_uint4(__float_as_uint(v[k]), __float_as_uint(v[k + 1]),
-                                        __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3])));
-      } else {
-#pragma unroll
-        for (int k = 0; k < 32; k += 8)
-          stage_row_piece<4>(to, k / 8,
-                             make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
-                                        pack_bf16x2(v[k + 4], v[k + 5]), pack_bf16x2(v[k + 6], v[k + 7])));
-      }
+      for (int k = 0; k < 32; k += 8)
+        stage_row_piece<4>(to, k / 8,
+                           make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
+                                      pack_bf16x2(v[k + 4], v[k + 5]), pack_bf16x2(v[k + 6], v[k + 7])));
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
@@ -571,6 +568,75 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
           }
         }
         if (steps > 0) release_sum();
+      } else if constexpr (kBackW) {
+        // columns 32 grp + 64 i: i = 0, 1 in registers, 2, 3 in the write-back areas, a
+        // row a lane as they leave
+        float sum[2][32];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int k = 0; k < 32; ++k) sum[i][k] = 0.f;
+        if (lane == 0) bulk_wait_read<0>();
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          stage_row_piece<8>(stg, k, make_uint4(0, 0, 0, 0));
+          stage_row_piece<8>(stg + 4096, k, make_uint4(0, 0, 0, 0));
+        }
+#pragma unroll 1
+        for (int k0 = 0; k0 < steps; k0 += Kind::kSteps) {
+          const uint32_t d = await_sum();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int c = kPairChunk * (grp + 2 * i);
+            if (c >= g.n) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float v[16];
+              tmem_ld16(d + c + 16 * h, v);
+              tmem_ld_wait();
+              if (i < 2) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) sum[i & 1][16 * h + k] += v[k];
+              } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  float4* const at =
+                      reinterpret_cast<float4*>(stg + (i - 2) * 4096 + stage_offset<8>(lane, 4 * h + k));
+                  const float4 was = *at;
+                  *at = make_float4(was.x + v[4 * k], was.y + v[4 * k + 1], was.z + v[4 * k + 2],
+                                    was.w + v[4 * k + 3]);
+                }
+              }
+            }
+          }
+          release_sum();
+        }
+        // the areas' columns leave, then the registers' through them
+#pragma unroll
+        for (int i = 2; i >= 0; i -= 2) {
+          if (i == 0) {
+            if (lane == 0) bulk_wait_read<0>();
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 32; k += 4)
+#pragma unroll
+              for (int o = 0; o < 2; ++o)
+                stage_row_piece<8>(stg + 4096 * o, k / 4,
+                                   make_uint4(__float_as_uint(sum[o][k]), __float_as_uint(sum[o][k + 1]),
+                                              __float_as_uint(sum[o][k + 2]), __float_as_uint(sum[o][k + 3])));
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && ok && f < p.N) {
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+              const int c = kPairChunk * (grp + 2 * (i + o));
+              if (c < g.n) tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(stg + 4096 * o));   // cut at N and K
+            }
+            bulk_commit();
+          }
+        }
       } else {
         // columns 32 grp + 64 i
         float sum[4][2][16];
@@ -588,8 +654,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float v[16];
-              if constexpr (kBackW) tmem_ld16(d + c + 16 * h, v);
-              else tmem_ld_frag32(d + c + (static_cast<uint32_t>(16 * h) << 16), v);
+              tmem_ld_frag32(d + c + (static_cast<uint32_t>(16 * h) << 16), v);
               tmem_ld_wait();
 #pragma unroll
               for (int k = 0; k < 16; ++k) sum[i][h][k] += v[k];
@@ -599,12 +664,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
         }
 #pragma unroll 1
         for (int c = kPairChunk * grp; c < g.n; c += 2 * kPairChunk) {
-          if constexpr (kBackW) {
-            if (!ok || f >= p.N) break;
-            put_rows(f, c, reinterpret_cast<const float(&)[32]>(sum[0]));
-          } else {
-            put_columns(f, c, sum[0]);
-          }
+          put_columns(f, c, sum[0]);
 #pragma unroll
           for (int i = 0; i < 3; ++i)
 #pragma unroll
@@ -615,7 +675,10 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
     if (lane == 0) bulk_wait_all();
     if (kBackX) cp_async_wait_all();
   } else {
-    if constexpr (kF32) regs_dealloc<Kind::kOtherRegs>();
+    if constexpr (Kind::kSplit) {
+      if (warp < 4) regs_dealloc<Kind::kFirstRegs>();
+      else regs_dealloc<Kind::kAuxRegs>();
+    }
     if (warp == 0) {
       // ------------------------------------------------------------- copies
       bool ok = true;
@@ -723,77 +786,6 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
         }
       }
       __syncwarp();
-    } else if (kGather && warp >= kGatherWarp && warp < kGatherWarp + 4) {
-      // ------------------------------------------------------------- gathered rows
-      // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
-      // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
-      const int l = tid - 32 * kGatherWarp;
-      constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
-      const int c = l % kPieces, r0 = l / kPieces;
-      bool ok = true;
-      int s = 0, use = 0;
-      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-        pair_tile<kWhat>(p, sm, t, g);
-        const int steps = pair_steps<kWhat>(p, g);
-        const int half = kBackW ? kPairN / 2 : g.width / 2;
-        const int b0 = g.i0 + rank * half;
-        const uint16_t* src[8];
-        // weight gradient: the 16 rows that this warp copies of each of eight stages, two
-        // stages a register; those of the eight after them are loaded meanwhile (a load
-        // waits up to 3000 cycles behind the operands: two stages ahead 62 us, not 41)
-        int row[4], row_next[4];
-        const auto load_rows = [&](int kt) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
-            row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
-          }
-        };
-        if constexpr (kFwd) {
-          // columns past the tile repeat its last slot
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            src[i] = p.x + 8 * c +
-                     p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
-        } else {
-          load_rows(0);
-        }
-#pragma unroll 1
-        for (int kt = 0; kt < steps; ++kt) {
-          if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
-          const uint32_t b = ring + s * kPairStageBytes + kPairABytes;
-          const int c0 = kt * kPairStep;
-          if constexpr (kFwd) {
-            const bool in = c0 + 8 * c < p.K;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (r0 + kRowStep * i < half)
-                cp_async16(b + sw128_offset(r0 + kRowStep * i, c), src[i] + (in ? c0 : 0), in);
-          } else {
-            const int col = b0 + 8 * c;
-            if (kt % 8 == 0) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) row[i] = row_next[i];
-              load_rows(kt + 8);
-            }
-            const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int r = r0 + kRowStep * i;
-              const int at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
-              const bool in = g.lo + c0 + r < g.hi && col < p.K;
-              cp_async16(b + (c >> 3) * kPairBoxBytes + sw128_offset(r, c & 7),
-                         p.x + (in ? at * p.ldx + col : 0), in);
-            }
-          }
-          cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
-          if (++s == kStages) {
-            s = 0;
-            ++use;
-          }
-        }
-      }
-      cp_async_wait_all();
     } else if (kGather && warp == 2) {
       // ------------------------------------------------------------- gathered rows handed over
       // What threads write to shared memory is ordered before the products by the proxy
@@ -819,49 +811,153 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
         }
       }
       __syncwarp();
-    } else if (kBackW && warp >= kSumWarp) {
+    } else if (warp >= kAuxWarp) {
+      const int l = tid - 32 * kAuxWarp;
+      bool ok = true;   // no early exit: the four warps meet at every tile with a bias sum
       // ------------------------------------------------------------- bias sums
       // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
-      // the 64 slots.
-      if (sums) {
-        const int l = tid - 32 * kSumWarp, w = l >> 5;
-        bool ok = true;   // no early exit: the four warps meet at every tile with a sum
-        int s = 0, use = 0;
+      // the 64 slots.  sum_fill() takes the next stage whose products are done and hands
+      // it back to the copies; fills come in the order of the tiles.  (Tile ts, of which
+      // left_s stages are to come; what else there is to know of it is found again.)
+      float part[4] = {};
+      int ts = pair, left_s = 0;
+      bool first_s = false;   // its first column block: the one that sums
+      const auto finish_sum = [&]() {
+        if (!first_s) return;
+        const int w = l >> 5;
+        float4& mine = *reinterpret_cast<float4*>(&sm.sums[w & 1][4 * lane]);
+        if (w >= 2) mine = make_float4(part[0], part[1], part[2], part[3]);
+        asm volatile("bar.sync 3, 128;" ::: "memory");
+        if (w < 2) mine = make_float4(part[0] + mine.x, part[1] + mine.y, part[2] + mine.z, part[3] + mine.w);
+        asm volatile("bar.sync 3, 128;" ::: "memory");
+        PairTile gs;
+        pair_tile<kWhat>(p, sm, ts, gs);
+        const int n = gs.f0 + rank * kPairM + l;
+        if (ok && n < p.N) p.dbias[static_cast<size_t>(gs.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
+        asm volatile("bar.sync 3, 128;" ::: "memory");
+        part[0] = part[1] = part[2] = part[3] = 0.f;
+      };
+      // to the next tile with a contraction; the bias of an expert without slots is 0
+      const auto seek_sum = [&]() {
+        for (; ts < tiles; ts = next_tile<kWhat>(ts, pair, pairs)) {
+          PairTile gs;
+          pair_tile<kWhat>(p, sm, ts, gs);
+          left_s = pair_steps<kWhat>(p, gs);
+          first_s = gs.i0 == 0;
+          if (left_s > 0) return;
+          finish_sum();
+        }
+      };
+      const auto sum_fill = [&](int stage, int parity) {
+        ok = ok && warp_wait(&sm.done[stage], parity, abort_flag);
+        if (ok && first_s) {
+          const uint8_t* at = base + stage * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
+#pragma unroll 4
+          for (int i = 0; i < 16; ++i) {
+            const uint2 v =
+                *reinterpret_cast<const uint2*>(at + sw128_offset(16 * (l >> 5) + i, (lane & 15) >> 1));
+            part[0] += bf_lo(v.x);
+            part[1] += bf_hi(v.x);
+            part[2] += bf_lo(v.y);
+            part[3] += bf_hi(v.y);
+          }
+        }
+        warp_arrive(&sm.empty[stage]);
+        if (--left_s == 0) {
+          finish_sum();
+          ts = next_tile<kWhat>(ts, pair, pairs);
+          seek_sum();
+        }
+      };
+      int s = 0, use = 0;   // stage of the next fill, and how often it was filled
+      if (sums) seek_sum();
+      if constexpr (kGather) {
+        // ------------------------------------------------------------- gathered rows
+        // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
+        // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
+        constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
+        const int c = l % kPieces, r0 = l / kPieces;
+        // this thread's piece of row r0 in a stage; rows r0 + kRowStep i lie 128 kRowStep i on
+        static_assert(kRowStep % 8 == 0, "the same swizzle");
+        const uint32_t to = kPairABytes + (c >> 3) * kPairBoxBytes + sw128_offset(r0, c & 7);
         for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
           pair_tile<kWhat>(p, sm, t, g);
           const int steps = pair_steps<kWhat>(p, g);
-          float a[4] = {};
+          const int half = kBackW ? kPairN / 2 : g.width / 2;
+          const int b0 = g.i0 + rank * half;
+          const uint16_t* src[8];
+          // weight gradient: the 16 rows that this warp copies of each of eight stages, two
+          // stages a register; those of the eight after them are loaded meanwhile (a load
+          // waits up to 3000 cycles behind the operands: four stages ahead 50 us, not 44)
+          int row[4], row_next[4];
+          const auto load_rows = [&](int kt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
+              row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
+            }
+          };
+          // (few instructions a copy: the four warps have a stage's time for them)
+          const int col = b0 + 8 * c;
+          const char* const x_col = reinterpret_cast<const char*>(p.x + (col < p.K ? col : 0));
+          const uint32_t row_bytes = static_cast<uint32_t>(p.ldx) * 2u;
+          if constexpr (kFwd) {
+            // columns past the tile repeat its last slot
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              src[i] = p.x + 8 * c +
+                       p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
+          } else {
+            load_rows(0);
+          }
 #pragma unroll 1
           for (int kt = 0; kt < steps; ++kt) {
-            ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
-            if (ok && g.i0 == 0) {
-              const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
+            if (use > 0) {
+              if (sums) sum_fill(s, (use - 1) & 1);   // of this stage's last fill
+              ok = ok && warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag);
+            }
+            if (!ok) continue;
+            const uint32_t dst = ring + s * kPairStageBytes + to;
+            const int c0 = kt * kPairStep;
+            if constexpr (kFwd) {
+              const bool in = c0 + 8 * c < p.K;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const uint2 v = *reinterpret_cast<const uint2*>(at + sw128_offset(16 * w + i, (lane & 15) >> 1));
-                a[0] += bf_lo(v.x);
-                a[1] += bf_hi(v.x);
-                a[2] += bf_lo(v.y);
-                a[3] += bf_hi(v.y);
+              for (int i = 0; i < 8; ++i)
+                if (r0 + kRowStep * i < half)
+                  cp_async16(dst + 128 * kRowStep * i, src[i] + (in ? c0 : 0), in);
+            } else {
+              if (kt % 8 == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) row[i] = row_next[i];
+                load_rows(kt + 8);
+              }
+              const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
+              const int left = col < p.K ? g.hi - g.lo - c0 - r0 : 0;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const uint32_t at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
+                cp_async16(dst + 128 * kRowStep * i, x_col + static_cast<uint64_t>(at) * row_bytes,
+                           kRowStep * i < left);
               }
             }
-            warp_arrive(&sm.empty[s]);
+            cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
             if (++s == kStages) {
               s = 0;
               ++use;
             }
           }
-          if (g.i0 == 0) {
-            float4& mine = *reinterpret_cast<float4*>(&sm.sums[w & 1][4 * lane]);
-            if (w >= 2) mine = make_float4(a[0], a[1], a[2], a[3]);
-            asm volatile("bar.sync 3, 128;" ::: "memory");
-            if (w < 2)
-              mine = make_float4(a[0] + mine.x, a[1] + mine.y, a[2] + mine.z, a[3] + mine.w);
-            asm volatile("bar.sync 3, 128;" ::: "memory");
-            const int n = g.f0 + rank * kPairM + l;
-            if (ok && n < p.N)
-              p.dbias[static_cast<size_t>(g.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
-            asm volatile("bar.sync 3, 128;" ::: "memory");
+        }
+        cp_async_wait_all();
+      }
+      if (sums) {
+        // the fills not yet summed: the ring's, or all where it was not filled once
+        if (kGather && use > 0) --use;
+        else s = 0;
+        while (ts < tiles) {
+          sum_fill(s, use & 1);
+          if (++s == kStages) {
+            s = 0;
+            ++use;
           }
         }
       }
