@@ -19,7 +19,7 @@
 //               TMA gathers of 128-byte rows took 81 cycles each, 8 x 1024 rows x 2
 //               experts 768 -> 1536 99 us against 34 without the gather
 //   four warps more (weight gradient) sum dy over the slots for the bias, from the
-//               stages in shared memory; the gathering warps, where there are some
+//               stages in shared memory (by the gathering warps 63 us instead of 46)
 // Operands as they lie in memory: K-major where the contraction is contiguous
 // (forward; dy in back (input)), else MN-major (W in back (input), both sides of the
 // weight gradient), 128-byte swizzle throughout.
@@ -60,13 +60,13 @@ struct PairKind {
   static constexpr int kSteps = kF32 ? kSpan : 1 << 30;   // stages an accumulator takes
   // Warps: four (copies, products), the write-back, four that gather, four that sum dy.
   static constexpr int kEpiWarps = kBackW || kF32 ? 8 : 16;
-  static constexpr int kAuxWarp = 4 + kEpiWarps;   // four that gather, or sum dy, or both
-  static constexpr int kThreads = 32 * (kAuxWarp + (kGather || kBackW ? 4 : 0));
+  static constexpr int kGatherWarp = 4 + kEpiWarps, kSumWarp = kGatherWarp + (kGather ? 4 : 0);
+  static constexpr int kThreads = 32 * (kSumWarp + (kBackW ? 4 : 0));
   // Registers where fp32 sums need them, of the write-back warps, of the first four and of
-  // the last four: what 65536 leave.
-  static constexpr bool kSplit = kF32 && !kBackW;
-  static constexpr int kEpiRegs = kThreads <= 384 ? 208 : 192;
-  static constexpr int kFirstRegs = kThreads <= 384 ? 88 : 56;
+  // the others: what 65536 (61440 with 640 threads) leave.
+  static constexpr bool kSplit = kF32 && (!kBackW || kGather);
+  static constexpr int kEpiRegs = kBackW ? 128 : kThreads <= 384 ? 208 : 192;
+  static constexpr int kFirstRegs = kBackW ? 72 : kThreads <= 384 ? 88 : 56;
   static constexpr int kAuxRegs = 72;
   // Write-back areas per warp.  Forward: a chunk of the output (bf16 2 KB, fp32 4) and one
   // of the value before GELU.  Back (weight): two chunks of 4 KB, the copy of one on its
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
   using Kind = PairKind<kWhat, kGather, kF32>;
   constexpr bool kFwd = Kind::kFwd, kBackX = Kind::kBackX, kBackW = Kind::kBackW;
   constexpr int kStages = Kind::kStages, kEpiWarps = Kind::kEpiWarps, kGroups = kEpiWarps / 4;
-  constexpr int kAuxWarp = Kind::kAuxWarp;
+  constexpr int kGatherWarp = Kind::kGatherWarp, kSumWarp = Kind::kSumWarp;
   static_assert(sizeof(PairSmem) + Kind::kDyn <= 227 * 1024, "one CTA's shared memory");
   const ExpertLinearParams& p = P.p;
   extern __shared__ uint8_t dyn_raw[];
@@ -811,14 +811,89 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
         }
       }
       __syncwarp();
-    } else if (warp >= kAuxWarp) {
-      const int l = tid - 32 * kAuxWarp;
+    } else if (kGather && warp >= kGatherWarp && warp < kGatherWarp + 4) {
+      // ------------------------------------------------------------- gathered rows
+      const int l = tid - 32 * kGatherWarp;
+      bool ok = true;
+      int s = 0, use = 0;
+      // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
+      // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
+      constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
+      const int c = l % kPieces, r0 = l / kPieces;
+      // this thread's piece of row r0 in a stage; rows r0 + kRowStep i lie 128 kRowStep i on
+      static_assert(kRowStep % 8 == 0, "the same swizzle");
+      const uint32_t to = kPairABytes + (c >> 3) * kPairBoxBytes + sw128_offset(r0, c & 7);
+      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
+        pair_tile<kWhat>(p, sm, t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+        const int half = kBackW ? kPairN / 2 : g.width / 2;
+        const int b0 = g.i0 + rank * half;
+        const uint16_t* src[8];
+        // weight gradient: the 16 rows that this warp copies of each of eight stages, two
+        // stages a register; those of the eight after them are loaded meanwhile (a load
+        // waits up to 3000 cycles behind the operands: four stages ahead 50 us, not 44)
+        int row[4], row_next[4];
+        const auto load_rows = [&](int kt) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
+            row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
+          }
+        };
+        // (few instructions a copy: the four warps have a stage's time for them)
+        const int col = b0 + 8 * c;
+        const char* const x_col = reinterpret_cast<const char*>(p.x + (col < p.K ? col : 0));
+        const uint32_t row_bytes = static_cast<uint32_t>(p.ldx) * 2u;
+        if constexpr (kFwd) {
+          // columns past the tile repeat its last slot
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            src[i] = p.x + 8 * c +
+                     p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
+        } else {
+          load_rows(0);
+        }
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          if (use > 0 && !(ok = warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag))) break;
+          const uint32_t dst = ring + s * kPairStageBytes + to;
+          const int c0 = kt * kPairStep;
+          if constexpr (kFwd) {
+            const bool in = c0 + 8 * c < p.K;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (r0 + kRowStep * i < half)
+                cp_async16(dst + 128 * kRowStep * i, src[i] + (in ? c0 : 0), in);
+          } else {
+            if (kt % 8 == 0) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) row[i] = row_next[i];
+              load_rows(kt + 8);
+            }
+            const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
+            const int left = col < p.K ? g.hi - g.lo - c0 - r0 : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
+              cp_async16(dst + 128 * kRowStep * i, x_col + static_cast<uint64_t>(at) * row_bytes,
+                         kRowStep * i < left);
+            }
+          }
+          cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
+          if (++s == kStages) {
+            s = 0;
+            ++use;
+          }
+        }
+      }
+      cp_async_wait_all();
+    } else if (kBackW && warp >= kSumWarp) {
+      const int l = tid - 32 * kSumWarp;
       bool ok = true;   // no early exit: the four warps meet at every tile with a bias sum
       // ------------------------------------------------------------- bias sums
       // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
       // the 64 slots.  sum_fill() takes the next stage whose products are done and hands
-      // it back to the copies; fills come in the order of the tiles.  (Tile ts, of which
-      // left_s stages are to come; what else there is to know of it is found again.)
+      // it back to the copies; fills come in the order of the tiles.
       float part[4] = {};
       int ts = pair, left_s = 0;
       bool first_s = false;   // its first column block: the one that sums
@@ -869,96 +944,13 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
           seek_sum();
         }
       };
-      int s = 0, use = 0;   // stage of the next fill, and how often it was filled
+      int s = 0, use = 0;
       if (sums) seek_sum();
-      if constexpr (kGather) {
-        // ------------------------------------------------------------- gathered rows
-        // forward: 8 pieces of each of up to 128 rows, the rows the same in every stage;
-        // weight gradient: 16 pieces of each of 64 rows, other rows in every stage
-        constexpr int kPieces = kFwd ? 8 : 16, kRowStep = 128 / kPieces;
-        const int c = l % kPieces, r0 = l / kPieces;
-        // this thread's piece of row r0 in a stage; rows r0 + kRowStep i lie 128 kRowStep i on
-        static_assert(kRowStep % 8 == 0, "the same swizzle");
-        const uint32_t to = kPairABytes + (c >> 3) * kPairBoxBytes + sw128_offset(r0, c & 7);
-        for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-          pair_tile<kWhat>(p, sm, t, g);
-          const int steps = pair_steps<kWhat>(p, g);
-          const int half = kBackW ? kPairN / 2 : g.width / 2;
-          const int b0 = g.i0 + rank * half;
-          const uint16_t* src[8];
-          // weight gradient: the 16 rows that this warp copies of each of eight stages, two
-          // stages a register; those of the eight after them are loaded meanwhile (a load
-          // waits up to 3000 cycles behind the operands: four stages ahead 50 us, not 44)
-          int row[4], row_next[4];
-          const auto load_rows = [&](int kt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int r = (r0 & ~1) + (lane & 1) + 8 * ((lane & 15) >> 1);
-              row_next[i] = expert_row(p, min(g.lo + (kt + 2 * i + (lane >> 4)) * kPairStep + r, p.M - 1));
-            }
-          };
-          // (few instructions a copy: the four warps have a stage's time for them)
-          const int col = b0 + 8 * c;
-          const char* const x_col = reinterpret_cast<const char*>(p.x + (col < p.K ? col : 0));
-          const uint32_t row_bytes = static_cast<uint32_t>(p.ldx) * 2u;
-          if constexpr (kFwd) {
-            // columns past the tile repeat its last slot
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              src[i] = p.x + 8 * c +
-                       p.ldx * expert_row(p, g.lo + min(b0 + r0 + kRowStep * i, g.i0 + g.n - 1));
-          } else {
-            load_rows(0);
-          }
-#pragma unroll 1
-          for (int kt = 0; kt < steps; ++kt) {
-            if (use > 0) {
-              if (sums) sum_fill(s, (use - 1) & 1);   // of this stage's last fill
-              ok = ok && warp_wait(&sm.empty[s], (use - 1) & 1, abort_flag);
-            }
-            if (!ok) continue;
-            const uint32_t dst = ring + s * kPairStageBytes + to;
-            const int c0 = kt * kPairStep;
-            if constexpr (kFwd) {
-              const bool in = c0 + 8 * c < p.K;
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                if (r0 + kRowStep * i < half)
-                  cp_async16(dst + 128 * kRowStep * i, src[i] + (in ? c0 : 0), in);
-            } else {
-              if (kt % 8 == 0) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) row[i] = row_next[i];
-                load_rows(kt + 8);
-              }
-              const int two = kt % 8 < 4 ? (kt % 8 < 2 ? row[0] : row[1]) : (kt % 8 < 6 ? row[2] : row[3]);
-              const int left = col < p.K ? g.hi - g.lo - c0 - r0 : 0;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const uint32_t at = __shfl_sync(0xffffffffu, two, 16 * (kt & 1) + 2 * i + (r0 & 1));
-                cp_async16(dst + 128 * kRowStep * i, x_col + static_cast<uint64_t>(at) * row_bytes,
-                           kRowStep * i < left);
-              }
-            }
-            cp_async_arrive(&sm.landed[s]);   // once this thread's copies have landed
-            if (++s == kStages) {
-              s = 0;
-              ++use;
-            }
-          }
-        }
-        cp_async_wait_all();
-      }
-      if (sums) {
-        // the fills not yet summed: the ring's, or all where it was not filled once
-        if (kGather && use > 0) --use;
-        else s = 0;
-        while (ts < tiles) {
-          sum_fill(s, use & 1);
-          if (++s == kStages) {
-            s = 0;
-            ++use;
-          }
+      while (sums && ts < tiles) {
+        sum_fill(s, use & 1);
+        if (++s == kStages) {
+          s = 0;
+          ++use;
         }
       }
     }
