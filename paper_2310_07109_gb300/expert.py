@@ -9,6 +9,7 @@ stream (or ``stream``), no CPU fallback.  Tokens are the rows of a [B][L] batch 
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -88,27 +89,50 @@ def _library():
     return _bound
 
 
+class _Entry:
+    """An entry point called with its argument block packed by ``struct``: a call on a few
+    rows is all launch time, and filling in a ctypes structure takes a tenth of that."""
+
+    def __init__(self, name):
+        self.name, self.call = name, None
+        args = _WITH_WORKSPACE.get(name) or _WITHOUT_WORKSPACE[name]
+        code = {_I: "i", _P: "P", _F: "f", _LL: "q"}
+        self.pack = struct.Struct("@" + "".join(code[t] for _, t in args._fields_)).pack
+
+    def bind(self):
+        rest = [_P, ctypes.c_size_t, _P] if self.name in _WITH_WORKSPACE else [_P]
+        self.call = ctypes.CFUNCTYPE(_I, _P, *rest)((self.name, _library()))
+        return self.call
+
+
+_ROUTE, _ROUTE_BACK = _Entry("sc_expert_route_forward"), _Entry("sc_expert_route_backward")
+_LINEAR, _COMBINE = _Entry("sc_expert_linear_forward"), _Entry("sc_expert_combine_forward")
+_BACK_X, _BACK_W = _Entry("sc_expert_linear_backward_input"), _Entry("sc_expert_linear_backward_weight")
+_COMBINE_BACK = _Entry("sc_expert_combine_backward")
+
+
 def _refuse(what):
     raise _b.SparseCoderError(_b.SC_ERR_INVALID_ARG, what)
 
 
-def _at(t, name, dtype, shape=None):
-    """The address of a contiguous cuda tensor of this type and shape; None for None."""
+def _at(t, name, dtype, shape):
+    """The address of a contiguous cuda tensor of this type and shape; 0 for None."""
     if t is None:
-        return None
-    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        _refuse("%s: a contiguous cuda tensor of %s is wanted" % (name, dtype))
-    if shape is not None and t.shape != shape:
-        _refuse("%s: shape %s is wanted, not %s" % (name, tuple(shape), tuple(t.shape)))
-    return t.data_ptr()
+        return 0
+    if t.dtype is dtype and t.is_contiguous() and t.is_cuda and t.shape == shape:
+        return t.data_ptr()
+    _refuse("%s: a contiguous cuda tensor of %s and shape %s is wanted" % (name, dtype, tuple(shape)))
 
 
 def _rows_at(t, name, dtype):
     """Address, rows, width and row distance of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype is not dtype or not t.is_cuda or (t.stride(1) != 1 and t.shape[1] > 1):
-        _refuse("%s: a cuda matrix of %s with contiguous rows is wanted" % (name, dtype))
+    if t.dim() != 2 or t.dtype is not dtype or not t.is_cuda:
+        _refuse("%s: a cuda matrix of %s is wanted" % (name, dtype))
     rows, width = t.shape
-    return t.data_ptr(), rows, width, t.stride(0) if rows > 1 else max(t.stride(0), width)
+    ld, step = t.stride()
+    if step != 1 and width > 1:
+        _refuse("%s: contiguous rows are wanted" % name)
+    return t.data_ptr(), rows, width, ld if rows > 1 else max(ld, width)
 
 
 def _stream(stream, t):
@@ -150,8 +174,14 @@ def _work(workspace, device, stream, B, L, E, k, D):
     return ws
 
 
-def _call(name, args, ws, stream):
-    rc = getattr(_library(), name)(args, ws.data_ptr(), ws.numel(), _stream(stream, ws))
+def _call(entry, args, ws, stream):
+    rc = (entry.call or entry.bind())(args, ws.data_ptr(), ws.numel(), _stream(stream, ws))
+    if rc:
+        _b._check(rc)
+
+
+def _call_plain(entry, args, t, stream):
+    rc = (entry.call or entry.bind())(args, _stream(stream, t))
     if rc:
         _b._check(rc)
 
@@ -169,12 +199,12 @@ def expert_route_forward(logits, *, k, B, L, rows=None, renormalize=True, out=No
         out = {"expert": new(T, k), "gate": new(T, k, dtype=torch.float32), "offsets": new(E + 1),
                "slot": new(T, k), "token": new(T * k)}
     i32 = torch.int32
-    a = RouteArgs(B, L, E, k, at, ld, _at(rows, "rows", i32, (B,)), 1 if renormalize else 0,
+    a = _ROUTE.pack(B, L, E, k, at, ld, _at(rows, "rows", i32, (B,)), 1 if renormalize else 0,
                   _at(out["expert"], "expert", i32, (T, k)),
                   _at(out["gate"], "gate", torch.float32, (T, k)),
                   _at(out["offsets"], "offsets", i32, (E + 1,)),
                   _at(out["slot"], "slot", i32, (T, k)), _at(out["token"], "token", i32, (T * k,)))
-    _call("sc_expert_route_forward", a, _work(workspace, logits.device, stream, B, L, E, k, 8), stream)
+    _call(_ROUTE, a, _work(workspace, logits.device, stream, B, L, E, k, 8), stream)
     return out
 
 
@@ -188,13 +218,11 @@ def expert_route_backward(logits, expert, gate, dgate, *, B, L, rows=None, renor
     if out is None:
         out = torch.empty((T, E), dtype=torch.float32, device=logits.device)
     f32 = torch.float32
-    a = RouteBackwardArgs(B, L, E, k, at, ld, _at(rows, "rows", torch.int32, (B,)),
+    a = _ROUTE_BACK.pack(B, L, E, k, at, ld, _at(rows, "rows", torch.int32, (B,)),
                           1 if renormalize else 0, _at(expert, "expert", torch.int32, (T, k)),
                           _at(gate, "gate", f32, (T, k)), _at(dgate, "dgate", f32, (T, k)),
                           _at(out, "dlogits", f32, (T, E)))
-    rc = _library().sc_expert_route_backward(a, _stream(stream, logits))
-    if rc:
-        _b._check(rc)
+    _call_plain(_ROUTE_BACK, a, logits, stream)
     return out
 
 
@@ -214,12 +242,12 @@ def expert_linear_forward(X, W, offsets, *, token=None, bias=None, gelu=False, p
     if out is None:
         out = torch.empty((M, N), dtype=torch.float32 if out_f32 else torch.bfloat16, device=X.device)
     i32 = torch.int32
-    a = ExpertLinearArgs(M, E, N, K, at, ld, xr, _at(token, "token", i32),
+    a = _LINEAR.pack(M, E, N, K, at, ld, xr, _at(token, "token", i32, (M,)),
                          _at(offsets, "offsets", i32, (E + 1,)), _at(W, "W", torch.bfloat16, (E, N, K)),
                          _at(bias, "bias", torch.float32, (E, N)), 1 if gelu else 0,
                          _at(pre, "pre", torch.bfloat16, (M, N)), _at(out, "out", out.dtype, (M, N)),
                          _out_type(out))
-    _call("sc_expert_linear_forward", a, _product_ws(workspace, X, stream), stream)
+    _call(_LINEAR, a, _product_ws(workspace, X, stream), stream)
     return out
 
 
@@ -231,11 +259,11 @@ def expert_linear_backward_input(dY, W, offsets, *, pre=None, out=None, out_f32=
     E, _, K = W.shape
     if out is None:
         out = torch.empty((M, K), dtype=torch.float32 if out_f32 else torch.bfloat16, device=dY.device)
-    a = ExpertLinearBackwardInputArgs(M, E, N, K, at, ld, _at(offsets, "offsets", torch.int32, (E + 1,)),
+    a = _BACK_X.pack(M, E, N, K, at, ld, _at(offsets, "offsets", torch.int32, (E + 1,)),
                                       _at(W, "W", torch.bfloat16, (E, N, K)),
                                       _at(pre, "pre", torch.bfloat16, (M, K)),
                                       _at(out, "out", out.dtype, (M, K)), _out_type(out))
-    _call("sc_expert_linear_backward_input", a, _product_ws(workspace, dY, stream), stream)
+    _call(_BACK_X, a, _product_ws(workspace, dY, stream), stream)
     return out
 
 
@@ -247,20 +275,18 @@ def expert_linear_backward_weight(dY, X, offsets, *, token=None, bias=True, out=
     ay, M, N, ldy = _rows_at(dY, "dY", torch.bfloat16)
     ax, xr, K, ldx = _rows_at(X, "X", torch.bfloat16)
     E = offsets.shape[0] - 1
-    if token is not None and token.shape[0] != M:
-        _refuse("token: one entry for each row of dY is wanted")
     if out is None:
         out = {"dW": torch.empty((E, N, K), dtype=torch.float32 if out_f32 else torch.bfloat16,
                                  device=X.device)}
         if bias:
             out["dbias"] = torch.empty((E, N), dtype=torch.float32, device=X.device)
     dW = out["dW"]
-    a = ExpertLinearBackwardWeightArgs(M, E, N, K, ay, ldy, ax, ldx, xr,
-                                       _at(token, "token", torch.int32),
-                                       _at(offsets, "offsets", torch.int32),
+    a = _BACK_W.pack(M, E, N, K, ay, ldy, ax, ldx, xr,
+                                       _at(token, "token", torch.int32, (M,)),
+                                       _at(offsets, "offsets", torch.int32, (E + 1,)),
                                        _at(dW, "dW", dW.dtype, (E, N, K)), _out_type(dW),
                                        _at(out.get("dbias"), "dbias", torch.float32, (E, N)))
-    _call("sc_expert_linear_backward_weight", a, _product_ws(workspace, X, stream), stream)
+    _call(_BACK_W, a, _product_ws(workspace, X, stream), stream)
     return out
 
 
@@ -276,14 +302,12 @@ def expert_combine_forward(Y, slot, gate=None, *, B, L, rows=None, res=None, res
         if gamma is not None:
             out["out"] = torch.empty((T, D), dtype=torch.bfloat16, device=Y.device)
     bf, f32 = torch.bfloat16, torch.float32
-    a = ExpertCombineArgs(B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf),
+    a = _COMBINE.pack(B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf, (M, D)),
                           _at(slot, "slot", torch.int32, (T, k)), _at(gate, "gate", f32, (T, k)),
                           _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)),
                           _at(beta, "beta", f32, (D,)), eps, _at(out.get("sum"), "sum", bf, (T, D)),
                           _at(out.get("out"), "out", bf, (T, D)))
-    rc = _library().sc_expert_combine_forward(a, _stream(stream, Y))
-    if rc:
-        _b._check(rc)
+    _call_plain(_COMBINE, a, Y, stream)
     return out
 
 
@@ -302,12 +326,12 @@ def expert_combine_backward(Y, slot, gate=None, *, B, L, dout=None, dsum=None, r
             out["dres"] = new(T, D, dtype=bf)
         if gamma is not None:
             out.update(dgamma=new(D), dbeta=new(D))
-    a = ExpertCombineBackwardArgs(
-        B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf),
+    a = _COMBINE_BACK.pack(
+        B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf, (M, D)),
         _at(slot, "slot", torch.int32, (T, k)), _at(gate, "gate", f32, (T, k)),
         _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)), eps,
         _at(dout, "dout", bf, (T, D)), _at(dsum, "dsum", bf, (T, D)), _at(out["dY"], "dY", bf, (M, D)),
         _at(out.get("dgate"), "dgate", f32, (T, k)), _at(out.get("dres"), "dres", bf, (T, D)),
         _at(out.get("dgamma"), "dgamma", f32, (D,)), _at(out.get("dbeta"), "dbeta", f32, (D,)))
-    _call("sc_expert_combine_backward", a, _work(workspace, Y.device, stream, B, L, 1, 1, D), stream)
+    _call(_COMBINE_BACK, a, _work(workspace, Y.device, stream, B, L, 1, 1, D), stream)
     return out
