@@ -24,24 +24,39 @@
 
 namespace sc {
 
-constexpr int kCombineWarps = 14;      // most of a CTA
-template <bool kBack>
-__host__ __device__ constexpr int combine_warps() { return kBack ? kCombineWarps : 8; }
+constexpr int kCombineWarps = 8;       // most of a CTA
 constexpr int kCombineChunk = 4;       // choices whose dot products are summed together
 
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+// Eight bf16 as four fp32 pairs, and back: the arithmetic runs on pairs (one instruction
+// each), because a gradient's row has some fifty operations a pair.
+__device__ __forceinline__ void unpack8(const uint4& v, uint64_t (&f)[4]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
+  for (int i = 0; i < 4; ++i) f[i] = f2_pack(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
 
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
-                    pack_bf16x2(f[6], f[7]));
+__device__ __forceinline__ uint4 pack8(const uint64_t (&f)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    f2_unpack(f[i], lo, hi);
+    w[i] = pack_bf16x2(lo, hi);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
+
+__device__ __forceinline__ uint64_t f2_both(float x) { return f2_pack(x, x); }
+__device__ __forceinline__ float f2_sum(uint64_t v) {
+  float lo, hi;
+  f2_unpack(v, lo, hi);
+  return lo + hi;
+}
+
+template <int N>
+struct Choices {
+  static constexpr int value = N;
+};
 
 // How a launch is cut: warps of a row, rows of a CTA at a time, copied tensors of a row,
 // rows on their way per row group (two, or one where two do not fit).
@@ -79,7 +94,7 @@ __device__ __forceinline__ void row_sum(const CombineCut& cut, CombineSmem& sm, 
 
 // V vectors of 8 features a thread; kRows rows on their way per row group.
 template <bool kBack, int V, int kRows>
-__global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
+__global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
     sc_combine_kernel(const __grid_constant__ CombineParams p, const CombineCut cut) {
   __shared__ CombineSmem sm;
   extern __shared__ uint4 fifo[];   // per warp [kRows][segs][V][32], then gamma (and beta)
@@ -110,9 +125,9 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
     }
     __syncthreads();
   }
-  const auto param = [&](const float4* v, int at, float (&f)[8]) {
+  const auto param = [&](const float4* v, int at, uint64_t (&f)[4]) {
     const float4 a = v[at], b = v[vecs + at];
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+    f[0] = f2_pack(a.x, a.y), f[1] = f2_pack(a.z, a.w), f[2] = f2_pack(b.x, b.y), f[3] = f2_pack(b.z, b.w);
   };
 
   // lane j has choice j of the row whose copies start next
@@ -125,18 +140,18 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
       in_next = t - b * p.L < __ldg(p.rows + b);
     }
     slot_next = -1;
-    gate_next = 1.f;
+    gate_next = 0.f;
     if (in_next && lane < p.k) {
       slot_next = __ldg(p.slot + t * p.k + lane);
       if (slot_next >= p.M) slot_next = -1;
-      if (p.gate != nullptr) gate_next = __ldg(p.gate + t * p.k + lane);
+      if (slot_next >= 0) gate_next = p.gate != nullptr ? __ldg(p.gate + t * p.k + lane) : 1.f;
     }
   };
-  const auto copy = [&](int r, int seg, const uint16_t* row) {
+  const auto copy = [&](int r, int seg, const uint16_t* row, bool there) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int at = at0 + v * at_step;
-      const bool in = at < vecs;
+      const bool in = there && at < vecs;
       cp_async16(smem_u32(mine + (r * cut.segs + seg) * V * 32 + 32 * v), row + (in ? 8 * at : 0), in);
     }
   };
@@ -150,22 +165,26 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
     if (lane == 0) sm.in[warp][r] = in_next;
     if (in_next) {
       for (int j = 0; j < p.k; ++j) {
-        const int s = __shfl_sync(0xffffffffu, slot_next, j);
-        if (s >= 0 && need_y) copy(r, j, p.y + static_cast<size_t>(s) * p.D);
+        const int s = __shfl_sync(0xffffffffu, slot_next, j);   // zeros where there is none
+        if (need_y) copy(r, j, p.y + static_cast<size_t>(max(s, 0)) * p.D, s >= 0);
       }
-      if (need_res) copy(r, seg_res, p.res + t * p.D);
-      if (kBack && norm) copy(r, seg_dout, p.dout + t * p.D);
-      if (kBack && p.dsum != nullptr) copy(r, seg_dsum, p.dsum + t * p.D);
+      if (need_res) copy(r, seg_res, p.res + t * p.D, true);
+      if (kBack && norm) copy(r, seg_dout, p.dout + t * p.D, true);
+      if (kBack && p.dsum != nullptr) copy(r, seg_dsum, p.dsum + t * p.D, true);
     }
     cp_async_commit();
     load_plan(t + step);
     __syncwarp();
   };
-  const auto piece = [&](int r, int seg, int v, float (&f)[8]) {
+  const auto piece = [&](int r, int seg, int v, uint64_t (&f)[4]) {
     unpack8(mine[(r * cut.segs + seg) * V * 32 + 32 * v], f);
   };
 
-  float dgam[kBack ? V : 1][8] = {}, dbet[kBack ? V : 1][8] = {};
+  uint64_t dgam[kBack ? V : 1][4], dbet[kBack ? V : 1][4];
+#pragma unroll
+  for (int v = 0; v < (kBack ? V : 1); ++v)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) dgam[v][q] = dbet[v][q] = f2_both(0.f);
   int turn = 0;
   long long t = static_cast<long long>(blockIdx.x) * cut.groups + group;
   load_plan(t);
@@ -179,28 +198,28 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
     }
     if (sm.in[warp][r]) {
       // S, and its normal form
-      float s[V][8], inv = 0.f;
+      uint64_t s[V][4];
+      float inv = 0.f;
       if (!kBack || norm) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
-          for (int q = 0; q < 8; ++q) s[v][q] = 0.f;
+          for (int q = 0; q < 4; ++q) s[v][q] = f2_both(0.f);
           if (need_res) {
-            float f[8];
-            piece(r, seg_res, v, f);
+            piece(r, seg_res, v, s[v]);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s[v][q] = p.res_scale * f[q];
+            for (int q = 0; q < 4; ++q) s[v][q] = f2_mul(s[v][q], f2_both(p.res_scale));
           }
         }
+#pragma unroll 2
         for (int j = 0; j < p.k; ++j) {
-          if (sm.slot[warp][r][j] < 0) continue;
-          const float g = sm.gate[warp][r][j];
+          const uint64_t g = f2_both(sm.gate[warp][r][j]);
 #pragma unroll
           for (int v = 0; v < V; ++v) {
-            float f[8];
+            uint64_t f[4];
             piece(r, j, v, f);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s[v][q] = fmaf(g, f[q], s[v][q]);
+            for (int q = 0; q < 4; ++q) s[v][q] = f2_fma(g, f[q], s[v][q]);
           }
         }
         if (!kBack && p.sum != nullptr)
@@ -211,29 +230,32 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
       }
       if (norm) {
         // two sums, so that a mean far from 0 costs no digits of the variance
-        float a[1] = {0.f};
+        uint64_t a2 = f2_both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int q = 0; q < 8; ++q) a[0] += s[v][q];
+          for (int q = 0; q < 4; ++q) a2 = f2_add(a2, s[v][q]);
+        float a[1] = {f2_sum(a2)};
         row_sum(cut, sm, group, w, turn, a);
         const float mean = a[0] / static_cast<float>(p.D);
-        a[0] = 0.f;
+        a2 = f2_both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const bool in = at0 + v * at_step < vecs;
+          // (features past D are and stay 0)
+          const uint64_t shift = f2_both(at0 + v * at_step < vecs ? -mean : 0.f);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            s[v][q] = in ? s[v][q] - mean : 0.f;
-            a[0] += s[v][q] * s[v][q];
+          for (int q = 0; q < 4; ++q) {
+            s[v][q] = f2_add(s[v][q], shift);
+            a2 = f2_fma(s[v][q], s[v][q], a2);
           }
         }
+        a[0] = f2_sum(a2);
         row_sum(cut, sm, group, w, turn, a);
         inv = 1.f / sqrtf(a[0] / static_cast<float>(p.D) + p.eps);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int q = 0; q < 8; ++q) s[v][q] *= inv;
+          for (int q = 0; q < 4; ++q) s[v][q] = f2_mul(s[v][q], f2_both(inv));
       }
       if constexpr (!kBack) {
         if (norm)
@@ -241,88 +263,97 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
           for (int v = 0; v < V; ++v) {
             const int at = at0 + v * at_step;
             if (at >= vecs) continue;
-            float ga[8], be[8];
+            uint64_t ga[4], be[4];
             param(gam, at, ga);
             param(bet, at, be);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) s[v][q] = fmaf(s[v][q], ga[q], be[q]);
+            for (int q = 0; q < 4; ++q) s[v][q] = f2_fma(s[v][q], ga[q], be[q]);
             reinterpret_cast<uint4*>(p.out + t * p.D)[at] = pack8(s[v]);
           }
       } else {
-        float ds[V][8];
-        float ab[2] = {0.f, 0.f};
+        uint64_t ds[V][4], ab0 = f2_both(0.f), ab1 = f2_both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
-          for (int q = 0; q < 8; ++q) ds[v][q] = 0.f;
+          for (int q = 0; q < 4; ++q) ds[v][q] = f2_both(0.f);
           const int at = at0 + v * at_step;
           if (!norm || at >= vecs) continue;
-          float f[8], ga[8];
+          uint64_t f[4], ga[4];
           piece(r, seg_dout, v, f);
           param(gam, at, ga);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            dgam[v][q] = fmaf(f[q], s[v][q], dgam[v][q]);
-            dbet[v][q] += f[q];
-            ds[v][q] = f[q] * ga[q];
-            ab[0] += ds[v][q];
-            ab[1] = fmaf(ds[v][q], s[v][q], ab[1]);
+          for (int q = 0; q < 4; ++q) {
+            dgam[v][q] = f2_fma(f[q], s[v][q], dgam[v][q]);
+            dbet[v][q] = f2_add(dbet[v][q], f[q]);
+            ds[v][q] = f2_mul(f[q], ga[q]);
+            ab0 = f2_add(ab0, ds[v][q]);
+            ab1 = f2_fma(ds[v][q], s[v][q], ab1);
           }
         }
         if (norm) {
+          float ab[2] = {f2_sum(ab0), f2_sum(ab1)};
           row_sum(cut, sm, group, w, turn, ab);
-          const float ma = ab[0] / static_cast<float>(p.D), mb = ab[1] / static_cast<float>(p.D);
+          // (dh - ma - h mb) / sigma
+          const uint64_t i2 = f2_both(inv), ma = f2_both(-ab[0] / static_cast<float>(p.D) * inv);
+          const uint64_t mb = f2_both(-ab[1] / static_cast<float>(p.D) * inv);
 #pragma unroll
           for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int q = 0; q < 8; ++q) ds[v][q] = inv * (ds[v][q] - ma - s[v][q] * mb);
+            for (int q = 0; q < 4; ++q) ds[v][q] = f2_fma(s[v][q], mb, f2_fma(ds[v][q], i2, ma));
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int at = at0 + v * at_step;
-          const bool in = at < vecs;
-          float f[8];
+          uint64_t f[4];
           if (p.dsum != nullptr) {
             piece(r, seg_dsum, v, f);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) ds[v][q] += f[q];
+            for (int q = 0; q < 4; ++q) ds[v][q] = f2_add(ds[v][q], f[q]);
           }
-          if (p.dres != nullptr && in) {
+          if (p.dres != nullptr && at < vecs) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) f[q] = p.res_scale * ds[v][q];
+            for (int q = 0; q < 4; ++q) f[q] = f2_mul(ds[v][q], f2_both(p.res_scale));
             reinterpret_cast<uint4*>(p.dres + t * p.D)[at] = pack8(f);
           }
         }
-        for (int j0 = 0; j0 < p.k; j0 += kCombineChunk) {
-          float dot[kCombineChunk];
+        // N choices together (past the last one again that one, unwritten): dY and dot products
+        const auto choices = [&](int j0, auto n) {
+          constexpr int N = decltype(n)::value;
+          float dot[N];
 #pragma unroll
-          for (int j = 0; j < kCombineChunk; ++j) {
-            dot[j] = 0.f;
-            const int sl = j0 + j < p.k ? sm.slot[warp][r][j0 + j] : -1;
-            if (sl < 0) continue;
-            const float g = sm.gate[warp][r][j0 + j];
-            uint4* const dy = reinterpret_cast<uint4*>(p.dy + static_cast<size_t>(sl) * p.D);
+          for (int i = 0; i < N; ++i) {
+            const int j = min(j0 + i, p.k - 1);
+            const int sl = j0 + i < p.k ? sm.slot[warp][r][j] : -1;
+            const uint64_t g = f2_both(sm.gate[warp][r][j]);
+            uint4* const dy = reinterpret_cast<uint4*>(p.dy + static_cast<size_t>(max(sl, 0)) * p.D);
+            uint64_t dot2 = f2_both(0.f);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
               const int at = at0 + v * at_step;
-              if (at >= vecs) continue;
-              float f[8];
+              uint64_t f[4];
               if (p.dgate != nullptr) {
-                piece(r, j0 + j, v, f);
+                piece(r, j, v, f);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) dot[j] = fmaf(ds[v][q], f[q], dot[j]);
+                for (int q = 0; q < 4; ++q) dot2 = f2_fma(ds[v][q], f[q], dot2);
               }
 #pragma unroll
-              for (int q = 0; q < 8; ++q) f[q] = g * ds[v][q];
-              dy[at] = pack8(f);
+              for (int q = 0; q < 4; ++q) f[q] = f2_mul(g, ds[v][q]);
+              if (sl >= 0 && at < vecs) dy[at] = pack8(f);
             }
+            dot[i] = f2_sum(dot2);
           }
           if (p.dgate != nullptr) {
             row_sum(cut, sm, group, w, turn, dot);
 #pragma unroll
-            for (int j = 0; j < kCombineChunk; ++j)
-              if (w == 0 && lane == 0 && j0 + j < p.k) p.dgate[t * p.k + j0 + j] = dot[j];
+            for (int i = 0; i < N; ++i)
+              if (w == 0 && lane == 0 && j0 + i < p.k)
+                p.dgate[t * p.k + j0 + i] = sm.slot[warp][r][j0 + i] >= 0 ? dot[i] : 0.f;
           }
+        };
+        if (p.k <= 2) {
+          choices(0, Choices<2>());
+        } else {
+          for (int j0 = 0; j0 < p.k; j0 += kCombineChunk) choices(j0, Choices<kCombineChunk>());
         }
       }
     } else if (kBack && p.dgate != nullptr && w == 0 && lane < p.k) {
@@ -341,9 +372,9 @@ __global__ void __launch_bounds__(32 * combine_warps<kBack>(), kBack ? 1 : 2)
       const int at = at0 + v * at_step;
       if (at >= vecs) continue;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        part[(2 * group) * p.D + 8 * at + q] = dgam[v][q];
-        part[(2 * group + 1) * p.D + 8 * at + q] = dbet[v][q];
+      for (int q = 0; q < 4; ++q) {
+        *reinterpret_cast<uint64_t*>(part + (2 * group) * p.D + 8 * at + 2 * q) = dgam[v][q];
+        *reinterpret_cast<uint64_t*>(part + (2 * group + 1) * p.D + 8 * at + 2 * q) = dbet[v][q];
       }
     }
     __syncthreads();
@@ -414,11 +445,9 @@ template <bool kBack>
 static cudaError_t combine(const CombineParams& p, cudaStream_t st) {
   const bool norm = p.gamma != nullptr;
   CombineCut cut;
-  // Forward: a warp a row up to 1024 features (three warps for 768 features: 25 us, not
-  // 16).  The gradient: half as many features a thread while a CTA has the warps, for its
-  // long chain of arithmetic a row.
-  const int per_warp = kBack && p.D <= 512 * kCombineWarps ? 512 : 1024;
-  cut.warps = (p.D + per_warp - 1) / per_warp;
+  // a warp a row up to 1024 features (more warps a row: 768 features forward, three, 25 us
+  // instead of 16; gradient of 1024, two or four, 57 or 63 us instead of 54)
+  cut.warps = (p.D + 1023) / 1024;
   const int vecs = (p.D + 256 * cut.warps - 1) / (256 * cut.warps);
   cut.segs = p.k + (p.res != nullptr && (!kBack || norm) ? 1 : 0) +
              (kBack ? (norm ? 1 : 0) + (p.dsum != nullptr ? 1 : 0) : 0);
@@ -428,7 +457,7 @@ static cudaError_t combine(const CombineParams& p, cudaStream_t st) {
   const size_t params = norm ? sizeof(float) * p.D * (kBack ? 1 : 2) : 0;
   const size_t most = (kBack ? kCombineBytes : kCombineBytes / 2) - params;
   const int rows = row * 2 <= most ? 2 : 1;
-  cut.groups = combine_warps<kBack>() / cut.warps;
+  cut.groups = kCombineWarps / cut.warps;
   while (cut.groups > 1 && row * rows * cut.groups > most) --cut.groups;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
