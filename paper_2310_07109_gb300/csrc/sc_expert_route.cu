@@ -24,6 +24,7 @@ constexpr int kRouteThreads = 1024;
 constexpr int kRouteBackThreads = 256;
 constexpr int kRouteWords = kRouteTokens / 32;
 constexpr int kRoutePerWarp = kRouteTokens / (kRouteThreads / 32);   // tokens of a warp per chunk
+static_assert(kRouteTokens * kMaxChoices <= kRouteThreads, "an item a thread");
 
 // Order-preserving map of a float to an unsigned number; 0 below every value that
 // may be chosen (NaN, -inf).
@@ -32,6 +33,11 @@ __device__ __forceinline__ uint32_t route_key(float x) {
   x += 0.f;   // -0 and +0 tie
   const uint32_t u = __float_as_uint(x);
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// The float of a key that is not 0.
+__device__ __forceinline__ float route_value(uint32_t key) {
+  return __uint_as_float((key & 0x80000000u) ? key & 0x7fffffffu : ~key);
 }
 
 // exp(x - m), m >= x the maximum of the row; 1 where x equals m.
@@ -67,12 +73,17 @@ __device__ __forceinline__ void scan_experts(const int* v, int n, int* to, int* 
   if (lane == 0) *total = run;
 }
 
-// From the ranks in `slot` to slots, and the slots' tokens: items i0 .. i1 (token x choice).
-__device__ __forceinline__ void place_items(const RouteParams& p, const int* base, int total, int i0, int i1) {
+// Where items (token x choice) i0 .. i1 go, from their ranks: slots, and the slots' tokens.
+// `expert` and `rank`: of item i0 + threadIdx.x, loaded before.
+__device__ __forceinline__ void place_items(const RouteParams& p, const int* base, int total, int i0, int i1,
+                                            int expert, int rank) {
   for (int i = i0 + threadIdx.x; i < i1; i += kRouteThreads) {
-    const int e = p.expert[i];
-    if (e >= 0) {
-      const int s = base[e] + p.slot[i];
+    if (i >= i0 + kRouteThreads) {
+      expert = p.expert[i];
+      rank = p.slot[i];
+    }
+    if (expert >= 0) {
+      const int s = base[expert] + rank;
       p.slot[i] = s;
       p.token[s] = i / p.k;
     }
@@ -89,6 +100,7 @@ template <int V>
 __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
     const __grid_constant__ RouteParams p) {
   __shared__ int count[kMaxExperts], base[kMaxExperts], total;   // count: before this chunk
+  __shared__ int16_t pick[kRouteTokens * kMaxChoices];
   extern __shared__ uint32_t mask[];                             // [E][kRouteWords]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   for (int i = tid; i < p.E * kRouteWords; i += kRouteThreads) mask[i] = 0;
@@ -98,6 +110,7 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
   __syncthreads();
   const int t0 = blockIdx.x * p.per_cta;
   const int t1 = static_cast<int>(min(static_cast<long long>(t0) + p.per_cta, p.T));
+  int first_expert = -1, first_rank = -1;
   for (int c0 = t0; c0 < t1; c0 += kRouteTokens) {
     const int n = min(t1 - c0, kRouteTokens);
     float x[kRoutePerWarp][V];
@@ -111,65 +124,79 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
         x[u][v] = in && e < p.E ? __ldg(p.logits + t * p.ld + e) : -INFINITY;
       }
     }
+    // choice by choice, the warp's tokens side by side
+    uint32_t key[kRoutePerWarp][V];
+    float top[kRoutePerWarp], mine[kRoutePerWarp];
+    int my_expert[kRoutePerWarp];
 #pragma unroll
     for (int u = 0; u < kRoutePerWarp; ++u) {
-      const int i = warp * kRoutePerWarp + u, t = c0 + i;
-      if (i >= n) break;
-      uint32_t key[V];
+      top[u] = mine[u] = 0.f;
+      my_expert[u] = -1;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        key[v] = route_key(x[u][v]);
-        if (key[v] == 0u) x[u][v] = -INFINITY;
+        key[u][v] = route_key(x[u][v]);
+        if (key[u][v] == 0u) x[u][v] = -INFINITY;
       }
-      float top = 0.f, sum = 0.f, mine = 0.f;
-      int my_expert = -1;
-      for (int j = 0; j < p.k; ++j) {
-        uint32_t best = key[0];
+    }
+    for (int j = 0; j < p.k; ++j) {
+      uint32_t best[kRoutePerWarp];
+      int at[kRoutePerWarp];
 #pragma unroll
-        for (int v = 1; v < V; ++v) best = max(best, key[v]);
-        best = __reduce_max_sync(0xffffffffu, best);
-        if (best == 0u) break;
-        int at = 0x7fffffff;
-        float val = 0.f;
+      for (int u = 0; u < kRoutePerWarp; ++u) {
+        best[u] = key[u][0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) best[u] = max(best[u], key[u][v]);
+        best[u] = __reduce_max_sync(0xffffffffu, best[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kRoutePerWarp; ++u) {
+        at[u] = 0x7fffffff;
 #pragma unroll
         for (int v = V - 1; v >= 0; --v)
-          if (key[v] == best) at = lane + 32 * v, val = x[u][v];
-        const int e = __reduce_min_sync(0xffffffffu, at);
-        val = __shfl_sync(0xffffffffu, val, e & 31);
+          if (key[u][v] == best[u]) at[u] = lane + 32 * v;
+        at[u] = __reduce_min_sync(0xffffffffu, at[u]);   // the lowest expert with it
+      }
+#pragma unroll
+      for (int u = 0; u < kRoutePerWarp; ++u) {
+        if (best[u] == 0u) continue;   // none is left
 #pragma unroll
         for (int v = 0; v < V; ++v)
-          if (e == lane + 32 * v) key[v] = 0u;
-        if (j == 0) {
-          top = val;
-          if (!p.renormalize) {
-            float all = 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) all += route_exp(x[u][v], top);
-            sum = warp_sum(all);
-          }
-        }
-        if (lane == j) mine = val, my_expert = e;
+          if (at[u] == lane + 32 * v) key[u][v] = 0u;
+        if (j == 0) top[u] = route_value(best[u]);
+        if (lane == j) mine[u] = route_value(best[u]), my_expert[u] = at[u];
       }
-      mine = my_expert >= 0 ? route_exp(mine, top) : 0.f;
-      if (p.renormalize) sum = warp_sum(mine);
-      if (lane < p.k) {
-        p.expert[t * p.k + lane] = my_expert;
-        p.gate[t * p.k + lane] = my_expert >= 0 ? mine / sum : 0.f;
-        if (my_expert >= 0)
-          atomicOr(&mask[my_expert * kRouteWords + (i >> 5)], 1u << (i & 31));
+    }
+#pragma unroll
+    for (int u = 0; u < kRoutePerWarp; ++u) {
+      const int i = warp * kRoutePerWarp + u;
+      const bool some = __any_sync(0xffffffffu, my_expert[u] >= 0);
+      mine[u] = my_expert[u] >= 0 ? route_exp(mine[u], top[u]) : 0.f;
+      float sum = mine[u];
+      if (!p.renormalize && some) {
+        sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum += route_exp(x[u][v], top[u]);
+      }
+      sum = warp_sum(sum);
+      if (lane < p.k && i < n) {
+        pick[i * p.k + lane] = static_cast<int16_t>(my_expert[u]);
+        p.gate[(c0 + i) * p.k + lane] = my_expert[u] >= 0 ? mine[u] / sum : 0.f;
+        if (my_expert[u] >= 0) atomicOr(&mask[my_expert[u] * kRouteWords + (i >> 5)], 1u << (i & 31));
       }
     }
     __syncthreads();
     for (int i = tid; i < n * p.k; i += kRouteThreads) {
-      const int at = c0 * p.k + i;
-      const int e = p.expert[at], r = i / p.k;
+      const int e = pick[i], r = i / p.k;
       int rank = -1;
       if (e >= 0) {
         rank = count[e];
         for (int q = 0; q < (r >> 5); ++q) rank += __popc(mask[e * kRouteWords + q]);
         rank += __popc(mask[e * kRouteWords + (r >> 5)] & ((1u << (r & 31)) - 1u));
       }
-      p.slot[at] = rank;
+      p.expert[c0 * p.k + i] = e;
+      p.slot[c0 * p.k + i] = rank;
+      first_expert = e;   // (one chunk of at most 1024 items: this thread's only one)
+      first_rank = rank;
     }
     __syncthreads();
     for (int e = tid; e < p.E; e += kRouteThreads) {
@@ -190,7 +217,7 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
   if (warp == 0) scan_experts(count, p.E, base, &total);
   __syncthreads();
   for (int e = tid; e <= p.E; e += kRouteThreads) p.offsets[e] = e < p.E ? base[e] : total;
-  place_items(p, base, total, t0 * p.k, t1 * p.k);
+  place_items(p, base, total, t0 * p.k, t1 * p.k, first_expert, first_rank);
 }
 
 // Adds up the counts: an expert's first slot, and within it this CTA's; then turns
@@ -203,6 +230,13 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_place_kernel(
   for (int e = tid; e < p.E; e += kRouteThreads) base[e] = all[e] = 0;
   pdl_wait();
   pdl_launch_dependents();
+  const int i0 = blockIdx.x * p.per_cta * p.k;
+  const int i1 = static_cast<int>(min(static_cast<long long>(i0) + p.per_cta * p.k, p.T * p.k));
+  int expert = -1, rank = -1;
+  if (i0 + tid < i1) {
+    expert = p.expert[i0 + tid];
+    rank = p.slot[i0 + tid];
+  }
   __syncthreads();
   // thread: expert tid % E of every (threads / E)-th CTA; whole numbers, any order
   const int per = kRouteThreads / p.E, e = tid % p.E, g = tid / p.E;
@@ -222,9 +256,7 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_place_kernel(
   __syncthreads();
   if (blockIdx.x == 0)   // its own slots begin where the experts' do
     for (int o = tid; o <= p.E; o += kRouteThreads) p.offsets[o] = o < p.E ? base[o] : total;
-  const int i0 = blockIdx.x * p.per_cta * p.k;
-  const int i1 = static_cast<int>(min(static_cast<long long>(i0) + p.per_cta * p.k, p.T * p.k));
-  place_items(p, base, total, i0, i1);
+  place_items(p, base, total, i0, i1, expert, rank);
 }
 
 // d logits of the gates.  With inner = sum_j g_j dg_j: at a chosen expert
