@@ -136,8 +136,8 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
   const auto load_plan = [&](long long t) {
     in_next = t < p.T;
     if (in_next && p.rows != nullptr) {
-      const long long b = t / p.L;
-      in_next = t - b * p.L < __ldg(p.rows + b);
+      const unsigned b = static_cast<unsigned>(t) / static_cast<unsigned>(p.L);   // t < 2^31
+      in_next = static_cast<int>(static_cast<unsigned>(t) - b * p.L) < __ldg(p.rows + b);
     }
     slot_next = -1;
     gate_next = 0.f;

@@ -122,9 +122,9 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// min(|x|, 16): the tail is 0 from there on, and a pair may share a reciprocal
-__device__ __forceinline__ uint64_t clamped_abs2(float x0, float x1) {
-  return f2_pack(fminf(fabsf(x0), 16.f), fminf(fabsf(x1), 16.f));
+// min(|x|, most), where the tail is next to nothing, so that a pair may share a reciprocal.
+__device__ __forceinline__ uint64_t clamped_abs2(float x0, float x1, float most) {
+  return f2_pack(fminf(fabsf(x0), most), fminf(fabsf(x1), most));
 }
 __device__ __forceinline__ float relu_nan(float x) {
   float y;
@@ -148,7 +148,8 @@ __device__ __forceinline__ void normal_tail2(uint64_t ax, uint64_t& qt, uint64_t
 }
 // GELU(x) = max(x, 0) - |x| Phi(-|x|)
 __device__ __forceinline__ void gelu2(float& x0, float& x1) {
-  const uint64_t ax = clamped_abs2(x0, x1);
+  // (at 8: the denominators are at most 1.3e14, and 8 Phi(-8) is taken for 3e-14)
+  const uint64_t ax = clamped_abs2(x0, x1, 8.f);
   // the coefficients times 2^(-i/2)
   uint64_t d = f2_fma(ax, f2_both(0.0000430638f * 0.125f), f2_both(0.0002765672f * 0.17677669529663688f));
   d = f2_fma(d, ax, f2_both(0.0001520143f * 0.25f));
@@ -159,7 +160,7 @@ __device__ __forceinline__ void gelu2(float& x0, float& x1) {
   d = f2_mul(d, d);
   d = f2_mul(d, d);
   d = f2_mul(d, d);
-  d = f2_mul(d, d);   // at most 3e34: where the product of two overflows, both tails are 0
+  d = f2_mul(d, d);
   float d0, d1;
   f2_unpack(d, d0, d1);
   const uint64_t h = f2_mul(f2_mul(ax, f2_both(-0.5f * rcp_approx(d0 * d1))), f2_pack(d1, d0));
@@ -167,7 +168,7 @@ __device__ __forceinline__ void gelu2(float& x0, float& x1) {
 }
 // y *= GELU'(x) = 1/2 + sign(x) (1/2 - Phi(-|x|) + |x| phi(x))
 __device__ __forceinline__ void gelu_slope2(float x0, float x1, float& y0, float& y1) {
-  const uint64_t ax = clamped_abs2(x0, x1);
+  const uint64_t ax = clamped_abs2(x0, x1, 16.f);
   uint64_t qt, e;
   normal_tail2(ax, qt, e);
   float u0, u1;

@@ -49,9 +49,9 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-__device__ __forceinline__ bool token_in_use(const int32_t* rows, int L, long long t) {
+__device__ __forceinline__ bool token_in_use(const int32_t* rows, int L, int t) {
   if (rows == nullptr) return true;
-  const long long b = t / L;
+  const int b = t / L;
   return t - b * L < __ldg(rows + b);
 }
 
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kRouteBackThreads) sc_route_back_kernel(
   const int lane = threadIdx.x & 31;
   const long long t = static_cast<long long>(blockIdx.x) * (kRouteBackThreads / 32) + (threadIdx.x >> 5);
   if (t >= p.T) return;
-  const bool in = token_in_use(p.rows, p.L, t);
+  const bool in = token_in_use(p.rows, p.L, static_cast<int>(t));
   int e = -1;
   float g = 0.f, dg = 0.f;
   if (lane < p.k && in) {

@@ -243,6 +243,7 @@ def product_inputs(seed, counts, rows, width, *, gather, pad, first=0, spare=5):
     (False, 8, False, False, True, False, 3),
     (True, 24, True, False, True, True, 2),
     (False, 0, False, True, False, True, 0),
+    (False, 16, True, True, True, True, 1),
 ])
 def test_expert_linear_forward(counts, N, K, gather, pad, gelu, pre, f32, bias, first):
     E = len(counts)
@@ -361,6 +362,91 @@ def test_expert_linear_keeps_rows_apart():
     got = sc.expert_linear_backward_weight(dY, bad, off)
     assert torch.equal(got["dW"][[0, 2]], clean["dW"][[0, 2]])
     assert bool(got["dW"][1].isnan().all())
+
+
+def test_expert_linear_offsets_out_of_range():
+    """Offsets and tokens outside their ranges are held inside them: nothing else is touched."""
+    M, N, K, rows = 40, 64, 72, 11
+    g = gen(1)
+    X, W = bf16(randn(g, rows, K)), bf16(randn(g, 3, N, K))
+    off = torch.tensor([-5, 25, 20, 90], dtype=torch.int32, device="cuda")     # not even in order
+    token = torch.tensor([-1, rows, 1 << 30] + [3] * (M - 3), dtype=torch.int32, device="cuda")
+    guard = torch.full((M + 2, N), 5.0, device="cuda", dtype=torch.bfloat16)
+    ws = sc.new_expert_workspace(1, 1, 1, 1, 8)
+    sc.expert_linear_forward(X, W, off, token=token, out=guard[1:-1], workspace=ws)
+    sc.expert_linear_backward_weight(bf16(randn(g, M, N)), X, off, token=token, workspace=ws)
+    assert sc.workspace_status(ws) == 0
+    assert bool((guard[0] == 5).all()) and bool((guard[-1] == 5).all())
+    want = X[3].double() @ W[0].double().T
+    check(guard[11], want, (K + 16) * U_F32 * (X[3].double().abs() @ W[0].double().abs().T), U_BF16, "slot 10")
+
+
+@pytest.mark.parametrize("M", [1, 7, 16, 17])
+@pytest.mark.parametrize("gelu,pre,f32", [(True, True, False), (False, False, True)])
+def test_expert_linear_few_slots(M, gelu, pre, f32):
+    """Around the number of slots below which another kernel runs, some of them not in use."""
+    E, N, K = 40, 152, 264
+    g = gen(M)
+    X, W, b = bf16(randn(g, 5, K)), bf16(randn(g, E, N, K) / 16), randn(g, E, N)
+    used = max(1, M - 2)
+    pick = torch.randint(0, E, (used,), device="cuda", generator=g).sort().values
+    off = torch.searchsorted(pick, torch.arange(E + 1, device="cuda")).int()
+    token = torch.randint(0, 5, (M,), device="cuda", generator=g).int()
+    out = torch.full((M, N), -7.0, device="cuda", dtype=torch.float32 if f32 else torch.bfloat16)
+    prev = torch.full((M, N), -9.0, device="cuda", dtype=torch.bfloat16) if pre else None
+    sc.expert_linear_forward(X, W, off, token=token, bias=b, gelu=gelu, pre=prev, out=out)
+    x = X[token[:used].long()].double()
+    y = torch.einsum("sk,snk->sn", x, W[pick].double()) + b[pick].double()
+    slack = (K + 16) * U_F32 * (torch.einsum("sk,snk->sn", x.abs(), W[pick].double().abs()) + b[pick].abs().double())
+    check(out[:used], gelu64(y) if gelu else y, 1.13 * slack + (4e-7 * (1 + y.abs()) if gelu else 0.0),
+          U_F32 if f32 else U_BF16, "out")
+    assert bool((out[used:] == -7.0).all())
+    if pre:
+        check(prev[:used], y, slack, U_BF16, "pre")
+        assert bool((prev[used:] == -9.0).all())
+
+
+def test_gelu_of_infinities_and_nan():
+    """Values that overflow, and NaN, next to ordinary ones: each stays its own."""
+    N, K, M = 64, 64, 40
+    W = torch.zeros(1, N, K, device="cuda", dtype=torch.bfloat16)
+    W[0, :, 0] = 1
+    vals = torch.tensor([math.inf, 1.0, -math.inf, -1.0, math.nan, 2.0, 3e38, -2.0, -3e38, 0.5], device="cuda")
+    X = torch.zeros(M, K, device="cuda", dtype=torch.bfloat16)
+    X[:, 0] = bf16(vals.repeat(4))
+    off = offsets_of([M])
+    want = torch.nn.functional.gelu(X[:, :1].double()).expand(M, N)
+    want = torch.where(X[:, :1].isinf() & (X[:, :1] < 0), 0.0, want)       # the limit, where the product is NaN
+    for rows in (M, 10):                                                   # both kernels
+        got = sc.expert_linear_forward(X[:rows], W, offsets_of([rows]), gelu=True).double()
+        ref = want[:rows]
+        assert bool((got.isnan() == ref.isnan()).all())
+        fin = ~ref.isnan()
+        same = (got == ref) | ((got - ref).abs() <= U_BF16 * ref.abs() + 1e-6)
+        assert bool(same[fin].all())
+
+
+@pytest.mark.parametrize("rows", [250, 16])
+def test_gelu_and_its_slope_beside_outliers(rows):
+    """Ordinary values whose neighbours are far out (the arithmetic runs on pairs)."""
+    N, K = 64, 64
+    x = torch.linspace(-7, 7, rows, device="cuda")
+    x[1::2] = torch.tensor([100.0, -9.0, 3e4, -1e6, 8.0], device="cuda").repeat(rows)[: rows // 2]
+    for shift in (0, 1):
+        X = torch.zeros(rows, K, device="cuda", dtype=torch.bfloat16)
+        X[:, 0] = bf16(x.roll(shift))
+        W = torch.zeros(1, N, K, device="cuda", dtype=torch.bfloat16)
+        W[0, :, 0] = 1
+        v = X[:, :1].double().expand(rows, N)
+        got = sc.expert_linear_forward(X, W, offsets_of([rows]), gelu=True, out_f32=True)
+        check(got, gelu64(v), 4e-7 * (1 + v.abs().clamp(max=10)), U_F32, "gelu")
+        pre = X[:, :1].expand(rows, K).contiguous()
+        dY = torch.zeros(rows, N, device="cuda", dtype=torch.bfloat16)
+        dY[:, 0] = 1
+        one = torch.zeros(1, N, K, device="cuda", dtype=torch.bfloat16)
+        one[0, 0] = 1
+        got = sc.expert_linear_backward_input(dY, one, offsets_of([rows]), pre=pre, out_f32=True)
+        check(got, gelu_slope64(pre.double()), 2e-6, U_F32, "slope")
 
 
 def test_expert_linear_on_another_stream():
