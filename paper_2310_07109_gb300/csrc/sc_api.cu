@@ -1580,7 +1580,17 @@ namespace sc {
 
 int api_fail(int code, const char* what, const char* detail) { return fail(code, what, detail); }
 int api_fail_cuda(const char* what, cudaError_t e) { return fail_cuda(what, e); }
-int api_ensure_configured() { return ensure_configured(); }
+// Once a device is set up, its number alone: a call on a few rows is all host time.
+int api_ensure_configured() {
+  static std::atomic<bool> ready[256];
+  int dev = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 256 &&
+      ready[dev].load(std::memory_order_acquire))
+    return SC_OK;
+  const int rc = ensure_configured();
+  if (rc == SC_OK && dev >= 0 && dev < 256) ready[dev].store(true, std::memory_order_release);
+  return rc;
+}
 PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder() { return get_encoder(); }
 
 }  // namespace sc

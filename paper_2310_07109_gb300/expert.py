@@ -101,7 +101,7 @@ class _Entry:
 
     def bind(self):
         rest = [_P, ctypes.c_size_t, _P] if self.name in _WITH_WORKSPACE else [_P]
-        self.call = ctypes.CFUNCTYPE(_I, _P, *rest)((self.name, _library()))
+        self.call = ctypes.CFUNCTYPE(_I, ctypes.c_char_p, *rest)((self.name, _library()))
         return self.call
 
 
@@ -115,13 +115,14 @@ def _refuse(what):
     raise _b.SparseCoderError(_b.SC_ERR_INVALID_ARG, what)
 
 
-def _at(t, name, dtype, shape):
-    """The address of a contiguous cuda tensor of this type and shape; 0 for None."""
+def _at(t, name, dtype, count):
+    """The address of a contiguous cuda tensor of this type with so many elements (their
+    shape may be any that the rows run through in order); 0 for None."""
     if t is None:
         return 0
-    if t.dtype is dtype and t.is_contiguous() and t.is_cuda and t.shape == shape:
+    if t.dtype is dtype and t.numel() == count and t.is_contiguous() and t.is_cuda:
         return t.data_ptr()
-    _refuse("%s: a contiguous cuda tensor of %s and shape %s is wanted" % (name, dtype, tuple(shape)))
+    _refuse("%s: a contiguous cuda tensor of %s with %d elements is wanted" % (name, dtype, count))
 
 
 def _rows_at(t, name, dtype):
@@ -199,11 +200,11 @@ def expert_route_forward(logits, *, k, B, L, rows=None, renormalize=True, out=No
         out = {"expert": new(T, k), "gate": new(T, k, dtype=torch.float32), "offsets": new(E + 1),
                "slot": new(T, k), "token": new(T * k)}
     i32 = torch.int32
-    a = _ROUTE.pack(B, L, E, k, at, ld, _at(rows, "rows", i32, (B,)), 1 if renormalize else 0,
-                  _at(out["expert"], "expert", i32, (T, k)),
-                  _at(out["gate"], "gate", torch.float32, (T, k)),
-                  _at(out["offsets"], "offsets", i32, (E + 1,)),
-                  _at(out["slot"], "slot", i32, (T, k)), _at(out["token"], "token", i32, (T * k,)))
+    a = _ROUTE.pack(B, L, E, k, at, ld, _at(rows, "rows", i32, B), 1 if renormalize else 0,
+                  _at(out["expert"], "expert", i32, T * k),
+                  _at(out["gate"], "gate", torch.float32, T * k),
+                  _at(out["offsets"], "offsets", i32, E + 1),
+                  _at(out["slot"], "slot", i32, T * k), _at(out["token"], "token", i32, T * k))
     _call(_ROUTE, a, _work(workspace, logits.device, stream, B, L, E, k, 8), stream)
     return out
 
@@ -218,10 +219,10 @@ def expert_route_backward(logits, expert, gate, dgate, *, B, L, rows=None, renor
     if out is None:
         out = torch.empty((T, E), dtype=torch.float32, device=logits.device)
     f32 = torch.float32
-    a = _ROUTE_BACK.pack(B, L, E, k, at, ld, _at(rows, "rows", torch.int32, (B,)),
-                          1 if renormalize else 0, _at(expert, "expert", torch.int32, (T, k)),
-                          _at(gate, "gate", f32, (T, k)), _at(dgate, "dgate", f32, (T, k)),
-                          _at(out, "dlogits", f32, (T, E)))
+    a = _ROUTE_BACK.pack(B, L, E, k, at, ld, _at(rows, "rows", torch.int32, B),
+                          1 if renormalize else 0, _at(expert, "expert", torch.int32, T * k),
+                          _at(gate, "gate", f32, T * k), _at(dgate, "dgate", f32, T * k),
+                          _at(out, "dlogits", f32, T * E))
     _call_plain(_ROUTE_BACK, a, logits, stream)
     return out
 
@@ -238,14 +239,14 @@ def expert_linear_forward(X, W, offsets, *, token=None, bias=None, gelu=False, p
     or the rows of X."""
     at, xr, K, ld = _rows_at(X, "X", torch.bfloat16)
     E, N, _ = W.shape
-    M = xr if token is None else token.shape[0]
+    M = xr if token is None else token.numel()
     if out is None:
         out = torch.empty((M, N), dtype=torch.float32 if out_f32 else torch.bfloat16, device=X.device)
     i32 = torch.int32
-    a = _LINEAR.pack(M, E, N, K, at, ld, xr, _at(token, "token", i32, (M,)),
-                         _at(offsets, "offsets", i32, (E + 1,)), _at(W, "W", torch.bfloat16, (E, N, K)),
-                         _at(bias, "bias", torch.float32, (E, N)), 1 if gelu else 0,
-                         _at(pre, "pre", torch.bfloat16, (M, N)), _at(out, "out", out.dtype, (M, N)),
+    a = _LINEAR.pack(M, E, N, K, at, ld, xr, _at(token, "token", i32, M),
+                         _at(offsets, "offsets", i32, E + 1), _at(W, "W", torch.bfloat16, E * N * K),
+                         _at(bias, "bias", torch.float32, E * N), 1 if gelu else 0,
+                         _at(pre, "pre", torch.bfloat16, M * N), _at(out, "out", out.dtype, M * N),
                          _out_type(out))
     _call(_LINEAR, a, _product_ws(workspace, X, stream), stream)
     return out
@@ -259,10 +260,10 @@ def expert_linear_backward_input(dY, W, offsets, *, pre=None, out=None, out_f32=
     E, _, K = W.shape
     if out is None:
         out = torch.empty((M, K), dtype=torch.float32 if out_f32 else torch.bfloat16, device=dY.device)
-    a = _BACK_X.pack(M, E, N, K, at, ld, _at(offsets, "offsets", torch.int32, (E + 1,)),
-                                      _at(W, "W", torch.bfloat16, (E, N, K)),
-                                      _at(pre, "pre", torch.bfloat16, (M, K)),
-                                      _at(out, "out", out.dtype, (M, K)), _out_type(out))
+    a = _BACK_X.pack(M, E, N, K, at, ld, _at(offsets, "offsets", torch.int32, E + 1),
+                                      _at(W, "W", torch.bfloat16, E * N * K),
+                                      _at(pre, "pre", torch.bfloat16, M * K),
+                                      _at(out, "out", out.dtype, M * K), _out_type(out))
     _call(_BACK_X, a, _product_ws(workspace, dY, stream), stream)
     return out
 
@@ -282,10 +283,10 @@ def expert_linear_backward_weight(dY, X, offsets, *, token=None, bias=True, out=
             out["dbias"] = torch.empty((E, N), dtype=torch.float32, device=X.device)
     dW = out["dW"]
     a = _BACK_W.pack(M, E, N, K, ay, ldy, ax, ldx, xr,
-                                       _at(token, "token", torch.int32, (M,)),
-                                       _at(offsets, "offsets", torch.int32, (E + 1,)),
-                                       _at(dW, "dW", dW.dtype, (E, N, K)), _out_type(dW),
-                                       _at(out.get("dbias"), "dbias", torch.float32, (E, N)))
+                                       _at(token, "token", torch.int32, M),
+                                       _at(offsets, "offsets", torch.int32, E + 1),
+                                       _at(dW, "dW", dW.dtype, E * N * K), _out_type(dW),
+                                       _at(out.get("dbias"), "dbias", torch.float32, E * N))
     _call(_BACK_W, a, _product_ws(workspace, X, stream), stream)
     return out
 
@@ -302,11 +303,11 @@ def expert_combine_forward(Y, slot, gate=None, *, B, L, rows=None, res=None, res
         if gamma is not None:
             out["out"] = torch.empty((T, D), dtype=torch.bfloat16, device=Y.device)
     bf, f32 = torch.bfloat16, torch.float32
-    a = _COMBINE.pack(B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf, (M, D)),
-                          _at(slot, "slot", torch.int32, (T, k)), _at(gate, "gate", f32, (T, k)),
-                          _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)),
-                          _at(beta, "beta", f32, (D,)), eps, _at(out.get("sum"), "sum", bf, (T, D)),
-                          _at(out.get("out"), "out", bf, (T, D)))
+    a = _COMBINE.pack(B, L, D, k, M, _at(rows, "rows", torch.int32, B), _at(Y, "Y", bf, M * D),
+                          _at(slot, "slot", torch.int32, T * k), _at(gate, "gate", f32, T * k),
+                          _at(res, "res", bf, T * D), res_scale, _at(gamma, "gamma", f32, D),
+                          _at(beta, "beta", f32, D), eps, _at(out.get("sum"), "sum", bf, T * D),
+                          _at(out.get("out"), "out", bf, T * D))
     _call_plain(_COMBINE, a, Y, stream)
     return out
 
@@ -327,11 +328,11 @@ def expert_combine_backward(Y, slot, gate=None, *, B, L, dout=None, dsum=None, r
         if gamma is not None:
             out.update(dgamma=new(D), dbeta=new(D))
     a = _COMBINE_BACK.pack(
-        B, L, D, k, M, _at(rows, "rows", torch.int32, (B,)), _at(Y, "Y", bf, (M, D)),
-        _at(slot, "slot", torch.int32, (T, k)), _at(gate, "gate", f32, (T, k)),
-        _at(res, "res", bf, (T, D)), res_scale, _at(gamma, "gamma", f32, (D,)), eps,
-        _at(dout, "dout", bf, (T, D)), _at(dsum, "dsum", bf, (T, D)), _at(out["dY"], "dY", bf, (M, D)),
-        _at(out.get("dgate"), "dgate", f32, (T, k)), _at(out.get("dres"), "dres", bf, (T, D)),
-        _at(out.get("dgamma"), "dgamma", f32, (D,)), _at(out.get("dbeta"), "dbeta", f32, (D,)))
+        B, L, D, k, M, _at(rows, "rows", torch.int32, B), _at(Y, "Y", bf, M * D),
+        _at(slot, "slot", torch.int32, T * k), _at(gate, "gate", f32, T * k),
+        _at(res, "res", bf, T * D), res_scale, _at(gamma, "gamma", f32, D), eps,
+        _at(dout, "dout", bf, T * D), _at(dsum, "dsum", bf, T * D), _at(out["dY"], "dY", bf, M * D),
+        _at(out.get("dgate"), "dgate", f32, T * k), _at(out.get("dres"), "dres", bf, T * D),
+        _at(out.get("dgamma"), "dgamma", f32, D), _at(out.get("dbeta"), "dbeta", f32, D))
     _call(_COMBINE_BACK, a, _work(workspace, Y.device, stream, B, L, 1, 1, D), stream)
     return out
