@@ -1024,6 +1024,205 @@ __global__ void __launch_bounds__(kFewThreads) sc_expert_few_kernel(
   else *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(p.out) + at) = pack_bf16x2(a[0], a[1]);
 }
 
+// Forward and back (input) with few slots an expert: the weights' bytes bound it, and the
+// pair kernel leaves SMs idle (96 tiles for 76 pairs: 400 slots of 16 experts, 768 -> 1536)
+// and takes 8 us for its set-up and one tile alone.  Here a CTA of four warps has 64
+// features x up to 32 slots of an expert, four CTAs share an SM, and the hardware deals
+// them out; products by warp-level MMA (the tensor rate does not matter), operands through
+// four stages of 64 of the contraction by 16-byte copies (six stages, three CTAs an SM:
+// 14.3 us; three and five: 13.1; four and four: 11.4; the pair kernel 15.2).
+constexpr int kSmallThreads = 128;
+constexpr int kSmallF = 64, kSmallS = 32, kSmallStages = 4;
+constexpr uint32_t kSmallABytes = kSmallF * 128, kSmallStage = kSmallABytes + kSmallS * 128;
+constexpr uint32_t kSmallDyn = kSmallStages * kSmallStage + 1024;
+
+template <ExpertProduct kWhat>
+__global__ void __launch_bounds__(kSmallThreads, 4)
+    sc_expert_small_kernel(const __grid_constant__ ExpertLinearParams p) {
+  constexpr bool kFwd = kWhat == ExpertProduct::kForward;
+  extern __shared__ uint8_t dyn_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_raw) + 1023) &
+                                             ~static_cast<uintptr_t>(1023));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int f0 = blockIdx.x * kSmallF;
+  const int width = kFwd ? p.N : p.K, depth = kFwd ? p.K : p.N;
+  pdl_wait();
+  pdl_launch_dependents();
+  // the expert and slots of tile blockIdx.y
+  int e = -1, lo = 0, hi = 0, before = 0;
+  for (int e0 = 0; e0 < p.E; e0 += 32) {
+    int a = 0, b = 0;
+    if (e0 + lane < p.E) expert_range(p, e0 + lane, a, b);
+    const int mine = (b - a + kSmallS - 1) / kSmallS;
+    int x = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {   // inclusive scan
+      const int y = __shfl_up_sync(0xffffffffu, x, off);
+      if (lane >= off) x += y;
+    }
+    const int t = static_cast<int>(blockIdx.y) - before;
+    const uint32_t has = __ballot_sync(0xffffffffu, t >= x - mine && t < x);
+    if (has != 0u) {
+      const int l = __ffs(has) - 1;
+      e = e0 + l;
+      lo = __shfl_sync(0xffffffffu, a + (t - x + mine) * kSmallS, l);
+      hi = __shfl_sync(0xffffffffu, b, l);
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, x, 31);
+  }
+  if (e < 0) return;
+  const int n = min(kSmallS, hi - lo);
+
+  // copies: piece c (16 bytes) of rows r0 + 16 i; weights: 64 rows of features (forward)
+  // or of the contraction, the other side: 32 slots, the last one again past the end
+  const int c = tid & 7, r0 = tid >> 3;
+  const uint16_t* const w = p.w + static_cast<size_t>(e) * p.N * p.K;
+  const uint16_t* rows[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int s = lo + min(r0 + 16 * i, n - 1);
+    rows[i] = kFwd ? p.x + expert_row(p, s) * p.ldx : p.dy + s * p.ldy;
+  }
+  const int steps = (depth + 63) / 64;
+  const auto copy = [&](int kt) {
+    const uint32_t at = smem_u32(base) + (kt % kSmallStages) * kSmallStage;
+    const int k = 64 * kt + 8 * c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = r0 + 16 * i;
+      const int row = kFwd ? f0 + r : 64 * kt + r, col = kFwd ? k : f0 + 8 * c;
+      const bool in = row < p.N && col < p.K;
+      cp_async16(at + sw128_offset(r, c), w + (in ? static_cast<size_t>(row) * p.K + col : 0), in);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      cp_async16(at + kSmallABytes + sw128_offset(r0 + 16 * i, c), rows[i] + (k < depth ? k : 0), k < depth);
+  };
+#pragma unroll
+  for (int i = 0; i < kSmallStages - 1; ++i) {
+    if (i < steps) copy(i);
+    cp_async_commit();
+  }
+  float acc[4][4] = {}, sum[4][4] = {};   // slots 8 j ..; sum: see kSpan
+  const int f = 16 * warp;                // this warp's features of the tile
+#pragma unroll 1
+  for (int kt = 0; kt < steps; ++kt) {
+    cp_async_wait<kSmallStages - 2>();
+    __syncthreads();   // the stage is there, and the one before it has been read by all
+    if (kt + kSmallStages - 1 < steps) copy(kt + kSmallStages - 1);
+    cp_async_commit();
+    const uint32_t a = smem_u32(base) + (kt % kSmallStages) * kSmallStage, b = a + kSmallABytes;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t av[4], bv[2][4];
+      if constexpr (kFwd)
+        ldmatrix4(a + sw128_offset(f + (lane & 15), 2 * k + (lane >> 4)), av);
+      else
+        ldmatrix4_trans(a + sw128_offset(16 * k + (lane & 7) + 8 * (lane >> 4), f / 8 + ((lane >> 3) & 1)), av);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        ldmatrix4(b + sw128_offset(16 * j + (lane & 7) + 8 * (lane >> 4), 2 * k + ((lane >> 3) & 1)), bv[j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mma_bf16(acc[j], av, bv[j >> 1][2 * (j & 1)], bv[j >> 1][2 * (j & 1) + 1]);
+    }
+    if (kt % kSpan == kSpan - 1 || kt == steps - 1) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sum[j][i] += acc[j][i];
+          acc[j][i] = 0.f;
+        }
+    }
+  }
+  // the lane has features fr, fr + 8 of slots 8 j + 2 (lane % 4), + 1
+  const int fr = f0 + f + (lane >> 2);
+  cp_async_wait_all();
+  __syncthreads();
+  // staging: 32 slots x 64 features in bf16, 128-byte rows; of `pre` and of the output
+  uint8_t* const stg_pre = base;
+  uint8_t* const stg = base + kSmallS * 128;
+  const auto at = [&](int j) {   // this lane's row of fragments of slots 8 j .. 8 j + 15
+    return sw128_offset(8 * j + (lane & 7) + 8 * (lane >> 4), f / 8 + ((lane >> 3) & 1));
+  };
+  const auto store = [&](uint8_t* to) {
+#pragma unroll
+    for (int j = 0; j < 4; j += 2)
+      stmatrix4_trans(smem_u32(to) + at(j), pack_bf16x2(sum[j][0], sum[j][1]), pack_bf16x2(sum[j][2], sum[j][3]),
+                      pack_bf16x2(sum[j + 1][0], sum[j + 1][1]), pack_bf16x2(sum[j + 1][2], sum[j + 1][3]));
+  };
+  const auto flush = [&](const uint8_t* from, uint16_t* out) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + 16 * i;
+      if (r < n && f0 + 8 * c < width)
+        *reinterpret_cast<uint4*>(out + static_cast<size_t>(lo + r) * width + f0 + 8 * c) =
+            *reinterpret_cast<const uint4*>(from + sw128_offset(r, c));
+    }
+  };
+  if constexpr (kFwd) {
+    if (p.bias != nullptr)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float bias = fr + 8 * h < p.N ? __ldg(p.bias + static_cast<size_t>(e) * p.N + fr + 8 * h) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sum[j][2 * h] += bias;
+          sum[j][2 * h + 1] += bias;
+        }
+      }
+    if (p.pre != nullptr) store(stg_pre);
+    if (p.gelu)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        gelu2(sum[j][0], sum[j][1]);
+        gelu2(sum[j][2], sum[j][3]);
+      }
+  } else if (p.pre_in != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + 16 * i;
+      const bool in = r < n && f0 + 8 * c < width;
+      cp_async16(smem_u32(stg_pre) + sw128_offset(r, c),
+                 p.pre_in + (in ? static_cast<size_t>(lo + r) * width + f0 + 8 * c : 0), in);
+    }
+    cp_async_wait_all();
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+      uint32_t z[4];
+      ldmatrix4_trans(smem_u32(stg_pre) + at(j), z);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        gelu_slope2(bf_lo(z[i]), bf_hi(z[i]), sum[j + (i >> 1)][2 * (i & 1)], sum[j + (i >> 1)][2 * (i & 1) + 1]);
+    }
+  }
+  if (p.out_f32) {
+    // eight lanes write 32 consecutive bytes of a slot
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = 8 * j + 2 * (lane & 3) + (i & 1), x = fr + 8 * (i >> 1);
+        if (s < n && x < width)
+          static_cast<float*>(p.out)[static_cast<size_t>(lo + s) * width + x] = sum[j][i];
+      }
+  } else {
+    store(stg);
+  }
+  __syncthreads();
+  if (!p.out_f32) flush(stg, static_cast<uint16_t*>(p.out));
+  if (kFwd && p.pre != nullptr) flush(stg_pre, p.pre);
+}
+
+// It runs for up to this many slots an expert on average, and while the pair kernel's tiles
+// would be at most two rounds: us here and there, the weights read anew,
+//   768 -> 1536,   8 experts,  16, 32, 64, 128 slots each: 8.3 10.5 11.3 15.8; 10.3 10.5 11.5 13.6
+//   768 -> 1536,  16 experts,  25, 64 slots each: 11.4 17.0; 15.2 17.1
+//   1024 -> 2048, 64 experts,  8, 32, 64 slots each (seven rounds): 46 62 88; 47 51 53
+constexpr int kSmallRows = 48;
+
 // ---------------------------------------------------------------------------
 // launch
 // ---------------------------------------------------------------------------
@@ -1097,6 +1296,14 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
     constexpr int per = kFewThreads / 32 * kFewFeatures;
     return launch_chained(sc_expert_few_kernel, dim3((p.N + per - 1) / per, p.M), dim3(kFewThreads), 0, st, p);
   }
+  const int width = what == ExpertProduct::kBackInput ? p.K : p.N;
+  if (what != ExpertProduct::kBackWeight && p.M <= static_cast<long long>(kSmallRows) * p.E &&
+      (p.E < p.M ? p.E : p.M) * ((width + 255) / 256) <= 2 * 76) {
+    const dim3 grid((width + kSmallF - 1) / kSmallF, p.M / kSmallS + (p.E < p.M ? p.E : p.M));
+    return launch_chained(what == ExpertProduct::kForward ? sc_expert_small_kernel<ExpertProduct::kForward>
+                                                          : sc_expert_small_kernel<ExpertProduct::kBackInput>,
+                          grid, dim3(kSmallThreads), kSmallDyn, st, p);
+  }
   PairParams P;
   P.p = p;
   const bool gather = p.token != nullptr;
@@ -1147,6 +1354,11 @@ cudaError_t configure_expert() {
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackInput, false>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackWeight, false>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackWeight, true>();
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sc_expert_small_kernel<ExpertProduct::kForward>, attr, static_cast<int>(kSmallDyn));
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(sc_expert_small_kernel<ExpertProduct::kBackInput>, attr, static_cast<int>(kSmallDyn));
   return e;
 }
 
