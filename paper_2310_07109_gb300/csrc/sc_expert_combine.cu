@@ -62,6 +62,7 @@ struct Choices {
 // rows on their way per row group (two, or one where two do not fit).
 struct CombineCut {
   int warps, groups, segs, ctas;
+  float inv_d;   // 1 / D (a division in the chain of a row costs as much as its sum)
 };
 
 struct CombineSmem {
@@ -135,16 +136,25 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
   float gate_next = 1.f;
   const auto load_plan = [&](long long t) {
     in_next = t < p.T;
-    if (in_next && p.rows != nullptr) {
-      const unsigned b = static_cast<unsigned>(t) / static_cast<unsigned>(p.L);   // t < 2^31
-      in_next = static_cast<int>(static_cast<unsigned>(t) - b * p.L) < __ldg(p.rows + b);
-    }
     slot_next = -1;
     gate_next = 0.f;
-    if (in_next && lane < p.k) {
-      slot_next = __ldg(p.slot + t * p.k + lane);
-      if (slot_next >= p.M) slot_next = -1;
-      if (slot_next >= 0) gate_next = p.gate != nullptr ? __ldg(p.gate + t * p.k + lane) : 1.f;
+    if (!in_next) return;
+    // (all three loads before the first use; a row not in use has a slot entry too)
+    int used = 1;
+    if (p.rows != nullptr) {
+      const unsigned b = static_cast<unsigned>(t) / static_cast<unsigned>(p.L);   // t < 2^31
+      used = __ldg(p.rows + b) - static_cast<int>(static_cast<unsigned>(t) - b * p.L);
+    }
+    int slot = -1;
+    float gate = 1.f;
+    if (lane < p.k) {
+      slot = __ldg(p.slot + t * p.k + lane);
+      if (p.gate != nullptr) gate = __ldg(p.gate + t * p.k + lane);
+    }
+    in_next = used > 0;
+    if (in_next && slot >= 0 && slot < p.M) {
+      slot_next = slot;
+      gate_next = gate;
     }
   };
   const auto copy = [&](int r, int seg, const uint16_t* row, bool there) {
@@ -237,7 +247,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
           for (int q = 0; q < 4; ++q) a2 = f2_add(a2, s[v][q]);
         float a[1] = {f2_sum(a2)};
         row_sum(cut, sm, group, w, turn, a);
-        const float mean = a[0] / static_cast<float>(p.D);
+        const float mean = a[0] * cut.inv_d;
         a2 = f2_both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -251,7 +261,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
         }
         a[0] = f2_sum(a2);
         row_sum(cut, sm, group, w, turn, a);
-        inv = 1.f / sqrtf(a[0] / static_cast<float>(p.D) + p.eps);
+        inv = rsqrtf(fmaf(a[0], cut.inv_d, p.eps));
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -294,8 +304,8 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
           float ab[2] = {f2_sum(ab0), f2_sum(ab1)};
           row_sum(cut, sm, group, w, turn, ab);
           // (dh - ma - h mb) / sigma
-          const uint64_t i2 = f2_both(inv), ma = f2_both(-ab[0] / static_cast<float>(p.D) * inv);
-          const uint64_t mb = f2_both(-ab[1] / static_cast<float>(p.D) * inv);
+          const float by = -cut.inv_d * inv;
+          const uint64_t i2 = f2_both(inv), ma = f2_both(ab[0] * by), mb = f2_both(ab[1] * by);
 #pragma unroll
           for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -447,6 +457,7 @@ static cudaError_t combine(const CombineParams& p, cudaStream_t st) {
   CombineCut cut;
   // a warp a row up to 1024 features (more warps a row: 768 features forward, three, 25 us
   // instead of 16; gradient of 1024, two or four, 57 or 63 us instead of 54)
+  cut.inv_d = 1.f / static_cast<float>(p.D);
   cut.warps = (p.D + 1023) / 1024;
   const int vecs = (p.D + 256 * cut.warps - 1) / (256 * cut.warps);
   cut.segs = p.k + (p.res != nullptr && (!kBack || norm) ? 1 : 0) +
