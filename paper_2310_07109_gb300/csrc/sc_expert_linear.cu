@@ -81,6 +81,9 @@ struct PairKind {
   static constexpr uint32_t kDyn = kStages * kPairStageBytes + kEpiWarps * kOutBytes + 1024;
 };
 
+// Weight gradient: most tiles beside the pairs' first ones that are dealt out.
+constexpr int kMaxDealt = 160;
+
 struct PairParams {
   ExpertLinearParams p;
   CUtensorMap map_a;     // forward: W, 128 x 64; back (input): W, 64 x 64; back (weight): dy, 64 x 64
@@ -102,11 +105,12 @@ struct PairSmem {
     alignas(16) float sums[2][kPairM];   // weight gradient: bias sums of two warps each
   };
   uint8_t order[kMaxExperts];   // weight gradient: experts by decreasing number of slots
+  // ... and the tiles this pair takes after its first, where they are dealt out
+  int deal, dealt_n;
+  uint64_t dealt_out;           // barrier: the list is there
+  uint16_t dealt[kMaxDealt];
 };
 
-__device__ __forceinline__ float bf(uint16_t v) {
-  return __uint_as_float(static_cast<uint32_t>(v) << 16);
-}
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
@@ -225,21 +229,79 @@ __device__ __forceinline__ void pair_tile(const ExpertLinearParams& p, const Pai
   g.width = (g.n + 63) & ~63;
 }
 
-// The tile a pair takes after tile t.  Weight gradient: its tiles come by decreasing
-// contraction, so the pairs take them in turn there and back (8 experts of 1002 to 3884
-// slots, two tiles a pair: the longest pair has 76 steps instead of 98, the mean is 61).
-template <ExpertProduct kWhat>
-__device__ __forceinline__ int next_tile(int t, int pair, int pairs) {
-  if constexpr (kWhat != ExpertProduct::kBackWeight) return t + pairs;
-  const bool there = t % pairs == pair && (t / pairs) % 2 == 0;
-  return t - t % pairs + pairs + (there ? pairs - 1 - pair : pair);
-}
-
 template <ExpertProduct kWhat>
 __device__ __forceinline__ int pair_steps(const ExpertLinearParams& p, const PairTile& g) {
   const int depth = kWhat == ExpertProduct::kForward ? p.K
                     : kWhat == ExpertProduct::kBackInput ? p.N : g.hi - g.lo;
   return (depth + kPairStep - 1) / kPairStep;
+}
+
+// The tiles of a pair, in order.  Forward, back (input): every pairs-th.  Weight gradient:
+// the tiles come by decreasing contraction, and where each pair has a few, they are
+// dealt out one by one to the pair with the least so far (8 experts of 1002 to 3884 slots,
+// two tiles a pair: every pairs-th 98 stages for the longest, there and back 76, dealt 68,
+// the mean 61); where they have more, there and back.
+template <ExpertProduct kWhat>
+struct TileWalk {
+  int t, i, pair, pairs, tiles;
+  __device__ __forceinline__ TileWalk(int pair_, int pairs_, int tiles_)
+      : t(pair_), i(0), pair(pair_), pairs(pairs_), tiles(tiles_) {}
+  __device__ __forceinline__ bool more() const { return t < tiles; }
+  __device__ __forceinline__ void next(PairSmem& sm) {
+    if constexpr (kWhat != ExpertProduct::kBackWeight) {
+      t += pairs;
+    } else if (sm.deal) {
+      // the dealing warp waits for nothing; whatever gives up elsewhere, all see the list
+      bool ok = false;
+      for (int polls = 0; !ok && polls < 1 << 22; ++polls) ok = mbar_try_wait_poll(&sm.dealt_out, 0);
+      t = ok && i < sm.dealt_n ? sm.dealt[i] : tiles;
+    } else {
+      t = (i + 1) * pairs + (i % 2 == 0 ? pairs - 1 - pair : pair);
+    }
+    ++i;
+  }
+};
+
+// Deals out tiles pairs .. tiles of the weight gradient, the first ones being the pairs'
+// own; one warp, while the first ones are at work.  A tile's cost: its stages, and six for
+// what it costs beside them.
+__device__ __forceinline__ void deal_tiles(const ExpertLinearParams& p, PairSmem& sm, int pair, int pairs,
+                                           int tiles) {
+  constexpr int kPer = 5;   // pairs a lane
+  const int lane = threadIdx.x & 31;
+  const int each = tiles / p.E;   // tiles of an expert
+  const auto cost = [&](int o) {
+    int lo, hi;
+    expert_range(p, sm.order[o], lo, hi);
+    return static_cast<uint32_t>(min((hi - lo + kPairStep - 1) / kPairStep, 1 << 20) + 6);
+  };
+  uint32_t load[kPer];
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    const int o = lane + 32 * q;
+    load[q] = o < pairs && o < tiles ? cost(o / each) : 0xffffffu;
+  }
+  int n = 0;
+  uint32_t now = 0;
+  for (int t = pairs; t < tiles; ++t) {
+    if (t == pairs || t % each == 0) now = cost(t / each);
+    uint32_t best = 0xffffffffu;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) best = min(best, min(load[q], 0xffffffu) << 8 | (lane + 32 * q));
+    const int to = static_cast<int>(__reduce_min_sync(0xffffffffu, best) & 255u);
+#pragma unroll
+    for (int q = 0; q < kPer; ++q)
+      if (to == lane + 32 * q) load[q] += now;
+    if (to == pair) {
+      if (lane == 0) sm.dealt[n] = static_cast<uint16_t>(t);
+      ++n;
+    }
+  }
+  if (lane == 0) {
+    sm.dealt_n = n;
+    mbar_arrive(&sm.dealt_out);
+  }
+  __syncwarp();
 }
 
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
@@ -315,6 +377,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       mbar_init(&sm.tfull[a], 1);
       mbar_init(&sm.tempty[a], 2 * kEpiWarps);
     }
+    mbar_init(&sm.dealt_out, 1);
     sm.abort = 0;
     fence_mbar_init();
   }
@@ -359,6 +422,10 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       sm.order[rank_e] = static_cast<uint8_t>(e);
     }
   }
+  if constexpr (kBackW) {
+    const int n = p.E * ((p.N + 255) / 256) * ((p.K + kPairN - 1) / kPairN);
+    if (tid == 0) sm.deal = pairs <= 160 && n > pairs && n - pairs <= kMaxDealt;
+  }
   tc_fence_before();
   __syncthreads();
   cluster_sync();   // the other CTA's barriers are set up
@@ -370,6 +437,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
                     (kBackW ? p.E * ((p.K + kPairN - 1) / kPairN) : sm.tile0[p.E]);
   PairTile g;
   g.e = 0;
+  TileWalk<kWhat> walk(pair, pairs, tiles);
 
   if (warp >= 4 && warp < 4 + kEpiWarps) {
     if constexpr (Kind::kSplit) regs_alloc<Kind::kEpiRegs>();
@@ -523,15 +591,15 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       if (kFwd && p.pre != nullptr) put_chunk<false>(P.map_pre, p.pre, stg_pre, slot0, left, f, width, ok);
       if (lane == 0) bulk_commit();
     };
-    for (int t = pair; t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-      pair_tile<kWhat>(p, sm, t, g);
+    for (; walk.more(); walk.next(sm)) {
+      pair_tile<kWhat>(p, sm, walk.t, g);
       const int steps = pair_steps<kWhat>(p, g);
       const int f = g.f0 + rank * kPairM + 32 * q;   // this warp's features
       if (kFwd && p.bias != nullptr) {
 #pragma unroll
         for (int u = 0; u < 4; ++u) bias[u >> 1][u & 1] = bias_next[u >> 1][u & 1];
-        if (t + pairs < tiles) {
-          pair_tile<kWhat>(p, sm, t + pairs, ahead);
+        if (walk.t + pairs < tiles) {
+          pair_tile<kWhat>(p, sm, walk.t + pairs, ahead);
           load_bias(ahead);
         }
       }
@@ -684,8 +752,8 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       // ------------------------------------------------------------- copies
       bool ok = true;
       int s = 0, use = 0;
-      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-        pair_tile<kWhat>(p, sm, t, g);
+      for (; ok && walk.more(); walk.next(sm)) {
+        pair_tile<kWhat>(p, sm, walk.t, g);
         const int steps = pair_steps<kWhat>(p, g);
         const int f = g.f0 + rank * kPairM;             // this CTA's features
         const int half = kBackW ? kPairN / 2 : g.width / 2;
@@ -745,8 +813,8 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       if (rank == 0 && elect_one()) {
         bool ok = true;
         int s = 0, use = 0, j = 0;
-        for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-          pair_tile<kWhat>(p, sm, t, g);
+        for (; ok && walk.more(); walk.next(sm)) {
+          pair_tile<kWhat>(p, sm, walk.t, g);
           const int steps = pair_steps<kWhat>(p, g);
           if (steps == 0) continue;
           const uint32_t idesc = idesc_bf16(256, kBackW ? kPairN : g.width, !kFwd, kBackW);
@@ -796,8 +864,8 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       if (elect_one()) {
         bool ok = true;
         int s = 0, use = 0;
-        for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-          pair_tile<kWhat>(p, sm, t, g);
+        for (; ok && walk.more(); walk.next(sm)) {
+          pair_tile<kWhat>(p, sm, walk.t, g);
           const int steps = pair_steps<kWhat>(p, g);
 #pragma unroll 1
           for (int kt = 0; kt < steps; ++kt) {
@@ -824,8 +892,8 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       // this thread's piece of row r0 in a stage; rows r0 + kRowStep i lie 128 kRowStep i on
       static_assert(kRowStep % 8 == 0, "the same swizzle");
       const uint32_t to = kPairABytes + (c >> 3) * kPairBoxBytes + sw128_offset(r0, c & 7);
-      for (int t = pair; ok && t < tiles; t = next_tile<kWhat>(t, pair, pairs)) {
-        pair_tile<kWhat>(p, sm, t, g);
+      for (; ok && walk.more(); walk.next(sm)) {
+        pair_tile<kWhat>(p, sm, walk.t, g);
         const int steps = pair_steps<kWhat>(p, g);
         const int half = kBackW ? kPairN / 2 : g.width / 2;
         const int b0 = g.i0 + rank * half;
@@ -893,67 +961,47 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       bool ok = true;   // no early exit: the four warps meet at every tile with a bias sum
       // ------------------------------------------------------------- bias sums
       // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
-      // the 64 slots.  sum_fill() takes the next stage whose products are done and hands
-      // it back to the copies; fills come in the order of the tiles.
-      float part[4] = {};
-      int ts = pair, left_s = 0;
-      bool first_s = false;   // its first column block: the one that sums
-      const auto finish_sum = [&]() {
-        if (!first_s) return;
+      // the 64 slots.  A stage whose products are done is summed, in the first column
+      // block of each expert and 256 features, and handed back to the copies.
+      int s = 0, use = 0;
+      for (; sums && walk.more(); walk.next(sm)) {
+        pair_tile<kWhat>(p, sm, walk.t, g);
+        const int steps = pair_steps<kWhat>(p, g);
+        float part[4] = {};
+#pragma unroll 1
+        for (int kt = 0; kt < steps; ++kt) {
+          ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
+          if (ok && g.i0 == 0) {
+            const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
+#pragma unroll 8
+            for (int i = 0; i < 16; ++i) {
+              const uint2 v =
+                  *reinterpret_cast<const uint2*>(at + sw128_offset(16 * (l >> 5) + i, (lane & 15) >> 1));
+              part[0] += bf_lo(v.x);
+              part[1] += bf_hi(v.x);
+              part[2] += bf_lo(v.y);
+              part[3] += bf_hi(v.y);
+            }
+          }
+          warp_arrive(&sm.empty[s]);
+          if (++s == kStages) {
+            s = 0;
+            ++use;
+          }
+        }
+        if (g.i0 != 0) continue;
         const int w = l >> 5;
         float4& mine = *reinterpret_cast<float4*>(&sm.sums[w & 1][4 * lane]);
         if (w >= 2) mine = make_float4(part[0], part[1], part[2], part[3]);
         asm volatile("bar.sync 3, 128;" ::: "memory");
         if (w < 2) mine = make_float4(part[0] + mine.x, part[1] + mine.y, part[2] + mine.z, part[3] + mine.w);
         asm volatile("bar.sync 3, 128;" ::: "memory");
-        PairTile gs;
-        pair_tile<kWhat>(p, sm, ts, gs);
-        const int n = gs.f0 + rank * kPairM + l;
-        if (ok && n < p.N) p.dbias[static_cast<size_t>(gs.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
+        const int n = g.f0 + rank * kPairM + l;
+        if (ok && n < p.N) p.dbias[static_cast<size_t>(g.e) * p.N + n] = sm.sums[0][l] + sm.sums[1][l];
         asm volatile("bar.sync 3, 128;" ::: "memory");
-        part[0] = part[1] = part[2] = part[3] = 0.f;
-      };
-      // to the next tile with a contraction; the bias of an expert without slots is 0
-      const auto seek_sum = [&]() {
-        for (; ts < tiles; ts = next_tile<kWhat>(ts, pair, pairs)) {
-          PairTile gs;
-          pair_tile<kWhat>(p, sm, ts, gs);
-          left_s = pair_steps<kWhat>(p, gs);
-          first_s = gs.i0 == 0;
-          if (left_s > 0) return;
-          finish_sum();
-        }
-      };
-      const auto sum_fill = [&](int stage, int parity) {
-        ok = ok && warp_wait(&sm.done[stage], parity, abort_flag);
-        if (ok && first_s) {
-          const uint8_t* at = base + stage * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
-#pragma unroll 4
-          for (int i = 0; i < 16; ++i) {
-            const uint2 v =
-                *reinterpret_cast<const uint2*>(at + sw128_offset(16 * (l >> 5) + i, (lane & 15) >> 1));
-            part[0] += bf_lo(v.x);
-            part[1] += bf_hi(v.x);
-            part[2] += bf_lo(v.y);
-            part[3] += bf_hi(v.y);
-          }
-        }
-        warp_arrive(&sm.empty[stage]);
-        if (--left_s == 0) {
-          finish_sum();
-          ts = next_tile<kWhat>(ts, pair, pairs);
-          seek_sum();
-        }
-      };
-      int s = 0, use = 0;
-      if (sums) seek_sum();
-      while (sums && ts < tiles) {
-        sum_fill(s, use & 1);
-        if (++s == kStages) {
-          s = 0;
-          ++use;
-        }
       }
+    } else if (kBackW && warp == 3) {
+      if (sm.deal) deal_tiles(p, sm, pair, pairs, tiles);
     }
   }
 
@@ -1338,8 +1386,24 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
                 : launch_pair<ExpertProduct::kBackWeight, false>(P, tiles, st);
 }
 
+// The register shares of the fp32 kernels sum up to what they are launched with: a
+// warpgroup that asks for more would wait for ever.
+template <ExpertProduct kWhat, bool kGather>
+static cudaError_t check_registers() {
+  using Kind = PairKind<kWhat, kGather, true>;
+  if (!Kind::kSplit) return cudaSuccess;
+  cudaFuncAttributes a;
+  const cudaError_t e = cudaFuncGetAttributes(&a, sc_expert_pair_kernel<kWhat, kGather, true>);
+  if (e != cudaSuccess) return e;
+  const int others = Kind::kThreads - 128 - 32 * Kind::kEpiWarps;
+  const int want = 32 * Kind::kEpiWarps * Kind::kEpiRegs + 128 * Kind::kFirstRegs + others * Kind::kAuxRegs;
+  return want <= a.numRegs * Kind::kThreads ? cudaSuccess : cudaErrorInvalidConfiguration;
+}
+
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t configure_pair() {
+  const cudaError_t regs = check_registers<kWhat, kGather>();
+  if (regs != cudaSuccess) return regs;
   const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
   const cudaError_t e = cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather, false>, attr,
                                              static_cast<int>(PairKind<kWhat, kGather, false>::kDyn));

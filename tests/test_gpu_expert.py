@@ -340,6 +340,31 @@ def test_expert_linear_backward_weight(counts, N, K, gather, pad, f32, bias, fir
         assert torch.equal(again[name], out[name]), name
 
 
+@pytest.mark.parametrize("E", [19, 20, 38, 58, 59, 60, 77])
+@pytest.mark.parametrize("f32", [True, False])
+def test_expert_linear_backward_weight_writes_every_tile(E, f32):
+    """Uneven experts of four tiles each, around one and three tiles for each pair of SMs."""
+    N, K = 1000, 200
+    counts = [(0, 1, 700, 64, 65, 3, 1900, 0, 130, 15, 400)[(7 * e) % 11] for e in range(E)]
+    X, token, M = product_inputs(5 + E, counts, 301, K, gather=f32, pad=0)
+    dY, _, _ = product_inputs(6 + E, counts, 0, N, gather=False, pad=0)
+    off = offsets_of(counts)
+    out = {"dW": torch.full((E, N, K), math.nan, device="cuda", dtype=torch.float32 if f32 else torch.bfloat16),
+           "dbias": torch.full((E, N), math.nan, device="cuda")}
+    ws = sc.new_expert_workspace(1, 1, 1, 1, 8)
+    sc.expert_linear_backward_weight(dY, X, off, token=token, out=out, workspace=ws)
+    assert sc.workspace_status(ws) == 0
+    lo = 0
+    for e, c in enumerate(counts):
+        hi = lo + c
+        rows = (X[lo:hi] if token is None else X[token[lo:hi].long()]).double()
+        dy = dY[lo:hi].double()
+        slack = (c + 16) * U_F32 * (dy.abs().T @ rows.abs())
+        check(out["dW"][e], dy.T @ rows, slack, U_F32 if f32 else U_BF16, "dW, expert %d" % e)
+        check(out["dbias"][e], dy.sum(dim=0), (c + 16) * U_F32 * dy.abs().sum(dim=0), 0.0, "dbias, expert %d" % e)
+        lo = hi
+
+
 def test_expert_linear_keeps_rows_apart():
     """A row of infinities or NaN reaches its own outputs alone."""
     counts, N, K = [60, 70, 130], 200, 136
