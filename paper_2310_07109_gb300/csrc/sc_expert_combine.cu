@@ -127,14 +127,6 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
   const long long step = static_cast<long long>(gridDim.x) * cut.groups;
   pdl_wait();
   pdl_launch_dependents();
-  if (norm) {
-    for (int i = threadIdx.x; i < p.D; i += blockDim.x) {
-      const int to = ((i >> 2 & 1) * vecs + (i >> 3)) * 4 + (i & 3);
-      reinterpret_cast<float*>(gam)[to] = __ldg(p.gamma + i);
-      if (!kBack) reinterpret_cast<float*>(bet)[to] = __ldg(p.beta + i);
-    }
-    __syncthreads();
-  }
   const auto param = [&](const float4* v, int at, uint64_t (&f)[4]) {
     const float4 a = v[at], b = v[vecs + at];
     f[0] = f2_pack(a.x, a.y), f[1] = f2_pack(a.z, a.w), f[2] = f2_pack(b.x, b.y), f[3] = f2_pack(b.z, b.w);
@@ -231,6 +223,14 @@ __global__ void __launch_bounds__(32 * kCombineWarps, kBack ? 1 : 2)
   long long t = static_cast<long long>(blockIdx.x) * cut.groups + group;
   load_plan(t);
   start(0, t, 0);
+  if (norm) {
+    for (int i = threadIdx.x; i < p.D; i += blockDim.x) {
+      const int to = ((i >> 2 & 1) * vecs + (i >> 3)) * 4 + (i & 3);
+      reinterpret_cast<float*>(gam)[to] = __ldg(p.gamma + i);
+      if (!kBack) reinterpret_cast<float*>(bet)[to] = __ldg(p.beta + i);
+    }
+    __syncthreads();
+  }
   for (int i = 0, r = 0; t < p.T; t += step, ++i, r = kRows == 2 ? r ^ 1 : 0) {
     const int* const slot_of = sm.slot[warp][i % (2 * kPlanRows)];
     const float* const gate_of = sm.gate[warp][i % (2 * kPlanRows)];
