@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
   int first_expert = -1, first_rank = -1;
   for (int c0 = t0; c0 < t1; c0 += kRouteTokens) {
     const int n = min(t1 - c0, kRouteTokens);
-    float x[kRoutePerWarp][V];
+    float x[kRoutePerWarp][V];   // all loads before the first use
 #pragma unroll
     for (int u = 0; u < kRoutePerWarp; ++u) {
       const int i = warp * kRoutePerWarp + u, t = c0 + i;
@@ -126,17 +126,14 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
     }
     // choice by choice, the warp's tokens side by side
     uint32_t key[kRoutePerWarp][V];
-    float top[kRoutePerWarp], mine[kRoutePerWarp];
+    uint32_t mine[kRoutePerWarp];   // lane j: choice j's key, 0 where none is left
     int my_expert[kRoutePerWarp];
 #pragma unroll
     for (int u = 0; u < kRoutePerWarp; ++u) {
-      top[u] = mine[u] = 0.f;
+      mine[u] = 0u;
       my_expert[u] = -1;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        key[u][v] = route_key(x[u][v]);
-        if (key[u][v] == 0u) x[u][v] = -INFINITY;
-      }
+      for (int v = 0; v < V; ++v) key[u][v] = route_key(x[u][v]);
     }
     for (int j = 0; j < p.k; ++j) {
       uint32_t best[kRoutePerWarp];
@@ -158,30 +155,34 @@ __global__ void __launch_bounds__(kRouteThreads) sc_route_choose_kernel(
       }
 #pragma unroll
       for (int u = 0; u < kRoutePerWarp; ++u) {
-        if (best[u] == 0u) continue;   // none is left
 #pragma unroll
         for (int v = 0; v < V; ++v)
           if (at[u] == lane + 32 * v) key[u][v] = 0u;
-        if (j == 0) top[u] = route_value(best[u]);
-        if (lane == j) mine[u] = route_value(best[u]), my_expert[u] = at[u];
+        if (lane == j) mine[u] = best[u], my_expert[u] = at[u];
       }
     }
 #pragma unroll
     for (int u = 0; u < kRoutePerWarp; ++u) {
       const int i = warp * kRoutePerWarp + u;
-      const bool some = __any_sync(0xffffffffu, my_expert[u] >= 0);
-      mine[u] = my_expert[u] >= 0 ? route_exp(mine[u], top[u]) : 0.f;
-      float sum = mine[u];
-      if (!p.renormalize && some) {
+      const bool chosen = mine[u] != 0u;
+      const float top = route_value(__shfl_sync(0xffffffffu, mine[u], 0));   // (where one is chosen)
+      const float own = chosen ? route_exp(route_value(mine[u]), top) : 0.f;
+      float sum = own;
+      if (!p.renormalize && __any_sync(0xffffffffu, chosen)) {
         sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum += route_exp(x[u][v], top[u]);
+        for (int v = 0; v < V; ++v) {
+          // (256 experts: loaded once more, the choices need the registers)
+          const int e = lane + 32 * v;
+          const float l = V <= 4 ? x[u][v] : e < p.E ? __ldg(p.logits + (c0 + i) * p.ld + e) : -INFINITY;
+          if (l > -INFINITY) sum += route_exp(l, top);
+        }
       }
       sum = warp_sum(sum);
       if (lane < p.k && i < n) {
-        pick[i * p.k + lane] = static_cast<int16_t>(my_expert[u]);
-        p.gate[(c0 + i) * p.k + lane] = my_expert[u] >= 0 ? mine[u] / sum : 0.f;
-        if (my_expert[u] >= 0) atomicOr(&mask[my_expert[u] * kRouteWords + (i >> 5)], 1u << (i & 31));
+        pick[i * p.k + lane] = static_cast<int16_t>(chosen ? my_expert[u] : -1);
+        p.gate[(c0 + i) * p.k + lane] = chosen ? own / sum : 0.f;
+        if (chosen) atomicOr(&mask[my_expert[u] * kRouteWords + (i >> 5)], 1u << (i & 31));
       }
     }
     __syncthreads();
