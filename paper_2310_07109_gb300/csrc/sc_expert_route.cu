@@ -27,7 +27,8 @@ constexpr int kRoutePerWarp = kRouteTokens / (kRouteThreads / 32);   // tokens o
 static_assert(kRouteTokens * kMaxChoices <= kRouteThreads, "an item a thread");
 // Eight lanes have a token, four tokens a warp: the search for the next choice costs a
 // warp's instructions once for all four (a warp a token and `redux`, four tokens in turn:
-// 16384 tokens, E = 64, k = 8, 13.1 us instead of 11.5; 8192 tokens, E = 16, k = 2, 6.4 instead of 4.7).
+// 16384 tokens, E = 64, k = 8, 13.1 us instead of 11.5; 8192 tokens, E = 16, k = 2, 6.4
+// instead of 4.7).
 constexpr int kRouteLanes = 8;
 static_assert(kRoutePerWarp == 32 / kRouteLanes && kMaxChoices <= kRouteLanes, "a lane a choice");
 
