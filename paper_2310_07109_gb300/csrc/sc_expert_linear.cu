@@ -38,7 +38,7 @@ PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder();
 constexpr int kPairM = 128;          // features per CTA, 256 per pair
 constexpr int kPairN = 256;          // widest tile on the other side; half of it per CTA
 constexpr int kPairStep = 64;        // contraction per stage: one 128-byte swizzle atom
-constexpr int kPairMaxStages = 5;
+constexpr int kPairMaxStages = 6;
 constexpr int kPairChunk = 32;       // columns read back at a time
 constexpr uint32_t kPairABytes = kPairM * kPairStep * 2;
 constexpr uint32_t kPairBBytes = kPairN / 2 * kPairStep * 2;
@@ -51,12 +51,13 @@ constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN
 // gradient: 64, and as many in the write-back areas, for the registers of the other
 // warps).  2048 slots: 4.8e-7, torch's fp32 product 3.9e-7.
 constexpr int kSpan = 8;
-template <ExpertProduct kWhat, bool kGather_, bool kF32_>
+// kPre: with the value before GELU, written (forward) or read (back, input).
+template <ExpertProduct kWhat, bool kGather_, bool kF32_, bool kPre_>
 struct PairKind {
   static constexpr bool kFwd = kWhat == ExpertProduct::kForward;
   static constexpr bool kBackX = kWhat == ExpertProduct::kBackInput;
   static constexpr bool kBackW = kWhat == ExpertProduct::kBackWeight;
-  static constexpr bool kGather = kGather_, kF32 = kF32_;
+  static constexpr bool kGather = kGather_, kF32 = kF32_, kPre = kPre_;
   static constexpr int kSteps = kF32 ? kSpan : 1 << 30;   // stages an accumulator takes
   // Warps: four (copies, products), the write-back, four that gather, four that sum dy.
   static constexpr int kEpiWarps = kBackW || kF32 ? 8 : 16;
@@ -72,12 +73,14 @@ struct PairKind {
   // of the value before GELU.  Back (weight): two chunks of 4 KB, the copy of one on its
   // way while the other is filled.  Back (input): a chunk of the output and a ring of two
   // chunks of the value before GELU, copied ahead across tiles: behind the copies of the
-  // operands a load waits 3000 cycles.
+  // operands a load waits 3000 cycles.  Where there is none, its room is a stage's (59,000
+  // slots, 2048 -> 1024: four stages 180 us, five 167, six 164).
   static constexpr uint32_t kChunkBytes = kF32 || kBackW ? 4096 : 2048;
   static constexpr uint32_t kPreBytes = 2048;
   static constexpr uint32_t kOutBytes =
-      kBackW || kF32 ? 8192 : kBackX ? kChunkBytes + 2 * kPreBytes : kChunkBytes + kPreBytes;
-  static constexpr int kStages = kBackX && !kF32 ? 4 : kPairMaxStages;
+      kBackW || kF32 ? 8192 : kChunkBytes + (!kPre ? 0 : kBackX ? 2 * kPreBytes : kPreBytes);
+  static constexpr int kStages = kBackW || kF32 ? 5 : !kPre ? 6 : kBackX ? 4 : 5;
+  static_assert(kStages <= kPairMaxStages, "barriers");
   static constexpr uint32_t kDyn = kStages * kPairStageBytes + kEpiWarps * kOutBytes + 1024;
 };
 
@@ -348,10 +351,10 @@ __device__ __forceinline__ void put_chunk(const CUtensorMap& map, void* out, con
   }
 }
 
-template <ExpertProduct kWhat, bool kGather, bool kF32>
-__global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
+template <ExpertProduct kWhat, bool kGather, bool kF32, bool kPre>
+__global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads, 1)
     sc_expert_pair_kernel(const __grid_constant__ PairParams P) {
-  using Kind = PairKind<kWhat, kGather, kF32>;
+  using Kind = PairKind<kWhat, kGather, kF32, kPre>;
   constexpr bool kFwd = Kind::kFwd, kBackX = Kind::kBackX, kBackW = Kind::kBackW;
   constexpr int kStages = Kind::kStages, kEpiWarps = Kind::kEpiWarps, kGroups = kEpiWarps / 4;
   constexpr int kGatherWarp = Kind::kGatherWarp, kSumWarp = Kind::kSumWarp;
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       cp_async_commit();
       slot_in ^= 1;
     };
-    if (kBackX && p.pre_in != nullptr) {
+    if (kBackX && kPre && p.pre_in != nullptr) {
       copy_pre();
       copy_pre();
     }
@@ -538,7 +541,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
             stmatrix4_trans(smem_u32(area + at(h, b)), w[h][2 * b], w[h][2 * b + 1], w[h][2 * b + 2],
                             w[h][2 * b + 3]);
       };
-      if (kBackX && p.pre_in != nullptr) {
+      if (kBackX && kPre && p.pre_in != nullptr) {
         // in the staging's layout, so that its fragments match the accumulator's
         uint32_t zf[2][2][4];
         cp_async_wait<1>();
@@ -579,7 +582,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
       if constexpr (kF32) {
         // (its sums leave no registers for the value before GELU beside them)
         to = next_area();
-        if (kFwd && p.pre != nullptr) {
+        if (kFwd && kPre && p.pre != nullptr) {
           pack(w);
           store(stg_pre, w);
         }
@@ -596,17 +599,17 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32>::kThreads, 1)
         // all arithmetic before the area is waited for (after it: 16384 slots,
         // 768 -> 1536 with GELU, 38.9 us instead of 37.7)
         uint32_t w_pre[2][8];
-        if (kFwd && p.pre != nullptr) pack(w_pre);
+        if (kFwd && kPre && p.pre != nullptr) pack(w_pre);
         if (kFwd && p.gelu) gelu();
         pack(w);
         to = next_area();
-        if (kFwd && p.pre != nullptr) store(stg_pre, w_pre);
+        if (kFwd && kPre && p.pre != nullptr) store(stg_pre, w_pre);
         store(to, w);
       }
       fence_proxy_async_smem();
       __syncwarp();
       put_chunk<kF32>(P.map_out, p.out, to, slot0, left, f, width, ok);
-      if (kFwd && p.pre != nullptr) put_chunk<false>(P.map_pre, p.pre, stg_pre, slot0, left, f, width, ok);
+      if (kFwd && kPre && p.pre != nullptr) put_chunk<false>(P.map_pre, p.pre, stg_pre, slot0, left, f, width, ok);
       if (lane == 0) bulk_commit();
     };
     for (; walk.more(); walk.next(sm)) {
@@ -1323,9 +1326,9 @@ static bool encode_out(CUtensorMap* m, void* base, bool f32, long long rows, int
              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <ExpertProduct kWhat, bool kGather, bool kF32>
+template <ExpertProduct kWhat, bool kGather, bool kF32, bool kPre>
 static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
-  using Kind = PairKind<kWhat, kGather, kF32>;
+  using Kind = PairKind<kWhat, kGather, kF32, kPre>;
   static int sms = 0;
   if (sms == 0) {
     int dev = 0;
@@ -1348,13 +1351,18 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, sc_expert_pair_kernel<kWhat, kGather, kF32>, P);
+  return cudaLaunchKernelEx(&cfg, sc_expert_pair_kernel<kWhat, kGather, kF32, kPre>, P);
 }
 
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
-  return P.p.out_f32 ? launch_pair<kWhat, kGather, true>(P, most_tiles, st)
-                     : launch_pair<kWhat, kGather, false>(P, most_tiles, st);
+  // (the fp32 kernels have the room anyway)
+  if (P.p.out_f32) return launch_pair<kWhat, kGather, true, true>(P, most_tiles, st);
+  if constexpr (kWhat != ExpertProduct::kBackWeight) {
+    if (P.p.pre != nullptr || P.p.pre_in != nullptr)
+      return launch_pair<kWhat, kGather, false, true>(P, most_tiles, st);
+  }
+  return launch_pair<kWhat, kGather, false, false>(P, most_tiles, st);
 }
 
 cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p, cudaStream_t st) {
@@ -1408,26 +1416,31 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
 // warpgroup that asks for more would wait for ever.
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t check_registers() {
-  using Kind = PairKind<kWhat, kGather, true>;
+  using Kind = PairKind<kWhat, kGather, true, true>;
   if (!Kind::kSplit) return cudaSuccess;
   cudaFuncAttributes a;
-  const cudaError_t e = cudaFuncGetAttributes(&a, sc_expert_pair_kernel<kWhat, kGather, true>);
+  const cudaError_t e = cudaFuncGetAttributes(&a, sc_expert_pair_kernel<kWhat, kGather, true, true>);
   if (e != cudaSuccess) return e;
   const int others = Kind::kThreads - 128 - 32 * Kind::kEpiWarps;
   const int want = 32 * Kind::kEpiWarps * Kind::kEpiRegs + 128 * Kind::kFirstRegs + others * Kind::kAuxRegs;
   return want <= a.numRegs * Kind::kThreads ? cudaSuccess : cudaErrorInvalidConfiguration;
 }
 
+template <ExpertProduct kWhat, bool kGather, bool kF32, bool kPre>
+static cudaError_t configure_room() {
+  return cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather, kF32, kPre>,
+                              cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(PairKind<kWhat, kGather, kF32, kPre>::kDyn));
+}
+
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t configure_pair() {
-  const cudaError_t regs = check_registers<kWhat, kGather>();
-  if (regs != cudaSuccess) return regs;
-  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  const cudaError_t e = cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather, false>, attr,
-                                             static_cast<int>(PairKind<kWhat, kGather, false>::kDyn));
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(sc_expert_pair_kernel<kWhat, kGather, true>, attr,
-                              static_cast<int>(PairKind<kWhat, kGather, true>::kDyn));
+  cudaError_t e = check_registers<kWhat, kGather>();
+  if (e == cudaSuccess) e = configure_room<kWhat, kGather, true, true>();
+  if (e == cudaSuccess) e = configure_room<kWhat, kGather, false, false>();
+  if constexpr (kWhat != ExpertProduct::kBackWeight)
+    if (e == cudaSuccess) e = configure_room<kWhat, kGather, false, true>();
+  return e;
 }
 
 cudaError_t configure_expert() {
