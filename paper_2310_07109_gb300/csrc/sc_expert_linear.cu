@@ -9,7 +9,7 @@
 // whose width follows what an expert has (64 to 256, evenly split over its tiles)
 // -- or, in the weight gradient, the contraction.  Persistent CTA pairs walk the
 // tiles that exist; every role counts them out from the offsets.
-//   warp 0      copies the operands, 64 of the contraction a stage, four or five stages
+//   warp 0      copies the operands, 64 of the contraction a stage, four to six stages
 //   warp 1      (even CTA) issues the products into one of two 256-column accumulators
 //   16 warps    (weight gradient: eight) read the other accumulator back, 32 features x
 //               32 columns at a time, through a staging area of the warp's own and tiled
@@ -23,6 +23,9 @@
 // Operands as they lie in memory: K-major where the contraction is contiguous
 // (forward; dy in back (input)), else MN-major (W in back (input), both sides of the
 // weight gradient), 128-byte swizzle throughout.
+// Bound by the operands' way from the L2 into shared memory, which the outputs' way out
+// shares: 59,000 slots 2048 -> 1024 164 us (1.5 PFLOP/s; without the copies 123), 16384
+// slots 768 -> 1536 35 us (1.1), with GELU and the value before it 43 (50 MB more to write).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>

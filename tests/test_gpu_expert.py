@@ -163,6 +163,12 @@ def test_route_backward(B, L, E, k, rows, kind, renorm):
     assert bool((got[~some] == 0).all())
 
 
+@pytest.mark.parametrize("E", [2, 8, 9, 16, 17, 24, 32, 33, 64, 65, 128, 129, 255, 256])
+@pytest.mark.parametrize("kind", ["ties", "masked", "extremes"])
+def test_route_of_every_number_of_experts(E, kind):
+    test_route(2, 133, E, min(E, 8), [133, 70], kind, E % 2 == 0)
+
+
 def test_route_backward_is_the_difference_quotient():
     """Where the choice does not change, dlogits is the gates' slope (differences in 64 bits)."""
     T, E, k, h = 6, 9, 3, 1e-4
@@ -669,6 +675,17 @@ def test_combine_backward(B, L, D, k, rows, gated, res, norm, dsum):
                                        out={n: t.clone() for n, t in out.items()}, **args)
     for name in out:
         assert torch.equal(again[name], out[name]), name
+
+
+@pytest.mark.parametrize("B,L,D,k,rows", [
+    (5, 8000, 64, 3, [8000, 1, 7999, 0, 4001]),     # ten rows and more for each warp
+    (3, 2100, 1032, 2, [2100, 999, 2]),             # of two warps
+    (2, 640, 8192, 8, [640, 633]),                  # one row at a time
+])
+@pytest.mark.parametrize("gated,res,norm,more", [(True, True, True, True), (False, False, True, False)])
+def test_combine_of_many_rows(B, L, D, k, rows, gated, res, norm, more):
+    test_combine_forward(B, L, D, k, rows, gated, res, norm, more)
+    test_combine_backward(B, L, D, k, rows, gated, res, norm, more)
 
 
 def test_combine_backward_is_the_difference_quotient():
