@@ -475,7 +475,7 @@ int sc_layer_norm_forward(int B, int L, int D, const int32_t* rows, const float*
  * offsets[e + 1].  No size below depends on a value the host would have to
  * read back: the sizes M, T = B L are capacities, offsets and rows live on the
  * device.  Rows and slots that are not in use are neither read nor written
- * unless a field says so.
+ * unless a field says so.  Arrays of 32-bit values lie at multiples of 4 bytes.
  */
 #define SC_MAX_EXPERTS 256
 #define SC_MAX_CHOICES 8
@@ -503,7 +503,7 @@ size_t sc_expert_workspace_size(int B, int L, int E, int k, int D);
  * slot     int32 [B L][k] out: the slot of each choice, or -1.  An expert's
  *          slots are in token order.
  * token    int32 [B L k] out: the token of each slot; -1 from offsets[E] on.
- * 1 <= k <= min(E, SC_MAX_CHOICES), E <= SC_MAX_EXPERTS, B L k < 2^31.
+ * 1 <= k <= min(E, SC_MAX_CHOICES), E <= SC_MAX_EXPERTS, B L k <= 2^31 - 4096.
  */
 typedef struct {
   int B, L, E, k;
@@ -560,8 +560,8 @@ int sc_expert_route_backward(const sc_expert_route_backward_args* args, void* st
  *          one without slots); dbias fp32 [E][N] or NULL.
  * Products of bf16 values, sums in fp32, one rounding at the end.  Two calls with
  * the same arguments give the same bits.
- * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; ldx and ldy multiples of 8
- * below 2^30; every bf16 pointer, out, dX and dW 16-byte aligned.
+ * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; M at most 2^31 - 4096; ldx and
+ * ldy multiples of 8 below 2^30; every bf16 pointer, out, dX and dW 16-byte aligned.
  */
 typedef struct {
   int M, E, N, K;

@@ -19,10 +19,16 @@ namespace {
 using namespace sc;
 
 constexpr size_t kAlign = 256;
-constexpr long long kMaxSlots = (1ll << 31) - 1;
+// (tiles and strides of threads may pass the last slot without passing 32 bits)
+constexpr long long kMaxSlots = (1ll << 31) - 4096;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) & ~(kAlign - 1); }
 bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+// int32 and fp32 arrays (null ones too)
+template <typename... T>
+bool words(const T*... p) {
+  return (aligned(p, 4) && ...);
+}
 
 struct ExpertLayout {
   size_t counts, part, total;
@@ -50,7 +56,7 @@ int check_workspace(const void* ws, size_t bytes, size_t need) {
 int check_product(int M, int E, int N, int K, const int32_t* offsets) {
   if (M < 1 || E < 1 || N < 8 || K < 8 || N % 8 || K % 8 || !offsets || !aligned(offsets, 4))
     return SC_ERR_INVALID_ARG;
-  if (E > kMaxExperts || N > kMaxExpertDim || K > kMaxExpertDim) return SC_ERR_UNSUPPORTED;
+  if (E > kMaxExperts || N > kMaxExpertDim || K > kMaxExpertDim || M > kMaxSlots) return SC_ERR_UNSUPPORTED;
   return SC_OK;
 }
 
@@ -87,7 +93,8 @@ extern "C" int sc_expert_route_forward(const sc_expert_route_args* a, void* work
   if (a->B < 1 || a->L < 1 || a->E < 1 || a->k < 1 || a->k > a->E) return SC_ERR_INVALID_ARG;
   if (a->E > kMaxExperts || a->k > kMaxChoices) return SC_ERR_UNSUPPORTED;
   if (!good_tokens(a->B, a->L, a->k)) return SC_ERR_INVALID_ARG;
-  if (!a->logits || a->ld < a->E || !a->expert || !a->gate || !a->offsets || !a->slot || !a->token)
+  if (!a->logits || a->ld < a->E || !a->expert || !a->gate || !a->offsets || !a->slot || !a->token ||
+      !words(a->logits, a->rows, a->expert, a->gate, a->offsets, a->slot, a->token))
     return SC_ERR_INVALID_ARG;
   const ExpertLayout lay = expert_layout(a->E, 8);
   int rc = check_workspace(workspace, ws_bytes, lay.part);
@@ -108,7 +115,8 @@ extern "C" int sc_expert_route_backward(const sc_expert_route_backward_args* a, 
   if (a->B < 1 || a->L < 1 || a->E < 1 || a->k < 1 || a->k > a->E) return SC_ERR_INVALID_ARG;
   if (a->E > kMaxExperts || a->k > kMaxChoices) return SC_ERR_UNSUPPORTED;
   if (!good_tokens(a->B, a->L, a->k)) return SC_ERR_INVALID_ARG;
-  if (!a->logits || a->ld < a->E || !a->expert || !a->gate || !a->dgate || !a->dlogits)
+  if (!a->logits || a->ld < a->E || !a->expert || !a->gate || !a->dgate || !a->dlogits ||
+      !words(a->logits, a->rows, a->expert, a->gate, a->dgate, a->dlogits))
     return SC_ERR_INVALID_ARG;
   const int rc = api_ensure_configured();
   if (rc != SC_OK) return rc;
@@ -128,7 +136,7 @@ extern "C" int sc_expert_linear_forward(const sc_expert_linear_args* a, void* wo
   if (rc != SC_OK) return rc;
   if (!good_matrix(a->X, a->ldx, a->K) || a->x_rows < 1 || (!a->token && a->x_rows < a->M) ||
       !a->W || !aligned(a->W, 16) || !a->out || !aligned(a->out, 16) || !aligned(a->pre, 16) ||
-      !aligned(a->bias, 4))
+      !words(a->token, a->bias))
     return SC_ERR_INVALID_ARG;
   if ((rc = check_workspace(workspace, ws_bytes, kAlign)) != SC_OK) return rc;
   ExpertLinearParams p{};
@@ -163,7 +171,7 @@ extern "C" int sc_expert_linear_backward_weight(const sc_expert_linear_backward_
   int rc = check_product(a->M, a->E, a->N, a->K, a->offsets);
   if (rc != SC_OK) return rc;
   if (!good_matrix(a->dY, a->ldy, a->N) || !good_matrix(a->X, a->ldx, a->K) || a->x_rows < 1 ||
-      (!a->token && a->x_rows < a->M) || !a->dW || !aligned(a->dW, 16) || !aligned(a->dbias, 4))
+      (!a->token && a->x_rows < a->M) || !a->dW || !aligned(a->dW, 16) || !words(a->token, a->dbias))
     return SC_ERR_INVALID_ARG;
   if ((rc = check_workspace(workspace, ws_bytes, kAlign)) != SC_OK) return rc;
   ExpertLinearParams p{};
@@ -180,7 +188,8 @@ extern "C" int sc_expert_combine_forward(const sc_expert_combine_args* a, void* 
   int rc = check_combine(a->B, a->L, a->D, a->k, a->M, a->Y, a->slot, a->res, a->gamma, a->eps);
   if (rc != SC_OK) return rc;
   if ((a->gamma == nullptr) != (a->beta == nullptr) || (a->gamma != nullptr && !a->out) ||
-      (!a->sum && !a->gamma) || !aligned(a->sum, 16) || !aligned(a->out, 16))
+      (!a->sum && !a->gamma) || !aligned(a->sum, 16) || !aligned(a->out, 16) ||
+      !words(a->rows, a->slot, a->gate, a->gamma, a->beta))
     return SC_ERR_INVALID_ARG;
   if ((rc = api_ensure_configured()) != SC_OK) return rc;
   CombineParams p{};
@@ -201,7 +210,8 @@ extern "C" int sc_expert_combine_backward(const sc_expert_combine_backward_args*
   const bool norm = a->gamma != nullptr;
   if (norm != (a->dout != nullptr) || norm != (a->dgamma != nullptr) ||
       norm != (a->dbeta != nullptr) || (!a->dout && !a->dsum) || !a->dY || !aligned(a->dY, 16) ||
-      !aligned(a->dout, 16) || !aligned(a->dsum, 16) || !aligned(a->dres, 16))
+      !aligned(a->dout, 16) || !aligned(a->dsum, 16) || !aligned(a->dres, 16) ||
+      !words(a->rows, a->slot, a->gate, a->gamma, a->dgate, a->dgamma, a->dbeta))
     return SC_ERR_INVALID_ARG;
   const ExpertLayout lay = expert_layout(1, a->D);
   if ((rc = check_workspace(workspace, ws_bytes, norm ? lay.total - lay.part + kAlign : kAlign)) != SC_OK)

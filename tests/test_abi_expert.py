@@ -86,6 +86,32 @@ def test_bad_arguments(lib, what, kw, code):
     assert call(lib, what, **kw) == code
 
 
+WORDS = {   # arrays of 32-bit values
+    "route": ("logits", "rows", "expert", "gate", "offsets", "slot", "token"),
+    "route_back": ("logits", "rows", "expert", "gate", "dgate", "dlogits"),
+    "linear": ("token", "offsets", "bias"), "back_x": ("offsets",), "back_w": ("token", "offsets", "dbias"),
+    "combine": ("rows", "slot", "gate", "gamma", "beta"),
+    "combine_back": ("rows", "slot", "gate", "gamma", "dgate", "dgamma", "dbeta"),
+}
+
+
+@pytest.mark.parametrize("what,name", [(w, n) for w, names in WORDS.items() for n in names])
+def test_words_lie_at_multiples_of_four(lib, what, name):
+    for by in (1, 2, 3):
+        assert call(lib, what, **{name: P + by}) == INVALID
+
+
+def test_most_slots(lib):
+    most = 2 ** 31 - 4096
+    for what in ("linear", "back_x", "back_w"):
+        rows = {} if what == "back_x" else dict(x_rows=2 ** 31 - 1)
+        assert call(lib, what, M=most + 1, **rows) == UNSUPPORTED
+        assert call(lib, what, M=most, ws=None, **rows) == WORKSPACE   # (the last check)
+    assert call(lib, "route", B=1, L=most // 2 + 1) == INVALID
+    assert call(lib, "route", B=1, L=most // 2, ws=None) == WORKSPACE
+    assert sc.expert_workspace_size(1, most + 1, 4, 1, 8) == 0 < sc.expert_workspace_size(1, most, 4, 1, 8)
+
+
 @pytest.mark.parametrize("what", list(OK))
 def test_missing_arguments(lib, what):
     _, name, with_ws, _ = OK[what]
