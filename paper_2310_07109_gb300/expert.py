@@ -141,6 +141,21 @@ def _stream(stream, t):
     return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
+def _shape(t, name, dims):
+    """The shape of a tensor of so many dimensions."""
+    if t.dim() != dims:
+        _refuse("%s: %d dimensions are wanted" % (name, dims))
+    return t.shape
+
+
+def _made(stream, *tensors):
+    """Outputs made on the current stream for a call on ``stream``."""
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream(tensors[0].device))   # what had the memory before
+        for t in tensors:
+            t.record_stream(stream)
+
+
 def _out_type(t):
     if t.dtype is torch.float32:
         return 1
@@ -199,6 +214,7 @@ def expert_route_forward(logits, *, k, B, L, rows=None, renormalize=True, out=No
         new = lambda *shape, dtype=torch.int32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
         out = {"expert": new(T, k), "gate": new(T, k, dtype=torch.float32), "offsets": new(E + 1),
                "slot": new(T, k), "token": new(T * k)}
+        _made(stream, *out.values())
     i32 = torch.int32
     a = _ROUTE.pack(B, L, E, k, at, ld, _at(rows, "rows", i32, B), 1 if renormalize else 0,
                   _at(out["expert"], "expert", i32, T * k),
@@ -215,9 +231,10 @@ def expert_route_backward(logits, expert, gate, dgate, *, B, L, rows=None, renor
     at, T, E, ld = _rows_at(logits, "logits", torch.float32)
     if T != B * L:
         _refuse("logits: B * L rows are wanted")
-    k = expert.shape[-1]
+    k = _shape(expert, "expert", 2)[1]
     if out is None:
         out = torch.empty((T, E), dtype=torch.float32, device=logits.device)
+        _made(stream, out)
     f32 = torch.float32
     a = _ROUTE_BACK.pack(B, L, E, k, at, ld, _at(rows, "rows", torch.int32, B),
                           1 if renormalize else 0, _at(expert, "expert", torch.int32, T * k),
@@ -238,10 +255,11 @@ def expert_linear_forward(X, W, offsets, *, token=None, bias=None, gelu=False, p
     bf16 [M, N] tensor that receives the values before GELU.  Returns out [M, N], M = len(token),
     or the rows of X."""
     at, xr, K, ld = _rows_at(X, "X", torch.bfloat16)
-    E, N, _ = W.shape
+    E, N, _ = _shape(W, "W", 3)
     M = xr if token is None else token.numel()
     if out is None:
         out = torch.empty((M, N), dtype=torch.float32 if out_f32 else torch.bfloat16, device=X.device)
+        _made(stream, out)
     i32 = torch.int32
     a = _LINEAR.pack(M, E, N, K, at, ld, xr, _at(token, "token", i32, M),
                          _at(offsets, "offsets", i32, E + 1), _at(W, "W", torch.bfloat16, E * N * K),
@@ -257,9 +275,10 @@ def expert_linear_backward_input(dY, W, offsets, *, pre=None, out=None, out_f32=
     """``sc_expert_linear_backward_input``: dY bf16 [M, N] (any row stride), W bf16 [E, N, K]; with
     ``pre`` bf16 [M, K] the result is multiplied by GELU'(pre).  Returns dX [M, K]."""
     at, M, N, ld = _rows_at(dY, "dY", torch.bfloat16)
-    E, _, K = W.shape
+    E, _, K = _shape(W, "W", 3)
     if out is None:
         out = torch.empty((M, K), dtype=torch.float32 if out_f32 else torch.bfloat16, device=dY.device)
+        _made(stream, out)
     a = _BACK_X.pack(M, E, N, K, at, ld, _at(offsets, "offsets", torch.int32, E + 1),
                                       _at(W, "W", torch.bfloat16, E * N * K),
                                       _at(pre, "pre", torch.bfloat16, M * K),
@@ -275,12 +294,13 @@ def expert_linear_backward_weight(dY, X, offsets, *, token=None, bias=True, out=
     ``out`` has none)."""
     ay, M, N, ldy = _rows_at(dY, "dY", torch.bfloat16)
     ax, xr, K, ldx = _rows_at(X, "X", torch.bfloat16)
-    E = offsets.shape[0] - 1
+    E = _shape(offsets, "offsets", 1)[0] - 1
     if out is None:
         out = {"dW": torch.empty((E, N, K), dtype=torch.float32 if out_f32 else torch.bfloat16,
                                  device=X.device)}
         if bias:
             out["dbias"] = torch.empty((E, N), dtype=torch.float32, device=X.device)
+        _made(stream, *out.values())
     dW = out["dW"]
     a = _BACK_W.pack(M, E, N, K, ay, ldy, ax, ldx, xr,
                                        _at(token, "token", torch.int32, M),
@@ -296,12 +316,13 @@ def expert_combine_forward(Y, slot, gate=None, *, B, L, rows=None, res=None, res
     """``sc_expert_combine_forward``: Y bf16 [M, D] rows of the slots, slot int32 [B*L, k], gate fp32
     [B*L, k] or None (1), res bf16 [B*L, D].  Returns dict(sum [B*L, D] bf16, out) (``out`` with
     gamma and beta only); a given ``out`` may lack "sum" where there is a norm."""
-    M, D = Y.shape
-    T, k = B * L, slot.shape[-1]
+    M, D = _shape(Y, "Y", 2)
+    T, k = B * L, _shape(slot, "slot", 2)[1]
     if out is None:
         out = {"sum": torch.empty((T, D), dtype=torch.bfloat16, device=Y.device)}
         if gamma is not None:
             out["out"] = torch.empty((T, D), dtype=torch.bfloat16, device=Y.device)
+        _made(stream, *out.values())
     bf, f32 = torch.bfloat16, torch.float32
     a = _COMBINE.pack(B, L, D, k, M, _at(rows, "rows", torch.int32, B), _at(Y, "Y", bf, M * D),
                           _at(slot, "slot", torch.int32, T * k), _at(gate, "gate", f32, T * k),
@@ -317,8 +338,8 @@ def expert_combine_backward(Y, slot, gate=None, *, B, L, dout=None, dsum=None, r
     """``sc_expert_combine_backward``: gradients from dout (with gamma) and dsum, bf16 [B*L, D].
     Returns dict(dY [M, D] bf16, dgate [B*L, k] fp32, dres [B*L, D] bf16 where res is given, dgamma
     and dbeta [D] fp32 where gamma is)."""
-    M, D = Y.shape
-    T, k = B * L, slot.shape[-1]
+    M, D = _shape(Y, "Y", 2)
+    T, k = B * L, _shape(slot, "slot", 2)[1]
     bf, f32 = torch.bfloat16, torch.float32
     if out is None:
         new = lambda *shape, dtype=f32: torch.empty(shape, dtype=dtype, device=Y.device)  # noqa: E731
@@ -327,6 +348,7 @@ def expert_combine_backward(Y, slot, gate=None, *, B, L, dout=None, dsum=None, r
             out["dres"] = new(T, D, dtype=bf)
         if gamma is not None:
             out.update(dgamma=new(D), dbeta=new(D))
+        _made(stream, *out.values())
     a = _COMBINE_BACK.pack(
         B, L, D, k, M, _at(rows, "rows", torch.int32, B), _at(Y, "Y", bf, M * D),
         _at(slot, "slot", torch.int32, T * k), _at(gate, "gate", f32, T * k),

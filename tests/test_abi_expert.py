@@ -155,3 +155,14 @@ def test_the_binding_refuses_wrong_tensors():
         with pytest.raises(sc.SparseCoderError) as e:
             call()
         assert e.value.code == INVALID
+
+
+def test_the_binding_refuses_wrong_dimensions():
+    bf = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)  # noqa: E731
+    one = torch.zeros((), dtype=torch.int32)
+    for call in (lambda: ex._shape(bf(8, 8), "W", 3), lambda: ex._shape(one, "offsets", 1),
+                 lambda: sc.expert_combine_forward(bf(4, 8, 1), one, B=1, L=4),
+                 lambda: sc.expert_combine_backward(bf(4, 8), torch.zeros(4, dtype=torch.int32), B=1, L=4)):
+        with pytest.raises(sc.SparseCoderError) as e:
+            call()
+        assert e.value.code == INVALID

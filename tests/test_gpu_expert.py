@@ -496,6 +496,36 @@ def test_expert_linear_on_another_stream():
     assert torch.equal(out, ref)
 
 
+def test_outputs_made_for_another_stream():
+    """Memory that the current stream still writes when a call on another stream is given it."""
+    rows, E, N, K = 4096, 2, 1024, 64
+    X, W = bf16(randn(gen(3), rows, K)), bf16(randn(gen(4), E, N, K))
+    off = offsets_of([1000, 3096])
+    logits = randn(gen(5), rows, 16)
+    ref = sc.expert_linear_forward(X, W, off)
+    ref_route = sc.expert_route_forward(logits, k=2, B=1, L=rows)
+    ws = sc.new_expert_workspace(1, rows, 16, 2, 8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = {}
+    torch.cuda.synchronize()
+    for name, call, nbytes in (
+            ("linear", lambda: {"out": sc.expert_linear_forward(X, W, off, workspace=ws, stream=side)}, rows * N * 2),
+            ("route", lambda: sc.expert_route_forward(logits, k=2, B=1, L=rows, workspace=ws, stream=side), rows * 8)):
+        busy = [torch.empty(nbytes, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        big = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+        for i in range(40):
+            big.fill_(i)
+        for t in busy:
+            t.fill_(7)
+        del busy, t
+        got[name] = call()
+    torch.cuda.synchronize()
+    assert torch.equal(got["linear"]["out"], ref)
+    for name in ref_route:
+        assert torch.equal(got["route"][name], ref_route[name]), name
+
+
 def test_expert_products_in_a_graph():
     """Captured, and replayed with other rows, another routing and other lengths."""
     T, E, k, D, F = 200, 8, 2, 256, 512
