@@ -483,15 +483,13 @@ static cudaError_t launch_cut(const CombineParams& p, const CombineCut& cut, siz
                         dim3(32 * cut.warps * cut.groups), smem, st, p, cut);
 }
 
-// A row of one warp always has room for two (22 KB at most); one of several warps has three
-// or four vectors a thread.
+// A row of one warp always has room for two (20 KB at most); one of several warps has three
+// or four vectors a thread, three up to 2304 features, where there is room for two rows too.
 template <bool kBack>
 static cudaError_t launch_vecs(const CombineParams& p, const CombineCut& cut, int vecs, int rows, size_t smem,
                                cudaStream_t st) {
   if (cut.warps > 1) {
-    if (rows == 1)
-      return vecs == 3 ? launch_cut<kBack, 3, 1, true>(p, cut, smem, st)
-                       : launch_cut<kBack, 4, 1, true>(p, cut, smem, st);
+    if (rows == 1) return launch_cut<kBack, 4, 1, true>(p, cut, smem, st);
     return vecs == 3 ? launch_cut<kBack, 3, 2, true>(p, cut, smem, st)
                      : launch_cut<kBack, 4, 2, true>(p, cut, smem, st);
   }
