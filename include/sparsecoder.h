@@ -560,6 +560,10 @@ int sc_expert_route_backward(const sc_expert_route_backward_args* args, void* st
  *          one without slots); dbias fp32 [E][N] or NULL.
  * Products of bf16 values, sums in fp32, one rounding at the end.  Two calls with
  * the same arguments give the same bits.
+ * GELU(y) = y Phi(y), Phi the normal distribution: before the rounding within
+ * (16 + y^2) 2^-24 of itself, GELU' within as much of Phi(y) + |y| Phi'(y), both down
+ * to 2^-122 and, for bf16 outputs, to 2^-17 of themselves.  GELU(-inf) = 0; GELU' of an
+ * infinity is NaN.
  * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; M at most 2^31 - 4096; ldx and
  * ldy multiples of 8 below 2^30; every bf16 pointer, out, dX and dW 16-byte aligned.
  */
