@@ -48,12 +48,18 @@ constexpr uint32_t kPairBBytes = kPairN / 2 * kPairStep * 2;
 constexpr uint32_t kPairStageBytes = kPairABytes + kPairBBytes;
 constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN-major operand
 // The tensor cores add to an fp32 accumulator with truncation, half a unit in the last
-// place per 16 of the contraction: 2048 slots, 3.7e-6.  bf16 outputs do not show it.  For
+// place per 16 of the contraction: 2048 slots, 3.7e-6, growing with their number.  For
 // fp32 outputs an accumulator takes kSpan stages (512 of the contraction) only; eight
 // write-back warps add it, rounded, to sums in their registers (128 a thread; weight
 // gradient: 64, and as many in the write-back areas, for the registers of the other
-// warps).  2048 slots: 4.8e-7, torch's fp32 product 3.9e-7.
+// warps).  2048 slots: 4.8e-7, torch's fp32 product 3.9e-7.  bf16 outputs do not show the
+// truncation of the forward product and of the rows' gradient, 8192 deep at most.  The
+// weight gradient's depth is the number of slots: past kLongSlots, where an expert might lose
+// 1.2e-4, a sixteenth of bf16's half unit, bf16 weights take the spans too (and no wait is for
+// more than eight stages).  65600 slots of 8 experts, 768 x 1536: 120 us without, 129 with them.
 constexpr int kSpan = 8;
+constexpr int kLongSlots = 65536;
+// kF32: sums over spans; of fp32 outputs, and of bf16 weight gradients of many slots.
 // kPre: with the value before GELU, written (forward) or read (back, input).
 template <ExpertProduct kWhat, bool kGather_, bool kF32_, bool kPre_>
 struct PairKind {
@@ -506,20 +512,22 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
       load_bias(ahead);
     }
     // weight gradient in bf16: 32 rows (features) of 32 columns, contiguous in memory, from
-    // column c
-    const auto put_rows = [&](int f, int c, const float (&v)[32]) {
-      uint8_t* const to = next_area();
+    // column c, a row a lane; from `to`, which no copy and no lane reads any more
+    const auto put_pieces = [&](uint8_t* to, int f, int c, const uint4 (&v)[4]) {
 #pragma unroll
-      for (int k = 0; k < 32; k += 8)
-        stage_row_piece<4>(to, k / 8,
-                           make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
-                                      pack_bf16x2(v[k + 4], v[k + 5]), pack_bf16x2(v[k + 6], v[k + 7])));
+      for (int k = 0; k < 4; ++k) stage_row_piece<4>(to, k, v[k]);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
         tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(to));   // cut at N and K
         bulk_commit();
       }
+    };
+    const auto pack_row = [&](uint4 (&w)[4], const float (&v)[32]) {
+#pragma unroll
+      for (int k = 0; k < 32; k += 8)
+        w[k / 8] = make_uint4(pack_bf16x2(v[k], v[k + 1]), pack_bf16x2(v[k + 2], v[k + 3]),
+                              pack_bf16x2(v[k + 4], v[k + 5]), pack_bf16x2(v[k + 6], v[k + 7]));
     };
     // forward, back (input): 32 rows (features) of the 32 columns (slots) from c, in
     // fragments, transposed on the way out
@@ -651,7 +659,9 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
 #pragma unroll
               for (int k = 0; k < 32; ++k) v[k] = 0.f;   // an expert without slots
             }
-            put_rows(f, c, v);
+            uint4 w[4];
+            pack_row(w, v);
+            put_pieces(next_area(), f, c, w);
           } else {
             float v[2][16];
             tmem_ld_frag32(d + c, v[0]);
@@ -705,28 +715,51 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
           release_sum();
         }
         // the areas' columns leave, then the registers' through them
+        if (!p.out_f32) {
 #pragma unroll
-        for (int i = 2; i >= 0; i -= 2) {
-          if (i == 0) {
-            if (lane == 0) bulk_wait_read<0>();
-            __syncwarp();
+          for (int o = 0; o < 4; ++o) {
+            uint8_t* const area = stg + (o & 1) * 4096;
+            const int c = kPairChunk * (grp + 2 * (o < 2 ? 2 + o : o - 2));
+            uint4 w[4];
+            if (o < 2) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 4)
-#pragma unroll
-              for (int o = 0; o < 2; ++o)
-                stage_row_piece<8>(stg + 4096 * o, k / 4,
-                                   make_uint4(__float_as_uint(sum[o][k]), __float_as_uint(sum[o][k + 1]),
-                                              __float_as_uint(sum[o][k + 2]), __float_as_uint(sum[o][k + 3])));
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0 && ok && f < p.N) {
-#pragma unroll
-            for (int o = 0; o < 2; ++o) {
-              const int c = kPairChunk * (grp + 2 * (i + o));
-              if (c < g.n) tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(stg + 4096 * o));   // cut at N and K
+              for (int k = 0; k < 4; ++k) {
+                const float4 a = *reinterpret_cast<const float4*>(area + stage_offset<8>(lane, 2 * k));
+                const float4 b = *reinterpret_cast<const float4*>(area + stage_offset<8>(lane, 2 * k + 1));
+                w[k] = make_uint4(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w), pack_bf16x2(b.x, b.y),
+                                  pack_bf16x2(b.z, b.w));
+              }
+            } else {
+              pack_row(w, sum[o & 1]);
+              if (o == 2 && lane == 0) bulk_wait_read<0>();
             }
-            bulk_commit();
+            __syncwarp();
+            if (ok && f < p.N && c < g.n) put_pieces(area, f, c, w);
+          }
+        } else {
+#pragma unroll
+          for (int i = 2; i >= 0; i -= 2) {
+            if (i == 0) {
+              if (lane == 0) bulk_wait_read<0>();
+              __syncwarp();
+#pragma unroll
+              for (int k = 0; k < 32; k += 4)
+#pragma unroll
+                for (int o = 0; o < 2; ++o)
+                  stage_row_piece<8>(stg + 4096 * o, k / 4,
+                                     make_uint4(__float_as_uint(sum[o][k]), __float_as_uint(sum[o][k + 1]),
+                                                __float_as_uint(sum[o][k + 2]), __float_as_uint(sum[o][k + 3])));
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && ok && f < p.N) {
+#pragma unroll
+              for (int o = 0; o < 2; ++o) {
+                const int c = kPairChunk * (grp + 2 * (i + o));
+                if (c < g.n) tma_store_3d(&P.map_out, g.i0 + c, f, g.e, smem_u32(stg + 4096 * o));   // cut at N and K
+              }
+              bulk_commit();
+            }
           }
         }
       } else {
@@ -1359,7 +1392,8 @@ static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaSt
 template <ExpertProduct kWhat, bool kGather>
 static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
   // (the fp32 kernels have the room anyway)
-  if (P.p.out_f32) return launch_pair<kWhat, kGather, true, true>(P, most_tiles, st);
+  if (P.p.out_f32 || (kWhat == ExpertProduct::kBackWeight && P.p.M > kLongSlots))
+    return launch_pair<kWhat, kGather, true, true>(P, most_tiles, st);
   if constexpr (kWhat != ExpertProduct::kBackWeight) {
     if (P.p.pre != nullptr || P.p.pre_in != nullptr)
       return launch_pair<kWhat, kGather, false, true>(P, most_tiles, st);
