@@ -1018,28 +1018,40 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
       // ------------------------------------------------------------- bias sums
       // A lane has four features (8 bytes of a 256-byte row of the stage), a warp 16 of
       // the 64 slots.  A stage whose products are done is summed, in the first column
-      // block of each expert and 256 features, and handed back to the copies.
+      // block of each expert and 256 features, and handed back to the copies.  The sums of
+      // 64 stages (4096 slots) are added up apart: one chain of all slots loses what is
+      // below a unit of the sum so far, each time.
       int s = 0, use = 0;
       for (; sums && walk.more(); walk.next(sm)) {
         pair_tile<kWhat>(p, sm, walk.t, g);
         const int steps = pair_steps<kWhat>(p, g);
-        float part[4] = {};
+        float part[4] = {}, block[4] = {};
 #pragma unroll 1
         for (int kt = 0; kt < steps; ++kt) {
           ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
+          float now[4] = {};
           if (ok && g.i0 == 0) {
             const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
 #pragma unroll 8
             for (int i = 0; i < 16; ++i) {
               const uint2 v =
                   *reinterpret_cast<const uint2*>(at + sw128_offset(16 * (l >> 5) + i, (lane & 15) >> 1));
-              part[0] += bf_lo(v.x);
-              part[1] += bf_hi(v.x);
-              part[2] += bf_lo(v.y);
-              part[3] += bf_hi(v.y);
+              now[0] += bf_lo(v.x);
+              now[1] += bf_hi(v.x);
+              now[2] += bf_lo(v.y);
+              now[3] += bf_hi(v.y);
             }
           }
           warp_arrive(&sm.empty[s]);
+          const bool full = kt % 64 == 63 || kt == steps - 1;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            block[i] += now[i];
+            if (full) {
+              part[i] += block[i];
+              block[i] = 0.f;
+            }
+          }
           if (++s == kStages) {
             s = 0;
             ++use;

@@ -51,3 +51,17 @@ def test_bf16_weight_gradient_of_millions_of_slots(gather):
 @pytest.mark.parametrize("gather,pad,bias", [(True, 0, True), (False, 8, True), (True, 16, False)])
 def test_bf16_weight_gradient_in_spans(counts, N, K, gather, pad, bias):
     ops.test_expert_linear_backward_weight(counts, N, K, gather, pad, False, bias, 3)
+
+
+@pytest.mark.parametrize("c", [1, 64, 65, 4096, 4200, 1 << 16])
+def test_bias_gradient_beside_a_large_value(c):
+    """A slot of 2^24 and ones: additions of single values to the sum so far would lose every one.
+    16 slots, 64 such sums and one more for each 4096 slots are added in turn, then four warps' sums."""
+    M, N, K = c + 3, 40, 8
+    dY = torch.ones(M, N, device="cuda", dtype=torch.bfloat16)
+    dY[0] = 2.0 ** 24
+    X = torch.zeros(M, K, device="cuda", dtype=torch.bfloat16)
+    got = sc.expert_linear_backward_weight(dY, X, ops.offsets_of([c, 0, 3]))["dbias"].double()
+    bound = (16 + 64 + c / 4096 + 4) * 2.0 ** -24 * (2.0 ** 24 + c - 1)
+    assert bool(((got[0] - (2.0 ** 24 + c - 1)).abs() <= bound).all()), "%g off" % float(2.0 ** 24 + c - 1 - got[0].min())
+    assert bool((got[1] == 0).all()) and bool((got[2] == 3).all())
