@@ -209,11 +209,12 @@ int sc_layer_noalloc_status(void* stream);
 /* Test hook of the failure path; not for production use.  While ns > 0, the
  * first MMA-issuing thread of every CTA of the per-layer attention kernel
  * (sc_layer_forward, sc_layer_forward_noalloc and the per-layer part of the
- * stacks) first waits at most ns nanoseconds on a barrier that nothing
- * completes.  That bounded wait expires: the CTA abandons its work, drains
- * its copies and matrix products, frees its tensor memory and records
- * SC_ERR_TIMEOUT in the status word, so the call's results are undefined and
- * the status query reports SC_ERR_TIMEOUT.  ns = 0 (the default) turns it off.
+ * stacks), and of every pair of CTAs of an expert product, first waits at
+ * most ns nanoseconds on a barrier that nothing completes.  That bounded wait
+ * expires: the CTA (or pair) abandons its work, drains its copies and matrix
+ * products, frees its tensor memory and records SC_ERR_TIMEOUT in the status
+ * word, so the call's results are undefined and the status query reports
+ * SC_ERR_TIMEOUT.  ns = 0 (the default) turns it off.
  * Process-wide; read when a call enqueues its kernels. */
 void sc_debug_stall_waits(unsigned long long ns);
 

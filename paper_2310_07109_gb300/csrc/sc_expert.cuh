@@ -72,6 +72,7 @@ struct ExpertLinearParams {
   int out_f32;
   float* dbias;              // kBackWeight: [E][N] or nullptr
   int* status;
+  unsigned long long stall_ns;   // test hook (0: off): a wait of the products that nothing ends
 };
 
 // Slots of expert e: the caller's offsets, held within [0, M].

@@ -12,6 +12,7 @@ namespace sc {
 int api_fail(int code, const char* what, const char* detail);
 int api_fail_cuda(const char* what, cudaError_t e);
 int api_ensure_configured();
+unsigned long long api_stall_ns();
 }  // namespace sc
 
 namespace {
@@ -64,9 +65,10 @@ bool good_matrix(const void* p, long long ld, int width) {
   return p && aligned(p, 16) && ld >= width && ld % 8 == 0 && ld < (1ll << 30);
 }
 
-int launch_product(ExpertProduct what, const ExpertLinearParams& p, void* stream) {
+int launch_product(ExpertProduct what, ExpertLinearParams& p, void* stream) {
   const int rc = api_ensure_configured();
   if (rc != SC_OK) return rc;
+  p.stall_ns = api_stall_ns();
   const cudaError_t e = launch_expert_linear(what, p, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? SC_OK : api_fail_cuda("launch expert product", e);
 }

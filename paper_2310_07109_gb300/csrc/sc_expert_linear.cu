@@ -110,8 +110,13 @@ struct PairSmem {
   uint64_t done[kPairMaxStages];                       // products done, the bias sums not yet
   uint64_t landed[kPairMaxStages];                     // this CTA's gathered rows
   uint64_t tfull[2], tempty[2];                     // tempty: of the even CTA
+  uint64_t fin;                                     // every product issued is done
+  uint64_t stall;                                   // test hook: never completed
   uint32_t tmem_base;
   int abort;
+  // after a wait that ran out in either CTA: fills of the even CTA's `full` barriers, by the
+  // two copying warps and the two threads that hand gathered rows over
+  int gave_up, fills[2], handed[2];
   union {
     int tile0[kMaxExperts + 1];   // forward, back (input): tiles of slots of the experts before
     alignas(16) float sums[2][kPairM];   // weight gradient: bias sums of two warps each
@@ -319,6 +324,36 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
   return __all_sync(0xffffffffu, mbar_wait_poll(bar, parity, abort));
 }
 
+// Bounded wait that ignores the abort flag (teardown: no copy or product may still use
+// this CTA's memory when it exits).
+__device__ __forceinline__ void drain_wait_pair(uint64_t* bar, uint32_t parity) {
+  int dummy = 0;
+  mbar_wait(bar, parity, &dummy, 1000000000ull);
+}
+
+// The copies of both CTAs that are on their way, awaited by one thread of the even CTA once
+// no role starts another: all of them count on its `full` barriers.  A stage is filled again
+// only after everyone's last fill of it, so the fills of a stage differ by one at most;
+// whoever gave up before the last one is stood in for.  (Not inlined: its registers cost the
+// fp32 weight gradient 100 bytes of spills.)
+template <int kStages, bool kGather>
+__device__ __noinline__ void drain_copies(PairSmem& sm) {
+#pragma unroll 1
+  for (int q = 0; q < kStages; ++q) {
+    const auto of = [&](int n) { return n / kStages + (q < n % kStages ? 1 : 0); };
+    int n[4] = {of(sm.fills[0]), of(sm.fills[1])};
+    if constexpr (kGather) n[2] = of(sm.handed[0]), n[3] = of(sm.handed[1]);
+    int most = 0;
+#pragma unroll
+    for (int i = 0; i < (kGather ? 4 : 2); ++i) most = max(most, n[i]);
+    if (most == 0) continue;
+#pragma unroll
+    for (int i = 0; i < (kGather ? 4 : 2); ++i)
+      if (n[i] < most) mbar_arrive(&sm.full[q]);
+    drain_wait_pair(&sm.full[q], (most - 1) & 1);
+  }
+}
+
 // The rows of a last, partial stage of the weight gradient: 64 slots x 128 columns of a
 // matrix into two 64 x 64 boxes, zeros past the expert's slots and the matrix's columns
 // (a product with what lies there would not be 0 for NaN), by the copying warp itself.
@@ -389,7 +424,9 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
       mbar_init(&sm.tempty[a], 2 * kEpiWarps);
     }
     mbar_init(&sm.dealt_out, 1);
-    sm.abort = 0;
+    mbar_init(&sm.fin, 1);
+    mbar_init(&sm.stall, 1);
+    sm.abort = sm.gave_up = 0;
     fence_mbar_init();
   }
   if (warp == 1) tmem_alloc_pair(&sm.tmem_base, 512);
@@ -864,10 +901,13 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
         const int fills = use + (q < s ? 1 : 0);
         if (fills > 0) warp_wait(&sm.empty[q], (fills - 1) & 1, abort_flag);
       }
+      // (the other CTA waits for this one's copies and products, and would for two seconds)
+      if (lane == 0 && *abort_flag) st_cluster_u32(dsmem_addr(smem_u32(&sm.abort), rank ^ 1), 1u);
+      if (lane == 0) st_cluster_u32(dsmem_addr(smem_u32(&sm.fills[rank]), 0), use * kStages + s);
     } else if (warp == 1) {
       // ------------------------------------------------------------- products
       if (rank == 0 && elect_one()) {
-        bool ok = true;
+        bool ok = p.stall_ns == 0 || mbar_wait(&sm.stall, 0, abort_flag, p.stall_ns);
         int s = 0, use = 0, j = 0;
         for (; ok && walk.more(); walk.next(sm)) {
           pair_tile<kWhat>(p, sm, walk.t, g);
@@ -909,6 +949,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
             }
           }
         }
+        umma_commit_pair(&sm.fin);
       }
       __syncwarp();
     } else if (kGather && warp == 2) {
@@ -934,6 +975,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
             }
           }
         }
+        st_cluster_u32(dsmem_addr(smem_u32(&sm.handed[rank]), 0), use * kStages + s);
       }
       __syncwarp();
     } else if (kGather && warp >= kGatherWarp && warp < kGatherWarp + 4) {
@@ -1028,9 +1070,9 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
         float part[4] = {}, block[4] = {};
 #pragma unroll 1
         for (int kt = 0; kt < steps; ++kt) {
-          ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag);
+          if (!(ok = ok && warp_wait(&sm.done[s], use & 1, abort_flag))) break;
           float now[4] = {};
-          if (ok && g.i0 == 0) {
+          if (g.i0 == 0) {
             const uint8_t* at = base + s * kPairStageBytes + (lane >> 4) * kPairBoxBytes + 8 * (lane & 1);
 #pragma unroll 8
             for (int i = 0; i < 16; ++i) {
@@ -1075,7 +1117,18 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
 
   tc_fence_before();
   __syncthreads();
-  cluster_sync();   // nothing of the pair is in flight to or from the other CTA
+  if (tid == 0 && sm.abort) {   // of either CTA, for both
+    st_cluster_u32(dsmem_addr(smem_u32(&sm.gave_up), 0), 1u);
+    st_cluster_u32(dsmem_addr(smem_u32(&sm.gave_up), 1), 1u);
+  }
+  cluster_sync();   // no role of the pair starts a copy or a product any more
+  if (warp == 1) drain_wait_pair(&sm.fin, 0);
+  __syncwarp();
+  if (sm.gave_up) {
+    if (rank == 0 && tid == 0) drain_copies<kStages, kGather>(sm);
+    __syncwarp();
+    cluster_sync();
+  }
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc_pair(tm, 512);

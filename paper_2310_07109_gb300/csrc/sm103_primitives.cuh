@@ -606,6 +606,10 @@ __device__ __forceinline__ uint32_t dsmem_addr(uint32_t saddr, uint32_t rank) {
   return r;
 }
 
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
 // A store into another CTA's shared memory that counts its 4 bytes on an mbarrier
 // there once it is visible to whoever waits for that barrier (both addresses in
 // the cluster's shared window).
