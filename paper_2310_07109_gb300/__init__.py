@@ -19,7 +19,8 @@ from .binding import (ENCODER_WEIGHTS, SC_ERR_CUDA, SC_ERR_INVALID_ARG, SC_ERR_T
 from .expert import (MAX_CHOICES, MAX_EXPERT_DIM, MAX_EXPERTS, expert_combine_backward,
                      expert_combine_forward, expert_linear_backward_input,
                      expert_linear_backward_weight, expert_linear_forward, expert_route_backward,
-                     expert_route_forward, expert_workspace_size, new_expert_workspace)
+                     expert_route_forward, expert_status, expert_workspace_size,
+                     new_expert_workspace)
 
 __all__ = ["ENCODER_WEIGHTS", "SC_ERR_CUDA", "SC_ERR_INVALID_ARG", "SC_ERR_TIMEOUT",
            "SC_ERR_UNSUPPORTED", "SC_ERR_WORKSPACE", "SC_KEEP_ABSOLUTE", "SC_KEEP_RELATIVE",
@@ -32,6 +33,6 @@ __all__ = ["ENCODER_WEIGHTS", "SC_ERR_CUDA", "SC_ERR_INVALID_ARG", "SC_ERR_TIMEO
            "MAX_CHOICES", "MAX_EXPERT_DIM", "MAX_EXPERTS", "expert_combine_backward",
            "expert_combine_forward", "expert_linear_backward_input",
            "expert_linear_backward_weight", "expert_linear_forward", "expert_route_backward",
-           "expert_route_forward", "expert_workspace_size", "new_expert_workspace",
+           "expert_route_forward", "expert_status", "expert_workspace_size", "new_expert_workspace",
            "stack_forward_host", "stack_host_workspace_size", "stack_launch_count",
            "status_string", "workspace_size", "workspace_status"]

@@ -269,8 +269,30 @@ def expert_route_backward(logits, expert, gate, dgate, *, B, L, rows=None, renor
     return out
 
 
-def _product_ws(workspace, t, stream):
-    return _work(workspace, t.device, stream, 1, 1, 1, 1, 8)
+# Per device: the workspace of products that are called without one.  They use its status
+# word alone, which only ever gains bits, so that calls on several streams may share it.
+_products = {}
+
+
+def _product_ws(workspace, t, dev, stream):
+    if workspace is not None:
+        return workspace
+    ws = _products.get(dev)
+    if ws is None:
+        if torch.cuda.is_current_stream_capturing():
+            return _work(None, t.device, stream, 1, 1, 1, 1, 8)   # a graph's memory is not kept
+        ws = new_expert_workspace(1, 1, 1, 1, 8, t.device)
+        torch.cuda.current_stream(t.device).synchronize()   # zeroed, for whatever stream comes first
+        ws = _products.setdefault(dev, ws)
+    return ws
+
+
+def expert_status(stream=None) -> int:
+    """Synchronise ``stream`` (the current one) and return, then clear, the status of the products
+    called without a workspace on the current device, outside a graph capture.  A workspace's
+    own status: ``workspace_status``."""
+    ws = _products.get(torch.cuda.current_device())
+    return _b.SC_OK if ws is None else _b.workspace_status(ws, stream)
 
 
 def expert_linear_forward(X, W, offsets, *, token=None, bias=None, gelu=False, pre=None, out=None,
@@ -292,7 +314,7 @@ def expert_linear_forward(X, W, offsets, *, token=None, bias=None, gelu=False, p
                          _at(bias, "bias", torch.float32, E * N, dev), 1 if gelu else 0,
                          _at(pre, "pre", torch.bfloat16, M * N, dev), _at(out, "out", out.dtype, M * N, dev),
                          _out_type(out))
-    _call(_LINEAR, a, _product_ws(workspace, X, stream), dev, stream)
+    _call(_LINEAR, a, _product_ws(workspace, X, dev, stream), dev, stream)
     return out
 
 
@@ -310,7 +332,7 @@ def expert_linear_backward_input(dY, W, offsets, *, pre=None, out=None, out_f32=
                                       _at(W, "W", torch.bfloat16, E * N * K, dev),
                                       _at(pre, "pre", torch.bfloat16, M * K, dev),
                                       _at(out, "out", out.dtype, M * K, dev), _out_type(out))
-    _call(_BACK_X, a, _product_ws(workspace, dY, stream), dev, stream)
+    _call(_BACK_X, a, _product_ws(workspace, dY, dev, stream), dev, stream)
     return out
 
 
@@ -335,7 +357,7 @@ def expert_linear_backward_weight(dY, X, offsets, *, token=None, bias=True, out=
                                        _at(offsets, "offsets", torch.int32, E + 1, dev),
                                        _at(dW, "dW", dW.dtype, E * N * K, dev), _out_type(dW),
                                        _at(out.get("dbias"), "dbias", torch.float32, E * N, dev))
-    _call(_BACK_W, a, _product_ws(workspace, X, stream), dev, stream)
+    _call(_BACK_W, a, _product_ws(workspace, X, dev, stream), dev, stream)
     return out
 
 

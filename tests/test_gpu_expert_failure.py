@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paper_2310_07109_gb300 as sc
+from paper_2310_07109_gb300 import expert as ex
 import test_gpu_expert as ops
 
 pytestmark = pytest.mark.gpu
@@ -22,9 +23,10 @@ def forward(f32, gather, pre):
     W = ops.bf16(ops.randn(g, len(COUNTS), N, K) / math.sqrt(K))
     z = torch.zeros(M, N, device="cuda", dtype=torch.bfloat16) if pre else None
     out = torch.zeros(M, N, device="cuda", dtype=torch.float32 if f32 else torch.bfloat16)
+    off = ops.offsets_of(COUNTS)
 
     def call(ws):
-        sc.expert_linear_forward(X, W, ops.offsets_of(COUNTS), token=token, gelu=pre, pre=z, out=out, workspace=ws)
+        sc.expert_linear_forward(X, W, off, token=token, gelu=pre, pre=z, out=out, workspace=ws)
         return [out] + ([z] if pre else [])
     return call
 
@@ -35,9 +37,10 @@ def backward_input(f32, pre):
     W = ops.bf16(ops.randn(g, len(COUNTS), N, K) / math.sqrt(N))
     z = ops.bf16(ops.randn(g, M, K)) if pre else None
     out = torch.zeros(M, K, device="cuda", dtype=torch.float32 if f32 else torch.bfloat16)
+    off = ops.offsets_of(COUNTS)
 
     def call(ws):
-        sc.expert_linear_backward_input(dY, W, ops.offsets_of(COUNTS), pre=z, out=out, workspace=ws)
+        sc.expert_linear_backward_input(dY, W, off, pre=z, out=out, workspace=ws)
         return [out]
     return call
 
@@ -49,9 +52,10 @@ def backward_weight(f32, gather, bias):
     out = {"dW": torch.zeros(E, N, K, device="cuda", dtype=torch.float32 if f32 else torch.bfloat16)}
     if bias:
         out["dbias"] = torch.zeros(E, N, device="cuda")
+    off = ops.offsets_of(COUNTS)
 
     def call(ws):
-        sc.expert_linear_backward_weight(dY, X, ops.offsets_of(COUNTS), token=token, out=out, workspace=ws)
+        sc.expert_linear_backward_weight(dY, X, off, token=token, out=out, workspace=ws)
         return list(out.values())
     return call
 
@@ -95,3 +99,45 @@ def test_expired_wait_is_reported_and_left_behind(what):
         for a, b in zip(call(ws), right):
             assert torch.equal(a, b)
         assert sc.workspace_status(ws) == sc.SC_OK
+
+
+def test_status_of_calls_without_a_workspace():
+    """Reported too, whichever stream the call was on, until it is asked for."""
+    calls = [CALLS[what]() for what in ("forward", "gradient of the rows", "gradient of the weights")]
+    right = [[t.clone() for t in call(None)] for call in calls]
+    assert sc.expert_status() == sc.SC_OK
+    side = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), side):
+        for i, call in enumerate(calls):
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                sc.debug_stall_waits(STALL_NS)
+                try:
+                    call(None)
+                finally:
+                    sc.debug_stall_waits(0)
+                got = [t.clone() for t in call(None)]   # (a later call does not clear it)
+            torch.cuda.synchronize()
+            assert sc.expert_status() == sc.SC_ERR_TIMEOUT
+            assert sc.expert_status() == sc.SC_OK
+            for a, b in zip(got, right[i]):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("first", [False, True])   # the first call without a workspace at all?
+def test_calls_without_a_workspace_in_a_graph(first, monkeypatch):
+    call = CALLS["forward"]()
+    right = [t.clone() for t in call(None)]
+    if first:
+        monkeypatch.setattr(ex, "_products", {})
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        out = call(None)
+    for t in out:
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(out, right):
+        assert torch.equal(a, b)
+    assert sc.expert_status() == sc.SC_OK
