@@ -1591,6 +1591,7 @@ int api_ensure_configured() {
   if (rc == SC_OK && dev >= 0 && dev < 256) ready[dev].store(true, std::memory_order_release);
   return rc;
 }
+int api_device_sms() { return device_sms(); }
 unsigned long long api_stall_ns() { return g_stall_ns.load(std::memory_order_relaxed); }
 PFN_cuTensorMapEncodeTiled_v12000 api_tensor_map_encoder() { return get_encoder(); }
 

@@ -469,16 +469,6 @@ static_assert(kCombineBytes + sizeof(CombineSmem) <= 227 * 1024, "one CTA's shar
 
 template <bool kBack, int V, int kRows, bool kWide>
 static cudaError_t launch_cut(const CombineParams& p, const CombineCut& cut, size_t smem, cudaStream_t st) {
-  static bool set[64] = {};   // per device
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 64 || !set[dev]) {
-    e = cudaFuncSetAttribute(sc_combine_kernel<kBack, V, kRows, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(kCombineBytes));
-    if (e != cudaSuccess) return e;
-    if (dev < 64) set[dev] = true;
-  }
   return launch_chained(sc_combine_kernel<kBack, V, kRows, kWide>, dim3(cut.ctas),
                         dim3(32 * cut.warps * cut.groups), smem, st, p, cut);
 }
@@ -519,17 +509,38 @@ static cudaError_t combine(const CombineParams& p, cudaStream_t st) {
   const int rows = row * 2 <= most ? 2 : 1;
   cut.groups = kCombineWarps / cut.warps;
   while (cut.groups > 1 && row * rows * cut.groups > most) --cut.groups;
-  int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
+  const int sms = api_device_sms();
+  if (sms < 1) return cudaErrorInvalidDevice;
   const long long want = (p.T + cut.groups - 1) / cut.groups;
   const long long room = kBack ? (sms < kCombineMaxParts ? sms : kCombineMaxParts) : 2ll * sms;
   cut.ctas = static_cast<int>(want < room ? want : room);
   const size_t smem = row * rows * cut.groups + params;
-  e = launch_vecs<kBack>(p, cut, vecs, rows, smem, st);
+  const cudaError_t e = launch_vecs<kBack>(p, cut, vecs, rows, smem, st);
   if (e != cudaSuccess || !kBack || !norm) return e;
   return launch_chained(sc_combine_reduce_kernel, dim3((2 * p.D + 31) / 32), dim3(1024), 0, st, p, cut.ctas);
+}
+
+template <bool kBack, int V, int kRows, bool kWide>
+static cudaError_t configure_cut() {
+  return cudaFuncSetAttribute(sc_combine_kernel<kBack, V, kRows, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(kCombineBytes));
+}
+
+template <bool kBack>
+static cudaError_t configure_cuts() {
+  cudaError_t e = configure_cut<kBack, 1, 2, false>();
+  if (e == cudaSuccess) e = configure_cut<kBack, 2, 2, false>();
+  if (e == cudaSuccess) e = configure_cut<kBack, 3, 2, false>();
+  if (e == cudaSuccess) e = configure_cut<kBack, 4, 2, false>();
+  if (e == cudaSuccess) e = configure_cut<kBack, 3, 2, true>();
+  if (e == cudaSuccess) e = configure_cut<kBack, 4, 2, true>();
+  if (e == cudaSuccess) e = configure_cut<kBack, 4, 1, true>();
+  return e;
+}
+
+cudaError_t configure_combine() {
+  const cudaError_t e = configure_cuts<false>();
+  return e == cudaSuccess ? configure_cuts<true>() : e;
 }
 
 cudaError_t launch_combine(const CombineParams& p, cudaStream_t st) { return combine<false>(p, st); }

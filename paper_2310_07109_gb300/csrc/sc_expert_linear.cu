@@ -1429,13 +1429,8 @@ static bool encode_out(CUtensorMap* m, void* base, bool f32, long long rows, int
 template <ExpertProduct kWhat, bool kGather, bool kF32, bool kPre>
 static cudaError_t launch_pair(const PairParams& P, long long most_tiles, cudaStream_t st) {
   using Kind = PairKind<kWhat, kGather, kF32, kPre>;
-  static int sms = 0;
-  if (sms == 0) {
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e != cudaSuccess) return e;
-  }
+  const int sms = api_device_sms();
+  if (sms < 2) return cudaErrorInvalidDevice;
   const long long pairs = most_tiles < sms / 2 ? most_tiles : sms / 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
@@ -1473,7 +1468,7 @@ cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p
   }
   const int width = what == ExpertProduct::kBackInput ? p.K : p.N;
   if (what != ExpertProduct::kBackWeight && p.M <= static_cast<long long>(kSmallRows) * p.E &&
-      (p.E < p.M ? p.E : p.M) * ((width + 255) / 256) <= 2 * 76) {
+      (p.E < p.M ? p.E : p.M) * ((width + 255) / 256) <= api_device_sms() / 2 * 2) {
     const dim3 grid((width + kSmallF - 1) / kSmallF, p.M / kSmallS + (p.E < p.M ? p.E : p.M));
     return launch_chained(what == ExpertProduct::kForward ? sc_expert_small_kernel<ExpertProduct::kForward>
                                                           : sc_expert_small_kernel<ExpertProduct::kBackInput>,
@@ -1545,7 +1540,8 @@ static cudaError_t configure_pair() {
 }
 
 cudaError_t configure_expert() {
-  cudaError_t e = configure_pair<ExpertProduct::kForward, false>();
+  cudaError_t e = configure_combine();
+  if (e == cudaSuccess) e = configure_pair<ExpertProduct::kForward, false>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kForward, true>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackInput, false>();
   if (e == cudaSuccess) e = configure_pair<ExpertProduct::kBackWeight, false>();
