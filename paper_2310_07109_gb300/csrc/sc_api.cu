@@ -1578,7 +1578,6 @@ extern "C" int sc_encoder_layer_forward(const sc_encoder_args* a, void* workspac
 // ---------------------------------------------------------------------------
 namespace sc {
 
-int api_fail(int code, const char* what, const char* detail) { return fail(code, what, detail); }
 int api_fail_cuda(const char* what, cudaError_t e) { return fail_cuda(what, e); }
 // Once a device is set up, its number alone: a call on a few rows is all host time.
 int api_ensure_configured() {

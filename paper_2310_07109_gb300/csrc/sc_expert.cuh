@@ -115,7 +115,6 @@ struct CombineParams {
 int api_device_sms();   // multiprocessors of the current device (0 if unknown)
 cudaError_t configure_expert();
 cudaError_t configure_combine();
-int route_ctas(long long T, int* per_cta);
 cudaError_t launch_route(const RouteParams& p, cudaStream_t st);
 cudaError_t launch_route_back(const RouteBackParams& p, cudaStream_t st);
 cudaError_t launch_expert_linear(ExpertProduct what, const ExpertLinearParams& p, cudaStream_t st);

@@ -9,7 +9,6 @@
 #include "sc_expert.cuh"
 
 namespace sc {
-int api_fail(int code, const char* what, const char* detail);
 int api_fail_cuda(const char* what, cudaError_t e);
 int api_ensure_configured();
 unsigned long long api_stall_ns();

@@ -52,7 +52,6 @@ __device__ __forceinline__ uint4 pack8(const uint64_t (&f)[4]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__device__ __forceinline__ uint64_t f2_both(float x) { return f2_pack(x, x); }
 __device__ __forceinline__ float f2_sum(uint64_t v) {
   float lo, hi;
   f2_unpack(v, lo, hi);

@@ -141,7 +141,6 @@ __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 
 // of the exponential.  Six (kShort) are for what is rounded to bf16, whose half unit is 400
 // times their error: 16384 slots, 768 -> 1536, GELU and the value before it 45.0 us (45.6
 // with eight), GELU' 46.9 (47.7).
-__device__ __forceinline__ uint64_t f2_both(float x) { return f2_pack(x, x); }
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

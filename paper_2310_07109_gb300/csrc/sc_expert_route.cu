@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(kRouteBackThreads) sc_route_back_kernel(
     if (lane + 32 * v < p.E) p.dlogits[t * p.E + lane + 32 * v] = d[v];
 }
 
-int route_ctas(long long T, int* per_cta) {
+static int route_ctas(long long T, int* per_cta) {
   const long long chunks = (T + kRouteTokens - 1) / kRouteTokens;
   const long long each = (chunks + kRouteMaxCtas - 1) / kRouteMaxCtas;
   *per_cta = static_cast<int>(each * kRouteTokens);
