@@ -1272,7 +1272,9 @@ __global__ void __launch_bounds__(kSmallThreads, 4)
     if (i < steps) copy(i);
     cp_async_commit();
   }
-  float acc[4][4] = {}, sum[4][4] = {};   // slots 8 j ..; sum: see kSpan
+  // slots 8 j ..; sum: see kSpan, for fp32 outputs stage by stage (2048 deep: 1.3e-7, as torch's
+  // fp32 product, where eight stages had 4.7e-7; 12.0 us for 400 slots of 16 experts, 11.9 before)
+  float acc[4][4] = {}, sum[4][4] = {};
   const int f = 16 * warp;                // this warp's features of the tile
 #pragma unroll 1
   for (int kt = 0; kt < steps; ++kt) {
@@ -1294,7 +1296,7 @@ __global__ void __launch_bounds__(kSmallThreads, 4)
 #pragma unroll
       for (int j = 0; j < 4; ++j) mma_bf16(acc[j], av, bv[j >> 1][2 * (j & 1)], bv[j >> 1][2 * (j & 1) + 1]);
     }
-    if (kt % kSpan == kSpan - 1 || kt == steps - 1) {
+    if (p.out_f32 || kt % kSpan == kSpan - 1 || kt == steps - 1) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
