@@ -53,7 +53,7 @@ class ExpertFeedForward:
         p, w, ws = self.params, self.half, workspace
         if ws is None:
             ws = sc.new_expert_workspace(B, L, self.E, self.k, max(self.D, self.F), H.device)
-        every = torch.tensor([0, B * L], dtype=torch.int32, device=H.device)
+        every = torch.arange(0, 2 * B * L, B * L, dtype=torch.int32, device=H.device)   # all rows, no copy from the host
         logits = sc.expert_linear_forward(H, w["W_r"], every, out_f32=True, workspace=ws)
         r = sc.expert_route_forward(logits, k=self.k, B=B, L=L, rows=rows, workspace=ws)
         pre = torch.empty(B * L * self.k, self.F, dtype=torch.bfloat16, device=H.device)
