@@ -19,13 +19,16 @@
 //               TMA gathers of 128-byte rows took 81 cycles each, 8 x 1024 rows x 2
 //               experts 768 -> 1536 99 us against 34 without the gather
 //   four warps more (weight gradient) sum dy over the slots for the bias, from the
-//               stages in shared memory (by the gathering warps 63 us instead of 46)
+//               stages in shared memory (by the gathering warps 63 us instead of 47)
 // Operands as they lie in memory: K-major where the contraction is contiguous
 // (forward; dy in back (input)), else MN-major (W in back (input), both sides of the
 // weight gradient), 128-byte swizzle throughout.
-// Bound by the operands' way from the L2 into shared memory, which the outputs' way out
-// shares: 59,000 slots 2048 -> 1024 164 us (1.5 PFLOP/s; without the copies 123), 16384
-// slots 768 -> 1536 35 us (1.1), with GELU and the value before it 43 (50 MB more to write).
+// A long contraction is bound by the operands' way from the L2 into shared memory, which the
+// outputs' way out shares: 59,000 slots 2048 -> 1024 164 us (1.5 PFLOP/s; without the copies
+// 123; 180 to 188 on other boxes).  A short one is not: 16384 slots 768 -> 1536 35 us (1.1), with
+// GELU and the value before it 43 (50 MB more to write).  There the tiles of eight uneven
+// experts are 5.3 to 5.45 rounds of the pairs, run as six, and launch, first copies and last
+// write-back cost 6 us a call (one expert of 16384 slots: 33 us, the library's product 25).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -52,11 +55,12 @@ constexpr uint32_t kPairBoxBytes = 64 * kPairStep * 2;   // 64 x 64 box of an MN
 // fp32 outputs an accumulator takes kSpan stages (512 of the contraction) only; eight
 // write-back warps add it, rounded, to sums in their registers (128 a thread; weight
 // gradient: 64, and as many in the write-back areas, for the registers of the other
-// warps).  2048 slots: 4.8e-7, torch's fp32 product 3.9e-7.  bf16 outputs do not show the
-// truncation of the forward product and of the rows' gradient, 8192 deep at most.  The
-// weight gradient's depth is the number of slots: past kLongSlots, where an expert might lose
-// 1.2e-4, a sixteenth of bf16's half unit, bf16 weights take the spans too (and no wait is for
-// more than eight stages).  65600 slots of 8 experts, 768 x 1536: 120 us without, 129 with them.
+// warps).  Any depth from 512: 4.7e-7, torch's fp32 product 1.3e-7 to 3.9e-7.  bf16 outputs
+// do not show the truncation of the forward product and of the rows' gradient, 8192 deep at
+// most.  The weight gradient's depth is the number of slots: past kLongSlots, where an expert
+// might lose 1.2e-4, a sixteenth of bf16's half unit, bf16 weights take the spans too (and no
+// wait is for more than eight stages).  65600 slots of 8 experts, 768 x 1536: 120 us without,
+// 130 with them.
 constexpr int kSpan = 8;
 constexpr int kLongSlots = 65536;
 // kF32: sums over spans; of fp32 outputs, and of bf16 weight gradients of many slots.
@@ -117,6 +121,7 @@ struct PairSmem {
   // after a wait that ran out in either CTA: fills of the even CTA's `full` barriers, by the
   // two copying warps and the two threads that hand gathered rows over
   int gave_up, fills[2], handed[2];
+  alignas(16) uint32_t mark[4];   // of the even CTA: written by the odd one's signals
   union {
     int tile0[kMaxExperts + 1];   // forward, back (input): tiles of slots of the experts before
     alignas(16) float sums[2][kPairM];   // weight gradient: bias sums of two warps each
@@ -328,6 +333,23 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volati
 __device__ __forceinline__ void drain_wait_pair(uint64_t* bar, uint32_t parity) {
   int dummy = 0;
   mbar_wait(bar, parity, &dummy, 1000000000ull);
+}
+
+// Hands a stage that threads of this CTA wrote (and ordered before the products by a proxy fence)
+// to the even CTA, whose product reads it: an arrival on `full` there.  The odd CTA's comes
+// with a copy of 16 bytes, issued after the fence: its completion is a release over the
+// cluster, to the product's acquire, and nobody waits for it here.  (An arrival of the CTA's scope
+// alone orders nothing across CTAs; one with a release over the cluster holds its thread
+// for most of a stage: 69 us, not 37, for 16384 slots 768 -> 1536.  GELU and the value before it
+// 46.3 us so, 44.8 with the bare arrival; the weight gradient 47.9 and 47.4.)
+__device__ __forceinline__ void hand_over(PairSmem& sm, int rank, int s) {
+  const uint32_t full = dsmem_addr(smem_u32(&sm.full[s]), 0);
+  if (rank == 0) {
+    mbar_arrive(&sm.full[s]);
+  } else {
+    mbar_arrive_expect_tx_cluster(full, 16);
+    bulk_copy16_cluster(dsmem_addr(smem_u32(sm.mark), 0), smem_u32(sm.mark), full);
+  }
 }
 
 // The copies of both CTAs that are on their way, awaited by one thread of the even CTA once
@@ -863,7 +885,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
             cp_async_wait_all();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(full);
+            if (lane == 0) hand_over(sm, rank, s);
           } else if (lane == 0) {
             mbar_arrive_expect_tx_cluster(full, bytes);
             if constexpr (kFwd) {
@@ -926,9 +948,11 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
                 !(ok = mbar_wait_poll(&sm.tempty[acc], ((j >> 1) - 1) & 1, abort_flag)))
               break;
             const uint32_t d = tm + acc * kPairN;
-            if (!(ok = mbar_wait_poll(&sm.full[s], use & 1, abort_flag))) break;
-            if (kGather || (kBackW && g.lo + (kt + 1) * kPairStep > g.hi)) {
-              fence_proxy_async_smem();   // written by threads
+            if (kGather || (kBackW && g.lo + (kt + 1) * kPairStep > g.hi)) {   // written by threads
+              if (!(ok = mbar_wait_cluster(&sm.full[s], use & 1, abort_flag))) break;
+              fence_proxy_async_smem();
+            } else if (!(ok = mbar_wait_poll(&sm.full[s], use & 1, abort_flag))) {
+              break;
             }
             tc_fence_after();
             const uint32_t at = ring + s * kPairStageBytes;
@@ -953,10 +977,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
       __syncwarp();
     } else if (kGather && warp == 2) {
       // ------------------------------------------------------------- gathered rows handed over
-      // What threads write to shared memory is ordered before the products by the proxy
-      // fence.  Only the signal crosses to the even CTA: the rows are read where they lie,
-      // by their own CTA's tensor core, so nothing has to become visible outside the CTA
-      // (a release over the cluster for each stage takes twice the time: 69 us, not 35).
+      // (what threads write to shared memory is ordered before the products by the proxy fence)
       if (elect_one()) {
         bool ok = true;
         int s = 0, use = 0;
@@ -967,7 +988,7 @@ __global__ void __launch_bounds__(PairKind<kWhat, kGather, kF32, kPre>::kThreads
           for (int kt = 0; kt < steps; ++kt) {
             if (!(ok = mbar_wait_poll(&sm.landed[s], use & 1, abort_flag))) break;
             fence_proxy_async_smem();
-            mbar_arrive_cluster(dsmem_addr(smem_u32(&sm.full[s]), 0));
+            hand_over(sm, rank, s);
             if (++s == kStages) {
               s = 0;
               ++use;

@@ -505,6 +505,15 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
       : "memory");
 }
 
+// 16 bytes from this CTA's shared memory to another CTA's of the cluster, completed on a barrier
+// there (`dst` and `bar` in the cluster's shared window).
+__device__ __forceinline__ void bulk_copy16_cluster(uint32_t dst, uint32_t src, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], 16, [%2];" ::"r"(dst),
+      "r"(src), "r"(bar)
+      : "memory");
+}
+
 // Tiled copies from shared memory, in groups of the issuing thread.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
