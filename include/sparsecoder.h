@@ -558,12 +558,13 @@ int sc_expert_route_backward(const sc_expert_route_backward_args* args, void* st
  *          NULL; backward, in [M][K] or NULL.
  * out, dX  [M][N], [M][K]: bf16, or fp32 when out_f32.
  * dW       [E][N][K]: bf16, or fp32 when out_f32, written for every expert (0 for
- *          one without slots); dbias fp32 [E][N] or NULL.
+ *          one without slots); dbias fp32 [E][N] or NULL (summed by 16 slots, by 64
+ *          such sums, then over all).
  * Products of bf16 values, sums in fp32, one rounding at the end.  Two calls with
  * the same arguments give the same bits.
  * GELU(y) = y Phi(y), Phi the normal distribution: before the rounding within
  * (16 + y^2) 2^-24 of itself, GELU' within as much of Phi(y) + |y| Phi'(y), both down
- * to 2^-122 and, for bf16 outputs, to 2^-17 of themselves.  GELU(-inf) = 0; GELU' of an
+ * to 2^-122 and, for bf16 outputs, to 2^-14 of themselves (2^-19 where |y| < 2).  GELU(-inf) = 0; GELU' of an
  * infinity is NaN.
  * N and K: multiples of 8, at most SC_MAX_EXPERT_DIM; M at most 2^31 - 4096; ldx and
  * ldy multiples of 8 below 2^30; every bf16 pointer, out, dX and dW 16-byte aligned.

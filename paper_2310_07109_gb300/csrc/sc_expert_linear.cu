@@ -140,12 +140,13 @@ __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 
 // pairs: the read-back warps bound products with GELU.  Phi(-a) = exp(-a^2 / 2) t P(t),
 // t = 1 / (1 + q a): with exp(a^2 / 2) taken out, what is left is smooth, and a polynomial P
 // has it to a relative precision over 0 .. 14 (least-squares fits, weighted until the largest
-// relative error was least: 1e-7 with eight terms, 5e-6 with six).  An approximation of erf
-// itself has no digits in the tail (x = -5 came 5 % off).  With eight terms GELU is within
-// (16 + x^2) 2^-24 of itself and its slope of Phi + |x| phi, x^2 for the rounded argument
-// of the exponential.  Six (kShort) are for what is rounded to bf16, whose half unit is 400
-// times their error: 16384 slots, 768 -> 1536, GELU and the value before it 45.0 us (45.6
-// with eight), GELU' 46.9 (47.7).
+// relative error was least: 1e-7 with eight terms).  An approximation of erf itself has no
+// digits in the tail (x = -5 came 5 % off).  With eight terms GELU is within (16 + x^2) 2^-24
+// of itself and its slope of Phi + |x| phi, x^2 for the rounded argument of the exponential.
+// Six terms (kShort) are for what is rounded to bf16: 1.1e-6 up to 2, where most arguments
+// lie, growing to 3.3e-5, a sixtieth of bf16's half unit, in the tail (5e-6 throughout moved four
+// times as many values across a rounding boundary).  16384 slots, 768 -> 1536, with the value
+// before GELU 45.9 us, GELU' 46.9; eight terms cost 0.6 and 0.8 more.
 __device__ __forceinline__ float rcp_approx(float x) {
   float y;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -161,17 +162,17 @@ __device__ __forceinline__ float relu_nan(float x) {
 template <bool kShort>
 __device__ __forceinline__ void normal_tail2(uint64_t na, uint64_t& qt, uint64_t& e) {
   float d0, d1, e0, e1;
-  f2_unpack(f2_fma(na, f2_both(kShort ? -0.31f : -0.304f), f2_both(1.f)), d0, d1);
+  f2_unpack(f2_fma(na, f2_both(kShort ? -0.3f : -0.304f), f2_both(1.f)), d0, d1);
   f2_unpack(f2_mul(f2_mul(na, na), f2_both(-0.5f * 1.44269504088896341f)), e0, e1);
   // 1 / d0 and 1 / d1 from one reciprocal
   const uint64_t t = f2_mul(f2_pack(d1, d0), f2_both(rcp_approx(d0 * d1)));
   uint64_t q;
   if constexpr (kShort) {
-    q = f2_fma(f2_both(-0.0739265946f), t, f2_both(0.180442969f));
-    q = f2_fma(q, t, f2_both(0.0157529143f));
-    q = f2_fma(q, t, f2_both(0.133425419f));
-    q = f2_fma(q, t, f2_both(0.120442386f));
-    q = f2_fma(q, t, f2_both(0.123860595f));
+    q = f2_fma(f2_both(-0.0807364211f), t, f2_both(0.226450577f));
+    q = f2_fma(q, t, f2_both(-0.0280712485f));
+    q = f2_fma(q, t, f2_both(0.149643015f));
+    q = f2_fma(q, t, f2_both(0.11254811f));
+    q = f2_fma(q, t, f2_both(0.120165424f));
   } else {
     q = f2_fma(f2_both(0.0366238666f), t, f2_both(-0.154347755f));
     q = f2_fma(q, t, f2_both(0.190593448f));
@@ -341,7 +342,7 @@ __device__ __forceinline__ void drain_wait_pair(uint64_t* bar, uint32_t parity) 
 // cluster, to the product's acquire, and nobody waits for it here.  (An arrival of the CTA's scope
 // alone orders nothing across CTAs; one with a release over the cluster holds its thread
 // for most of a stage: 69 us, not 37, for 16384 slots 768 -> 1536.  GELU and the value before it
-// 46.3 us so, 44.8 with the bare arrival; the weight gradient 47.9 and 47.4.)
+// 45.9 to 46.3 us so, 44.8 with the bare arrival; the weight gradient 47.9 and 47.4.)
 __device__ __forceinline__ void hand_over(PairSmem& sm, int rank, int s) {
   const uint32_t full = dsmem_addr(smem_u32(&sm.full[s]), 0);
   if (rank == 0) {
