@@ -68,8 +68,12 @@ typedef enum {
   SC_ERR_UNSUPPORTED = 2, /* L > SC_MAX_LEN, too many globals, window too wide */
   SC_ERR_CUDA = 3,        /* a CUDA runtime/driver call failed */
   SC_ERR_TIMEOUT = 4,     /* a bounded device-side wait expired (from sc_workspace_status) */
-  SC_ERR_WORKSPACE = 5    /* workspace missing, too small or misaligned */
+  SC_ERR_WORKSPACE = 5,   /* workspace missing, too small or misaligned */
+  SC_ERR_CAPACITY = 6     /* a cache had no room for some tokens (from sc_workspace_status) */
 } sc_status;
+
+/* Types of the 16-bit values of the calls that take either. */
+typedef enum { SC_BF16 = 0, SC_FP16 = 1 } sc_dtype;
 
 /* What decides that a token survives a layer (the value `alpha` of a layer). */
 typedef enum {
@@ -681,6 +685,233 @@ typedef struct {
 
 int sc_expert_combine_backward(const sc_expert_combine_backward_args* args, void* workspace,
                                size_t workspace_bytes, void* stream);
+
+/*
+ * Norm and rotation of query and key heads, in one pass.  A token is a row (b, r)
+ * of a [B][L] batch, number t = b L + r, in use when r < rows[b] (rows == NULL: all);
+ * its position is p = pos[t] (pos == NULL: r).  For every head x of d features:
+ *   y = x / sqrt(mean(x^2) + eps) * gamma      (gamma == NULL: y = x)
+ *   out_i, out_i' = mscale (y_i cos a - y_i' sin a, y_i' cos a + y_i sin a),
+ *                   a = p freq[m], for the rot / 2 pairs m of the first rot features:
+ *                   (i, i') = (m, m + rot / 2), or (2 m, 2 m + 1) when interleaved != 0
+ *   out_i = y_i for i >= rot
+ * Angles are exact to 2^-20 for every 32-bit position and freq up to 1, all else is
+ * computed in fp32 and rounded once.
+ *
+ * Q, K      dtype (sc_dtype): token t's Hq (Hk) heads of d at t ldq (t ldk), one behind
+ *           the other: slices of one projection's output will do.  Hq or Hk may be 0 (its
+ *           pointers are then not used).
+ * gamma_q, gamma_k  fp32 [d], each may be NULL.
+ * freq      double [rot / 2], radians a position; finite.  Scaled forms for long contexts are
+ *           other frequencies and mscale.  Not used when rot is 0.
+ * Q_out, K_out  as Q and K; may be Q and K themselves (with their distances).
+ * d: a multiple of 16 up to SC_MAX_HEAD_WIDTH; rot: a multiple of 16, 0 to d; distances
+ * multiples of 8 below 2^30; 16-bit pointers 16-byte aligned, freq 8-byte aligned;
+ * B L <= 2^31 - 4096; Hq + Hk <= SC_MAX_HEADS.  Rows not in use are neither read nor written.
+ */
+#define SC_MAX_HEAD_WIDTH 256
+#define SC_MAX_HEADS 1024
+typedef struct {
+  int B, L, Hq, Hk, d, dtype;
+  const void* Q;
+  long long ldq;
+  const void* K;
+  long long ldk;
+  const int32_t* rows;
+  const int32_t* pos;
+  const float* gamma_q;
+  const float* gamma_k;
+  float eps;
+  int rot;
+  int interleaved;
+  const double* freq;
+  float mscale;
+  void* Q_out;
+  long long ldq_out;
+  void* K_out;
+  long long ldk_out;
+} sc_rotate_args;
+
+int sc_rotate_forward(const sc_rotate_args* args, void* stream);
+
+/*
+ * Its gradients: dQ, dK from dQ_out, dK_out (all dtype; tokens ldq, ... elements apart), and
+ * dgamma_q, dgamma_k, fp32 [d] (NULL exactly when gamma_q, gamma_k is): the sums over all tokens in
+ * use and all heads, taken in a fixed order.  Q, K: the forward call's inputs, used only where
+ * there is a norm.  dQ, dK may be dQ_out, dK_out themselves (with their distances).
+ */
+typedef struct {
+  int B, L, Hq, Hk, d, dtype;
+  const void* dQ_out;
+  long long ldq_out;
+  const void* dK_out;
+  long long ldk_out;
+  const void* Q;
+  long long ldq;
+  const void* K;
+  long long ldk;
+  const int32_t* rows;
+  const int32_t* pos;
+  const float* gamma_q;
+  const float* gamma_k;
+  float eps;
+  int rot;
+  int interleaved;
+  const double* freq;
+  float mscale;
+  void* dQ;
+  long long ldq_grad;
+  void* dK;
+  long long ldk_grad;
+  float* dgamma_q;
+  float* dgamma_k;
+} sc_rotate_backward_args;
+
+/* Bytes of workspace sc_rotate_backward needs (256-byte aligned, zeroed once; 0 on an
+ * invalid width). */
+size_t sc_rotate_workspace_size(int d);
+
+int sc_rotate_backward(const sc_rotate_backward_args* args, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * A pruned key-value cache: the method for tokens that come one or a few at a time.
+ * Every step appends its keys and values, attends over the cache, adds the weights
+ * of that attention up for each slot (the vertical sums of Sec. "Pruning", over query
+ * rows and heads), and evicts the slots with the least when a list grows past its budget.
+ *
+ * K, V      dtype: slot c of head h of sequence b has its d values at b stride_b + h stride_h +
+ *           c stride_c (elements; the same for K and V).
+ * G         lists of slots a sequence; it divides Hk.  List g has the heads g Hk / G ..
+ *           (g + 1) Hk / G - 1 of K and V, which keep and drop slots together (G = 1: all
+ *           heads, G = Hk: each head for itself).
+ * acc       fp32 [B][G][C]: the accumulated weight of each slot.
+ * pos       int32 [B][G][C]: the position of the token in each slot.  Slots come in no order.
+ * len       int32 [B][G]: slots in use, the first ones (held within 0 .. C).
+ * seen      int32 [B]: positions given out so far.
+ * Slots from len on are not read; the calls write to them only what their text says.  A NaN or
+ * infinity in a slot in use may reach rows that do not see it.
+ * H a multiple of Hk; d 64 or 128 (sc_cache_append and sc_cache_evict: as sc_rotate_forward);
+ * C at most SC_MAX_CACHE; strides multiples of 8 and at least d; K, V 16-byte aligned.
+ * Every call takes a workspace of sc_cache_workspace_size() bytes (256-byte aligned, zeroed
+ * once).  One serves all calls of one stream; calls that overlap need one each.
+ */
+#define SC_MAX_CACHE 262144
+#define SC_MAX_STEP 4096 /* most tokens a sequence of one sc_cache_attend */
+
+/* T: most tokens a sequence that one sc_cache_attend brings.  0 on invalid sizes. */
+size_t sc_cache_workspace_size(int B, int C, int H, int Hk, int G, int d, int T);
+
+/*
+ * Appends up to L tokens a sequence: token (b, r) in use (r < rows[b]; rows == NULL: all L) has
+ * position p = seen[b] + r and goes to slot len[b][g] + r of each list, where its acc is set to 0.
+ * Q and K are normed and rotated as by sc_rotate_forward, V is copied:
+ *   Q_out[t] = rotated Q[t];  K[slot] = rotated K_in[t];  V[slot] = V_in[t]
+ *   len_out = len + rows;  seen_out = seen + rows
+ * Tokens beyond slot C - 1 are not stored (len_out stops at C), and sc_workspace_status
+ * reports SC_ERR_CAPACITY.
+ * Q, V_in, K_in   distances ldq, ldk, ldv as in sc_rotate_args; H may be 0 (no queries).
+ * Q_out     may be Q.  len_out, seen_out may be len, seen.
+ */
+typedef struct {
+  int B, C, H, Hk, G, d, dtype;
+  void* K;
+  void* V;
+  long long stride_b, stride_h, stride_c;
+  float* acc;
+  int32_t* pos;
+  const int32_t* len;
+  const int32_t* seen;
+  int L;
+  const void* Q;
+  long long ldq;
+  const void* K_in;
+  long long ldk;
+  const void* V_in;
+  long long ldv;
+  const int32_t* rows;
+  const float* gamma_q;
+  const float* gamma_k;
+  float eps;
+  int rot;
+  int interleaved;
+  const double* freq;
+  float mscale;
+  void* Q_out;
+  long long ldq_out;
+  int32_t* len_out;
+  int32_t* seen_out;
+} sc_cache_append_args;
+
+int sc_cache_append(const sc_cache_append_args* args, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * Attention of the newest tokens over the cache.  Row r < rows[b] (rows == NULL: all T) of sequence
+ * b has position p = seen[b] - rows[b] + r (of what sc_cache_append just appended) and sees the
+ * slots in use with 0 <= pos <= p.  Head h reads head h Hk / H of K and V:
+ *   P_h[r] = softmax of scale q . k over the slots it sees;  O_h[r] = sum_c P_h[r][c] v_c
+ *   acc_out[c] = decay acc[c] + sum_r mean_h P_h[r][c]     (c < len; h over the list's H / G heads)
+ * A row that sees no slot has O = 0 and adds nothing.  Sequences without rows in use keep their acc.
+ * Q, O      dtype: row b T + r has its H heads at ldq, ldo times its number.
+ * acc_out   fp32 [B][G][C], may be acc.
+ * scale     finite; T at most SC_MAX_STEP.  Scores, weights and sums in fp32; the weights are
+ *           rounded to dtype for their product with V.  Two calls with the same
+ *           arguments give the same bits.
+ */
+typedef struct {
+  int B, C, H, Hk, G, d, dtype;
+  const void* K;
+  const void* V;
+  long long stride_b, stride_h, stride_c;
+  const float* acc;
+  const int32_t* pos;
+  const int32_t* len;
+  const int32_t* seen;
+  int T;
+  const void* Q;
+  long long ldq;
+  const int32_t* rows;
+  float scale;
+  float decay;
+  void* O;
+  long long ldo;
+  float* acc_out;
+} sc_cache_attend_args;
+
+int sc_cache_attend(const sc_cache_attend_args* args, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * Eviction.  A list with n = len > budget + slack slots in use is brought down to budget; the
+ * others stay as they are.  Slots rank by: protected ones first (pos < sinks, or pos >= seen -
+ * recent), then by acc, the largest first (a NaN, or a slot whose pos is below 0, last); ties to the lower slot.  The budget best
+ * survive.  Those in slots below budget stay where they are; the others fill, in order, the
+ * places that are free below budget (K, V, acc and pos; no more rows than these move).
+ *   len_out = budget, or len;  acc_out, pos_out: the first len_out slots
+ * acc_out, pos_out, len_out may be acc, pos, len.  Slots of K and V from len_out on are left as they
+ * were.  budget >= 1, slack, sinks, recent >= 0, sinks + recent <= budget.
+ */
+typedef struct {
+  int B, C, Hk, G, d, dtype;
+  void* K;
+  void* V;
+  long long stride_b, stride_h, stride_c;
+  const float* acc;
+  const int32_t* pos;
+  const int32_t* len;
+  const int32_t* seen;
+  int budget;
+  int slack;
+  int sinks;
+  int recent;
+  float* acc_out;
+  int32_t* pos_out;
+  int32_t* len_out;
+} sc_cache_evict_args;
+
+int sc_cache_evict(const sc_cache_evict_args* args, void* workspace, size_t workspace_bytes,
+                   void* stream);
 
 /* Static, human-readable name of a status code. */
 const char* sc_status_string(int status);

@@ -22,7 +22,7 @@ SC_MAX_LEN = 4096
 SC_MAX_GLOBAL = 16
 SC_MAX_WINDOW = 512
 
-SC_OK, SC_ERR_INVALID_ARG, SC_ERR_UNSUPPORTED, SC_ERR_CUDA, SC_ERR_TIMEOUT, SC_ERR_WORKSPACE = range(6)
+SC_OK, SC_ERR_INVALID_ARG, SC_ERR_UNSUPPORTED, SC_ERR_CUDA, SC_ERR_TIMEOUT, SC_ERR_WORKSPACE, SC_ERR_CAPACITY = range(7)
 
 
 class SparseCoderError(RuntimeError):
@@ -97,7 +97,9 @@ EXPORTED = ["sc_layer_forward", "sc_layer_forward_noalloc", "sc_stack_forward",
             "sc_expert_workspace_size", "sc_expert_route_forward", "sc_expert_route_backward",
             "sc_expert_linear_forward", "sc_expert_linear_backward_input",
             "sc_expert_linear_backward_weight", "sc_expert_combine_forward",
-            "sc_expert_combine_backward"]
+            "sc_expert_combine_backward",
+            "sc_rotate_forward", "sc_rotate_backward", "sc_rotate_workspace_size",
+            "sc_cache_workspace_size", "sc_cache_append", "sc_cache_attend", "sc_cache_evict"]
 
 
 def library_path() -> str:

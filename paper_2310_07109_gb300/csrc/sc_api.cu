@@ -34,6 +34,7 @@ cudaError_t launch_gemm(const GemmParams& p, cudaStream_t st);
 cudaError_t launch_layernorm(const LayerNormParams& p, cudaStream_t st);
 cudaError_t launch_row_gather(const RowGatherParams& p, cudaStream_t st);
 cudaError_t configure_expert();
+cudaError_t configure_cache();
 }  // namespace sc
 
 namespace {
@@ -232,6 +233,7 @@ int ensure_configured() {
     if (e == cudaSuccess) e = configure_tail();
     if (e == cudaSuccess) e = configure_encoder();
     if (e == cudaSuccess) e = configure_expert();
+    if (e == cudaSuccess) e = configure_cache();
     if (e != cudaSuccess) return fail_cuda("kernel attributes", e);
     done[dev] = true;
   }
@@ -380,6 +382,7 @@ const char* sc_status_string(int status) {
     case SC_ERR_CUDA: return "SC_ERR_CUDA: a CUDA call failed";
     case SC_ERR_TIMEOUT: return "SC_ERR_TIMEOUT: a bounded device-side wait expired";
     case SC_ERR_WORKSPACE: return "SC_ERR_WORKSPACE: workspace missing, too small or misaligned";
+    case SC_ERR_CAPACITY: return "SC_ERR_CAPACITY: a cache had no room for some tokens";
     default: return "unknown sparsecoder status";
   }
 }
@@ -1255,7 +1258,7 @@ int sc_workspace_status(void* workspace, size_t ws_bytes, void* stream) {
     return SC_ERR_CUDA;
   if (word == 0) return SC_OK;
   if (cudaMemset(workspace, 0, sizeof(int)) != cudaSuccess) return SC_ERR_CUDA;
-  return (word & kStatusTimeout) ? SC_ERR_TIMEOUT : SC_ERR_CUDA;
+  return (word & kStatusTimeout) ? SC_ERR_TIMEOUT : (word & kStatusFull) ? SC_ERR_CAPACITY : SC_ERR_CUDA;
 }
 
 }  // extern "C"

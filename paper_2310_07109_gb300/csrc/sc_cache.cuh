@@ -1,0 +1,149 @@
+// sc_cache.cuh -- parameter blocks and launchers of the pruned key-value cache (norm
+// and rotation of heads, append, attention with accumulated weights, eviction), and
+// the 16-bit types that its kernels take.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "../../include/sparsecoder.h"
+#include "sm103_primitives.cuh"
+
+namespace sc {
+
+constexpr int kCacheSms = 152;   // what splits and workspaces are sized for
+
+// The two 16-bit types: eight values <-> fp32, and the warp product of their fragments.
+struct Bf16 {
+  static __device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi) {
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
+  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    mma_bf16(c, a, b0, b1);
+  }
+  // The weights' reference lies this far (a power of two) below the largest score.
+  static constexpr float kHeadroom = 0.f;
+};
+
+struct Fp16 {
+  static __device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    lo = f.x;
+    hi = f.y;
+  }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+  // A weight of 2^-24 is fp16's smallest: up to 2^12 instead of 1, so that the many small
+  // weights of a long list keep eleven bits down to 2^-26 of the largest.
+  static constexpr float kHeadroom = 12.f;
+};
+
+// One side of a rotation: heads of all tokens, `ld` elements a token.
+struct HeadsIn {
+  const uint16_t* p;
+  long long ld;
+};
+struct HeadsOut {
+  uint16_t* p;
+  long long ld;
+};
+
+struct RotateParams {
+  int B, L, Hq, Hk, d;
+  long long T;               // B L
+  HeadsIn q, k;              // forward: the heads; backward: the forward call's heads
+  HeadsIn dq, dk;            // backward: gradients of the outputs
+  HeadsOut q_out, k_out;     // the outputs, or the gradients of the inputs
+  const int32_t* rows;       // [B] or nullptr
+  const int32_t* pos;        // [T] or nullptr (the row)
+  const float* gamma_q;      // [d] or nullptr
+  const float* gamma_k;
+  float eps;
+  int rot, interleaved;
+  const double* freq;        // [rot / 2]
+  float mscale;
+  float* dgamma_q;           // [d] or nullptr
+  float* dgamma_k;
+  float* part;               // workspace: [CTAs][2][d]
+  // append: where keys and values go instead of k_out
+  HeadsIn v;
+  uint16_t* cache_k;         // nullptr: not an append
+  uint16_t* cache_v;
+  long long stride_b, stride_h, stride_c;
+  int C, G;
+  float* acc;
+  int32_t* slot_pos;
+  const int32_t* len;
+  const int32_t* seen;
+  int32_t* len_out;
+  int32_t* seen_out;
+  int* status;
+  unsigned* done;            // workspace: CTAs that have read len and seen
+};
+
+constexpr int kRotateMaxParts = 456;   // CTAs of the gradient
+
+struct AttendParams {
+  int B, C, H, Hk, G, T;
+  int R, M;                  // query heads a key head; rows a key head (T R)
+  const uint16_t* k;
+  const uint16_t* v;
+  long long stride_b, stride_h, stride_c;
+  const float* acc;
+  const int32_t* pos;
+  const int32_t* len;
+  const int32_t* seen;
+  const uint16_t* q;
+  long long ldq;
+  const int32_t* rows;       // [B] or nullptr
+  float scale2;              // scale log2(e)
+  float decay;
+  uint16_t* o;
+  long long ldo;
+  float* acc_out;
+  int splits;                // parts of a list that CTAs take
+  float* lse;                // workspace: [B][Hk][M], base 2; +inf: the row adds nothing
+  float2* ml;                // workspace: [B][Hk][splits][M] reference, sum of weights
+  float* part;               // workspace: [B][Hk][splits][M][d]
+};
+
+struct EvictParams {
+  int B, C, Hk, G, d;
+  uint16_t* k;
+  uint16_t* v;
+  long long stride_b, stride_h, stride_c;
+  const float* acc;
+  const int32_t* pos;
+  const int32_t* len;
+  const int32_t* seen;
+  int budget, slack, sinks, recent;
+  float* acc_out;
+  int32_t* pos_out;
+  int32_t* len_out;
+  int32_t* moved;            // workspace: [B][G] rows that move
+  int2* pairs;               // workspace: [B][G][pair_pitch] (to, from)
+  long long pair_pitch;
+};
+
+int api_device_sms();
+cudaError_t configure_attend();
+cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st);
+cudaError_t launch_rotate_back(const RotateParams& p, int dtype, cudaStream_t st);
+cudaError_t launch_attend(const AttendParams& p, int d, int dtype, cudaStream_t st);
+cudaError_t launch_evict(const EvictParams& p, cudaStream_t st);
+
+}  // namespace sc

@@ -23,6 +23,7 @@ constexpr uint32_t kGTileBytes = kMaxGlobal * kHeadDim * 2;
 // status word bits (workspace)
 constexpr int kStatusTimeout = 1;
 constexpr int kStatusInternal = 2;   // an invariant of the launch sequence did not hold
+constexpr int kStatusFull = 4;   // a cache had no room for some tokens
 
 // Sequences with at most kTailMax current tokens run their remaining layers in
 // the cluster kernel (one CTA per head); the per-layer kernels skip them.
