@@ -115,11 +115,23 @@ struct AttendParams {
   uint16_t* o;
   long long ldo;
   float* acc_out;
+  // workspace, many rows
   int splits;                // parts of a list that CTAs take
-  float* lse;                // workspace: [B][Hk][M], base 2; +inf: the row adds nothing
-  float2* ml;                // workspace: [B][Hk][splits][M] reference, sum of weights
-  float* part;               // workspace: [B][Hk][splits][M][d]
+  float* lse;                // [B][Hk][M], base 2; +inf: the row adds nothing
+  // workspace, few rows
+  int warps;                 // at work on the tiles of all lists
+  int* share;                // tiles a warp, then [B][Hk] the first tile of each unit
+  float* scores;             // [B][Hk][M][pitch] scale log2(e) q . k; -inf: not seen
+  int pitch;
+  // both: parts (many rows: [B][Hk][splits]; few: a warp's number + a unit's)
+  float2* ml;                // [part][M] reference, sum of weights
+  float* part;               // [part][M][d]
 };
+
+constexpr int kFewRows = 16;                 // most rows a key head that the kernel for few rows takes
+constexpr int kFewTile = 16;                 // slots a warp takes at a time
+constexpr int kFewMinTiles = 2;              // fewest tiles of a warp
+constexpr int few_warps_sm(int d) { return d == 64 ? 12 : 8; }
 
 struct EvictParams {
   int B, C, Hk, G, d;

@@ -18,7 +18,7 @@ using namespace sc;
 
 constexpr size_t kAlign = 256;
 constexpr long long kMaxTokens = (1ll << 31) - 4096;
-constexpr int kRowsTile = 64, kKeysTile = 64;   // of the attention kernels
+constexpr int kRowsTile = 64;   // of the attention kernels
 
 size_t align_up(size_t x) { return (x + kAlign - 1) & ~(kAlign - 1); }
 bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -52,8 +52,8 @@ int check_rotate(int B, int L, int Hq, int Hk, int d, int dtype, const int32_t* 
 }
 
 struct CacheLayout {
-  size_t lse, ml, part, moved, pairs, total;
-  int splits;
+  size_t lse, share, scores, ml, part, moved, pairs, total;
+  int splits, warps, pitch;
   long long pair_pitch;
 };
 
@@ -68,12 +68,21 @@ int splits_of(int B, int C, int Hk, int M) {
 // the next one of its stream starts, so they share the space).
 CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   CacheLayout w;
-  const size_t rows = static_cast<size_t>(B) * H * T, lists = static_cast<size_t>(B) * G;
-  w.splits = splits_of(B, C, Hk, T * (H / Hk));
-  w.lse = kAlign;
-  w.ml = align_up(w.lse + sizeof(float) * rows);
-  w.part = align_up(w.ml + sizeof(float2) * rows * w.splits);
-  const size_t attend = align_up(w.part + sizeof(float) * rows * w.splits * d);
+  const size_t units = static_cast<size_t>(B) * Hk, lists = static_cast<size_t>(B) * G;
+  const size_t M = static_cast<size_t>(T) * (H / Hk);
+  const bool few = M <= kFewRows;
+  // no more warps than the most tiles give work to
+  w.splits = few ? 1 : splits_of(B, C, Hk, static_cast<int>(M));
+  const size_t tiles = units * ((C + kFewTile - 1) / kFewTile);
+  const size_t cta = kFewMinTiles * few_warps_sm(d);   // fewest tiles of a CTA
+  w.warps = static_cast<int>(std::min<size_t>(kCacheSms, (tiles + cta - 1) / cta)) * few_warps_sm(d);
+  w.pitch = (C + 3) & ~3;
+  const size_t parts = few ? w.warps + units : units * w.splits;
+  w.lse = w.share = kAlign;
+  w.scores = align_up(w.share + sizeof(int) * (1 + units));
+  w.ml = few ? align_up(w.scores + sizeof(float) * units * M * w.pitch) : align_up(w.lse + sizeof(float) * units * M);
+  w.part = align_up(w.ml + sizeof(float2) * parts * M);
+  const size_t attend = align_up(w.part + sizeof(float) * parts * M * d);
   w.pair_pitch = C / 2 + 1;
   w.moved = kAlign;
   w.pairs = align_up(w.moved + sizeof(int32_t) * lists);
@@ -85,7 +94,7 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
 int check_cache_sizes(int B, int C, int H, int Hk, int G, int d) {
   if (B < 1 || C < 1 || H < 0 || Hk < 1 || G < 1 || Hk % G || H % Hk || d < 16 || d % 16) return SC_ERR_INVALID_ARG;
   if (C > SC_MAX_CACHE || d > SC_MAX_HEAD_WIDTH || static_cast<long long>(H) + Hk > SC_MAX_HEADS ||
-      static_cast<long long>(B) * Hk * ((C + kKeysTile - 1) / kKeysTile) > kMaxTokens)
+      static_cast<long long>(B) * Hk * ((C + kFewTile - 1) / kFewTile) > kMaxTokens)
     return SC_ERR_UNSUPPORTED;
   return SC_OK;
 }
@@ -225,9 +234,11 @@ extern "C" int sc_cache_attend(const sc_cache_attend_args* a, void* workspace, s
   p.scale2 = static_cast<float>(static_cast<double>(a->scale) * 1.4426950408889634);   // log2(e)
   p.decay = a->decay;
   p.o = static_cast<uint16_t*>(a->O); p.ldo = a->ldo; p.acc_out = a->acc_out;
-  p.splits = w.splits;
+  p.splits = w.splits; p.warps = w.warps; p.pitch = w.pitch;
   char* ws = static_cast<char*>(workspace);
   p.lse = reinterpret_cast<float*>(ws + w.lse);
+  p.share = reinterpret_cast<int*>(ws + w.share);
+  p.scores = reinterpret_cast<float*>(ws + w.scores);
   p.ml = reinterpret_cast<float2*>(ws + w.ml);
   p.part = reinterpret_cast<float*>(ws + w.part);
   const cudaError_t e = launch_attend(p, a->d, a->dtype, static_cast<cudaStream_t>(stream));

@@ -386,11 +386,481 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
   }
 }
 
+// ---------------------------------------------------------------------------
+// few rows: a warp's tiles
+// ---------------------------------------------------------------------------
+// A unit is a key head of a sequence.  The tiles of all units, one behind the other, are dealt out to the warps in
+// equal runs, whatever the lengths of the lists; a warp's piece of a unit has the number warp + unit, which no
+// other has (from a piece to the next one, at least one of the two goes up).
+__device__ __forceinline__ int list_tiles(const AttendParams& p, int list) {
+  const int rows = p.rows != nullptr ? __ldg(p.rows + list / p.G) : p.T;
+  const int n = min(max(__ldg(p.len + list), 0), p.C);
+  return rows > 0 ? (n + kFewTile - 1) / kFewTile : 0;
+}
+
+// Where a warp's run is: list, head of the list, tile of the head.
+struct Cursor {
+  int list, head, tile, tiles;
+};
+
+__device__ __forceinline__ void next_list(const AttendParams& p, Cursor& c) {
+  const int lists = p.B * p.G;
+  c.head = c.tile = 0;
+  do {
+    ++c.list;
+    c.tiles = c.list < lists ? list_tiles(p, c.list) : 1;
+  } while (c.tiles == 0);
+}
+
+__device__ __forceinline__ void advance(const AttendParams& p, int of, Cursor& c) {
+  if (++c.tile < c.tiles) return;
+  c.tile = 0;
+  if (++c.head == of) next_list(p, c);
+}
+
+template <int D>
+struct FewShape {
+  static constexpr int kStages = D == 64 ? 4 : 3;
+  static constexpr int kTileBytes = kFewTile * D * 2;
+  static constexpr int kStageBytes = 2 * kTileBytes + kFewTile * 4;
+  static constexpr int kWarpBytes = kStages * kStageBytes;
+  static constexpr int kWarps = few_warps_sm(D);     // a CTA, which has an SM to itself
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kPitch = D + 8;               // floats of a row of O in shared memory: rows in different banks
+  static constexpr int kBytes = kWarps * kWarpBytes + 128;
+};
+static_assert(FewShape<64>::kWarpBytes >= kFewRows * FewShape<64>::kPitch * 4 && FewShape<64>::kBytes <= 230000 &&
+              FewShape<128>::kWarpBytes >= kFewRows * FewShape<128>::kPitch * 4 && FewShape<128>::kBytes <= 230000,
+              "a warp's stages hold its O, and an SM the stages");
+
+template <class T, int D>
+__global__ void __launch_bounds__(FewShape<D>::kThreads, 1) attend_few_kernel(const AttendParams p) {
+  using S = FewShape<D>;
+  extern __shared__ char raw[];
+  __shared__ int units[S::kWarps];
+  __shared__ float2 ends[S::kWarps][kFewRows];   // reference and sum of the rows of each warp's last piece
+  const int lane = threadIdx.x & 31, me = threadIdx.x >> 5, warp = blockIdx.x * S::kWarps + me;
+  const uint32_t all = (smem_u32(raw) + 127) & ~127u, mine = all + me * S::kWarpBytes;
+  char* own = raw + (mine - smem_u32(raw));
+  pdl_wait();
+  pdl_launch_dependents();
+  const int of = p.Hk / p.G, lists = p.B * p.G;
+  // the run: all tiles, then the list in which it starts
+  int total = 0;
+  for (int i = lane; i < lists; i += 32) total += list_tiles(p, i);
+  total = __reduce_add_sync(0xffffffffu, total) * of;
+  const int share = max(kFewMinTiles, (total + p.warps - 1) / p.warps);
+  if (warp == 0 && lane == 0) p.share[0] = share;
+  const int from = min(warp * share, total), count = min(share, total - from);
+  Cursor at{};
+  if (count > 0) {
+    int before = 0;   // tiles of the lists before i
+    for (int i = 0;; i += 32) {
+      const int t = i + lane < lists ? list_tiles(p, i + lane) * of : 0;
+      int upto = t;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const unsigned there = __ballot_sync(0xffffffffu, before + upto > from);
+      if (there != 0) {
+        const int l = __ffs(there) - 1;
+        const int tiles = __shfl_sync(0xffffffffu, t, l) / of;
+        const int rest = from - before - (__shfl_sync(0xffffffffu, upto, l) - tiles * of);
+        at.list = i + l;
+        at.tiles = tiles;
+        at.head = rest / tiles;
+        at.tile = rest - at.head * tiles;
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+  }
+  Cursor ahead = at;
+  int to_load = count, loaded = 0;
+  // this lane's chunks of a tile: rows lane / (D / 8) + ..., chunk lane % (D / 8)
+  constexpr int kLanesRow = D / 8, kRowsOnce = 32 / kLanesRow;
+  const int row0 = lane / kLanesRow, chunk = lane % kLanesRow;
+  auto load = [&]() {
+    if (to_load > 0) {
+      const int b = ahead.list / p.G, g = ahead.list - b * p.G, hk = g * of + ahead.head;
+      const int n = min(__ldg(p.len + ahead.list), p.C), j0 = ahead.tile * kFewTile;
+      const uint32_t base = mine + (loaded % S::kStages) * S::kStageBytes;
+      const long long head = b * p.stride_b + hk * p.stride_h + j0 * p.stride_c + chunk * 8;
+#pragma unroll
+      for (int i = 0; i < kFewTile / kRowsOnce; ++i) {
+        const int row = row0 + i * kRowsOnce;
+        const bool live = j0 + row < n;
+        const long long off = live ? head + row * p.stride_c : 0;
+        cp_async16(chunk_at<D>(base, row, chunk), p.k + off, live);
+        cp_async16(chunk_at<D>(base + S::kTileBytes, row, chunk), p.v + off, live);
+      }
+      if (lane < kFewTile) {
+        const bool live = j0 + lane < n;
+        cp_async4(base + 2 * S::kTileBytes + lane * 4, p.pos + static_cast<long long>(ahead.list) * p.C + (live ? j0 + lane : 0), live);
+      }
+      --to_load;
+      ++loaded;
+      advance(p, of, ahead);
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < S::kStages - 1; ++i) load();
+
+  uint32_t q[D / 16][4];
+  float o[D / 8][4], ref[2], sum[2];
+  int seen_to[2], last = 0, unit = -1, n = 0, rows_m = 0;
+  bool fresh = true;
+  for (int step = 0; step < count; ++step) {
+    if (fresh) {
+      fresh = false;
+      const int b = at.list / p.G, g = at.list - b * p.G, hk = g * of + at.head;
+      const ListOf l = list_of(p, b, g);
+      unit = b * p.Hk + hk;
+      n = l.n;
+      rows_m = l.rows * p.R;
+      last = l.first + l.rows - 1;
+      if (at.tile == 0 && lane == 0) p.share[1 + unit] = from + step;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int m = (lane >> 2) + 8 * u, tok = m / p.R;
+        seen_to[u] = l.first + tok;
+        const bool live = m < rows_m;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(
+            p.q + (static_cast<long long>(b) * p.T + (live ? tok : 0)) * p.ldq + (hk * p.R + (live ? m % p.R : 0)) * D) + (lane & 3);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          q[k][u] = live ? __ldg(src + 8 * k) : 0u;
+          q[k][2 + u] = live ? __ldg(src + 8 * k + 4) : 0u;
+        }
+        ref[u] = -INFINITY;
+        sum[u] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
+    }
+    load();
+    cp_async_wait<S::kStages - 1>();
+    const uint32_t sk = mine + (step % S::kStages) * S::kStageBytes, sv = sk + S::kTileBytes;
+    char* stage = own + (step % S::kStages) * S::kStageBytes;
+    const int j0 = at.tile * kFewTile;
+    // a slot that no row sees may hold anything: its V is taken as 0
+    bool unseen = false;
+    if (lane < kFewTile) {
+      const int where = reinterpret_cast<const int*>(stage + 2 * S::kTileBytes)[lane];
+      unseen = j0 + lane < n && (where < 0 || where > last);
+    }
+    __syncwarp();
+    const unsigned blank = __ballot_sync(0xffffffffu, unseen);
+    if (blank != 0) {
+      for (int r = 0; r < kFewTile; ++r)
+        if (blank >> r & 1u && lane < D / 8) *reinterpret_cast<uint4*>(stage + S::kTileBytes + r * D * 2 + lane * 16) = make_uint4(0, 0, 0, 0);
+      __syncwarp();
+    }
+    float c[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      uint32_t f[4];
+      load_b<D>(sk, 0, k, lane, f);
+      T::mma(c[0], q[k], f[0], f[1]);
+      T::mma(c[1], q[k], f[2], f[3]);
+    }
+    float top[2] = {ref[0], ref[1]};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int key = 8 * i + 2 * (lane & 3);
+      const int2 where = *reinterpret_cast<const int2*>(stage + 2 * S::kTileBytes + key * 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int w = k & 1 ? where.y : where.x;
+        const bool sees = j0 + key + (k & 1) < n && w >= 0 && w <= seen_to[k >> 1];
+        c[i][k] = sees ? c[i][k] * p.scale2 : -INFINITY;
+        top[k >> 1] = fmaxf(top[k >> 1], c[i][k] - T::kHeadroom);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int m = (lane >> 2) + 8 * u;
+        if (m < rows_m && j0 + key < n)   // (pitch is even: the second slot has room)
+          *reinterpret_cast<float2*>(p.scores + (static_cast<long long>(unit) * p.M + m) * p.pitch + j0 + key) =
+              make_float2(c[i][2 * u], c[i][2 * u + 1]);
+      }
+    }
+    bool moved = false;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 1));
+      top[u] = fmaxf(top[u], __shfl_xor_sync(0xffffffffu, top[u], 2));
+      moved |= top[u] != ref[u];
+    }
+    if (__any_sync(0xffffffffu, moved)) {
+      float keep[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        keep[u] = top[u] == ref[u] ? 1.f : ex2(ref[u] - top[u]);   // (both -inf: nothing so far)
+        ref[u] = top[u];
+        sum[u] *= keep[u];
+      }
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        o[i][0] *= keep[0];
+        o[i][1] *= keep[0];
+        o[i][2] *= keep[1];
+        o[i][3] *= keep[1];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) top[u] = ref[u] == -INFINITY ? 0.f : ref[u];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) c[i][k] = ex2(c[i][k] - top[k >> 1]);
+      sum[0] += c[i][0] + c[i][1];
+      sum[1] += c[i][2] + c[i][3];
+    }
+    const uint32_t a[4] = {T::pack(c[0][0], c[0][1]), T::pack(c[0][2], c[0][3]), T::pack(c[1][0], c[1][1]), T::pack(c[1][2], c[1][3])};
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      uint32_t f[4];
+      load_v<D>(sv, 0, i, lane, f);
+      T::mma(o[2 * i], a, f[0], f[1]);
+      T::mma(o[2 * i + 1], a, f[2], f[3]);
+    }
+    __syncwarp();   // the stage is free
+    const int was_list = at.list, was_head = at.head;
+    advance(p, of, at);
+    if (step + 1 == count || (at.list == was_list && at.head == was_head)) continue;
+    // the unit goes on in other warps at most: what this one has of it
+    fresh = true;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
+      sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
+      const int m = (lane >> 2) + 8 * u;
+      if (m >= rows_m) continue;
+      const long long at_row = (static_cast<long long>(warp) + unit) * p.M + m;
+      if ((lane & 3) == 0) p.ml[at_row] = make_float2(ref[u], sum[u]);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        *reinterpret_cast<float2*>(p.part + at_row * D + 8 * i + 2 * (lane & 3)) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
+    }
+  }
+  // The warps' last pieces, joined where neighbours have the same unit: the first of them writes one piece, the
+  // others' are empty.
+  cp_async_wait_all();   // (none is left but empty groups)
+  if (unit >= 0) {
+    float* mo = reinterpret_cast<float*>(own);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
+      sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
+      const int m = (lane >> 2) + 8 * u;
+      if ((lane & 3) == 0) ends[me][m] = make_float2(ref[u], sum[u]);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        *reinterpret_cast<float2*>(mo + m * S::kPitch + 8 * i + 2 * (lane & 3)) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
+    }
+  }
+  if (lane == 0) units[me] = unit;
+  __syncthreads();
+  if (unit < 0) return;
+  int w0 = me, w1 = me + 1;
+  while (w0 > 0 && units[w0 - 1] == unit) --w0;
+  while (w1 < S::kWarps && units[w1] == unit) ++w1;
+  for (int m = lane; m < rows_m; m += 32)
+    if (me != w0) p.ml[(static_cast<long long>(warp) + unit) * p.M + m] = make_float2(-INFINITY, 0.f);
+  const float* first = reinterpret_cast<const float*>(raw + (all - smem_u32(raw)));
+  const long long to_row = (static_cast<long long>(blockIdx.x) * S::kWarps + w0 + unit) * p.M;
+  for (int e = (me - w0) * 32 + lane; e < rows_m * (D / 4); e += (w1 - w0) * 32) {
+    const int m = e / (D / 4), c = e % (D / 4) * 4;
+    float top = -INFINITY, total = 0.f;
+    for (int w = w0; w < w1; ++w) top = fmaxf(top, ends[w][m].x);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = w0; w < w1; ++w) {
+      const float2 end = ends[w][m];
+      const float k = end.x == top ? 1.f : end.x == -INFINITY && end.y == 0.f ? 0.f : ex2(end.x - top);
+      const float4 f = *reinterpret_cast<const float4*>(first + w * (S::kWarpBytes / 4) + m * S::kPitch + c);
+      v.x += k * f.x;
+      v.y += k * f.y;
+      v.z += k * f.z;
+      v.w += k * f.w;
+      total += k * end.y;
+    }
+    *reinterpret_cast<float4*>(p.part + (to_row + m) * D + c) = v;
+    if (c == 0) p.ml[to_row + m] = make_float2(top, total);
+  }
+}
+
+// The warps that have parts of a unit: all that write one in its first and its last CTA, and the first of each CTA in
+// between, which has the unit in all its warps.
+template <int kWarps>
+struct Pieces {
+  int unit, w0, first, between, count;
+  __device__ __forceinline__ Pieces(int unit_, int n, int share, int from) : unit(unit_) {
+    const int tiles = (n + kFewTile - 1) / kFewTile;
+    if (tiles == 0) {
+      w0 = first = between = count = 0;
+      return;
+    }
+    w0 = from / share;
+    const int w1 = (from + tiles - 1) / share, c0 = w0 / kWarps, c1 = w1 / kWarps;
+    first = min(w1, c0 * kWarps + kWarps - 1) - w0 + 1;
+    between = c1 > c0 ? c1 - c0 - 1 : 0;
+    count = first + between + (c1 > c0 ? w1 - c1 * kWarps + 1 : 0);
+  }
+  // the number of part i
+  __device__ __forceinline__ long long at(int i) const {
+    const int c = w0 / kWarps + 1;   // the CTA after the first
+    const int w = i < first ? w0 + i : i < first + between ? (c + i - first) * kWarps : (c + between) * kWarps + i - first - between;
+    return static_cast<long long>(w) + unit;
+  }
+};
+
+// The first `row_ctas` CTAs join a row each; the others have kSumSlots slots of a list each, whose weights
+// they add up over the list's rows from the scores and the rows' LSE.
+constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32;
+constexpr int kSumSlots = kSumThreads * 2;
+constexpr int kSumRows = kSumThreads / 8;   // rows whose LSE are found at once, by eight lanes each
+template <class T, int D>
+__global__ void __launch_bounds__(kSumThreads) attend_few_join_kernel(const AttendParams p, int row_ctas) {
+  using Parts = Pieces<FewShape<D>::kWarps>;
+  constexpr int kOwn = D / 32;
+  __shared__ float part[kSumWarps][D];
+  __shared__ float2 ends[kSumWarps];
+  __shared__ float lse[kSumRows];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int share = __ldcg(p.share);
+  if (static_cast<int>(blockIdx.x) < row_ctas) {
+    const int unit = static_cast<int>(blockIdx.x) / p.M, m = static_cast<int>(blockIdx.x) - unit * p.M;
+    const int b = unit / p.Hk, hk = unit - b * p.Hk, from = __ldcg(p.share + 1 + unit);
+    const ListOf l = list_of(p, b, hk / (p.Hk / p.G));
+    if (m >= l.rows * p.R) return;
+    const Parts ps(unit, l.n, share, from);
+    float ref = -INFINITY, total = 0.f, o[kOwn] = {};
+    // eight parts a warp at a time
+    for (int s0 = warp * 8; s0 < ps.count; s0 += kSumWarps * 8) {
+      const int s = s0 + (lane & 7);
+      const float2 ml = s < ps.count ? p.ml[ps.at(s) * p.M + m] : make_float2(-INFINITY, 0.f);
+      const bool some = ml.x != -INFINITY || ml.y != 0.f;   // (nothing but NaN: the sum is one)
+      const unsigned have = __ballot_sync(0xffffffffu, some) & 0xffu;
+      float2 f[8][kOwn / 2];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int i = 0; i < kOwn; i += 2)
+          f[u][i / 2] = have >> u & 1u ? *reinterpret_cast<const float2*>(p.part + (ps.at(s0 + u) * p.M + m) * D + lane * kOwn + i)
+                                       : make_float2(0.f, 0.f);
+      float top = fmaxf(ref, ml.x);
+#pragma unroll
+      for (int i = 4; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+      const float w = !some ? 0.f : ml.x == top ? 1.f : ex2(ml.x - top);
+      const float keep = ref == top ? 1.f : ex2(ref - top);
+      ref = top;
+      total = total * keep + (some ? w * ml.y : 0.f);   // of the parts lane & 7, + 8 ..
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) o[i] *= keep;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float wu = __shfl_sync(0xffffffffu, w, u);
+#pragma unroll
+        for (int i = 0; i < kOwn; i += 2) {
+          o[i] += wu * f[u][i / 2].x;
+          o[i + 1] += wu * f[u][i / 2].y;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 4; i > 0; i >>= 1) total += __shfl_xor_sync(0xffffffffu, total, i);
+    if (lane == 0) ends[warp] = make_float2(ref, total);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) part[warp][lane * kOwn + i] = o[i];
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) >= D / 2) return;
+    float top = -INFINITY, sum = 0.f, v[2] = {0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kSumWarps; ++w) top = fmaxf(top, ends[w].x);
+#pragma unroll
+    for (int w = 0; w < kSumWarps; ++w) {
+      const float2 end = ends[w];
+      const float k = end.x == top ? 1.f : end.x == -INFINITY && end.y == 0.f ? 0.f : ex2(end.x - top);
+      sum += k * end.y;
+      v[0] += k * part[w][2 * threadIdx.x];
+      v[1] += k * part[w][2 * threadIdx.x + 1];
+    }
+    const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+    reinterpret_cast<uint32_t*>(p.o + (static_cast<long long>(b) * p.T + m / p.R) * p.ldo +
+                                static_cast<long long>(hk * p.R + m % p.R) * D)[threadIdx.x] = T::pack(v[0] * inv, v[1] * inv);
+    return;
+  }
+  const int chunks = (p.C + kSumSlots - 1) / kSumSlots, id = blockIdx.x - row_ctas;
+  const int list = id / chunks, b = list / p.G, g = list - b * p.G, of = p.Hk / p.G, unit0 = b * p.Hk + g * of;
+  const ListOf l = list_of(p, b, g);
+  const int j0 = (id - list * chunks) * kSumSlots, j = j0 + static_cast<int>(threadIdx.x) * 2;
+  if (j0 >= l.n) return;
+  const int rows_m = l.rows * p.R, rows = of * rows_m;
+  const long long at = static_cast<long long>(list) * p.C + j;
+  float old[2] = {}, sum[2] = {};
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (j + i < l.n) old[i] = p.acc[at + i];
+  for (int r0 = 0; r0 < rows; r0 += kSumRows) {
+    const int here = min(kSumRows, rows - r0), i = threadIdx.x / 8;
+    const int h = r0 / rows_m, m0 = r0 - h * rows_m;
+    __syncthreads();
+    // (whole warps: four rows each)
+    const int mine = m0 + min(i, here - 1), hi = mine / rows_m, unit = unit0 + h + hi;
+    const Parts ps(unit, l.n, share, __ldcg(p.share + 1 + unit));
+    float ref = -INFINITY, total = 0.f;
+    for (int s0 = lane & 7; s0 < ps.count; s0 += 32) {
+      float2 ml[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        ml[u] = s0 + 8 * u < ps.count ? p.ml[ps.at(s0 + 8 * u) * p.M + mine - hi * rows_m] : make_float2(-INFINITY, 0.f);
+      const float top = fmaxf(fmaxf(fmaxf(ref, ml[0].x), fmaxf(ml[1].x, ml[2].x)), ml[3].x);
+      total *= ref == top ? 1.f : ex2(ref - top);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (ml[u].x != -INFINITY || ml[u].y != 0.f) total += ml[u].y * (ml[u].x == top ? 1.f : ex2(ml[u].x - top));
+      ref = top;
+    }
+    float top = ref;
+#pragma unroll
+    for (int k = 4; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    if (ref != top && (ref != -INFINITY || total != 0.f)) total *= ex2(ref - top);
+#pragma unroll
+    for (int k = 4; k > 0; k >>= 1) total += __shfl_xor_sync(0xffffffffu, total, k);
+    if ((lane & 7) == 0 && i < here) lse[i] = top == -INFINITY && total == 0.f ? INFINITY : top + log2f(total);
+    __syncthreads();
+    if (j >= l.n) continue;
+    int m = m0;
+    const float* row = p.scores + (static_cast<long long>(unit0 + h) * p.M + m) * p.pitch + j;
+#pragma unroll 8
+    for (int k = 0; k < here; ++k) {
+      const float2 t = *reinterpret_cast<const float2*>(row);
+      const bool end = ++m == rows_m;   // of the head's rows in use
+      row += static_cast<long long>(end ? p.M - rows_m + 1 : 1) * p.pitch;
+      m = end ? 0 : m;
+      sum[0] += ex2(t.x - lse[k]);
+      sum[1] += ex2(t.y - lse[k]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (j + i < l.n) p.acc_out[at + i] = l.rows > 0 ? p.decay * old[i] + sum[i] / static_cast<float>(p.H / p.G) : old[i];
+}
+
 namespace {
 
 template <class T, int D>
 cudaError_t configure_of() {
   cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(RowsSmem<D>) + 128);
+  if (e != cudaSuccess) return e;
+  e = cudaFuncSetAttribute(attend_few_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kBytes);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(attend_sums_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SumsSmem<D>) + 128);
 }
@@ -398,6 +868,14 @@ cudaError_t configure_of() {
 template <class T, int D>
 cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
   const long long units = static_cast<long long>(p.B) * p.Hk;
+  if (p.M <= kFewRows) {
+    cudaError_t e = launch_chained(attend_few_kernel<T, D>, dim3(p.warps / FewShape<D>::kWarps), dim3(FewShape<D>::kThreads),
+                                   FewShape<D>::kBytes, st, p);
+    if (e != cudaSuccess) return e;
+    const int row_ctas = static_cast<int>(units * p.M);
+    const long long sums = static_cast<long long>(p.B) * p.G * ((p.C + kSumSlots - 1) / kSumSlots);
+    return launch_chained(attend_few_join_kernel<T, D>, dim3(static_cast<unsigned>(row_ctas + sums)), dim3(kSumThreads), 0, st, p, row_ctas);
+  }
   const int tiles_m = (p.M + kRowTile - 1) / kRowTile;
   cudaError_t e = launch_chained(attend_rows_kernel<T, D>, dim3(static_cast<unsigned>(units * tiles_m * p.splits)),
                                  dim3(kAttendThreads), sizeof(RowsSmem<D>) + 128, st, p);
