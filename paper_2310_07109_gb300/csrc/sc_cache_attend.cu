@@ -721,11 +721,12 @@ struct Pieces {
 
 // The first `row_ctas` CTAs join a row each; the others have kSumSlots slots of a list each, whose weights
 // they add up over the list's rows from the scores and the rows' LSE.
-constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32;
+constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32;
 constexpr int kSumSlots = kSumThreads * 2;
+constexpr int kSumAhead = 8;
 constexpr int kSumRows = kSumThreads / 8;   // rows whose LSE are found at once, by eight lanes each
 template <class T, int D>
-__global__ void __launch_bounds__(kSumThreads) attend_few_join_kernel(const AttendParams p, int row_ctas) {
+__global__ void __launch_bounds__(kSumThreads, 8) attend_few_join_kernel(const AttendParams p, int row_ctas) {
   using Parts = Pieces<FewShape<D>::kWarps>;
   constexpr int kOwn = D / 32;
   __shared__ float part[kSumWarps][D];
@@ -747,14 +748,15 @@ __global__ void __launch_bounds__(kSumThreads) attend_few_join_kernel(const Atte
       const int s = s0 + (lane & 7);
       const float2 ml = s < ps.count ? p.ml[ps.at(s) * p.M + m] : make_float2(-INFINITY, 0.f);
       const bool some = ml.x != -INFINITY || ml.y != 0.f;   // (nothing but NaN: the sum is one)
-      const unsigned have = __ballot_sync(0xffffffffu, some) & 0xffu;
+      // (asked for before it is known which are empty: theirs hold anything)
       float2 f[8][kOwn / 2];
 #pragma unroll
       for (int u = 0; u < 8; ++u)
 #pragma unroll
         for (int i = 0; i < kOwn; i += 2)
-          f[u][i / 2] = have >> u & 1u ? *reinterpret_cast<const float2*>(p.part + (ps.at(s0 + u) * p.M + m) * D + lane * kOwn + i)
-                                       : make_float2(0.f, 0.f);
+          f[u][i / 2] = s0 + u < ps.count ? *reinterpret_cast<const float2*>(p.part + (ps.at(s0 + u) * p.M + m) * D + lane * kOwn + i)
+                                          : make_float2(0.f, 0.f);
+      const unsigned have = __ballot_sync(0xffffffffu, some) & 0xffu;
       float top = fmaxf(ref, ml.x);
 #pragma unroll
       for (int i = 4; i > 0; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
@@ -767,6 +769,7 @@ __global__ void __launch_bounds__(kSumThreads) attend_few_join_kernel(const Atte
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const float wu = __shfl_sync(0xffffffffu, w, u);
+        if (!(have >> u & 1u)) continue;
 #pragma unroll
         for (int i = 0; i < kOwn; i += 2) {
           o[i] += wu * f[u][i / 2].x;
@@ -811,6 +814,20 @@ __global__ void __launch_bounds__(kSumThreads) attend_few_join_kernel(const Atte
   for (int r0 = 0; r0 < rows; r0 += kSumRows) {
     const int here = min(kSumRows, rows - r0), i = threadIdx.x / 8;
     const int h = r0 / rows_m, m0 = r0 - h * rows_m;
+    // the first rows' scores are asked for before the LSE are known
+    const float* row = p.scores + (static_cast<long long>(unit0 + h) * p.M + m0) * p.pitch + j;
+    int m = m0;
+    auto next = [&]() {
+      const float2 t = *reinterpret_cast<const float2*>(row);
+      const bool end = ++m == rows_m;   // of the head's rows in use
+      row += static_cast<long long>(end ? p.M - rows_m + 1 : 1) * p.pitch;
+      m = end ? 0 : m;
+      return t;
+    };
+    float2 ahead[kSumAhead];
+#pragma unroll
+    for (int k = 0; k < kSumAhead; ++k)
+      if (k < here && j < l.n) ahead[k] = next();
     __syncthreads();
     // (whole warps: four rows each)
     const int mine = m0 + min(i, here - 1), hi = mine / rows_m, unit = unit0 + h + hi;
@@ -837,14 +854,15 @@ __global__ void __launch_bounds__(kSumThreads) attend_few_join_kernel(const Atte
     if ((lane & 7) == 0 && i < here) lse[i] = top == -INFINITY && total == 0.f ? INFINITY : top + log2f(total);
     __syncthreads();
     if (j >= l.n) continue;
-    int m = m0;
-    const float* row = p.scores + (static_cast<long long>(unit0 + h) * p.M + m) * p.pitch + j;
+#pragma unroll
+    for (int k = 0; k < kSumAhead; ++k)
+      if (k < here) {
+        sum[0] += ex2(ahead[k].x - lse[k]);
+        sum[1] += ex2(ahead[k].y - lse[k]);
+      }
 #pragma unroll 8
-    for (int k = 0; k < here; ++k) {
-      const float2 t = *reinterpret_cast<const float2*>(row);
-      const bool end = ++m == rows_m;   // of the head's rows in use
-      row += static_cast<long long>(end ? p.M - rows_m + 1 : 1) * p.pitch;
-      m = end ? 0 : m;
+    for (int k = kSumAhead; k < here; ++k) {
+      const float2 t = next();
       sum[0] += ex2(t.x - lse[k]);
       sum[1] += ex2(t.y - lse[k]);
     }
