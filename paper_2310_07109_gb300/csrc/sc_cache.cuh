@@ -65,6 +65,7 @@ struct HeadsOut {
 struct RotateParams {
   int B, L, Hq, Hk, d;
   long long T;               // B L
+  float over_d;              // 1 / d
   HeadsIn q, k;              // forward: the heads; backward: the forward call's heads
   HeadsIn dq, dk;            // backward: gradients of the outputs
   HeadsOut q_out, k_out;     // the outputs, or the gradients of the inputs
@@ -95,7 +96,7 @@ struct RotateParams {
   unsigned* done;            // workspace: CTAs that have read len and seen
 };
 
-constexpr int kRotateMaxParts = 456;   // CTAs of the gradient
+constexpr int kRotateMaxParts = 1216;   // CTAs of the gradient
 
 struct AttendParams {
   int B, C, H, Hk, G, T;

@@ -135,6 +135,7 @@ extern "C" int sc_rotate_forward(const sc_rotate_args* a, void* stream) {
   RotateParams p{};
   p.B = a->B; p.L = a->L; p.Hq = a->Hq; p.Hk = a->Hk; p.d = a->d;
   p.T = static_cast<long long>(a->B) * a->L;
+  p.over_d = 1.f / static_cast<float>(a->d);
   p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
   p.k = {static_cast<const uint16_t*>(a->K), a->ldk};
   p.q_out = {static_cast<uint16_t*>(a->Q_out), a->ldq_out};
@@ -162,6 +163,7 @@ extern "C" int sc_rotate_backward(const sc_rotate_backward_args* a, void* worksp
   RotateParams p{};
   p.B = a->B; p.L = a->L; p.Hq = a->Hq; p.Hk = a->Hk; p.d = a->d;
   p.T = static_cast<long long>(a->B) * a->L;
+  p.over_d = 1.f / static_cast<float>(a->d);
   p.dq = {static_cast<const uint16_t*>(a->dQ_out), a->ldq_out};
   p.dk = {static_cast<const uint16_t*>(a->dK_out), a->ldk_out};
   p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
@@ -197,6 +199,7 @@ extern "C" int sc_cache_append(const sc_cache_append_args* a, void* workspace, s
   RotateParams p{};
   p.B = a->B; p.L = a->L; p.Hq = a->H; p.Hk = a->Hk; p.d = a->d;
   p.T = static_cast<long long>(a->B) * a->L;
+  p.over_d = 1.f / static_cast<float>(a->d);
   p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
   p.k = {static_cast<const uint16_t*>(a->K_in), a->ldk};
   p.v = {static_cast<const uint16_t*>(a->V_in), a->ldv};

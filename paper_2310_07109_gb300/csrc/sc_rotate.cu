@@ -9,15 +9,17 @@
 // Angles: a pair's frequency is kept as the fraction of a turn that one position adds, in
 // units of 2^-64.  An integer product with the position wraps at whole turns by itself, so
 // its top 32 bits are the angle, whatever the position (an fp32 product is off by 0.06 rad at
-// position 10^6).
+// position 10^6).  Sine and cosine of it are the hardware's, within 2^-21.
 //
-// Bound by memory: each value is read once and written once.  A lane has the two 16-byte vectors
-// of a head that hold both members of its eight pairs, so rotating takes no exchange between
-// lanes and a norm's sum is a few shuffles; a warp has 32 / W heads of a token at once and
-// loads kBatch such groups before it works on the first.  A token's angles are computed once for all
-// its heads, one pair a lane, and passed on through shared memory.
-#include <cuda_runtime.h>
+// Each value is read once and written once, but a group of heads takes so few bytes that the instructions
+// it takes count as much.  So all that does not change from token to token is settled before the loop: the
+// heads of a token (queries, keys and, in an append, values) are one list, a warp has one group of 32 / W of
+// them for all its tokens, and a lane the two 16-byte vectors of a head that hold both members of its
+// eight pairs (no exchange between lanes but a norm's sum).  The warps of a CTA have the groups of the same few
+// tokens, whose angles they compute together, one for each pair, whatever the number of heads.  Two tokens go
+// through the stages together, the next two on their way; the arithmetic runs on fp32 pairs.
 #include <algorithm>
+#include <cuda_runtime.h>
 #include <cstdint>
 
 #include "sc_cache.cuh"
@@ -26,47 +28,65 @@
 
 namespace sc {
 
-constexpr int kRotateWarps = 8;
+constexpr int kRotateWarps = 8;         // most of a CTA
 constexpr int kRotateThreads = kRotateWarps * 32;
-constexpr int kMaxPairs = SC_MAX_HEAD_WIDTH / 2;
-constexpr int kPairsLane = kMaxPairs / 32;
+constexpr int kRotateCtas = 2;          // an SM
+constexpr int kTileTokens = 16;         // most tokens of a CTA at a time
+constexpr int kPairsLane = SC_MAX_HEAD_WIDTH / 64;
 
-struct RotateSmem {
-  float2 turn[kRotateWarps][kMaxPairs];        // m cos, m sin of the warp's token
-  float gamma[2][SC_MAX_HEAD_WIDTH];
+// How the work is cut: `wg` warps side by side for groups, `wt` for tokens, each `nt` tokens at a time.
+struct RotatePlan {
+  int wg, wt, nt, ctas;
 };
 
-// The fraction of a turn that one position adds, in 2^-64.
-__device__ __forceinline__ uint64_t turn_of(double freq) {
-  double t = freq * 0.15915494309189533577;   // 1 / (2 pi)
-  t -= floor(t);
-  return __double2ull_rn(t * 18446744073709551616.0);
+// The fraction of a turn that one position adds, freq / (2 pi), in 2^-64: the 53-bit significand times
+// 2^66 / (2 pi) as a 117-bit product, shifted by the exponent (fp64 arithmetic would take longer than all else).
+__device__ __forceinline__ unsigned long long turn_of(double freq) {
+  const unsigned long long bits = static_cast<unsigned long long>(__double_as_longlong(freq));
+  const unsigned long long m = (bits & 0xfffffffffffffull) | 0x10000000000000ull, c = 11743562013128004906ull;
+  const unsigned long long hi = __umul64hi(m, c), lo = m * c;
+  const int right = 54 + 1023 - static_cast<int>(bits >> 52 & 2047u);   // of the product, for freq = m 2^(e - 52)
+  unsigned long long t;
+  if (right >= 128) t = 0;
+  else if (right >= 64) t = hi >> (right - 64);
+  else if (right > 0) t = hi << (64 - right) | lo >> right;
+  else t = right > -64 ? lo << -right : 0;
+  return bits >> 63 ? 0 - t : t;
 }
 
-// cos and sin of `pos` times that fraction.
-__device__ __forceinline__ float2 turned(uint64_t turn, int pos, float m) {
-  const uint64_t at = turn * static_cast<uint64_t>(static_cast<int64_t>(pos));
-  const int top = static_cast<int>((at + 0x80000000ull) >> 32);   // of half a turn, in 2^-31
-  float s, c;
-  sincospif(static_cast<float>(top) * 4.656612873077393e-10f, &s, &c);
-  return make_float2(m * c, m * s);
+// First and second members of a lane's pairs as fp32 pairs, and back: the two vectors (kInter false), or
+// the even and the odd values of both.
+template <class T, bool kInter>
+__device__ __forceinline__ void unpack(const uint4& va, const uint4& vb, uint64_t (&a)[4], uint64_t (&b)[4]) {
+  const uint32_t w[8] = {va.x, va.y, va.z, va.w, vb.x, vb.y, vb.z, vb.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x0, y0, x1, y1;
+    if (kInter) {
+      T::unpack(w[2 * i], x0, y0);
+      T::unpack(w[2 * i + 1], x1, y1);
+    } else {
+      T::unpack(w[i], x0, x1);
+      T::unpack(w[4 + i], y0, y1);
+    }
+    a[i] = f2_pack(x0, x1);
+    b[i] = f2_pack(y0, y1);
+  }
 }
 
-template <class T>
-__device__ __forceinline__ void unpack16(const uint4& a, const uint4& b, float (&x)[16]) {
-  T::unpack(a.x, x[0], x[1]);
-  T::unpack(a.y, x[2], x[3]);
-  T::unpack(a.z, x[4], x[5]);
-  T::unpack(a.w, x[6], x[7]);
-  T::unpack(b.x, x[8], x[9]);
-  T::unpack(b.y, x[10], x[11]);
-  T::unpack(b.z, x[12], x[13]);
-  T::unpack(b.w, x[14], x[15]);
-}
-
-template <class T>
-__device__ __forceinline__ uint4 pack8(const float* x) {
-  return make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
+template <class T, bool kInter>
+__device__ __forceinline__ void pack(const uint64_t (&a)[4], const uint64_t (&b)[4], uint4& va, uint4& vb) {
+  uint32_t w[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x0, x1, y0, y1;
+    f2_unpack(a[i], x0, x1);
+    f2_unpack(b[i], y0, y1);
+    w[kInter ? 2 * i : i] = kInter ? T::pack(x0, y0) : T::pack(x0, x1);
+    w[kInter ? 2 * i + 1 : 4 + i] = kInter ? T::pack(x1, y1) : T::pack(y0, y1);
+  }
+  va = make_uint4(w[0], w[1], w[2], w[3]);
+  vb = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
 template <int W>
@@ -76,377 +96,492 @@ __device__ __forceinline__ float sum_lanes(float v) {
   return v;
 }
 
-// What a lane has of every head: vectors va and vb, both members of pairs 8 q .. 8 q + 7.
+__device__ __forceinline__ float f2_total(uint64_t v) {
+  float lo, hi;
+  f2_unpack(v, lo, hi);
+  return lo + hi;
+}
+
+// The sum of squares of the lane's sixteen values, over the head's lanes.
+template <int W>
+__device__ __forceinline__ float squares(const uint64_t (&a)[4], const uint64_t (&b)[4]) {
+  uint64_t s = f2_mul(a[0], a[0]), t = f2_mul(b[0], b[0]);
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
+    s = f2_fma(a[i], a[i], s);
+    t = f2_fma(b[i], b[i], t);
+  }
+  return sum_lanes<W>(f2_total(f2_add(s, t)));
+}
+
+__device__ __forceinline__ void load4(const float* from, uint64_t (&v)[4]) {
+  const ulonglong2* f = reinterpret_cast<const ulonglong2*>(from);
+  const ulonglong2 x = f[0], y = f[1];
+  v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
+}
+
+// (a, b) -> (a cos - b sin, b cos + a sin), or, backward, (a cos + b sin, b cos - a sin)
+template <bool kBack>
+__device__ __forceinline__ void rotate(uint64_t (&a)[4], uint64_t (&b)[4], const float* cos, const float* sin) {
+  uint64_t c[4], s[4];
+  load4(cos, c);
+  load4(sin, s);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t x = a[i], as = f2_mul(x, s[i]), bs = f2_mul(b[i], s[i]), minus = (kBack ? as : bs) ^ 0x8000000080000000ull;
+    a[i] = f2_fma(x, c[i], kBack ? bs : minus);
+    b[i] = f2_fma(b[i], c[i], kBack ? minus : as);
+  }
+}
+
+// What a lane does for every token.
 struct LaneShare {
-  int va, vb;
-  bool live, turns, inter;
-  __device__ LaneShare(const RotateParams& p, int q) {
+  int group, sub, q;   // its warp's group; head of the group and lane of the head
+  int head;            // of the list of queries, keys and values; one that there is
+  int side, of_side;   // 0 queries, 1 keys, 2 values; the head's number among them
+  int va, vb;          // its vectors of the head
+  bool live, turns;    // it has a part of a head; which is rotated
+  __device__ __forceinline__ LaneShare(const RotateParams& p, const RotatePlan& plan, int w, bool inter, bool append) {
+    const int lane = threadIdx.x & 31, at_once = 32 / w, turned = p.Hq + p.Hk, heads = turned + (append ? p.Hk : 0);
+    group = blockIdx.y * plan.wg + (threadIdx.x >> 5) % plan.wg;
+    q = lane % w;
+    sub = lane / w;
+    const int mine = group * at_once + sub;
+    head = min(mine, heads - 1);
+    side = head < p.Hq ? 0 : head < turned ? 1 : 2;
+    of_side = head - (side == 0 ? 0 : side == 1 ? p.Hq : turned);
     const int half = p.rot / 16;
-    live = q < p.d / 16;
-    turns = live && q < half;
-    inter = p.interleaved != 0;
+    const bool in = q < p.d / 16;
+    live = in && mine < heads;
+    turns = in && q < half;
     const bool apart = turns && !inter;
-    va = apart ? q : 2 * q;
-    vb = apart ? q + half : 2 * q + 1;
+    va = apart ? q : in ? 2 * q : 0;   // (lanes beyond the head read its start)
+    vb = apart ? q + half : in ? 2 * q + 1 : 0;
   }
 };
 
-// A token's angles into the warp's table.
-__device__ __forceinline__ void table(const RotateParams& p, const uint64_t (&turn)[kPairsLane], int pos,
-                                      float2* to, int lane) {
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < kPairsLane; ++i)
-    if (i * 32 + lane < p.rot / 2) to[i * 32 + lane] = turned(turn[i], pos, p.mscale);
-  __syncwarp();
-}
+// The tile of tokens of a CTA: lane i has its token t0 + i's sequence, row, position, and whether it is in use.
+struct TileTokens {
+  int b, r, pos;
+  unsigned used;   // of all lanes
+  __device__ __forceinline__ TileTokens(const RotateParams& p, long long t0, int count, bool append) {
+    const int lane = threadIdx.x & 31;
+    const long long t = t0 + lane;
+    bool in = lane < count && t < p.T;
+    b = r = pos = 0;
+    if (in) {
+      b = static_cast<int>(static_cast<unsigned>(t) / static_cast<unsigned>(p.L));
+      r = static_cast<int>(static_cast<unsigned>(t) - static_cast<unsigned>(b) * static_cast<unsigned>(p.L));
+      pos = append ? __ldg(p.seen + b) + r : p.pos != nullptr ? __ldg(p.pos + t) : r;
+      in = p.rows == nullptr || r < __ldg(p.rows + b);
+    }
+    used = __ballot_sync(0xffffffffu, in);
+  }
+};
 
-// Rotates the pairs of x, which hold (a, b) as x[i], x[8 + i], or as x[2 i], x[2 i + 1].
-template <bool kBack>
-__device__ __forceinline__ void rotate16(float (&x)[16], const LaneShare& s, const float2* turn) {
-  if (!s.turns) return;
-  const float4* t4 = reinterpret_cast<const float4*>(turn);
+// The tile's angles, cos and sin of [token][rot / 2]: a warp a token, a lane a pair.
+__device__ __forceinline__ void angles(const RotateParams& p, const TileTokens& at, int count, const unsigned long long (&turn)[kPairsLane],
+                                       float* cos, float* sin) {
+  const int lane = threadIdx.x & 31, pairs = p.rot / 2;
+  for (int i = threadIdx.x >> 5; i < count; i += blockDim.x >> 5) {
+    const long long pos = __shfl_sync(0xffffffffu, at.pos, i);
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    const float4 f = t4[i / 2];
-    const float2 cs[2] = {make_float2(f.x, kBack ? -f.y : f.y), make_float2(f.z, kBack ? -f.w : f.w)};
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int k = i + j;
-      if (s.inter) {
-        const float a = x[2 * k], b = x[2 * k + 1];
-        x[2 * k] = a * cs[j].x - b * cs[j].y;
-        x[2 * k + 1] = b * cs[j].x + a * cs[j].y;
-      } else {
-        const float a = x[k], b = x[8 + k];
-        x[k] = a * cs[j].x - b * cs[j].y;
-        x[8 + k] = b * cs[j].x + a * cs[j].y;
-      }
+    for (int k = 0; k < kPairsLane; ++k) {
+      if (k * 32 + lane >= pairs) break;
+      const unsigned long long a = turn[k] * static_cast<unsigned long long>(pos);
+      const int top = static_cast<int>((a + 0x80000000ull) >> 32);   // of half a turn, in 2^-31
+      const float angle = static_cast<float>(top) * 1.4629180792671596e-9f;   // pi 2^-31
+      cos[i * pairs + k * 32 + lane] = p.mscale * __cosf(angle);
+      sin[i * pairs + k * 32 + lane] = p.mscale * __sinf(angle);
     }
   }
 }
 
-__device__ __forceinline__ void gamma16(const float* gamma, const LaneShare& s, float (&g)[16]) {
+__device__ __forceinline__ void turns_of(const RotateParams& p, unsigned long long (&turn)[kPairsLane]) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float4 a = reinterpret_cast<const float4*>(gamma)[2 * s.va + i];
-    const float4 b = reinterpret_cast<const float4*>(gamma)[2 * s.vb + i];
-    g[4 * i] = a.x; g[4 * i + 1] = a.y; g[4 * i + 2] = a.z; g[4 * i + 3] = a.w;
-    g[8 + 4 * i] = b.x; g[8 + 4 * i + 1] = b.y; g[8 + 4 * i + 2] = b.z; g[8 + 4 * i + 3] = b.w;
-  }
+  for (int k = 0; k < kPairsLane; ++k) turn[k] = k * 32 + lane < p.rot / 2 ? turn_of(__ldg(p.freq + k * 32 + lane)) : 0;
 }
 
-__device__ __forceinline__ void load_gamma(const RotateParams& p, RotateSmem& sm) {
-  for (int i = threadIdx.x; i < p.d; i += kRotateThreads) {
-    sm.gamma[0][i] = p.gamma_q != nullptr ? __ldg(p.gamma_q + i) : 0.f;
-    sm.gamma[1][i] = p.gamma_k != nullptr ? __ldg(p.gamma_k + i) : 0.f;
+// gamma of the lane's first and second members (1 where there is none).
+__device__ __forceinline__ void gamma_of(const float* gamma, const LaneShare& s, bool inter, uint64_t (&a)[4], uint64_t (&b)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[i] = b[i] = f2_both(1.f);
+    if (gamma == nullptr) continue;
+    const float* x = gamma + 8 * s.va;
+    const float* y = gamma + 8 * s.vb;
+    if (inter) {   // the sixteen values from x on, in turn
+      const float* z = i < 2 ? x + 4 * i : y + 4 * (i - 2);
+      a[i] = f2_pack(__ldg(z), __ldg(z + 2));
+      b[i] = f2_pack(__ldg(z + 1), __ldg(z + 3));
+    } else {
+      a[i] = f2_pack(__ldg(x + 2 * i), __ldg(x + 2 * i + 1));
+      b[i] = f2_pack(__ldg(y + 2 * i), __ldg(y + 2 * i + 1));
+    }
   }
 }
 
 __device__ __forceinline__ int cache_len(const RotateParams& p, int list) {
-  return min(max(__ldcg(p.len + list), 0), p.C);
+  return min(max(p.len[list], 0), p.C);
 }
 
-// Forward, and append where cache_k is set.  A warp's work: the groups of heads `part`, part + parts, ...
-// of a token; with few tokens several warps share one.
-template <class T, int W>
-__global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const RotateParams p, int parts) {
-  constexpr int kAtOnce = 32 / W;   // heads of a group
-  constexpr int kBatch = 4;         // groups whose loads are under way together
-  __shared__ RotateSmem sm;
+// Forward, and append where cache_k is set.
+template <class T, int W, bool kInter, bool kNorm>
+__global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_kernel(const RotateParams p, const RotatePlan plan) {
+  extern __shared__ __align__(16) float table[];   // [2][cos, sin][wt nt][rot / 2]
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int q = lane & (W - 1), sub = lane / W;
-  const LaneShare share(p, q);
   const bool append = p.cache_k != nullptr;
-  const int gq = (p.Hq + kAtOnce - 1) / kAtOnce, gk = (p.Hk + kAtOnce - 1) / kAtOnce;
-  const int groups = gq + gk + (append ? gk : 0);
-  uint64_t turn[kPairsLane];
+  const LaneShare s(p, plan, W, kInter, append);
+  const int count = plan.wt * plan.nt, pairs = p.rot / 2, mine = (threadIdx.x >> 5) / plan.wg * plan.nt;
+  const bool whole = (p.d & (p.d - 1)) == 0 && p.d >= 16 * W;   // no lane is beyond a head
+  const HeadsIn in = s.side == 0 ? p.q : s.side == 1 ? p.k : p.v;
+  const HeadsOut out = s.side == 0 ? p.q_out : p.k_out;
+  const bool to_cache = append && s.side > 0;
+  const uint16_t* src = in.p + s.of_side * p.d;
+  uint16_t* dst = !to_cache ? out.p + s.of_side * p.d : (s.side == 1 ? p.cache_k : p.cache_v) + s.of_side * p.stride_h;
+  const int of = p.Hk / p.G, list = to_cache ? s.of_side / of : 0;
+  const bool marks = to_cache && s.live && s.side == 1 && s.q == 0 && s.of_side % of == 0;
+  unsigned long long turn[kPairsLane];
+  turns_of(p, turn);
+  uint64_t ga[4], gb[4];
+  const float* gamma = s.side == 0 ? p.gamma_q : s.side == 1 ? p.gamma_k : nullptr;
+  if (kNorm) gamma_of(gamma, s, kInter, ga, gb);
+  uint4 va[2] = {}, vb[2] = {};
+  auto load = [&](const TileTokens& at, long long t0, int i) {   // tokens i, i + 1 of the warp's
 #pragma unroll
-  for (int i = 0; i < kPairsLane; ++i)
-    turn[i] = i * 32 + lane < p.rot / 2 ? turn_of(__ldg(p.freq + i * 32 + lane)) : 0;
-  load_gamma(p, sm);
-  __syncthreads();
-  const unsigned L = static_cast<unsigned>(p.L);
-  const long long items = p.T * parts, step = static_cast<long long>(gridDim.x) * kRotateWarps;
-  for (long long it = static_cast<long long>(blockIdx.x) * kRotateWarps + warp; it < items; it += step) {
-    const unsigned t = static_cast<unsigned>(it / parts);
-    const int part = static_cast<int>(it - static_cast<long long>(t) * parts);
-    const int b = static_cast<int>(t / L), r = static_cast<int>(t - b * L);
-    if (p.rows != nullptr && r >= __ldg(p.rows + b)) continue;
-    const int pos = append ? __ldcg(p.seen + b) + r : p.pos != nullptr ? __ldg(p.pos + t) : r;
-    table(p, turn, pos, sm.turn[warp], lane);
-    for (int g0 = part; g0 < groups; g0 += parts * kBatch) {
-      uint4 va[kBatch], vb[kBatch];
+    for (int u = 0; u < 2; ++u) {
+      if (i + u >= plan.nt || !(at.used >> (mine + i + u) & 1u)) continue;
+      const uint4* from = reinterpret_cast<const uint4*>(src + (t0 + mine + i + u) * in.ld);
+      va[u] = from[s.va];
+      vb[u] = from[s.vb];
+    }
+  };
+  long long t0 = static_cast<long long>(blockIdx.x) * count;
+  int buffer = 0;
+  for (; t0 < p.T; t0 += static_cast<long long>(gridDim.x) * count, buffer ^= 1) {
+    const TileTokens at(p, t0, count, append);
+    load(at, t0, 0);
+    float *cos = table + buffer * 2 * count * pairs, *sin = cos + count * pairs;
+    angles(p, at, count, turn, cos, sin);
+    __syncthreads();   // (the other table is free when all have come here again)
+    for (int i = 0; i < plan.nt; i += 2) {
+      uint64_t a[2][4], b[2][4];
+      uint4 xa[2], xb[2];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int g = g0 + u * parts;
-        const int side = g < gq ? 0 : g < gq + gk ? 1 : 2;
-        const int head = (g - (side == 0 ? 0 : side == 1 ? gq : gq + gk)) * kAtOnce + sub;
-        const HeadsIn in = side == 0 ? p.q : side == 1 ? p.k : p.v;
-        va[u] = vb[u] = make_uint4(0, 0, 0, 0);
-        if (g < groups && share.live && head < (side == 0 ? p.Hq : p.Hk)) {
-          const uint4* src = reinterpret_cast<const uint4*>(in.p + t * in.ld + static_cast<long long>(head) * p.d);
-          va[u] = src[share.va];
-          vb[u] = src[share.vb];
+      for (int u = 0; u < 2; ++u) {
+        if (!whole && s.q >= p.d / 16) va[u] = vb[u] = make_uint4(0, 0, 0, 0);
+        xa[u] = va[u];
+        xb[u] = vb[u];
+        unpack<T, kInter>(va[u], vb[u], a[u], b[u]);
+      }
+      load(at, t0, i + 2);
+      if (kNorm) {
+        float ss[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) ss[u] = squares<W>(a[u], b[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint64_t inv = f2_both(gamma != nullptr ? rsqrtf(fmaf(ss[u], p.over_d, p.eps)) : 1.f);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            a[u][k] = f2_mul(a[u][k], f2_mul(ga[k], inv));
+            b[u][k] = f2_mul(b[u][k], f2_mul(gb[k], inv));
+          }
+        }
+      }
+      if (s.turns) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int row = (mine + min(i + u, plan.nt - 1)) * pairs + 8 * s.q;
+          rotate<false>(a[u], b[u], cos + row, sin + row);
         }
       }
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int g = g0 + u * parts;
-        if (g >= groups) break;
-        const int side = g < gq ? 0 : g < gq + gk ? 1 : 2;
-        const int head = (g - (side == 0 ? 0 : side == 1 ? gq : gq + gk)) * kAtOnce + sub;
-        const bool live = share.live && head < (side == 0 ? p.Hq : p.Hk);
-        if (side < 2) {
-          float x[16];
-          unpack16<T>(va[u], vb[u], x);
-          if ((side == 0 ? p.gamma_q : p.gamma_k) != nullptr) {
-            float ss = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
-            const float inv = rsqrtf(sum_lanes<W>(ss) / static_cast<float>(p.d) + p.eps);
-            if (share.live) {
-              float gm[16];
-              gamma16(sm.gamma[side], share, gm);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] *= inv * gm[i];
-            }
+      for (int u = 0; u < 2; ++u) {
+        const int token = mine + i + u;
+        const bool used = i + u < plan.nt && (at.used >> token & 1u);
+        const int b_u = __shfl_sync(0xffffffffu, at.b, token & 31), r_u = __shfl_sync(0xffffffffu, at.r, token & 31);
+        if (!used || !s.live) continue;
+        uint4 ya, yb;
+        pack<T, kInter>(a[u], b[u], ya, yb);
+        uint16_t* to = dst + (t0 + token) * out.ld;
+        if (to_cache) {
+          const int c = cache_len(p, b_u * p.G + list) + r_u;
+          if (c >= p.C) continue;
+          to = dst + b_u * p.stride_b + c * p.stride_c;
+          if (s.side == 2) {
+            ya = xa[u];
+            yb = xb[u];
           }
-          rotate16<false>(x, share, sm.turn[warp] + 8 * q);
-          va[u] = pack8<T>(x);
-          vb[u] = pack8<T>(x + 8);
-        }
-        if (!live) continue;
-        uint16_t* to;
-        if (side == 0) {
-          to = p.q_out.p + t * p.q_out.ld + static_cast<long long>(head) * p.d;
-        } else if (!append) {
-          to = p.k_out.p + t * p.k_out.ld + static_cast<long long>(head) * p.d;
-        } else {
-          const int of = p.Hk / p.G, list = b * p.G + head / of;
-          const int slot = cache_len(p, list) + r;
-          if (slot >= p.C) continue;
-          to = (side == 1 ? p.cache_k : p.cache_v) + b * p.stride_b + head * p.stride_h + slot * p.stride_c;
-          if (side == 1 && q == 0 && head % of == 0) {
-            p.acc[static_cast<long long>(list) * p.C + slot] = 0.f;
-            p.slot_pos[static_cast<long long>(list) * p.C + slot] = pos;
+          if (marks) {
+            const long long slot = (static_cast<long long>(b_u) * p.G + list) * p.C + c;
+            p.acc[slot] = 0.f;
+            p.slot_pos[slot] = __ldg(p.seen + b_u) + r_u;
           }
         }
-        reinterpret_cast<uint4*>(to)[share.va] = va[u];
-        reinterpret_cast<uint4*>(to)[share.vb] = vb[u];
+        reinterpret_cast<uint4*>(to)[s.va] = ya;
+        reinterpret_cast<uint4*>(to)[s.vb] = yb;
       }
     }
   }
   if (!append) return;
   // The last CTA to be done with len and seen moves them on.
   __shared__ bool last;
+  const unsigned ctas = gridDim.x * gridDim.y;
   __syncthreads();
   if (threadIdx.x == 0) {
     __threadfence();
-    last = atomicInc(p.done, gridDim.x - 1) == gridDim.x - 1;   // back to 0 after the last
+    last = atomicInc(p.done, ctas - 1) == ctas - 1;   // back to 0 after the last
     __threadfence();
   }
   __syncthreads();
   if (!last) return;
-  for (int i = threadIdx.x; i < p.B * p.G; i += kRotateThreads) {
+  for (int i = threadIdx.x; i < p.B * p.G; i += blockDim.x) {
     const int b = i / p.G;
     const int come = p.rows != nullptr ? min(max(__ldg(p.rows + b), 0), p.L) : p.L;
     const long long n = static_cast<long long>(cache_len(p, i)) + come;
     if (n > p.C) atomicOr(p.status, kStatusFull);
     p.len_out[i] = static_cast<int>(min(n, static_cast<long long>(p.C)));
   }
-  for (int b = threadIdx.x; b < p.B; b += kRotateThreads)
-    p.seen_out[b] = __ldcg(p.seen + b) + (p.rows != nullptr ? min(max(__ldg(p.rows + b), 0), p.L) : p.L);
+  for (int b = threadIdx.x; b < p.B; b += blockDim.x)
+    p.seen_out[b] = __ldg(p.seen + b) + (p.rows != nullptr ? min(max(__ldg(p.rows + b), 0), p.L) : p.L);
 }
 
-// Gradient.  dgamma: a lane adds up its features over its heads and tokens, the CTA its lanes, in order;
-// the parts of the CTAs are added, in order, by rotate_gamma_kernel.
-template <class T, int W>
-__global__ void __launch_bounds__(kRotateThreads, 2) rotate_back_kernel(const RotateParams p) {
-  constexpr int kAtOnce = 32 / W;
-  constexpr int kBatch = 2;
-  __shared__ RotateSmem sm;
+// Gradient.  dgamma: a lane adds up its features of its head over its tokens, the CTA its lanes and warps, in order;
+// the parts of the CTAs (blockIdx.y has groups of its own) are added, in order, by rotate_gamma_kernel.
+template <class T, int W, bool kInter, bool kNorm>
+__global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_back_kernel(const RotateParams p, const RotatePlan plan) {
+  constexpr int kAt = 1;   // tokens that go through the stages together (two: registers do not suffice)
+  extern __shared__ __align__(16) float table[];
   __shared__ float sums[kRotateWarps][SC_MAX_HEAD_WIDTH];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int q = lane & (W - 1), sub = lane / W;
-  const LaneShare share(p, q);
-  uint64_t turn[kPairsLane];
+  const LaneShare s(p, plan, W, kInter, false);
+  const int count = plan.wt * plan.nt, pairs = p.rot / 2, warp = threadIdx.x >> 5, mine = warp / plan.wg * plan.nt;
+  const bool beyond = s.q >= p.d / 16;
+  const HeadsIn dy = s.side == 0 ? p.dq : p.dk, in = s.side == 0 ? p.q : p.k;
+  const HeadsOut out = s.side == 0 ? p.q_out : p.k_out;
+  const float* gamma = s.side == 0 ? p.gamma_q : p.gamma_k;
+  const uint16_t *src = dy.p + s.of_side * p.d, *src_x = in.p + s.of_side * p.d;
+  uint16_t* dst = out.p + s.of_side * p.d;
+  unsigned long long turn[kPairsLane];
+  turns_of(p, turn);
+  uint64_t ga[4], gb[4], total[8];
 #pragma unroll
-  for (int i = 0; i < kPairsLane; ++i)
-    turn[i] = i * 32 + lane < p.rot / 2 ? turn_of(__ldg(p.freq + i * 32 + lane)) : 0;
-  load_gamma(p, sm);
-  __syncthreads();
-  float total[2][16];
+  for (int k = 0; k < 8; ++k) total[k] = 0;
+  if (kNorm) gamma_of(gamma, s, kInter, ga, gb);
+  uint4 va[kAt] = {}, vb[kAt] = {}, wa[kAt] = {}, wb[kAt] = {};
+  auto load = [&](const TileTokens& at, long long t0, int i) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) total[0][i] = total[1][i] = 0.f;
-  const unsigned L = static_cast<unsigned>(p.L);
-  const long long step = static_cast<long long>(gridDim.x) * kRotateWarps;
-  const float over_d = 1.f / static_cast<float>(p.d);
-  for (long long it = static_cast<long long>(blockIdx.x) * kRotateWarps + warp; it < p.T; it += step) {
-    const unsigned t = static_cast<unsigned>(it);
-    const int b = static_cast<int>(t / L), r = static_cast<int>(t - b * L);
-    if (p.rows != nullptr && r >= __ldg(p.rows + b)) continue;
-    table(p, turn, p.pos != nullptr ? __ldg(p.pos + t) : r, sm.turn[warp], lane);
+    for (int u = 0; u < kAt; ++u) {
+      if (i + u >= plan.nt || !(at.used >> (mine + i + u) & 1u)) continue;
+      const long long t = t0 + mine + i + u;
+      const uint4* from = reinterpret_cast<const uint4*>(src + t * dy.ld);
+      va[u] = from[s.va];
+      vb[u] = from[s.vb];
+      if (!kNorm || gamma == nullptr) continue;
+      from = reinterpret_cast<const uint4*>(src_x + t * in.ld);
+      wa[u] = from[s.va];
+      wb[u] = from[s.vb];
+    }
+  };
+  long long t0 = static_cast<long long>(blockIdx.x) * count;
+  int buffer = 0;
+  for (; t0 < p.T; t0 += static_cast<long long>(gridDim.x) * count, buffer ^= 1) {
+    const TileTokens at(p, t0, count, false);
+    load(at, t0, 0);
+    float *cos = table + buffer * 2 * count * pairs, *sin = cos + count * pairs;
+    angles(p, at, count, turn, cos, sin);
+    __syncthreads();
+    for (int i = 0; i < plan.nt; i += kAt) {
+      uint64_t a[kAt][4], b[kAt][4], x[kAt][4], y[kAt][4];
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-      const int heads = side == 0 ? p.Hq : p.Hk;
-      const bool norm = (side == 0 ? p.gamma_q : p.gamma_k) != nullptr;
-      const HeadsIn dy = side == 0 ? p.dq : p.dk, in = side == 0 ? p.q : p.k;
-      const HeadsOut out = side == 0 ? p.q_out : p.k_out;
-      for (int h0 = 0; h0 < heads; h0 += kBatch * kAtOnce) {
-        uint4 va[kBatch], vb[kBatch], xa[kBatch], xb[kBatch];
+      for (int u = 0; u < kAt; ++u) {
+        if (beyond) va[u] = vb[u] = wa[u] = wb[u] = make_uint4(0, 0, 0, 0);
+        unpack<T, kInter>(va[u], vb[u], a[u], b[u]);
+        if (kNorm) unpack<T, kInter>(wa[u], wb[u], x[u], y[u]);
+      }
+      load(at, t0, i + kAt);
+      if (s.turns) {
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const int head = h0 + u * kAtOnce + sub;
-          va[u] = vb[u] = xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
-          if (!share.live || head >= heads) continue;
-          const uint4* src = reinterpret_cast<const uint4*>(dy.p + t * dy.ld + static_cast<long long>(head) * p.d);
-          va[u] = src[share.va];
-          vb[u] = src[share.vb];
-          if (!norm) continue;
-          src = reinterpret_cast<const uint4*>(in.p + t * in.ld + static_cast<long long>(head) * p.d);
-          xa[u] = src[share.va];
-          xb[u] = src[share.vb];
+        for (int u = 0; u < kAt; ++u) {
+          const int row = (mine + min(i + u, plan.nt - 1)) * pairs + 8 * s.q;
+          rotate<true>(a[u], b[u], cos + row, sin + row);
         }
+      }
+      if (kNorm) {
+        float ss[kAt];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const int head = h0 + u * kAtOnce + sub;
-          float g[16];
-          unpack16<T>(va[u], vb[u], g);
-          rotate16<true>(g, share, sm.turn[warp] + 8 * q);
-          if (norm) {
-            float x[16], gm[16];
-            unpack16<T>(xa[u], xb[u], x);
-            float ss = 0.f;
+        for (int u = 0; u < kAt; ++u) ss[u] = squares<W>(x[u], y[u]);
+        uint64_t inv[kAt], inner[kAt];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ss += x[i] * x[i];
-            const float inv = rsqrtf(sum_lanes<W>(ss) * over_d + p.eps);
-            gamma16(sm.gamma[side], share.live ? share : LaneShare(p, 0), gm);
-            float inner = 0.f;
+        for (int u = 0; u < kAt; ++u) {
+          inv[u] = f2_both(gamma != nullptr ? rsqrtf(fmaf(ss[u], p.over_d, p.eps)) : 1.f);
+          const bool used = i + u < plan.nt && (at.used >> (mine + i + u) & 1u);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              x[i] *= inv;
-              total[side][i] += g[i] * x[i];
-              g[i] *= gm[i];
-              inner += g[i] * x[i];
-            }
-            inner = sum_lanes<W>(inner) * over_d;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) g[i] = inv * (g[i] - x[i] * inner);
+          for (int k = 0; k < 4; ++k) {
+            x[u][k] = f2_mul(x[u][k], inv[u]);
+            y[u][k] = f2_mul(y[u][k], inv[u]);
           }
-          if (!share.live || head >= heads) continue;
-          uint4* to = reinterpret_cast<uint4*>(out.p + t * out.ld + static_cast<long long>(head) * p.d);
-          to[share.va] = pack8<T>(g);
-          to[share.vb] = pack8<T>(g + 8);
+          if (used) {   // (of the whole warp)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              total[k] = f2_fma(a[u][k], x[u][k], total[k]);
+              total[4 + k] = f2_fma(b[u][k], y[u][k], total[4 + k]);
+            }
+          }
+          inner[u] = 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            a[u][k] = f2_mul(a[u][k], ga[k]);
+            b[u][k] = f2_mul(b[u][k], gb[k]);
+            inner[u] = f2_fma(a[u][k], x[u][k], inner[u]);
+            inner[u] = f2_fma(b[u][k], y[u][k], inner[u]);
+          }
         }
+#pragma unroll
+        for (int u = 0; u < kAt; ++u) {
+          const float mean = -sum_lanes<W>(f2_total(inner[u])) * p.over_d;
+          if (gamma == nullptr) continue;   // (of the lane's head)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            a[u][k] = f2_mul(inv[u], f2_fma(x[u][k], f2_both(mean), a[u][k]));
+            b[u][k] = f2_mul(inv[u], f2_fma(y[u][k], f2_both(mean), b[u][k]));
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAt; ++u) {
+        const int token = mine + i + u;
+        if (i + u >= plan.nt || !(at.used >> token & 1u) || !s.live) continue;
+        uint4 ya, yb;
+        pack<T, kInter>(a[u], b[u], ya, yb);
+        uint4* to = reinterpret_cast<uint4*>(dst + (t0 + token) * out.ld);
+        to[s.va] = ya;
+        to[s.vb] = yb;
       }
     }
   }
-  if (p.gamma_q == nullptr && p.gamma_k == nullptr) return;
+  if (!kNorm) return;
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = total[side][i];
+    for (int i = 0; i < 8; ++i) {
+      float v[2];
+      f2_unpack(total[i], v[0], v[1]);
 #pragma unroll
-      for (int o = W; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (share.live && sub == 0) sums[warp][8 * (i < 8 ? share.va : share.vb) + (i & 7)] = v;
+      for (int k = 0; k < 2; ++k) {
+        v[k] = s.live && s.side == side ? v[k] : 0.f;
+#pragma unroll
+        for (int o = W; o < 32; o <<= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        const int member = 2 * (i & 3) + k, second = i / 4;   // pair of the lane's eight
+        if (!beyond && s.sub == 0) sums[warp][kInter ? 16 * s.q + 2 * member + second : 8 * (second ? s.vb : s.va) + member] = v[k];
+      }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < p.d; i += kRotateThreads) {
+    for (int i = threadIdx.x; i < p.d; i += blockDim.x) {
       float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < kRotateWarps; ++w) v += sums[w][i];
-      p.part[(static_cast<long long>(blockIdx.x) * 2 + side) * p.d + i] = v;
+      for (int w = 0; w < static_cast<int>(blockDim.x >> 5); ++w) v += sums[w][i];
+      p.part[((static_cast<long long>(blockIdx.y) * gridDim.x + blockIdx.x) * 2 + side) * p.d + i] = v;
     }
     __syncthreads();
   }
 }
 
-// dgamma from the CTAs' parts: 32 features a CTA, eight warps with every eighth part each.
+// dgamma from the CTAs' parts: eight features a CTA, every 32nd part a thread.
 __global__ void __launch_bounds__(kRotateThreads) rotate_gamma_kernel(const RotateParams p, int ctas) {
-  __shared__ float sums[kRotateWarps][32];
+  __shared__ float sums[kRotateWarps][8];
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int i = blockIdx.x * 32 + lane;   // of [2][d]
+  const int f = threadIdx.x & 7, i = blockIdx.x * 8 + f, from = threadIdx.x / 8, lane = threadIdx.x & 31;   // of [2][d]
   float v = 0.f;
-  if (i < 2 * p.d)
-    for (int c = warp; c < ctas; c += kRotateWarps) v += p.part[static_cast<long long>(c) * 2 * p.d + i];
-  sums[warp][lane] = v;
+#pragma unroll 10
+  for (int c = from; c < ctas; c += 32) v += __ldcg(p.part + static_cast<long long>(c) * 2 * p.d + i);
+  v += __shfl_xor_sync(0xffffffffu, v, 8);
+  v += __shfl_xor_sync(0xffffffffu, v, 16);
+  if (lane < 8) sums[threadIdx.x >> 5][f] = v;
   __syncthreads();
-  if (warp != 0 || i >= 2 * p.d) return;
+  if (threadIdx.x >= 8) return;
   v = 0.f;
 #pragma unroll
-  for (int w = 0; w < kRotateWarps; ++w) v += sums[w][lane];
+  for (int w = 0; w < kRotateWarps; ++w) v += sums[w][f];
   float* to = i < p.d ? p.dgamma_q : p.dgamma_k;
   if (to != nullptr) to[i < p.d ? i : i - p.d] = v;
 }
 
 namespace {
 
-int lanes_of(int d) {
-  int w = 1;
-  while (16 * w < d) w *= 2;
-  return w;
+// Lanes that a head takes: a power of two, four at least.
+int lanes_of(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+
+// All groups of a few tokens to a CTA; the fewer tokens there are, the fewer at a time, until the SMs have a CTA each.
+RotatePlan plan_of(const RotateParams& p, int groups, int most_ctas) {
+  RotatePlan plan;
+  plan.wg = std::min(groups, kRotateWarps);
+  plan.wt = kRotateWarps / plan.wg;
+  const int columns = (groups + plan.wg - 1) / plan.wg;
+  plan.nt = 8;
+  while (plan.nt > 1 && (plan.wt * plan.nt > kTileTokens ||
+                         (p.T + plan.wt * plan.nt - 1) / (plan.wt * plan.nt) * columns < 2 * kCacheSms)) plan.nt /= 2;
+  while (plan.wt > 1 && (p.T + plan.wt - 1) / plan.wt * columns < kCacheSms) --plan.wt;
+  const long long tiles = (p.T + plan.wt * plan.nt - 1) / (plan.wt * plan.nt);
+  plan.ctas = static_cast<int>(std::min<long long>(tiles, std::max(1, most_ctas / columns)));
+  return plan;
 }
 
-template <class T, int W>
-cudaError_t forward(const RotateParams& p, cudaStream_t st) {
-  const int at_once = 32 / W;
-  const int gq = (p.Hq + at_once - 1) / at_once, gk = (p.Hk + at_once - 1) / at_once;
-  const int groups = gq + gk * (p.cache_k != nullptr ? 2 : 1);
-  // few tokens: a warp for each group of heads, until the SMs have some warps each
-  const long long want = static_cast<long long>(kCacheSms) * 32;
-  int parts = 1;
-  if (p.T < want) parts = static_cast<int>(std::min<long long>(groups, (want + p.T - 1) / p.T));
-  const long long ctas = (p.T * parts + kRotateWarps - 1) / kRotateWarps;
-  const dim3 grid(static_cast<unsigned>(std::min<long long>(ctas, kCacheSms * 6)));
-  return launch_chained(rotate_kernel<T, W>, grid, dim3(kRotateThreads), 0, st, p, parts);
-}
+template <class T, int W, bool kInter, bool kNorm>
+struct Rotation {
+  static int groups_of(int heads) { return (heads + 32 / W - 1) / (32 / W); }
+  static size_t table(const RotateParams& p, const RotatePlan& plan) {
+    return sizeof(float) * 2 * 2 * plan.wt * plan.nt * (p.rot / 2);
+  }
+  static cudaError_t forward(const RotateParams& p, cudaStream_t st) {
+    const int groups = groups_of(p.Hq + p.Hk * (p.cache_k != nullptr ? 2 : 1));
+    const RotatePlan plan = plan_of(p, groups, kCacheSms * kRotateCtas * 2);
+    return launch_chained(rotate_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, (groups + plan.wg - 1) / plan.wg),
+                          dim3(plan.wg * plan.wt * 32), table(p, plan), st, p, plan);
+  }
+  static cudaError_t backward(const RotateParams& p, cudaStream_t st) {
+    const int groups = groups_of(p.Hq + p.Hk);
+    const RotatePlan plan = plan_of(p, groups, kRotateMaxParts);
+    const int columns = (groups + plan.wg - 1) / plan.wg;
+    cudaError_t e = launch_chained(rotate_back_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, columns),
+                                   dim3(plan.wg * plan.wt * 32), table(p, plan), st, p, plan);
+    if (e != cudaSuccess || !kNorm) return e;
+    return launch_chained(rotate_gamma_kernel, dim3(p.d / 4), dim3(kRotateThreads), 0, st, p, plan.ctas * columns);
+  }
+};
 
-template <class T, int W>
-cudaError_t backward(const RotateParams& p, cudaStream_t st) {
-  const int ctas = static_cast<int>(std::min<long long>((p.T + kRotateWarps - 1) / kRotateWarps, kRotateMaxParts));
-  cudaError_t e = launch_chained(rotate_back_kernel<T, W>, dim3(ctas), dim3(kRotateThreads), 0, st, p);
-  if (e != cudaSuccess || (p.gamma_q == nullptr && p.gamma_k == nullptr)) return e;
-  return launch_chained(rotate_gamma_kernel, dim3((2 * p.d + 31) / 32), dim3(kRotateThreads), 0, st, p, ctas);
+// what(Rotation<..>) of the lanes a head takes, the layout of its pairs, and whether there is a norm
+template <class T, int W, class What>
+cudaError_t of_layout(const RotateParams& p, const What& what) {
+  if (p.gamma_q != nullptr || p.gamma_k != nullptr)
+    return p.interleaved ? what(Rotation<T, W, true, true>()) : what(Rotation<T, W, false, true>());
+  return p.interleaved ? what(Rotation<T, W, true, false>()) : what(Rotation<T, W, false, false>());
 }
-
-template <class T>
-cudaError_t forward_of(const RotateParams& p, cudaStream_t st) {
+template <class T, class What>
+cudaError_t of_width(const RotateParams& p, const What& what) {
   switch (lanes_of(p.d)) {
-    case 1: return forward<T, 1>(p, st);
-    case 2: return forward<T, 2>(p, st);
-    case 4: return forward<T, 4>(p, st);
-    case 8: return forward<T, 8>(p, st);
-    default: return forward<T, 16>(p, st);
+    case 4: return of_layout<T, 4>(p, what);
+    case 8: return of_layout<T, 8>(p, what);
+    default: return of_layout<T, 16>(p, what);
   }
 }
-
-template <class T>
-cudaError_t backward_of(const RotateParams& p, cudaStream_t st) {
-  switch (lanes_of(p.d)) {
-    case 1: return backward<T, 1>(p, st);
-    case 2: return backward<T, 2>(p, st);
-    case 4: return backward<T, 4>(p, st);
-    case 8: return backward<T, 8>(p, st);
-    default: return backward<T, 16>(p, st);
-  }
+template <class What>
+cudaError_t of_type(int dtype, const RotateParams& p, const What& what) {
+  return dtype == SC_FP16 ? of_width<Fp16>(p, what) : of_width<Bf16>(p, what);
 }
 
 }  // namespace
 
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st) {
-  return dtype == SC_FP16 ? forward_of<Fp16>(p, st) : forward_of<Bf16>(p, st);
+  return of_type(dtype, p, [&](auto r) { return r.forward(p, st); });
 }
 
 cudaError_t launch_rotate_back(const RotateParams& p, int dtype, cudaStream_t st) {
-  return dtype == SC_FP16 ? backward_of<Fp16>(p, st) : backward_of<Bf16>(p, st);
+  return of_type(dtype, p, [&](auto r) { return r.backward(p, st); });
 }
 
 }  // namespace sc
