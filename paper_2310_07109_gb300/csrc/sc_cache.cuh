@@ -66,6 +66,7 @@ struct RotateParams {
   int B, L, Hq, Hk, d;
   long long T;               // B L
   float over_d;              // 1 / d
+  unsigned long long per_row;   // 2^63 / L, rounded up: t / L is the high half of 2 t times it (t < 2^31)
   HeadsIn q, k;              // forward: the heads; backward: the forward call's heads
   HeadsIn dq, dk;            // backward: gradients of the outputs
   HeadsOut q_out, k_out;     // the outputs, or the gradients of the inputs
@@ -96,7 +97,7 @@ struct RotateParams {
   unsigned* done;            // workspace: CTAs that have read len and seen
 };
 
-constexpr int kRotateMaxParts = 1216;   // CTAs of the gradient
+constexpr int kRotateMaxParts = 304;   // CTAs of the gradient
 
 struct AttendParams {
   int B, C, H, Hk, G, T;
@@ -154,6 +155,7 @@ struct EvictParams {
 
 int api_device_sms();
 cudaError_t configure_attend();
+cudaError_t configure_rotate();
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_rotate_back(const RotateParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_attend(const AttendParams& p, int d, int dtype, cudaStream_t st);

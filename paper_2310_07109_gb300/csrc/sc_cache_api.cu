@@ -9,7 +9,10 @@
 namespace sc {
 int api_fail_cuda(const char* what, cudaError_t e);
 int api_ensure_configured();
-cudaError_t configure_cache() { return configure_attend(); }
+cudaError_t configure_cache() {
+  const cudaError_t e = configure_attend();
+  return e == cudaSuccess ? configure_rotate() : e;
+}
 }  // namespace sc
 
 namespace {
@@ -136,6 +139,7 @@ extern "C" int sc_rotate_forward(const sc_rotate_args* a, void* stream) {
   p.B = a->B; p.L = a->L; p.Hq = a->Hq; p.Hk = a->Hk; p.d = a->d;
   p.T = static_cast<long long>(a->B) * a->L;
   p.over_d = 1.f / static_cast<float>(a->d);
+  p.per_row = (1ull << 63) / static_cast<unsigned>(a->L) + 1;
   p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
   p.k = {static_cast<const uint16_t*>(a->K), a->ldk};
   p.q_out = {static_cast<uint16_t*>(a->Q_out), a->ldq_out};
@@ -164,6 +168,7 @@ extern "C" int sc_rotate_backward(const sc_rotate_backward_args* a, void* worksp
   p.B = a->B; p.L = a->L; p.Hq = a->Hq; p.Hk = a->Hk; p.d = a->d;
   p.T = static_cast<long long>(a->B) * a->L;
   p.over_d = 1.f / static_cast<float>(a->d);
+  p.per_row = (1ull << 63) / static_cast<unsigned>(a->L) + 1;
   p.dq = {static_cast<const uint16_t*>(a->dQ_out), a->ldq_out};
   p.dk = {static_cast<const uint16_t*>(a->dK_out), a->ldk_out};
   p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
@@ -200,6 +205,7 @@ extern "C" int sc_cache_append(const sc_cache_append_args* a, void* workspace, s
   p.B = a->B; p.L = a->L; p.Hq = a->H; p.Hk = a->Hk; p.d = a->d;
   p.T = static_cast<long long>(a->B) * a->L;
   p.over_d = 1.f / static_cast<float>(a->d);
+  p.per_row = (1ull << 63) / static_cast<unsigned>(a->L) + 1;
   p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
   p.k = {static_cast<const uint16_t*>(a->K_in), a->ldk};
   p.v = {static_cast<const uint16_t*>(a->V_in), a->ldv};

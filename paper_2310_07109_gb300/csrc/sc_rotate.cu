@@ -14,10 +14,11 @@
 // Each value is read once and written once, but a group of heads takes so few bytes that the instructions
 // it takes count as much.  So all that does not change from token to token is settled before the loop: the
 // heads of a token (queries, keys and, in an append, values) are one list, a warp has one group of 32 / W of
-// them for all its tokens, and a lane the two 16-byte vectors of a head that hold both members of its
-// eight pairs (no exchange between lanes but a norm's sum).  The warps of a CTA have the groups of the same few
-// tokens, whose angles they compute together, one for each pair, whatever the number of heads.  Two tokens go
-// through the stages together, the next two on their way; the arithmetic runs on fp32 pairs.
+// them for all its tokens, and a lane two 16-byte vectors of a head, which hold both members of its eight pairs (no
+// exchange between lanes but a norm's sum) and lie where its neighbours' do (every request has whole sectors).  The warps of a CTA have the groups of the same few
+// tokens, whose angles they compute together, one for each pair, whatever the number of heads.  Each thread copies
+// its own vectors of the next tokens into shared memory of its own (cp.async) while it works on these ones, side
+// by side where all of a warp's are in use; the arithmetic runs on fp32 pairs.
 #include <algorithm>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -30,9 +31,11 @@ namespace sc {
 
 constexpr int kRotateWarps = 8;         // most of a CTA
 constexpr int kRotateThreads = kRotateWarps * 32;
-constexpr int kRotateCtas = 2;          // an SM
+constexpr int kRotateCtas = 2;          // an SM, forward (three leave too few registers: what spills costs half of the time again)
+constexpr int kRotateBackCtas = 2;      // an SM, backward
+constexpr int kWarpTokens = 4;          // most tokens of a warp at a time, forward
+constexpr int kWarpTokensBack = 2;      // backward (twice the vectors)
 constexpr int kTileTokens = 16;         // most tokens of a CTA at a time
-constexpr int kPairsLane = SC_MAX_HEAD_WIDTH / 64;
 
 // How the work is cut: `wg` warps side by side for groups, `wt` for tokens, each `nt` tokens at a time.
 struct RotatePlan {
@@ -120,27 +123,14 @@ __device__ __forceinline__ void load4(const float* from, uint64_t (&v)[4]) {
   v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
 }
 
-// (a, b) -> (a cos - b sin, b cos + a sin), or, backward, (a cos + b sin, b cos - a sin)
-template <bool kBack>
-__device__ __forceinline__ void rotate(uint64_t (&a)[4], uint64_t (&b)[4], const float* cos, const float* sin) {
-  uint64_t c[4], s[4];
-  load4(cos, c);
-  load4(sin, s);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint64_t x = a[i], as = f2_mul(x, s[i]), bs = f2_mul(b[i], s[i]), minus = (kBack ? as : bs) ^ 0x8000000080000000ull;
-    a[i] = f2_fma(x, c[i], kBack ? bs : minus);
-    b[i] = f2_fma(b[i], c[i], kBack ? minus : as);
-  }
-}
-
 // What a lane does for every token.
 struct LaneShare {
   int group, sub, q;   // its warp's group; head of the group and lane of the head
   int head;            // of the list of queries, keys and values; one that there is
   int side, of_side;   // 0 queries, 1 keys, 2 values; the head's number among them
   int va, vb;          // its vectors of the head
-  bool live, turns;    // it has a part of a head; which is rotated
+  bool live;           // it has a part of a head
+  bool turn_a, turn_b; // which is rotated: with the layout of halves all of it or nothing, else vector by vector
   __device__ __forceinline__ LaneShare(const RotateParams& p, const RotatePlan& plan, int w, bool inter, bool append) {
     const int lane = threadIdx.x & 31, at_once = 32 / w, turned = p.Hq + p.Hk, heads = turned + (append ? p.Hk : 0);
     group = blockIdx.y * plan.wg + (threadIdx.x >> 5) % plan.wg;
@@ -150,15 +140,44 @@ struct LaneShare {
     head = min(mine, heads - 1);
     side = head < p.Hq ? 0 : head < turned ? 1 : 2;
     of_side = head - (side == 0 ? 0 : side == 1 ? p.Hq : turned);
-    const int half = p.rot / 16;
-    const bool in = q < p.d / 16;
+    const int lanes = p.d / 16, half = p.rot / 16;
+    const bool in = q < lanes;
     live = in && mine < heads;
-    turns = in && q < half;
-    const bool apart = turns && !inter;
-    va = apart ? q : in ? 2 * q : 0;   // (lanes beyond the head read its start)
-    vb = apart ? q + half : in ? 2 * q + 1 : 0;
+    // halves: vectors q and q + half, and for the rest of the head those behind; else q and q + lanes
+    const bool apart = !inter && q < half;
+    va = !in ? 0 : inter || apart ? q : q + half;   // (lanes beyond the head read its start)
+    vb = !in ? 0 : apart ? q + half : q + lanes;
+    turn_a = in && (inter ? va < 2 * half : apart);
+    turn_b = in && (inter ? vb < 2 * half : apart);
   }
 };
+
+// (a, b) -> (a cos - b sin, b cos + a sin), or, backward, (a cos + b sin, b cos - a sin); row: the token's in the tables
+template <bool kBack, bool kInter>
+__device__ __forceinline__ void rotate(uint64_t (&a)[4], uint64_t (&b)[4], const float* cos, const float* sin, const LaneShare& s) {
+  if (!s.turn_a && !s.turn_b) return;
+  // pairs 8 q ..., or those of the two vectors
+  const int first = kInter ? 4 * s.va : 8 * s.q, then = kInter ? (s.turn_b ? 4 * s.vb : first) : 8 * s.q + 4;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const ulonglong2 c2 = *reinterpret_cast<const ulonglong2*>(cos + (h == 0 ? first : then));
+    const ulonglong2 s2 = *reinterpret_cast<const ulonglong2*>(sin + (h == 0 ? first : then));
+    if (kInter && !(h == 0 ? s.turn_a : s.turn_b)) continue;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = 2 * h + k;
+      const uint64_t c = k == 0 ? c2.x : c2.y, sn = k == 0 ? s2.x : s2.y;
+      const uint64_t x = a[i], as = f2_mul(x, sn), bs = f2_mul(b[i], sn), minus = (kBack ? as : bs) ^ 0x8000000080000000ull;
+      a[i] = f2_fma(x, c, kBack ? bs : minus);
+      b[i] = f2_fma(b[i], c, kBack ? minus : as);
+    }
+  }
+}
+
+// Shared memory: the vectors of two tiles, [warp][tile][token][vector][lane], then two tables of angles.
+__host__ __device__ inline size_t ring_bytes(const RotatePlan& plan, int vectors) {
+  return static_cast<size_t>(plan.wg) * plan.wt * 2 * plan.nt * vectors * 32 * sizeof(uint4);
+}
 
 // The tile of tokens of a CTA: lane i has its token t0 + i's sequence, row, position, and whether it is in use.
 struct TileTokens {
@@ -170,7 +189,7 @@ struct TileTokens {
     bool in = lane < count && t < p.T;
     b = r = pos = 0;
     if (in) {
-      b = static_cast<int>(static_cast<unsigned>(t) / static_cast<unsigned>(p.L));
+      b = static_cast<int>(__umul64hi(static_cast<unsigned long long>(t) * 2, p.per_row));   // t / L
       r = static_cast<int>(static_cast<unsigned>(t) - static_cast<unsigned>(b) * static_cast<unsigned>(p.L));
       pos = append ? __ldg(p.seen + b) + r : p.pos != nullptr ? __ldg(p.pos + t) : r;
       in = p.rows == nullptr || r < __ldg(p.rows + b);
@@ -180,27 +199,24 @@ struct TileTokens {
 };
 
 // The tile's angles, cos and sin of [token][rot / 2]: a warp a token, a lane a pair.
-__device__ __forceinline__ void angles(const RotateParams& p, const TileTokens& at, int count, const unsigned long long (&turn)[kPairsLane],
+__device__ __forceinline__ void angles(const RotateParams& p, const TileTokens& at, int count, const unsigned long long* turn,
                                        float* cos, float* sin) {
   const int lane = threadIdx.x & 31, pairs = p.rot / 2;
   for (int i = threadIdx.x >> 5; i < count; i += blockDim.x >> 5) {
     const long long pos = __shfl_sync(0xffffffffu, at.pos, i);
-#pragma unroll
-    for (int k = 0; k < kPairsLane; ++k) {
-      if (k * 32 + lane >= pairs) break;
+    for (int k = lane; k < pairs; k += 32) {
       const unsigned long long a = turn[k] * static_cast<unsigned long long>(pos);
       const int top = static_cast<int>((a + 0x80000000ull) >> 32);   // of half a turn, in 2^-31
       const float angle = static_cast<float>(top) * 1.4629180792671596e-9f;   // pi 2^-31
-      cos[i * pairs + k * 32 + lane] = p.mscale * __cosf(angle);
-      sin[i * pairs + k * 32 + lane] = p.mscale * __sinf(angle);
+      cos[i * pairs + k] = p.mscale * __cosf(angle);
+      sin[i * pairs + k] = p.mscale * __sinf(angle);
     }
   }
 }
 
-__device__ __forceinline__ void turns_of(const RotateParams& p, unsigned long long (&turn)[kPairsLane]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int k = 0; k < kPairsLane; ++k) turn[k] = k * 32 + lane < p.rot / 2 ? turn_of(__ldg(p.freq + k * 32 + lane)) : 0;
+__device__ __forceinline__ void turns_of(const RotateParams& p, unsigned long long* turn) {
+  for (int k = threadIdx.x; k < p.rot / 2; k += blockDim.x) turn[k] = turn_of(__ldg(p.freq + k));
+  __syncthreads();
 }
 
 // gamma of the lane's first and second members (1 where there is none).
@@ -229,13 +245,15 @@ __device__ __forceinline__ int cache_len(const RotateParams& p, int list) {
 // Forward, and append where cache_k is set.
 template <class T, int W, bool kInter, bool kNorm>
 __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_kernel(const RotateParams p, const RotatePlan plan) {
-  extern __shared__ __align__(16) float table[];   // [2][cos, sin][wt nt][rot / 2]
+  extern __shared__ __align__(16) char raw[];
+  __shared__ unsigned long long turn[SC_MAX_HEAD_WIDTH / 2];
+  float* table = reinterpret_cast<float*>(raw + ring_bytes(plan, 2));   // [2][cos, sin][wt nt][rot / 2]
   pdl_wait();
   pdl_launch_dependents();
   const bool append = p.cache_k != nullptr;
   const LaneShare s(p, plan, W, kInter, append);
   const int count = plan.wt * plan.nt, pairs = p.rot / 2, mine = (threadIdx.x >> 5) / plan.wg * plan.nt;
-  const bool whole = (p.d & (p.d - 1)) == 0 && p.d >= 16 * W;   // no lane is beyond a head
+  const bool beyond = s.q >= p.d / 16;   // (zeros)
   const HeadsIn in = s.side == 0 ? p.q : s.side == 1 ? p.k : p.v;
   const HeadsOut out = s.side == 0 ? p.q_out : p.k_out;
   const bool to_cache = append && s.side > 0;
@@ -243,87 +261,92 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_kernel(con
   uint16_t* dst = !to_cache ? out.p + s.of_side * p.d : (s.side == 1 ? p.cache_k : p.cache_v) + s.of_side * p.stride_h;
   const int of = p.Hk / p.G, list = to_cache ? s.of_side / of : 0;
   const bool marks = to_cache && s.live && s.side == 1 && s.q == 0 && s.of_side % of == 0;
-  unsigned long long turn[kPairsLane];
-  turns_of(p, turn);
   uint64_t ga[4], gb[4];
   const float* gamma = s.side == 0 ? p.gamma_q : s.side == 1 ? p.gamma_k : nullptr;
   if (kNorm) gamma_of(gamma, s, kInter, ga, gb);
-  uint4 va[2] = {}, vb[2] = {};
-  auto load = [&](const TileTokens& at, long long t0, int i) {   // tokens i, i + 1 of the warp's
+  uint4* ring = reinterpret_cast<uint4*>(raw) + (threadIdx.x >> 5) * (2 * plan.nt * 64) + (threadIdx.x & 31);
+  const unsigned every = (1u << plan.nt) - 1;   // a warp's tokens of a tile
+  auto load = [&](const TileTokens& at, long long t0, int half) {
+    uint32_t to = smem_u32(ring + half * plan.nt * 64);
+    const uint16_t *from_a = src + (t0 + mine) * in.ld + 8 * s.va, *from_b = from_a + 8 * (s.vb - s.va);
+    unsigned left = at.used >> mine & every;
+    if (left == (1u << kWarpTokens) - 1) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if (i + u >= plan.nt || !(at.used >> (mine + i + u) & 1u)) continue;
-      const uint4* from = reinterpret_cast<const uint4*>(src + (t0 + mine + i + u) * in.ld);
-      va[u] = from[s.va];
-      vb[u] = from[s.vb];
+      for (int i = 0; i < kWarpTokens; ++i, from_a += in.ld, from_b += in.ld) {
+        cp_async16(to + i * 1024, from_a, !beyond);
+        cp_async16(to + i * 1024 + 512, from_b, !beyond);
+      }
+    } else {
+      for (; left != 0; left >>= 1, to += 1024, from_a += in.ld, from_b += in.ld)
+        if (left & 1u) {
+          cp_async16(to, from_a, !beyond);
+          cp_async16(to + 512, from_b, !beyond);
+        }
     }
+    cp_async_commit();
   };
+  auto token = [&](const uint4* own, const float* cos, const float* sin, const TileTokens& at, int number, uint16_t* to) {
+    const uint4 xa = own[0], xb = own[32];
+    uint64_t a[4], b[4];
+    unpack<T, kInter>(xa, xb, a, b);
+    if (kNorm) {
+      const float ss = squares<W>(a, b);
+      const uint64_t inv = f2_both(gamma != nullptr ? rsqrtf(fmaf(ss, p.over_d, p.eps)) : 1.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a[k] = f2_mul(a[k], f2_mul(ga[k], inv));
+        b[k] = f2_mul(b[k], f2_mul(gb[k], inv));
+      }
+    }
+    rotate<false, kInter>(a, b, cos, sin, s);
+    uint4 ya, yb;
+    pack<T, kInter>(a, b, ya, yb);
+    if (append) {
+      const int b_u = __shfl_sync(0xffffffffu, at.b, number), r_u = __shfl_sync(0xffffffffu, at.r, number);
+      const int pos = __shfl_sync(0xffffffffu, at.pos, number);
+      if (to_cache) {
+        const int c = cache_len(p, b_u * p.G + list) + r_u;
+        if (c >= p.C) return;
+        to = dst + b_u * p.stride_b + c * p.stride_c;
+        if (s.side == 2) {
+          ya = xa;
+          yb = xb;
+        }
+        if (marks) {
+          const long long slot = (static_cast<long long>(b_u) * p.G + list) * p.C + c;
+          p.acc[slot] = 0.f;
+          p.slot_pos[slot] = pos;
+        }
+      }
+    }
+    if (!s.live) return;
+    reinterpret_cast<uint4*>(to)[s.va] = ya;
+    reinterpret_cast<uint4*>(to)[s.vb] = yb;
+  };
+  const long long step = static_cast<long long>(gridDim.x) * count;
   long long t0 = static_cast<long long>(blockIdx.x) * count;
-  int buffer = 0;
-  for (; t0 < p.T; t0 += static_cast<long long>(gridDim.x) * count, buffer ^= 1) {
-    const TileTokens at(p, t0, count, append);
-    load(at, t0, 0);
-    float *cos = table + buffer * 2 * count * pairs, *sin = cos + count * pairs;
+  TileTokens next(p, t0, count, append);
+  load(next, t0, 0);
+  turns_of(p, turn);
+  for (int half = 0; t0 < p.T; t0 += step, half ^= 1) {
+    const TileTokens at = next;
+    next = TileTokens(p, t0 + step, count, append);
+    load(next, t0 + step, half ^ 1);
+    float *cos = table + half * 2 * count * pairs, *sin = cos + count * pairs;
     angles(p, at, count, turn, cos, sin);
+    cp_async_wait<1>();
     __syncthreads();   // (the other table is free when all have come here again)
-    for (int i = 0; i < plan.nt; i += 2) {
-      uint64_t a[2][4], b[2][4];
-      uint4 xa[2], xb[2];
+    cos += mine * pairs;
+    sin += mine * pairs;
+    const uint4* own = ring + half * plan.nt * 64;
+    uint16_t* to = dst + (t0 + mine) * out.ld;
+    unsigned left = at.used >> mine & every;
+    if (left == (1u << kWarpTokens) - 1) {   // all of them, side by side
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (!whole && s.q >= p.d / 16) va[u] = vb[u] = make_uint4(0, 0, 0, 0);
-        xa[u] = va[u];
-        xb[u] = vb[u];
-        unpack<T, kInter>(va[u], vb[u], a[u], b[u]);
-      }
-      load(at, t0, i + 2);
-      if (kNorm) {
-        float ss[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) ss[u] = squares<W>(a[u], b[u]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint64_t inv = f2_both(gamma != nullptr ? rsqrtf(fmaf(ss[u], p.over_d, p.eps)) : 1.f);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            a[u][k] = f2_mul(a[u][k], f2_mul(ga[k], inv));
-            b[u][k] = f2_mul(b[u][k], f2_mul(gb[k], inv));
-          }
-        }
-      }
-      if (s.turns) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int row = (mine + min(i + u, plan.nt - 1)) * pairs + 8 * s.q;
-          rotate<false>(a[u], b[u], cos + row, sin + row);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int token = mine + i + u;
-        const bool used = i + u < plan.nt && (at.used >> token & 1u);
-        const int b_u = __shfl_sync(0xffffffffu, at.b, token & 31), r_u = __shfl_sync(0xffffffffu, at.r, token & 31);
-        if (!used || !s.live) continue;
-        uint4 ya, yb;
-        pack<T, kInter>(a[u], b[u], ya, yb);
-        uint16_t* to = dst + (t0 + token) * out.ld;
-        if (to_cache) {
-          const int c = cache_len(p, b_u * p.G + list) + r_u;
-          if (c >= p.C) continue;
-          to = dst + b_u * p.stride_b + c * p.stride_c;
-          if (s.side == 2) {
-            ya = xa[u];
-            yb = xb[u];
-          }
-          if (marks) {
-            const long long slot = (static_cast<long long>(b_u) * p.G + list) * p.C + c;
-            p.acc[slot] = 0.f;
-            p.slot_pos[slot] = __ldg(p.seen + b_u) + r_u;
-          }
-        }
-        reinterpret_cast<uint4*>(to)[s.va] = ya;
-        reinterpret_cast<uint4*>(to)[s.vb] = yb;
-      }
+      for (int i = 0; i < kWarpTokens; ++i) token(own + i * 64, cos + i * pairs, sin + i * pairs, at, mine + i, to + i * out.ld);
+    } else {
+      for (int i = mine; left != 0; left >>= 1, ++i, own += 64, cos += pairs, sin += pairs, to += out.ld)
+        if (left & 1u) token(own, cos, sin, at, i, to);
     }
   }
   if (!append) return;
@@ -352,9 +375,11 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_kernel(con
 // Gradient.  dgamma: a lane adds up its features of its head over its tokens, the CTA its lanes and warps, in order;
 // the parts of the CTAs (blockIdx.y has groups of its own) are added, in order, by rotate_gamma_kernel.
 template <class T, int W, bool kInter, bool kNorm>
-__global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_back_kernel(const RotateParams p, const RotatePlan plan) {
+__global__ void __launch_bounds__(kRotateThreads, kRotateBackCtas) rotate_back_kernel(const RotateParams p, const RotatePlan plan) {
   constexpr int kAt = 1;   // tokens that go through the stages together (two: registers do not suffice)
-  extern __shared__ __align__(16) float table[];
+  extern __shared__ __align__(16) char raw[];
+  __shared__ unsigned long long turn[SC_MAX_HEAD_WIDTH / 2];
+  float* table = reinterpret_cast<float*>(raw + ring_bytes(plan, 4));
   __shared__ float sums[kRotateWarps][SC_MAX_HEAD_WIDTH];
   pdl_wait();
   pdl_launch_dependents();
@@ -366,50 +391,50 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_back_kerne
   const float* gamma = s.side == 0 ? p.gamma_q : p.gamma_k;
   const uint16_t *src = dy.p + s.of_side * p.d, *src_x = in.p + s.of_side * p.d;
   uint16_t* dst = out.p + s.of_side * p.d;
-  unsigned long long turn[kPairsLane];
-  turns_of(p, turn);
   uint64_t ga[4], gb[4], total[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) total[k] = 0;
   if (kNorm) gamma_of(gamma, s, kInter, ga, gb);
-  uint4 va[kAt] = {}, vb[kAt] = {}, wa[kAt] = {}, wb[kAt] = {};
-  auto load = [&](const TileTokens& at, long long t0, int i) {
-#pragma unroll
-    for (int u = 0; u < kAt; ++u) {
-      if (i + u >= plan.nt || !(at.used >> (mine + i + u) & 1u)) continue;
-      const long long t = t0 + mine + i + u;
-      const uint4* from = reinterpret_cast<const uint4*>(src + t * dy.ld);
-      va[u] = from[s.va];
-      vb[u] = from[s.vb];
-      if (!kNorm || gamma == nullptr) continue;
-      from = reinterpret_cast<const uint4*>(src_x + t * in.ld);
-      wa[u] = from[s.va];
-      wb[u] = from[s.vb];
-    }
+  uint4* ring = reinterpret_cast<uint4*>(raw) + warp * (2 * plan.nt * 128) + (threadIdx.x & 31);
+  auto load = [&](const TileTokens& at, long long t0, int half) {
+    const uint32_t to = smem_u32(ring + half * plan.nt * 128);
+    const uint16_t *from = src + (t0 + mine) * dy.ld, *from_x = src_x + (t0 + mine) * in.ld;
+    for (int i = 0; i < plan.nt; ++i, from += dy.ld, from_x += in.ld)
+      if (at.used >> (mine + i) & 1u) {
+        cp_async16(to + i * 2048, from + 8 * s.va, !beyond);
+        cp_async16(to + i * 2048 + 512, from + 8 * s.vb, !beyond);
+        if (kNorm) {
+          cp_async16(to + i * 2048 + 1024, from_x + 8 * s.va, !beyond && gamma != nullptr);
+          cp_async16(to + i * 2048 + 1536, from_x + 8 * s.vb, !beyond && gamma != nullptr);
+        }
+      }
+    cp_async_commit();
   };
+  const long long step = static_cast<long long>(gridDim.x) * count;
   long long t0 = static_cast<long long>(blockIdx.x) * count;
-  int buffer = 0;
-  for (; t0 < p.T; t0 += static_cast<long long>(gridDim.x) * count, buffer ^= 1) {
-    const TileTokens at(p, t0, count, false);
-    load(at, t0, 0);
-    float *cos = table + buffer * 2 * count * pairs, *sin = cos + count * pairs;
+  TileTokens next(p, t0, count, false);
+  load(next, t0, 0);
+  turns_of(p, turn);
+  for (int half = 0; t0 < p.T; t0 += step, half ^= 1) {
+    const TileTokens at = next;
+    next = TileTokens(p, t0 + step, count, false);
+    load(next, t0 + step, half ^ 1);
+    float *cos = table + half * 2 * count * pairs, *sin = cos + count * pairs;
     angles(p, at, count, turn, cos, sin);
+    cp_async_wait<1>();
     __syncthreads();
     for (int i = 0; i < plan.nt; i += kAt) {
       uint64_t a[kAt][4], b[kAt][4], x[kAt][4], y[kAt][4];
 #pragma unroll
       for (int u = 0; u < kAt; ++u) {
-        if (beyond) va[u] = vb[u] = wa[u] = wb[u] = make_uint4(0, 0, 0, 0);
-        unpack<T, kInter>(va[u], vb[u], a[u], b[u]);
-        if (kNorm) unpack<T, kInter>(wa[u], wb[u], x[u], y[u]);
+        const uint4* own = ring + (half * plan.nt + min(i + u, plan.nt - 1)) * 128;
+        unpack<T, kInter>(own[0], own[32], a[u], b[u]);
+        if (kNorm) unpack<T, kInter>(own[64], own[96], x[u], y[u]);
       }
-      load(at, t0, i + kAt);
-      if (s.turns) {
 #pragma unroll
-        for (int u = 0; u < kAt; ++u) {
-          const int row = (mine + min(i + u, plan.nt - 1)) * pairs + 8 * s.q;
-          rotate<true>(a[u], b[u], cos + row, sin + row);
-        }
+      for (int u = 0; u < kAt; ++u) {
+        const int row = (mine + min(i + u, plan.nt - 1)) * pairs;
+        rotate<true, kInter>(a[u], b[u], cos + row, sin + row, s);
       }
       if (kNorm) {
         float ss[kAt];
@@ -464,7 +489,7 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_back_kerne
       }
     }
   }
-  if (!kNorm) return;
+  if constexpr (kNorm) {
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
 #pragma unroll
@@ -477,7 +502,8 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_back_kerne
 #pragma unroll
         for (int o = W; o < 32; o <<= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
         const int member = 2 * (i & 3) + k, second = i / 4;   // pair of the lane's eight
-        if (!beyond && s.sub == 0) sums[warp][kInter ? 16 * s.q + 2 * member + second : 8 * (second ? s.vb : s.va) + member] = v[k];
+        const int feature = kInter ? 8 * (member < 4 ? s.va : s.vb) + 2 * (member & 3) + second : 8 * (second ? s.vb : s.va) + member;
+        if (!beyond && s.sub == 0) sums[warp][feature] = v[k];
       }
     }
     __syncthreads();
@@ -487,6 +513,7 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_back_kerne
       p.part[((static_cast<long long>(blockIdx.y) * gridDim.x + blockIdx.x) * 2 + side) * p.d + i] = v;
     }
     __syncthreads();
+  }
   }
 }
 
@@ -517,12 +544,12 @@ namespace {
 int lanes_of(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
 // All groups of a few tokens to a CTA; the fewer tokens there are, the fewer at a time, until the SMs have a CTA each.
-RotatePlan plan_of(const RotateParams& p, int groups, int most_ctas) {
+RotatePlan plan_of(const RotateParams& p, int groups, int most_tokens, int most_ctas) {
   RotatePlan plan;
   plan.wg = std::min(groups, kRotateWarps);
   plan.wt = kRotateWarps / plan.wg;
   const int columns = (groups + plan.wg - 1) / plan.wg;
-  plan.nt = 8;
+  plan.nt = most_tokens;
   while (plan.nt > 1 && (plan.wt * plan.nt > kTileTokens ||
                          (p.T + plan.wt * plan.nt - 1) / (plan.wt * plan.nt) * columns < 2 * kCacheSms)) plan.nt /= 2;
   while (plan.wt > 1 && (p.T + plan.wt - 1) / plan.wt * columns < kCacheSms) --plan.wt;
@@ -534,21 +561,28 @@ RotatePlan plan_of(const RotateParams& p, int groups, int most_ctas) {
 template <class T, int W, bool kInter, bool kNorm>
 struct Rotation {
   static int groups_of(int heads) { return (heads + 32 / W - 1) / (32 / W); }
-  static size_t table(const RotateParams& p, const RotatePlan& plan) {
-    return sizeof(float) * 2 * 2 * plan.wt * plan.nt * (p.rot / 2);
+  static size_t bytes(const RotateParams& p, const RotatePlan& plan, int vectors) {
+    return ring_bytes(plan, vectors) + sizeof(float) * 2 * 2 * plan.wt * plan.nt * (p.rot / 2);
+  }
+  static cudaError_t configure() {   // the most: the ring of eight warps, and angles of the most tokens
+    const int ring = kRotateWarps * 2 * kWarpTokens * 2 * 512, angles = 4 * 4 * kTileTokens * (SC_MAX_HEAD_WIDTH / 2);
+    static_assert(kWarpTokens * 2 == kWarpTokensBack * 4, "the same bytes backward");
+    const cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T, W, kInter, kNorm>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring + angles);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(rotate_back_kernel<T, W, kInter, kNorm>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring + angles);
   }
   static cudaError_t forward(const RotateParams& p, cudaStream_t st) {
     const int groups = groups_of(p.Hq + p.Hk * (p.cache_k != nullptr ? 2 : 1));
-    const RotatePlan plan = plan_of(p, groups, kCacheSms * kRotateCtas * 2);
+    const RotatePlan plan = plan_of(p, groups, kWarpTokens, kCacheSms * kRotateCtas);
     return launch_chained(rotate_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, (groups + plan.wg - 1) / plan.wg),
-                          dim3(plan.wg * plan.wt * 32), table(p, plan), st, p, plan);
+                          dim3(plan.wg * plan.wt * 32), bytes(p, plan, 2), st, p, plan);
   }
   static cudaError_t backward(const RotateParams& p, cudaStream_t st) {
     const int groups = groups_of(p.Hq + p.Hk);
-    const RotatePlan plan = plan_of(p, groups, kRotateMaxParts);
+    const RotatePlan plan = plan_of(p, groups, kWarpTokensBack, kCacheSms * kRotateBackCtas);
     const int columns = (groups + plan.wg - 1) / plan.wg;
     cudaError_t e = launch_chained(rotate_back_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, columns),
-                                   dim3(plan.wg * plan.wt * 32), table(p, plan), st, p, plan);
+                                   dim3(plan.wg * plan.wt * 32), bytes(p, plan, 4), st, p, plan);
     if (e != cudaSuccess || !kNorm) return e;
     return launch_chained(rotate_gamma_kernel, dim3(p.d / 4), dim3(kRotateThreads), 0, st, p, plan.ctas * columns);
   }
@@ -575,6 +609,21 @@ cudaError_t of_type(int dtype, const RotateParams& p, const What& what) {
 }
 
 }  // namespace
+
+cudaError_t configure_rotate() {
+  static const float some = 1.f;
+  for (int dtype : {SC_BF16, SC_FP16})
+    for (int d : {64, 128, 256})
+      for (int kind = 0; kind < 4; ++kind) {
+        RotateParams p{};
+        p.d = d;
+        p.interleaved = kind & 1;
+        p.gamma_q = kind & 2 ? &some : nullptr;
+        const cudaError_t e = of_type(dtype, p, [](auto r) { return r.configure(); });
+        if (e != cudaSuccess) return e;
+      }
+  return cudaSuccess;
+}
 
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st) {
   return of_type(dtype, p, [&](auto r) { return r.forward(p, st); });
