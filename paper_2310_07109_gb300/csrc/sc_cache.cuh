@@ -131,6 +131,7 @@ struct AttendParams {
 };
 
 constexpr int kFewRows = 16;                 // most rows a key head that the kernel for few rows takes
+constexpr int kStoredRows = 32;              // most rows whose scores are kept for the sums of the weights
 constexpr int kFewTile = 16;                 // slots a warp takes at a time
 constexpr int kFewMinTiles = 2;              // fewest tiles of a warp
 constexpr int few_warps_sm(int d) { return d == 64 ? 12 : 8; }

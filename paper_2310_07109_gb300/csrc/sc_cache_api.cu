@@ -60,10 +60,11 @@ struct CacheLayout {
   long long pair_pitch;
 };
 
-// Parts that the attention takes a list in: until the GPU has two CTAs an SM, parts of 256 slots at least.
-int splits_of(int B, int C, int Hk, int M) {
+// Parts that the attention takes a list in: as many CTAs as SMs have room for (three, two of wide heads), parts of 256
+// slots at least.
+int splits_of(int B, int C, int Hk, int M, int d) {
   const long long ctas = static_cast<long long>(B) * Hk * ((M + kRowsTile - 1) / kRowsTile);
-  const long long want = std::max<long long>(1, 2 * kCacheSms / ctas);
+  const long long want = std::max<long long>(1, (d == 64 ? 3 : 2) * kCacheSms / ctas);
   return static_cast<int>(std::min<long long>(want, (C + 255) / 256));
 }
 
@@ -73,9 +74,9 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   CacheLayout w;
   const size_t units = static_cast<size_t>(B) * Hk, lists = static_cast<size_t>(B) * G;
   const size_t M = static_cast<size_t>(T) * (H / Hk);
-  const bool few = M <= kFewRows;
+  const bool few = M <= kFewRows, stored = M <= kStoredRows;
   // no more warps than the most tiles give work to
-  w.splits = few ? 1 : splits_of(B, C, Hk, static_cast<int>(M));
+  w.splits = few ? 1 : splits_of(B, C, Hk, static_cast<int>(M), d);
   const size_t tiles = units * ((C + kFewTile - 1) / kFewTile);
   const size_t cta = kFewMinTiles * few_warps_sm(d);   // fewest tiles of a CTA
   w.warps = static_cast<int>(std::min<size_t>(kCacheSms, (tiles + cta - 1) / cta)) * few_warps_sm(d);
@@ -83,7 +84,7 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   const size_t parts = few ? w.warps + units : units * w.splits;
   w.lse = w.share = kAlign;
   w.scores = align_up(w.share + sizeof(int) * (1 + units));
-  w.ml = few ? align_up(w.scores + sizeof(float) * units * M * w.pitch) : align_up(w.lse + sizeof(float) * units * M);
+  w.ml = stored ? align_up(w.scores + sizeof(float) * units * M * w.pitch) : align_up(w.lse + sizeof(float) * units * M);
   w.part = align_up(w.ml + sizeof(float2) * parts * M);
   const size_t attend = align_up(w.part + sizeof(float) * parts * M * d);
   w.pair_pitch = C / 2 + 1;

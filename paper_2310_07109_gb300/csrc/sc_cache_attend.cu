@@ -62,10 +62,20 @@ __device__ __forceinline__ ListOf list_of(const AttendParams& p, int b, int g) {
   return l;
 }
 
+// A lane's scores of slots j, j + 1 for the rows m0 + lane / 4 and that + 8 (the pitch is even: the second has room).
+__device__ __forceinline__ void store_scores(const AttendParams& p, float* of_unit, int m0, int rows_m, int j, int n, const float (&c)[4]) {
+  if (j >= n) return;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int m = m0 + static_cast<int>(threadIdx.x & 31) / 4 + 8 * u;
+    if (m < rows_m) *reinterpret_cast<float2*>(of_unit + static_cast<long long>(m) * p.pitch + j) = make_float2(c[2 * u], c[2 * u + 1]);
+  }
+}
+
 // Rows m0 .. of key head hk into a tile; zeros beyond the rows in use.
 template <int D>
-__device__ __forceinline__ void load_q(const AttendParams& p, int b, int hk, int m0, int rows, uint32_t base) {
-  for (int i = threadIdx.x; i < kRowTile * (D / 8); i += kAttendThreads) {
+__device__ __forceinline__ void load_q(const AttendParams& p, int b, int hk, int m0, int rows, int tile_rows, uint32_t base) {
+  for (int i = threadIdx.x; i < tile_rows * (D / 8); i += kAttendThreads) {
     const int row = i / (D / 8), c = i % (D / 8), m = m0 + row;
     const int tok = m / p.R, h = hk * p.R + m % p.R;
     const bool live = m < p.M && tok < rows;
@@ -84,44 +94,54 @@ __device__ __forceinline__ void load_keys(const AttendParams& p, const uint16_t*
   }
 }
 
+// Tiles on their way: as many as let an SM have kRowsCtas CTAs.
 template <int D>
 struct RowsSmem {
+  static constexpr int kStages = D == 64 ? 4 : 3;
   alignas(128) uint16_t q[kRowTile * D];
-  alignas(128) uint16_t k[2][kKeyTile * D];
-  alignas(128) uint16_t v[2][kKeyTile * D];
-  int pos[2][kKeyTile];
+  alignas(128) uint16_t k[kStages][kKeyTile * D];
+  alignas(128) uint16_t v[kStages][kKeyTile * D];
+  int pos[kStages][kKeyTile];
 };
 
-template <class T, int D>
+// kGroups 2: at most 32 rows, which two warps have for the first half of each tile's slots and two for the second.
+template <class T, int D, int kGroups>
 __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const AttendParams p) {
+  constexpr int kStages = RowsSmem<D>::kStages, kKeys = kKeyTile / kGroups, kRowWarps = kAttendWarps / kGroups;
+  constexpr int kRows = 16 * kRowWarps;
   extern __shared__ char raw[];
   RowsSmem<D>& sm = *reinterpret_cast<RowsSmem<D>*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~uintptr_t(127));
   pdl_wait();
   pdl_launch_dependents();
-  const int tiles_m = (p.M + kRowTile - 1) / kRowTile;
+  const int tiles_m = (p.M + kRows - 1) / kRows;
   long long id = blockIdx.x;
   const int split = static_cast<int>(id % p.splits);
   id /= p.splits;
-  const int m0 = static_cast<int>(id % tiles_m) * kRowTile;
+  const int m0 = static_cast<int>(id % tiles_m) * kRows;
   id /= tiles_m;
   const int hk = static_cast<int>(id % p.Hk), b = static_cast<int>(id / p.Hk);
   const int g = hk / (p.Hk / p.G);
   const ListOf l = list_of(p, b, g);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row0 = warp % kRowWarps * 16, key0 = warp / kRowWarps * kKeys;   // of the tiles
+  const int rows_m = l.rows * p.R;
   const int tiles = (l.n + kKeyTile - 1) / kKeyTile, per = (tiles + p.splits - 1) / p.splits;
-  const int t0 = min(split * per, tiles), t1 = m0 < l.rows * p.R ? min(t0 + per, tiles) : t0;
+  const int t0 = min(split * per, tiles), t1 = m0 < rows_m ? min(t0 + per, tiles) : t0;
   const uint16_t* kh = p.k + b * p.stride_b + hk * p.stride_h;
   const uint16_t* vh = p.v + b * p.stride_b + hk * p.stride_h;
   const int32_t* pos = p.pos + (static_cast<long long>(b) * p.G + g) * p.C;
   const uint32_t sq = smem_u32(sm.q);
+  float* scores = p.scores + (static_cast<long long>(b) * p.Hk + hk) * p.M * p.pitch;
 
-  auto load = [&](int tile, int s) {
-    const int j0 = tile * kKeyTile;
-    load_keys<D>(p, kh, j0, l.n, smem_u32(sm.k[s]));
-    load_keys<D>(p, vh, j0, l.n, smem_u32(sm.v[s]));
-    if (threadIdx.x < kKeyTile) {
-      const int j = j0 + threadIdx.x;
-      cp_async4(smem_u32(&sm.pos[s][threadIdx.x]), pos + min(j, l.n - 1), j < l.n);
+  auto load = [&](int tile) {
+    if (tile < t1) {
+      const int j0 = tile * kKeyTile, s = (tile - t0) % kStages;
+      load_keys<D>(p, kh, j0, l.n, smem_u32(sm.k[s]));
+      load_keys<D>(p, vh, j0, l.n, smem_u32(sm.v[s]));
+      if (threadIdx.x < kKeyTile) {
+        const int j = j0 + threadIdx.x;
+        cp_async4(smem_u32(&sm.pos[s][threadIdx.x]), pos + min(j, l.n - 1), j < l.n);
+      }
     }
     cp_async_commit();
   };
@@ -134,61 +154,69 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
     for (int k = 0; k < 4; ++k) o[i][k] = 0.f;
   int at[2];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) at[u] = l.first + (m0 + warp * 16 + (lane >> 2) + 8 * u) / p.R;
-  const int last = l.first + min(m0 + kRowTile - 1, l.rows * p.R - 1) / p.R;   // the latest row of the tile
+  for (int u = 0; u < 2; ++u) at[u] = l.first + (m0 + row0 + (lane >> 2) + 8 * u) / p.R;
+  const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R;   // the latest row of the tile
 
-  if (t0 < t1) {
-    load_q<D>(p, b, hk, m0, l.rows, sq);
-    load(t0, 0);
-  }
+  if (t0 < t1) load_q<D>(p, b, hk, m0, l.rows, kRows, sq);
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) load(t0 + i);
   for (int tile = t0; tile < t1; ++tile) {
-    const int s = (tile - t0) & 1;
-    if (tile + 1 < t1) {
-      load(tile + 1, s ^ 1);
-      cp_async_wait<1>();
-    } else {
-      cp_async_wait<0>();
-    }
+    const int s = (tile - t0) % kStages;
+    cp_async_wait<kStages - 2>();
     // a slot that no row of the tile sees may hold anything: its V is taken as 0
     bool unseen = false;
     if (threadIdx.x < kKeyTile) {
       const int at_key = sm.pos[s][threadIdx.x];
-      unseen = tile * kKeyTile + threadIdx.x < l.n && (at_key < 0 || at_key > last);
+      unseen = tile * kKeyTile + static_cast<int>(threadIdx.x) >= l.n || at_key < 0 || at_key > last;
     }
-    if (__syncthreads_or(unseen)) {
+    const int hidden = __syncthreads_count(unseen);   // (and the tile before this one is done with)
+    load(tile + kStages - 1);
+    if (hidden == kKeyTile) {
+      if (kGroups == 2) {   // (the sums read every score)
+        const int j = tile * kKeyTile + static_cast<int>(threadIdx.x) % kKeyTile;
+        for (int m = m0 + threadIdx.x / kKeyTile; m < rows_m && j < l.n; m += kAttendThreads / kKeyTile)
+          scores[static_cast<long long>(m) * p.pitch + j] = -INFINITY;
+      }
+      continue;
+    }
+    if (hidden != 0) {
       if (unseen)
         for (int c = 0; c < D / 8; ++c)
           *reinterpret_cast<uint4*>(reinterpret_cast<char*>(sm.v[s]) + threadIdx.x * D * 2 + c * 16) = make_uint4(0, 0, 0, 0);
       __syncthreads();
     }
+    if (m0 + row0 >= rows_m) continue;   // a warp without rows
     const uint32_t sk = smem_u32(sm.k[s]), sv = smem_u32(sm.v[s]);
-    float c[kKeyTile / 8][4];
+    float c[kKeys / 8][4];
 #pragma unroll
-    for (int i = 0; i < kKeyTile / 8; ++i)
+    for (int i = 0; i < kKeys / 8; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k) c[i][k] = 0.f;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       uint32_t a[4];
-      load_a<D>(sq, warp * 16, k, lane, a);
+      load_a<D>(sq, row0, k, lane, a);
 #pragma unroll
-      for (int n = 0; n < kKeyTile / 16; ++n) {
+      for (int n = 0; n < kKeys / 16; ++n) {
         uint32_t f[4];
-        load_b<D>(sk, n * 16, k, lane, f);
+        load_b<D>(sk, key0 + n * 16, k, lane, f);
         T::mma(c[2 * n], a, f[0], f[1]);
         T::mma(c[2 * n + 1], a, f[2], f[3]);
       }
     }
     float top[2] = {ref[0], ref[1]};
 #pragma unroll
-    for (int i = 0; i < kKeyTile / 8; ++i) {
+    for (int i = 0; i < kKeys / 8; ++i) {
+      const int key = key0 + 8 * i + 2 * (lane & 3);
+      const int2 where = *reinterpret_cast<const int2*>(&sm.pos[s][key]);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int key = 8 * i + 2 * (lane & 3) + (k & 1), where = sm.pos[s][key];
-        const bool sees = tile * kKeyTile + key < l.n && where >= 0 && where <= at[k >> 1];
+        const int w = k & 1 ? where.y : where.x;
+        const bool sees = tile * kKeyTile + key + (k & 1) < l.n && w >= 0 && w <= at[k >> 1];
         c[i][k] = sees ? c[i][k] * p.scale2 : -INFINITY;
         top[k >> 1] = fmaxf(top[k >> 1], c[i][k] - T::kHeadroom);
       }
+      if (kGroups == 2) store_scores(p, scores, m0 + row0, rows_m, tile * kKeyTile + key, l.n, c[i]);
     }
     float keep[2];
 #pragma unroll
@@ -200,41 +228,80 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
       sum[u] *= keep[u];
       top[u] = top[u] == -INFINITY ? 0.f : top[u];
     }
+    if (__any_sync(0xffffffffu, keep[0] != 1.f || keep[1] != 1.f)) {
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      o[i][0] *= keep[0];
-      o[i][1] *= keep[0];
-      o[i][2] *= keep[1];
-      o[i][3] *= keep[1];
+      for (int i = 0; i < D / 8; ++i) {
+        o[i][0] *= keep[0];
+        o[i][1] *= keep[0];
+        o[i][2] *= keep[1];
+        o[i][3] *= keep[1];
+      }
     }
 #pragma unroll
-    for (int i = 0; i < kKeyTile / 8; ++i) {
+    for (int i = 0; i < kKeys / 8; ++i) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) c[i][k] = ex2(c[i][k] - top[k >> 1]);
       sum[0] += c[i][0] + c[i][1];
       sum[1] += c[i][2] + c[i][3];
     }
 #pragma unroll
-    for (int k = 0; k < kKeyTile / 16; ++k) {
+    for (int k = 0; k < kKeys / 16; ++k) {
       const uint32_t a[4] = {T::pack(c[2 * k][0], c[2 * k][1]), T::pack(c[2 * k][2], c[2 * k][3]),
                              T::pack(c[2 * k + 1][0], c[2 * k + 1][1]), T::pack(c[2 * k + 1][2], c[2 * k + 1][3])};
 #pragma unroll
       for (int n = 0; n < D / 16; ++n) {
         uint32_t f[4];
-        load_v<D>(sv, k * 16, n, lane, f);
+        load_v<D>(sv, key0 + k * 16, n, lane, f);
         T::mma(o[2 * n], a, f[0], f[1]);
         T::mma(o[2 * n + 1], a, f[2], f[3]);
       }
     }
-    __syncthreads();   // the stage is free
   }
-  const long long unit = static_cast<long long>(b) * p.Hk + hk;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 1);
     sum[u] += __shfl_xor_sync(0xffffffffu, sum[u], 2);
-    const int m = m0 + warp * 16 + (lane >> 2) + 8 * u;
-    if (m >= l.rows * p.R) continue;
+  }
+  if (kGroups == 2) {   // the second half's warps hand theirs over
+    cp_async_wait_all();
+    __syncthreads();
+    constexpr int kPitch = D + 8;
+    float2* ends = reinterpret_cast<float2*>(sm.v);
+    float* part = reinterpret_cast<float*>(sm.k);
+    static_assert(sizeof(sm.k) >= kRows * kPitch * 4, "room for the second half's O");
+    if (warp >= kRowWarps) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int m = row0 + (lane >> 2) + 8 * u;
+        if ((lane & 3) == 0) ends[m] = make_float2(ref[u], sum[u]);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+          *reinterpret_cast<float2*>(part + m * kPitch + 8 * i + 2 * (lane & 3)) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
+      }
+    }
+    __syncthreads();
+    if (warp >= kRowWarps) return;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int m = row0 + (lane >> 2) + 8 * u;
+      const float2 end = ends[m];
+      const float top = fmaxf(ref[u], end.x);
+      const float mine = ref[u] == top ? 1.f : ex2(ref[u] - top), other = end.x == top ? 1.f : ex2(end.x - top);
+      ref[u] = top;
+      sum[u] = mine * sum[u] + other * end.y;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        const float2 f = *reinterpret_cast<const float2*>(part + m * kPitch + 8 * i + 2 * (lane & 3));
+        o[i][2 * u] = mine * o[i][2 * u] + other * f.x;
+        o[i][2 * u + 1] = mine * o[i][2 * u + 1] + other * f.y;
+      }
+    }
+  }
+  const long long unit = static_cast<long long>(b) * p.Hk + hk;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int m = m0 + row0 + (lane >> 2) + 8 * u;
+    if (m >= rows_m) continue;
     const long long at_row = (unit * p.splits + split) * p.M + m;
     if ((lane & 3) == 0) p.ml[at_row] = make_float2(ref[u], sum[u]);
 #pragma unroll
@@ -286,103 +353,134 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const Atte
   if (lane == 0) p.lse[row] = none ? INFINITY : ref + log2f(total);
 }
 
+// Slots of a CTA of the sums: four tiles, or two of wider heads.
+constexpr int sum_tiles(int d) { return d == 64 ? 4 : 2; }
 template <int D>
 struct SumsSmem {
-  alignas(128) uint16_t k[kKeyTile * D];
+  static constexpr int kTiles = sum_tiles(D), kSlots = kTiles * kKeyTile;
+  alignas(128) uint16_t k[kSlots * D];
   alignas(128) uint16_t q[2][kRowTile * D];
-  int pos[kKeyTile];
-  float sum[kAttendWarps][kKeyTile];
+  int pos[kSlots];
+  int least[kTiles];   // the least position of each tile's slots
+  float sum[kAttendWarps][kSlots];   // by 16 rows of a row tile
 };
 
-// A CTA has a tile of a list's slots: the weights of all rows of the list's heads.
+// A CTA has a stretch of a list's slots: the weights of all rows of the list's heads.  The keys of a head stay in shared memory
+// while its rows pass, a tile of them at a time.
 template <class T, int D>
 __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const AttendParams p) {
+  using S = SumsSmem<D>;
+  constexpr int kRows = kRowTile;
   extern __shared__ char raw[];
-  SumsSmem<D>& sm = *reinterpret_cast<SumsSmem<D>*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~uintptr_t(127));
+  S& sm = *reinterpret_cast<S*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~uintptr_t(127));
   pdl_wait();
   pdl_launch_dependents();
-  const int tiles = (p.C + kKeyTile - 1) / kKeyTile;
-  const int tile = blockIdx.x % tiles, list = blockIdx.x / tiles, b = list / p.G, g = list - b * p.G;
+  const int pieces = (p.C + S::kSlots - 1) / S::kSlots;
+  const int piece = blockIdx.x % pieces, list = blockIdx.x / pieces, b = list / p.G, g = list - b * p.G;
   const ListOf l = list_of(p, b, g);
-  const int j0 = tile * kKeyTile, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int j0 = piece * S::kSlots, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (j0 >= l.n) return;
   const long long at0 = static_cast<long long>(list) * p.C + j0;
   if (l.rows == 0) {
-    if (threadIdx.x < kKeyTile && j0 + threadIdx.x < l.n) p.acc_out[at0 + threadIdx.x] = p.acc[at0 + threadIdx.x];
+    for (int j = threadIdx.x; j < S::kSlots && j0 + j < l.n; j += kAttendThreads) p.acc_out[at0 + j] = p.acc[at0 + j];
     return;
   }
-  const int of = p.Hk / p.G, rows_m = l.rows * p.R, tiles_m = (rows_m + kRowTile - 1) / kRowTile;
-  if (threadIdx.x < kKeyTile) {
-    const int j = j0 + threadIdx.x;
-    sm.pos[threadIdx.x] = j < l.n ? __ldg(p.pos + at0 + threadIdx.x) : -1;
-  }
-  float sum[kKeyTile / 8][2] = {};   // this lane's keys 2 (lane & 3), + 1 of each eight
+  const int of = p.Hk / p.G, rows_m = l.rows * p.R, tiles_m = (rows_m + kRows - 1) / kRows;
+  const int row0 = warp * 16, tiles = min(S::kTiles, (l.n - j0 + kKeyTile - 1) / kKeyTile);
   const int steps = of * tiles_m;
   auto load = [&](int step) {
-    load_q<D>(p, b, g * of + step / tiles_m, step % tiles_m * kRowTile, l.rows, smem_u32(sm.q[step & 1]));
-    cp_async_commit();
+    load_q<D>(p, b, g * of + step / tiles_m, step % tiles_m * kRows, l.rows, kRows, smem_u32(sm.q[step & 1]));
+  };
+  auto keys = [&](int hk) {
+    for (int t = 0; t < tiles; ++t)
+      load_keys<D>(p, p.k + b * p.stride_b + hk * p.stride_h, j0 + t * kKeyTile, l.n, smem_u32(sm.k + t * kKeyTile * D));
   };
   load(0);
+  keys(g * of);
+  cp_async_commit();
+  for (int t = warp; t < S::kTiles; t += kAttendWarps) {
+    int least = 0x7fffffff;
+    for (int j = t * kKeyTile + lane; j < (t + 1) * kKeyTile; j += 32) {
+      const int where = j0 + j < l.n ? __ldg(p.pos + at0 + j) : -1;
+      sm.pos[j] = where < 0 ? 0x7fffffff : where;   // (seen by no row)
+      least = min(least, sm.pos[j]);
+    }
+    least = __reduce_min_sync(0xffffffffu, least);
+    if (lane == 0) sm.least[t] = least;
+  }
+  for (int i = threadIdx.x; i < kAttendWarps * S::kSlots; i += kAttendThreads) (&sm.sum[0][0])[i] = 0.f;
   for (int step = 0; step < steps; ++step) {
-    const int hk = g * of + step / tiles_m, m0 = step % tiles_m * kRowTile;
-    if (step % tiles_m == 0) {
-      load_keys<D>(p, p.k + b * p.stride_b + hk * p.stride_h, j0, l.n, smem_u32(sm.k));
-      cp_async_commit();
-    }
-    cp_async_wait<0>();
-    __syncthreads();
-    if (step + 1 < steps) load(step + 1);
-    const uint32_t sq = smem_u32(sm.q[step & 1]), sk = smem_u32(sm.k);
-    float c[kKeyTile / 8][4];
-#pragma unroll
-    for (int i = 0; i < kKeyTile / 8; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) c[i][k] = 0.f;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      uint32_t a[4];
-      load_a<D>(sq, warp * 16, k, lane, a);
-#pragma unroll
-      for (int n = 0; n < kKeyTile / 16; ++n) {
-        uint32_t f[4];
-        load_b<D>(sk, n * 16, k, lane, f);
-        T::mma(c[2 * n], a, f[0], f[1]);
-        T::mma(c[2 * n + 1], a, f[2], f[3]);
-      }
-    }
+    const int hk = g * of + step / tiles_m, m0 = step % tiles_m * kRows;
     float lse[2];
     int at[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int m = m0 + warp * 16 + (lane >> 2) + 8 * u;
+      const int m = m0 + row0 + (lane >> 2) + 8 * u;
       lse[u] = m < rows_m ? p.lse[(static_cast<long long>(b) * p.Hk + hk) * p.M + m] : INFINITY;
       at[u] = m < rows_m ? l.first + m / p.R : -1;
     }
-#pragma unroll
-    for (int i = 0; i < kKeyTile / 8; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int where = sm.pos[8 * i + 2 * (lane & 3) + (k & 1)];
-        if (where >= 0 && where <= at[k >> 1]) sum[i][k & 1] += ex2(c[i][k] * p.scale2 - lse[k >> 1]);
-      }
+    cp_async_wait_all();
     __syncthreads();
-  }
+    if (step + 1 < steps) load(step + 1);
+    cp_async_commit();
+    const uint32_t sq = smem_u32(sm.q[step & 1]);
+    const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R;
+    if (m0 + row0 < rows_m) {
+      uint32_t a[D / 16][4];
 #pragma unroll
-  for (int i = 0; i < kKeyTile / 8; ++i)
+      for (int k = 0; k < D / 16; ++k) load_a<D>(sq, row0, k, lane, a[k]);
+      for (int t = 0; t < tiles; ++t) {
+        if (sm.least[t] > last) continue;
+        const uint32_t sk = smem_u32(sm.k + t * kKeyTile * D);
+        float c[kKeyTile / 8][4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float v = sum[i][k];
-      v += __shfl_xor_sync(0xffffffffu, v, 4);
-      v += __shfl_xor_sync(0xffffffffu, v, 8);
-      v += __shfl_xor_sync(0xffffffffu, v, 16);
-      if (lane < 4) sm.sum[warp][8 * i + 2 * lane + k] = v;
+        for (int i = 0; i < kKeyTile / 8; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) c[i][k] = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (int n = 0; n < kKeyTile / 16; ++n) {
+            uint32_t f[4];
+            load_b<D>(sk, n * 16, k, lane, f);
+            T::mma(c[2 * n], a[k], f[0], f[1]);
+            T::mma(c[2 * n + 1], a[k], f[2], f[3]);
+          }
+#pragma unroll
+        for (int i = 0; i < kKeyTile / 8; ++i) {
+          const int key = t * kKeyTile + 8 * i + 2 * (lane & 3);
+          const int2 where = *reinterpret_cast<const int2*>(&sm.pos[key]);
+          float v[2];
+          // (a NaN of an unseen slot is kept out by the choice, not by a product)
+          v[0] = (where.x <= at[0] ? ex2(c[i][0] * p.scale2 - lse[0]) : 0.f) + (where.x <= at[1] ? ex2(c[i][2] * p.scale2 - lse[1]) : 0.f);
+          v[1] = (where.y <= at[0] ? ex2(c[i][1] * p.scale2 - lse[0]) : 0.f) + (where.y <= at[1] ? ex2(c[i][3] * p.scale2 - lse[1]) : 0.f);
+          // over the eight pairs of rows; each of them keeps two of the sums' sixteen columns
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            v[k] += __shfl_xor_sync(0xffffffffu, v[k], 4);
+            v[k] += __shfl_xor_sync(0xffffffffu, v[k], 8);
+            v[k] += __shfl_xor_sync(0xffffffffu, v[k], 16);
+          }
+          if (lane < 4) {
+            float2* to = reinterpret_cast<float2*>(&sm.sum[warp][key]);
+            const float2 old = *to;
+            *to = make_float2(old.x + v[0], old.y + v[1]);
+          }
+        }
+      }
     }
+    if (step + 1 < steps && (step + 1) % tiles_m == 0) {   // the next head's keys
+      __syncthreads();
+      keys(hk + 1);
+      cp_async_commit();
+    }
+  }
   __syncthreads();
-  if (threadIdx.x < kKeyTile && j0 + threadIdx.x < l.n) {
+  for (int j = threadIdx.x; j < S::kSlots && j0 + j < l.n; j += kAttendThreads) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < kAttendWarps; ++w) v += sm.sum[w][threadIdx.x];
-    p.acc_out[at0 + threadIdx.x] = p.decay * p.acc[at0 + threadIdx.x] + v / static_cast<float>(p.H / p.G);
+    for (int w = 0; w < kAttendWarps; ++w) v += sm.sum[w][j];
+    p.acc_out[at0 + j] = p.decay * p.acc[at0 + j] + v / static_cast<float>(p.H / p.G);
   }
 }
 
@@ -581,13 +679,7 @@ __global__ void __launch_bounds__(FewShape<D>::kThreads, 1) attend_few_kernel(co
         c[i][k] = sees ? c[i][k] * p.scale2 : -INFINITY;
         top[k >> 1] = fmaxf(top[k >> 1], c[i][k] - T::kHeadroom);
       }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int m = (lane >> 2) + 8 * u;
-        if (m < rows_m && j0 + key < n)   // (pitch is even: the second slot has room)
-          *reinterpret_cast<float2*>(p.scores + (static_cast<long long>(unit) * p.M + m) * p.pitch + j0 + key) =
-              make_float2(c[i][2 * u], c[i][2 * u + 1]);
-      }
+      store_scores(p, p.scores + static_cast<long long>(unit) * p.M * p.pitch, 0, rows_m, j0 + key, n, c[i]);
     }
     bool moved = false;
 #pragma unroll
@@ -719,15 +811,29 @@ struct Pieces {
   }
 };
 
+// The parts that CTAs of at most 32 rows make of a unit.
+struct SplitPieces {
+  int unit, count;
+  __device__ __forceinline__ SplitPieces(int unit_, int splits) : unit(unit_), count(splits) {}
+  __device__ __forceinline__ long long at(int i) const { return static_cast<long long>(unit) * count + i; }
+};
+// kWarps: of attend_few_kernel's CTAs, or 0 for the parts of attend_rows_kernel
+template <int kWarps>
+__device__ __forceinline__ auto parts_of(const AttendParams& p, int unit, int n, int share) {
+  if constexpr (kWarps == 0)
+    return SplitPieces(unit, p.splits);
+  else
+    return Pieces<kWarps>(unit, n, share, __ldcg(p.share + 1 + unit));
+}
+
 // The first `row_ctas` CTAs join a row each; the others have kSumSlots slots of a list each, whose weights
 // they add up over the list's rows from the scores and the rows' LSE.
 constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32;
 constexpr int kSumSlots = kSumThreads * 2;
 constexpr int kSumAhead = 8;
 constexpr int kSumRows = kSumThreads / 8;   // rows whose LSE are found at once, by eight lanes each
-template <class T, int D>
-__global__ void __launch_bounds__(kSumThreads, 8) attend_few_join_kernel(const AttendParams p, int row_ctas) {
-  using Parts = Pieces<FewShape<D>::kWarps>;
+template <class T, int D, int kWarps>
+__global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(const AttendParams p, int row_ctas) {
   constexpr int kOwn = D / 32;
   __shared__ float part[kSumWarps][D];
   __shared__ float2 ends[kSumWarps];
@@ -735,13 +841,13 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_few_join_kernel(const A
   pdl_wait();
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int share = __ldcg(p.share);
+  const int share = kWarps != 0 ? __ldcg(p.share) : 0;
   if (static_cast<int>(blockIdx.x) < row_ctas) {
     const int unit = static_cast<int>(blockIdx.x) / p.M, m = static_cast<int>(blockIdx.x) - unit * p.M;
-    const int b = unit / p.Hk, hk = unit - b * p.Hk, from = __ldcg(p.share + 1 + unit);
+    const int b = unit / p.Hk, hk = unit - b * p.Hk;
     const ListOf l = list_of(p, b, hk / (p.Hk / p.G));
     if (m >= l.rows * p.R) return;
-    const Parts ps(unit, l.n, share, from);
+    const auto ps = parts_of<kWarps>(p, unit, l.n, share);
     float ref = -INFINITY, total = 0.f, o[kOwn] = {};
     // eight parts a warp at a time
     for (int s0 = warp * 8; s0 < ps.count; s0 += kSumWarps * 8) {
@@ -831,7 +937,7 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_few_join_kernel(const A
     __syncthreads();
     // (whole warps: four rows each)
     const int mine = m0 + min(i, here - 1), hi = mine / rows_m, unit = unit0 + h + hi;
-    const Parts ps(unit, l.n, share, __ldcg(p.share + 1 + unit));
+    const auto ps = parts_of<kWarps>(p, unit, l.n, share);
     float ref = -INFINITY, total = 0.f;
     for (int s0 = lane & 7; s0 < ps.count; s0 += 32) {
       float2 ml[4];
@@ -876,33 +982,42 @@ namespace {
 
 template <class T, int D>
 cudaError_t configure_of() {
-  cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(RowsSmem<D>) + 128);
-  if (e != cudaSuccess) return e;
-  e = cudaFuncSetAttribute(attend_few_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<D>::kBytes);
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(attend_sums_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SumsSmem<D>) + 128);
+  auto set = [](auto kernel, size_t bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  };
+  cudaError_t e = set(attend_rows_kernel<T, D, 1>, sizeof(RowsSmem<D>) + 128);
+  if (e == cudaSuccess) e = set(attend_rows_kernel<T, D, 2>, sizeof(RowsSmem<D>) + 128);
+  if (e == cudaSuccess) e = set(attend_sums_kernel<T, D>, sizeof(SumsSmem<D>) + 128);
+  if (e == cudaSuccess) e = set(attend_few_kernel<T, D>, FewShape<D>::kBytes);
+  return e;
 }
 
 template <class T, int D>
 cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
   const long long units = static_cast<long long>(p.B) * p.Hk;
-  if (p.M <= kFewRows) {
-    cudaError_t e = launch_chained(attend_few_kernel<T, D>, dim3(p.warps / FewShape<D>::kWarps), dim3(FewShape<D>::kThreads),
-                                   FewShape<D>::kBytes, st, p);
+  const dim3 threads(kAttendThreads);
+  const int tiles_m = (p.M + kRowTile - 1) / kRowTile;
+  const dim3 rows(static_cast<unsigned>(units * tiles_m * p.splits));
+  const size_t rows_bytes = sizeof(RowsSmem<D>) + 128;
+  if (p.M <= kStoredRows) {   // scores kept
+    constexpr int kWarps = FewShape<D>::kWarps;
+    const bool few = p.M <= kFewRows;
+    cudaError_t e = few ? launch_chained(attend_few_kernel<T, D>, dim3(p.warps / kWarps), dim3(FewShape<D>::kThreads), FewShape<D>::kBytes, st, p)
+                        : launch_chained(attend_rows_kernel<T, D, 2>, rows, threads, rows_bytes, st, p);
     if (e != cudaSuccess) return e;
     const int row_ctas = static_cast<int>(units * p.M);
     const long long sums = static_cast<long long>(p.B) * p.G * ((p.C + kSumSlots - 1) / kSumSlots);
-    return launch_chained(attend_few_join_kernel<T, D>, dim3(static_cast<unsigned>(row_ctas + sums)), dim3(kSumThreads), 0, st, p, row_ctas);
+    const dim3 grid(static_cast<unsigned>(row_ctas + sums));
+    return few ? launch_chained(attend_stored_join_kernel<T, D, kWarps>, grid, dim3(kSumThreads), 0, st, p, row_ctas)
+               : launch_chained(attend_stored_join_kernel<T, D, 0>, grid, dim3(kSumThreads), 0, st, p, row_ctas);
   }
-  const int tiles_m = (p.M + kRowTile - 1) / kRowTile;
-  cudaError_t e = launch_chained(attend_rows_kernel<T, D>, dim3(static_cast<unsigned>(units * tiles_m * p.splits)),
-                                 dim3(kAttendThreads), sizeof(RowsSmem<D>) + 128, st, p);
+  cudaError_t e = launch_chained(attend_rows_kernel<T, D, 1>, rows, threads, rows_bytes, st, p);
   if (e != cudaSuccess) return e;
   e = launch_chained(attend_join_kernel<T, D>, dim3(static_cast<unsigned>((units * p.M + kJoinWarps - 1) / kJoinWarps)),
                      dim3(kJoinWarps * 32), 0, st, p);
   if (e != cudaSuccess) return e;
-  const long long tiles = (p.C + kKeyTile - 1) / kKeyTile;
-  return launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(tiles * p.B * p.G)), dim3(kAttendThreads),
+  const long long pieces = (p.C + SumsSmem<D>::kSlots - 1) / SumsSmem<D>::kSlots;
+  return launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(pieces * p.B * p.G)), threads,
                         sizeof(SumsSmem<D>) + 128, st, p);
 }
 
