@@ -152,11 +152,14 @@ struct EvictParams {
   int32_t* moved;            // workspace: [B][G] rows that move
   int2* pairs;               // workspace: [B][G][pair_pitch] (to, from)
   long long pair_pitch;
+  uint8_t* free_places;      // workspace: [B][G][free_pitch] a bit for each slot below budget
+  long long free_pitch;
 };
 
 int api_device_sms();
 cudaError_t configure_attend();
 cudaError_t configure_rotate();
+cudaError_t configure_evict();
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_rotate_back(const RotateParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_attend(const AttendParams& p, int d, int dtype, cudaStream_t st);

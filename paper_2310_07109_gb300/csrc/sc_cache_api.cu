@@ -10,8 +10,9 @@ namespace sc {
 int api_fail_cuda(const char* what, cudaError_t e);
 int api_ensure_configured();
 cudaError_t configure_cache() {
-  const cudaError_t e = configure_attend();
-  return e == cudaSuccess ? configure_rotate() : e;
+  cudaError_t e = configure_attend();
+  if (e == cudaSuccess) e = configure_rotate();
+  return e == cudaSuccess ? configure_evict() : e;
 }
 }  // namespace sc
 
@@ -55,9 +56,9 @@ int check_rotate(int B, int L, int Hq, int Hk, int d, int dtype, const int32_t* 
 }
 
 struct CacheLayout {
-  size_t lse, share, scores, ml, part, moved, pairs, total;
+  size_t lse, share, scores, ml, part, moved, pairs, free_places, evict, total;
   int splits, warps, pitch;
-  long long pair_pitch;
+  long long pair_pitch, free_pitch;
 };
 
 // Parts that the attention takes a list in: as many CTAs as SMs have room for (three, two of wide heads), parts of 256
@@ -90,7 +91,10 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   w.pair_pitch = C / 2 + 1;
   w.moved = kAlign;
   w.pairs = align_up(w.moved + sizeof(int32_t) * lists);
-  w.total = std::max(attend, align_up(w.pairs + sizeof(int2) * lists * w.pair_pitch));
+  w.free_places = align_up(w.pairs + sizeof(int2) * lists * w.pair_pitch);
+  w.free_pitch = (C + 7) / 8;
+  w.evict = align_up(w.free_places + lists * w.free_pitch);
+  w.total = std::max(attend, w.evict);
   return w;
 }
 
@@ -265,8 +269,7 @@ extern "C" int sc_cache_evict(const sc_cache_evict_args* a, void* workspace, siz
       !words(a->acc_out, a->pos_out, a->len_out))
     return SC_ERR_INVALID_ARG;
   const CacheLayout w = cache_layout(a->B, a->C, a->Hk, a->Hk, a->G, a->d, 1);
-  const size_t need = w.pairs + sizeof(int2) * static_cast<size_t>(a->B) * a->G * w.pair_pitch;
-  if ((rc = check_workspace(workspace, ws_bytes, need)) != SC_OK || (rc = api_ensure_configured()) != SC_OK) return rc;
+  if ((rc = check_workspace(workspace, ws_bytes, w.evict)) != SC_OK || (rc = api_ensure_configured()) != SC_OK) return rc;
   EvictParams p{};
   p.B = a->B; p.C = a->C; p.Hk = a->Hk; p.G = a->G; p.d = a->d;
   p.k = static_cast<uint16_t*>(a->K); p.v = static_cast<uint16_t*>(a->V);
@@ -278,6 +281,8 @@ extern "C" int sc_cache_evict(const sc_cache_evict_args* a, void* workspace, siz
   p.moved = reinterpret_cast<int32_t*>(ws + w.moved);
   p.pairs = reinterpret_cast<int2*>(ws + w.pairs);
   p.pair_pitch = w.pair_pitch;
+  p.free_places = reinterpret_cast<uint8_t*>(ws + w.free_places);
+  p.free_pitch = w.free_pitch;
   const cudaError_t e = launch_evict(p, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? SC_OK : api_fail_cuda("launch cache eviction", e);
 }

@@ -7,10 +7,13 @@
 // nearly every row behind the first one (half of 8192 slots: 2048 rows instead of 4096).
 //
 // Two launches:
-//   pick   a CTA a list: the cut by a radix search over 32-bit keys, eight bits at a time (acc's bits in
-//          an order-preserving form), then ranks of ties, free places and their fillers from ballots: warps
-//          have consecutive stretches of slots, so that ranks follow the slots
-//   move   the rows of K and V, bound by memory
+//   pick   a CTA a list.  Its slots' 32-bit keys (acc's bits in an order-preserving form) go into shared memory; the
+//          cut is found in passes over them, each of which cuts the range that holds it into at most 256 equal parts
+//          (by bits of the difference to its lower end: keys are logarithms nearly, so weights spread over the parts;
+//          digits of the keys themselves put most of them into two or three, whose additions wait for one another:
+//          13000 cycles a pass instead of 1000).  Then a bit a slot, and ranks of ties, free places and their fillers
+//          from prefix sums over the bits.  8000 slots: 22 us before, 5 now
+//   move   the rows of K and V, bound by memory, and acc and pos
 #include <algorithm>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -23,7 +26,10 @@ namespace sc {
 constexpr int kPickThreads = 1024;
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kMoveThreads = 256;
+constexpr int kMoveSlots = 1024;   // whose acc and pos a CTA moves
 constexpr uint32_t kProtected = 0xffffffffu;
+constexpr int kKeysHeld = 40960;   // most keys in shared memory (160 KB); longer lists are read again for each pass
+constexpr int kParts = 256;
 
 // What a slot ranks by: protected, then acc in order (-0 as 0); a NaN, or a slot without a position, last.
 __device__ __forceinline__ uint32_t rank_key(const EvictParams& p, float acc, int pos, int late) {
@@ -35,29 +41,33 @@ __device__ __forceinline__ uint32_t rank_key(const EvictParams& p, float acc, in
 }
 
 struct PickSmem {
-  uint32_t hist[256];
-  int warp_sum[kPickWarps][2];
-  int found[2];   // digit, how many of it are still to take
+  uint32_t hist[kParts];
+  uint32_t low[kPickWarps], high[kPickWarps];
+  int count[kPickWarps][2];
+  int found[3];   // part, how many of it are still to take, how many it has
 };
 
-// Exclusive prefixes over the warps of two sums, and their totals.
-__device__ __forceinline__ void scan_warps(PickSmem& sm, int a, int b, int& before_a, int& before_b, int& all_a, int& all_b) {
+// Exclusive prefix over the CTA's threads of two counts (each below 2^16 in all, packed), and their totals.
+__device__ __forceinline__ uint32_t scan_cta(PickSmem& sm, uint32_t v, uint32_t& all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  __syncthreads();
-  if (lane == 0) {
-    sm.warp_sum[warp][0] = a;
-    sm.warp_sum[warp][1] = b;
+  uint32_t upto = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
   }
+  __syncthreads();   // (the last one's have been read)
+  if (lane == 31) sm.low[warp] = upto;
   __syncthreads();
-  const int va = sm.warp_sum[lane][0], vb = sm.warp_sum[lane][1];
-  before_a = __reduce_add_sync(0xffffffffu, lane < warp ? va : 0);
-  before_b = __reduce_add_sync(0xffffffffu, lane < warp ? vb : 0);
-  all_a = __reduce_add_sync(0xffffffffu, va);
-  all_b = __reduce_add_sync(0xffffffffu, vb);
+  const uint32_t w = sm.low[lane];
+  all = __reduce_add_sync(0xffffffffu, w);
+  return __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + upto - v;
 }
 
-__global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictParams p) {
+__global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const EvictParams p) {
+  static_assert(kPickWarps == 32, "a lane a warp");
   __shared__ PickSmem sm;
+  extern __shared__ uint32_t held[];   // keys, then two bits a slot
   pdl_wait();
   pdl_launch_dependents();
   const int list = blockIdx.x, b = list / p.G, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -66,12 +76,7 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
   const int32_t* pos = p.pos + base;
   const int n = min(max(__ldcg(p.len + list), 0), p.C), k = p.budget;
   const int late = __ldg(p.seen + b) - p.recent;
-  const bool apart_acc = p.acc_out != p.acc, apart_pos = p.pos_out != p.pos;
   if (n <= k || n - k <= p.slack) {
-    for (int j = tid; j < n; j += kPickThreads) {
-      if (apart_acc) p.acc_out[base + j] = acc[j];
-      if (apart_pos) p.pos_out[base + j] = pos[j];
-    }
     __syncthreads();   // len is read
     if (tid == 0) {
       p.moved[list] = 0;
@@ -79,18 +84,78 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
     }
     return;
   }
-  // the cut: keys above it survive, and the first `ties` of those equal to it
-  uint32_t cut = 0, mask = 0;
-  int ties = k;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) sm.hist[tid] = 0;
+  const bool hold = n <= kKeysHeld;
+  uint32_t* above = held + min(p.C, kKeysHeld);
+  uint32_t* tied = above + (p.C + 31) / 32;
+  // protected ones and those that rank last apart, the range of the others' keys
+  uint32_t low = 0xffffffffu, high = 0;
+  int safe = 0, none = 0;
+  constexpr int kBatch = 8;
+  for (int j0 = tid; j0 < n; j0 += kBatch * kPickThreads) {
+    float a[kBatch];
+    int q[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int j = j0 + u * kPickThreads;
+      a[u] = 0.f;
+      q[u] = -1;
+      if (j < n) {
+        a[u] = __ldcg(acc + j);
+        q[u] = __ldcg(pos + j);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int j = j0 + u * kPickThreads;
+      if (j >= n) break;
+      const uint32_t key = rank_key(p, a[u], q[u], late);
+      if (hold) held[j] = key;
+      safe += key == kProtected;
+      none += key == 0;
+      if (key != kProtected && key != 0) {
+        low = min(low, key);
+        high = max(high, key);
+      }
+    }
+  }
+  low = __reduce_min_sync(0xffffffffu, low);
+  high = __reduce_max_sync(0xffffffffu, high);
+  safe = __reduce_add_sync(0xffffffffu, safe);
+  none = __reduce_add_sync(0xffffffffu, none);
+  if (lane == 0) {
+    sm.low[warp] = low;
+    sm.high[warp] = high;
+    sm.count[warp][0] = safe;
+    sm.count[warp][1] = none;
+  }
+  __syncthreads();
+  low = __reduce_min_sync(0xffffffffu, sm.low[lane]);
+  high = __reduce_max_sync(0xffffffffu, sm.high[lane]);
+  safe = __reduce_add_sync(0xffffffffu, sm.count[lane][0]);
+  none = __reduce_add_sync(0xffffffffu, sm.count[lane][1]);
+  auto key_at = [&](int j) { return hold ? held[j] : rank_key(p, __ldcg(acc + j), __ldcg(pos + j), late); };
+  // keys above `high` survive, and the first `want` of the `count` ones from low to high: all of them, or low is high
+  int want = k - safe, count = n - safe - none;
+  if (want <= 0) {
+    low = high = kProtected;
+    want = k;
+    count = safe;
+  } else if (want > count) {
+    low = high = 0;
+    want -= count;
+    count = none;
+  }
+  while (low != high && want != count) {
+    const int shift = max(0, 24 - __clz(high - low));   // at most 256 parts of 2^shift
+    if (tid < kParts) sm.hist[tid] = 0;
     __syncthreads();
+#pragma unroll 4
     for (int j = tid; j < n; j += kPickThreads) {
-      const uint32_t key = rank_key(p, acc[j], pos[j], late);
-      if ((key & mask) == cut) atomicAdd(&sm.hist[(key >> shift) & 255], 1u);
+      const uint32_t key = key_at(j);
+      if (key >= low && key <= high) atomicAdd(&sm.hist[(key - low) >> shift], 1u);
     }
     __syncthreads();
-    if (warp == 0) {   // lane l has digits 255 - 8 l .. 248 - 8 l, the largest first
+    if (warp == 0) {   // lane l has parts 255 - 8 l .. 248 - 8 l, the largest first
       int own[8], total = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) total += own[i] = static_cast<int>(sm.hist[255 - 8 * lane - i]);
@@ -101,84 +166,123 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictPar
         if (lane >= o) upto += v;
       }
       int before = upto - total;
-      if (before < ties && ties <= upto) {
+      if (before < want && want <= upto) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (before < ties && ties <= before + own[i]) {
+          if (before < want && want <= before + own[i]) {
             sm.found[0] = 255 - 8 * lane - i;
-            sm.found[1] = ties - before;
+            sm.found[1] = want - before;
+            sm.found[2] = own[i];
           }
           before += own[i];
         }
       }
     }
     __syncthreads();
-    cut |= static_cast<uint32_t>(sm.found[0]) << shift;
-    mask |= 255u << shift;
-    ties = sm.found[1];
-    __syncthreads();
+    low += static_cast<uint32_t>(sm.found[0]) << shift;
+    high = min(high, low + ((1u << shift) - 1u));
+    want = sm.found[1];
+    count = sm.found[2];
   }
-  // ranks: each warp a stretch of slots
-  const int stretch = ((n + kPickWarps - 1) / kPickWarps + 31) & ~31;
-  const int j0 = min(warp * stretch, n), j1 = min(j0 + stretch, n);
-  int equal = 0, tied, unused, all, none;
-  for (int j = j0 + lane; j - lane < j1; j += 32)
-    equal += __popc(__ballot_sync(0xffffffffu, j < j1 && rank_key(p, acc[j], pos[j], late) == cut));
-  scan_warps(sm, equal, 0, tied, unused, all, none);
-  // (a lambda over the warp's stretch: survivors' ballots in order)
-  const uint32_t below = (1u << lane) - 1u;
-  auto over = [&](auto&& each) {
-    int run = tied;
-    for (int j = j0 + lane; j - lane < j1; j += 32) {
-      const uint32_t key = j < j1 ? rank_key(p, acc[j], pos[j], late) : 0u;
-      const uint32_t eq = __ballot_sync(0xffffffffu, j < j1 && key == cut);
-      const bool keep = j < j1 && (key > cut || (key == cut && run + __popc(eq & below) < ties));
-      run += __popc(eq);
-      each(j, j < j1 && j < k && !keep, keep && j >= k);
+  // a bit a slot
+#pragma unroll 4
+  for (int j0 = 0; j0 < n; j0 += kPickThreads) {
+    const int j = j0 + tid;
+    const uint32_t key = j < n ? key_at(j) : 0;
+    const uint32_t over = __ballot_sync(0xffffffffu, j < n && key > high);
+    const uint32_t in = __ballot_sync(0xffffffffu, j < n && key >= low && key <= high);
+    if (lane == 0 && j < n) {
+      above[j / 32] = over;
+      tied[j / 32] = in;
     }
-  };
-  int free_ = 0, fill = 0;
-  over([&](int, bool is_free, bool is_fill) {
-    free_ += __popc(__ballot_sync(0xffffffffu, is_free));
-    fill += __popc(__ballot_sync(0xffffffffu, is_fill));
-  });
-  int free_at, fill_at, all_free, all_fill;
-  scan_warps(sm, free_, fill, free_at, fill_at, all_free, all_fill);
-  int2* pairs = p.pairs + list * p.pair_pitch;
-  over([&](int j, bool is_free, bool is_fill) {
-    const uint32_t f = __ballot_sync(0xffffffffu, is_free), g = __ballot_sync(0xffffffffu, is_fill);
-    if (is_free) pairs[free_at + __popc(f & below)].x = j;
-    if (is_fill) pairs[fill_at + __popc(g & below)].y = j;
-    free_at += __popc(f);
-    fill_at += __popc(g);
-  });
+  }
   __syncthreads();
-  // acc and pos: places that stay, then the filled ones
-  if (apart_acc || apart_pos) {
-    for (int j = tid; j < k; j += kPickThreads) {
-      if (apart_acc) p.acc_out[base + j] = acc[j];
-      if (apart_pos) p.pos_out[base + j] = pos[j];
+  const uint8_t* above8 = reinterpret_cast<const uint8_t*>(above);
+  uint8_t* tied8 = reinterpret_cast<uint8_t*>(tied);
+  const int bytes = (n + 7) / 8;
+  if (want != count) {   // the first `want` of equal ones
+    int done = 0;
+    for (int i0 = 0; i0 < bytes; i0 += kPickThreads) {
+      const int i = i0 + tid;
+      uint32_t in = i < bytes ? tied8[i] : 0u, all;
+      const int before = done + static_cast<int>(scan_cta(sm, __popc(in), all));
+      for (int left = want - before; __popc(in) > max(left, 0);) in &= ~(1u << (31 - __clz(in)));
+      if (i < bytes) tied8[i] = static_cast<uint8_t>(in);
+      done += static_cast<int>(all);
     }
-    __syncthreads();
   }
-  for (int i = tid; i < all_free; i += kPickThreads) {
-    const int2 m = pairs[i];
-    const float a = acc[m.y];
-    const int q = pos[m.y];
-    p.acc_out[base + m.x] = a;
-    p.pos_out[base + m.x] = q;
+  // free places below k and survivors from k on, in order
+  int2* pairs = p.pairs + list * p.pair_pitch;
+  uint8_t* free8 = p.free_places + list * p.free_pitch;
+  int free_at = 0, fill_at = 0;
+  for (int i0 = 0; i0 < bytes; i0 += kPickThreads) {
+    const int i = i0 + tid, j = 8 * i;
+    uint32_t keep = i < bytes ? above8[i] | tied8[i] : 0u;
+    const uint32_t low_ones = j >= k ? 0u : k - j >= 8 ? 0xffu : (1u << (k - j)) - 1u;   // slots below k
+    uint32_t places = i < bytes ? ~keep & low_ones : 0u, all;
+    uint32_t fills = keep & ~low_ones & 0xffu;
+    const uint32_t before = scan_cta(sm, __popc(places) | __popc(fills) << 16, all);
+    if (low_ones != 0) free8[i] = static_cast<uint8_t>(places);
+    for (int at = free_at + static_cast<int>(before & 0xffffu); places != 0; places &= places - 1) pairs[at++].x = j + __ffs(places) - 1;
+    for (int at = fill_at + static_cast<int>(before >> 16); fills != 0; fills &= fills - 1) pairs[at++].y = j + __ffs(fills) - 1;
+    free_at += static_cast<int>(all & 0xffffu);
+    fill_at += static_cast<int>(all >> 16);
   }
   if (tid == 0) {
-    p.moved[list] = all_free;
+    p.moved[list] = free_at;
     p.len_out[list] = k;
   }
 }
 
-// A CTA has every chunks-th piece of the moves of a head; d / 8 lanes a row, K and V together.
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p, int chunks) {
+// acc and pos of 1024 slots of a list: those that stay (where the outputs lie apart), and as many that move.
+__device__ __forceinline__ void move_weights(const EvictParams& p, int id, int chunks) {
+  const int list = id / chunks, i0 = (id - list * chunks) * kMoveSlots;
+  const int m = __ldcg(p.moved + list), n = __ldcg(p.len_out + list);
+  const long long base = static_cast<long long>(list) * p.C;
+  const bool apart_acc = p.acc_out != p.acc, apart_pos = p.pos_out != p.pos;
+  const uint8_t* free8 = p.free_places + list * p.free_pitch;
+  const int2* pairs = p.pairs + list * p.pair_pitch;
+  constexpr int kBatch = kMoveSlots / kMoveThreads;
+  int2 at[kBatch];
+  float acc[kBatch], moved_acc[kBatch];
+  int pos[kBatch], moved_pos[kBatch];
+  bool stays[kBatch];
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    const int i = i0 + u * kMoveThreads + static_cast<int>(threadIdx.x);
+    stays[u] = (apart_acc || apart_pos) && i < n && (m == 0 || !(__ldcg(free8 + i / 8) >> (i & 7) & 1));
+    if ((apart_acc || apart_pos) && i < n) {
+      acc[u] = __ldcg(p.acc + base + i);
+      pos[u] = __ldcg(p.pos + base + i);
+    }
+    if (i < m) at[u] = __ldcg(pairs + i);
+  }
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    if (i0 + u * kMoveThreads + static_cast<int>(threadIdx.x) >= m) continue;
+    moved_acc[u] = __ldcg(p.acc + base + at[u].y);
+    moved_pos[u] = __ldcg(p.pos + base + at[u].y);
+  }
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) {
+    const int i = i0 + u * kMoveThreads + static_cast<int>(threadIdx.x);
+    if (stays[u] && apart_acc) p.acc_out[base + i] = acc[u];
+    if (stays[u] && apart_pos) p.pos_out[base + i] = pos[u];
+    if (i < m) {
+      p.acc_out[base + at[u].x] = moved_acc[u];
+      p.pos_out[base + at[u].x] = moved_pos[u];
+    }
+  }
+}
+
+// The first CTAs move acc and pos; of the others each has every chunks-th piece of the moves of a head, d / 8 lanes a
+// row, K and V together.
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams p, int chunks, int weight_chunks) {
   pdl_wait();
   pdl_launch_dependents();
-  const int unit = blockIdx.x / chunks, chunk = blockIdx.x - unit * chunks;
+  const int weight_ctas = p.B * p.G * weight_chunks, id = static_cast<int>(blockIdx.x) - weight_ctas;
+  if (id < 0) return move_weights(p, blockIdx.x, weight_chunks);
+  const int unit = id / chunks, chunk = id - unit * chunks;
   const int b = unit / p.Hk, hk = unit - b * p.Hk, list = b * p.G + hk / (p.Hk / p.G);
   const int m = __ldcg(p.moved + list), lanes = p.d / 8, at_once = kMoveThreads / lanes;
   const int c = threadIdx.x % lanes, r = threadIdx.x / lanes;
@@ -210,14 +314,25 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
   }
 }
 
+cudaError_t configure_evict() {
+  return cudaFuncSetAttribute(evict_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysHeld * 4 + SC_MAX_CACHE / 8 * 2);
+}
+
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
-  cudaError_t e = launch_chained(evict_pick_kernel, dim3(p.B * p.G), dim3(kPickThreads), 0, st, p);
-  if (e != cudaSuccess || p.budget >= p.C) return e;   // (no list is over its budget)
+  const size_t held = sizeof(uint32_t) * (std::min(p.C, kKeysHeld) + 2 * ((p.C + 31) / 32));
+  cudaError_t e = launch_chained(evict_pick_kernel, dim3(p.B * p.G), dim3(kPickThreads), held, st, p);
+  const bool evicts = p.budget < p.C, apart = p.acc_out != p.acc || p.pos_out != p.pos;
+  if (e != cudaSuccess || (!evicts && !apart)) return e;
   const long long units = static_cast<long long>(p.B) * p.Hk;
-  const int most = std::min(p.budget, p.C - p.budget), rows = 4 * (kMoveThreads / (p.d / 8));
-  const long long want = std::max<long long>(1, kCacheSms * 8 / units);
-  const int chunks = static_cast<int>(std::min<long long>(want, (most + rows - 1) / rows));
-  return launch_chained(evict_move_kernel, dim3(static_cast<unsigned>(units * chunks)), dim3(kMoveThreads), 0, st, p, chunks);
+  int chunks = 0;
+  if (evicts) {
+    const int most = std::min(p.budget, p.C - p.budget), rows = 4 * (kMoveThreads / (p.d / 8));
+    chunks = static_cast<int>(std::min<long long>(std::max<long long>(1, kCacheSms * 8 / units), (most + rows - 1) / rows));
+  }
+  const long long slots = std::min<long long>(p.C, static_cast<long long>(p.budget) + p.slack);
+  const int weight_chunks = static_cast<int>((slots + kMoveSlots - 1) / kMoveSlots);
+  const long long ctas = units * chunks + static_cast<long long>(p.B) * p.G * weight_chunks;
+  return launch_chained(evict_move_kernel, dim3(static_cast<unsigned>(ctas)), dim3(kMoveThreads), 0, st, p, chunks, weight_chunks);
 }
 
 }  // namespace sc
