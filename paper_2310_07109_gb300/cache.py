@@ -21,7 +21,7 @@ import struct
 import torch
 
 from . import binding as _b
-from .expert import _at, _device, _made, _refuse, _rows_at, _stream
+from .expert import _at, _device, _made, _refuse, _stream
 
 MAX_HEAD_WIDTH = 256
 MAX_HEADS = 1024
@@ -191,10 +191,12 @@ def _heads_at(t, name, dtype, T, d, dev):
     """Address, heads and token distance of a matrix [T, heads * d]; none for None."""
     if t is None:
         return 0, 0, 0
-    at, rows, width, ld = _rows_at(t, name, dtype, dev)
-    if rows != T or width % d:
-        _refuse("%s: %d rows of heads of %d features are wanted" % (name, T, d))
-    return at, width // d, ld
+    shape = t.shape
+    if len(shape) == 2 and t.dtype is dtype and t.get_device() == dev and shape[0] == T and shape[1] % d == 0:
+        ld, step = t.stride()
+        if step == 1 or shape[1] == 1:
+            return t.data_ptr(), shape[1] // d, ld if T > 1 else max(ld, shape[1])
+    _refuse("%s: %d rows of heads of %d features, of %s on cuda:%d and contiguous, are wanted" % (name, T, d, dtype, dev))
 
 
 def _turn_at(freq, gamma_q, gamma_k, d, dev):
@@ -275,24 +277,24 @@ def rotate_backward(dQ, dK=None, Q=None, K=None, *, width, B, L, rows=None, pos=
     return out
 
 
-def _cache_at(cache, dev, t=None):
+def _cache_at(cache, dev):
     """(B, Hk, C, G, d, dtype of torch), and the argument block's part on the cache."""
-    K, V = cache["K"], cache["V"]
-    if K.dim() != 4 or V.shape != K.shape or V.dtype is not K.dtype or K.get_device() != dev or V.get_device() != dev:
+    K, V, acc, pos, length, seen = cache["K"], cache["V"], cache["acc"], cache["pos"], cache["len"], cache["seen"]
+    shape, strides, dt = K.shape, K.stride(), K.dtype
+    if len(shape) != 4 or V.shape != shape or V.dtype is not dt or K.get_device() != dev or V.get_device() != dev:
         _refuse("K, V: two tensors [B, heads, C, d] of one type on cuda:%d are wanted" % dev)
-    B, Hk, C, d = K.shape
-    sb, sh, sc, one = K.stride()
-    if V.stride() != K.stride() or (one != 1 and d > 1):
+    if V.stride() != strides or (strides[3] != 1 and shape[3] > 1):
         _refuse("K, V: the same strides, with contiguous features, are wanted")
-    sb, sh, sc = sb if B > 1 else 0, sh if Hk > 1 else 0, sc if C > 1 else d
-    if cache["len"].dim() != 2:
-        _refuse("len: 2 dimensions are wanted")
-    G = cache["len"].shape[1]
-    i32 = torch.int32
-    return (B, Hk, C, G, d, K.dtype), (
-        d, _type(K), K.data_ptr(), V.data_ptr(), sb, sh, sc, _at(cache["acc"], "acc", torch.float32, B * G * C, dev),
-        _at(cache["pos"], "pos", i32, B * G * C, dev), _at(cache["len"], "len", i32, B * G, dev),
-        _at(cache["seen"], "seen", i32, B, dev))
+    B, Hk, C, d = shape
+    lists = length.shape
+    if len(lists) != 2 or lists[0] != B:
+        _refuse("len: [B, lists] is wanted")
+    G, i32 = lists[1], torch.int32
+    sb, sh, sc, _ = strides
+    return (B, Hk, C, G, d, dt), (
+        d, _type(K), K.data_ptr(), V.data_ptr(), sb if B > 1 else 0, sh if Hk > 1 else 0, sc if C > 1 else d,
+        _at(acc, "acc", torch.float32, B * G * C, dev), _at(pos, "pos", i32, B * G * C, dev),
+        _at(length, "len", i32, B * G, dev), _at(seen, "seen", i32, B, dev))
 
 
 def cache_append(cache, Q, K, V, *, L, rows=None, freq=None, interleaved=False, mscale=1.0, gamma_q=None, gamma_k=None,
@@ -313,7 +315,8 @@ def cache_append(cache, Q, K, V, *, L, rows=None, freq=None, interleaved=False, 
         if H:
             out["Q"] = torch.empty((T, H * d), dtype=dt, device=K.device)
             _made(stream, out["Q"])
-    out = {"len": cache["len"], "seen": cache["seen"], **out}
+    if "len" not in out or "seen" not in out:
+        out = {"len": cache["len"], "seen": cache["seen"], **out}
     qo, ho, ldqo = _heads_at(out["Q"] if H else None, "out Q", dt, T, d, dev)
     _same(ho, H, "out Q")
     gq, gk, rot, f = _turn_at(freq, gamma_q, gamma_k, d, dev)
@@ -336,7 +339,8 @@ def cache_attend(cache, Q, *, T, rows=None, scale=None, decay=1.0, out=None, wor
     if out is None:
         out = {"O": torch.empty((B * T, H * d), dtype=dt, device=Q.device)}
         _made(stream, out["O"])
-    out = {"acc": cache["acc"], **out}
+    if "acc" not in out:
+        out = {"acc": cache["acc"], **out}
     o, ho, ldo = _heads_at(out["O"], "O", dt, B * T, d, dev)
     _same(ho, H, "O")
     a = _ATTEND.pack(B, C, H, Hk, G, *view, T, q, ldq, _at(rows, "rows", torch.int32, B, dev),
@@ -354,7 +358,8 @@ def cache_evict(cache, *, budget, slack=0, sinks=0, recent=0, out=None, workspac
     K = cache["K"]
     dev = _device(K, "K")
     (B, Hk, C, G, d, dt), view = _cache_at(cache, dev)
-    out = {"acc": cache["acc"], "pos": cache["pos"], "len": cache["len"], **(out or {})}
+    if out is None or len(out) < 3:
+        out = {"acc": cache["acc"], "pos": cache["pos"], "len": cache["len"], **(out or {})}
     i32 = torch.int32
     a = _EVICT.pack(B, C, Hk, G, *view, budget, slack, sinks, recent, _at(out["acc"], "out acc", torch.float32, B * G * C, dev),
                     _at(out["pos"], "out pos", i32, B * G * C, dev), _at(out["len"], "out len", i32, B * G, dev))

@@ -97,7 +97,7 @@ struct RotateParams {
   unsigned* done;            // workspace: CTAs that have read len and seen
 };
 
-constexpr int kRotateMaxParts = 304;   // CTAs of the gradient
+constexpr int kRotateMaxParts = 152 * 5;   // CTAs of the gradient
 
 struct AttendParams {
   int B, C, H, Hk, G, T;

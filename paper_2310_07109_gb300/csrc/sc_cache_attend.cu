@@ -826,14 +826,14 @@ __device__ __forceinline__ auto parts_of(const AttendParams& p, int unit, int n,
     return Pieces<kWarps>(unit, n, share, __ldcg(p.share + 1 + unit));
 }
 
-// The first `row_ctas` CTAs join a row each; the others have kSumSlots slots of a list each, whose weights
-// they add up over the list's rows from the scores and the rows' LSE.
+// The first `row_ctas` CTAs join rows, one each or, with many rows (`together`), a warp a row; the others have kSumSlots
+// slots of a list each, whose weights they add up over the list's rows from the scores and the rows' LSE.
 constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32;
-constexpr int kSumSlots = kSumThreads * 2;
-constexpr int kSumAhead = 8;
+constexpr int kSumSlots = kSumThreads * 4;
+constexpr int kSumAhead = 4;
 constexpr int kSumRows = kSumThreads / 8;   // rows whose LSE are found at once, by eight lanes each
 template <class T, int D, int kWarps>
-__global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(const AttendParams p, int row_ctas) {
+__global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(const AttendParams p, int row_ctas, int together) {
   constexpr int kOwn = D / 32;
   __shared__ float part[kSumWarps][D];
   __shared__ float2 ends[kSumWarps];
@@ -843,14 +843,16 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int share = kWarps != 0 ? __ldcg(p.share) : 0;
   if (static_cast<int>(blockIdx.x) < row_ctas) {
-    const int unit = static_cast<int>(blockIdx.x) / p.M, m = static_cast<int>(blockIdx.x) - unit * p.M;
+    const int row = together ? static_cast<int>(blockIdx.x) * kSumWarps + warp : static_cast<int>(blockIdx.x);
+    const int unit = row / p.M, m = row - unit * p.M;
+    if (unit >= p.B * p.Hk) return;
     const int b = unit / p.Hk, hk = unit - b * p.Hk;
     const ListOf l = list_of(p, b, hk / (p.Hk / p.G));
     if (m >= l.rows * p.R) return;
     const auto ps = parts_of<kWarps>(p, unit, l.n, share);
     float ref = -INFINITY, total = 0.f, o[kOwn] = {};
     // eight parts a warp at a time
-    for (int s0 = warp * 8; s0 < ps.count; s0 += kSumWarps * 8) {
+    for (int s0 = together ? 0 : warp * 8; s0 < ps.count; s0 += together ? 8 : kSumWarps * 8) {
       const int s = s0 + (lane & 7);
       const float2 ml = s < ps.count ? p.ml[ps.at(s) * p.M + m] : make_float2(-INFINITY, 0.f);
       const bool some = ml.x != -INFINITY || ml.y != 0.f;   // (nothing but NaN: the sum is one)
@@ -885,6 +887,13 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
     }
 #pragma unroll
     for (int i = 4; i > 0; i >>= 1) total += __shfl_xor_sync(0xffffffffu, total, i);
+    uint16_t* out = p.o + (static_cast<long long>(b) * p.T + m / p.R) * p.ldo + static_cast<long long>(hk * p.R + m % p.R) * D;
+    if (together) {
+      const float inv = ref == -INFINITY && total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+      for (int i = 0; i < kOwn; i += 2) reinterpret_cast<uint32_t*>(out)[(lane * kOwn + i) / 2] = T::pack(o[i] * inv, o[i + 1] * inv);
+      return;
+    }
     if (lane == 0) ends[warp] = make_float2(ref, total);
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) part[warp][lane * kOwn + i] = o[i];
@@ -902,20 +911,19 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
       v[1] += k * part[w][2 * threadIdx.x + 1];
     }
     const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
-    reinterpret_cast<uint32_t*>(p.o + (static_cast<long long>(b) * p.T + m / p.R) * p.ldo +
-                                static_cast<long long>(hk * p.R + m % p.R) * D)[threadIdx.x] = T::pack(v[0] * inv, v[1] * inv);
+    reinterpret_cast<uint32_t*>(out)[threadIdx.x] = T::pack(v[0] * inv, v[1] * inv);
     return;
   }
   const int chunks = (p.C + kSumSlots - 1) / kSumSlots, id = blockIdx.x - row_ctas;
   const int list = id / chunks, b = list / p.G, g = list - b * p.G, of = p.Hk / p.G, unit0 = b * p.Hk + g * of;
   const ListOf l = list_of(p, b, g);
-  const int j0 = (id - list * chunks) * kSumSlots, j = j0 + static_cast<int>(threadIdx.x) * 2;
+  const int j0 = (id - list * chunks) * kSumSlots, j = j0 + static_cast<int>(threadIdx.x) * 4;
   if (j0 >= l.n) return;
   const int rows_m = l.rows * p.R, rows = of * rows_m;
   const long long at = static_cast<long long>(list) * p.C + j;
-  float old[2] = {}, sum[2] = {};
+  float old[4] = {}, sum[4] = {};
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 4; ++i)
     if (j + i < l.n) old[i] = p.acc[at + i];
   for (int r0 = 0; r0 < rows; r0 += kSumRows) {
     const int here = min(kSumRows, rows - r0), i = threadIdx.x / 8;
@@ -924,13 +932,13 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
     const float* row = p.scores + (static_cast<long long>(unit0 + h) * p.M + m0) * p.pitch + j;
     int m = m0;
     auto next = [&]() {
-      const float2 t = *reinterpret_cast<const float2*>(row);
+      const float4 t = *reinterpret_cast<const float4*>(row);
       const bool end = ++m == rows_m;   // of the head's rows in use
       row += static_cast<long long>(end ? p.M - rows_m + 1 : 1) * p.pitch;
       m = end ? 0 : m;
       return t;
     };
-    float2 ahead[kSumAhead];
+    float4 ahead[kSumAhead];
 #pragma unroll
     for (int k = 0; k < kSumAhead; ++k)
       if (k < here && j < l.n) ahead[k] = next();
@@ -965,16 +973,20 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
       if (k < here) {
         sum[0] += ex2(ahead[k].x - lse[k]);
         sum[1] += ex2(ahead[k].y - lse[k]);
+        sum[2] += ex2(ahead[k].z - lse[k]);
+        sum[3] += ex2(ahead[k].w - lse[k]);
       }
-#pragma unroll 8
+#pragma unroll 4
     for (int k = kSumAhead; k < here; ++k) {
-      const float2 t = next();
+      const float4 t = next();
       sum[0] += ex2(t.x - lse[k]);
       sum[1] += ex2(t.y - lse[k]);
+      sum[2] += ex2(t.z - lse[k]);
+      sum[3] += ex2(t.w - lse[k]);
     }
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 4; ++i)
     if (j + i < l.n) p.acc_out[at + i] = l.rows > 0 ? p.decay * old[i] + sum[i] / static_cast<float>(p.H / p.G) : old[i];
 }
 
@@ -1005,11 +1017,13 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
     cudaError_t e = few ? launch_chained(attend_few_kernel<T, D>, dim3(p.warps / kWarps), dim3(FewShape<D>::kThreads), FewShape<D>::kBytes, st, p)
                         : launch_chained(attend_rows_kernel<T, D, 2>, rows, threads, rows_bytes, st, p);
     if (e != cudaSuccess) return e;
-    const int row_ctas = static_cast<int>(units * p.M);
+    const long long all_rows = units * p.M;
+    const int together = all_rows > 2 * kCacheSms;
+    const int row_ctas = static_cast<int>(together ? (all_rows + kSumWarps - 1) / kSumWarps : all_rows);
     const long long sums = static_cast<long long>(p.B) * p.G * ((p.C + kSumSlots - 1) / kSumSlots);
     const dim3 grid(static_cast<unsigned>(row_ctas + sums));
-    return few ? launch_chained(attend_stored_join_kernel<T, D, kWarps>, grid, dim3(kSumThreads), 0, st, p, row_ctas)
-               : launch_chained(attend_stored_join_kernel<T, D, 0>, grid, dim3(kSumThreads), 0, st, p, row_ctas);
+    return few ? launch_chained(attend_stored_join_kernel<T, D, kWarps>, grid, dim3(kSumThreads), 0, st, p, row_ctas, together)
+               : launch_chained(attend_stored_join_kernel<T, D, 0>, grid, dim3(kSumThreads), 0, st, p, row_ctas, together);
   }
   cudaError_t e = launch_chained(attend_rows_kernel<T, D, 1>, rows, threads, rows_bytes, st, p);
   if (e != cudaSuccess) return e;

@@ -31,8 +31,7 @@ namespace sc {
 
 constexpr int kRotateWarps = 8;         // most of a CTA
 constexpr int kRotateThreads = kRotateWarps * 32;
-constexpr int kRotateCtas = 2;          // an SM, forward (three leave too few registers: what spills costs half of the time again)
-constexpr int kRotateBackCtas = 2;      // an SM, backward
+constexpr int kSmWarps = 16;            // an SM's: 128 registers a thread (what spills with 80 costs half of the time again)
 constexpr int kWarpTokens = 4;          // most tokens of a warp at a time, forward
 constexpr int kWarpTokensBack = 2;      // backward (twice the vectors)
 constexpr int kTileTokens = 16;         // most tokens of a CTA at a time
@@ -244,7 +243,7 @@ __device__ __forceinline__ int cache_len(const RotateParams& p, int list) {
 
 // Forward, and append where cache_k is set.
 template <class T, int W, bool kInter, bool kNorm>
-__global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_kernel(const RotateParams p, const RotatePlan plan) {
+__global__ void __launch_bounds__(kRotateThreads, kSmWarps / kRotateWarps) rotate_kernel(const RotateParams p, const RotatePlan plan) {
   extern __shared__ __align__(16) char raw[];
   __shared__ unsigned long long turn[SC_MAX_HEAD_WIDTH / 2];
   float* table = reinterpret_cast<float*>(raw + ring_bytes(plan, 2));   // [2][cos, sin][wt nt][rot / 2]
@@ -375,7 +374,7 @@ __global__ void __launch_bounds__(kRotateThreads, kRotateCtas) rotate_kernel(con
 // Gradient.  dgamma: a lane adds up its features of its head over its tokens, the CTA its lanes and warps, in order;
 // the parts of the CTAs (blockIdx.y has groups of its own) are added, in order, by rotate_gamma_kernel.
 template <class T, int W, bool kInter, bool kNorm>
-__global__ void __launch_bounds__(kRotateThreads, kRotateBackCtas) rotate_back_kernel(const RotateParams p, const RotatePlan plan) {
+__global__ void __launch_bounds__(kRotateThreads, kSmWarps / kRotateWarps) rotate_back_kernel(const RotateParams p, const RotatePlan plan) {
   constexpr int kAt = 1;   // tokens that go through the stages together (two: registers do not suffice)
   extern __shared__ __align__(16) char raw[];
   __shared__ unsigned long long turn[SC_MAX_HEAD_WIDTH / 2];
@@ -543,18 +542,18 @@ namespace {
 // Lanes that a head takes: a power of two, four at least.
 int lanes_of(int d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
 
-// All groups of a few tokens to a CTA; the fewer tokens there are, the fewer at a time, until the SMs have a CTA each.
-RotatePlan plan_of(const RotateParams& p, int groups, int most_tokens, int most_ctas) {
+// All groups of a few tokens to a CTA of three warps at least (the smaller, the more evenly they fill an SM's sixteen
+// warps of 128 registers); the fewer tokens there are, the fewer at a time, until each SM has two CTAs.
+RotatePlan plan_of(const RotateParams& p, int groups, int most_tokens) {
   RotatePlan plan;
   plan.wg = std::min(groups, kRotateWarps);
-  plan.wt = kRotateWarps / plan.wg;
+  plan.wt = plan.wg >= 3 ? 1 : plan.wg == 2 ? 2 : 4;
   const int columns = (groups + plan.wg - 1) / plan.wg;
   plan.nt = most_tokens;
-  while (plan.nt > 1 && (plan.wt * plan.nt > kTileTokens ||
-                         (p.T + plan.wt * plan.nt - 1) / (plan.wt * plan.nt) * columns < 2 * kCacheSms)) plan.nt /= 2;
+  while (plan.nt > 1 && (p.T + plan.wt * plan.nt - 1) / (plan.wt * plan.nt) * columns < 2 * kCacheSms) plan.nt /= 2;
   while (plan.wt > 1 && (p.T + plan.wt - 1) / plan.wt * columns < kCacheSms) --plan.wt;
   const long long tiles = (p.T + plan.wt * plan.nt - 1) / (plan.wt * plan.nt);
-  plan.ctas = static_cast<int>(std::min<long long>(tiles, std::max(1, most_ctas / columns)));
+  plan.ctas = static_cast<int>(std::min<long long>(tiles, std::max(1, kCacheSms * (kSmWarps / (plan.wg * plan.wt)) / columns)));
   return plan;
 }
 
@@ -573,13 +572,13 @@ struct Rotation {
   }
   static cudaError_t forward(const RotateParams& p, cudaStream_t st) {
     const int groups = groups_of(p.Hq + p.Hk * (p.cache_k != nullptr ? 2 : 1));
-    const RotatePlan plan = plan_of(p, groups, kWarpTokens, kCacheSms * kRotateCtas);
+    const RotatePlan plan = plan_of(p, groups, kWarpTokens);
     return launch_chained(rotate_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, (groups + plan.wg - 1) / plan.wg),
                           dim3(plan.wg * plan.wt * 32), bytes(p, plan, 2), st, p, plan);
   }
   static cudaError_t backward(const RotateParams& p, cudaStream_t st) {
     const int groups = groups_of(p.Hq + p.Hk);
-    const RotatePlan plan = plan_of(p, groups, kWarpTokensBack, kCacheSms * kRotateBackCtas);
+    const RotatePlan plan = plan_of(p, groups, kWarpTokensBack);
     const int columns = (groups + plan.wg - 1) / plan.wg;
     cudaError_t e = launch_chained(rotate_back_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, columns),
                                    dim3(plan.wg * plan.wt * 32), bytes(p, plan, 4), st, p, plan);
