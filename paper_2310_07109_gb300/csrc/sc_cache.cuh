@@ -123,6 +123,8 @@ struct AttendParams {
   // workspace, few rows
   int warps;                 // at work on the tiles of all lists
   int* share;                // tiles a warp, then [B][Hk] the first tile of each unit
+  int stored;                // the scores are kept
+  float* sums;               // [B][Hk][pitch] where they are not: the weights' sums over a key head's rows
   float* scores;             // [B][Hk][M][pitch] scale log2(e) q . k; -inf: not seen
   int pitch;
   // both: parts (many rows: [B][Hk][splits]; few: a warp's number + a unit's)
@@ -131,7 +133,8 @@ struct AttendParams {
 };
 
 constexpr int kFewRows = 16;                 // most rows a key head that the kernel for few rows takes
-constexpr int kStoredRows = 32;              // most rows whose scores are kept for the sums of the weights
+constexpr int kJoinedRows = 32;              // most rows that one launch joins and adds the weights of
+constexpr size_t kStoredBytes = 32u << 20;   // most bytes of the scores of more rows, else they are computed again
 constexpr int kFewTile = 16;                 // slots a warp takes at a time
 constexpr int kFewMinTiles = 2;              // fewest tiles of a warp
 constexpr int few_warps_sm(int d) { return d == 64 ? 12 : 8; }

@@ -56,8 +56,9 @@ int check_rotate(int B, int L, int Hq, int Hk, int d, int dtype, const int32_t* 
 }
 
 struct CacheLayout {
-  size_t lse, share, scores, ml, part, moved, pairs, free_places, evict, total;
+  size_t lse, share, scores, sums, ml, part, moved, pairs, free_places, evict, total;
   int splits, warps, pitch;
+  bool stored;
   long long pair_pitch, free_pitch;
 };
 
@@ -75,7 +76,7 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   CacheLayout w;
   const size_t units = static_cast<size_t>(B) * Hk, lists = static_cast<size_t>(B) * G;
   const size_t M = static_cast<size_t>(T) * (H / Hk);
-  const bool few = M <= kFewRows, stored = M <= kStoredRows;
+  const bool few = M <= kFewRows;
   // no more warps than the most tiles give work to
   w.splits = few ? 1 : splits_of(B, C, Hk, static_cast<int>(M), d);
   const size_t tiles = units * ((C + kFewTile - 1) / kFewTile);
@@ -83,9 +84,12 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   w.warps = static_cast<int>(std::min<size_t>(kCacheSms, (tiles + cta - 1) / cta)) * few_warps_sm(d);
   w.pitch = (C + 3) & ~3;
   const size_t parts = few ? w.warps + units : units * w.splits;
-  w.lse = w.share = kAlign;
-  w.scores = align_up(w.share + sizeof(int) * (1 + units));
-  w.ml = stored ? align_up(w.scores + sizeof(float) * units * M * w.pitch) : align_up(w.lse + sizeof(float) * units * M);
+  const size_t scores = sizeof(float) * units * M * w.pitch;
+  w.stored = M <= kJoinedRows || scores <= kStoredBytes;
+  w.share = w.lse = kAlign;
+  w.scores = align_up(kAlign + std::max(sizeof(int) * (1 + units), sizeof(float) * units * M));
+  w.sums = w.scores;
+  w.ml = align_up(w.scores + (w.stored ? scores : sizeof(float) * units * w.pitch));
   w.part = align_up(w.ml + sizeof(float2) * parts * M);
   const size_t attend = align_up(w.part + sizeof(float) * parts * M * d);
   w.pair_pitch = C / 2 + 1;
@@ -248,11 +252,12 @@ extern "C" int sc_cache_attend(const sc_cache_attend_args* a, void* workspace, s
   p.scale2 = static_cast<float>(static_cast<double>(a->scale) * 1.4426950408889634);   // log2(e)
   p.decay = a->decay;
   p.o = static_cast<uint16_t*>(a->O); p.ldo = a->ldo; p.acc_out = a->acc_out;
-  p.splits = w.splits; p.warps = w.warps; p.pitch = w.pitch;
+  p.splits = w.splits; p.warps = w.warps; p.pitch = w.pitch; p.stored = w.stored;
   char* ws = static_cast<char*>(workspace);
   p.lse = reinterpret_cast<float*>(ws + w.lse);
   p.share = reinterpret_cast<int*>(ws + w.share);
   p.scores = reinterpret_cast<float*>(ws + w.scores);
+  p.sums = reinterpret_cast<float*>(ws + w.sums);
   p.ml = reinterpret_cast<float2*>(ws + w.ml);
   p.part = reinterpret_cast<float*>(ws + w.part);
   const cudaError_t e = launch_attend(p, a->d, a->dtype, static_cast<cudaStream_t>(stream));

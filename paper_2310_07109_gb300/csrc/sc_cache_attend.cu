@@ -172,9 +172,9 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
     const int hidden = __syncthreads_count(unseen);   // (and the tile before this one is done with)
     load(tile + kStages - 1);
     if (hidden == kKeyTile) {
-      if (kGroups == 2) {   // (the sums read every score)
+      if (kGroups == 2 || p.stored) {   // (the sums read every score)
         const int j = tile * kKeyTile + static_cast<int>(threadIdx.x) % kKeyTile;
-        for (int m = m0 + threadIdx.x / kKeyTile; m < rows_m && j < l.n; m += kAttendThreads / kKeyTile)
+        for (int m = m0 + threadIdx.x / kKeyTile; m < min(rows_m, m0 + kRows) && j < l.n; m += kAttendThreads / kKeyTile)
           scores[static_cast<long long>(m) * p.pitch + j] = -INFINITY;
       }
       continue;
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
         c[i][k] = sees ? c[i][k] * p.scale2 : -INFINITY;
         top[k >> 1] = fmaxf(top[k >> 1], c[i][k] - T::kHeadroom);
       }
-      if (kGroups == 2) store_scores(p, scores, m0 + row0, rows_m, tile * kKeyTile + key, l.n, c[i]);
+      if (kGroups == 2 || p.stored) store_scores(p, scores, m0 + row0, rows_m, tile * kKeyTile + key, l.n, c[i]);
     }
     float keep[2];
 #pragma unroll
@@ -365,8 +365,8 @@ struct SumsSmem {
   float sum[kAttendWarps][kSlots];   // by 16 rows of a row tile
 };
 
-// A CTA has a stretch of a list's slots: the weights of all rows of the list's heads.  The keys of a head stay in shared memory
-// while its rows pass, a tile of them at a time.
+// A CTA has a stretch of a key head's slots: the weights of all its rows.  The keys stay in shared memory while the
+// rows pass, a tile of them at a time.
 template <class T, int D>
 __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const AttendParams p) {
   using S = SumsSmem<D>;
@@ -376,27 +376,20 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
   pdl_wait();
   pdl_launch_dependents();
   const int pieces = (p.C + S::kSlots - 1) / S::kSlots;
-  const int piece = blockIdx.x % pieces, list = blockIdx.x / pieces, b = list / p.G, g = list - b * p.G;
-  const ListOf l = list_of(p, b, g);
+  const int piece = blockIdx.x % pieces, unit = blockIdx.x / pieces, b = unit / p.Hk, hk = unit - b * p.Hk;
+  const int list = b * p.G + hk / (p.Hk / p.G);
+  const ListOf l = list_of(p, b, list - b * p.G);
   const int j0 = piece * S::kSlots, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (j0 >= l.n) return;
+  if (j0 >= l.n || l.rows == 0) return;
   const long long at0 = static_cast<long long>(list) * p.C + j0;
-  if (l.rows == 0) {
-    for (int j = threadIdx.x; j < S::kSlots && j0 + j < l.n; j += kAttendThreads) p.acc_out[at0 + j] = p.acc[at0 + j];
-    return;
-  }
-  const int of = p.Hk / p.G, rows_m = l.rows * p.R, tiles_m = (rows_m + kRows - 1) / kRows;
+  const int rows_m = l.rows * p.R, tiles_m = (rows_m + kRows - 1) / kRows;
   const int row0 = warp * 16, tiles = min(S::kTiles, (l.n - j0 + kKeyTile - 1) / kKeyTile);
-  const int steps = of * tiles_m;
   auto load = [&](int step) {
-    load_q<D>(p, b, g * of + step / tiles_m, step % tiles_m * kRows, l.rows, kRows, smem_u32(sm.q[step & 1]));
+    load_q<D>(p, b, hk, step * kRows, l.rows, kRows, smem_u32(sm.q[step & 1]));
   };
-  auto keys = [&](int hk) {
-    for (int t = 0; t < tiles; ++t)
-      load_keys<D>(p, p.k + b * p.stride_b + hk * p.stride_h, j0 + t * kKeyTile, l.n, smem_u32(sm.k + t * kKeyTile * D));
-  };
+  for (int t = 0; t < tiles; ++t)
+    load_keys<D>(p, p.k + b * p.stride_b + hk * p.stride_h, j0 + t * kKeyTile, l.n, smem_u32(sm.k + t * kKeyTile * D));
   load(0);
-  keys(g * of);
   cp_async_commit();
   for (int t = warp; t < S::kTiles; t += kAttendWarps) {
     int least = 0x7fffffff;
@@ -409,19 +402,19 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
     if (lane == 0) sm.least[t] = least;
   }
   for (int i = threadIdx.x; i < kAttendWarps * S::kSlots; i += kAttendThreads) (&sm.sum[0][0])[i] = 0.f;
-  for (int step = 0; step < steps; ++step) {
-    const int hk = g * of + step / tiles_m, m0 = step % tiles_m * kRows;
+  for (int step = 0; step < tiles_m; ++step) {
+    const int m0 = step * kRows;
     float lse[2];
     int at[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int m = m0 + row0 + (lane >> 2) + 8 * u;
-      lse[u] = m < rows_m ? p.lse[(static_cast<long long>(b) * p.Hk + hk) * p.M + m] : INFINITY;
+      lse[u] = m < rows_m ? p.lse[static_cast<long long>(unit) * p.M + m] : INFINITY;
       at[u] = m < rows_m ? l.first + m / p.R : -1;
     }
     cp_async_wait_all();
     __syncthreads();
-    if (step + 1 < steps) load(step + 1);
+    if (step + 1 < tiles_m) load(step + 1);
     cp_async_commit();
     const uint32_t sq = smem_u32(sm.q[step & 1]);
     const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R;
@@ -469,19 +462,82 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
         }
       }
     }
-    if (step + 1 < steps && (step + 1) % tiles_m == 0) {   // the next head's keys
-      __syncthreads();
-      keys(hk + 1);
-      cp_async_commit();
-    }
   }
   __syncthreads();
   for (int j = threadIdx.x; j < S::kSlots && j0 + j < l.n; j += kAttendThreads) {
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < kAttendWarps; ++w) v += sm.sum[w][j];
-    p.acc_out[at0 + j] = p.decay * p.acc[at0 + j] + v / static_cast<float>(p.H / p.G);
+    p.sums[static_cast<long long>(unit) * p.pitch + j0 + j] = v;
   }
+}
+
+// A list's slots, one a thread: the sums of its heads, in order.
+__global__ void __launch_bounds__(256) attend_heads_kernel(const AttendParams p) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int pieces = (p.C + 255) / 256, list = blockIdx.x / pieces, b = list / p.G, g = list - b * p.G, of = p.Hk / p.G;
+  const int j = (blockIdx.x - list * pieces) * 256 + static_cast<int>(threadIdx.x);
+  const ListOf l = list_of(p, b, g);
+  if (j >= l.n) return;
+  const long long at = static_cast<long long>(list) * p.C + j;
+  const float* sums = p.sums + (static_cast<long long>(b) * p.Hk + g * of) * p.pitch + j;
+  float v = 0.f;
+  if (l.rows > 0) {
+#pragma unroll 8
+    for (int h = 0; h < of; ++h) v += sums[static_cast<long long>(h) * p.pitch];
+  }
+  p.acc_out[at] = l.rows > 0 ? p.decay * p.acc[at] + v / static_cast<float>(p.H / p.G) : p.acc[at];
+}
+
+// Slots of a list whose scores are kept and whose rows' LSE are known: eight warps have every eighth row each of 128
+// slots, and their sums are added in order.
+constexpr int kStoredSlots = 128;
+__global__ void __launch_bounds__(256) attend_stored_sums_kernel(const AttendParams p) {
+  __shared__ float4 part[8][kStoredSlots / 4];
+  pdl_wait();
+  pdl_launch_dependents();
+  const int pieces = (p.C + kStoredSlots - 1) / kStoredSlots, list = blockIdx.x / pieces, b = list / p.G, g = list - b * p.G;
+  const int of = p.Hk / p.G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int j0 = (blockIdx.x - list * pieces) * kStoredSlots, j = j0 + 4 * lane;
+  const ListOf l = list_of(p, b, g);
+  if (j0 >= l.n) return;
+  const int rows_m = l.rows * p.R, rows = of * rows_m;
+  const long long unit0 = static_cast<long long>(b) * p.Hk + g * of, at = static_cast<long long>(list) * p.C + j0 + threadIdx.x;
+  const bool mine = threadIdx.x < kStoredSlots && j0 + static_cast<int>(threadIdx.x) < l.n;
+  const float old = mine ? p.acc[at] : 0.f;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kAhead = 8;
+  if (j < l.n)
+    for (int r0 = warp; r0 < rows; r0 += 8 * kAhead) {
+      float4 t[kAhead];
+      float x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int r = r0 + 8 * u, h = r / rows_m;
+        const long long row = (unit0 + h) * p.M + r - h * rows_m;
+        x[u] = INFINITY;
+        t[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < rows) {
+          x[u] = p.lse[row];
+          t[u] = *reinterpret_cast<const float4*>(p.scores + row * p.pitch + j);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        sum.x += ex2(t[u].x - x[u]);
+        sum.y += ex2(t[u].y - x[u]);
+        sum.z += ex2(t[u].z - x[u]);
+        sum.w += ex2(t[u].w - x[u]);
+      }
+    }
+  part[warp][lane] = sum;
+  __syncthreads();
+  if (!mine) return;
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) v += reinterpret_cast<const float*>(part[w])[threadIdx.x];
+  p.acc_out[at] = l.rows > 0 ? p.decay * old + v / static_cast<float>(p.H / p.G) : old;
 }
 
 // ---------------------------------------------------------------------------
@@ -1011,7 +1067,7 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
   const int tiles_m = (p.M + kRowTile - 1) / kRowTile;
   const dim3 rows(static_cast<unsigned>(units * tiles_m * p.splits));
   const size_t rows_bytes = sizeof(RowsSmem<D>) + 128;
-  if (p.M <= kStoredRows) {   // scores kept
+  if (p.M <= kJoinedRows) {   // scores kept, rows and weights in one launch
     constexpr int kWarps = FewShape<D>::kWarps;
     const bool few = p.M <= kFewRows;
     cudaError_t e = few ? launch_chained(attend_few_kernel<T, D>, dim3(p.warps / kWarps), dim3(FewShape<D>::kThreads), FewShape<D>::kBytes, st, p)
@@ -1030,9 +1086,14 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
   e = launch_chained(attend_join_kernel<T, D>, dim3(static_cast<unsigned>((units * p.M + kJoinWarps - 1) / kJoinWarps)),
                      dim3(kJoinWarps * 32), 0, st, p);
   if (e != cudaSuccess) return e;
+  const long long lists = static_cast<long long>(p.B) * p.G;
+  if (p.stored)
+    return launch_chained(attend_stored_sums_kernel, dim3(static_cast<unsigned>(lists * ((p.C + kStoredSlots - 1) / kStoredSlots))),
+                          dim3(256), 0, st, p);
   const long long pieces = (p.C + SumsSmem<D>::kSlots - 1) / SumsSmem<D>::kSlots;
-  return launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(pieces * p.B * p.G)), threads,
-                        sizeof(SumsSmem<D>) + 128, st, p);
+  e = launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(pieces * units)), threads, sizeof(SumsSmem<D>) + 128, st, p);
+  if (e != cudaSuccess) return e;
+  return launch_chained(attend_heads_kernel, dim3(static_cast<unsigned>(lists * ((p.C + 255) / 256))), dim3(256), 0, st, p);
 }
 
 }  // namespace

@@ -194,6 +194,11 @@ ATTEND = [  # B, T, H, Hk, G, d, C, lens, rows, dtype, order
     (1, 130, 3, 1, 1, 64, 130, [130], None, HF, None),
     (1, 1, 2, 2, 1, 64, 9000, [8999], None, BF, None),             # many parts of a list
     (1, 2, 4, 1, 1, 128, 5000, [4097], None, BF, None),
+    (2, 20, 4, 2, 1, 64, 301, [300, 128], [20, 0], HF, (0, 2, 1, 3)),   # 40 rows a key head, two heads a list
+    (3, 9, 30, 5, 5, 64, 35, [35, 9, [10, 35, 0, 9, 12]], None, BF, None),
+    (1, 512, 4, 2, 1, 64, 4200, [4100], [500], BF, None),          # scores of more than 32 MB
+    (1, 600, 2, 1, 1, 128, 7200, [7150], None, HF, (2, 0, 1, 3)),
+    (2, 700, 3, 3, 3, 64, 3000, [[3000, 700, 64], 2990], [700, 3], BF, None),
 ]
 
 
