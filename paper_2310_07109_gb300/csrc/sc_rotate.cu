@@ -237,8 +237,9 @@ __device__ __forceinline__ void gamma_of(const float* gamma, const LaneShare& s,
   }
 }
 
+// (as it stands when all CTAs have read it)
 __device__ __forceinline__ int cache_len(const RotateParams& p, int list) {
-  return min(max(p.len[list], 0), p.C);
+  return min(max(__ldcg(p.len + list), 0), p.C);
 }
 
 // Forward, and append where cache_k is set.
@@ -300,25 +301,25 @@ __global__ void __launch_bounds__(kRotateThreads, kSmWarps / kRotateWarps) rotat
     rotate<false, kInter>(a, b, cos, sin, s);
     uint4 ya, yb;
     pack<T, kInter>(a, b, ya, yb);
+    bool live = s.live;
     if (append) {
       const int b_u = __shfl_sync(0xffffffffu, at.b, number), r_u = __shfl_sync(0xffffffffu, at.r, number);
-      const int pos = __shfl_sync(0xffffffffu, at.pos, number);
       if (to_cache) {
-        const int c = cache_len(p, b_u * p.G + list) + r_u;
-        if (c >= p.C) return;
+        const int c = min(max(__ldg(p.len + b_u * p.G + list), 0), p.C) + r_u;
         to = dst + b_u * p.stride_b + c * p.stride_c;
-        if (s.side == 2) {
-          ya = xa;
-          yb = xb;
-        }
-        if (marks) {
+        live = live && c < p.C;
+        if (marks && live) {
           const long long slot = (static_cast<long long>(b_u) * p.G + list) * p.C + c;
           p.acc[slot] = 0.f;
-          p.slot_pos[slot] = pos;
+          p.slot_pos[slot] = __ldg(p.seen + b_u) + r_u;
         }
       }
+      if (s.side == 2) {
+        ya = xa;
+        yb = xb;
+      }
     }
-    if (!s.live) return;
+    if (!live) return;
     reinterpret_cast<uint4*>(to)[s.va] = ya;
     reinterpret_cast<uint4*>(to)[s.vb] = yb;
   };
