@@ -7,7 +7,7 @@
 // nearly every row behind the first one (half of 8192 slots: 2048 rows instead of 4096).
 //
 // Two launches:
-//   pick   a CTA a list.  Its slots' 32-bit keys (acc's bits in an order-preserving form) go into shared memory; the
+//   pick   a CTA a list, or a cluster of up to eight with a stretch of a long list each.  Its slots' 32-bit keys (acc's bits in an order-preserving form) go into shared memory; the
 //          cut is found in passes over them, each of which cuts the range that holds it into at most 256 equal parts
 //          (by bits of the difference to its lower end: keys are logarithms nearly, so weights spread over the parts;
 //          digits of the keys themselves put most of them into two or three, whose additions wait for one another:
@@ -28,7 +28,8 @@ constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kMoveThreads = 256;
 constexpr int kMoveSlots = 1024;   // whose acc and pos a CTA moves
 constexpr uint32_t kProtected = 0xffffffffu;
-constexpr int kKeysHeld = 40960;   // most keys in shared memory (160 KB); longer lists are read again for each pass
+constexpr int kPickSlots = 8192;     // of a CTA, where there are SMs for more CTAs
+constexpr int kMostSlots = SC_MAX_CACHE / 8;
 constexpr int kParts = 256;
 
 // What a slot ranks by: protected, then acc in order (-0 as 0); a NaN, or a slot without a position, last.
@@ -41,13 +42,23 @@ __device__ __forceinline__ uint32_t rank_key(const EvictParams& p, float acc, in
 }
 
 struct PickSmem {
-  uint32_t hist[kParts];
+  uint32_t hist[2][kParts];   // of every other pass: the cluster's CTAs read one while the next is cleared
   uint32_t low[kPickWarps], high[kPickWarps];
   int count[kPickWarps][2];
-  int found[3];   // part, how many of it are still to take, how many it has
+  uint32_t range[4];   // of the CTA: lowest and highest key, protected ones, those that rank last
+  int ties;            // of the CTA
+  uint32_t places;     // of the CTA: free ones, fillers << 16
+  int found[3];        // part, how many of it are still to take, how many it has
 };
 
-// Exclusive prefix over the CTA's threads of two counts (each below 2^16 in all, packed), and their totals.
+// A word of the shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t of_rank(const void* word, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(smem_u32(word), rank)) : "memory");
+  return v;
+}
+
+// Exclusive prefix over the CTA's threads of two counts (each below 2^16 in all, packed; or of one), and their totals.
 __device__ __forceinline__ uint32_t scan_cta(PickSmem& sm, uint32_t v, uint32_t& all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t upto = v;
@@ -64,34 +75,44 @@ __device__ __forceinline__ uint32_t scan_cta(PickSmem& sm, uint32_t v, uint32_t&
   return __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + upto - v;
 }
 
+template <int kCtas>
 __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const EvictParams p) {
   static_assert(kPickWarps == 32, "a lane a warp");
   __shared__ PickSmem sm;
   extern __shared__ uint32_t held[];   // keys, then two bits a slot
   pdl_wait();
   pdl_launch_dependents();
-  const int list = blockIdx.x, b = list / p.G, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int list = blockIdx.x / kCtas, rank = blockIdx.x % kCtas, b = list / p.G, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long base = static_cast<long long>(list) * p.C;
-  const float* acc = p.acc + base;
-  const int32_t* pos = p.pos + base;
   const int n = min(max(__ldcg(p.len + list), 0), p.C), k = p.budget;
   const int late = __ldg(p.seen + b) - p.recent;
-  if (n <= k || n - k <= p.slack) {
-    __syncthreads();   // len is read
-    if (tid == 0) {
+  auto sync = [&]() {
+    if (kCtas > 1)
+      cluster_sync();
+    else
+      __syncthreads();
+  };
+  if (n <= k || n - k <= p.slack) {   // (of all CTAs of the list)
+    sync();   // len is read
+    if (tid == 0 && rank == 0) {
       p.moved[list] = 0;
       p.len_out[list] = n;
     }
     return;
   }
-  const bool hold = n <= kKeysHeld;
-  uint32_t* above = held + min(p.C, kKeysHeld);
-  uint32_t* tied = above + (p.C + 31) / 32;
+  // this CTA's slots first .. first + own - 1
+  const int stretch = (((n + kCtas - 1) / kCtas) + 31) & ~31, first = min(rank * stretch, n), own = min(stretch, n - first);
+  const float* acc = p.acc + base + first;
+  const int32_t* pos = p.pos + base + first;
+  const int room = ((p.C + kCtas - 1) / kCtas + 31) & ~31;
+  uint32_t* above = held + room;
+  uint32_t* tied = above + room / 32;
+  if (tid < kParts) sm.hist[0][tid] = 0;
   // protected ones and those that rank last apart, the range of the others' keys
   uint32_t low = 0xffffffffu, high = 0;
   int safe = 0, none = 0;
   constexpr int kBatch = 8;
-  for (int j0 = tid; j0 < n; j0 += kBatch * kPickThreads) {
+  for (int j0 = tid; j0 < own; j0 += kBatch * kPickThreads) {
     float a[kBatch];
     int q[kBatch];
 #pragma unroll
@@ -99,7 +120,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
       const int j = j0 + u * kPickThreads;
       a[u] = 0.f;
       q[u] = -1;
-      if (j < n) {
+      if (j < own) {
         a[u] = __ldcg(acc + j);
         q[u] = __ldcg(pos + j);
       }
@@ -107,9 +128,9 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       const int j = j0 + u * kPickThreads;
-      if (j >= n) break;
+      if (j >= own) break;
       const uint32_t key = rank_key(p, a[u], q[u], late);
-      if (hold) held[j] = key;
+      held[j] = key;
       safe += key == kProtected;
       none += key == 0;
       if (key != kProtected && key != 0) {
@@ -133,7 +154,21 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
   high = __reduce_max_sync(0xffffffffu, sm.high[lane]);
   safe = __reduce_add_sync(0xffffffffu, sm.count[lane][0]);
   none = __reduce_add_sync(0xffffffffu, sm.count[lane][1]);
-  auto key_at = [&](int j) { return hold ? held[j] : rank_key(p, __ldcg(acc + j), __ldcg(pos + j), late); };
+  if (kCtas > 1) {
+    if (tid == 0) {
+      sm.range[0] = low;
+      sm.range[1] = high;
+      sm.range[2] = safe;
+      sm.range[3] = none;
+    }
+    cluster_sync();
+    const uint32_t r = lane < kCtas ? lane : 0;
+    low = __reduce_min_sync(0xffffffffu, of_rank(&sm.range[0], r));
+    high = __reduce_max_sync(0xffffffffu, of_rank(&sm.range[1], r));
+    const uint32_t s = of_rank(&sm.range[2], r), z = of_rank(&sm.range[3], r);
+    safe = __reduce_add_sync(0xffffffffu, lane < kCtas ? s : 0);
+    none = __reduce_add_sync(0xffffffffu, lane < kCtas ? z : 0);
+  }
   // keys above `high` survive, and the first `want` of the `count` ones from low to high: all of them, or low is high
   int want = k - safe, count = n - safe - none;
   if (want <= 0) {
@@ -145,20 +180,30 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
     want -= count;
     count = none;
   }
-  while (low != high && want != count) {
+  for (int pass = 0; low != high && want != count; pass ^= 1) {
+    uint32_t* hist = sm.hist[pass];
     const int shift = max(0, 24 - __clz(high - low));   // at most 256 parts of 2^shift
-    if (tid < kParts) sm.hist[tid] = 0;
-    __syncthreads();
 #pragma unroll 4
-    for (int j = tid; j < n; j += kPickThreads) {
-      const uint32_t key = key_at(j);
-      if (key >= low && key <= high) atomicAdd(&sm.hist[(key - low) >> shift], 1u);
+    for (int j = tid; j < own; j += kPickThreads) {
+      const uint32_t key = held[j];
+      if (key >= low && key <= high) atomicAdd(&hist[(key - low) >> shift], 1u);
     }
-    __syncthreads();
-    if (warp == 0) {   // lane l has parts 255 - 8 l .. 248 - 8 l, the largest first
-      int own[8], total = 0;
+    sync();
+    if (tid < kParts) {
+      if (kCtas > 1) {
+        uint32_t all = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) total += own[i] = static_cast<int>(sm.hist[255 - 8 * lane - i]);
+        for (int r = 0; r < kCtas; ++r) all += of_rank(&hist[tid], r);
+        held[room + room / 16 + tid] = all;   // (behind the bits)
+      }
+      sm.hist[pass ^ 1][tid] = 0;
+    }
+    const uint32_t* counts = kCtas > 1 ? held + room + room / 16 : hist;
+    if (kCtas > 1) __syncthreads();
+    if (warp == 0) {   // lane l has parts 255 - 8 l .. 248 - 8 l, the largest first
+      int mine[8], total = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) total += mine[i] = static_cast<int>(counts[255 - 8 * lane - i]);
       int upto = total;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -169,12 +214,12 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
       if (before < want && want <= upto) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (before < want && want <= before + own[i]) {
+          if (before < want && want <= before + mine[i]) {
             sm.found[0] = 255 - 8 * lane - i;
             sm.found[1] = want - before;
-            sm.found[2] = own[i];
+            sm.found[2] = mine[i];
           }
-          before += own[i];
+          before += mine[i];
         }
       }
     }
@@ -186,12 +231,12 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
   }
   // a bit a slot
 #pragma unroll 4
-  for (int j0 = 0; j0 < n; j0 += kPickThreads) {
+  for (int j0 = 0; j0 < own; j0 += kPickThreads) {
     const int j = j0 + tid;
-    const uint32_t key = j < n ? key_at(j) : 0;
-    const uint32_t over = __ballot_sync(0xffffffffu, j < n && key > high);
-    const uint32_t in = __ballot_sync(0xffffffffu, j < n && key >= low && key <= high);
-    if (lane == 0 && j < n) {
+    const uint32_t key = j < own ? held[j] : 0;
+    const uint32_t over = __ballot_sync(0xffffffffu, j < own && key > high);
+    const uint32_t in = __ballot_sync(0xffffffffu, j < own && key >= low && key <= high);
+    if (lane == 0 && j < own) {
       above[j / 32] = over;
       tied[j / 32] = in;
     }
@@ -199,9 +244,19 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
   __syncthreads();
   const uint8_t* above8 = reinterpret_cast<const uint8_t*>(above);
   uint8_t* tied8 = reinterpret_cast<uint8_t*>(tied);
-  const int bytes = (n + 7) / 8;
+  const int bytes = (own + 7) / 8;
   if (want != count) {   // the first `want` of equal ones
     int done = 0;
+    if (kCtas > 1) {   // those of the CTAs before this one
+      int mine = 0;
+      for (int i = tid; i < bytes; i += kPickThreads) mine += __popc(tied8[i]);
+      uint32_t all;
+      scan_cta(sm, mine, all);
+      if (tid == 0) sm.ties = static_cast<int>(all);
+      cluster_sync();
+      const uint32_t c = of_rank(&sm.ties, lane < kCtas ? lane : 0);
+      done = __reduce_add_sync(0xffffffffu, lane < rank ? c : 0);
+    }
     for (int i0 = 0; i0 < bytes; i0 += kPickThreads) {
       const int i = i0 + tid;
       uint32_t in = i < bytes ? tied8[i] : 0u, all;
@@ -213,23 +268,43 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
   }
   // free places below k and survivors from k on, in order
   int2* pairs = p.pairs + list * p.pair_pitch;
-  uint8_t* free8 = p.free_places + list * p.free_pitch;
-  int free_at = 0, fill_at = 0;
+  uint8_t* free8 = p.free_places + list * p.free_pitch + first / 8;
+  auto of_byte = [&](int i, uint32_t& places, uint32_t& fills, uint32_t& low_ones) {
+    const int j = first + 8 * i;
+    const uint32_t keep = i < bytes ? above8[i] | tied8[i] : 0u;
+    low_ones = j >= k ? 0u : k - j >= 8 ? 0xffu : (1u << (k - j)) - 1u;   // slots below k
+    places = i < bytes ? ~keep & low_ones : 0u;
+    fills = keep & ~low_ones & 0xffu;
+  };
+  int free_at = 0, fill_at = 0, all_free = 0;
+  if (kCtas > 1) {   // those of the CTAs before this one (its own are at most 2^15 each)
+    uint32_t mine = 0, all, places, fills, low_ones;
+    for (int i = tid; i < bytes; i += kPickThreads) {
+      of_byte(i, places, fills, low_ones);
+      mine += __popc(places) | __popc(fills) << 16;
+    }
+    scan_cta(sm, mine, all);
+    if (tid == 0) sm.places = all;
+    cluster_sync();
+    const uint32_t c = of_rank(&sm.places, lane < kCtas ? lane : 0);
+    free_at = __reduce_add_sync(0xffffffffu, lane < rank ? c & 0xffffu : 0);
+    fill_at = __reduce_add_sync(0xffffffffu, lane < rank ? c >> 16 : 0);
+    all_free = __reduce_add_sync(0xffffffffu, lane < kCtas ? c & 0xffffu : 0);
+  }
   for (int i0 = 0; i0 < bytes; i0 += kPickThreads) {
-    const int i = i0 + tid, j = 8 * i;
-    uint32_t keep = i < bytes ? above8[i] | tied8[i] : 0u;
-    const uint32_t low_ones = j >= k ? 0u : k - j >= 8 ? 0xffu : (1u << (k - j)) - 1u;   // slots below k
-    uint32_t places = i < bytes ? ~keep & low_ones : 0u, all;
-    uint32_t fills = keep & ~low_ones & 0xffu;
+    const int i = i0 + tid, j = first + 8 * i;
+    uint32_t places, fills, low_ones, all;
+    of_byte(i, places, fills, low_ones);
     const uint32_t before = scan_cta(sm, __popc(places) | __popc(fills) << 16, all);
-    if (low_ones != 0) free8[i] = static_cast<uint8_t>(places);
+    if (low_ones != 0 && i < bytes) free8[i] = static_cast<uint8_t>(places);
     for (int at = free_at + static_cast<int>(before & 0xffffu); places != 0; places &= places - 1) pairs[at++].x = j + __ffs(places) - 1;
     for (int at = fill_at + static_cast<int>(before >> 16); fills != 0; fills &= fills - 1) pairs[at++].y = j + __ffs(fills) - 1;
     free_at += static_cast<int>(all & 0xffffu);
     fill_at += static_cast<int>(all >> 16);
   }
-  if (tid == 0) {
-    p.moved[list] = free_at;
+  if (kCtas > 1) cluster_sync();   // (all have read all; len too)
+  if (tid == 0 && rank == 0) {
+    p.moved[list] = kCtas > 1 ? all_free : free_at;
     p.len_out[list] = k;
   }
 }
@@ -314,13 +389,55 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
   }
 }
 
+namespace {
+
+// Keys of a CTA's share of a list, two bits a slot, and the cluster's counts.
+template <int kCtas>
+size_t pick_bytes(int C) {
+  const int room = ((C + kCtas - 1) / kCtas + 31) & ~31;
+  return sizeof(uint32_t) * (room + room / 16 + (kCtas > 1 ? kParts : 0));
+}
+
+template <int kCtas>
+cudaError_t launch_pick(const EvictParams& p, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.B * p.G * kCtas);
+  cfg.blockDim = dim3(kPickThreads);
+  cfg.dynamicSmemBytes = pick_bytes<kCtas>(p.C);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCtas;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = kCtas > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, evict_pick_kernel<kCtas>, p);
+}
+
+template <int kCtas>
+cudaError_t configure_pick() {
+  return cudaFuncSetAttribute(evict_pick_kernel<kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(pick_bytes<kCtas>(std::min(SC_MAX_CACHE, kMostSlots * kCtas))));
+}
+
+}  // namespace
+
 cudaError_t configure_evict() {
-  return cudaFuncSetAttribute(evict_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeysHeld * 4 + SC_MAX_CACHE / 8 * 2);
+  cudaError_t e = configure_pick<1>();
+  if (e == cudaSuccess) e = configure_pick<2>();
+  if (e == cudaSuccess) e = configure_pick<4>();
+  return e == cudaSuccess ? configure_pick<8>() : e;
 }
 
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
-  const size_t held = sizeof(uint32_t) * (std::min(p.C, kKeysHeld) + 2 * ((p.C + 31) / 32));
-  cudaError_t e = launch_chained(evict_pick_kernel, dim3(p.B * p.G), dim3(kPickThreads), held, st, p);
+  // CTAs of a list: as many as its slots need, and more while there are SMs for them
+  int n = 1;
+  while (n < 8 && ((p.C + n - 1) / n > kMostSlots ||
+                   ((p.C + n - 1) / n > kPickSlots && static_cast<long long>(p.B) * p.G * n < kCacheSms)))
+    n *= 2;
+  cudaError_t e = n == 1 ? launch_pick<1>(p, st) : n == 2 ? launch_pick<2>(p, st) : n == 4 ? launch_pick<4>(p, st) : launch_pick<8>(p, st);
   const bool evicts = p.budget < p.C, apart = p.acc_out != p.acc || p.pos_out != p.pos;
   if (e != cudaSuccess || (!evicts && !apart)) return e;
   const long long units = static_cast<long long>(p.B) * p.Hk;

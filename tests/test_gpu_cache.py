@@ -344,6 +344,10 @@ def check_evict(cache, **kw):
     (3, 1, 1, 16, 40, [40, 39, 3], dict(budget=1000), BF, None),
     (1, 1, 1, 96, 70001, [70000], dict(budget=30000, recent=5000), BF, None),
     (1, 2, 2, 64, 5000, [[5000, 2500]], dict(budget=2500, recent=2500), BF, None),
+    (2, 1, 1, 16, 9000, [9000, 33], dict(budget=32), BF, None),                       # two CTAs a list
+    (1, 2, 2, 16, 20001, [[20001, 10]], dict(budget=10000, sinks=3, recent=99), HF, None),   # four
+    (3, 1, 1, 16, 50003, [50003, 40000, 7], dict(budget=7000, slack=100), BF, None),      # eight
+    (200, 1, 1, 16, 8300, [8300 - i for i in range(200)], dict(budget=8200), BF, None),    # too many for more than one
 ])
 def test_evict(B, Hk, G, d, C, lens, kw, dtype, order):
     g = gen(C + d)
@@ -351,7 +355,7 @@ def test_evict(B, Hk, G, d, C, lens, kw, dtype, order):
 
 
 @pytest.mark.parametrize("kind", ["equal", "zeros", "coarse", "extremes", "negative", "hidden", "same top bits"])
-@pytest.mark.parametrize("n,budget", [(200, 64), (3000, 1500), (3000, 2999)])
+@pytest.mark.parametrize("n,budget", [(200, 64), (3000, 1500), (3000, 2999), (33000, 20000)])
 def test_evict_ranks(kind, n, budget):
     g = gen(n + budget)
     cache = make_cache(g, 2, 2, n + 3, 64, 2, [n, n - 7])
