@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
   int at[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) at[u] = l.first + (m0 + row0 + (lane >> 2) + 8 * u) / p.R;
-  const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R;   // the latest row of the tile
+  const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R;   // the latest row of the tile,
+  const int first_at = l.first + (m0 + row0) / p.R;                   // and the warp's earliest
 
   if (t0 < t1) load_q<D>(p, b, hk, m0, l.rows, kRows, sq);
 #pragma unroll
@@ -205,17 +206,25 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
       }
     }
     float top[2] = {ref[0], ref[1]};
+    // whether every row sees every slot of the tile: looked up once for the tile, not for each score
+    const int w0 = sm.pos[s][lane], w1 = sm.pos[s][32 + lane];
+    const bool whole = __all_sync(0xffffffffu, (tile + 1) * kKeyTile <= l.n && w0 >= 0 && w0 <= first_at && w1 >= 0 && w1 <= first_at);
 #pragma unroll
     for (int i = 0; i < kKeys / 8; ++i) {
       const int key = key0 + 8 * i + 2 * (lane & 3);
-      const int2 where = *reinterpret_cast<const int2*>(&sm.pos[s][key]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int w = k & 1 ? where.y : where.x;
-        const bool sees = tile * kKeyTile + key + (k & 1) < l.n && w >= 0 && w <= at[k >> 1];
-        c[i][k] = sees ? c[i][k] * p.scale2 : -INFINITY;
-        top[k >> 1] = fmaxf(top[k >> 1], c[i][k] - T::kHeadroom);
+      for (int k = 0; k < 4; ++k) c[i][k] *= p.scale2;
+      if (!whole) {
+        const int2 where = *reinterpret_cast<const int2*>(&sm.pos[s][key]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int w = k & 1 ? where.y : where.x;
+          const bool sees = tile * kKeyTile + key + (k & 1) < l.n && w >= 0 && w <= at[k >> 1];
+          c[i][k] = sees ? c[i][k] : -INFINITY;
+        }
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) top[k >> 1] = fmaxf(top[k >> 1], c[i][k] - T::kHeadroom);
       if (kGroups == 2 || p.stored) store_scores(p, scores, m0 + row0, rows_m, tile * kKeyTile + key, l.n, c[i]);
     }
     float keep[2];
@@ -361,7 +370,7 @@ struct SumsSmem {
   alignas(128) uint16_t k[kSlots * D];
   alignas(128) uint16_t q[2][kRowTile * D];
   int pos[kSlots];
-  int least[kTiles];   // the least position of each tile's slots
+  int least[kTiles], most[kTiles];   // the least and the greatest position of each tile's slots
   float sum[kAttendWarps][kSlots];   // by 16 rows of a row tile
 };
 
@@ -392,14 +401,19 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
   load(0);
   cp_async_commit();
   for (int t = warp; t < S::kTiles; t += kAttendWarps) {
-    int least = 0x7fffffff;
+    int least = 0x7fffffff, most = 0;
     for (int j = t * kKeyTile + lane; j < (t + 1) * kKeyTile; j += 32) {
       const int where = j0 + j < l.n ? __ldg(p.pos + at0 + j) : -1;
       sm.pos[j] = where < 0 ? 0x7fffffff : where;   // (seen by no row)
       least = min(least, sm.pos[j]);
+      most = max(most, sm.pos[j]);
     }
     least = __reduce_min_sync(0xffffffffu, least);
-    if (lane == 0) sm.least[t] = least;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) {
+      sm.least[t] = least;
+      sm.most[t] = most;
+    }
   }
   for (int i = threadIdx.x; i < kAttendWarps * S::kSlots; i += kAttendThreads) (&sm.sum[0][0])[i] = 0.f;
   for (int step = 0; step < tiles_m; ++step) {
@@ -417,13 +431,14 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
     if (step + 1 < tiles_m) load(step + 1);
     cp_async_commit();
     const uint32_t sq = smem_u32(sm.q[step & 1]);
-    const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R;
+    const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R, first_at = l.first + (m0 + row0) / p.R;
     if (m0 + row0 < rows_m) {
       uint32_t a[D / 16][4];
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) load_a<D>(sq, row0, k, lane, a[k]);
       for (int t = 0; t < tiles; ++t) {
         if (sm.least[t] > last) continue;
+        const bool whole = sm.most[t] <= first_at;   // (every row of the warp sees every slot)
         const uint32_t sk = smem_u32(sm.k + t * kKeyTile * D);
         float c[kKeyTile / 8][4];
 #pragma unroll
@@ -442,11 +457,15 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
 #pragma unroll
         for (int i = 0; i < kKeyTile / 8; ++i) {
           const int key = t * kKeyTile + 8 * i + 2 * (lane & 3);
-          const int2 where = *reinterpret_cast<const int2*>(&sm.pos[key]);
           float v[2];
-          // (a NaN of an unseen slot is kept out by the choice, not by a product)
-          v[0] = (where.x <= at[0] ? ex2(c[i][0] * p.scale2 - lse[0]) : 0.f) + (where.x <= at[1] ? ex2(c[i][2] * p.scale2 - lse[1]) : 0.f);
-          v[1] = (where.y <= at[0] ? ex2(c[i][1] * p.scale2 - lse[0]) : 0.f) + (where.y <= at[1] ? ex2(c[i][3] * p.scale2 - lse[1]) : 0.f);
+          if (whole) {
+            v[0] = ex2(c[i][0] * p.scale2 - lse[0]) + ex2(c[i][2] * p.scale2 - lse[1]);
+            v[1] = ex2(c[i][1] * p.scale2 - lse[0]) + ex2(c[i][3] * p.scale2 - lse[1]);
+          } else {   // (a NaN of an unseen slot is kept out by the choice, not by a product)
+            const int2 where = *reinterpret_cast<const int2*>(&sm.pos[key]);
+            v[0] = (where.x <= at[0] ? ex2(c[i][0] * p.scale2 - lse[0]) : 0.f) + (where.x <= at[1] ? ex2(c[i][2] * p.scale2 - lse[1]) : 0.f);
+            v[1] = (where.y <= at[0] ? ex2(c[i][1] * p.scale2 - lse[0]) : 0.f) + (where.y <= at[1] ? ex2(c[i][3] * p.scale2 - lse[1]) : 0.f);
+          }
           // over the eight pairs of rows; each of them keeps two of the sums' sixteen columns
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
