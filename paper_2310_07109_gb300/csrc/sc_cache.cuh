@@ -124,7 +124,8 @@ struct AttendParams {
   int warps;                 // at work on the tiles of all lists
   int* share;                // tiles a warp, then [B][Hk] the first tile of each unit
   int stored;                // the scores are kept
-  float* sums;               // [B][Hk][pitch] where they are not: the weights' sums over a key head's rows
+  int row_parts;             // where they are not: parts that CTAs take a key head's rows in,
+  float* sums;               // [B][Hk][row_parts][pitch] and the weights' sums over each
   float* scores;             // [B][Hk][M][pitch] scale log2(e) q . k; -inf: not seen
   int pitch;
   // both: parts (many rows: [B][Hk][splits]; few: a warp's number + a unit's)
@@ -133,6 +134,8 @@ struct AttendParams {
 };
 
 constexpr int kFewRows = 16;                 // most rows a key head that the kernel for few rows takes
+// Slots of a CTA that computes scores again: four tiles of 64, or two of wider heads.
+constexpr int sum_tiles(int d) { return d == 64 ? 4 : 2; }
 constexpr int kJoinedRows = 32;              // most rows that one launch joins and adds the weights of
 constexpr size_t kStoredBytes = 32u << 20;   // most bytes of the scores of more rows, else they are computed again
 constexpr int kFewTile = 16;                 // slots a warp takes at a time

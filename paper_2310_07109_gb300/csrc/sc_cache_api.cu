@@ -57,7 +57,7 @@ int check_rotate(int B, int L, int Hq, int Hk, int d, int dtype, const int32_t* 
 
 struct CacheLayout {
   size_t lse, share, scores, sums, ml, part, moved, pairs, free_places, evict, total;
-  int splits, warps, pitch;
+  int splits, warps, pitch, row_parts;
   bool stored;
   long long pair_pitch, free_pitch;
 };
@@ -86,10 +86,13 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   const size_t parts = few ? w.warps + units : units * w.splits;
   const size_t scores = sizeof(float) * units * M * w.pitch;
   w.stored = M <= kJoinedRows || scores <= kStoredBytes;
+  // parts of the rows, until the SMs have three CTAs each
+  const size_t ctas = units * ((C + 64 * sum_tiles(d) - 1) / (64 * sum_tiles(d)));
+  w.row_parts = static_cast<int>(std::max<size_t>(1, std::min<size_t>(3 * kCacheSms / ctas, (M + kRowsTile - 1) / kRowsTile)));
   w.share = w.lse = kAlign;
   w.scores = align_up(kAlign + std::max(sizeof(int) * (1 + units), sizeof(float) * units * M));
   w.sums = w.scores;
-  w.ml = align_up(w.scores + (w.stored ? scores : sizeof(float) * units * w.pitch));
+  w.ml = align_up(w.scores + (w.stored ? scores : sizeof(float) * units * w.row_parts * w.pitch));
   w.part = align_up(w.ml + sizeof(float2) * parts * M);
   const size_t attend = align_up(w.part + sizeof(float) * parts * M * d);
   w.pair_pitch = C / 2 + 1;
@@ -253,6 +256,7 @@ extern "C" int sc_cache_attend(const sc_cache_attend_args* a, void* workspace, s
   p.decay = a->decay;
   p.o = static_cast<uint16_t*>(a->O); p.ldo = a->ldo; p.acc_out = a->acc_out;
   p.splits = w.splits; p.warps = w.warps; p.pitch = w.pitch; p.stored = w.stored;
+  p.row_parts = w.row_parts;
   char* ws = static_cast<char*>(workspace);
   p.lse = reinterpret_cast<float*>(ws + w.lse);
   p.share = reinterpret_cast<int*>(ws + w.share);

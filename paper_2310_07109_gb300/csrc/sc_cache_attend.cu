@@ -362,8 +362,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const Atte
   if (lane == 0) p.lse[row] = none ? INFINITY : ref + log2f(total);
 }
 
-// Slots of a CTA of the sums: four tiles, or two of wider heads.
-constexpr int sum_tiles(int d) { return d == 64 ? 4 : 2; }
 template <int D>
 struct SumsSmem {
   static constexpr int kTiles = sum_tiles(D), kSlots = kTiles * kKeyTile;
@@ -374,8 +372,8 @@ struct SumsSmem {
   float sum[kAttendWarps][kSlots];   // by 16 rows of a row tile
 };
 
-// A CTA has a stretch of a key head's slots: the weights of all its rows.  The keys stay in shared memory while the
-// rows pass, a tile of them at a time.
+// A CTA has a stretch of a key head's slots: the weights of its rows, or of one of `row_parts` parts of them.  The keys
+// stay in shared memory while the rows pass, a tile of them at a time.
 template <class T, int D>
 __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const AttendParams p) {
   using S = SumsSmem<D>;
@@ -385,20 +383,21 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
   pdl_wait();
   pdl_launch_dependents();
   const int pieces = (p.C + S::kSlots - 1) / S::kSlots;
-  const int piece = blockIdx.x % pieces, unit = blockIdx.x / pieces, b = unit / p.Hk, hk = unit - b * p.Hk;
-  const int list = b * p.G + hk / (p.Hk / p.G);
+  const int piece = blockIdx.x % pieces, part = blockIdx.x / pieces % p.row_parts, unit = blockIdx.x / pieces / p.row_parts;
+  const int b = unit / p.Hk, hk = unit - b * p.Hk, list = b * p.G + hk / (p.Hk / p.G);
   const ListOf l = list_of(p, b, list - b * p.G);
   const int j0 = piece * S::kSlots, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (j0 >= l.n || l.rows == 0) return;
   const long long at0 = static_cast<long long>(list) * p.C + j0;
-  const int rows_m = l.rows * p.R, tiles_m = (rows_m + kRows - 1) / kRows;
+  const int rows_m = l.rows * p.R, tiles_m = (rows_m + kRows - 1) / kRows, per = (tiles_m + p.row_parts - 1) / p.row_parts;
+  const int step0 = min(part * per, tiles_m), step1 = min(step0 + per, tiles_m);
   const int row0 = warp * 16, tiles = min(S::kTiles, (l.n - j0 + kKeyTile - 1) / kKeyTile);
   auto load = [&](int step) {
     load_q<D>(p, b, hk, step * kRows, l.rows, kRows, smem_u32(sm.q[step & 1]));
   };
   for (int t = 0; t < tiles; ++t)
     load_keys<D>(p, p.k + b * p.stride_b + hk * p.stride_h, j0 + t * kKeyTile, l.n, smem_u32(sm.k + t * kKeyTile * D));
-  load(0);
+  if (step0 < step1) load(step0);
   cp_async_commit();
   for (int t = warp; t < S::kTiles; t += kAttendWarps) {
     int least = 0x7fffffff, most = 0;
@@ -416,7 +415,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
     }
   }
   for (int i = threadIdx.x; i < kAttendWarps * S::kSlots; i += kAttendThreads) (&sm.sum[0][0])[i] = 0.f;
-  for (int step = 0; step < tiles_m; ++step) {
+  for (int step = step0; step < step1; ++step) {
     const int m0 = step * kRows;
     float lse[2];
     int at[2];
@@ -428,7 +427,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
     }
     cp_async_wait_all();
     __syncthreads();
-    if (step + 1 < tiles_m) load(step + 1);
+    if (step + 1 < step1) load(step + 1);
     cp_async_commit();
     const uint32_t sq = smem_u32(sm.q[step & 1]);
     const int last = l.first + min(m0 + kRows - 1, rows_m - 1) / p.R, first_at = l.first + (m0 + row0) / p.R;
@@ -487,11 +486,11 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < kAttendWarps; ++w) v += sm.sum[w][j];
-    p.sums[static_cast<long long>(unit) * p.pitch + j0 + j] = v;
+    p.sums[(static_cast<long long>(unit) * p.row_parts + part) * p.pitch + j0 + j] = v;
   }
 }
 
-// A list's slots, one a thread: the sums of its heads, in order.
+// A list's slots, one a thread: the sums of its heads and their parts, in order.
 __global__ void __launch_bounds__(256) attend_heads_kernel(const AttendParams p) {
   pdl_wait();
   pdl_launch_dependents();
@@ -500,11 +499,11 @@ __global__ void __launch_bounds__(256) attend_heads_kernel(const AttendParams p)
   const ListOf l = list_of(p, b, g);
   if (j >= l.n) return;
   const long long at = static_cast<long long>(list) * p.C + j;
-  const float* sums = p.sums + (static_cast<long long>(b) * p.Hk + g * of) * p.pitch + j;
+  const float* sums = p.sums + (static_cast<long long>(b) * p.Hk + g * of) * p.row_parts * p.pitch + j;
   float v = 0.f;
   if (l.rows > 0) {
 #pragma unroll 8
-    for (int h = 0; h < of; ++h) v += sums[static_cast<long long>(h) * p.pitch];
+    for (int h = 0; h < of * p.row_parts; ++h) v += sums[static_cast<long long>(h) * p.pitch];
   }
   p.acc_out[at] = l.rows > 0 ? p.decay * p.acc[at] + v / static_cast<float>(p.H / p.G) : p.acc[at];
 }
@@ -1110,7 +1109,7 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
     return launch_chained(attend_stored_sums_kernel, dim3(static_cast<unsigned>(lists * ((p.C + kStoredSlots - 1) / kStoredSlots))),
                           dim3(256), 0, st, p);
   const long long pieces = (p.C + SumsSmem<D>::kSlots - 1) / SumsSmem<D>::kSlots;
-  e = launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(pieces * units)), threads, sizeof(SumsSmem<D>) + 128, st, p);
+  e = launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(pieces * units * p.row_parts)), threads, sizeof(SumsSmem<D>) + 128, st, p);
   if (e != cudaSuccess) return e;
   return launch_chained(attend_heads_kernel, dim3(static_cast<unsigned>(lists * ((p.C + 255) / 256))), dim3(256), 0, st, p);
 }
