@@ -34,7 +34,6 @@ cudaError_t launch_gemm(const GemmParams& p, cudaStream_t st);
 cudaError_t launch_layernorm(const LayerNormParams& p, cudaStream_t st);
 cudaError_t launch_row_gather(const RowGatherParams& p, cudaStream_t st);
 cudaError_t configure_expert();
-cudaError_t configure_cache();
 }  // namespace sc
 
 namespace {
@@ -233,7 +232,6 @@ int ensure_configured() {
     if (e == cudaSuccess) e = configure_tail();
     if (e == cudaSuccess) e = configure_encoder();
     if (e == cudaSuccess) e = configure_expert();
-    if (e == cudaSuccess) e = configure_cache();
     if (e != cudaSuccess) return fail_cuda("kernel attributes", e);
     done[dev] = true;
   }

@@ -3,6 +3,7 @@
 // the 16-bit types that its kernels take.
 #pragma once
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -162,10 +163,20 @@ struct EvictParams {
   long long free_pitch;
 };
 
-int api_device_sms();
-cudaError_t configure_attend();
-cudaError_t configure_rotate();
-cudaError_t configure_evict();
+// A kernel's most dynamic shared memory, set before its first launch on a device (and not at set-up: who does not use
+// the cache need not load its kernels).
+template <auto kKernel>
+cudaError_t allow_shared(size_t bytes) {
+  static std::atomic<bool> ready[256];
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < 256 && ready[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  const cudaError_t set = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (set == cudaSuccess && dev >= 0 && dev < 256) ready[dev].store(true, std::memory_order_release);
+  return set;
+}
+
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_rotate_back(const RotateParams& p, int dtype, cudaStream_t st);
 cudaError_t launch_attend(const AttendParams& p, int d, int dtype, cudaStream_t st);

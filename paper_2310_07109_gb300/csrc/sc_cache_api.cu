@@ -9,11 +9,6 @@
 namespace sc {
 int api_fail_cuda(const char* what, cudaError_t e);
 int api_ensure_configured();
-cudaError_t configure_cache() {
-  cudaError_t e = configure_attend();
-  if (e == cudaSuccess) e = configure_rotate();
-  return e == cudaSuccess ? configure_evict() : e;
-}
 }  // namespace sc
 
 namespace {

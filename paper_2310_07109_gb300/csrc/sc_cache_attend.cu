@@ -1066,30 +1066,24 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
 
 namespace {
 
-template <class T, int D>
-cudaError_t configure_of() {
-  auto set = [](auto kernel, size_t bytes) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-  };
-  cudaError_t e = set(attend_rows_kernel<T, D, 1>, sizeof(RowsSmem<D>) + 128);
-  if (e == cudaSuccess) e = set(attend_rows_kernel<T, D, 2>, sizeof(RowsSmem<D>) + 128);
-  if (e == cudaSuccess) e = set(attend_sums_kernel<T, D>, sizeof(SumsSmem<D>) + 128);
-  if (e == cudaSuccess) e = set(attend_few_kernel<T, D>, FewShape<D>::kBytes);
-  return e;
+// launch_chained with the kernel's dynamic shared memory allowed
+template <auto kKernel, typename... Args>
+cudaError_t launch_with(dim3 grid, int threads, size_t bytes, cudaStream_t st, const Args&... args) {
+  const cudaError_t e = allow_shared<kKernel>(bytes);
+  return e == cudaSuccess ? launch_chained(kKernel, grid, dim3(threads), bytes, st, args...) : e;
 }
 
 template <class T, int D>
 cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
   const long long units = static_cast<long long>(p.B) * p.Hk;
-  const dim3 threads(kAttendThreads);
   const int tiles_m = (p.M + kRowTile - 1) / kRowTile;
   const dim3 rows(static_cast<unsigned>(units * tiles_m * p.splits));
   const size_t rows_bytes = sizeof(RowsSmem<D>) + 128;
   if (p.M <= kJoinedRows) {   // scores kept, rows and weights in one launch
     constexpr int kWarps = FewShape<D>::kWarps;
     const bool few = p.M <= kFewRows;
-    cudaError_t e = few ? launch_chained(attend_few_kernel<T, D>, dim3(p.warps / kWarps), dim3(FewShape<D>::kThreads), FewShape<D>::kBytes, st, p)
-                        : launch_chained(attend_rows_kernel<T, D, 2>, rows, threads, rows_bytes, st, p);
+    cudaError_t e = few ? launch_with<attend_few_kernel<T, D>>(dim3(p.warps / kWarps), FewShape<D>::kThreads, FewShape<D>::kBytes, st, p)
+                        : launch_with<attend_rows_kernel<T, D, 2>>(rows, kAttendThreads, rows_bytes, st, p);
     if (e != cudaSuccess) return e;
     const long long all_rows = units * p.M;
     const int together = all_rows > 2 * kCacheSms;
@@ -1099,7 +1093,7 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
     return few ? launch_chained(attend_stored_join_kernel<T, D, kWarps>, grid, dim3(kSumThreads), 0, st, p, row_ctas, together)
                : launch_chained(attend_stored_join_kernel<T, D, 0>, grid, dim3(kSumThreads), 0, st, p, row_ctas, together);
   }
-  cudaError_t e = launch_chained(attend_rows_kernel<T, D, 1>, rows, threads, rows_bytes, st, p);
+  cudaError_t e = launch_with<attend_rows_kernel<T, D, 1>>(rows, kAttendThreads, rows_bytes, st, p);
   if (e != cudaSuccess) return e;
   e = launch_chained(attend_join_kernel<T, D>, dim3(static_cast<unsigned>((units * p.M + kJoinWarps - 1) / kJoinWarps)),
                      dim3(kJoinWarps * 32), 0, st, p);
@@ -1109,20 +1103,12 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
     return launch_chained(attend_stored_sums_kernel, dim3(static_cast<unsigned>(lists * ((p.C + kStoredSlots - 1) / kStoredSlots))),
                           dim3(256), 0, st, p);
   const long long pieces = (p.C + SumsSmem<D>::kSlots - 1) / SumsSmem<D>::kSlots;
-  e = launch_chained(attend_sums_kernel<T, D>, dim3(static_cast<unsigned>(pieces * units * p.row_parts)), threads, sizeof(SumsSmem<D>) + 128, st, p);
+  e = launch_with<attend_sums_kernel<T, D>>(dim3(static_cast<unsigned>(pieces * units * p.row_parts)), kAttendThreads, sizeof(SumsSmem<D>) + 128, st, p);
   if (e != cudaSuccess) return e;
   return launch_chained(attend_heads_kernel, dim3(static_cast<unsigned>(lists * ((p.C + 255) / 256))), dim3(256), 0, st, p);
 }
 
 }  // namespace
-
-cudaError_t configure_attend() {
-  cudaError_t e = configure_of<Bf16, 64>();
-  if (e == cudaSuccess) e = configure_of<Bf16, 128>();
-  if (e == cudaSuccess) e = configure_of<Fp16, 64>();
-  if (e == cudaSuccess) e = configure_of<Fp16, 128>();
-  return e;
-}
 
 cudaError_t launch_attend(const AttendParams& p, int d, int dtype, cudaStream_t st) {
   if (dtype == SC_FP16) return d == 64 ? launch_of<Fp16, 64>(p, st) : launch_of<Fp16, 128>(p, st);

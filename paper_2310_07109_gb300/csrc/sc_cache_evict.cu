@@ -400,6 +400,8 @@ size_t pick_bytes(int C) {
 
 template <int kCtas>
 cudaError_t launch_pick(const EvictParams& p, cudaStream_t st) {
+  const cudaError_t e = allow_shared<evict_pick_kernel<kCtas>>(pick_bytes<kCtas>(std::min(SC_MAX_CACHE, kMostSlots * kCtas)));
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.B * p.G * kCtas);
   cfg.blockDim = dim3(kPickThreads);
@@ -416,20 +418,7 @@ cudaError_t launch_pick(const EvictParams& p, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, evict_pick_kernel<kCtas>, p);
 }
 
-template <int kCtas>
-cudaError_t configure_pick() {
-  return cudaFuncSetAttribute(evict_pick_kernel<kCtas>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              static_cast<int>(pick_bytes<kCtas>(std::min(SC_MAX_CACHE, kMostSlots * kCtas))));
-}
-
 }  // namespace
-
-cudaError_t configure_evict() {
-  cudaError_t e = configure_pick<1>();
-  if (e == cudaSuccess) e = configure_pick<2>();
-  if (e == cudaSuccess) e = configure_pick<4>();
-  return e == cudaSuccess ? configure_pick<8>() : e;
-}
 
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
   // CTAs of a list: as many as its slots need, and more while there are SMs for them

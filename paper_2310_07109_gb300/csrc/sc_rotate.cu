@@ -564,16 +564,14 @@ struct Rotation {
   static size_t bytes(const RotateParams& p, const RotatePlan& plan, int vectors) {
     return ring_bytes(plan, vectors) + sizeof(float) * 2 * 2 * plan.wt * plan.nt * (p.rot / 2);
   }
-  static cudaError_t configure() {   // the most: the ring of eight warps, and angles of the most tokens
-    const int ring = kRotateWarps * 2 * kWarpTokens * 2 * 512, angles = 4 * 4 * kTileTokens * (SC_MAX_HEAD_WIDTH / 2);
-    static_assert(kWarpTokens * 2 == kWarpTokensBack * 4, "the same bytes backward");
-    const cudaError_t e = cudaFuncSetAttribute(rotate_kernel<T, W, kInter, kNorm>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring + angles);
-    if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(rotate_back_kernel<T, W, kInter, kNorm>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring + angles);
-  }
+  // the most: the ring of eight warps, and angles of the most tokens
+  static constexpr size_t kMost = kRotateWarps * 2 * kWarpTokens * 2 * 512 + 4 * 4 * kTileTokens * (SC_MAX_HEAD_WIDTH / 2);
+  static_assert(kWarpTokens * 2 == kWarpTokensBack * 4, "the same bytes backward");
   static cudaError_t forward(const RotateParams& p, cudaStream_t st) {
     const int groups = groups_of(p.Hq + p.Hk * (p.cache_k != nullptr ? 2 : 1));
     const RotatePlan plan = plan_of(p, groups, kWarpTokens);
+    const cudaError_t e = allow_shared<rotate_kernel<T, W, kInter, kNorm>>(kMost);
+    if (e != cudaSuccess) return e;
     return launch_chained(rotate_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, (groups + plan.wg - 1) / plan.wg),
                           dim3(plan.wg * plan.wt * 32), bytes(p, plan, 2), st, p, plan);
   }
@@ -581,7 +579,9 @@ struct Rotation {
     const int groups = groups_of(p.Hq + p.Hk);
     const RotatePlan plan = plan_of(p, groups, kWarpTokensBack);
     const int columns = (groups + plan.wg - 1) / plan.wg;
-    cudaError_t e = launch_chained(rotate_back_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, columns),
+    cudaError_t e = allow_shared<rotate_back_kernel<T, W, kInter, kNorm>>(kMost);
+    if (e != cudaSuccess) return e;
+    e = launch_chained(rotate_back_kernel<T, W, kInter, kNorm>, dim3(plan.ctas, columns),
                                    dim3(plan.wg * plan.wt * 32), bytes(p, plan, 4), st, p, plan);
     if (e != cudaSuccess || !kNorm) return e;
     return launch_chained(rotate_gamma_kernel, dim3(p.d / 4), dim3(kRotateThreads), 0, st, p, plan.ctas * columns);
@@ -609,21 +609,6 @@ cudaError_t of_type(int dtype, const RotateParams& p, const What& what) {
 }
 
 }  // namespace
-
-cudaError_t configure_rotate() {
-  static const float some = 1.f;
-  for (int dtype : {SC_BF16, SC_FP16})
-    for (int d : {64, 128, 256})
-      for (int kind = 0; kind < 4; ++kind) {
-        RotateParams p{};
-        p.d = d;
-        p.interleaved = kind & 1;
-        p.gamma_q = kind & 2 ? &some : nullptr;
-        const cudaError_t e = of_type(dtype, p, [](auto r) { return r.configure(); });
-        if (e != cudaSuccess) return e;
-      }
-  return cudaSuccess;
-}
 
 cudaError_t launch_rotate(const RotateParams& p, int dtype, cudaStream_t st) {
   return of_type(dtype, p, [&](auto r) { return r.forward(p, st); });

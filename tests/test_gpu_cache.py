@@ -450,6 +450,42 @@ def test_steps(G, Hk, H, d, graph):
     assert int(cache["len"].max()) <= budget + 7 + T
 
 
+def test_lengths_out_of_range():
+    """len and rows are held within the cache and the call on the device."""
+    g = gen(44)
+    cache = make_cache(g, 3, 2, 40, 64, 1, [40, 0, 20])
+    cache["len"][0, 0], cache["len"][1, 0] = 1000, -5
+    for T, rows in ((1, [5, 1, -3]), (3, [3, 2, 100]), (25, [25, 26, 1])):
+        check_attend(cache, randn(g, 3 * T, 4 * 64).to(BF), T, rows)
+    check_evict(copy(cache), budget=30)
+    held = copy(cache)
+    K, V = randn(g, 6, 128).to(BF), randn(g, 6, 128).to(BF)
+    ws = sc.new_cache_workspace(3, 40, 2, 2)
+    sc.cache_append(cache, None, K, V, L=2, rows=i32(1, 7, -1), workspace=ws)
+    assert cache["len"].tolist() == [[40], [2], [20]] and (cache["seen"] - held["seen"]).tolist() == [1, 2, 0]
+    assert sc.workspace_status(ws) == sc.SC_ERR_CAPACITY
+    held["K"][1, :, :2] = K[2:4].reshape(2, 2, 64).transpose(0, 1)
+    assert same(cache["K"], held["K"])
+
+
+def test_one_workspace_for_caches_of_different_sizes():
+    """Calls of one stream share a workspace, whatever the sizes of each."""
+    g = gen(45)
+    caches = [make_cache(g, 2, 4, 700, 64, 4, [650, 700], new=1), make_cache(g, 1, 2, 3000, 128, 1, [2999], HF, new=1)]
+    size = max(sc.cache_workspace_size(2, 702, 8, 4, lists=4, T=70), sc.cache_workspace_size(1, 3001, 16, 2, width=128, T=70))
+    raw = torch.zeros(size + 256, dtype=torch.uint8, device="cuda")
+    ws = raw[-raw.data_ptr() % 256:][:size]
+    for i in range(3):
+        for c, H in zip(caches, (8, 16)):
+            B, Hk, C, d = c["K"].shape
+            for T in (1, 40, 70):
+                check_attend(c, randn(g, B * T, H * d).to(c["K"].dtype), T, ws=ws, decay=0.5, in_place=True)
+            out = sc.cache_evict(c, budget=C - 100 - i, workspace=ws)
+            sc.cache_append(c, None, randn(g, B * 2, Hk * d).to(c["K"].dtype), randn(g, B * 2, Hk * d).to(c["K"].dtype), L=2, workspace=ws)
+            assert int(out["len"].min()) >= 2 and int(c["len"].max()) == C - 98 - i
+    assert sc.workspace_status(ws) == sc.SC_OK
+
+
 def test_matches_the_whole_sequence_layer():
     """One head, everything seen by the last token: its weights are the rows that the framework's layer
     accumulates, when that token is global and the window covers nothing else."""

@@ -228,6 +228,21 @@ def test_backward_undoes_the_rotation():
     assert torch.equal(back, sc.rotate_forward(y, pos=(-pos).contiguous(), **kw)["Q"])
 
 
+def test_tokens_far_apart_in_memory():
+    """More than 2^31 elements between the first token and the last."""
+    T, ld = 2500, 1 << 20
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 20 GB")
+    x = torch.empty(T * ld, dtype=BF, device="cuda").as_strided((T, 128), (ld, 1))
+    x.copy_(randn(gen(8), T, 128))
+    kw = dict(width=64, B=1, L=T, freq=frequencies(64), gamma_q=torch.ones(64, device="cuda"))
+    want, dy = sc.rotate_forward(x.contiguous(), **kw)["Q"], randn(gen(9), T, 128).to(BF)
+    back = sc.rotate_backward(dy, None, x.contiguous(), **kw)
+    got = sc.rotate_backward(dy, None, x, **kw)
+    assert all(torch.equal(back[n], got[n]) for n in back)
+    assert torch.equal(sc.rotate_forward(x, out={"Q": x}, **kw)["Q"], want)
+
+
 def test_two_calls_give_the_same_bits():
     case = (4, 700, 12, 4, 64, 64, False, "qk", [700, 3, 0, 512], BF)
     Q, K, kw, used = make(case)
