@@ -2,13 +2,21 @@
 // with the weights added up for each slot.
 //
 //   t = scale log2(e) q . k;   P = 2^(t - LSE);   O = P V;   acc = decay acc + sum over rows, mean over heads of P
-// Three launches:
-//   rows    one pass over K and V with the running reference (the largest t so far) and sum of a row's weights;
-//           a CTA has up to 64 rows of a key head (tokens x query heads) and a part of the list's
-//           slots, four warps of 16 rows each; S = Q K^T and P V by warp products, P in registers
-//   join    the parts of a list: LSE = reference + log2(sum) of all, O scaled and rounded
-//   sums    each slot's weights from K and the rows' LSE: 2^(t - LSE) summed down the key's column over
-//           rows and heads in a fixed order
+// A key head of a sequence (a unit) has M = T R rows, R query heads to a key head.  Bound by the bytes of K and V (each read
+// once at M <= 32) as long as there are few rows.  Products are warp-level ones (16 rows at least, which a token of
+// grouped heads does not fill; they take 17 % of the tensor pipe), with S, P and O in registers; softmax with the
+// running reference (the largest t so far) and sum of each row; P rounded to the 16-bit type where it meets V.
+//   M <= 16   attend_few_kernel: the 16-slot tiles of all units dealt out to warps in equal runs, each warp with a
+//             pipeline of its own.  32 streams of 3000 to 8000 slots, 16 heads over 4 of 128: 63 to 67 us for
+//             390 MB (6 TB/s), the call 76; 252 as many rows below
+//   M <= 32   attend_rows_kernel<.., 2>: a CTA a part of a unit, two pairs of warps on either half of each 64-slot
+//             tile.  Four sequences of 12 heads of 64, 32 tokens, 4096 slots: the call 29 us, 50 as many rows below
+//     both keep the scores t, 4 bytes a row and slot, and attend_stored_join_kernel joins the parts of the units
+//     (LSE = reference + log2(sum) of all, O scaled and rounded) and adds 2^(t - LSE) up over the list's rows and heads
+//     in a fixed order (the 32 tokens: 37 us where K is read again for the sums)
+//   M > 32    attend_rows_kernel<.., 1>, attend_join_kernel, and the sums from scores kept (attend_stored_sums_kernel,
+//             up to kStoredBytes) or computed again (attend_sums_kernel, attend_heads_kernel).  A prompt of 4096
+//             tokens, 16 heads over 4 of 128: 836 us (164 TFLOP/s of 4 T n d H)
 #include <algorithm>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -24,8 +32,8 @@ constexpr int kRowTile = 16 * kAttendWarps;
 constexpr int kKeyTile = 64;
 constexpr int kJoinWarps = 8;
 
-// A tile of `kKeyTile` (or kRowTile) rows of D values: 16-byte chunk c of row r lies at chunk c ^ (r & 7), so that the eight rows of
-// a fragment are in eight different banks.
+// Tiles are rows of D values: 16-byte chunk c of row r lies at chunk c ^ (r & 7), so that the eight rows of a fragment are
+// in eight different banks.
 template <int D>
 __device__ __forceinline__ uint32_t chunk_at(uint32_t base, int row, int chunk) {
   return base + static_cast<uint32_t>(row * (D * 2) + ((chunk ^ (row & 7)) << 4));
@@ -94,7 +102,7 @@ __device__ __forceinline__ void load_keys(const AttendParams& p, const uint16_t*
   }
 }
 
-// Tiles on their way: as many as let an SM have kRowsCtas CTAs.
+// Tiles on their way: as many as leave an SM room for three CTAs (two of wide heads).
 template <int D>
 struct RowsSmem {
   static constexpr int kStages = D == 64 ? 4 : 3;
@@ -328,7 +336,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) attend_join_kernel(const Atte
   const long long row = static_cast<long long>(blockIdx.x) * kJoinWarps + (threadIdx.x >> 5);
   if (row >= static_cast<long long>(p.B) * p.Hk * p.M) return;
   const long long unit = row / p.M;
-  const int m = static_cast<int>(row - unit * p.M), b = static_cast<int>(unit / p.Hk), hk = static_cast<int>(unit - static_cast<long long>(b) * p.Hk);
+  const int m = static_cast<int>(row - unit * p.M), b = static_cast<int>(unit / p.Hk);
+  const int hk = static_cast<int>(unit - static_cast<long long>(b) * p.Hk);
   const ListOf l = list_of(p, b, hk / (p.Hk / p.G));
   if (m >= l.rows * p.R) {
     if (lane == 0) p.lse[row] = INFINITY;
@@ -462,10 +471,12 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
             v[1] = ex2(c[i][1] * p.scale2 - lse[0]) + ex2(c[i][3] * p.scale2 - lse[1]);
           } else {   // (a NaN of an unseen slot is kept out by the choice, not by a product)
             const int2 where = *reinterpret_cast<const int2*>(&sm.pos[key]);
-            v[0] = (where.x <= at[0] ? ex2(c[i][0] * p.scale2 - lse[0]) : 0.f) + (where.x <= at[1] ? ex2(c[i][2] * p.scale2 - lse[1]) : 0.f);
-            v[1] = (where.y <= at[0] ? ex2(c[i][1] * p.scale2 - lse[0]) : 0.f) + (where.y <= at[1] ? ex2(c[i][3] * p.scale2 - lse[1]) : 0.f);
+            v[0] = (where.x <= at[0] ? ex2(c[i][0] * p.scale2 - lse[0]) : 0.f) +
+                   (where.x <= at[1] ? ex2(c[i][2] * p.scale2 - lse[1]) : 0.f);
+            v[1] = (where.y <= at[0] ? ex2(c[i][1] * p.scale2 - lse[0]) : 0.f) +
+                   (where.y <= at[1] ? ex2(c[i][3] * p.scale2 - lse[1]) : 0.f);
           }
-          // over the eight pairs of rows; each of them keeps two of the sums' sixteen columns
+          // over the warp's other rows: lanes four apart
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             v[k] += __shfl_xor_sync(0xffffffffu, v[k], 4);
@@ -730,7 +741,8 @@ __global__ void __launch_bounds__(FewShape<D>::kThreads, 1) attend_few_kernel(co
     const unsigned blank = __ballot_sync(0xffffffffu, unseen);
     if (blank != 0) {
       for (int r = 0; r < kFewTile; ++r)
-        if (blank >> r & 1u && lane < D / 8) *reinterpret_cast<uint4*>(stage + S::kTileBytes + r * D * 2 + lane * 16) = make_uint4(0, 0, 0, 0);
+        if (blank >> r & 1u && lane < D / 8)
+          *reinterpret_cast<uint4*>(stage + S::kTileBytes + r * D * 2 + lane * 16) = make_uint4(0, 0, 0, 0);
       __syncwarp();
     }
     float c[2][4] = {};
@@ -1103,7 +1115,8 @@ cudaError_t launch_of(const AttendParams& p, cudaStream_t st) {
     return launch_chained(attend_stored_sums_kernel, dim3(static_cast<unsigned>(lists * ((p.C + kStoredSlots - 1) / kStoredSlots))),
                           dim3(256), 0, st, p);
   const long long pieces = (p.C + SumsSmem<D>::kSlots - 1) / SumsSmem<D>::kSlots;
-  e = launch_with<attend_sums_kernel<T, D>>(dim3(static_cast<unsigned>(pieces * units * p.row_parts)), kAttendThreads, sizeof(SumsSmem<D>) + 128, st, p);
+  e = launch_with<attend_sums_kernel<T, D>>(dim3(static_cast<unsigned>(pieces * units * p.row_parts)), kAttendThreads,
+                                            sizeof(SumsSmem<D>) + 128, st, p);
   if (e != cudaSuccess) return e;
   return launch_chained(attend_heads_kernel, dim3(static_cast<unsigned>(lists * ((p.C + 255) / 256))), dim3(256), 0, st, p);
 }

@@ -7,13 +7,14 @@
 // nearly every row behind the first one (half of 8192 slots: 2048 rows instead of 4096).
 //
 // Two launches:
-//   pick   a CTA a list, or a cluster of up to eight with a stretch of a long list each.  Its slots' 32-bit keys (acc's bits in an order-preserving form) go into shared memory; the
-//          cut is found in passes over them, each of which cuts the range that holds it into at most 256 equal parts
-//          (by bits of the difference to its lower end: keys are logarithms nearly, so weights spread over the parts;
-//          digits of the keys themselves put most of them into two or three, whose additions wait for one another:
-//          13000 cycles a pass instead of 1000).  Then a bit a slot, and ranks of ties, free places and their fillers
-//          from prefix sums over the bits.  8000 slots: 22 us before, 5 now
-//   move   the rows of K and V, bound by memory, and acc and pos
+//   pick   a CTA a list, or a cluster of up to eight with a stretch of a long list each.  Its slots' 32-bit keys (acc's
+//          bits in an order-preserving form) go into shared memory; the cut is found in passes over them, each of
+//          which cuts the range that holds it into at most 256 equal parts (by bits of the difference to its lower end:
+//          keys are logarithms nearly, so weights spread over the parts; digits of the keys themselves put most of
+//          them into two or three, whose additions wait for one another: 13000 cycles a pass instead of 2300).
+//          Then a bit a slot, and ranks of ties, free places and their fillers from prefix sums over the bits, put
+//          together in shared memory (stores of single words to the plan took 4600 cycles of a list of 8000 slots)
+//   move   the rows of K and V, bound by memory (32 x 4 lists of 8000 slots, 128 features: 40 us, 6.7 TB/s), and acc and pos
 #include <algorithm>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -42,7 +43,7 @@ __device__ __forceinline__ uint32_t rank_key(const EvictParams& p, float acc, in
 }
 
 struct PickSmem {
-  uint32_t hist[2][kParts];   // of every other pass: the cluster's CTAs read one while the next is cleared
+  alignas(16) uint32_t hist[2][kParts];   // of every other pass: the cluster's CTAs read one while the next is cleared
   uint32_t low[kPickWarps], high[kPickWarps];
   int count[kPickWarps][2];
   uint32_t range[4];   // of the CTA: lowest and highest key, protected ones, those that rank last
@@ -75,11 +76,23 @@ __device__ __forceinline__ uint32_t scan_cta(PickSmem& sm, uint32_t v, uint32_t&
   return __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u) + upto - v;
 }
 
+// Shared memory of a CTA in words: keys of its share of a list, two bits a slot up to a multiple of 16 bytes, and
+// the cluster's counts.
+template <int kCtas>
+__host__ __device__ constexpr int pick_room(int C) {
+  return ((C + kCtas - 1) / kCtas + 31) & ~31;
+}
+__host__ __device__ constexpr int pick_bits_end(int room) { return (room + room / 16 + 3) & ~3; }
+template <int kCtas>
+constexpr size_t pick_bytes(int C) {
+  return sizeof(uint32_t) * (pick_bits_end(pick_room<kCtas>(C)) + (kCtas > 1 ? kParts : 0));
+}
+
 template <int kCtas>
 __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const EvictParams p) {
   static_assert(kPickWarps == 32, "a lane a warp");
   __shared__ PickSmem sm;
-  extern __shared__ uint32_t held[];   // keys, then two bits a slot
+  extern __shared__ __align__(16) uint32_t held[];   // keys, then two bits a slot, then the cluster's counts
   pdl_wait();
   pdl_launch_dependents();
   const int list = blockIdx.x / kCtas, rank = blockIdx.x % kCtas, b = list / p.G, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -104,9 +117,10 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
   const int stretch = (((n + kCtas - 1) / kCtas) + 31) & ~31, first = min(rank * stretch, n), own = min(stretch, n - first);
   const float* acc = p.acc + base + first;
   const int32_t* pos = p.pos + base + first;
-  const int room = ((p.C + kCtas - 1) / kCtas + 31) & ~31;
+  const int room = pick_room<kCtas>(p.C);
   uint32_t* above = held + room;
   uint32_t* tied = above + room / 32;
+  uint32_t* cluster_hist = held + pick_bits_end(room);
   if (tid < kParts) sm.hist[0][tid] = 0;
   // protected ones and those that rank last apart, the range of the others' keys
   uint32_t low = 0xffffffffu, high = 0;
@@ -194,16 +208,18 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
         uint32_t all = 0;
 #pragma unroll
         for (int r = 0; r < kCtas; ++r) all += of_rank(&hist[tid], r);
-        held[room + room / 16 + tid] = all;   // (behind the bits)
+        cluster_hist[tid] = all;
       }
       sm.hist[pass ^ 1][tid] = 0;
     }
-    const uint32_t* counts = kCtas > 1 ? held + room + room / 16 : hist;
+    const uint32_t* counts = kCtas > 1 ? cluster_hist : hist;
     if (kCtas > 1) __syncthreads();
     if (warp == 0) {   // lane l has parts 255 - 8 l .. 248 - 8 l, the largest first
       int mine[8], total = 0;
+      const uint4 hi = reinterpret_cast<const uint4*>(counts)[63 - 2 * lane], lo = reinterpret_cast<const uint4*>(counts)[62 - 2 * lane];
+      const uint32_t eight[8] = {hi.w, hi.z, hi.y, hi.x, lo.w, lo.z, lo.y, lo.x};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) total += mine[i] = static_cast<int>(counts[255 - 8 * lane - i]);
+      for (int i = 0; i < 8; ++i) total += mine[i] = static_cast<int>(eight[i]);
       int upto = total;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -291,20 +307,29 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
     fill_at = __reduce_add_sync(0xffffffffu, lane < rank ? c >> 16 : 0);
     all_free = __reduce_add_sync(0xffffffffu, lane < kCtas ? c & 0xffffu : 0);
   }
+  // (the keys are done with: places from their start on, fillers from their end back)
+  int my_free = 0, my_fill = 0;
   for (int i0 = 0; i0 < bytes; i0 += kPickThreads) {
     const int i = i0 + tid, j = first + 8 * i;
     uint32_t places, fills, low_ones, all;
     of_byte(i, places, fills, low_ones);
     const uint32_t before = scan_cta(sm, __popc(places) | __popc(fills) << 16, all);
     if (low_ones != 0 && i < bytes) free8[i] = static_cast<uint8_t>(places);
-    for (int at = free_at + static_cast<int>(before & 0xffffu); places != 0; places &= places - 1) pairs[at++].x = j + __ffs(places) - 1;
-    for (int at = fill_at + static_cast<int>(before >> 16); fills != 0; fills &= fills - 1) pairs[at++].y = j + __ffs(fills) - 1;
-    free_at += static_cast<int>(all & 0xffffu);
-    fill_at += static_cast<int>(all >> 16);
+    for (int at = my_free + static_cast<int>(before & 0xffffu); places != 0; places &= places - 1) held[at++] = j + __ffs(places) - 1;
+    for (int at = room - 1 - my_fill - static_cast<int>(before >> 16); fills != 0; fills &= fills - 1) held[at--] = j + __ffs(fills) - 1;
+    my_free += static_cast<int>(all & 0xffffu);
+    my_fill += static_cast<int>(all >> 16);
+  }
+  __syncthreads();
+  if (kCtas == 1) {
+    for (int i = tid; i < my_free; i += kPickThreads) pairs[i] = make_int2(held[i], held[room - 1 - i]);
+  } else {
+    for (int i = tid; i < my_free; i += kPickThreads) pairs[free_at + i].x = held[i];
+    for (int i = tid; i < my_fill; i += kPickThreads) pairs[fill_at + i].y = held[room - 1 - i];
   }
   if (kCtas > 1) cluster_sync();   // (all have read all; len too)
   if (tid == 0 && rank == 0) {
-    p.moved[list] = kCtas > 1 ? all_free : free_at;
+    p.moved[list] = kCtas > 1 ? all_free : my_free;
     p.len_out[list] = k;
   }
 }
@@ -390,13 +415,6 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictPar
 }
 
 namespace {
-
-// Keys of a CTA's share of a list, two bits a slot, and the cluster's counts.
-template <int kCtas>
-size_t pick_bytes(int C) {
-  const int room = ((C + kCtas - 1) / kCtas + 31) & ~31;
-  return sizeof(uint32_t) * (room + room / 16 + (kCtas > 1 ? kParts : 0));
-}
 
 template <int kCtas>
 cudaError_t launch_pick(const EvictParams& p, cudaStream_t st) {
