@@ -916,10 +916,10 @@ __device__ __forceinline__ auto parts_of(const AttendParams& p, int unit, int n,
 // slots of a list each, whose weights they add up over the list's rows from the scores and the rows' LSE.
 constexpr int kSumThreads = 128, kSumWarps = kSumThreads / 32;
 constexpr int kSumSlots = kSumThreads * 4;
-constexpr int kSumAhead = 4;
-constexpr int kSumRows = kSumThreads / 8;   // rows whose LSE are found at once, by eight lanes each
+constexpr int kSumAhead = 8;
+constexpr int kSumRows = kSumThreads / 4;   // most rows whose LSE are found at once, by four lanes each or more
 template <class T, int D, int kWarps>
-__global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(const AttendParams p, int row_ctas, int together) {
+__global__ void __launch_bounds__(kSumThreads, 6) attend_stored_join_kernel(const AttendParams p, int row_ctas, int together) {
   constexpr int kOwn = D / 32;
   __shared__ float part[kSumWarps][D];
   __shared__ float2 ends[kSumWarps];
@@ -1011,8 +1011,9 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (j + i < l.n) old[i] = p.acc[at + i];
+  const int lanes = rows <= kSumThreads / 16 ? 16 : rows <= kSumThreads / 8 ? 8 : 4;   // of a row's LSE
   for (int r0 = 0; r0 < rows; r0 += kSumRows) {
-    const int here = min(kSumRows, rows - r0), i = threadIdx.x / 8;
+    const int here = min(kSumRows, rows - r0), i = threadIdx.x / lanes;
     const int h = r0 / rows_m, m0 = r0 - h * rows_m;
     // the first rows' scores are asked for before the LSE are known
     const float* row = p.scores + (static_cast<long long>(unit0 + h) * p.M + m0) * p.pitch + j;
@@ -1029,15 +1030,15 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
     for (int k = 0; k < kSumAhead; ++k)
       if (k < here && j < l.n) ahead[k] = next();
     __syncthreads();
-    // (whole warps: four rows each)
+    // (whole warps: several rows each)
     const int mine = m0 + min(i, here - 1), hi = mine / rows_m, unit = unit0 + h + hi;
     const auto ps = parts_of<kWarps>(p, unit, l.n, share);
     float ref = -INFINITY, total = 0.f;
-    for (int s0 = lane & 7; s0 < ps.count; s0 += 32) {
+    for (int s0 = lane & (lanes - 1); s0 < ps.count; s0 += 4 * lanes) {
       float2 ml[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        ml[u] = s0 + 8 * u < ps.count ? p.ml[ps.at(s0 + 8 * u) * p.M + mine - hi * rows_m] : make_float2(-INFINITY, 0.f);
+        ml[u] = s0 + lanes * u < ps.count ? p.ml[ps.at(s0 + lanes * u) * p.M + mine - hi * rows_m] : make_float2(-INFINITY, 0.f);
       const float top = fmaxf(fmaxf(fmaxf(ref, ml[0].x), fmaxf(ml[1].x, ml[2].x)), ml[3].x);
       total *= ref == top ? 1.f : ex2(ref - top);
 #pragma unroll
@@ -1046,12 +1047,10 @@ __global__ void __launch_bounds__(kSumThreads, 8) attend_stored_join_kernel(cons
       ref = top;
     }
     float top = ref;
-#pragma unroll
-    for (int k = 4; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+    for (int k = lanes / 2; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
     if (ref != top && (ref != -INFINITY || total != 0.f)) total *= ex2(ref - top);
-#pragma unroll
-    for (int k = 4; k > 0; k >>= 1) total += __shfl_xor_sync(0xffffffffu, total, k);
-    if ((lane & 7) == 0 && i < here) lse[i] = top == -INFINITY && total == 0.f ? INFINITY : top + log2f(total);
+    for (int k = lanes / 2; k > 0; k >>= 1) total += __shfl_xor_sync(0xffffffffu, total, k);
+    if ((lane & (lanes - 1)) == 0 && i < here) lse[i] = top == -INFINITY && total == 0.f ? INFINITY : top + log2f(total);
     __syncthreads();
     if (j >= l.n) continue;
 #pragma unroll
