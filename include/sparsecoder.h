@@ -704,7 +704,8 @@ int sc_expert_combine_backward(const sc_expert_combine_backward_args* args, void
  * gamma_q, gamma_k  fp32 [d], each may be NULL.
  * freq      double [rot / 2], radians a position; finite.  Scaled forms for long contexts are
  *           other frequencies and mscale.  Not used when rot is 0.
- * Q_out, K_out  as Q and K; may be Q and K themselves (with their distances).
+ * Q_out, K_out  as Q and K; may be Q and K themselves (with their distances), else they do not
+ *           overlap an input.
  * d: a multiple of 16 up to SC_MAX_HEAD_WIDTH; rot: a multiple of 16, 0 to d; distances
  * multiples of 8 below 2^30; 16-bit pointers 16-byte aligned, freq 8-byte aligned;
  * B L <= 2^31 - 4096; Hq + Hk <= SC_MAX_HEADS.  Rows not in use are neither read nor written.
@@ -853,7 +854,7 @@ int sc_cache_append(const sc_cache_append_args* args, void* workspace, size_t wo
  *   P_h[r] = softmax of scale q . k over the slots it sees;  O_h[r] = sum_c P_h[r][c] v_c
  *   acc_out[c] = decay acc[c] + sum_r mean_h P_h[r][c]     (c < len; h over the list's H / G heads)
  * A row that sees no slot has O = 0 and adds nothing.  Sequences without rows in use keep their acc.
- * Q, O      dtype: row b T + r has its H heads at ldq, ldo times its number.
+ * Q, O      dtype: row b T + r has its H heads at ldq, ldo times its number; O does not overlap Q.
  * acc_out   fp32 [B][G][C], may be acc.
  * scale     finite; T at most SC_MAX_STEP.  Scores, weights and sums in fp32; the weights are
  *           rounded to dtype for their product with V.  Two calls with the same

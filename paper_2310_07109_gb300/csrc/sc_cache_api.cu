@@ -236,7 +236,7 @@ extern "C" int sc_cache_attend(const sc_cache_attend_args* a, void* workspace, s
   if (rc == SC_OK) rc = check_attend_sizes(a->B, a->H, a->Hk, a->d, a->T);
   if (rc != SC_OK) return rc;
   if (!good_heads(a->Q, a->ldq, a->H, a->d) || !good_heads(a->O, a->ldo, a->H, a->d) || !a->acc_out ||
-      !words(a->acc_out, a->rows) || !std::isfinite(a->scale) || !std::isfinite(a->decay))
+      a->O == a->Q || !words(a->acc_out, a->rows) || !std::isfinite(a->scale) || !std::isfinite(a->decay))
     return SC_ERR_INVALID_ARG;
   const CacheLayout w = cache_layout(a->B, a->C, a->H, a->Hk, a->G, a->d, a->T);
   if ((rc = check_workspace(workspace, ws_bytes, w.total)) != SC_OK || (rc = api_ensure_configured()) != SC_OK) return rc;

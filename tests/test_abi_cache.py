@@ -28,7 +28,7 @@ OK = dict(
             dict(**CACHE, H=8, L=3, Q=P, ldq=512, K_in=P, ldk=256, V_in=P, ldv=256, rows=None, **TURN, Q_out=P, ldq_out=512,
                  len_out=P, seen_out=P)),
     attend=(ca.CacheAttendArgs, "sc_cache_attend", True,
-            dict(**CACHE, H=8, T=3, Q=P, ldq=512, rows=None, scale=0.125, decay=1.0, O=P, ldo=512, acc_out=P)),
+            dict(**CACHE, H=8, T=3, Q=P, ldq=512, rows=None, scale=0.125, decay=1.0, O=P + 4096, ldo=512, acc_out=P)),
     evict=(ca.CacheEvictArgs, "sc_cache_evict", True,
            dict(**CACHE, budget=100, slack=0, sinks=4, recent=50, acc_out=P, pos_out=P, len_out=P)),
 )
@@ -56,7 +56,7 @@ BAD = {
         (dict(V_in=P + 8), INVALID), (dict(ldv=248), INVALID), (dict(len_out=None), INVALID), (dict(seen_out=None), INVALID)],
     "attend": BAD_CACHE + [
         (dict(H=0), INVALID), (dict(H=6), INVALID), (dict(T=0), INVALID), (dict(T=4097), UNSUPPORTED), (dict(d=80, stride_c=80), UNSUPPORTED),
-        (dict(d=32), UNSUPPORTED), (dict(Q=None), INVALID), (dict(ldq=504), INVALID), (dict(O=None), INVALID), (dict(O=P + 8), INVALID),
+        (dict(d=32), UNSUPPORTED), (dict(Q=None), INVALID), (dict(ldq=504), INVALID), (dict(O=None), INVALID), (dict(O=P + 8), INVALID), (dict(O=P), INVALID),
         (dict(ldo=516), INVALID), (dict(acc_out=None), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
         (dict(decay=math.nan), INVALID)],
     "evict": BAD_CACHE + [
