@@ -178,8 +178,9 @@ extern "C" int sc_rotate_backward(const sc_rotate_backward_args* a, void* worksp
   p.per_row = (1ull << 63) / static_cast<unsigned>(a->L) + 1;
   p.dq = {static_cast<const uint16_t*>(a->dQ_out), a->ldq_out};
   p.dk = {static_cast<const uint16_t*>(a->dK_out), a->ldk_out};
-  p.q = {static_cast<const uint16_t*>(a->Q), a->ldq};
-  p.k = {static_cast<const uint16_t*>(a->K), a->ldk};
+  // without a norm Q and K are not read, and nothing was checked of them: no address is made from them
+  p.q = a->gamma_q ? HeadsIn{static_cast<const uint16_t*>(a->Q), a->ldq} : p.dq;
+  p.k = a->gamma_k ? HeadsIn{static_cast<const uint16_t*>(a->K), a->ldk} : p.dk;
   p.q_out = {static_cast<uint16_t*>(a->dQ), a->ldq_grad};
   p.k_out = {static_cast<uint16_t*>(a->dK), a->ldk_grad};
   p.rows = a->rows; p.pos = a->pos; p.gamma_q = a->gamma_q; p.gamma_k = a->gamma_k; p.eps = a->eps;

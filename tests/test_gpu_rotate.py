@@ -289,3 +289,29 @@ def test_on_another_stream():
     side.synchronize()
     for a, b in itertools.chain(((got[n], want[n]) for n in want), ((got_back[n], back[n]) for n in back)):
         assert torch.equal(a, b)
+
+
+def test_backward_without_a_norm_makes_nothing_of_q_and_k():
+    """Q and K are not used without a norm: no address and distance given for them matters, odd ones included."""
+    import ctypes
+
+    from paper_2310_07109_gb300 import binding, cache
+
+    B, L, Hq, Hk, d = 2, 21, 5, 2, 96
+    g = gen(5)
+    dQ, dK = randn(g, B * L, Hq * d).to(BF), randn(g, B * L, Hk * d).to(BF)
+    freq, gamma = frequencies(32), 1 + 0.3 * randn(g, d)
+    X = randn(g, B * L, Hq * d).to(BF)
+    ws = sc.new_rotate_workspace(d)
+    for norm in (False, True):   # of the queries; the keys have none
+        want = sc.rotate_backward(dQ, dK, X if norm else None, width=d, B=B, L=L, freq=freq, gamma_q=gamma if norm else None, workspace=ws)
+        got = {n: torch.full_like(t, float("nan")) for n, t in want.items()}
+        a = cache.RotateBackwardArgs(
+            B=B, L=L, Hq=Hq, Hk=Hk, d=d, dtype=0, dQ_out=dQ.data_ptr(), ldq_out=Hq * d, dK_out=dK.data_ptr(), ldk_out=Hk * d,
+            Q=X.data_ptr() if norm else 3, ldq=Hq * d if norm else 5, K=3, ldk=7, gamma_q=gamma.data_ptr() if norm else None,
+            eps=EPS, rot=32, freq=freq.data_ptr(), mscale=1.0, dQ=got["dQ"].data_ptr(), ldq_grad=Hq * d, dK=got["dK"].data_ptr(),
+            ldk_grad=Hk * d, dgamma_q=got["dgamma_q"].data_ptr() if norm else None)
+        rc = binding.load().sc_rotate_backward(ctypes.byref(a), ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        for n in want:
+            assert torch.equal(got[n], want[n]), n
