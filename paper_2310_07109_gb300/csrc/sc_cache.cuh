@@ -17,6 +17,10 @@ namespace sc {
 
 constexpr int kCacheSms = 152;   // what splits and workspaces are sized for
 
+// Every kernel of the cache is launched while the one before it still runs, and waits for it.  What that one may write
+// (len, seen, pos, rows, queries) is therefore read by ordinary loads: the read-only path wants data that
+// nobody writes while the kernel lives, from before its wait on.
+
 // The two 16-bit types: eight values <-> fp32, and the warp product of their fragments.
 struct Bf16 {
   static __device__ __forceinline__ void unpack(uint32_t w, float& lo, float& hi) {

@@ -64,9 +64,9 @@ struct ListOf {
 };
 __device__ __forceinline__ ListOf list_of(const AttendParams& p, int b, int g) {
   ListOf l;
-  l.n = min(max(__ldg(p.len + b * p.G + g), 0), p.C);
-  l.rows = p.rows != nullptr ? min(max(__ldg(p.rows + b), 0), p.T) : p.T;
-  l.first = __ldg(p.seen + b) - l.rows;
+  l.n = min(max(p.len[b * p.G + g], 0), p.C);
+  l.rows = p.rows != nullptr ? min(max(p.rows[b], 0), p.T) : p.T;
+  l.first = p.seen[b] - l.rows;
   return l;
 }
 
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kAttendThreads) attend_sums_kernel(const Atten
   for (int t = warp; t < S::kTiles; t += kAttendWarps) {
     int least = 0x7fffffff, most = 0;
     for (int j = t * kKeyTile + lane; j < (t + 1) * kKeyTile; j += 32) {
-      const int where = j0 + j < l.n ? __ldg(p.pos + at0 + j) : -1;
+      const int where = j0 + j < l.n ? p.pos[at0 + j] : -1;
       sm.pos[j] = where < 0 ? 0x7fffffff : where;   // (seen by no row)
       least = min(least, sm.pos[j]);
       most = max(most, sm.pos[j]);
@@ -576,8 +576,8 @@ __global__ void __launch_bounds__(256) attend_stored_sums_kernel(const AttendPar
 // equal runs, whatever the lengths of the lists; a warp's piece of a unit has the number warp + unit, which no
 // other has (from a piece to the next one, at least one of the two goes up).
 __device__ __forceinline__ int list_tiles(const AttendParams& p, int list) {
-  const int rows = p.rows != nullptr ? __ldg(p.rows + list / p.G) : p.T;
-  const int n = min(max(__ldg(p.len + list), 0), p.C);
+  const int rows = p.rows != nullptr ? p.rows[list / p.G] : p.T;
+  const int n = min(max(p.len[list], 0), p.C);
   return rows > 0 ? (n + kFewTile - 1) / kFewTile : 0;
 }
 
@@ -668,7 +668,7 @@ __global__ void __launch_bounds__(FewShape<D>::kThreads, 1) attend_few_kernel(co
   auto load = [&]() {
     if (to_load > 0) {
       const int b = ahead.list / p.G, g = ahead.list - b * p.G, hk = g * of + ahead.head;
-      const int n = min(__ldg(p.len + ahead.list), p.C), j0 = ahead.tile * kFewTile;
+      const int n = min(p.len[ahead.list], p.C), j0 = ahead.tile * kFewTile;
       const uint32_t base = mine + (loaded % S::kStages) * S::kStageBytes;
       const long long head = b * p.stride_b + hk * p.stride_h + j0 * p.stride_c + chunk * 8;
 #pragma unroll
@@ -715,8 +715,8 @@ __global__ void __launch_bounds__(FewShape<D>::kThreads, 1) attend_few_kernel(co
             p.q + (static_cast<long long>(b) * p.T + (live ? tok : 0)) * p.ldq + (hk * p.R + (live ? m % p.R : 0)) * D) + (lane & 3);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          q[k][u] = live ? __ldg(src + 8 * k) : 0u;
-          q[k][2 + u] = live ? __ldg(src + 8 * k + 4) : 0u;
+          q[k][u] = live ? src[8 * k] : 0u;
+          q[k][2 + u] = live ? src[8 * k + 4] : 0u;
         }
         ref[u] = -INFINITY;
         sum[u] = 0.f;

@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
   const int list = blockIdx.x / kCtas, rank = blockIdx.x % kCtas, b = list / p.G, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long base = static_cast<long long>(list) * p.C;
   const int n = min(max(__ldcg(p.len + list), 0), p.C), k = p.budget;
-  const int late = __ldg(p.seen + b) - p.recent;
+  const int late = p.seen[b] - p.recent;
   auto sync = [&]() {
     if (kCtas > 1)
       cluster_sync();

@@ -192,8 +192,8 @@ struct TileTokens {
     if (in) {
       b = static_cast<int>(__umul64hi(static_cast<unsigned long long>(t) * 2, p.per_row));   // t / L
       r = static_cast<int>(static_cast<unsigned>(t) - static_cast<unsigned>(b) * static_cast<unsigned>(p.L));
-      pos = append ? __ldg(p.seen + b) + r : p.pos != nullptr ? __ldg(p.pos + t) : r;
-      in = p.rows == nullptr || r < __ldg(p.rows + b);
+      pos = append ? p.seen[b] + r : p.pos != nullptr ? p.pos[t] : r;
+      in = p.rows == nullptr || r < p.rows[b];
     }
     used = __ballot_sync(0xffffffffu, in);
   }
@@ -310,13 +310,13 @@ __global__ void __launch_bounds__(kRotateThreads, kSmWarps / kRotateWarps) rotat
     if (append) {
       const int b_u = __shfl_sync(0xffffffffu, at.b, number), r_u = __shfl_sync(0xffffffffu, at.r, number);
       if (to_cache) {
-        const int c = min(max(__ldg(p.len + b_u * p.G + list), 0), p.C) + r_u;
+        const int c = min(max(p.len[b_u * p.G + list], 0), p.C) + r_u;
         to = dst + b_u * p.stride_b + c * p.stride_c;
         live = live && c < p.C;
         if (marks && live) {
           const long long slot = (static_cast<long long>(b_u) * p.G + list) * p.C + c;
           p.acc[slot] = 0.f;
-          p.slot_pos[slot] = __ldg(p.seen + b_u) + r_u;
+          p.slot_pos[slot] = p.seen[b_u] + r_u;
         }
       }
       if (s.side == 2) {
@@ -368,13 +368,13 @@ __global__ void __launch_bounds__(kRotateThreads, kSmWarps / kRotateWarps) rotat
   if (!last) return;
   for (int i = threadIdx.x; i < p.B * p.G; i += blockDim.x) {
     const int b = i / p.G;
-    const int come = p.rows != nullptr ? min(max(__ldg(p.rows + b), 0), p.L) : p.L;
+    const int come = p.rows != nullptr ? min(max(p.rows[b], 0), p.L) : p.L;
     const long long n = static_cast<long long>(cache_len(p, i)) + come;
     if (n > p.C) atomicOr(p.status, kStatusFull);
     p.len_out[i] = static_cast<int>(min(n, static_cast<long long>(p.C)));
   }
   for (int b = threadIdx.x; b < p.B; b += blockDim.x)
-    p.seen_out[b] = __ldg(p.seen + b) + (p.rows != nullptr ? min(max(__ldg(p.rows + b), 0), p.L) : p.L);
+    p.seen_out[b] = p.seen[b] + (p.rows != nullptr ? min(max(p.rows[b], 0), p.L) : p.L);
 }
 
 // Gradient.  dgamma: a lane adds up its features of its head over its tokens, the CTA its lanes and warps, in order;
