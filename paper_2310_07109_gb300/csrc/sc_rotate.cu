@@ -118,12 +118,6 @@ __device__ __forceinline__ float squares(const uint64_t (&a)[4], const uint64_t 
   return sum_lanes<W>(f2_total(f2_add(s, t)));
 }
 
-__device__ __forceinline__ void load4(const float* from, uint64_t (&v)[4]) {
-  const ulonglong2* f = reinterpret_cast<const ulonglong2*>(from);
-  const ulonglong2 x = f[0], y = f[1];
-  v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
-}
-
 // What a lane does for every token.
 struct LaneShare {
   int group, sub, q;   // its warp's group; head of the group and lane of the head
