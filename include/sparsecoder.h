@@ -813,6 +813,7 @@ size_t sc_cache_workspace_size(int B, int C, int H, int Hk, int G, int d, int T)
  * reports SC_ERR_CAPACITY.
  * Q, V_in, K_in   distances ldq, ldk, ldv as in sc_rotate_args; H may be 0 (no queries).
  * Q_out     may be Q.  len_out, seen_out may be len, seen.
+ * Positions have 32 bits: seen + rows stays below 2^31.
  */
 typedef struct {
   int B, C, H, Hk, G, d, dtype;
@@ -853,7 +854,8 @@ int sc_cache_append(const sc_cache_append_args* args, void* workspace, size_t wo
  * slots in use with 0 <= pos <= p.  Head h reads head h Hk / H of K and V:
  *   P_h[r] = softmax of scale q . k over the slots it sees;  O_h[r] = sum_c P_h[r][c] v_c
  *   acc_out[c] = decay acc[c] + sum_r mean_h P_h[r][c]     (c < len; h over the list's H / G heads)
- * A row that sees no slot has O = 0 and adds nothing.  Sequences without rows in use keep their acc.
+ * A row that sees no slot has O = 0 and adds nothing.  Sequences without rows in use keep their acc.  O of
+ * rows not in use, and acc_out of slots from len on, are not written.
  * Q, O      dtype: row b T + r has its H heads at ldq, ldo times its number; O does not overlap Q.
  * acc_out   fp32 [B][G][C], may be acc.
  * scale     finite; T at most SC_MAX_STEP.  Scores, weights and sums in fp32; the weights are

@@ -10,7 +10,7 @@ workspace and the stream are of the current device.
 Tokens are the rows of a [B][L] batch with ``rows[b]`` of them in use.  A cache is a dict of
 tensors (``new_cache``): K, V [B, Hk, C, d] of bfloat16 or float16 (any strides that are multiples of 8; d
 contiguous), acc fp32 and pos int32 [B, lists, C], len int32 [B, lists], seen int32 [B].  Its calls
-change it in place; ``out`` may name other tensors for what they replace.
+change it in place; ``out`` may name other tensors for what they replace, and for any of the new ones.
 """
 from __future__ import annotations
 
@@ -211,6 +211,14 @@ def _same(a, b, what):
         _refuse("%s: as many heads as of the input are wanted" % what)
 
 
+def _rest(out, wanted, device, stream):
+    """``out`` and a new tensor for each output that it does not name; wanted: name, shape, type."""
+    made = {n: torch.empty(shape, dtype=dt, device=device) for n, shape, dt in wanted if out is None or n not in out}
+    if made:
+        _made(stream, *made.values())
+    return {**(out or {}), **made} if made or out is None else out
+
+
 def rotate_forward(Q, K=None, *, width, B, L, rows=None, pos=None, freq=None, interleaved=False, mscale=1.0, gamma_q=None,
                    gamma_k=None, eps=1e-6, out=None, stream=None):
     """``sc_rotate_forward``: Q [B*L, Hq * width], K [B*L, Hk * width] (any row strides; one may be None),
@@ -223,9 +231,7 @@ def rotate_forward(Q, K=None, *, width, B, L, rows=None, pos=None, freq=None, in
         _refuse("width: at least 1 is wanted")
     q, Hq, ldq = _heads_at(Q, "Q", dt, B * L, width, dev)
     k, Hk, ldk = _heads_at(K, "K", dt, B * L, width, dev)
-    if out is None:
-        out = {n: torch.empty((B * L, h * width), dtype=dt, device=first.device) for n, h in (("Q", Hq), ("K", Hk)) if h}
-        _made(stream, *out.values())
+    out = _rest(out, [(n, (B * L, h * width), dt) for n, h in (("Q", Hq), ("K", Hk)) if h], first.device, stream)
     qo, hq, ldqo = _heads_at(out["Q"] if Hq else None, "out Q", dt, B * L, width, dev)
     ko, hk, ldko = _heads_at(out["K"] if Hk else None, "out K", dt, B * L, width, dev)
     _same(hq, Hq, "out Q")
@@ -256,12 +262,9 @@ def rotate_backward(dQ, dK=None, Q=None, K=None, *, width, B, L, rows=None, pos=
     k, hk, ldk = _heads_at(K if gamma_k is not None and Hk else None, "K", dt, B * L, width, dev)
     if (gamma_q is not None and hq != Hq) or (gamma_k is not None and hk != Hk):
         _refuse("Q, K: the forward call's inputs are wanted where there is a norm")
-    if out is None:
-        out = {n: torch.empty((B * L, h * width), dtype=dt, device=first.device) for n, h in (("dQ", Hq), ("dK", Hk)) if h}
-        for n, gamma in (("dgamma_q", gamma_q), ("dgamma_k", gamma_k)):
-            if gamma is not None:
-                out[n] = torch.empty(width, dtype=torch.float32, device=first.device)
-        _made(stream, *out.values())
+    wanted = [(n, (B * L, h * width), dt) for n, h in (("dQ", Hq), ("dK", Hk)) if h]
+    wanted += [(n, (width,), torch.float32) for n, gamma in (("dgamma_q", gamma_q), ("dgamma_k", gamma_k)) if gamma is not None]
+    out = _rest(out, wanted, first.device, stream)
     qg, hq, ldqg = _heads_at(out["dQ"] if Hq else None, "out dQ", dt, B * L, width, dev)
     kg, hk, ldkg = _heads_at(out["dK"] if Hk else None, "out dK", dt, B * L, width, dev)
     _same(hq, Hq, "out dQ")
@@ -301,7 +304,8 @@ def cache_append(cache, Q, K, V, *, L, rows=None, freq=None, interleaved=False, 
                  eps=1e-6, out=None, workspace=None, stream=None):
     """``sc_cache_append``: Q [B*L, H * d] (None: no queries), K and V [B*L, Hk * d] (any row strides) of
     up to L tokens a sequence.  Returns dict(Q, len, seen): the rotated queries, and len and seen moved on,
-    which are the cache's own unless ``out`` has others."""
+    which are the cache's own unless ``out`` has others.  ``workspace_status`` of the workspace reports a cache that was
+    full: without a workspace of the caller's nothing does."""
     dev = _device(K, "K")
     (B, Hk, C, G, d, dt), view = _cache_at(cache, dev)
     T = B * L
@@ -310,11 +314,8 @@ def cache_append(cache, Q, K, V, *, L, rows=None, freq=None, interleaved=False, 
     v, hv, ldv = _heads_at(V, "V", dt, T, d, dev)
     if hk != Hk or hv != Hk:
         _refuse("K, V: the cache's heads are wanted")
-    if out is None:
-        out = {}
-        if H:
-            out["Q"] = torch.empty((T, H * d), dtype=dt, device=K.device)
-            _made(stream, out["Q"])
+    if out is None or (H and "Q" not in out):
+        out = _rest(out, [("Q", (T, H * d), dt)] if H else [], K.device, stream)
     if "len" not in out or "seen" not in out:
         out = {"len": cache["len"], "seen": cache["seen"], **out}
     qo, ho, ldqo = _heads_at(out["Q"] if H else None, "out Q", dt, T, d, dev)
@@ -336,9 +337,8 @@ def cache_attend(cache, Q, *, T, rows=None, scale=None, decay=1.0, out=None, wor
     dev = _device(Q, "Q")
     (B, Hk, C, G, d, dt), view = _cache_at(cache, dev)
     q, H, ldq = _heads_at(Q, "Q", dt, B * T, d, dev)
-    if out is None:
-        out = {"O": torch.empty((B * T, H * d), dtype=dt, device=Q.device)}
-        _made(stream, out["O"])
+    if out is None or "O" not in out:
+        out = _rest(out, [("O", (B * T, H * d), dt)], Q.device, stream)
     if "acc" not in out:
         out = {"acc": cache["acc"], **out}
     o, ho, ldo = _heads_at(out["O"], "O", dt, B * T, d, dev)

@@ -133,3 +133,36 @@ def test_a_stream_of_another_device(what):
     stream.device_index = 0
     with pytest.raises(Reached):
         CALLS[what][0](tensors(), stream=stream)
+
+
+def test_outputs_that_are_not_named_are_made(monkeypatch):
+    """Any part of ``out`` may be left out; of what is there, nothing is replaced."""
+    monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: on(*([shape] if isinstance(shape, int) else shape), dtype=dtype))
+    for what in CALLS:
+        monkeypatch.setattr(getattr(ca, {"rotate": "_ROTATE", "back": "_ROTATE_BACK", "append": "_APPEND", "attend": "_ATTEND",
+                                         "evict": "_EVICT"}[what]), "call", lambda *_: 0)
+    t = tensors()
+    c = cache(t)
+    whole = {
+        "rotate": (lambda out: sc.rotate_forward(t.Q, t.K, width=d, B=B, L=L, out=out, **TURN(t)), dict(Q=t.Qo, K=t.Ko)),
+        "back": (lambda out: sc.rotate_backward(t.dQ, t.dK, t.Q, t.K, width=d, B=B, L=L, workspace=t.ws, out=out, **TURN(t)),
+                 dict(dQ=t.Qo, dK=t.Ko, dgamma_q=t.dgq, dgamma_k=t.dgk)),
+        "append": (lambda out: sc.cache_append(c, t.Q, t.K, t.V, L=L, workspace=t.ws, out=out), dict(Q=t.Qo, len=t.len2, seen=t.seen2)),
+        "attend": (lambda out: sc.cache_attend(c, t.Q, T=L, workspace=t.ws, out=out), dict(O=t.Qo, acc=t.acc2)),
+        "evict": (lambda out: sc.cache_evict(c, budget=8, workspace=t.ws, out=out), dict(acc=t.acc2, pos=t.pos2, len=t.len2)),
+    }
+    for what, (call, names) in whole.items():
+        for n in range(2 ** len(names)):
+            given = {name: v for i, (name, v) in enumerate(names.items()) if n >> i & 1}
+            before = dict(given)
+            got = call(given)
+            assert list(given) == list(before)
+            assert set(got) == set(names)
+            for name, v in names.items():
+                if name in given:
+                    assert got[name] is v, (what, name)
+                elif name in ("len", "seen", "acc", "pos"):
+                    assert got[name] is c[name], (what, name)
+                else:
+                    assert got[name] is not v and got[name].shape == v.shape and got[name].dtype == v.dtype, (what, name)
+        assert set(call(None)) == set(names)
