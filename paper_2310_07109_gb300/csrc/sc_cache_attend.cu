@@ -10,7 +10,7 @@
 //             pipeline of its own.  32 streams of 3000 to 8000 slots, 16 heads over 4 of 128: 63 to 67 us for
 //             390 MB (6 TB/s), the call 76; 252 as many rows below
 //   M <= 32   attend_rows_kernel<.., 2>: a CTA a part of a unit, two pairs of warps on either half of each 64-slot
-//             tile.  Four sequences of 12 heads of 64, 32 tokens, 4096 slots: the call 29 us, 50 as many rows below
+//             tile.  Four sequences of 12 heads of 64, 32 tokens, 4096 slots: the call 27 us, 50 as many rows below
 //     both keep the scores t, 4 bytes a row and slot, and attend_stored_join_kernel joins the parts of the units
 //     (LSE = reference + log2(sum) of all, O scaled and rounded) and adds 2^(t - LSE) up over the list's rows and heads
 //     in a fixed order (the 32 tokens: 37 us where K is read again for the sums)
