@@ -546,3 +546,42 @@ def test_two_calls_give_the_same_bits():
         Q = randn(g, 2 * T, 8 * 64).to(BF)
         a, b = (sc.cache_attend(copy(cache), Q, T=T) for _ in range(2))
         assert torch.equal(a["O"], b["O"]) and same(a["acc"], b["acc"])
+
+
+def test_two_graphs_share_a_workspace():
+    """Steps of two caches in a graph each, with one workspace, replayed in turn: bit for bit the eager steps with a
+    workspace each."""
+    g = gen(46)
+    shapes = [(2, 4, 300, 64, 4, 8, 1, BF), (1, 2, 2100, 128, 1, 8, 6, HF)]   # B, Hk, C, d, G, H, T, type
+    ws = torch.zeros(256 + max(sc.cache_workspace_size(B, C, H, Hk, lists=G, width=d, T=T) for B, Hk, C, d, G, H, T, _ in shapes),
+                     dtype=torch.uint8, device="cuda")
+    ws = ws[-ws.data_ptr() % 256:]
+    sides = []
+    for B, Hk, C, d, G, H, T, dt in shapes:
+        cache = make_cache(g, B, Hk, C, d, G, [C - 2 * T] * B, dt)
+        cache = {n: t.clone() for n, t in cache.items()}
+        ins = [randn(g, B * T, h * d).to(dt) for h in (H, Hk, Hk)]
+        freq, budget = sc.rotary_frequencies(d)[0], C - 2 * T - 20
+
+        def step(c, w, ins=ins, T=T, freq=freq, budget=budget):
+            q = sc.cache_append(c, *ins, L=T, freq=freq, workspace=w)["Q"]
+            O = sc.cache_attend(c, q, T=T, decay=0.9, workspace=w)["O"]  # noqa: E741
+            sc.cache_evict(c, budget=budget, slack=15, sinks=1, recent=4, workspace=w)
+            return O
+
+        mine = {n: t.clone() for n, t in cache.items()}
+        captured = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(captured):
+            O = step(mine, ws)  # noqa: E741
+        own = sc.new_cache_workspace(B, C, H, Hk, lists=G, width=d, T=T)
+        sides.append((cache, mine, ins, captured, O, step, own))
+    for i in range(12):
+        for cache, mine, ins, captured, O, step, own in sides:
+            for t in ins:
+                t.copy_(randn(g, *t.shape).to(t.dtype))
+            captured.replay()
+            want = step(cache, own)
+            assert torch.equal(O, want), i
+            for n in cache:
+                assert same(mine[n], cache[n]), (i, n)
+    assert sc.workspace_status(ws) == sc.SC_OK
