@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
     }
     __syncthreads();
     low += static_cast<uint32_t>(sm.found[0]) << shift;
-    high = min(high, low + ((1u << shift) - 1u));
+    high = low + min(high - low, (1u << shift) - 1u);   // (the part's own end may lie beyond 2^32)
     want = sm.found[1];
     count = sm.found[2];
   }
@@ -321,15 +321,18 @@ __global__ void __launch_bounds__(kPickThreads, 1) evict_pick_kernel(const Evict
     my_fill += static_cast<int>(all >> 16);
   }
   __syncthreads();
+  // As many are free as fill them, min(k, n - k) at most, which a plan has room for; none goes beyond it all the same.
+  const int plan = static_cast<int>(p.pair_pitch);
   if (kCtas == 1) {
+    my_free = min(my_free, plan);
     for (int i = tid; i < my_free; i += kPickThreads) pairs[i] = make_int2(held[i], held[room - 1 - i]);
   } else {
-    for (int i = tid; i < my_free; i += kPickThreads) pairs[free_at + i].x = held[i];
-    for (int i = tid; i < my_fill; i += kPickThreads) pairs[fill_at + i].y = held[room - 1 - i];
+    for (int i = tid; i < min(my_free, plan - free_at); i += kPickThreads) pairs[free_at + i].x = held[i];
+    for (int i = tid; i < min(my_fill, plan - fill_at); i += kPickThreads) pairs[fill_at + i].y = held[room - 1 - i];
   }
   if (kCtas > 1) cluster_sync();   // (all have read all; len too)
   if (tid == 0 && rank == 0) {
-    p.moved[list] = kCtas > 1 ? all_free : my_free;
+    p.moved[list] = kCtas > 1 ? min(all_free, plan) : my_free;
     p.len_out[list] = k;
   }
 }
