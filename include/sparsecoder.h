@@ -858,9 +858,9 @@ int sc_cache_append(const sc_cache_append_args* args, void* workspace, size_t wo
  * rows not in use, and acc_out of slots from len on, are not written.
  * Q, O      dtype: row b T + r has its H heads at ldq, ldo times its number; O does not overlap Q.
  * acc_out   fp32 [B][G][C], may be acc.
- * scale     finite; T at most SC_MAX_STEP.  Scores, weights and sums in fp32; the weights are
- *           rounded to dtype for their product with V.  Two calls with the same
- *           arguments give the same bits.
+ * scale     finite; T at most SC_MAX_STEP.  Scores, weights and sums in fp32; the product with V
+ *           takes each weight to 2^-15 of itself (bf16; 2^-20 of fp16), and O is rounded
+ *           once.  Two calls with the same arguments give the same bits.
  */
 typedef struct {
   int B, C, H, Hk, G, d, dtype;

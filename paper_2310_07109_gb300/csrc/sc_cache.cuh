@@ -33,6 +33,12 @@ struct Bf16 {
   }
   // The weights' reference lies this far (a power of two) below the largest score.
   static constexpr float kHeadroom = 0.f;
+  // A pair of weights x, y >= 0 as sums of two values each, the second positive wherever the first is.
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& first, uint32_t& second) {
+    const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+    first = __byte_perm(a, b, 0x7632);   // (cut off, not rounded)
+    second = pack(fmaf(x, 1.f + 0x1p-20f, -__uint_as_float(a & 0xffff0000u)), fmaf(y, 1.f + 0x1p-20f, -__uint_as_float(b & 0xffff0000u)));
+  }
 };
 
 struct Fp16 {
@@ -55,7 +61,17 @@ struct Fp16 {
   // A weight of 2^-24 is fp16's smallest: up to 2^12 instead of 1, so that the many small
   // weights of a long list keep eleven bits down to 2^-26 of the largest.
   static constexpr float kHeadroom = 12.f;
+  static __device__ __forceinline__ void split(float x, float y, uint32_t& first, uint32_t& second) {
+    first = pack((1.f - 0x1p-10f) * x, (1.f - 0x1p-10f) * y);
+    float a, b;
+    unpack(first, a, b);
+    second = pack(x - a, y - b);
+  }
 };
+
+// The softmax's weights meet V as two 16-bit values each, one product after the other: one value's half step (2^-8 of
+// a bf16 weight) is about what the one rounding of O may change, the sum's (2^-15; fp16: 2^-20) is not seen.  The second value is
+// never 0 where the first is not, so that infinities in V stay what they are.
 
 // One side of a rotation: heads of all tokens, `ld` elements a token.
 struct HeadsIn {

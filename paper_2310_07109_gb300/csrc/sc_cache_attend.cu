@@ -5,7 +5,9 @@
 // A key head of a sequence (a unit) has M = T R rows, R query heads to a key head.  Bound by the bytes of K and V (each read
 // once at M <= 32) as long as there are few rows.  Products are warp-level ones (16 rows at least, which a token of
 // grouped heads does not fill; they take 17 % of the tensor pipe), with S, P and O in registers; softmax with the
-// running reference (the largest t so far) and sum of each row; P rounded to the 16-bit type where it meets V.
+// running reference (the largest t so far) and sum of each row; P meets V as two 16-bit values, one product each (as one value:
+// attend_batch 76 us and 76.5 with two, attend_window 27 and 28.5, prompts an eighth less; O was then off by 1.9e-3 of 64
+// bits, with two by the 1.7e-3 of its one rounding).
 //   M <= 16   attend_few_kernel: the 16-slot tiles of all units dealt out to warps in equal runs, each warp with a
 //             pipeline of its own.  32 streams of 3000 to 8000 slots, 16 heads over 4 of 128: 63 to 67 us for
 //             390 MB (6 TB/s), the call 76; 252 as many rows below
@@ -57,6 +59,22 @@ __device__ __forceinline__ void load_b(uint32_t base, int key0, int k, int lane,
 template <int D>
 __device__ __forceinline__ void load_v(uint32_t base, int key0, int n, int lane, uint32_t (&b)[4]) {
   ldmatrix4_trans(chunk_at<D>(base, key0 + (lane & 15), 2 * n + (lane >> 4)), b);
+}
+
+// O += (first + second) V of 16 keys, four fragments of O at a time.
+template <class T, int D>
+__device__ __forceinline__ void add_values(float (&o)[D / 8][4], const uint32_t (&first)[4], const uint32_t (&second)[4], uint32_t base,
+                                           int key0, int lane) {
+#pragma unroll
+  for (int n = 0; n < D / 16; n += 2) {
+    uint32_t f[2][4];
+    load_v<D>(base, key0, n, lane, f[0]);
+    load_v<D>(base, key0, n + 1, lane, f[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) T::mma(o[2 * n + i], first, f[i / 2][i % 2 * 2], f[i / 2][i % 2 * 2 + 1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) T::mma(o[2 * n + i], second, f[i / 2][i % 2 * 2], f[i / 2][i % 2 * 2 + 1]);
+  }
 }
 
 struct ListOf {
@@ -263,15 +281,10 @@ __global__ void __launch_bounds__(kAttendThreads) attend_rows_kernel(const Atten
     }
 #pragma unroll
     for (int k = 0; k < kKeys / 16; ++k) {
-      const uint32_t a[4] = {T::pack(c[2 * k][0], c[2 * k][1]), T::pack(c[2 * k][2], c[2 * k][3]),
-                             T::pack(c[2 * k + 1][0], c[2 * k + 1][1]), T::pack(c[2 * k + 1][2], c[2 * k + 1][3])};
+      uint32_t a[4], rest[4];
 #pragma unroll
-      for (int n = 0; n < D / 16; ++n) {
-        uint32_t f[4];
-        load_v<D>(sv, key0 + k * 16, n, lane, f);
-        T::mma(o[2 * n], a, f[0], f[1]);
-        T::mma(o[2 * n + 1], a, f[2], f[3]);
-      }
+      for (int i = 0; i < 4; ++i) T::split(c[2 * k + i / 2][i % 2 * 2], c[2 * k + i / 2][i % 2 * 2 + 1], a[i], rest[i]);
+      add_values<T, D>(o, a, rest, sv, key0 + k * 16, lane);
     }
   }
 #pragma unroll
@@ -799,14 +812,10 @@ __global__ void __launch_bounds__(FewShape<D>::kThreads, 1) attend_few_kernel(co
       sum[0] += c[i][0] + c[i][1];
       sum[1] += c[i][2] + c[i][3];
     }
-    const uint32_t a[4] = {T::pack(c[0][0], c[0][1]), T::pack(c[0][2], c[0][3]), T::pack(c[1][0], c[1][1]), T::pack(c[1][2], c[1][3])};
+    uint32_t a[4], rest[4];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-      uint32_t f[4];
-      load_v<D>(sv, 0, i, lane, f);
-      T::mma(o[2 * i], a, f[0], f[1]);
-      T::mma(o[2 * i + 1], a, f[2], f[3]);
-    }
+    for (int i = 0; i < 4; ++i) T::split(c[i / 2][i % 2 * 2], c[i / 2][i % 2 * 2 + 1], a[i], rest[i]);
+    add_values<T, D>(o, a, rest, sv, 0, lane);
     __syncwarp();   // the stage is free
     const int was_list = at.list, was_head = at.head;
     advance(p, of, at);
