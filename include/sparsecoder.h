@@ -800,7 +800,8 @@ int sc_rotate_backward(const sc_rotate_backward_args* args, void* workspace,
 #define SC_MAX_CACHE 262144
 #define SC_MAX_STEP 4096 /* most tokens a sequence of one sc_cache_attend */
 
-/* T: most tokens a sequence that one sc_cache_attend brings.  0 on invalid sizes. */
+/* T: most tokens a sequence that one sc_cache_attend brings (calls of fewer need no more than
+ * this).  0 on invalid sizes. */
 size_t sc_cache_workspace_size(int B, int C, int H, int Hk, int G, int d, int T);
 
 /*

@@ -100,6 +100,22 @@ CacheLayout cache_layout(int B, int C, int H, int Hk, int G, int d, int T) {
   return w;
 }
 
+// The most that a call of 1 to T tokens a sequence needs.  Its bytes grow with the tokens but where few rows become more, scores are no
+// longer kept, or one more tile of rows leaves a list fewer parts: the last sizes before these, and T itself.
+size_t most_bytes(int B, int C, int H, int Hk, int G, int d, int T) {
+  const long long R = H / Hk, M = T * R, units = static_cast<long long>(B) * Hk, pitch = (C + 3) & ~3;
+  size_t most = 0;
+  const auto up_to = [&](long long rows) {   // the most tokens of no more than these rows
+    if (rows >= R) most = std::max(most, cache_layout(B, C, H, Hk, G, d, static_cast<int>(std::min(rows, M) / R)).total);
+  };
+  up_to(kFewRows);
+  up_to(kJoinedRows);
+  up_to(static_cast<long long>(kStoredBytes) / (static_cast<long long>(sizeof(float)) * units * pitch));
+  for (long long rows = kRowsTile; rows < M && splits_of(B, C, Hk, static_cast<int>(rows), d) > 1; rows += kRowsTile) up_to(rows);
+  up_to(M);
+  return most;
+}
+
 // SC_OK for sizes of a cache that the calls take (H: 0 where there are no queries).
 int check_cache_sizes(int B, int C, int H, int Hk, int G, int d) {
   if (B < 1 || C < 1 || H < 0 || Hk < 1 || G < 1 || Hk % G || H % Hk || d < 16 || d % 16) return SC_ERR_INVALID_ARG;
@@ -194,7 +210,7 @@ extern "C" int sc_rotate_backward(const sc_rotate_backward_args* a, void* worksp
 extern "C" size_t sc_cache_workspace_size(int B, int C, int H, int Hk, int G, int d, int T) {
   if (check_cache_sizes(B, C, H, Hk, G, d) != SC_OK) return 0;
   if (T < 1 || (d == 64 || d == 128 ? check_attend_sizes(B, std::max(H, Hk), Hk, d, T) != SC_OK : T > 1)) return 0;
-  return cache_layout(B, C, std::max(H, Hk), Hk, G, d, T).total;
+  return most_bytes(B, C, std::max(H, Hk), Hk, G, d, T);
 }
 
 extern "C" int sc_cache_append(const sc_cache_append_args* a, void* workspace, size_t ws_bytes, void* stream) {
