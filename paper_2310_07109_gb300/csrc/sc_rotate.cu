@@ -304,9 +304,10 @@ __global__ void __launch_bounds__(kRotateThreads, kSmWarps / kRotateWarps) rotat
     if (append) {
       const int b_u = __shfl_sync(0xffffffffu, at.b, number), r_u = __shfl_sync(0xffffffffu, at.r, number);
       if (to_cache) {
-        const int c = min(max(p.len[b_u * p.G + list], 0), p.C) + r_u;
+        const int held = min(max(p.len[b_u * p.G + list], 0), p.C), room = p.C - held;
+        const int c = held + min(r_u, room);   // (held + r_u may pass 2^31)
         to = dst + b_u * p.stride_b + c * p.stride_c;
-        live = live && c < p.C;
+        live = live && r_u < room;
         if (marks && live) {
           const long long slot = (static_cast<long long>(b_u) * p.G + list) * p.C + c;
           p.acc[slot] = 0.f;
