@@ -358,7 +358,7 @@ def cache_evict(cache, *, budget, slack=0, sinks=0, recent=0, out=None, workspac
     K = cache["K"]
     dev = _device(K, "K")
     (B, Hk, C, G, d, dt), view = _cache_at(cache, dev)
-    if out is None or len(out) < 3:
+    if out is None or "acc" not in out or "pos" not in out or "len" not in out:
         out = {"acc": cache["acc"], "pos": cache["pos"], "len": cache["len"], **(out or {})}
     i32 = torch.int32
     a = _EVICT.pack(B, C, Hk, G, *view, budget, slack, sinks, recent, _at(out["acc"], "out acc", torch.float32, B * G * C, dev),
