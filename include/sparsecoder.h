@@ -813,7 +813,7 @@ size_t sc_cache_workspace_size(int B, int C, int H, int Hk, int G, int d, int T)
  * Tokens beyond slot C - 1 are not stored (len_out stops at C), and sc_workspace_status
  * reports SC_ERR_CAPACITY.
  * Q, V_in, K_in   distances ldq, ldk, ldv as in sc_rotate_args; H may be 0 (no queries).
- * Q_out     may be Q.  len_out, seen_out may be len, seen.
+ * Q_out     may be Q (with its distance).  len_out, seen_out may be len, seen.
  * Positions have 32 bits: seen + rows stays below 2^31.
  */
 typedef struct {

@@ -36,6 +36,11 @@ bool good_heads(const void* p, long long ld, int heads, int d) {
   return p && aligned(p, 16) && ld >= static_cast<long long>(heads) * d && ld % 8 == 0 && ld < (1ll << 30);
 }
 
+// Whether outputs lie apart from the inputs or, in their place, with their distances (one token has none).
+bool good_place(const void* in, long long ld_in, const void* out, long long ld_out, int B, int L) {
+  return in != out || ld_in == ld_out || static_cast<long long>(B) * L == 1;
+}
+
 int check_rotate(int B, int L, int Hq, int Hk, int d, int dtype, const int32_t* rows, const float* gamma_q,
                  const float* gamma_k, float eps, int rot, const double* freq, float mscale) {
   if (B < 1 || L < 1 || Hq < 0 || Hk < 0 || Hq + static_cast<long long>(Hk) < 1 || d < 16 || d % 16 || !good_dtype(dtype) ||
@@ -155,7 +160,9 @@ extern "C" int sc_rotate_forward(const sc_rotate_args* a, void* stream) {
                         a->freq, a->mscale);
   if (rc != SC_OK) return rc;
   if (!words(a->pos) || (a->Hq > 0 && (!good_heads(a->Q, a->ldq, a->Hq, a->d) || !good_heads(a->Q_out, a->ldq_out, a->Hq, a->d))) ||
-      (a->Hk > 0 && (!good_heads(a->K, a->ldk, a->Hk, a->d) || !good_heads(a->K_out, a->ldk_out, a->Hk, a->d))))
+      (a->Hk > 0 && (!good_heads(a->K, a->ldk, a->Hk, a->d) || !good_heads(a->K_out, a->ldk_out, a->Hk, a->d))) ||
+      (a->Hq > 0 && !good_place(a->Q, a->ldq, a->Q_out, a->ldq_out, a->B, a->L)) ||
+      (a->Hk > 0 && !good_place(a->K, a->ldk, a->K_out, a->ldk_out, a->B, a->L)))
     return SC_ERR_INVALID_ARG;
   if ((rc = api_ensure_configured()) != SC_OK) return rc;
   RotateParams p{};
@@ -183,7 +190,9 @@ extern "C" int sc_rotate_backward(const sc_rotate_backward_args* a, void* worksp
       (a->Hq > 0 && (!good_heads(a->dQ_out, a->ldq_out, a->Hq, a->d) || !good_heads(a->dQ, a->ldq_grad, a->Hq, a->d) ||
                      (a->gamma_q && !good_heads(a->Q, a->ldq, a->Hq, a->d)))) ||
       (a->Hk > 0 && (!good_heads(a->dK_out, a->ldk_out, a->Hk, a->d) || !good_heads(a->dK, a->ldk_grad, a->Hk, a->d) ||
-                     (a->gamma_k && !good_heads(a->K, a->ldk, a->Hk, a->d)))))
+                     (a->gamma_k && !good_heads(a->K, a->ldk, a->Hk, a->d)))) ||
+      (a->Hq > 0 && !good_place(a->dQ_out, a->ldq_out, a->dQ, a->ldq_grad, a->B, a->L)) ||
+      (a->Hk > 0 && !good_place(a->dK_out, a->ldk_out, a->dK, a->ldk_grad, a->B, a->L)))
     return SC_ERR_INVALID_ARG;
   if ((rc = check_workspace(workspace, ws_bytes, sc_rotate_workspace_size(a->d))) != SC_OK) return rc;
   if ((rc = api_ensure_configured()) != SC_OK) return rc;
@@ -220,7 +229,8 @@ extern "C" int sc_cache_append(const sc_cache_append_args* a, void* workspace, s
   if (rc == SC_OK)
     rc = check_rotate(a->B, a->L, a->H, a->Hk, a->d, a->dtype, a->rows, a->gamma_q, a->gamma_k, a->eps, a->rot, a->freq, a->mscale);
   if (rc != SC_OK) return rc;
-  if ((a->H > 0 && (!good_heads(a->Q, a->ldq, a->H, a->d) || !good_heads(a->Q_out, a->ldq_out, a->H, a->d))) ||
+  if ((a->H > 0 && (!good_heads(a->Q, a->ldq, a->H, a->d) || !good_heads(a->Q_out, a->ldq_out, a->H, a->d) ||
+                    !good_place(a->Q, a->ldq, a->Q_out, a->ldq_out, a->B, a->L))) ||
       !good_heads(a->K_in, a->ldk, a->Hk, a->d) || !good_heads(a->V_in, a->ldv, a->Hk, a->d) || !a->len_out ||
       !a->seen_out || !words(a->len_out, a->seen_out))
     return SC_ERR_INVALID_ARG;
