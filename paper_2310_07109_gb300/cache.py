@@ -195,7 +195,7 @@ def _heads_at(t, name, dtype, T, d, dev):
     if len(shape) == 2 and t.dtype is dtype and t.get_device() == dev and shape[0] == T and shape[1] % d == 0:
         ld, step = t.stride()
         if step == 1 or shape[1] == 1:
-            return t.data_ptr(), shape[1] // d, ld if T > 1 else max(ld, shape[1])
+            return t.data_ptr(), shape[1] // d, ld if T > 1 else shape[1]
     _refuse("%s: %d rows of heads of %d features, of %s on cuda:%d and contiguous, are wanted" % (name, T, d, dtype, dev))
 
 
@@ -221,7 +221,7 @@ def _rest(out, wanted, device, stream):
 
 def rotate_forward(Q, K=None, *, width, B, L, rows=None, pos=None, freq=None, interleaved=False, mscale=1.0, gamma_q=None,
                    gamma_k=None, eps=1e-6, out=None, stream=None):
-    """``sc_rotate_forward``: Q [B*L, Hq * width], K [B*L, Hk * width] (any row strides; one may be None),
+    """``sc_rotate_forward``: Q [B*L, Hq * width], K [B*L, Hk * width] (row strides multiples of 8; one may be None),
     pos int32 [B, L] (None: the row), freq float64 [rot / 2] (None: no rotation).  Returns dict(Q, K) of what was given."""
     first = Q if Q is not None else K
     if first is None:
@@ -302,7 +302,7 @@ def _cache_at(cache, dev):
 
 def cache_append(cache, Q, K, V, *, L, rows=None, freq=None, interleaved=False, mscale=1.0, gamma_q=None, gamma_k=None,
                  eps=1e-6, out=None, workspace=None, stream=None):
-    """``sc_cache_append``: Q [B*L, H * d] (None: no queries), K and V [B*L, Hk * d] (any row strides) of
+    """``sc_cache_append``: Q [B*L, H * d] (None: no queries), K and V [B*L, Hk * d] (row strides multiples of 8) of
     up to L tokens a sequence.  Returns dict(Q, len, seen): the rotated queries, and len and seen moved on,
     which are the cache's own unless ``out`` has others.  ``workspace_status`` of the workspace reports a cache that was
     full: without a workspace of the caller's nothing does."""
@@ -331,7 +331,7 @@ def cache_append(cache, Q, K, V, *, L, rows=None, freq=None, interleaved=False, 
 
 
 def cache_attend(cache, Q, *, T, rows=None, scale=None, decay=1.0, out=None, workspace=None, stream=None):
-    """``sc_cache_attend``: Q [B*T, H * d] (any row stride), the rotated queries of the tokens that
+    """``sc_cache_attend``: Q [B*T, H * d] (a row stride that is a multiple of 8), the rotated queries of the tokens that
     ``cache_append`` just brought; scale: 1 / sqrt(d) where None.  Returns dict(O [B*T, H * d], acc), acc being the
     cache's own unless ``out`` has another."""
     dev = _device(Q, "Q")
