@@ -29,7 +29,10 @@ constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kMoveThreads = 256;
 constexpr int kMoveSlots = 1024;   // whose acc and pos a CTA moves
 constexpr uint32_t kProtected = 0xffffffffu;
-constexpr int kPickSlots = 8192;     // of a CTA, where there are SMs for more CTAs
+// Slots of a CTA where there are SMs for more CTAs: eight lists of 12000 take 14.8 us with two CTAs each and 14.3 with one, of 16384
+// 16.2 and 16.7, of 20000 17.4 with four and 20.2 with two.  An SM holds one of these CTAs: 128 lists of 8224 take 51 us with
+// two CTAs each (two waves), 40 with one.
+constexpr int kPickSlots = 8192;
 constexpr int kMostSlots = SC_MAX_CACHE / 8;
 constexpr int kParts = 256;
 
@@ -442,10 +445,10 @@ cudaError_t launch_pick(const EvictParams& p, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t st) {
-  // CTAs of a list: as many as its slots need, and more while there are SMs for them
+  // CTAs of a list: as many as its slots need, and twice as many while there are SMs for these
   int n = 1;
   while (n < 8 && ((p.C + n - 1) / n > kMostSlots ||
-                   ((p.C + n - 1) / n > kPickSlots && static_cast<long long>(p.B) * p.G * n < kCacheSms)))
+                   ((p.C + n - 1) / n > kPickSlots && static_cast<long long>(p.B) * p.G * n * 2 <= kCacheSms)))
     n *= 2;
   cudaError_t e = n == 1 ? launch_pick<1>(p, st) : n == 2 ? launch_pick<2>(p, st) : n == 4 ? launch_pick<4>(p, st) : launch_pick<8>(p, st);
   const bool evicts = p.budget < p.C, apart = p.acc_out != p.acc || p.pos_out != p.pos;
