@@ -157,7 +157,11 @@ struct AttendParams {
 constexpr int kFewRows = 16;                 // most rows a key head that the kernel for few rows takes
 // Slots of a CTA that computes scores again: four tiles of 64, or two of wider heads.
 constexpr int sum_tiles(int d) { return d == 64 ? 4 : 2; }
-constexpr int kJoinedRows = 32;              // most rows that one launch joins and adds the weights of
+// Most rows that one launch joins and adds the weights of, from scores that are kept whatever they take (4 bytes a row and slot, in the
+// workspace too: for 32 rows half of the bytes of K and V of 64 features).  32 rows, 65536 slots: 8 x 8 heads of 64 434 us, and
+// 548 by the launches for more rows, which compute them again; 2 x 8 of 64 162 and 155; 2 x 8 of 128 203 and 301.  (16384
+// slots, 2 x 8 heads of 64: 67 and 44, as few units make many parts, whose rows' LSE every CTA of sums finds for itself.)
+constexpr int kJoinedRows = 32;
 constexpr size_t kStoredBytes = 32u << 20;   // most bytes of the scores of more rows, else they are computed again
 constexpr int kFewTile = 16;                 // slots a warp takes at a time
 constexpr int kFewMinTiles = 2;              // fewest tiles of a warp

@@ -4,21 +4,21 @@
 //   t = scale log2(e) q . k;   P = 2^(t - LSE);   O = P V;   acc = decay acc + sum over rows, mean over heads of P
 // A key head of a sequence (a unit) has M = T R rows, R query heads to a key head.  Bound by the bytes of K and V (each read
 // once at M <= 32) as long as there are few rows.  Products are warp-level ones (16 rows at least, which a token of
-// grouped heads does not fill; they take 17 % of the tensor pipe), with S, P and O in registers; softmax with the
+// grouped heads does not fill; they take 25 % of the tensor pipe), with S, P and O in registers; softmax with the
 // running reference (the largest t so far) and sum of each row; P meets V as two 16-bit values, one product each (as one value:
 // attend_batch 76 us and 76.5 with two, attend_window 27 and 28.5, prompts an eighth less; O was then off by 1.9e-3 of 64
 // bits, with two by the 1.7e-3 of its one rounding).
 //   M <= 16   attend_few_kernel: the 16-slot tiles of all units dealt out to warps in equal runs, each warp with a
-//             pipeline of its own.  32 streams of 3000 to 8000 slots, 16 heads over 4 of 128: 63 to 67 us for
-//             390 MB (6 TB/s), the call 76; 252 as many rows below
+//             pipeline of its own.  32 streams of 3000 to 8000 slots, 16 heads over 4 of 128: the call 76.5 us
+//             for 390 MB, this kernel on its own with cold caches 71 (5.5 TB/s); 252 as many rows below
 //   M <= 32   attend_rows_kernel<.., 2>: a CTA a part of a unit, two pairs of warps on either half of each 64-slot
-//             tile.  Four sequences of 12 heads of 64, 32 tokens, 4096 slots: the call 27 us, 50 as many rows below
+//             tile.  Four sequences of 12 heads of 64, 32 tokens, 4096 slots: the call 28.5 us, 50 as many rows below
 //     both keep the scores t, 4 bytes a row and slot, and attend_stored_join_kernel joins the parts of the units
 //     (LSE = reference + log2(sum) of all, O scaled and rounded) and adds 2^(t - LSE) up over the list's rows and heads
-//     in a fixed order (the 32 tokens: 37 us where K is read again for the sums)
+//     in a fixed order (the 32 tokens: 30 us when first built so, 37 where K is read again for the sums)
 //   M > 32    attend_rows_kernel<.., 1>, attend_join_kernel, and the sums from scores kept (attend_stored_sums_kernel,
 //             up to kStoredBytes) or computed again (attend_sums_kernel, attend_heads_kernel).  A prompt of 4096
-//             tokens, 16 heads over 4 of 128: 836 us (164 TFLOP/s of 4 T n d H)
+//             tokens, 16 heads over 4 of 128: 946 us (145 TFLOP/s of 4 T n d H)
 #include <algorithm>
 #include <cuda_runtime.h>
 #include <cstdint>

@@ -11,10 +11,11 @@
 //          bits in an order-preserving form) go into shared memory; the cut is found in passes over them, each of
 //          which cuts the range that holds it into at most 256 equal parts (by bits of the difference to its lower end:
 //          keys are logarithms nearly, so weights spread over the parts; digits of the keys themselves put most of
-//          them into two or three, whose additions wait for one another: 13000 cycles a pass instead of 2300).
-//          Then a bit a slot, and ranks of ties, free places and their fillers from prefix sums over the bits, put
-//          together in shared memory (stores of single words to the plan took 4600 cycles of a list of 8000 slots)
-//   move   the rows of K and V, bound by memory (32 x 4 lists of 8000 slots, 128 features: 40 us, 6.7 TB/s), and acc and pos
+//          them into two or three, whose additions wait for one another).  Then a bit a slot, and ranks of ties, free places and
+//          their fillers from prefix sums over the bits, put together in shared memory.  128 lists of 7400 to 8192 slots, a CTA
+//          each: 13 us with cold caches (the first version, with digits: 29)
+//   move   the rows of K and V, bound by memory, and acc and pos.  Half of the same lists' slots go, 128 features: 45 us with
+//          cold caches, 220 MB of DRAM traffic (4.9 TB/s); the call 55.6
 #include <algorithm>
 #include <cuda_runtime.h>
 #include <cstdint>
