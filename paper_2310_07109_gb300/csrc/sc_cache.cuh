@@ -33,7 +33,7 @@ struct Bf16 {
   }
   // The weights' reference lies this far (a power of two) below the largest score.
   static constexpr float kHeadroom = 0.f;
-  // A pair of weights x, y >= 0 as sums of two values each, the second positive wherever the first is.
+  // A pair of weights x, y >= 0 as sums of two values each.
   static __device__ __forceinline__ void split(float x, float y, uint32_t& first, uint32_t& second) {
     const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
     first = __byte_perm(a, b, 0x7632);   // (cut off, not rounded)
@@ -71,7 +71,8 @@ struct Fp16 {
 
 // The softmax's weights meet V as two 16-bit values each, one product after the other: one value's half step (2^-8 of
 // a bf16 weight) is about what the one rounding of O may change, the sum's (2^-15; fp16: 2^-20) is not seen.  The second value is
-// never 0 where the first is not, so that infinities in V stay what they are.
+// positive where the first is, so that infinities in V stay what they are (but for weights whose second value the type cannot
+// hold: of fp16 those below 2^-26 of the largest, whose product with an infinity may be a NaN).
 
 // One side of a rotation: heads of all tokens, `ld` elements a token.
 struct HeadsIn {
